@@ -220,6 +220,7 @@ def prepare(case, seed):
         s["new_refs"] = torch.empty_like(s["refs"])
         if case["op"] == "fork":
             s["parents"] = _ints(plan["parents"])
+            s["more"] = torch.full((case["children"],), case["rows"], dtype=torch.int32, device="cuda")     # rows to come, for each branch
             s["new_table"] = torch.empty(case["children"], width, dtype=torch.int32, device="cuda")
             s["new_lens"] = torch.empty(case["children"], dtype=torch.int32, device="cuda")
         else:
@@ -330,7 +331,7 @@ def _fork(s):
     if own:
         s["ctx"].tts_kv_fork(s["pools"], s["table"], s["prefix"], s["lens"], s["n"], s["parents"], s["parents"].numel(), s["refs"],
                              s["new_table"], s["new_lens"], s["new_refs"])
-        s["ctx"].tts_kv_grow(s["new_table"], s["prefix"], s["new_lens"], s["case"]["rows"], s["parents"].numel(), s["new_refs"])
+        s["ctx"].tts_kv_grow(s["new_table"], s["prefix"], s["new_lens"], s["more"], s["parents"].numel(), s["new_refs"])
     else:
         parent = s["parents"].long()
         first = (parent[:, None] == parent[None, :]).int().argmax(1) == torch.arange(parent.numel(), device="cuda")
@@ -346,7 +347,7 @@ def _fork(s):
         s["v"][:, page[partial]] = s["v"][:, source[partial]]
         refs = s["refs"] - _count(s["table"], s["refs"]) + _count(new, s["refs"])
         # room for the next rows
-        after = tokens + s["case"]["rows"]
+        after = tokens + s["more"]
         wanted = (new < 0) & (column < ((after + PAGE - 1) // PAGE)[:, None])
         new = torch.where(wanted, _lowest_free(refs, wanted), new)
         s["new_table"].copy_(new)
