@@ -46,7 +46,8 @@ typedef enum {
     TTS_ERR_CUDA = -3,           /* a CUDA call failed; tts_last_cuda_error() has the code */
     TTS_ERR_DEVICE_BOUNDS = -4,  /* (via tts_last_status) a kernel saw a page id / token out of range */
     TTS_ERR_DEVICE_TIMEOUT = -5, /* (via tts_last_status) a bounded device-side wait ran out */
-    TTS_ERR_SCRATCH = -6         /* tts_verify_attn_noalloc: the problem needs more than the fixed scratch array */
+    TTS_ERR_SCRATCH = -6,        /* tts_verify_attn_noalloc: the problem needs more than the fixed scratch array */
+    TTS_ERR_DEVICE_PAGES = -7    /* (via tts_last_status) a page call found too few free pages and changed nothing */
 } tts_status;
 
 enum { TTS_MASK_CAUSAL = 0, TTS_MASK_TREE = 1 };
@@ -362,6 +363,124 @@ TTS_API int tts_kv_append(tts_ctx* ctx, const void* k_new, const void* v_new, vo
                           int n_branches, int rows);
 TTS_API int tts_kv_rollback(tts_ctx* ctx, int32_t* branch_lens, const int32_t* accepted_len, int n_branches,
                             int gamma);
+
+/*
+ * Chunks: the new tokens of several branches in one call, any number per branch (Section 3.2: the prompt of a
+ * question enters the cache before its branches decode; the paper's prefill discussion has prompts of up to 800
+ * tokens).  The rows of all chunks lie behind one another: branch b owns rows row_start[b] .. row_start[b+1] - 1
+ * of q, out and the other per-row arrays (row_start device [n_branches+1] i32, non-decreasing), c_b of them, and
+ * c_b may be 0.  Rows before row_start[0] and from row_start[n_branches] on belong to no branch and their results
+ * are left as they were.  branch_lens[b] counts the private tokens INCLUDING the chunk, as in tts_verify_attn.
+ *
+ * tts_chunk_reserve allocates what tts_chunk_attn needs for calls of up to max_rows rows (about 80 MB of partial
+ *   results and the schedule's tables).  Call it once per context; a later call with a smaller or equal number
+ *   returns TTS_OK, a larger one TTS_ERR_INVALID (captured graphs hold the workspace's addresses).
+ *   TTS_ERR_UNSUPPORTED when more than 128 query heads share a KV head.
+ *
+ * tts_chunk_attn: exact softmax attention of the chunks over the paged cache, keys and values of the chunk being in
+ *   the pages already:
+ *     out[r][h] = sum_t softmax_t(scale * <q[r][h], K[t][h/G]>) * V[t][h/G],   lse[r][h] = log sum_t exp(scale * <..>)
+ *   over the keys t <= prefix_len + branch_lens[b] - c_b + i that row i of branch b's chunk sees (its own place and
+ *   everything before it).  A row that sees nothing (a chunk longer than prefix_len + branch_lens[b]) gets out = 0 and
+ *   lse = -infinity.
+ *     q            device  rows of [Hq][128] bf16, q_row_stride elements from row to row (>= Hq * 128, a multiple of
+ *                          8), so that q may be a slice of a fused projection; 16-byte aligned
+ *     out          device  [total_rows][Hq][128], cfg.out_dtype
+ *     lse          device  [total_rows][Hq] fp32, or NULL
+ *     total_rows   host    rows of the arrays, <= the reserved number; 0 launches nothing
+ *     k_pages, v_pages, block_table, prefix_len (host, a multiple of 16; the first prefix_len / 16 entries of the rows
+ *     may, but need not be equal), branch_lens: as in tts_verify_attn
+ *   cfg.max_ctas bounds the grid, cfg.softmax_scale and cfg.out_dtype apply; cfg.attn_impl does not.
+ *   Reported through tts_last_status, whatever cfg.debug_bounds: row starts that decrease or leave [0, total_rows],
+ *   negative lengths, or branches longer than the table row compute nothing (TTS_ERR_DEVICE_BOUNDS); a page id outside
+ *   the pool is read as zeros (TTS_ERR_DEVICE_BOUNDS).  Slots past a branch's end may hold anything, NaN included.
+ *   Everything up to a branch's end must be finite in V where a row of the same chunk may not see it yet: a
+ *   probability of zero times an infinity would be NaN.
+ *
+ * One context's chunk and page calls share its workspace: order them on the GPU (one stream, or events).  Graphs
+ * captured from them replay in any number, one at a time.
+ */
+TTS_API int tts_chunk_reserve(tts_ctx* ctx, int max_rows);
+TTS_API int tts_chunk_attn(tts_ctx* ctx, const void* q, int64_t q_row_stride, const void* k_pages, const void* v_pages,
+                           const int32_t* block_table, int prefix_len, const int32_t* branch_lens,
+                           const int32_t* row_start, int n_branches, int total_rows, void* out, float* lse);
+
+/*
+ * Rotary positions on the way into the cache: per row of the chunks, rotates the queries into q_out, rotates the keys
+ * and writes them, with the values as they are, to the row's place in the pages (token prefix_len + branch_lens[b] -
+ * c_b + i of branch b): what stands between the QKV projection and the attention of the same rows, for tts_chunk_attn
+ * and, with gamma+1 rows per branch, for tts_verify_attn.  Pair i of a head vector turns by the angle
+ * positions[axis[i]][row] * inv_freq[i]:  (x_lo, x_hi) -> (x_lo cos - x_hi sin, x_lo sin + x_hi cos).
+ *   rope         host    n_axes (1..8) position axes: 1 for text; time, height, width for images and video;
+ *                        n_pairs (1..64) pairs are turned, dims from 2 * n_pairs on pass through;
+ *                        pair i is dims (i, i + n_pairs), or (2i, 2i + 1) when interleaved != 0;
+ *                        axis[i] < n_axes is the axis that turns pair i, inv_freq[i] its radians per position, so any
+ *                        base and any scaling of the frequencies can be given
+ *   q, k, v      device  rows of [Hq][128], [Hkv][128], [Hkv][128] bf16; q_row_stride / kv_row_stride elements from row
+ *                        to row (multiples of 8); 16-byte aligned
+ *   positions    device  [n_axes][total_rows] i32, any values; the angle is formed in 64 bits
+ *   q_out        device  [total_rows][Hq][128] bf16; may be q itself when q is dense; other overlaps are refused
+ *   k_pages, v_pages are written, the other arguments as in tts_chunk_attn (total_rows is not bounded by a reserve)
+ * A branch shorter than its chunk, a token beyond the table row or a page outside the pool writes no key and value for
+ * that row and raises TTS_ERR_DEVICE_BOUNDS; the query is rotated all the same.
+ */
+typedef struct {
+    int32_t n_axes, n_pairs, interleaved;
+    uint8_t axis[64];
+    double inv_freq[64];
+} tts_rope;
+TTS_API int tts_kv_append_rope(tts_ctx* ctx, const tts_rope* rope, const void* q, int64_t q_row_stride, const void* k,
+                               const void* v, int64_t kv_row_stride, const int32_t* positions, void* k_pages,
+                               void* v_pages, const int32_t* block_table, int prefix_len, const int32_t* branch_lens,
+                               const int32_t* row_start, int n_branches, int total_rows, void* q_out);
+
+/*
+ * Pages of the cache.  Branch-wise parallelism (Section 3.2) as a search runs it: branches are dropped, continued in
+ * several copies, grow, and finish at different times.  These calls keep the books on the device, asynchronously on
+ * the context's stream and without reading anything back:
+ *   block_table  a row holds the pages of its branch, entries >= 0, and -1 where it has none.  Pages a branch holds
+ *                beyond its length (after tts_kv_rollback) stay its own
+ *   page_refs    device [num_pages] i32, 16-byte aligned: how many table entries name each page; 0 = free.  Free pages
+ *                are handed out lowest id first, to the branches in their order, so results do not depend on timing
+ *   k_pools, v_pools  host arrays of n_layers (1..128) device pointers: a page id names the same page in all of them
+ * A page id outside the pool, a length outside the table row, or an entry that page_refs does not know raises
+ * TTS_ERR_DEVICE_BOUNDS (tts_last_status).  A call that needs more pages than are free raises TTS_ERR_DEVICE_PAGES.
+ *
+ *   tts_kv_copy_pages  page src_pages[i] -> dst_pages[i] in every pool (device arrays, n_copies entries; a negative id
+ *                      on either side skips the entry).  A page must not be the target of two entries, nor the target
+ *                      of one and the source of another.
+ *   tts_kv_fork        the next generation of branches: child i continues branch parents[i] (device [n_children] i32,
+ *                      -1: an empty row).  The first child of a branch takes over its row; every further one shares the
+ *                      full pages (one more reference) and gets a copy of the part-filled last page in a fresh page;
+ *                      the pages of branches without a child are given back.  Reads block_table [n_branches],
+ *                      branch_lens, page_refs; writes new_table [n_children][max_blocks_per_branch], new_lens, new_refs
+ *                      (which may be page_refs).  Pages given back by the call are not handed out by it.  With too few
+ *                      free pages new_table and new_lens are left as they were and new_refs equals page_refs.
+ *   tts_kv_grow        room for n_new[b] >= 0 more tokens of every branch (device [n_branches] i32): entries up to the
+ *                      new length that hold no page get a free one, and branch_lens[b] += n_new[b].  All or nothing: a
+ *                      bad length or too few pages change nothing.
+ *   tts_kv_free        gives back all pages of the branches with freed[b] != 0 (device [n_branches] i32): the row
+ *                      becomes -1, the length 0.
+ *   tts_kv_compact     closes the holes of the pool: with n_used pages in use, the pages from n_used on move to the
+ *                      free ids below it, lowest to lowest, in every pool, and new_table / new_refs follow.  page_map
+ *                      device [num_pages] i32 gets the new id of every page (-1: free), for tables of the caller's own;
+ *                      n_used device [1] i32.  block_table must hold all references that page_refs counts, or the
+ *                      others have to be mapped by the caller.  new_table may be block_table, new_refs page_refs.
+ * TTS_ERR_INVALID for null or misaligned pointers, sizes outside the context's limits and overlaps not named above.
+ */
+TTS_API int tts_kv_copy_pages(tts_ctx* ctx, int n_layers, void* const* k_pools, void* const* v_pools,
+                              const int32_t* src_pages, const int32_t* dst_pages, int n_copies);
+TTS_API int tts_kv_fork(tts_ctx* ctx, int n_layers, void* const* k_pools, void* const* v_pools,
+                        const int32_t* block_table, int prefix_len, const int32_t* branch_lens, int n_branches,
+                        const int32_t* parents, int n_children, const int32_t* page_refs, int32_t* new_table,
+                        int32_t* new_lens, int32_t* new_refs);
+TTS_API int tts_kv_grow(tts_ctx* ctx, int32_t* block_table, int prefix_len, int32_t* branch_lens, const int32_t* n_new,
+                        int n_branches, int32_t* page_refs);
+TTS_API int tts_kv_free(tts_ctx* ctx, int32_t* block_table, int32_t* branch_lens, const int32_t* freed, int n_branches,
+                        int32_t* page_refs);
+TTS_API int tts_kv_compact(tts_ctx* ctx, int n_layers, void* const* k_pools, void* const* v_pools,
+                           const int32_t* block_table, int n_branches, const int32_t* page_refs, int32_t* new_table,
+                           int32_t* new_refs, int32_t* page_map, int32_t* n_used);
 
 /*
  * One whole verify step from HOST buffers (the end-to-end path): for each of n_layers layers,

@@ -7,7 +7,7 @@ missing, loading raises.
 from __future__ import annotations
 
 import ctypes
-from ctypes import POINTER, byref, c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_void_p
+from ctypes import POINTER, byref, c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_uint8, c_void_p
 from pathlib import Path
 from typing import Optional, Sequence
 
@@ -25,6 +25,7 @@ EXPORTED_SYMBOLS = (
     "tts_accept", "tts_accept_logits", "tts_verify_step_host_logits", "tts_majority_vote", "tts_confidence_max", "tts_greedy_search", "tts_grid_search", "tts_last_status",
     "tts_last_cuda_error", "tts_launch_count", "tts_strerror", "tts_verify_step_host",
     "tts_profile_enable", "tts_profile_read", "tts_debug_wait_timeout", "tts_verify_attn_noalloc", "tts_kv_append", "tts_kv_rollback", "tts_accept_tree",
+    "tts_chunk_reserve", "tts_chunk_attn", "tts_kv_append_rope", "tts_kv_copy_pages", "tts_kv_fork", "tts_kv_grow", "tts_kv_free", "tts_kv_compact",
 )
 
 
@@ -46,6 +47,28 @@ class TtsConfig(ctypes.Structure):
 
 class TtsSearchLimits(ctypes.Structure):
     _fields_ = [("max_branches", c_int32), ("max_gamma", c_int32), ("max_steps", c_int32)]
+
+
+class TtsRope(ctypes.Structure):
+    """Rotary positions of a model: axis[i] and inv_freq[i] (radians per position) for every turned pair."""
+    _fields_ = [("n_axes", c_int32), ("n_pairs", c_int32), ("interleaved", c_int32), ("axis", c_uint8 * 64), ("inv_freq", c_double * 64)]
+
+    def __init__(self, axis: Sequence[int], inv_freq: Sequence[float], interleaved: bool = False):
+        if not 1 <= len(inv_freq) <= 64 or len(axis) != len(inv_freq) or min(axis) < 0 or max(axis) > 7:
+            raise ValueError("one axis (0..7) and one frequency for each of 1..64 pairs")
+        super().__init__(max(axis) + 1, len(inv_freq), 1 if interleaved else 0, (c_uint8 * 64)(*axis), (c_double * 64)(*inv_freq))
+
+
+class TtsPools:
+    """The K and V pools of all layers, as the page calls take them (tensors or addresses; it keeps the tensors alive)."""
+
+    def __init__(self, k_pools: Sequence, v_pools: Sequence):
+        if len(k_pools) != len(v_pools):
+            raise ValueError("as many K pools as V pools")
+        self.n_layers = len(k_pools)
+        self._alive = (list(k_pools), list(v_pools))
+        self.k = (c_void_p * self.n_layers)(*[_ptr(x).value for x in k_pools])
+        self.v = (c_void_p * self.n_layers)(*[_ptr(x).value for x in v_pools])
 
 
 _TASK_FN = ctypes.CFUNCTYPE(c_double, c_int, c_int, c_void_p)
@@ -83,6 +106,15 @@ def load_library() -> ctypes.CDLL:
     lib.tts_accept_tree.argtypes = [vp, vp, vp, vp, vp, vp, c_int, c_int, c_int, vp, vp, vp]
     lib.tts_kv_append.argtypes = [vp, vp, vp, vp, vp, vp, c_int, vp, c_int, c_int]
     lib.tts_kv_rollback.argtypes = [vp, vp, vp, c_int, c_int]
+    pp, i64 = POINTER(c_void_p), c_int64
+    lib.tts_chunk_reserve.argtypes = [vp, c_int]
+    lib.tts_chunk_attn.argtypes = [vp, vp, i64, vp, vp, vp, c_int, vp, vp, c_int, c_int, vp, vp]
+    lib.tts_kv_append_rope.argtypes = [vp, POINTER(TtsRope), vp, i64, vp, vp, i64, vp, vp, vp, vp, c_int, vp, vp, c_int, c_int, vp]
+    lib.tts_kv_copy_pages.argtypes = [vp, c_int, pp, pp, vp, vp, c_int]
+    lib.tts_kv_fork.argtypes = [vp, c_int, pp, pp, vp, c_int, vp, c_int, vp, c_int, vp, vp, vp, vp]
+    lib.tts_kv_grow.argtypes = [vp, vp, c_int, vp, vp, c_int, vp]
+    lib.tts_kv_free.argtypes = [vp, vp, vp, vp, c_int, vp]
+    lib.tts_kv_compact.argtypes = [vp, c_int, pp, pp, vp, c_int, vp, vp, vp, vp, vp]
     lib.tts_majority_vote.argtypes = [POINTER(c_int64), POINTER(c_float), c_int, POINTER(c_int64), POINTER(c_int)]
     lib.tts_confidence_max.argtypes = lib.tts_majority_vote.argtypes
     lib.tts_greedy_search.argtypes = [_TASK_FN, vp, POINTER(TtsSearchLimits), POINTER(c_int), POINTER(c_int),
@@ -127,6 +159,14 @@ def _ptr(x) -> c_void_p:
     if hasattr(x, "ctypes"):
         return c_void_p(x.ctypes.data)
     raise TypeError(f"cannot take the address of {type(x)}")
+
+
+def _addr(x):
+    """The same as a plain integer (None stays None): cheaper where a call's time is its latency."""
+    if x is None or isinstance(x, int):
+        return x
+    data_ptr = getattr(x, "data_ptr", None)
+    return data_ptr() if data_ptr is not None else _ptr(x).value
 
 
 class TtsContext:
@@ -241,6 +281,52 @@ class TtsContext:
     def tts_kv_rollback(self, branch_lens, accepted_len, n_branches: int, gamma: int):
         self._check(self._lib.tts_kv_rollback(self._h, _ptr(branch_lens), _ptr(accepted_len), int(n_branches),
                                               int(gamma)), "tts_kv_rollback")
+
+    def tts_chunk_reserve(self, max_rows: int):
+        self._check(self._lib.tts_chunk_reserve(self._h, int(max_rows)), "tts_chunk_reserve")
+
+    def tts_chunk_attn(self, q, q_row_stride: int, k_pages, v_pages, block_table, prefix_len: int, branch_lens, row_start,
+                       n_branches: int, total_rows: int, out, lse=None):
+        rc = self._lib.tts_chunk_attn(self._h, _addr(q), q_row_stride, _addr(k_pages), _addr(v_pages), _addr(block_table), prefix_len,
+                                      _addr(branch_lens), _addr(row_start), n_branches, total_rows, _addr(out), _addr(lse))
+        if rc:
+            self._check(rc, "tts_chunk_attn")
+
+    def tts_kv_append_rope(self, rope: TtsRope, q, q_row_stride: int, k, v, kv_row_stride: int, positions, k_pages, v_pages, block_table,
+                           prefix_len: int, branch_lens, row_start, n_branches: int, total_rows: int, q_out):
+        rc = self._lib.tts_kv_append_rope(self._h, byref(rope), _addr(q), q_row_stride, _addr(k), _addr(v), kv_row_stride, _addr(positions),
+                                          _addr(k_pages), _addr(v_pages), _addr(block_table), prefix_len, _addr(branch_lens),
+                                          _addr(row_start), n_branches, total_rows, _addr(q_out))
+        if rc:
+            self._check(rc, "tts_kv_append_rope")
+
+    def tts_kv_copy_pages(self, pools: TtsPools, src_pages, dst_pages, n_copies: int):
+        rc = self._lib.tts_kv_copy_pages(self._h, pools.n_layers, pools.k, pools.v, _addr(src_pages), _addr(dst_pages), n_copies)
+        if rc:
+            self._check(rc, "tts_kv_copy_pages")
+
+    def tts_kv_fork(self, pools: TtsPools, block_table, prefix_len: int, branch_lens, n_branches: int, parents, n_children: int, page_refs,
+                    new_table, new_lens, new_refs):
+        rc = self._lib.tts_kv_fork(self._h, pools.n_layers, pools.k, pools.v, _addr(block_table), prefix_len, _addr(branch_lens), n_branches,
+                                   _addr(parents), n_children, _addr(page_refs), _addr(new_table), _addr(new_lens), _addr(new_refs))
+        if rc:
+            self._check(rc, "tts_kv_fork")
+
+    def tts_kv_grow(self, block_table, prefix_len: int, branch_lens, n_new, n_branches: int, page_refs):
+        rc = self._lib.tts_kv_grow(self._h, _addr(block_table), prefix_len, _addr(branch_lens), _addr(n_new), n_branches, _addr(page_refs))
+        if rc:
+            self._check(rc, "tts_kv_grow")
+
+    def tts_kv_free(self, block_table, branch_lens, freed, n_branches: int, page_refs):
+        rc = self._lib.tts_kv_free(self._h, _addr(block_table), _addr(branch_lens), _addr(freed), n_branches, _addr(page_refs))
+        if rc:
+            self._check(rc, "tts_kv_free")
+
+    def tts_kv_compact(self, pools: TtsPools, block_table, n_branches: int, page_refs, new_table, new_refs, page_map, n_used):
+        rc = self._lib.tts_kv_compact(self._h, pools.n_layers, pools.k, pools.v, _addr(block_table), n_branches, _addr(page_refs),
+                                      _addr(new_table), _addr(new_refs), _addr(page_map), _addr(n_used))
+        if rc:
+            self._check(rc, "tts_kv_compact")
 
     def tts_last_status(self) -> int:
         st = c_int(0)

@@ -1,0 +1,601 @@
+// Attention of ragged chunks of new tokens over the paged cache: prompts on their way in, a serving step's mix
+// of prompt pieces and single tokens.
+//
+//   out[r] = sum_t p_t V_t / sum_t p_t,  p_t = exp(scale <q_r, K_t> - m_r),  lse[r] = m_r + log sum_t p_t,
+//
+// over the keys t below the row's limit (its own place in the sequence + 1), in one pass over the KV tiles with
+// a running maximum and sum.  Scores, probabilities, sums and O are fp32; the probabilities are rounded to
+// bf16 (2^-9 each, averaging out over the keys) where they become an operand of the second contraction.
+//
+// Bound by the tensor cores for long chunks (4 x 128 operations per query row and key) and by HBM for single
+// tokens.  One persistent CTA per SM takes pieces (chunk_attn.cuh) from a list.  A CTA has two *sides*, each
+// with a 128-row score tile and a 128 x 128 fp32 accumulator in TMEM and a softmax warpgroup of its own, so
+// that one side's exponentials run while the tensor pipe works for the other:
+//   wide piece     side s holds row tile s; both go over the same KV tiles, which are loaded once for 256 rows
+//   narrow piece   both sides hold the same rows; side s takes every second KV tile; side 0 joins the two
+//
+//   warps 0-3, 4-7  softmax of side 0, 1: one thread per row.  It reads its 128 scores from TMEM, writes the
+//                   probabilities as bf16 pairs over the first half of its own score columns (the A operand of
+//                   P V comes from TMEM), rescales O in TMEM only when the maximum has moved by more than 2^8
+//                   (l carries the same reference, so the result is the same), and at the end divides and
+//                   stores its row, or leaves (m, l, O) for the last piece of the entry to join.
+//   warp 8          takes pieces, hands them to the other roles through a ring of two, loads Q
+//   warp 9, 10      load the K and V tiles: one TMA box per 4 KiB page tile, rings of three and two slots
+//   warp 11         issues the MMAs.  Per side the order is S(0); then for each tile P V(j), S(j+1): the tensor
+//                   pipe keeps issue order, so S(j+1) may overwrite the columns that held P(j), and when S(j+1)
+//                   is complete P V(j) is as well -- the only wait on O that the softmax needs.
+//
+// Page ids outside the pool and entries beyond the table row read as zeros (and are reported); tokens past the
+// end of a branch never contribute: their scores are replaced before the maximum and their V rows are zeroed in
+// shared memory, whatever the page holds there.  All waits are bounded (umma_ptx.cuh).
+#include <cuda.h>
+
+#include "chunk_attn.cuh"
+#include "launch.cuh"
+#include "umma_ptx.cuh"
+
+namespace tts {
+
+namespace {
+
+using namespace ptx;
+
+constexpr int kTile = kChunkTile;
+constexpr int kRows = 128;
+constexpr int kSideThreads = 128;
+constexpr int kThreadsChunk = 2 * kSideThreads + 128;
+constexpr int kTakeWarp = 8, kKWarp = 9, kVWarp = 10, kMmaWarp = 11;
+constexpr int kHalfBytes = kRows * 128;
+constexpr int kOperandBytes = 2 * kHalfBytes;
+constexpr int kRingK = 3, kRingV = 2, kRingPiece = 2;
+constexpr uint32_t kTmemCols = 512;
+
+constexpr int kOffQ = 0;                                       // two row tiles
+constexpr int kOffK = kOffQ + 2 * kOperandBytes;
+constexpr int kOffV = kOffK + kRingK * kOperandBytes;
+constexpr int kOffBar = kOffV + kRingV * kOperandBytes;
+enum Bar {
+    K_FULL = 0, K_EMPTY = K_FULL + kRingK, V_FULL = K_EMPTY + kRingK, V_EMPTY = V_FULL + kRingV, V_TAIL = V_EMPTY + kRingV,
+    Q_FULL, Q_EMPTY = Q_FULL + 2, S_FULL = Q_EMPTY + 2, P_FULL = S_FULL + 2, O_FULL = P_FULL + 2, PIECE_FULL = O_FULL + 2,
+    PIECE_EMPTY = PIECE_FULL + kRingPiece, JOIN_FULL = PIECE_EMPTY + kRingPiece, JOIN_EMPTY, kNumBars
+};
+constexpr int kOffMisc = kOffBar + ((kNumBars * 8 + 15) & ~15);   // [0] abort, [1] TMEM base, [2, 3] scratch, [4, 5] last-piece flags
+constexpr int kOffPiece = kOffMisc + 32;                       // ring of pieces (+ their KV head)
+constexpr int kPieceBytes = 64;
+constexpr int kOffJoin = kOffPiece + kRingPiece * kPieceBytes; // side 1's (m, l) of a narrow piece
+constexpr int kSmemBytes = kOffJoin + kRows * 8 + 1024;
+static_assert(kSmemBytes <= 227 * 1024, "shared memory");
+
+__device__ __forceinline__ void warp_arrive(uint32_t bar, int lane) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar);
+}
+
+// A piece as every role sees it.
+struct Work {
+    ChunkPiece x;
+    int kvh;
+    bool wide;
+    int n[2];        // KV tiles of each side
+    int loads;       // KV tiles to load
+};
+
+__device__ __forceinline__ void derive(Work& w, int T) {
+    const ChunkPiece& x = w.x;
+    w.wide = x.n_tok > T;
+    const int tiles = x.tile_end - x.tile_begin;
+    if (w.wide) {
+        // side 0 stops at the tile of its last token's last key
+        const int limit = min(x.keys, max(0, x.limit0 + T - 1));
+        w.n[0] = max(0, min(x.tile_end, ceil_div(limit, kTile)) - x.tile_begin);
+        w.n[1] = tiles;
+    } else {
+        w.n[0] = (tiles + 1) >> 1;
+        w.n[1] = tiles >> 1;
+    }
+    w.loads = tiles;
+}
+
+// Next piece from the ring; false at the end of the list or when the CTA is aborting.
+__device__ __forceinline__ bool next_piece(Work& w, int it, const unsigned char* smem, uint32_t bar0, int lane, int T, const Abort& ab) {
+    const int slot = it % kRingPiece;
+    const bool ok = __all_sync(0xffffffffu, mbar_wait(bar0 + 8u * (PIECE_FULL + slot), (it / kRingPiece) & 1, ab));
+    if (!ok) return false;
+    const int4* src = reinterpret_cast<const int4*>(smem + kOffPiece + slot * kPieceBytes);
+    int4* dst = reinterpret_cast<int4*>(&w.x);
+    dst[0] = src[0]; dst[1] = src[1]; dst[2] = src[2];
+    w.kvh = src[3].x;
+    warp_arrive(bar0 + 8u * (PIECE_EMPTY + slot), lane);
+    if (w.kvh < 0) return false;
+    derive(w, T);
+    return true;
+}
+
+__device__ __forceinline__ void tma_load_rows(uint32_t dst, const CUtensorMap* map, int dim, int head, int row, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+        ::"r"(dst), "l"(map), "r"(dim), "r"(head), "r"(row), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void tma_load_page_keep(uint32_t dst, const CUtensorMap* map, int page_head, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %2, %2, %2, %3}], [%4];"
+        ::"r"(dst), "l"(map), "r"(0), "r"(page_head), "r"(bar) : "memory");
+}
+
+// 32 bytes per thread: whole sectors, although every thread writes a row of its own
+__device__ __forceinline__ void st_global_32(void* p, const uint32_t (&r)[8]) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
+
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// Eight values of a result row, columns [col, col + 8)
+__device__ __forceinline__ void store_out(const ChunkParams& p, size_t row_head, int col, const float (&v)[8]) {
+    if (p.out_dtype == TTS_OUT_FP32) {
+        uint32_t r[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r[i] = __float_as_uint(v[i]);
+        st_global_32(static_cast<float*>(p.out) + row_head * kHeadDim + col, r);
+    } else {
+        *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + row_head * kHeadDim + col) =
+            make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
+    }
+}
+
+__global__ void __launch_bounds__(kThreadsChunk, 1)
+chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
+                  const __grid_constant__ CUtensorMap tm_v) {
+    extern __shared__ unsigned char smem_dyn[];
+    unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~(uintptr_t)1023);
+    const uint32_t sbase = smem_u32(smem);
+    const uint32_t bar0 = sbase + kOffBar;
+    auto bar = [&](int i) { return bar0 + 8u * i; };
+    volatile int* misc = reinterpret_cast<volatile int*>(smem + kOffMisc);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const Abort ab{misc, p.status};
+
+    if (tid == 0) {
+        misc[0] = 0;
+        for (int i = 0; i < kRingK; ++i) { mbar_init(bar(K_FULL + i), 1); mbar_init(bar(K_EMPTY + i), 1); }
+        for (int i = 0; i < kRingV; ++i) { mbar_init(bar(V_FULL + i), 1); mbar_init(bar(V_EMPTY + i), 1); }
+        mbar_init(bar(V_TAIL), 1);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar(Q_FULL + i), 1); mbar_init(bar(Q_EMPTY + i), 1); mbar_init(bar(S_FULL + i), 1);
+            mbar_init(bar(P_FULL + i), kSideThreads / 32); mbar_init(bar(O_FULL + i), 1);
+        }
+        for (int i = 0; i < kRingPiece; ++i) { mbar_init(bar(PIECE_FULL + i), 1); mbar_init(bar(PIECE_EMPTY + i), 11); }   // all warps but the taker
+        mbar_init(bar(JOIN_FULL), kSideThreads / 32); mbar_init(bar(JOIN_EMPTY), kSideThreads / 32);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == kMmaWarp) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(sbase + kOffMisc + 4), "r"(kTmemCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = (uint32_t)misc[1];
+    grid_dependency_wait();
+    grid_launch_dependents();
+
+    if (warp == kTakeWarp) {
+        // =========================== takes pieces, loads Q ===========================
+        if (lane == 0) {
+            const int per_head = p.head->pieces_per_head, total = per_head * p.Hkv;
+            int index = blockIdx.x, used[2] = {0, 0};
+            bool alive = true;
+            for (int it = 0; alive; ++it) {
+                const int slot = it % kRingPiece;
+                Work w;
+                w.kvh = -1;
+                if (index < total) {
+                    w.kvh = index / per_head;
+                    const int4* src = reinterpret_cast<const int4*>(p.pieces + (index - w.kvh * per_head));
+                    int4* dst = reinterpret_cast<int4*>(&w.x);
+                    dst[0] = src[0]; dst[1] = src[1]; dst[2] = src[2];
+                }
+                alive = mbar_wait(bar(PIECE_EMPTY + slot), ((it / kRingPiece) & 1) ^ 1, ab);
+                if (!alive) break;
+                int4* ring = reinterpret_cast<int4*>(smem + kOffPiece + slot * kPieceBytes);
+                const int4* src = reinterpret_cast<const int4*>(&w.x);
+                ring[0] = src[0]; ring[1] = src[1]; ring[2] = src[2];
+                ring[3] = make_int4(w.kvh, 0, 0, 0);
+                mbar_arrive(bar(PIECE_FULL + slot));
+                if (w.kvh < 0) break;
+                index = atomicAdd(&p.head->next, 1);
+                derive(w, p.T);
+                for (int s = 0; s < (w.wide ? 2 : 1) && alive; ++s) {
+                    if (w.n[s] == 0) continue;
+                    alive = mbar_wait(bar(Q_EMPTY + s), (used[s] & 1) ^ 1, ab);
+                    if (!alive) break;
+                    ++used[s];
+                    mbar_arrive_expect_tx(bar(Q_FULL + s), (uint32_t)(p.T * p.G) * 256u);
+                    const uint32_t dst = sbase + kOffQ + s * kOperandBytes;
+                    tma_load_rows(dst, &tm_q, 0, w.kvh * p.G, w.x.row0 + s * p.T, bar(Q_FULL + s));
+                    tma_load_rows(dst + kHalfBytes, &tm_q, 64, w.kvh * p.G, w.x.row0 + s * p.T, bar(Q_FULL + s));
+                }
+            }
+            // copies in flight land before the CTA may end: the consumers wait for them, unless they gave up
+            if (*ab.flag)
+                for (int s = 0; s < 2; ++s)
+                    if (used[s] > 0) {
+                        const Abort quiet{misc + 2, p.status};
+                        misc[2] = 0;
+                        mbar_wait(bar(Q_FULL + s), (used[s] - 1) & 1, quiet);
+                    }
+        }
+    } else if (warp == kKWarp || warp == kVWarp) {
+        // =========================== K and V tiles ===========================
+        const bool is_v = warp == kVWarp;
+        const int ring_n = is_v ? kRingV : kRingK;
+        const int full0 = is_v ? V_FULL : K_FULL, empty0 = is_v ? V_EMPTY : K_EMPTY;
+        const int ring_off = is_v ? kOffV : kOffK;
+        const CUtensorMap* tm = is_v ? &tm_v : &tm_k;
+        const uint64_t once = l2_policy_evict_first();
+        int slot = 0, round = 0, issued = 0, tails = 0;
+        bool alive = true;
+        Work w;
+        for (int it = 0; alive && next_piece(w, it, smem, bar0, lane, p.T, ab); ++it) {
+            const int32_t* bt = p.block_table + (size_t)w.x.branch * p.max_blocks;
+            auto page_of = [&](int t) -> int {                          // this lane's page of KV tile t
+                const int blk = t * (kTile / kPage) + lane;
+                if (lane >= kTile / kPage || blk * kPage >= w.x.keys) return -2;
+                const int page = blk < p.max_blocks ? bt[blk] : -1;
+                if (page < 0 || page >= p.num_pages) { atomicMin(p.status, (int)TTS_ERR_DEVICE_BOUNDS); return -1; }
+                return page;
+            };
+            int page = w.loads > 0 ? page_of(w.x.tile_begin) : -2;
+            for (int j = 0; j < w.loads; ++j) {
+                const int tok0 = (w.x.tile_begin + j) * kTile;
+                const int n_valid = min(kTile, w.x.keys - tok0), n_pages = ceil_div(n_valid, kPage);
+                const bool tail = is_v && n_valid < kTile;
+                const int full = tail ? (int)V_TAIL : full0 + slot;
+                const int next = j + 1 < w.loads ? page_of(w.x.tile_begin + j + 1) : -2;
+                if (lane == 0) {
+                    alive = mbar_wait(bar(empty0 + slot), round ^ 1, ab);
+                    if (alive) mbar_arrive_expect_tx(bar(full), (uint32_t)n_pages * 4096u);
+                }
+                alive = __shfl_sync(0xffffffffu, alive, 0);
+                if (!alive) break;
+                const uint32_t dst = sbase + ring_off + slot * kOperandBytes;
+                if (lane < n_pages) {
+                    // a page outside the pool: a coordinate outside the map, which reads as zeros
+                    const int page_head = page < 0 ? -1 : page * p.Hkv + w.kvh;
+                    if (w.x.once) tma_load_page(dst + lane * 4096, tm, page_head, bar(full), once);
+                    else tma_load_page_keep(dst + lane * 4096, tm, page_head, bar(full));
+                }
+                ++issued;
+                if (tail) {
+                    // no row sees the tokens past the end, but 0 x NaN would be NaN: their V rows become zeros
+                    alive = __all_sync(0xffffffffu, mbar_wait(bar(V_TAIL), tails & 1, ab));
+                    ++tails;
+                    if (!alive) break;
+                    for (int i = lane; i < (kTile - n_valid) * 16; i += 32) {
+                        const int row = n_valid + i / 16, c = i % 16;
+                        *reinterpret_cast<uint4*>(smem + kOffV + slot * kOperandBytes + (row >> 4) * 4096 + ((row >> 3) & 1) * 2048 +
+                                                  (c >> 3) * 1024 + (row & 7) * 128 + ((c & 7) << 4)) = make_uint4(0, 0, 0, 0);
+                    }
+                    fence_proxy_async();
+                    warp_arrive(bar(full0 + slot), lane);
+                }
+                page = next;
+                if (++slot == ring_n) { slot = 0; round ^= 1; }
+            }
+        }
+        if (*ab.flag && lane == 0) {
+            const Abort quiet{misc + 2 + is_v, p.status};
+            for (int back = 1; back <= ring_n && back <= issued; ++back) {
+                const int i = issued - back;
+                misc[2 + is_v] = 0;
+                mbar_wait(bar(full0 + i % ring_n), (i / ring_n) & 1, quiet);
+            }
+        }
+    } else if (warp == kMmaWarp) {
+        // =========================== MMA issuer ===========================
+        constexpr uint32_t idesc_qk = instr_desc(kRows, kTile, false, false), idesc_pv = instr_desc(kRows, kHeadDim, false, true);
+        int k_base = 0, v_base = 0, q_used[2] = {0, 0}, s_done[2] = {0, 0};
+        bool alive = true;
+        Work w;
+        for (int it = 0; alive && next_piece(w, it, smem, bar0, lane, p.T, ab); ++it) {
+            if (lane == 0) {
+            const int n_max = max(w.n[0], w.n[1]);
+            // S of side s, its jj-th tile
+            auto scores = [&](int s, int jj) -> bool {
+                const int kt = k_base + (w.wide ? jj : 2 * jj + s), slot = kt % kRingK;
+                const int q = w.wide ? s : 0;
+                if (jj == 0 && (w.wide || s == 0) && !mbar_wait(bar(Q_FULL + q), q_used[q] & 1, ab)) return false;
+                if (!mbar_wait(bar(K_FULL + slot), (kt / kRingK) & 1, ab)) return false;
+                tc_fence_after();
+                const uint32_t qa = sbase + kOffQ + q * kOperandBytes, ka = sbase + kOffK + slot * kOperandBytes;
+#pragma unroll
+                for (int ks = 0; ks < 8; ++ks)
+                    umma_bf16(tmem + s * 128u, smem_desc(qa + (ks >> 2) * kHalfBytes + (ks & 3) * 32, 16, 1024),
+                              smem_desc(ka + (ks >> 2) * 1024 + (ks & 3) * 32, 16, 2048), idesc_qk, ks > 0);
+                umma_commit(bar(S_FULL + s));
+                if (!w.wide || s == 1) umma_commit(bar(K_EMPTY + slot));
+                // the last reader of a Q tile gives it back
+                if (w.wide ? jj + 1 == w.n[s] : 2 * jj + s + 1 == w.loads) umma_commit(bar(Q_EMPTY + q));
+                return true;
+            };
+            auto values = [&](int s, int jj) -> bool {
+                const int vt = v_base + (w.wide ? jj : 2 * jj + s), slot = vt % kRingV;
+                if (!mbar_wait(bar(P_FULL + s), (s_done[s] + jj) & 1, ab) || !mbar_wait(bar(V_FULL + slot), (vt / kRingV) & 1, ab)) return false;
+                tc_fence_after();
+                const uint32_t va = sbase + kOffV + slot * kOperandBytes;
+#pragma unroll
+                for (int ks = 0; ks < 8; ++ks)
+                    umma_bf16_tmem_a(tmem + 256u + s * 128u, tmem + s * 128u + ks * 8u, smem_desc(va + ks * 4096, 1024, 2048), idesc_pv,
+                                     (jj > 0 || ks > 0) ? 1u : 0u);
+                if (!w.wide || s == 1) umma_commit(bar(V_EMPTY + slot));
+                if (jj + 1 == w.n[s]) umma_commit(bar(O_FULL + s));
+                return true;
+            };
+            for (int s = 0; s < 2 && alive; ++s)
+                if (w.n[s] > 0) alive = scores(s, 0);
+            for (int jj = 0; jj < n_max && alive; ++jj)
+                for (int s = 0; s < 2 && alive; ++s) {
+                    if (jj < w.n[s]) alive = values(s, jj);
+                    if (alive && jj + 1 < w.n[s]) alive = scores(s, jj + 1);
+                }
+            k_base += w.loads; v_base += w.loads;
+            for (int s = 0; s < 2; ++s) { s_done[s] += w.n[s]; q_used[s] += (w.wide || s == 0) && w.n[s] > 0; }
+            }
+            alive = __shfl_sync(0xffffffffu, alive, 0);
+        }
+    } else {
+        // =========================== softmax ===========================
+        const int side = warp >> 2, quarter = warp & 3;
+        const int L = quarter * 32 + lane;                  // row of the tile = TMEM lane
+        const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
+        const uint32_t t_s = tmem + side * 128u + lane_base, t_o = tmem + 256u + side * 128u + lane_base;
+        const int tl = L / p.G, gl = L - tl * p.G;          // token of the tile and head of the group
+        float2* join = reinterpret_cast<float2*>(smem + kOffJoin);
+        int s_seen = 0, o_seen = 0, joins = 0;              // phases of S_FULL, O_FULL of this side; joined pieces
+        int o_other = 0;                                    // phases of the other side's O_FULL (side 0 waits for it in narrow pieces)
+        bool alive = true;
+        Work w;
+        for (int it = 0; alive && next_piece(w, it, smem, bar0, lane, p.T, ab); ++it) {
+            const ChunkPiece& x = w.x;
+            const int tok0 = w.wide ? side * p.T : 0;                       // first token of this side's rows
+            const int n_tok = min(p.T, x.n_tok - tok0);
+            const bool valid = tl < n_tok;                                  // (L >= T G has tl >= T)
+            const int n = w.n[side];
+            const int step = w.wide ? kTile : 2 * kTile;
+            int key0 = x.tile_begin * kTile + (w.wide ? 0 : side * kTile);  // first key of the tile at hand
+            const int limit = min(x.keys, x.limit0 + tok0 + min(tl, n_tok - 1));   // keys this row sees (<= 0: none)
+            const int limit_min = x.limit0 + tok0;                          // the fewest that a row of the tile sees
+            float m_ref = -INFINITY, l_sum = 0.f;
+            for (int jj = 0; jj < n; ++jj, key0 += step) {
+                alive = __all_sync(0xffffffffu, mbar_wait(bar(S_FULL + side), (s_seen + jj) & 1, ab));
+                if (!alive) break;
+                tc_fence_after();
+                float sv[kTile];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) tmem_ld32(t_s + 32u * c, reinterpret_cast<uint32_t*>(sv) + 32 * c);
+                tmem_wait_ld();
+                if (key0 + kTile > min(limit_min, x.keys)) {                // uniform over the side
+                    const int seen = limit - key0;
+#pragma unroll
+                    for (int c = 0; c < kTile; ++c) if (c >= seen) sv[c] = -INFINITY;
+                }
+                float mx4[4] = {sv[0], sv[1], sv[2], sv[3]};
+#pragma unroll
+                for (int c = 4; c < kTile; c += 8) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) mx4[i] = fmaxf(fmaxf(mx4[i], sv[c + i]), sv[(c + 4 + i) % kTile]);
+                }
+                const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * p.scale_log2;
+                const bool move = mx > m_ref + 8.f || (m_ref == -INFINITY && mx > -INFINITY);
+                const float m_new = move ? mx : m_ref;
+                const float factor = (move && m_ref != -INFINITY) ? ex2(m_ref - m_new) : 1.f;
+                if (jj > 0 && __any_sync(0xffffffffu, valid && factor != 1.f)) {
+                    // S of this tile is complete, so the previous P V is as well: O may be touched
+                    for (int ch = 0; ch < 4; ++ch) {
+                        uint32_t ov[32];
+                        tmem_ld32(t_o + 32u * ch, ov);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) ov[c] = __float_as_uint(__uint_as_float(ov[c]) * factor);
+                        tmem_st32(t_o + 32u * ch, ov);
+                    }
+                }
+                l_sum *= factor;
+                m_ref = m_new;
+                const float neg_m = (m_ref == -INFINITY) ? 0.f : -m_ref;
+                float l4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int ch = 0; ch < 2; ++ch) {
+                    uint32_t pw[32];
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) {
+                        const float e0 = ex2(fmaf(sv[64 * ch + 2 * c], p.scale_log2, neg_m));
+                        const float e1 = ex2(fmaf(sv[64 * ch + 2 * c + 1], p.scale_log2, neg_m));
+                        l4[c & 1] += e0; l4[2 + (c & 1)] += e1;
+                        pw[c] = bf16_pair(e0, e1);
+                    }
+                    tmem_st32(t_s + 32u * ch, pw);
+                }
+                l_sum += (l4[0] + l4[1]) + (l4[2] + l4[3]);
+                tmem_wait_st();
+                tc_fence_before();
+                if (side == 1 && jj == 0 && joins > 0) {
+                    // side 0 has read this side's O of the last joined piece before it is overwritten
+                    alive = __all_sync(0xffffffffu, mbar_wait(bar(JOIN_EMPTY), (joins - 1) & 1, ab));
+                    if (!alive) break;
+                }
+                warp_arrive(bar(P_FULL + side), lane);
+            }
+            if (!alive) break;
+            s_seen += n;
+
+            // ---- the piece's result ----
+            const bool joined = !w.wide && w.n[1] > 0;                      // both sides hold a part of the same rows
+            if (joined && side == 1) {
+                if (joins > 0) {
+                    alive = __all_sync(0xffffffffu, mbar_wait(bar(JOIN_EMPTY), (joins - 1) & 1, ab));
+                    if (!alive) break;
+                }
+                join[L] = make_float2(m_ref, l_sum);
+                ++joins; o_seen += 1;
+                warp_arrive(bar(JOIN_FULL), lane);
+                continue;
+            }
+            if (!w.wide && side == 1) continue;
+            if (n > 0) {
+                alive = __all_sync(0xffffffffu, mbar_wait(bar(O_FULL + side), o_seen & 1, ab));
+                ++o_seen;
+                if (!alive) break;
+            }
+            float f0 = 1.f, f1 = 0.f;                                       // what each side's O counts
+            if (joined) {
+                alive = __all_sync(0xffffffffu, mbar_wait(bar(JOIN_FULL), joins & 1, ab) && mbar_wait(bar(O_FULL + 1), o_other & 1, ab));
+                if (!alive) break;
+                ++joins;
+                const float2 o = join[L];
+                const float m = fmaxf(m_ref, o.x);
+                f0 = m_ref == -INFINITY ? 0.f : ex2(m_ref - m);
+                f1 = o.x == -INFINITY ? 0.f : ex2(o.x - m);
+                l_sum = l_sum * f0 + o.y * f1;
+                m_ref = m;
+            }
+            if (w.n[1] > 0) ++o_other;
+            tc_fence_after();
+            const bool direct = x.parts == 1;
+            const float inv = direct ? (l_sum > 0.f ? 1.f / l_sum : (l_sum == 0.f ? 0.f : l_sum)) : 1.f;
+            f0 *= inv; f1 *= inv;
+            const int rows = n_tok * p.G;                                   // valid rows of this side
+            // partial results of an entry: side 0's pieces, then side 1's
+            const size_t part0 = (size_t)w.kvh * p.head->rows_per_head + x.part_row + (side == 1 ? (size_t)x.parts * p.T * p.G : 0);
+            const size_t part_at = part0 + (size_t)x.part * rows + L;
+            const size_t row_head = (size_t)(x.row0 + tok0 + tl) * p.Hq + w.kvh * p.G + gl;
+            for (int ch = 0; ch < 4; ++ch) {
+                uint32_t ov[32];
+                if (n > 0) { tmem_ld32(t_o + 32u * ch, ov); tmem_wait_ld(); }
+                float o[32];
+#pragma unroll
+                for (int c = 0; c < 32; ++c) o[c] = n > 0 && f0 != 0.f ? __uint_as_float(ov[c]) * f0 : 0.f;
+                if (joined) {
+                    tmem_ld32(t_o + 128u + 32u * ch, ov);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) if (f1 != 0.f) o[c] = fmaf(__uint_as_float(ov[c]), f1, o[c]);
+                }
+                if (valid) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const float v[8] = {o[8 * c], o[8 * c + 1], o[8 * c + 2], o[8 * c + 3], o[8 * c + 4], o[8 * c + 5], o[8 * c + 6], o[8 * c + 7]};
+                        if (direct) store_out(p, row_head, 32 * ch + 8 * c, v);
+                        else {
+                            uint32_t r[8];
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) r[i] = __float_as_uint(v[i]);
+                            st_global_32(p.part_o + part_at * kHeadDim + 32 * ch + 8 * c, r);
+                        }
+                    }
+                }
+            }
+            tc_fence_before();
+            if (joined) warp_arrive(bar(JOIN_EMPTY), lane);
+            if (direct) {
+                if (valid && p.lse) p.lse[row_head] = l_sum == 0.f ? -INFINITY : m_ref * 0.69314718055994530942f + logf(l_sum);
+                continue;
+            }
+            if (valid) p.part_ml[part_at] = make_float2(m_ref, l_sum);
+            // the last piece of the entry to arrive here joins all of them, in their order
+            __threadfence();
+            asm volatile("barrier.cta.sync %0, %1;" ::"r"(1 + side), "n"(kSideThreads) : "memory");
+            if ((tid & (kSideThreads - 1)) == 0) {
+                int* counter = p.arrived + ((size_t)w.kvh * p.head->entries + x.entry) * 2 + side;
+                misc[4 + side] = atomicAdd(counter, 1) == x.parts - 1;
+            }
+            asm volatile("barrier.cta.sync %0, %1;" ::"r"(1 + side), "n"(kSideThreads) : "memory");
+            if (misc[4 + side]) {
+                __threadfence();
+                for (int u = tid & (kSideThreads - 1); u < rows * (kHeadDim / 8); u += kSideThreads) {
+                    const int row = u / (kHeadDim / 8), col = (u % (kHeadDim / 8)) * 8;
+                    float m = -INFINITY, l = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                    for (int k = 0; k < x.parts; ++k) {
+                        const size_t at = part0 + (size_t)k * rows + row;
+                        const float2 ml = __ldcg(p.part_ml + at);
+                        const float4 a = __ldcg(reinterpret_cast<const float4*>(p.part_o + at * kHeadDim + col));
+                        const float4 b = __ldcg(reinterpret_cast<const float4*>(p.part_o + at * kHeadDim + col) + 1);
+                        if (ml.x == -INFINITY) continue;                    // that piece holds no key this row sees
+                        const float m_new = fmaxf(m, ml.x), fa = m == -INFINITY ? 0.f : ex2(m - m_new), fb = ex2(ml.x - m_new);
+                        const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) acc[i] = acc[i] * fa + v[i] * fb;
+                        l = l * fa + ml.y * fb;
+                        m = m_new;
+                    }
+                    const float scale = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) acc[i] *= scale;
+                    const int t = row / p.G;
+                    const size_t to = (size_t)(x.row0 + tok0 + t) * p.Hq + w.kvh * p.G + (row - t * p.G);
+                    store_out(p, to, col, acc);
+                    if (col == 0 && p.lse) p.lse[to] = l == 0.f ? -INFINITY : m * 0.69314718055994530942f + logf(l);
+                }
+            }
+            asm volatile("barrier.cta.sync %0, %1;" ::"r"(1 + side), "n"(kSideThreads) : "memory");   // the flag is free again
+        }
+    }
+
+    // ---- everyone arrives here, normally or after an abort ----
+    tc_fence_before();
+    __syncthreads();
+    if (warp == kMmaWarp) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+    }
+}
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiledFn encode_fn() {
+    static EncodeTiledFn fn = [] {
+        void* sym = nullptr;
+        cudaDriverEntryPointQueryResult res;
+        return cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &sym, cudaEnableDefault, &res) == cudaSuccess && res == cudaDriverEntryPointSuccess
+                   ? reinterpret_cast<EncodeTiledFn>(sym) : nullptr;
+    }();
+    return fn;
+}
+
+bool encode(CUtensorMap* map, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
+    const cuuint32_t ones[5] = {1, 1, 1, 1, 1};
+    const EncodeTiledFn fn = encode_fn();
+    return fn && fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                    CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace
+
+cudaError_t launch_chunk_attn(const ChunkParams& p, const void* q, long q_stride, const void* k_pages, const void* v_pages, cudaStream_t st) {
+    CUtensorMap tm_q, tm_k, tm_v;
+    {
+        // queries: (dim, head, row); a box is half the dims of G heads of T rows
+        const cuuint64_t dims[3] = {(cuuint64_t)kHeadDim, (cuuint64_t)p.Hq, (cuuint64_t)p.total_rows};
+        const cuuint64_t strides[2] = {kHeadDim * 2, (cuuint64_t)q_stride * 2};
+        const cuuint32_t box[3] = {64, (cuuint32_t)p.G, (cuuint32_t)p.T};
+        if (!encode(&tm_q, q, 3, dims, strides, box)) return cudaErrorInvalidValue;
+    }
+    {
+        // pages: (64 dims, 8 tokens, dim half, token half, page-head); a box is one page of one head, laid out
+        // [token half][dim half][8 tokens][128 bytes], so that a tile's pages form one MMA operand
+        const cuuint64_t dims[5] = {64, 8, 2, 2, (cuuint64_t)p.num_pages * p.Hkv};
+        const cuuint64_t strides[4] = {256, 128, 2048, 4096};
+        const cuuint32_t box[5] = {64, 8, 2, 2, 1};
+        if (!encode(&tm_k, k_pages, 5, dims, strides, box) || !encode(&tm_v, v_pages, 5, dims, strides, box)) return cudaErrorInvalidValue;
+    }
+    const cudaError_t e = cudaFuncSetAttribute(chunk_attn_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+    if (e != cudaSuccess) return e;
+    return launch_dependent(chunk_attn_kernel, p.grid, kThreadsChunk, kSmemBytes, st, p, tm_q, tm_k, tm_v);
+}
+
+}  // namespace tts

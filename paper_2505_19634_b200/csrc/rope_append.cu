@@ -1,0 +1,181 @@
+// Rotary positions on the way into the cache: the queries and keys of ragged chunks of new tokens are
+// rotated, the keys and values go to their page slots, the rotated queries to a dense array.
+//
+//   pair i of a head vector x is turned by angle a = positions[axis[i]][row] * inv_freq[i]:
+//       (x_lo, x_hi) -> (x_lo cos a - x_hi sin a, x_lo sin a + x_hi cos a)
+//
+// The angle is formed in 64 bits as a number of whole turns, of which only the fraction is kept: far
+// positions (2^20 and more) lose their phase in 32 bits.  Sine and cosine of the fraction and the rotation
+// itself are fp32, with one rounding to bf16 at the end.
+//
+// Bound by HBM: q, k and v are read once, q, K and V written once; there is no reuse between rows.  Eight
+// lanes handle one head vector, each two 16-byte chunks that hold both members of its pairs, so a rotation
+// needs no exchange between lanes; a lane's eight sines and cosines serve all heads of the row that its
+// warp walks through, four heads at a time.
+#include "launch.cuh"
+#include "tts_internal.cuh"
+
+namespace tts {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWarps = kThreads / 32;
+
+// The branch whose rows [row_start[b], row_start[b+1]) hold `row`, or -1: the whole warp looks at 32 starts
+// per step (two steps for up to 1024 branches).
+__device__ __forceinline__ int branch_of_row(const int32_t* row_start, int n, int row, int lane) {
+    int lo = 0;
+    if (n > 32) {                                       // 32 blocks of 32 starts
+        const int at = lane * 32;
+        lo = (__popc(__ballot_sync(0xffffffffu, at < n && row_start[at] <= row)) - 1) * 32;
+        if (lo < 0) return -1;
+    }
+    const int at = lo + lane;
+    const int b = lo + __popc(__ballot_sync(0xffffffffu, at < n && row_start[at] <= row)) - 1;
+    return b < lo || row >= row_start[b + 1] ? -1 : b;
+}
+
+__device__ __forceinline__ void unpack(const uint4& v, float (&x)[8]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+}
+__device__ __forceinline__ uint4 pack(const float (&x)[8]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+        w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// kMode 0: all 64 pairs, pair i = dims (i, i + 64); 1: neighbours (2i, 2i+1), any number of pairs; 2: pair i =
+// dims (i, i + n_pairs) with fewer than 64 pairs (partners fetched one by one).
+// A warp takes one row and every parts-th group of four head vectors of it; with few rows several warps share
+// a row, so that small calls still fill the GPU.
+template <int kMode>
+__global__ void __launch_bounds__(kThreads)
+append_rope_kernel(const __grid_constant__ RopeParams p) {
+    __shared__ double turns[kHeadDim / 2];              // inv_freq / (2 pi)
+    __shared__ int axis_of[kHeadDim / 2];
+    for (int i = threadIdx.x; i < kHeadDim / 2; i += kThreads) {
+        turns[i] = i < p.n_pairs ? p.turns[i] : 0.0;
+        axis_of[i] = i < p.n_pairs ? p.axis[i] : 0;
+    }
+    __syncthreads();
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int lane = threadIdx.x & 31, sub = lane & 7, group = lane >> 3;
+    const int vectors = p.Hq + 2 * p.Hkv;
+    for (long w = blockIdx.x * (long)kWarps + (threadIdx.x >> 5); w < (long)p.total_rows * p.parts; w += (long)gridDim.x * kWarps) {
+        const int row = (int)(w / p.parts), part = (int)(w - (long)row * p.parts);
+        const int b = branch_of_row(p.row_start, p.n_branches, row, lane);
+        if (b < 0) continue;                            // a row of no branch: left as it is
+        // where the row's key and value go
+        const int start = p.row_start[b], c = p.row_start[b + 1] - start, L = p.branch_lens[b];
+        const long tok = (long)p.prefix_len + L - c + (row - start);
+        int page = -1;
+        if (L >= c && tok < (long)p.max_blocks * kPage) page = p.block_table[(size_t)b * p.max_blocks + tok / kPage];
+        const bool store_kv = page >= 0 && page < p.num_pages;
+        if (!store_kv && lane == 0) atomicMin(p.status, (int)TTS_ERR_DEVICE_BOUNDS);
+
+        // mode 0 and 2: chunk sub holds the low members of pairs 8 sub .. 8 sub + 7 (mode 2: where there are
+        // such pairs); mode 1: chunk sub holds pairs 4 sub .. + 3 and chunk sub + 8 pairs 32 + 4 sub .. + 3
+        float cs[8], sn[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int pair = kMode == 1 ? (i < 4 ? 4 * sub + i : 32 + 4 * sub + i - 4) : 8 * sub + i;
+            double t = (double)p.positions[(size_t)axis_of[pair] * p.total_rows + row] * turns[pair];
+            t -= rint(t);
+            sincospif(2.f * (float)t, &sn[i], &cs[i]);
+        }
+        for (int h0 = part * 4; h0 < vectors; h0 += p.parts * 4) {
+            const int h = h0 + group;
+            const bool live = h < vectors;
+            const bool is_q = h < p.Hq, is_v = h >= p.Hq + p.Hkv;
+            const int hk = is_q ? 0 : is_v ? h - p.Hq - p.Hkv : h - p.Hq;
+            const __nv_bfloat16* src = is_q ? p.q + (size_t)row * p.q_stride + (size_t)h * kHeadDim
+                                            : (is_v ? p.v : p.k) + (size_t)row * p.kv_stride + (size_t)hk * kHeadDim;
+            uint4 lo4 = make_uint4(0, 0, 0, 0), hi4 = lo4;
+            if (live) { lo4 = reinterpret_cast<const uint4*>(src)[sub]; hi4 = reinterpret_cast<const uint4*>(src)[sub + 8]; }
+            if (kMode == 2) {
+                // this lane writes the same two chunks; each dim's partner is n_pairs away
+                float lo[8], hi[8];
+                unpack(lo4, lo); unpack(hi4, hi);
+                if (live && !is_v) {
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        float(&x)[8] = half ? hi : lo;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const int dim = 8 * (sub + 8 * half) + i;
+                            if (dim >= 2 * p.n_pairs) continue;
+                            const bool low = dim < p.n_pairs;
+                            const int pair = low ? dim : dim - p.n_pairs;
+                            const float other = __bfloat162float(src[low ? dim + p.n_pairs : pair]);
+                            float s = sn[i], co = cs[i];
+                            if (pair != 8 * sub + i) {          // not one of this lane's own angles
+                                double t = (double)p.positions[(size_t)axis_of[pair] * p.total_rows + row] * turns[pair];
+                                t -= rint(t);
+                                sincospif(2.f * (float)t, &s, &co);
+                            }
+                            x[i] = low ? x[i] * co - other * s : other * s + x[i] * co;
+                        }
+                    }
+                }
+                lo4 = pack(lo); hi4 = pack(hi);
+                __syncwarp();                           // the partners have been read before anything is written in place
+            } else if (!is_v) {
+                float lo[8], hi[8];
+                unpack(lo4, lo); unpack(hi4, hi);
+                if (kMode == 0) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float a = lo[i], z = hi[i];
+                        lo[i] = a * cs[i] - z * sn[i];
+                        hi[i] = a * sn[i] + z * cs[i];
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float a = lo[2 * i], z = lo[2 * i + 1], d = hi[2 * i], e = hi[2 * i + 1];
+                        if (4 * sub + i < p.n_pairs) {
+                            lo[2 * i] = a * cs[i] - z * sn[i];
+                            lo[2 * i + 1] = a * sn[i] + z * cs[i];
+                        }
+                        if (32 + 4 * sub + i < p.n_pairs) {
+                            hi[2 * i] = d * cs[4 + i] - e * sn[4 + i];
+                            hi[2 * i + 1] = d * sn[4 + i] + e * cs[4 + i];
+                        }
+                    }
+                }
+                lo4 = pack(lo); hi4 = pack(hi);
+            }
+            if (!live || (!is_q && !store_kv)) continue;
+            uint4* dst = is_q ? reinterpret_cast<uint4*>(p.q_out + ((size_t)row * p.Hq + h) * kHeadDim)
+                              : reinterpret_cast<uint4*>((is_v ? p.v_pages : p.k_pages) +
+                                                         ((((size_t)page * p.Hkv + hk) * kPage + (size_t)(tok % kPage)) * kHeadDim));
+            dst[sub] = lo4; dst[sub + 8] = hi4;
+        }
+    }
+}
+
+}  // namespace
+
+cudaError_t launch_append_rope(RopeParams p, int n_sms, cudaStream_t st) {
+    // rows x parts warps; parts grows until the GPU's 64 warps per SM have work or a warp has one group of heads
+    const int groups = ceil_div(p.Hq + 2 * p.Hkv, 4);
+    p.parts = 1;
+    while (p.parts < groups && (long)p.total_rows * p.parts * 2 <= 64l * n_sms) p.parts *= 2;
+    if (p.parts > groups) p.parts = groups;
+    const long warps = (long)p.total_rows * p.parts;
+    const long blocks = (warps + kWarps - 1) / kWarps;
+    const int grid = (int)(blocks < 16l * n_sms ? blocks : 16l * n_sms);
+    if (p.interleaved) return launch_dependent(append_rope_kernel<1>, grid, kThreads, 0, st, p);
+    if (p.n_pairs == kHeadDim / 2) return launch_dependent(append_rope_kernel<0>, grid, kThreads, 0, st, p);
+    return launch_dependent(append_rope_kernel<2>, grid, kThreads, 0, st, p);
+}
+
+}  // namespace tts

@@ -305,8 +305,10 @@ int tts_create(const tts_config* cfg, tts_ctx** out) {
     if (e == cudaSuccess) e = cudaMalloc(&c->d_status, sizeof(int32_t));
     if (e == cudaSuccess) e = cudaMemset(c->d_status, 0, sizeof(int32_t));
     if (e == cudaSuccess) e = alloc_workspace(c);
+    if (e == cudaSuccess) e = cache_alloc(c);
     if (e != cudaSuccess) {
         free_workspace(c);
+        cache_release(c);
         cudaFree(c->d_status);
         delete c;
         return TTS_ERR_CUDA;
@@ -319,6 +321,7 @@ int tts_destroy(tts_ctx* ctx) {
     Ctx* c = reinterpret_cast<Ctx*>(ctx);
     if (!c) return TTS_ERR_INVALID;
     free_workspace(c);
+    cache_release(c);
     cudaFree(c->d_status);
     cudaFree(c->stage);
     if (c->host_ev) {
@@ -647,6 +650,7 @@ const char* tts_strerror(int status) {
         case TTS_ERR_DEVICE_BOUNDS: return "device-side bounds check failed";
         case TTS_ERR_DEVICE_TIMEOUT: return "device-side wait timed out";
         case TTS_ERR_SCRATCH: return "problem exceeds the fixed scratch array of the no-allocation entry point";
+        case TTS_ERR_DEVICE_PAGES: return "not enough free pages in the pool";
         default: return "unknown status";
     }
 }

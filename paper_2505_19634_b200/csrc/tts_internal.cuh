@@ -294,6 +294,12 @@ struct Ctx {
     cudaStream_t h2d_stream, d2h_stream;   // copies of the host entry point that overlap the kernels (created on first use)
     cudaEvent_t* host_ev;                  // kHostEvents events ordering them against the context's stream
     void* tmap_cache;                  // opaque: tensor maps keyed by pool pointer
+    // cache operators
+    int32_t* page_work;                // PageWork (kv_pages.cu)
+    struct ChunkHead* chunk_head; struct ChunkPiece* chunk_pieces; int2* chunk_entries; int* chunk_arrived;   // chunk attention,
+    float* chunk_part_o; float2* chunk_part_ml;                                                               // from tts_chunk_reserve on
+    int chunk_rows, chunk_max_entries, chunk_max_pieces;
+    long chunk_part_rows;
     // profiling aid
     int profiling, prof_n;
     cudaEvent_t* prof_ev;              // 3 events per recorded call
@@ -321,6 +327,42 @@ cudaError_t launch_kv_append(const void* k_new, const void* v_new, void* k_pages
                              const int32_t* branch_lens, int N, int R, int Hkv, int32_t* status, cudaStream_t st);
 cudaError_t launch_kv_rollback(int32_t* branch_lens, const int32_t* accepted_len, int N, int gamma, int32_t* status,
                                cudaStream_t st);
+// cache operators (kv_pages.cu, rope_append.cu, cache_api.cu)
+constexpr int kMaxLayers = 128;
+struct PagePools { void* p[2 * kMaxLayers]; int n_layers; };       // K and V pools of the layers, in any order
+struct PageWork {
+    int32_t* head;          // [0] pages to copy, [1] the plan stands
+    int4* child;            // [max_branches] (parent, entries kept, fresh page or -1, length)
+    int32_t* childless;     // [max_branches]
+    int32_t* list_src;      // [num_pages]
+    int32_t* list_dst;      // [num_pages]
+};
+struct RopeParams {
+    const __nv_bfloat16 *q, *k, *v;
+    long q_stride, kv_stride;          // elements from row to row
+    const int32_t* positions;          // [n_axes][total_rows]
+    __nv_bfloat16 *q_out, *k_pages, *v_pages;
+    const int32_t *block_table, *branch_lens, *row_start;
+    int32_t* status;
+    int Hq, Hkv, n_pairs, interleaved, prefix_len, n_branches, total_rows, max_blocks, num_pages, parts;
+    unsigned char axis[kHeadDim / 2];
+    double turns[kHeadDim / 2];        // inv_freq / (2 pi)
+};
+cudaError_t launch_copy_pages(const PagePools& pools, const int32_t* src, const int32_t* dst, int n, int Hkv, int num_pages, int n_sms,
+                              int32_t* status, cudaStream_t st);
+cudaError_t launch_fork(const PagePools& pools, const int32_t* table, int max_blocks, int prefix_len, const int32_t* lens, int n_branches,
+                        const int32_t* parents, int n_children, const int32_t* refs, int32_t* new_table, int32_t* new_lens, int32_t* new_refs,
+                        int Hkv, int num_pages, int n_sms, const PageWork& wk, int32_t* status, cudaStream_t st);
+cudaError_t launch_grow(int32_t* table, int max_blocks, int prefix_len, int32_t* lens, const int32_t* n_new, int n_branches, int32_t* refs,
+                        int num_pages, const PageWork& wk, int32_t* status, cudaStream_t st);
+cudaError_t launch_free(int32_t* table, int max_blocks, int32_t* lens, const int32_t* freed, int n_branches, int32_t* refs, int num_pages,
+                        int32_t* status, cudaStream_t st);
+cudaError_t launch_compact(const PagePools& pools, const int32_t* table, int max_blocks, int n_branches, const int32_t* refs, int32_t* new_table,
+                           int32_t* new_refs, int32_t* page_map, int32_t* n_used, int Hkv, int num_pages, int n_sms, const PageWork& wk,
+                           int32_t* status, cudaStream_t st);
+cudaError_t launch_append_rope(RopeParams p, int n_sms, cudaStream_t st);
+cudaError_t cache_alloc(Ctx* c);       // page_work
+void cache_release(Ctx* c);
 cudaError_t launch_wait_probe(int32_t* status, long long limit_ns, int* gave_up, cudaStream_t st);
 int simt_rb_rows(int nr);
 constexpr int kSimtTileTokens = 64;
