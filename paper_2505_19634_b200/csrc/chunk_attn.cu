@@ -30,6 +30,8 @@
 // shared memory, whatever the page holds there.  All waits are bounded (umma_ptx.cuh).
 #include <cuda.h>
 
+#include <type_traits>
+
 #include "chunk_attn.cuh"
 #include "launch.cuh"
 #include "umma_ptx.cuh"
@@ -48,7 +50,14 @@ constexpr int kTakeWarp = 8, kKWarp = 9, kVWarp = 10, kMmaWarp = 11;
 constexpr int kHalfBytes = kRows * 128;
 constexpr int kOperandBytes = 2 * kHalfBytes;
 constexpr int kRingK = 3, kRingV = 2, kRingPiece = 2;
+#ifndef POLY
+#define POLY 0
+#endif
+constexpr int kPolyEvery = POLY, kPolyOf = 8;
 constexpr uint32_t kTmemCols = 512;
+// registers per thread: at launch, and after the softmax warpgroups have taken from the third one
+constexpr int kLaunchRegs = 168, kSoftmaxRegs = 224, kHelperRegs = 56;
+static_assert(2 * kSoftmaxRegs + kHelperRegs <= 3 * kLaunchRegs, "the split draws on what the block was launched with");
 
 constexpr int kOffQ = 0;                                       // two row tiles
 constexpr int kOffK = kOffQ + 2 * kOperandBytes;
@@ -56,7 +65,7 @@ constexpr int kOffV = kOffK + kRingK * kOperandBytes;
 constexpr int kOffBar = kOffV + kRingV * kOperandBytes;
 enum Bar {
     K_FULL = 0, K_EMPTY = K_FULL + kRingK, V_FULL = K_EMPTY + kRingK, V_EMPTY = V_FULL + kRingV, V_TAIL = V_EMPTY + kRingV,
-    Q_FULL, Q_EMPTY = Q_FULL + 2, S_FULL = Q_EMPTY + 2, P_FULL = S_FULL + 2, O_FULL = P_FULL + 2, PIECE_FULL = O_FULL + 2,
+    Q_FULL, Q_EMPTY = Q_FULL + 2, S_FULL = Q_EMPTY + 2, P_HALF = S_FULL + 2, P_FULL = P_HALF + 2, O_FULL = P_FULL + 2, PIECE_FULL = O_FULL + 2,
     PIECE_EMPTY = PIECE_FULL + kRingPiece, JOIN_FULL = PIECE_EMPTY + kRingPiece, JOIN_EMPTY, kNumBars
 };
 constexpr int kOffMisc = kOffBar + ((kNumBars * 8 + 15) & ~15);   // [0] abort, [1] TMEM base, [2, 3] scratch, [4, 5] last-piece flags
@@ -65,6 +74,12 @@ constexpr int kPieceBytes = 64;
 constexpr int kOffJoin = kOffPiece + kRingPiece * kPieceBytes; // side 1's (m, l) of a narrow piece
 constexpr int kSmemBytes = kOffJoin + kRows * 8 + 1024;
 static_assert(kSmemBytes <= 227 * 1024, "shared memory");
+
+__device__ __forceinline__ bool elect_one() {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok));
+    return ok != 0;
+}
 
 __device__ __forceinline__ void warp_arrive(uint32_t bar, int lane) {
     __syncwarp();
@@ -76,7 +91,7 @@ struct Work {
     ChunkPiece x;
     int kvh;
     bool wide;
-    int n[2];        // KV tiles of each side
+    int n0, n1;      // KV tiles of each side
     int loads;       // KV tiles to load
 };
 
@@ -87,11 +102,11 @@ __device__ __forceinline__ void derive(Work& w, int T) {
     if (w.wide) {
         // side 0 stops at the tile of its last token's last key
         const int limit = min(x.keys, max(0, x.limit0 + T - 1));
-        w.n[0] = max(0, min(x.tile_end, ceil_div(limit, kTile)) - x.tile_begin);
-        w.n[1] = tiles;
+        w.n0 = max(0, min(x.tile_end, ceil_div(limit, kTile)) - x.tile_begin);
+        w.n1 = tiles;
     } else {
-        w.n[0] = (tiles + 1) >> 1;
-        w.n[1] = tiles >> 1;
+        w.n0 = (tiles + 1) >> 1;
+        w.n1 = tiles >> 1;
     }
     w.loads = tiles;
 }
@@ -128,6 +143,13 @@ __device__ __forceinline__ void st_global_32(void* p, const uint32_t (&r)[8]) {
                  ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
 }
 
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+          "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+
 __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&h);
@@ -144,6 +166,37 @@ __device__ __forceinline__ void store_out(const ChunkParams& p, size_t row_head,
         *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + row_head * kHeadDim + col) =
             make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
     }
+}
+
+// two fp32 values in a 64-bit register pair: Blackwell's packed fma and add
+__device__ __forceinline__ uint64_t pack2(float a, float b) { uint64_t r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ float2 unpack2(uint64_t v) { float2 r; asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v)); return r; }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) { uint64_t r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) { uint64_t r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ float max3(float a, float b, float c) { float r; asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
+__device__ __forceinline__ uint32_t bf16_pair2(uint64_t v) { const float2 f = unpack2(v); return bf16_pair(f.x, f.y); }
+
+__device__ __forceinline__ uint64_t exp2_sfu2(uint64_t y) {
+    const float2 f = unpack2(y);
+    return pack2(ex2(f.x), ex2(f.y));
+}
+// 2^y for two y <= 8 on the FMA pipe: y = n + f with |f| <= 1/2 (adding 1.5 x 2^23 leaves n in the low bits), a
+// polynomial of degree 4 fitted to 2^f for the smallest largest relative error (2.6e-6, far below the rounding
+// of P to bf16), and n added to the exponent.  Below -126 the result is 2^-126, not 0: the caller uses it only
+// where no key is masked, and such a weight is lost in the sum either way.
+__device__ __forceinline__ uint64_t exp2_poly2(uint64_t y) {
+    float2 v = unpack2(y);
+    v.x = fmaxf(v.x, -126.f); v.y = fmaxf(v.y, -126.f);
+    y = pack2(v.x, v.y);
+    const uint64_t magic = pack2(12582912.f, 12582912.f), back = pack2(-12582912.f, -12582912.f), minus1 = pack2(-1.f, -1.f);
+    const uint64_t t = add2(y, magic);
+    const uint64_t f = fma2(add2(t, back), minus1, y);
+    uint64_t q = fma2(f, pack2(0.009570101911165427f, 0.009570101911165427f), pack2(0.055917860319388245f, 0.055917860319388245f));
+    q = fma2(q, f, pack2(0.2402474482786378f, 0.2402474482786378f));
+    q = fma2(q, f, pack2(0.6931218147366892f, 0.6931218147366892f));
+    q = fma2(q, f, pack2(0.9999992614457122f, 0.9999992614457122f));
+    const float2 n = unpack2(t), r = unpack2(q);
+    return pack2(__uint_as_float(__float_as_uint(r.x) + (__float_as_uint(n.x) << 23)), __uint_as_float(__float_as_uint(r.y) + (__float_as_uint(n.y) << 23)));
 }
 
 __global__ void __launch_bounds__(kThreadsChunk, 1)
@@ -165,7 +218,7 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
         mbar_init(bar(V_TAIL), 1);
         for (int i = 0; i < 2; ++i) {
             mbar_init(bar(Q_FULL + i), 1); mbar_init(bar(Q_EMPTY + i), 1); mbar_init(bar(S_FULL + i), 1);
-            mbar_init(bar(P_FULL + i), kSideThreads / 32); mbar_init(bar(O_FULL + i), 1);
+            mbar_init(bar(P_HALF + i), kSideThreads / 32); mbar_init(bar(P_FULL + i), kSideThreads / 32); mbar_init(bar(O_FULL + i), 1);
         }
         for (int i = 0; i < kRingPiece; ++i) { mbar_init(bar(PIECE_FULL + i), 1); mbar_init(bar(PIECE_EMPTY + i), 11); }   // all warps but the taker
         mbar_init(bar(JOIN_FULL), kSideThreads / 32); mbar_init(bar(JOIN_EMPTY), kSideThreads / 32);
@@ -182,6 +235,8 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
     grid_dependency_wait();
     grid_launch_dependents();
 
+    if (warp >= 2 * kSideThreads / 32) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kHelperRegs));
     if (warp == kTakeWarp) {
         // =========================== takes pieces, loads Q ===========================
         if (lane == 0) {
@@ -209,7 +264,7 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                 index = atomicAdd(&p.head->next, 1);
                 derive(w, p.T);
                 for (int s = 0; s < (w.wide ? 2 : 1) && alive; ++s) {
-                    if (w.n[s] == 0) continue;
+                    if ((s ? w.n1 : w.n0) == 0) continue;
                     alive = mbar_wait(bar(Q_EMPTY + s), (used[s] & 1) ^ 1, ab);
                     if (!alive) break;
                     ++used[s];
@@ -294,60 +349,82 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                 mbar_wait(bar(full0 + i % ring_n), (i / ring_n) & 1, quiet);
             }
         }
-    } else if (warp == kMmaWarp) {
+    } else {
         // =========================== MMA issuer ===========================
         constexpr uint32_t idesc_qk = instr_desc(kRows, kTile, false, false), idesc_pv = instr_desc(kRows, kHeadDim, false, true);
-        int k_base = 0, v_base = 0, q_used[2] = {0, 0}, s_done[2] = {0, 0};
+        // The whole warp walks the loop and waits, so that addresses and descriptors stay in uniform registers; one
+        // elected lane issues.  (A single lane that does everything spends more time preparing operands than the
+        // tensor pipe needs for them: 4500 instead of 2900 clocks for a KV tile of both sides.)
+        const bool leader = elect_one();
+        const uint64_t q_desc = smem_desc(sbase + kOffQ, 16, 1024), k_desc = smem_desc(sbase + kOffK, 16, 2048), v_desc = smem_desc(sbase + kOffV, 1024, 2048);
+        int k_slot = 0, k_round = 0, v_slot = 0, v_round = 0, q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
         bool alive = true;
         Work w;
         for (int it = 0; alive && next_piece(w, it, smem, bar0, lane, p.T, ab); ++it) {
-            if (lane == 0) {
-            const int n_max = max(w.n[0], w.n[1]);
-            // S of side s, its jj-th tile
-            auto scores = [&](int s, int jj) -> bool {
-                const int kt = k_base + (w.wide ? jj : 2 * jj + s), slot = kt % kRingK;
-                const int q = w.wide ? s : 0;
-                if (jj == 0 && (w.wide || s == 0) && !mbar_wait(bar(Q_FULL + q), q_used[q] & 1, ab)) return false;
-                if (!mbar_wait(bar(K_FULL + slot), (kt / kRingK) & 1, ab)) return false;
+            const bool wide = w.wide;
+            const int n0 = w.n0, n1 = w.n1, n_max = max(n0, n1);
+            // S of side `s`, its jj-th tile
+            auto scores = [&](auto side, int jj) {
+                constexpr int s = decltype(side)::value;
+                const int n = s ? n1 : n0;
+                const bool own_q = wide || s == 0;                       // a narrow piece has one Q tile for both sides
+                if (jj == 0 && own_q) { alive = mbar_wait(bar(Q_FULL + s), q_phase[s], ab); q_phase[s] ^= 1; }
+                alive = alive && mbar_wait(bar(K_FULL + k_slot), k_round, ab);
+                if (!__all_sync(0xffffffffu, alive)) { alive = false; return; }
                 tc_fence_after();
-                const uint32_t qa = sbase + kOffQ + q * kOperandBytes, ka = sbase + kOffK + slot * kOperandBytes;
+                // descriptors hold addresses in units of 16 bytes; Q: two 64-dim blocks of 128 rows, K: dim halves 1 KiB apart inside a page
+                const uint64_t qd = q_desc + (own_q ? s * kOperandBytes / 16 : 0), kd = k_desc + (uint32_t)(k_slot * (kOperandBytes / 16));
+                const bool last_k = s == 1 || !wide;                     // the last reader of a K or V tile, and of a Q tile, gives it back
+                const bool last_q = wide ? jj + 1 == n : 2 * jj + s + 1 == w.loads;
+                if (leader) {
 #pragma unroll
-                for (int ks = 0; ks < 8; ++ks)
-                    umma_bf16(tmem + s * 128u, smem_desc(qa + (ks >> 2) * kHalfBytes + (ks & 3) * 32, 16, 1024),
-                              smem_desc(ka + (ks >> 2) * 1024 + (ks & 3) * 32, 16, 2048), idesc_qk, ks > 0);
-                umma_commit(bar(S_FULL + s));
-                if (!w.wide || s == 1) umma_commit(bar(K_EMPTY + slot));
-                // the last reader of a Q tile gives it back
-                if (w.wide ? jj + 1 == w.n[s] : 2 * jj + s + 1 == w.loads) umma_commit(bar(Q_EMPTY + q));
-                return true;
-            };
-            auto values = [&](int s, int jj) -> bool {
-                const int vt = v_base + (w.wide ? jj : 2 * jj + s), slot = vt % kRingV;
-                if (!mbar_wait(bar(P_FULL + s), (s_done[s] + jj) & 1, ab) || !mbar_wait(bar(V_FULL + slot), (vt / kRingV) & 1, ab)) return false;
-                tc_fence_after();
-                const uint32_t va = sbase + kOffV + slot * kOperandBytes;
-#pragma unroll
-                for (int ks = 0; ks < 8; ++ks)
-                    umma_bf16_tmem_a(tmem + 256u + s * 128u, tmem + s * 128u + ks * 8u, smem_desc(va + ks * 4096, 1024, 2048), idesc_pv,
-                                     (jj > 0 || ks > 0) ? 1u : 0u);
-                if (!w.wide || s == 1) umma_commit(bar(V_EMPTY + slot));
-                if (jj + 1 == w.n[s]) umma_commit(bar(O_FULL + s));
-                return true;
-            };
-            for (int s = 0; s < 2 && alive; ++s)
-                if (w.n[s] > 0) alive = scores(s, 0);
-            for (int jj = 0; jj < n_max && alive; ++jj)
-                for (int s = 0; s < 2 && alive; ++s) {
-                    if (jj < w.n[s]) alive = values(s, jj);
-                    if (alive && jj + 1 < w.n[s]) alive = scores(s, jj + 1);
+                    for (int ks = 0; ks < 8; ++ks)
+                        umma_bf16(tmem + s * 128u, qd + ((ks >> 2) * kHalfBytes + (ks & 3) * 32) / 16, kd + ((ks >> 2) * 1024 + (ks & 3) * 32) / 16, idesc_qk, ks > 0);
+                    umma_commit(bar(S_FULL + s));
+                    if (last_k) umma_commit(bar(K_EMPTY + k_slot));
+                    if (last_q) umma_commit(bar(Q_EMPTY + (own_q ? s : 0)));
                 }
-            k_base += w.loads; v_base += w.loads;
-            for (int s = 0; s < 2; ++s) { s_done[s] += w.n[s]; q_used[s] += (w.wide || s == 0) && w.n[s] > 0; }
+                __syncwarp();
+                if (last_k && ++k_slot == kRingK) { k_slot = 0; k_round ^= 1; }
+            };
+            auto values = [&](auto side, int jj) {
+                constexpr int s = decltype(side)::value;
+                const bool last_v = s == 1 || !wide, last = jj + 1 == (s ? n1 : n0);
+                alive = mbar_wait(bar(V_FULL + v_slot), v_round, ab);
+                const uint64_t vd = v_desc + (uint32_t)(v_slot * (kOperandBytes / 16));       // one page (16 tokens) per step
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {       // the first 64 keys' probabilities are there before the others
+                    alive = alive && mbar_wait(bar((half ? P_FULL : P_HALF) + s), p_phase[s], ab);
+                    if (!__all_sync(0xffffffffu, alive)) { alive = false; return; }
+                    tc_fence_after();
+                    if (leader) {
+#pragma unroll
+                        for (int ks = 4 * half; ks < 4 * half + 4; ++ks)
+                            umma_bf16_tmem_a(tmem + 256u + s * 128u, tmem + s * 128u + ks * 8u, vd + ks * 4096 / 16, idesc_pv, (jj > 0 || ks > 0) ? 1u : 0u);
+                        if (half) {
+                            if (last_v) umma_commit(bar(V_EMPTY + v_slot));
+                            if (last) umma_commit(bar(O_FULL + s));
+                        }
+                    }
+                    __syncwarp();
+                }
+                p_phase[s] ^= 1;
+                if (last_v && ++v_slot == kRingV) { v_slot = 0; v_round ^= 1; }
+            };
+            const std::integral_constant<int, 0> side0;
+            const std::integral_constant<int, 1> side1;
+#pragma unroll 1
+            for (int jj = -1; jj < n_max && alive; ++jj) {
+                if (jj >= 0 && jj < n0) values(side0, jj);
+                if (alive && jj + 1 < n0) scores(side0, jj + 1);
+                if (alive && jj >= 0 && jj < n1) values(side1, jj);
+                if (alive && jj + 1 < n1) scores(side1, jj + 1);
             }
-            alive = __shfl_sync(0xffffffffu, alive, 0);
         }
+    }
     } else {
         // =========================== softmax ===========================
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
         const int side = warp >> 2, quarter = warp & 3;
         const int L = quarter * 32 + lane;                  // row of the tile = TMEM lane
         const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
@@ -363,7 +440,7 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
             const int tok0 = w.wide ? side * p.T : 0;                       // first token of this side's rows
             const int n_tok = min(p.T, x.n_tok - tok0);
             const bool valid = tl < n_tok;                                  // (L >= T G has tl >= T)
-            const int n = w.n[side];
+            const int n = side ? w.n1 : w.n0;
             const int step = w.wide ? kTile : 2 * kTile;
             int key0 = x.tile_begin * kTile + (w.wide ? 0 : side * kTile);  // first key of the tile at hand
             const int limit = min(x.keys, x.limit0 + tok0 + min(tl, n_tok - 1));   // keys this row sees (<= 0: none)
@@ -377,63 +454,73 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
 #pragma unroll
                 for (int c = 0; c < 4; ++c) tmem_ld32(t_s + 32u * c, reinterpret_cast<uint32_t*>(sv) + 32 * c);
                 tmem_wait_ld();
-                if (key0 + kTile > min(limit_min, x.keys)) {                // uniform over the side
+                const bool masked = key0 + kTile > min(limit_min, x.keys);  // uniform over the side
+                if (masked) {
                     const int seen = limit - key0;
 #pragma unroll
                     for (int c = 0; c < kTile; ++c) if (c >= seen) sv[c] = -INFINITY;
                 }
                 float mx4[4] = {sv[0], sv[1], sv[2], sv[3]};
 #pragma unroll
-                for (int c = 4; c < kTile; c += 8) {
+                for (int c = 4; c + 8 <= kTile; c += 8)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) mx4[i] = fmaxf(fmaxf(mx4[i], sv[c + i]), sv[(c + 4 + i) % kTile]);
-                }
+                    for (int i = 0; i < 4; ++i) mx4[i] = max3(mx4[i], sv[c + i], sv[c + 4 + i]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) mx4[i] = fmaxf(mx4[i], sv[kTile - 4 + i]);
                 const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * p.scale_log2;
                 const bool move = mx > m_ref + 8.f || (m_ref == -INFINITY && mx > -INFINITY);
-                const float m_new = move ? mx : m_ref;
-                const float factor = (move && m_ref != -INFINITY) ? ex2(m_ref - m_new) : 1.f;
-                if (jj > 0 && __any_sync(0xffffffffu, valid && factor != 1.f)) {
-                    // S of this tile is complete, so the previous P V is as well: O may be touched
-                    for (int ch = 0; ch < 4; ++ch) {
-                        uint32_t ov[32];
-                        tmem_ld32(t_o + 32u * ch, ov);
-                        tmem_wait_ld();
+                if (__any_sync(0xffffffffu, move)) {
+                    const float factor = move && m_ref != -INFINITY ? ex2(m_ref - mx) : 1.f;
+                    if (move) m_ref = mx;
+                    l_sum *= factor;
+                    if (jj > 0 && __any_sync(0xffffffffu, valid && factor != 1.f))
+                        // S of this tile is complete, so the previous P V is as well: O may be touched
+#pragma unroll 1
+                        for (int ch = 0; ch < 4; ++ch) {
+                            uint32_t ov[32];
+                            tmem_ld32(t_o + 32u * ch, ov);
+                            tmem_wait_ld();
 #pragma unroll
-                        for (int c = 0; c < 32; ++c) ov[c] = __float_as_uint(__uint_as_float(ov[c]) * factor);
-                        tmem_st32(t_o + 32u * ch, ov);
-                    }
+                            for (int c = 0; c < 32; ++c) ov[c] = __float_as_uint(__uint_as_float(ov[c]) * factor);
+                            tmem_st32(t_o + 32u * ch, ov);
+                        }
                 }
-                l_sum *= factor;
-                m_ref = m_new;
-                const float neg_m = (m_ref == -INFINITY) ? 0.f : -m_ref;
-                float l4[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int ch = 0; ch < 2; ++ch) {
-                    uint32_t pw[32];
-#pragma unroll
-                    for (int c = 0; c < 32; ++c) {
-                        const float e0 = ex2(fmaf(sv[64 * ch + 2 * c], p.scale_log2, neg_m));
-                        const float e1 = ex2(fmaf(sv[64 * ch + 2 * c + 1], p.scale_log2, neg_m));
-                        l4[c & 1] += e0; l4[2 + (c & 1)] += e1;
-                        pw[c] = bf16_pair(e0, e1);
-                    }
-                    tmem_st32(t_s + 32u * ch, pw);
-                }
-                l_sum += (l4[0] + l4[1]) + (l4[2] + l4[3]);
-                tmem_wait_st();
-                tc_fence_before();
                 if (side == 1 && jj == 0 && joins > 0) {
                     // side 0 has read this side's O of the last joined piece before it is overwritten
                     alive = __all_sync(0xffffffffu, mbar_wait(bar(JOIN_EMPTY), (joins - 1) & 1, ab));
                     if (!alive) break;
                 }
-                warp_arrive(bar(P_FULL + side), lane);
+                const float neg_m = (m_ref == -INFINITY) ? 0.f : -m_ref;
+                const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2), neg2 = pack2(neg_m, neg_m);
+                uint64_t sum2[2] = {0, 0};
+                auto weights = [&](auto with_poly) {
+#pragma unroll
+                    for (int part = 0; part < 4; ++part) {
+                        uint32_t pw[16];
+#pragma unroll
+                        for (int c = 0; c < 16; ++c) {
+                            const uint64_t y = fma2(pack2(sv[32 * part + 2 * c], sv[32 * part + 2 * c + 1]), scale2, neg2);
+                            const uint64_t e = decltype(with_poly)::value && kPolyEvery > 0 && c % kPolyOf >= kPolyOf - kPolyEvery ? exp2_poly2(y) : exp2_sfu2(y);
+                            sum2[c & 1] = add2(sum2[c & 1], e);
+                            pw[c] = bf16_pair2(e);
+                        }
+                        tmem_st16(t_s + 16u * part, pw);
+                        if (part & 1) {
+                            tmem_wait_st();
+                            tc_fence_before();
+                            warp_arrive(bar((part == 1 ? P_HALF : P_FULL) + side), lane);
+                        }
+                    }
+                };
+                if (masked) weights(std::false_type{}); else weights(std::true_type{});
+                float2 sum = unpack2(add2(sum2[0], sum2[1]));
+                l_sum += sum.x + sum.y;
             }
             if (!alive) break;
             s_seen += n;
 
             // ---- the piece's result ----
-            const bool joined = !w.wide && w.n[1] > 0;                      // both sides hold a part of the same rows
+            const bool joined = !w.wide && w.n1 > 0;                      // both sides hold a part of the same rows
             if (joined && side == 1) {
                 if (joins > 0) {
                     alive = __all_sync(0xffffffffu, mbar_wait(bar(JOIN_EMPTY), (joins - 1) & 1, ab));
@@ -462,7 +549,7 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                 l_sum = l_sum * f0 + o.y * f1;
                 m_ref = m;
             }
-            if (w.n[1] > 0) ++o_other;
+            if (w.n1 > 0) ++o_other;
             tc_fence_after();
             const bool direct = x.parts == 1;
             const float inv = direct ? (l_sum > 0.f ? 1.f / l_sum : (l_sum == 0.f ? 0.f : l_sum)) : 1.f;
@@ -472,6 +559,7 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
             const size_t part0 = (size_t)w.kvh * p.head->rows_per_head + x.part_row + (side == 1 ? (size_t)x.parts * p.T * p.G : 0);
             const size_t part_at = part0 + (size_t)x.part * rows + L;
             const size_t row_head = (size_t)(x.row0 + tok0 + tl) * p.Hq + w.kvh * p.G + gl;
+#pragma unroll 1
             for (int ch = 0; ch < 4; ++ch) {
                 uint32_t ov[32];
                 if (n > 0) { tmem_ld32(t_o + 32u * ch, ov); tmem_wait_ld(); }
@@ -515,9 +603,11 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
             asm volatile("barrier.cta.sync %0, %1;" ::"r"(1 + side), "n"(kSideThreads) : "memory");
             if (misc[4 + side]) {
                 __threadfence();
+#pragma unroll 1
                 for (int u = tid & (kSideThreads - 1); u < rows * (kHeadDim / 8); u += kSideThreads) {
                     const int row = u / (kHeadDim / 8), col = (u % (kHeadDim / 8)) * 8;
                     float m = -INFINITY, l = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 2
                     for (int k = 0; k < x.parts; ++k) {
                         const size_t at = part0 + (size_t)k * rows + row;
                         const float2 ml = __ldcg(p.part_ml + at);
@@ -593,8 +683,10 @@ cudaError_t launch_chunk_attn(const ChunkParams& p, const void* q, long q_stride
         const cuuint32_t box[5] = {64, 8, 2, 2, 1};
         if (!encode(&tm_k, k_pages, 5, dims, strides, box) || !encode(&tm_v, v_pages, 5, dims, strides, box)) return cudaErrorInvalidValue;
     }
-    const cudaError_t e = cudaFuncSetAttribute(chunk_attn_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+    cudaError_t e = cudaFuncSetAttribute(chunk_attn_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
     if (e != cudaSuccess) return e;
+    static const int regs = [] { cudaFuncAttributes a; return cudaFuncGetAttributes(&a, chunk_attn_kernel) == cudaSuccess ? a.numRegs : 0; }();
+    if (regs < kLaunchRegs) return cudaErrorInvalidConfiguration;       // the register split needs what it was computed from
     return launch_dependent(chunk_attn_kernel, p.grid, kThreadsChunk, kSmemBytes, st, p, tm_q, tm_k, tm_v);
 }
 
