@@ -50,13 +50,13 @@ constexpr int kTakeWarp = 8, kKWarp = 9, kVWarp = 10, kMmaWarp = 11;
 constexpr int kHalfBytes = kRows * 128;
 constexpr int kOperandBytes = 2 * kHalfBytes;
 constexpr int kRingK = 3, kRingV = 2, kRingPiece = 2;
-#ifndef POLY
-#define POLY 0
+#ifndef AFTER
+#define AFTER 16
 #endif
-constexpr int kPolyEvery = POLY, kPolyOf = 8;
+constexpr int kAfter = AFTER;
 constexpr uint32_t kTmemCols = 512;
 // registers per thread: at launch, and after the softmax warpgroups have taken from the third one
-constexpr int kLaunchRegs = 168, kSoftmaxRegs = 224, kHelperRegs = 56;
+constexpr int kLaunchRegs = 168, kSoftmaxRegs = 216, kHelperRegs = 72;
 static_assert(2 * kSoftmaxRegs + kHelperRegs <= 3 * kLaunchRegs, "the split draws on what the block was launched with");
 
 constexpr int kOffQ = 0;                                       // two row tiles
@@ -111,7 +111,9 @@ __device__ __forceinline__ void derive(Work& w, int T) {
     w.loads = tiles;
 }
 
-// Next piece from the ring; false at the end of the list or when the CTA is aborting.
+// Next piece from the ring; false at the end of the list or when the CTA is aborting.  A role that keeps reading the
+// ring's entry (kKeep) gives it back itself.
+template <bool kKeep = false>
 __device__ __forceinline__ bool next_piece(Work& w, int it, const unsigned char* smem, uint32_t bar0, int lane, int T, const Abort& ab) {
     const int slot = it % kRingPiece;
     const bool ok = __all_sync(0xffffffffu, mbar_wait(bar0 + 8u * (PIECE_FULL + slot), (it / kRingPiece) & 1, ab));
@@ -120,7 +122,7 @@ __device__ __forceinline__ bool next_piece(Work& w, int it, const unsigned char*
     int4* dst = reinterpret_cast<int4*>(&w.x);
     dst[0] = src[0]; dst[1] = src[1]; dst[2] = src[2];
     w.kvh = src[3].x;
-    warp_arrive(bar0 + 8u * (PIECE_EMPTY + slot), lane);
+    if (!kKeep) warp_arrive(bar0 + 8u * (PIECE_EMPTY + slot), lane);
     if (w.kvh < 0) return false;
     derive(w, T);
     return true;
@@ -138,30 +140,19 @@ __device__ __forceinline__ void tma_load_page_keep(uint32_t dst, const CUtensorM
 }
 
 // 32 bytes per thread: whole sectors, although every thread writes a row of its own
-__device__ __forceinline__ void st_global_32(void* p, const uint32_t (&r)[8]) {
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
-                 ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+__device__ __forceinline__ void st_global_32(void* to, const float* v) {
+    asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"l"(to), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]) : "memory");
 }
-
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
-        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
-          "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
-}
-
 __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&h);
 }
-
-// Eight values of a result row, columns [col, col + 8)
-__device__ __forceinline__ void store_out(const ChunkParams& p, size_t row_head, int col, const float (&v)[8]) {
+// 8 values of a result row from column `col` on
+__device__ __forceinline__ void store_out8(const ChunkParams& p, size_t row_head, int col, const float* v) {
     if (p.out_dtype == TTS_OUT_FP32) {
-        uint32_t r[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) r[i] = __float_as_uint(v[i]);
-        st_global_32(static_cast<float*>(p.out) + row_head * kHeadDim + col, r);
+        float4* to = reinterpret_cast<float4*>(static_cast<float*>(p.out) + row_head * kHeadDim + col);
+        to[0] = make_float4(v[0], v[1], v[2], v[3]); to[1] = make_float4(v[4], v[5], v[6], v[7]);
     } else {
         *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + row_head * kHeadDim + col) =
             make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
@@ -180,25 +171,6 @@ __device__ __forceinline__ uint64_t exp2_sfu2(uint64_t y) {
     const float2 f = unpack2(y);
     return pack2(ex2(f.x), ex2(f.y));
 }
-// 2^y for two y <= 8 on the FMA pipe: y = n + f with |f| <= 1/2 (adding 1.5 x 2^23 leaves n in the low bits), a
-// polynomial of degree 4 fitted to 2^f for the smallest largest relative error (2.6e-6, far below the rounding
-// of P to bf16), and n added to the exponent.  Below -126 the result is 2^-126, not 0: the caller uses it only
-// where no key is masked, and such a weight is lost in the sum either way.
-__device__ __forceinline__ uint64_t exp2_poly2(uint64_t y) {
-    float2 v = unpack2(y);
-    v.x = fmaxf(v.x, -126.f); v.y = fmaxf(v.y, -126.f);
-    y = pack2(v.x, v.y);
-    const uint64_t magic = pack2(12582912.f, 12582912.f), back = pack2(-12582912.f, -12582912.f), minus1 = pack2(-1.f, -1.f);
-    const uint64_t t = add2(y, magic);
-    const uint64_t f = fma2(add2(t, back), minus1, y);
-    uint64_t q = fma2(f, pack2(0.009570101911165427f, 0.009570101911165427f), pack2(0.055917860319388245f, 0.055917860319388245f));
-    q = fma2(q, f, pack2(0.2402474482786378f, 0.2402474482786378f));
-    q = fma2(q, f, pack2(0.6931218147366892f, 0.6931218147366892f));
-    q = fma2(q, f, pack2(0.9999992614457122f, 0.9999992614457122f));
-    const float2 n = unpack2(t), r = unpack2(q);
-    return pack2(__uint_as_float(__float_as_uint(r.x) + (__float_as_uint(n.x) << 23)), __uint_as_float(__float_as_uint(r.y) + (__float_as_uint(n.y) << 23)));
-}
-
 __global__ void __launch_bounds__(kThreadsChunk, 1)
 chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                   const __grid_constant__ CUtensorMap tm_v) {
@@ -425,55 +397,65 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
     } else {
         // =========================== softmax ===========================
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
-        const int side = warp >> 2, quarter = warp & 3;
-        const int L = quarter * 32 + lane;                  // row of the tile = TMEM lane
-        const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
-        const uint32_t t_s = tmem + side * 128u + lane_base, t_o = tmem + 256u + side * 128u + lane_base;
-        const int tl = L / p.G, gl = L - tl * p.G;          // token of the tile and head of the group
-        float2* join = reinterpret_cast<float2*>(smem + kOffJoin);
-        int s_seen = 0, o_seen = 0, joins = 0;              // phases of S_FULL, O_FULL of this side; joined pieces
-        int o_other = 0;                                    // phases of the other side's O_FULL (side 0 waits for it in narrow pieces)
+        // What the loop over the tiles does not need stays in shared memory (the piece's record is given back at the
+        // piece's end) or is worked out again: the loop's 128 scores leave few registers, and every spill is a stall.
+        const int side = warp >> 2;
+        const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t t_s = tmem + side * 128u + lane_base, t_o = t_s + 256u;
+        uint32_t phases = 0;                                // bits: S_FULL, O_FULL of this side, O_FULL of the other, JOIN, a JOIN has been
+        enum { S_PHASE = 1, O_PHASE = 2, OTHER_PHASE = 4, JOIN_PHASE = 8, JOINED = 16 };
         bool alive = true;
-        Work w;
-        for (int it = 0; alive && next_piece(w, it, smem, bar0, lane, p.T, ab); ++it) {
-            const ChunkPiece& x = w.x;
-            const int tok0 = w.wide ? side * p.T : 0;                       // first token of this side's rows
-            const int n_tok = min(p.T, x.n_tok - tok0);
-            const bool valid = tl < n_tok;                                  // (L >= T G has tl >= T)
-            const int n = side ? w.n1 : w.n0;
-            const int step = w.wide ? kTile : 2 * kTile;
-            int key0 = x.tile_begin * kTile + (w.wide ? 0 : side * kTile);  // first key of the tile at hand
-            const int limit = min(x.keys, x.limit0 + tok0 + min(tl, n_tok - 1));   // keys this row sees (<= 0: none)
-            const int limit_min = x.limit0 + tok0;                          // the fewest that a row of the tile sees
-            float m_ref = -INFINITY, l_sum = 0.f;
-            for (int jj = 0; jj < n; ++jj, key0 += step) {
-                alive = __all_sync(0xffffffffu, mbar_wait(bar(S_FULL + side), (s_seen + jj) & 1, ab));
+        for (int it = 0; alive; ++it) {
+            int n, key0, step, limit, limit_min;
+            {
+                Work w;
+                if (!next_piece<true>(w, it, smem, bar0, lane, p.T, ab)) break;
+                const int tok0 = w.wide ? side * p.T : 0;                           // first token of this side's rows
+                const int tl = ((warp & 3) * 32 + lane) / p.G, last = min(p.T, w.x.n_tok - tok0) - 1;
+                n = side ? w.n1 : w.n0;
+                step = w.wide ? kTile : 2 * kTile;
+                key0 = w.x.tile_begin * kTile + (w.wide ? 0 : side * kTile);
+                limit = min(w.x.keys, w.x.limit0 + tok0 + min(tl, last));           // keys this row sees (<= 0: none)
+                limit_min = min(w.x.keys, w.x.limit0 + tok0);                       // the fewest that a row of the tile sees
+            }
+            if (side == 1 && n > 0 && (phases & JOINED)) {
+                // side 0 has read what this side left of the last joined piece (O in TMEM, maxima and sums)
+                alive = __all_sync(0xffffffffu, mbar_wait(bar(JOIN_EMPTY), phases & JOIN_PHASE ? 0 : 1, ab));
                 if (!alive) break;
+            }
+            float m_ref = -INFINITY, l_sum = 0.f;
+#pragma unroll 1
+            for (int jj = 0; jj < n; ++jj, key0 += step) {
+                alive = __all_sync(0xffffffffu, mbar_wait(bar(S_FULL + side), phases & S_PHASE ? 1 : 0, ab));
+                if (!alive) break;
+                phases ^= S_PHASE;
                 tc_fence_after();
+                const bool masked = key0 + kTile > limit_min;               // uniform over the side
+                const int seen = limit - key0;
                 float sv[kTile];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) tmem_ld32(t_s + 32u * c, reinterpret_cast<uint32_t*>(sv) + 32 * c);
+                float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                tmem_ld32(t_s, reinterpret_cast<uint32_t*>(sv));
+                tmem_ld32(t_s + 32u, reinterpret_cast<uint32_t*>(sv) + 32);
                 tmem_wait_ld();
-                const bool masked = key0 + kTile > min(limit_min, x.keys);  // uniform over the side
-                if (masked) {
-                    const int seen = limit - key0;
+                tmem_ld32(t_s + 64u, reinterpret_cast<uint32_t*>(sv) + 64);  // on their way while the maximum of the first half is taken
+                tmem_ld32(t_s + 96u, reinterpret_cast<uint32_t*>(sv) + 96);
 #pragma unroll
-                    for (int c = 0; c < kTile; ++c) if (c >= seen) sv[c] = -INFINITY;
+                for (int half = 0; half < 2; ++half) {
+                    if (half) tmem_wait_ld();
+                    if (masked) {
+#pragma unroll
+                        for (int c = 64 * half; c < 64 * half + 64; ++c) if (c >= seen) sv[c] = -INFINITY;
+                    }
+#pragma unroll
+                    for (int c = 32 * half; c < 32 * half + 32; ++c) mx4[c & 3] = max3(mx4[c & 3], sv[2 * c], sv[2 * c + 1]);
                 }
-                float mx4[4] = {sv[0], sv[1], sv[2], sv[3]};
-#pragma unroll
-                for (int c = 4; c + 8 <= kTile; c += 8)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) mx4[i] = max3(mx4[i], sv[c + i], sv[c + 4 + i]);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) mx4[i] = fmaxf(mx4[i], sv[kTile - 4 + i]);
-                const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * p.scale_log2;
+                const float mx = max3(fmaxf(mx4[0], mx4[1]), mx4[2], mx4[3]) * p.scale_log2;
                 const bool move = mx > m_ref + 8.f || (m_ref == -INFINITY && mx > -INFINITY);
                 if (__any_sync(0xffffffffu, move)) {
                     const float factor = move && m_ref != -INFINITY ? ex2(m_ref - mx) : 1.f;
                     if (move) m_ref = mx;
                     l_sum *= factor;
-                    if (jj > 0 && __any_sync(0xffffffffu, valid && factor != 1.f))
+                    if (jj > 0 && __any_sync(0xffffffffu, factor != 1.f))
                         // S of this tile is complete, so the previous P V is as well: O may be touched
 #pragma unroll 1
                         for (int ch = 0; ch < 4; ++ch) {
@@ -485,63 +467,70 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                             tmem_st32(t_o + 32u * ch, ov);
                         }
                 }
-                if (side == 1 && jj == 0 && joins > 0) {
-                    // side 0 has read this side's O of the last joined piece before it is overwritten
-                    alive = __all_sync(0xffffffffu, mbar_wait(bar(JOIN_EMPTY), (joins - 1) & 1, ab));
-                    if (!alive) break;
-                }
                 const float neg_m = (m_ref == -INFINITY) ? 0.f : -m_ref;
                 const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2), neg2 = pack2(neg_m, neg_m);
                 uint64_t sum2[2] = {0, 0};
-                auto weights = [&](auto with_poly) {
+                uint32_t pw[kTile / 2];
+                auto weights = [&](int c0, int c1) {                         // columns [2 c0, 2 c1)
 #pragma unroll
-                    for (int part = 0; part < 4; ++part) {
-                        uint32_t pw[16];
-#pragma unroll
-                        for (int c = 0; c < 16; ++c) {
-                            const uint64_t y = fma2(pack2(sv[32 * part + 2 * c], sv[32 * part + 2 * c + 1]), scale2, neg2);
-                            const uint64_t e = decltype(with_poly)::value && kPolyEvery > 0 && c % kPolyOf >= kPolyOf - kPolyEvery ? exp2_poly2(y) : exp2_sfu2(y);
-                            sum2[c & 1] = add2(sum2[c & 1], e);
-                            pw[c] = bf16_pair2(e);
-                        }
-                        tmem_st16(t_s + 16u * part, pw);
-                        if (part & 1) {
-                            tmem_wait_st();
-                            tc_fence_before();
-                            warp_arrive(bar((part == 1 ? P_HALF : P_FULL) + side), lane);
-                        }
+                    for (int c = c0; c < c1; ++c) {
+                        const uint64_t e = exp2_sfu2(fma2(pack2(sv[2 * c], sv[2 * c + 1]), scale2, neg2));
+                        sum2[c & 1] = add2(sum2[c & 1], e);
+                        pw[c] = bf16_pair2(e);
                     }
                 };
-                if (masked) weights(std::false_type{}); else weights(std::true_type{});
-                float2 sum = unpack2(add2(sum2[0], sum2[1]));
+                weights(0, 32);
+                tmem_st32(t_s, pw);
+                weights(32, 32 + kAfter);                                    // while the first half is stored
+                tmem_wait_st();
+                tc_fence_before();
+                warp_arrive(bar(P_HALF + side), lane);
+                weights(32 + kAfter, 64);
+                tmem_st32(t_s + 32u, pw + 32);
+                tmem_wait_st();
+                tc_fence_before();
+                warp_arrive(bar(P_FULL + side), lane);
+                const float2 sum = unpack2(add2(sum2[0], sum2[1]));
                 l_sum += sum.x + sum.y;
             }
             if (!alive) break;
-            s_seen += n;
-
             // ---- the piece's result ----
-            const bool joined = !w.wide && w.n1 > 0;                      // both sides hold a part of the same rows
-            if (joined && side == 1) {
-                if (joins > 0) {
-                    alive = __all_sync(0xffffffffu, mbar_wait(bar(JOIN_EMPTY), (joins - 1) & 1, ab));
-                    if (!alive) break;
+            Work w;
+            {
+                const int4* src = reinterpret_cast<const int4*>(smem + kOffPiece + (it % kRingPiece) * kPieceBytes);
+                int4* dst = reinterpret_cast<int4*>(&w.x);
+                dst[0] = src[0]; dst[1] = src[1]; dst[2] = src[2];
+                w.kvh = src[3].x;
+                derive(w, p.T);
+                warp_arrive(bar(PIECE_EMPTY + it % kRingPiece), lane);
+            }
+            const ChunkPiece& x = w.x;
+            const int L = (warp & 3) * 32 + lane;           // row of the tile = TMEM lane
+            const int tl = L / p.G, gl = L - tl * p.G;      // token of the tile and head of the group
+            const int tok0 = w.wide ? side * p.T : 0, n_tok = min(p.T, x.n_tok - tok0);
+            const bool valid = tl < n_tok;                  // (L >= T G has tl >= T)
+            const bool joined = !w.wide && w.n1 > 0;        // both sides hold a part of the same rows
+            float2* join = reinterpret_cast<float2*>(smem + kOffJoin);
+            if (!w.wide && side == 1) {
+                if (joined) {
+                    phases ^= O_PHASE;                      // side 0 waits for this side's O
+                    join[L] = make_float2(m_ref, l_sum);
+                    phases = (phases ^ JOIN_PHASE) | JOINED;
+                    warp_arrive(bar(JOIN_FULL), lane);
                 }
-                join[L] = make_float2(m_ref, l_sum);
-                ++joins; o_seen += 1;
-                warp_arrive(bar(JOIN_FULL), lane);
                 continue;
             }
-            if (!w.wide && side == 1) continue;
             if (n > 0) {
-                alive = __all_sync(0xffffffffu, mbar_wait(bar(O_FULL + side), o_seen & 1, ab));
-                ++o_seen;
+                alive = __all_sync(0xffffffffu, mbar_wait(bar(O_FULL + side), phases & O_PHASE ? 1 : 0, ab));
+                phases ^= O_PHASE;
                 if (!alive) break;
             }
-            float f0 = 1.f, f1 = 0.f;                                       // what each side's O counts
+            float f0 = 1.f, f1 = 0.f;                       // what each side's O counts
             if (joined) {
-                alive = __all_sync(0xffffffffu, mbar_wait(bar(JOIN_FULL), joins & 1, ab) && mbar_wait(bar(O_FULL + 1), o_other & 1, ab));
+                alive = __all_sync(0xffffffffu, mbar_wait(bar(JOIN_FULL), phases & JOIN_PHASE ? 1 : 0, ab) &&
+                                                mbar_wait(bar(O_FULL + 1), phases & OTHER_PHASE ? 1 : 0, ab));
                 if (!alive) break;
-                ++joins;
+                phases ^= JOIN_PHASE;
                 const float2 o = join[L];
                 const float m = fmaxf(m_ref, o.x);
                 f0 = m_ref == -INFINITY ? 0.f : ex2(m_ref - m);
@@ -549,12 +538,12 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                 l_sum = l_sum * f0 + o.y * f1;
                 m_ref = m;
             }
-            if (w.n1 > 0) ++o_other;
+            if (w.n1 > 0) phases ^= OTHER_PHASE;
             tc_fence_after();
             const bool direct = x.parts == 1;
             const float inv = direct ? (l_sum > 0.f ? 1.f / l_sum : (l_sum == 0.f ? 0.f : l_sum)) : 1.f;
             f0 *= inv; f1 *= inv;
-            const int rows = n_tok * p.G;                                   // valid rows of this side
+            const int rows = n_tok * p.G;                   // valid rows of this side
             // partial results of an entry: side 0's pieces, then side 1's
             const size_t part0 = (size_t)w.kvh * p.head->rows_per_head + x.part_row + (side == 1 ? (size_t)x.parts * p.T * p.G : 0);
             const size_t part_at = part0 + (size_t)x.part * rows + L;
@@ -572,18 +561,11 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
 #pragma unroll
                     for (int c = 0; c < 32; ++c) if (f1 != 0.f) o[c] = fmaf(__uint_as_float(ov[c]), f1, o[c]);
                 }
-                if (valid) {
+                if (!valid) continue;
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        const float v[8] = {o[8 * c], o[8 * c + 1], o[8 * c + 2], o[8 * c + 3], o[8 * c + 4], o[8 * c + 5], o[8 * c + 6], o[8 * c + 7]};
-                        if (direct) store_out(p, row_head, 32 * ch + 8 * c, v);
-                        else {
-                            uint32_t r[8];
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) r[i] = __float_as_uint(v[i]);
-                            st_global_32(p.part_o + part_at * kHeadDim + 32 * ch + 8 * c, r);
-                        }
-                    }
+                for (int c = 0; c < 4; ++c) {
+                    if (direct) store_out8(p, row_head, 32 * ch + 8 * c, o + 8 * c);
+                    else st_global_32(p.part_o + part_at * kHeadDim + 32 * ch + 8 * c, o + 8 * c);
                 }
             }
             tc_fence_before();
@@ -626,7 +608,7 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                     for (int i = 0; i < 8; ++i) acc[i] *= scale;
                     const int t = row / p.G;
                     const size_t to = (size_t)(x.row0 + tok0 + t) * p.Hq + w.kvh * p.G + (row - t * p.G);
-                    store_out(p, to, col, acc);
+                    store_out8(p, to, col, acc);
                     if (col == 0 && p.lse) p.lse[to] = l == 0.f ? -INFINITY : m * 0.69314718055994530942f + logf(l);
                 }
             }
