@@ -67,9 +67,9 @@ cudaError_t cache_alloc(Ctx* c) {
 
 void cache_release(Ctx* c) {
     cudaFree(c->page_work);
-    cudaFree(c->chunk_head); cudaFree(c->chunk_pieces); cudaFree(c->chunk_entries); cudaFree(c->chunk_arrived);
+    cudaFree(c->chunk_head); cudaFree(c->chunk_pieces); cudaFree(c->chunk_arrived);
     cudaFree(c->chunk_part_o); cudaFree(c->chunk_part_ml);
-    c->page_work = nullptr; c->chunk_head = nullptr; c->chunk_pieces = nullptr; c->chunk_entries = nullptr; c->chunk_arrived = nullptr;
+    c->page_work = nullptr; c->chunk_head = nullptr; c->chunk_pieces = nullptr; c->chunk_arrived = nullptr;
     c->chunk_part_o = nullptr; c->chunk_part_ml = nullptr; c->chunk_rows = 0;
 }
 
@@ -91,16 +91,18 @@ int tts_chunk_reserve(tts_ctx* ctx, int max_rows) {
     if (entries * f.n_kv_heads * 2 >= (1l << 31) || pieces * f.n_kv_heads >= (1l << 31)) return TTS_ERR_UNSUPPORTED;
     cudaError_t e = cudaMalloc(&c->chunk_head, sizeof(ChunkHead));
     if (e == cudaSuccess) e = cudaMalloc(&c->chunk_pieces, (size_t)pieces * sizeof(ChunkPiece));
-    if (e == cudaSuccess) e = cudaMalloc(&c->chunk_entries, (size_t)entries * sizeof(int2));
-    if (e == cudaSuccess) e = cudaMalloc(&c->chunk_arrived, (size_t)entries * f.n_kv_heads * 2 * sizeof(int));
+    const size_t arrived = (size_t)entries * f.n_kv_heads * 2 * sizeof(unsigned);
+    if (e == cudaSuccess) e = cudaMalloc(&c->chunk_arrived, arrived);
+    if (e == cudaSuccess) e = cudaMemset(c->chunk_arrived, 0, arrived);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(cudaStreamLegacy);       // before work on a stream that does not wait for it
     if (e == cudaSuccess) e = cudaMalloc(&c->chunk_part_o, (size_t)part_rows * kHeadDim * sizeof(float));
     if (e == cudaSuccess) e = cudaMalloc(&c->chunk_part_ml, (size_t)part_rows * sizeof(float2));
     if (e != cudaSuccess) {
-        cudaFree(c->chunk_head); cudaFree(c->chunk_pieces); cudaFree(c->chunk_entries); cudaFree(c->chunk_arrived); cudaFree(c->chunk_part_o);
-        c->chunk_head = nullptr; c->chunk_pieces = nullptr; c->chunk_entries = nullptr; c->chunk_arrived = nullptr; c->chunk_part_o = nullptr;
+        cudaFree(c->chunk_head); cudaFree(c->chunk_pieces); cudaFree(c->chunk_arrived); cudaFree(c->chunk_part_o);
+        c->chunk_head = nullptr; c->chunk_pieces = nullptr; c->chunk_arrived = nullptr; c->chunk_part_o = nullptr;
         return finish(c, e, 0);
     }
-    c->chunk_rows = max_rows; c->chunk_max_entries = (int)entries; c->chunk_max_pieces = (int)pieces; c->chunk_part_rows = part_rows;
+    c->chunk_rows = max_rows; c->chunk_arrived_bytes = arrived; c->chunk_max_pieces = (int)pieces; c->chunk_part_rows = part_rows;
     return TTS_OK;
 }
 
@@ -122,7 +124,9 @@ int tts_chunk_attn(tts_ctx* ctx, const void* q, int64_t q_row_stride, const void
     memset(&p, 0, sizeof p);
     p.block_table = block_table; p.branch_lens = branch_lens; p.row_start = row_start;
     p.out = out; p.lse = lse;
-    p.head = c->chunk_head; p.pieces = c->chunk_pieces; p.entry_tiles = c->chunk_entries; p.arrived = c->chunk_arrived;
+    // the entries of a call: at most one per branch and one per 2 T rows
+    const bool small = (long)total_rows / (2 * (128 / (f.n_q_heads / f.n_kv_heads))) + n_branches <= kChunkSmall;
+    p.head = small ? nullptr : c->chunk_head; p.pieces = c->chunk_pieces; p.arrived = c->chunk_arrived;
     p.part_o = c->chunk_part_o; p.part_ml = c->chunk_part_ml;
     p.status = c->d_status;
     p.Hq = f.n_q_heads; p.Hkv = f.n_kv_heads; p.G = p.Hq / p.Hkv; p.T = 128 / p.G;
@@ -131,9 +135,12 @@ int tts_chunk_attn(tts_ctx* ctx, const void* q, int64_t q_row_stride, const void
     p.grid = f.max_ctas > 0 && f.max_ctas < c->n_sms ? f.max_ctas : c->n_sms;
     p.out_dtype = f.out_dtype;
     p.scale_log2 = (f.softmax_scale > 0.f ? f.softmax_scale : 1.0f / sqrtf((float)f.head_dim)) * 1.4426950408889634f;
-    cudaError_t e = launch_chunk_plan(p, c->stream);
-    if (e != cudaSuccess) return finish(c, e, 0);
-    c->launches += 1;
+    cudaError_t e;
+    if (!small) {
+        e = launch_chunk_plan(p, c->stream);
+        if (e != cudaSuccess) return finish(c, e, 0);
+        c->launches += 1;
+    }
     e = launch_chunk_attn(p, q, (long)q_row_stride, k_pages, v_pages, c->stream);
     return finish(c, e, 1);
 }

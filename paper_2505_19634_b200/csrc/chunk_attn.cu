@@ -75,6 +75,22 @@ constexpr int kOffJoin = kOffPiece + kRingPiece * kPieceBytes; // side 1's (m, l
 constexpr int kSmemBytes = kOffJoin + kRows * 8 + 1024;
 static_assert(kSmemBytes <= 227 * 1024, "shared memory");
 
+// tcgen05.mma with descriptors as two words each; `accumulate` 0: the first step of a sum
+__device__ __forceinline__ void umma_ss(uint32_t d, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\t"
+        "mov.b64 a, {%1, %2};\n\tmov.b64 b, {%3, %4};\n\tsetp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %5, p;\n\t}"
+        ::"r"(d), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void umma_ts(uint32_t d, uint32_t a_tmem, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 b;\n\tmov.b64 b, {%2, %3};\n\tsetp.ne.b32 p, %5, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n\t}"
+        ::"r"(d), "r"(a_tmem), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate) : "memory");
+}
+
+// true in one lane of the warp; used right where it guards, which the compiler knows how to treat
 __device__ __forceinline__ bool elect_one() {
     uint32_t ok;
     asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok));
@@ -89,7 +105,7 @@ __device__ __forceinline__ void warp_arrive(uint32_t bar, int lane) {
 // A piece as every role sees it.
 struct Work {
     ChunkPiece x;
-    int kvh;
+    int kvh, part_rows;
     bool wide;
     int n0, n1;      // KV tiles of each side
     int loads;       // KV tiles to load
@@ -126,6 +142,75 @@ __device__ __forceinline__ bool next_piece(Work& w, int it, const unsigned char*
     if (w.kvh < 0) return false;
     derive(w, T);
     return true;
+}
+
+// The schedule of a call of up to kChunkSmall entries, one entry per lane: made by every CTA for itself, so that the
+// smallest calls, whose time is latency, are one launch.
+struct SmallPlan {
+    ChunkEntry e;      // this lane's entry
+    int k, at, row;    // its pieces, its first piece's place, its first partial row
+    int pieces, part_rows;
+};
+
+__device__ __forceinline__ int warp_scan(int v, int lane, int* total) {        // exclusive
+    int s = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { const int n = __shfl_up_sync(0xffffffffu, s, o); if (lane >= o) s += n; }
+    *total = __shfl_sync(0xffffffffu, s, 31);
+    return s - v;
+}
+
+__device__ SmallPlan small_plan(const ChunkParams& p, int lane) {
+    SmallPlan sp;
+    int lo = 0, c = 0, keys = 0;
+    bool bad = false;
+    if (lane < p.n_branches) {
+        lo = p.row_start[lane];
+        const int hi = p.row_start[lane + 1], len = p.branch_lens[lane];
+        bad = !chunk_branch_ok(p, lo, hi, len);
+        c = hi - lo; keys = p.prefix_len + len;
+    }
+    bad = __any_sync(0xffffffffu, bad);
+    if (bad && lane == 0) atomicMin(p.status, (int)TTS_ERR_DEVICE_BOUNDS);
+    int n;
+    const int first = warp_scan(bad ? 0 : ceil_div(c, 2 * p.T), lane, &n);
+    // the branch of entry `lane`: the last one that starts at or before it
+    int b = 0;
+    for (int i = 0; i < min(p.n_branches, 32); ++i) if (__shfl_sync(0xffffffffu, first, i) <= lane) b = i;
+    sp.e = chunk_entry(p.T, b, ceil_div(__shfl_sync(0xffffffffu, c, b), 2 * p.T) - 1 - (lane - __shfl_sync(0xffffffffu, first, b)), __shfl_sync(0xffffffffu, lo, b), __shfl_sync(0xffffffffu, c, b),
+                       __shfl_sync(0xffffffffu, keys, b));
+    const bool mine = lane < n;
+    const int cost = mine ? chunk_cost(sp.e, p.T) : -1, rows = mine ? sp.e.n_tok * p.G : 0;
+    // costliest first, equal ones in their order
+    int after = 0, total = 0;                           // cost of this entry and those behind it; of all
+    unsigned ahead = 0;                                 // the lanes whose entries come before this one
+    for (int i = 0; i < n; ++i) {
+        const int c_i = __shfl_sync(0xffffffffu, cost, i);
+        total += c_i;
+        if (c_i > cost || (c_i == cost && i < lane)) ahead |= 1u << i; else after += c_i;
+    }
+    for (int bound = chunk_bound(p, (float)total);; bound = bound >= 4096 ? kChunkNoBound : bound * 4) {
+        sp.k = mine ? chunk_cuts(p, sp.e, (float)after, bound) : 0;
+        sp.part_rows = __reduce_add_sync(0xffffffffu, sp.k > 1 ? sp.k * rows : 0);
+        if (bound == kChunkNoBound || (long)sp.part_rows * p.Hkv <= p.part_rows) break;     // else too much for the workspace
+    }
+    sp.pieces = __reduce_add_sync(0xffffffffu, sp.k);
+    sp.at = sp.row = 0;
+    for (int i = 0; i < n; ++i) {
+        const int k_i = __shfl_sync(0xffffffffu, sp.k, i), rows_i = __shfl_sync(0xffffffffu, sp.k > 1 ? sp.k * rows : 0, i);
+        if (ahead >> i & 1) { sp.at += k_i; sp.row += rows_i; }
+    }
+    return sp;
+}
+
+__device__ ChunkPiece small_piece(const ChunkParams& p, const SmallPlan& sp, int i, int lane) {
+    const bool here = sp.at <= i && i < sp.at + sp.k;
+    const int e = __ffs(__ballot_sync(0xffffffffu, here)) - 1;
+    ChunkPiece x = chunk_piece(sp.e, lane, i - sp.at, max(1, sp.k), sp.row);
+    int* w = reinterpret_cast<int*>(&x);
+#pragma unroll
+    for (int k = 0; k < (int)(sizeof x / 4); ++k) w[k] = __shfl_sync(0xffffffffu, w[k], e);
+    return x;
 }
 
 __device__ __forceinline__ void tma_load_rows(uint32_t dst, const CUtensorMap* map, int dim, int head, int row, uint32_t bar) {
@@ -211,41 +296,56 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kHelperRegs));
     if (warp == kTakeWarp) {
         // =========================== takes pieces, loads Q ===========================
-        if (lane == 0) {
-            const int per_head = p.head->pieces_per_head, total = per_head * p.Hkv;
-            int index = blockIdx.x, used[2] = {0, 0};
-            bool alive = true;
-            for (int it = 0; alive; ++it) {
-                const int slot = it % kRingPiece;
-                Work w;
-                w.kvh = -1;
-                if (index < total) {
-                    w.kvh = index / per_head;
-                    const int4* src = reinterpret_cast<const int4*>(p.pieces + (index - w.kvh * per_head));
+        SmallPlan small;
+        if (!p.head) small = small_plan(p, lane);
+        const int total = (p.head ? p.head->pieces : small.pieces) * p.Hkv, part_rows = p.head ? p.head->part_rows : small.part_rows;
+        int index = blockIdx.x, used[2] = {0, 0};
+        bool alive = true;
+        for (int it = 0; alive; ++it) {
+            const int slot = it % kRingPiece;
+            Work w;
+            w.kvh = -1;
+            if (index < total) {
+                const int i = index / p.Hkv;                            // all KV heads of a piece follow one another
+                w.kvh = index - i * p.Hkv;
+                if (p.head) {
+                    const int4* src = reinterpret_cast<const int4*>(p.pieces + i);
                     int4* dst = reinterpret_cast<int4*>(&w.x);
                     dst[0] = src[0]; dst[1] = src[1]; dst[2] = src[2];
-                }
-                alive = mbar_wait(bar(PIECE_EMPTY + slot), ((it / kRingPiece) & 1) ^ 1, ab);
-                if (!alive) break;
-                int4* ring = reinterpret_cast<int4*>(smem + kOffPiece + slot * kPieceBytes);
-                const int4* src = reinterpret_cast<const int4*>(&w.x);
-                ring[0] = src[0]; ring[1] = src[1]; ring[2] = src[2];
-                ring[3] = make_int4(w.kvh, 0, 0, 0);
-                mbar_arrive(bar(PIECE_FULL + slot));
-                if (w.kvh < 0) break;
-                index = atomicAdd(&p.head->next, 1);
-                derive(w, p.T);
-                for (int s = 0; s < (w.wide ? 2 : 1) && alive; ++s) {
-                    if ((s ? w.n1 : w.n0) == 0) continue;
-                    alive = mbar_wait(bar(Q_EMPTY + s), (used[s] & 1) ^ 1, ab);
-                    if (!alive) break;
-                    ++used[s];
-                    mbar_arrive_expect_tx(bar(Q_FULL + s), (uint32_t)(p.T * p.G) * 256u);
-                    const uint32_t dst = sbase + kOffQ + s * kOperandBytes;
-                    tma_load_rows(dst, &tm_q, 0, w.kvh * p.G, w.x.row0 + s * p.T, bar(Q_FULL + s));
-                    tma_load_rows(dst + kHalfBytes, &tm_q, 64, w.kvh * p.G, w.x.row0 + s * p.T, bar(Q_FULL + s));
+                } else {
+                    w.x = small_piece(p, small, i, lane);
                 }
             }
+            if (lane == 0) {
+                alive = mbar_wait(bar(PIECE_EMPTY + slot), ((it / kRingPiece) & 1) ^ 1, ab);
+                if (alive) {
+                    int4* ring = reinterpret_cast<int4*>(smem + kOffPiece + slot * kPieceBytes);
+                    const int4* src = reinterpret_cast<const int4*>(&w.x);
+                    ring[0] = src[0]; ring[1] = src[1]; ring[2] = src[2];
+                    ring[3] = make_int4(w.kvh, part_rows, 0, 0);
+                    mbar_arrive(bar(PIECE_FULL + slot));
+                    if (w.kvh < 0) alive = false;
+                }
+                // the next one, while this one is worked on; a small call has few pieces, which need no counter
+                if (alive) {
+                    index = p.head ? atomicAdd(&p.head->next, 1) : index + p.grid;
+                    derive(w, p.T);
+                    for (int s = 0; s < (w.wide ? 2 : 1) && alive; ++s) {
+                        if ((s ? w.n1 : w.n0) == 0) continue;
+                        alive = mbar_wait(bar(Q_EMPTY + s), (used[s] & 1) ^ 1, ab);
+                        if (!alive) break;
+                        ++used[s];
+                        mbar_arrive_expect_tx(bar(Q_FULL + s), (uint32_t)(p.T * p.G) * 256u);
+                        const uint32_t dst = sbase + kOffQ + s * kOperandBytes;
+                        tma_load_rows(dst, &tm_q, 0, w.kvh * p.G, w.x.row0 + s * p.T, bar(Q_FULL + s));
+                        tma_load_rows(dst + kHalfBytes, &tm_q, 64, w.kvh * p.G, w.x.row0 + s * p.T, bar(Q_FULL + s));
+                    }
+                }
+            }
+            alive = __shfl_sync(0xffffffffu, alive, 0);
+            index = __shfl_sync(0xffffffffu, index, 0);
+        }
+        if (lane == 0) {
             // copies in flight land before the CTA may end: the consumers wait for them, unless they gave up
             if (*ab.flag)
                 for (int s = 0; s < 2; ++s)
@@ -327,14 +427,18 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
         // The whole warp walks the loop and waits, so that addresses and descriptors stay in uniform registers; one
         // elected lane issues.  (A single lane that does everything spends more time preparing operands than the
         // tensor pipe needs for them: 4500 instead of 2900 clocks for a KV tile of both sides.)
-        const bool leader = elect_one();
+        // low and high words of the operands' descriptors: addresses count in units of 16 bytes in the low word
         const uint64_t q_desc = smem_desc(sbase + kOffQ, 16, 1024), k_desc = smem_desc(sbase + kOffK, 16, 2048), v_desc = smem_desc(sbase + kOffV, 1024, 2048);
+        const uint32_t q_lo = (uint32_t)q_desc, q_hi = (uint32_t)(q_desc >> 32), k_lo = (uint32_t)k_desc, k_hi = (uint32_t)(k_desc >> 32),
+                       v_lo = (uint32_t)v_desc, v_hi = (uint32_t)(v_desc >> 32);
+        const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);              // (a shuffle tells the compiler that the value is uniform)
         int k_slot = 0, k_round = 0, v_slot = 0, v_round = 0, q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
         bool alive = true;
         Work w;
         for (int it = 0; alive && next_piece(w, it, smem, bar0, lane, p.T, ab); ++it) {
-            const bool wide = w.wide;
-            const int n0 = w.n0, n1 = w.n1, n_max = max(n0, n1);
+            const bool wide = __shfl_sync(0xffffffffu, (int)w.wide, 0) != 0;
+            const int n0 = __shfl_sync(0xffffffffu, w.n0, 0), n1 = __shfl_sync(0xffffffffu, w.n1, 0), loads = __shfl_sync(0xffffffffu, w.loads, 0);
+            const int n_max = max(n0, n1);
             // S of side `s`, its jj-th tile
             auto scores = [&](auto side, int jj) {
                 constexpr int s = decltype(side)::value;
@@ -344,14 +448,14 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                 alive = alive && mbar_wait(bar(K_FULL + k_slot), k_round, ab);
                 if (!__all_sync(0xffffffffu, alive)) { alive = false; return; }
                 tc_fence_after();
-                // descriptors hold addresses in units of 16 bytes; Q: two 64-dim blocks of 128 rows, K: dim halves 1 KiB apart inside a page
-                const uint64_t qd = q_desc + (own_q ? s * kOperandBytes / 16 : 0), kd = k_desc + (uint32_t)(k_slot * (kOperandBytes / 16));
+                // Q: two 64-dim blocks of 128 rows, K: dim halves 1 KiB apart inside a page
+                const uint32_t qd = q_lo + (own_q ? s * kOperandBytes / 16 : 0), kd = k_lo + (uint32_t)(k_slot * (kOperandBytes / 16));
                 const bool last_k = s == 1 || !wide;                     // the last reader of a K or V tile, and of a Q tile, gives it back
-                const bool last_q = wide ? jj + 1 == n : 2 * jj + s + 1 == w.loads;
-                if (leader) {
+                const bool last_q = wide ? jj + 1 == n : 2 * jj + s + 1 == loads;
+                if (elect_one()) {
 #pragma unroll
                     for (int ks = 0; ks < 8; ++ks)
-                        umma_bf16(tmem + s * 128u, qd + ((ks >> 2) * kHalfBytes + (ks & 3) * 32) / 16, kd + ((ks >> 2) * 1024 + (ks & 3) * 32) / 16, idesc_qk, ks > 0);
+                        umma_ss(tm + s * 128u, qd + ((ks >> 2) * kHalfBytes + (ks & 3) * 32) / 16, q_hi, kd + ((ks >> 2) * 1024 + (ks & 3) * 32) / 16, k_hi, idesc_qk, ks > 0);
                     umma_commit(bar(S_FULL + s));
                     if (last_k) umma_commit(bar(K_EMPTY + k_slot));
                     if (last_q) umma_commit(bar(Q_EMPTY + (own_q ? s : 0)));
@@ -363,16 +467,16 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                 constexpr int s = decltype(side)::value;
                 const bool last_v = s == 1 || !wide, last = jj + 1 == (s ? n1 : n0);
                 alive = mbar_wait(bar(V_FULL + v_slot), v_round, ab);
-                const uint64_t vd = v_desc + (uint32_t)(v_slot * (kOperandBytes / 16));       // one page (16 tokens) per step
+                const uint32_t vd = v_lo + (uint32_t)(v_slot * (kOperandBytes / 16));       // one page (16 tokens) per step
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {       // the first 64 keys' probabilities are there before the others
                     alive = alive && mbar_wait(bar((half ? P_FULL : P_HALF) + s), p_phase[s], ab);
                     if (!__all_sync(0xffffffffu, alive)) { alive = false; return; }
                     tc_fence_after();
-                    if (leader) {
+                    if (elect_one()) {
 #pragma unroll
                         for (int ks = 4 * half; ks < 4 * half + 4; ++ks)
-                            umma_bf16_tmem_a(tmem + 256u + s * 128u, tmem + s * 128u + ks * 8u, vd + ks * 4096 / 16, idesc_pv, (jj > 0 || ks > 0) ? 1u : 0u);
+                            umma_ts(tm + 256u + s * 128u, tm + s * 128u + ks * 8u, vd + ks * 4096 / 16, v_hi, idesc_pv, ks > 0 || jj > 0);
                         if (half) {
                             if (last_v) umma_commit(bar(V_EMPTY + v_slot));
                             if (last) umma_commit(bar(O_FULL + s));
@@ -407,11 +511,13 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
         bool alive = true;
         for (int it = 0; alive; ++it) {
             int n, key0, step, limit, limit_min;
+            bool idle;
             {
                 Work w;
                 if (!next_piece<true>(w, it, smem, bar0, lane, p.T, ab)) break;
                 const int tok0 = w.wide ? side * p.T : 0;                           // first token of this side's rows
                 const int tl = ((warp & 3) * 32 + lane) / p.G, last = min(p.T, w.x.n_tok - tok0) - 1;
+                idle = (warp & 3) * 32 >= (last + 1) * p.G;                         // no row of this piece is this warp's
                 n = side ? w.n1 : w.n0;
                 step = w.wide ? kTile : 2 * kTile;
                 key0 = w.x.tile_begin * kTile + (w.wide ? 0 : side * kTile);
@@ -430,6 +536,11 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                 if (!alive) break;
                 phases ^= S_PHASE;
                 tc_fence_after();
+                if (idle) {                                 // (what its P rows hold reaches no row of the result)
+                    warp_arrive(bar(P_HALF + side), lane);
+                    warp_arrive(bar(P_FULL + side), lane);
+                    continue;
+                }
                 const bool masked = key0 + kTile > limit_min;               // uniform over the side
                 const int seen = limit - key0;
                 float sv[kTile];
@@ -500,7 +611,7 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                 const int4* src = reinterpret_cast<const int4*>(smem + kOffPiece + (it % kRingPiece) * kPieceBytes);
                 int4* dst = reinterpret_cast<int4*>(&w.x);
                 dst[0] = src[0]; dst[1] = src[1]; dst[2] = src[2];
-                w.kvh = src[3].x;
+                w.kvh = src[3].x; w.part_rows = src[3].y;
                 derive(w, p.T);
                 warp_arrive(bar(PIECE_EMPTY + it % kRingPiece), lane);
             }
@@ -545,7 +656,7 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
             f0 *= inv; f1 *= inv;
             const int rows = n_tok * p.G;                   // valid rows of this side
             // partial results of an entry: side 0's pieces, then side 1's
-            const size_t part0 = (size_t)w.kvh * p.head->rows_per_head + x.part_row + (side == 1 ? (size_t)x.parts * p.T * p.G : 0);
+            const size_t part0 = (size_t)w.kvh * w.part_rows + x.part_row + (side == 1 ? (size_t)x.parts * p.T * p.G : 0);
             const size_t part_at = part0 + (size_t)x.part * rows + L;
             const size_t row_head = (size_t)(x.row0 + tok0 + tl) * p.Hq + w.kvh * p.G + gl;
 #pragma unroll 1
@@ -579,37 +690,57 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
             __threadfence();
             asm volatile("barrier.cta.sync %0, %1;" ::"r"(1 + side), "n"(kSideThreads) : "memory");
             if ((tid & (kSideThreads - 1)) == 0) {
-                int* counter = p.arrived + ((size_t)w.kvh * p.head->entries + x.entry) * 2 + side;
-                misc[4 + side] = atomicAdd(counter, 1) == x.parts - 1;
+                unsigned* counter = p.arrived + ((size_t)x.entry * p.Hkv + w.kvh) * 2 + side;
+                misc[4 + side] = atomicInc(counter, (unsigned)x.parts - 1u) == (unsigned)x.parts - 1u;   // back to 0 for the next call
             }
             asm volatile("barrier.cta.sync %0, %1;" ::"r"(1 + side), "n"(kSideThreads) : "memory");
             if (misc[4 + side]) {
                 __threadfence();
+                // a unit is 8 columns of a row; four units and two parts at a time keep 16 loads in flight per thread
+                const int units = rows * (kHeadDim / 8);
 #pragma unroll 1
-                for (int u = tid & (kSideThreads - 1); u < rows * (kHeadDim / 8); u += kSideThreads) {
-                    const int row = u / (kHeadDim / 8), col = (u % (kHeadDim / 8)) * 8;
-                    float m = -INFINITY, l = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                for (int u0 = tid & (kSideThreads - 1); u0 < units; u0 += 4 * kSideThreads) {
+                    float m[4], l[4], acc[4][8];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        m[i] = -INFINITY; l[i] = 0.f;
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) acc[i][c] = 0.f;
+                    }
 #pragma unroll 2
                     for (int k = 0; k < x.parts; ++k) {
-                        const size_t at = part0 + (size_t)k * rows + row;
-                        const float2 ml = __ldcg(p.part_ml + at);
-                        const float4 a = __ldcg(reinterpret_cast<const float4*>(p.part_o + at * kHeadDim + col));
-                        const float4 b = __ldcg(reinterpret_cast<const float4*>(p.part_o + at * kHeadDim + col) + 1);
-                        if (ml.x == -INFINITY) continue;                    // that piece holds no key this row sees
-                        const float m_new = fmaxf(m, ml.x), fa = m == -INFINITY ? 0.f : ex2(m - m_new), fb = ex2(ml.x - m_new);
-                        const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+                        float2 ml[4];
+                        float4 va[4], vb[4];
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) acc[i] = acc[i] * fa + v[i] * fb;
-                        l = l * fa + ml.y * fb;
-                        m = m_new;
+                        for (int i = 0; i < 4; ++i) {
+                            const int u = min(u0 + i * kSideThreads, units - 1);
+                            const size_t at = part0 + (size_t)k * rows + u / (kHeadDim / 8);
+                            const float4* src = reinterpret_cast<const float4*>(p.part_o + at * kHeadDim + (u % (kHeadDim / 8)) * 8);
+                            ml[i] = __ldcg(p.part_ml + at); va[i] = __ldcg(src); vb[i] = __ldcg(src + 1);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            if (ml[i].x == -INFINITY) continue;             // that piece holds no key this row sees
+                            const float m_new = fmaxf(m[i], ml[i].x), fa = m[i] == -INFINITY ? 0.f : ex2(m[i] - m_new), fb = ex2(ml[i].x - m_new);
+                            const float v[8] = {va[i].x, va[i].y, va[i].z, va[i].w, vb[i].x, vb[i].y, vb[i].z, vb[i].w};
+#pragma unroll
+                            for (int c = 0; c < 8; ++c) acc[i][c] = acc[i][c] * fa + v[c] * fb;
+                            l[i] = l[i] * fa + ml[i].y * fb;
+                            m[i] = m_new;
+                        }
                     }
-                    const float scale = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) acc[i] *= scale;
-                    const int t = row / p.G;
-                    const size_t to = (size_t)(x.row0 + tok0 + t) * p.Hq + w.kvh * p.G + (row - t * p.G);
-                    store_out8(p, to, col, acc);
-                    if (col == 0 && p.lse) p.lse[to] = l == 0.f ? -INFINITY : m * 0.69314718055994530942f + logf(l);
+                    for (int i = 0; i < 4; ++i) {
+                        const int u = u0 + i * kSideThreads;
+                        if (u >= units) continue;
+                        const int row = u / (kHeadDim / 8), col = (u % (kHeadDim / 8)) * 8, t = row / p.G;
+                        const float scale = l[i] > 0.f ? 1.f / l[i] : (l[i] == 0.f ? 0.f : l[i]);
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) acc[i][c] *= scale;
+                        const size_t to = (size_t)(x.row0 + tok0 + t) * p.Hq + w.kvh * p.G + (row - t * p.G);
+                        store_out8(p, to, col, acc[i]);
+                        if (col == 0 && p.lse) p.lse[to] = l[i] == 0.f ? -INFINITY : m[i] * 0.69314718055994530942f + logf(l[i]);
+                    }
                 }
             }
             asm volatile("barrier.cta.sync %0, %1;" ::"r"(1 + side), "n"(kSideThreads) : "memory");   // the flag is free again

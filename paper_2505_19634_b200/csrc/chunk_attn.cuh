@@ -25,13 +25,14 @@ struct ChunkPiece {
 static_assert(sizeof(ChunkPiece) == 48, "read as three 16-byte words");
 
 constexpr int kChunkTile = 128;                       // KV tokens per tile
-constexpr int kChunkPartsPerSm = 4;                   // pieces with partial results that the workspace has room for, per SM
+constexpr int kChunkPartsPerSm = 4;                   // wide pieces with partial results that the workspace has room for, per SM
+constexpr int kChunkSmall = 32;                       // calls of up to so many entries are scheduled inside the attention kernel
 
 struct ChunkHead {
-    int pieces_per_head;
+    int pieces;        // per KV head
     int next;          // the next piece that nobody has taken yet
-    int rows_per_head; // partial-result rows of one KV head
-    int entries;
+    int part_rows;     // partial-result rows of one KV head
+    int pad;
 };
 
 struct ChunkParams {
@@ -40,10 +41,9 @@ struct ChunkParams {
     const int32_t* row_start;
     void* out;
     float* lse;                    // may be null
-    ChunkHead* head;
+    ChunkHead* head;               // null: small, see kChunkSmall
     ChunkPiece* pieces;
-    int2* entry_tiles;             // [entries] KV tiles and new tokens of each entry
-    int* arrived;                  // [Hkv][entries][2] pieces that have left their partial result
+    unsigned* arrived;             // [entries][Hkv][2] pieces that have left their partial result; the last one sets it back to 0
     float* part_o;                 // [part_rows][128]
     float2* part_ml;               // [part_rows] (max in log2 units, sum)
     int32_t* status;
@@ -55,6 +55,51 @@ struct ChunkParams {
     int out_dtype;
     float scale_log2;
 };
+
+// ---- what both places that make a schedule share (the reasons are in chunk_plan.cu) ----
+struct ChunkEntry { int b, row0, n_tok, limit0, keys, tiles, once; };
+
+// The `index`-th entry of branch b, whose rows start at `start` (c of them) and which holds `keys` tokens.
+__device__ __forceinline__ ChunkEntry chunk_entry(int T, int b, int index, int start, int c, int keys) {
+    const int tok0 = index * 2 * T;
+    ChunkEntry r;
+    r.b = b; r.row0 = start + tok0; r.n_tok = min(2 * T, c - tok0); r.keys = keys;
+    r.limit0 = keys - c + tok0 + 1;
+    r.tiles = ceil_div(min(keys, max(0, r.limit0 + r.n_tok - 1)), kChunkTile);
+    r.once = c <= 2 * T;
+    return r;
+}
+__device__ __forceinline__ ChunkPiece chunk_piece(const ChunkEntry& r, int e, int part, int parts, int part_row) {
+    ChunkPiece x;
+    x.branch = r.b; x.row0 = r.row0; x.n_tok = r.n_tok; x.limit0 = r.limit0; x.keys = r.keys;
+    x.tile_begin = (int)((long)r.tiles * part / parts); x.tile_end = (int)((long)r.tiles * (part + 1) / parts);
+    x.parts = parts; x.part = part; x.part_row = part_row; x.entry = e; x.once = r.once;
+    return x;
+}
+// A call whose row starts or lengths make no sense computes nothing.
+__device__ __forceinline__ bool chunk_branch_ok(const ChunkParams& p, int lo, int hi, int len) {
+    return lo >= 0 && hi >= lo && hi <= p.total_rows && len >= 0 && (long)p.prefix_len + len <= (long)p.max_blocks * kPage;
+}
+__device__ __forceinline__ int chunk_cost(const ChunkEntry& r, int T) { return r.tiles * (r.n_tok > T ? 2 : 1); }
+
+constexpr float kChunkGuide = 1.5f;
+constexpr int kChunkNoBound = 1 << 30;                // leaves every entry whole
+
+// How small the pieces of a call may become, `total` being the cost of all its entries per KV head: a sixteenth of a
+// CTA's share, but not less than six tiles, whose time is several times what a piece costs by itself; where a share is
+// less than that, about the share, so that every CTA has one piece.
+__device__ __forceinline__ int chunk_bound(const ChunkParams& p, float total) {
+    const float share = total * p.Hkv / p.grid;
+    return share < 6.f ? max(2, (int)ceilf(share)) : max(6, (int)(share / 16.f));
+}
+// Pieces of entry r when `left` per KV head is still to be handed out, its own cost included.  A wide piece's partial
+// result is 256 rows to write and to join, worth three times a narrow one's bound.
+__device__ __forceinline__ int chunk_cuts(const ChunkParams& p, const ChunkEntry& r, float left, int bound) {
+    if (bound == kChunkNoBound) return 1;
+    const bool wide = r.n_tok > p.T;
+    const float limit = fmaxf((float)(wide ? 3 * bound : bound), left * p.Hkv / (kChunkGuide * p.grid));
+    return max(1, min(r.tiles, (int)ceilf((float)(wide ? 2 * r.tiles : r.tiles) / limit)));
+}
 
 cudaError_t launch_chunk_plan(const ChunkParams& p, cudaStream_t st);
 cudaError_t launch_chunk_attn(const ChunkParams& p, const void* q, long q_stride, const void* k_pages, const void* v_pages, cudaStream_t st);

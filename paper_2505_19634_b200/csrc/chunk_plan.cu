@@ -1,11 +1,19 @@
 // The schedule of one chunk-attention call, worked out on the device by one CTA: entries, how their KV
 // tiles are cut into pieces, and the order in which the pieces are handed out.
 //
-// How long a piece may be is chosen so that the estimated time of the call is smallest: with C KV tiles per
-// piece at most, P pieces in all and an overhead of kOverhead tiles per piece, that is C + overhead where
-// every piece has a CTA of its own, and (all tiles + P x overhead) / CTAs + half a piece where they queue.
-// 32 values of C are tried, a warp each.  Pieces go out longest first within a KV head, and one KV head after
-// the other, so that CTAs that run at the same time read the same keys.
+// The unit of cost is one KV tile of a narrow entry; a wide entry's tile costs two (256 query rows instead of
+// 128).  First come the branches with wide entries, then the others; a branch's last (costliest) entry goes
+// first, and all KV heads of a piece one after the other, so that CTAs that run at the same time read
+// neighbouring keys.  An entry is cut so that no
+// piece costs more than the work that is still to be handed out when its turn comes, divided by kChunkGuide x
+// CTAs: early pieces are whole entries, later ones smaller and smaller, down to the call's bound
+// (chunk_bound), and all CTAs end within about one small piece of each other.  With whole entries alone the
+// last CTA ended 8 % behind the mean at 8192 new tokens over 24576 (1280 entries for 148 CTAs), 30 % behind it
+// with 64 single tokens over 1 k to 8 k keys.  Everything here is a function of the lengths alone: the cuts,
+// and with them the results, do not depend on timing.
+//
+// The kernel is latency: its code runs once, cold.  Sorting the entries and trying 32 bounds took 15 us where
+// this takes about 6, for no better balance.
 #include "chunk_attn.cuh"
 #include "launch.cuh"
 
@@ -14,145 +22,127 @@ namespace tts {
 namespace {
 
 constexpr int kThreads = 1024;
-constexpr int kBuckets = 1024;                        // pieces are ordered by their entry's KV tiles
-constexpr float kOverhead = 1.5f, kSplitOverhead = 2.5f;   // in KV tiles; the second: of a piece that leaves a partial result
-// into how many pieces the longest entry is cut
-__constant__ int kCuts[32] = {1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 12, 14, 16, 18, 20, 24, 28, 32, 37, 42, 49, 56, 64, 74, 86, 99, 114, 132, 148, 170, 222, 296};
+constexpr int kPer = 2;                               // entries per thread
+constexpr int kMaxCut = kThreads * kPer;              // calls with more entries do not cut them: 14 and more per CTA even
+                                                      // themselves out
 
-__device__ int block_scan(int v, int* sums, int* total) {
+struct Scan { unsigned long long warp[33]; };
+
+__device__ unsigned long long block_scan(unsigned long long v, Scan& sc, unsigned long long* total) {       // exclusive, over the block
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int s = v;
+    unsigned long long s = v;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) { const int n = __shfl_up_sync(0xffffffffu, s, o); if (lane >= o) s += n; }
+    for (int o = 1; o < 32; o <<= 1) { const unsigned long long n = __shfl_up_sync(0xffffffffu, s, o); if (lane >= o) s += n; }
     __syncthreads();
-    if (lane == 31) sums[warp] = s;
+    if (lane == 31) sc.warp[warp] = s;
     __syncthreads();
     if (warp == 0) {
-        const int w = sums[lane];
-        int t = w;
+        const unsigned long long w = sc.warp[lane];
+        unsigned long long t = w;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) { const int n = __shfl_up_sync(0xffffffffu, t, o); if (lane >= o) t += n; }
-        sums[lane] = t - w;
-        if (lane == 31) sums[32] = t;
+        for (int o = 1; o < 32; o <<= 1) { const unsigned long long n = __shfl_up_sync(0xffffffffu, t, o); if (lane >= o) t += n; }
+        sc.warp[lane] = t - w;
+        if (lane == 31) sc.warp[32] = t;
     }
     __syncthreads();
-    *total = sums[32];
-    return sums[warp] + s - v;
+    *total = sc.warp[32];
+    return sc.warp[warp] + s - v;
+}
+
+struct Branches {
+    int first[2][kMaxBranches + 1];                    // entries ahead of branch b's among those of its kind: narrow (0), wide (1)
+    int start[kMaxBranches + 1], keys[kMaxBranches];
+};
+
+__device__ ChunkEntry entry_of(const ChunkParams& p, const Branches& br, int e, int n_wide) {
+    const int* first = br.first[e < n_wide];
+    const int at = e < n_wide ? e : e - n_wide;
+    int lo = 0, hi = p.n_branches - 1;                 // the last branch whose first entry is at or before this one
+    while (lo < hi) { const int mid = (lo + hi + 1) >> 1; if (first[mid] <= at) lo = mid; else hi = mid - 1; }
+    return chunk_entry(p.T, lo, first[lo + 1] - 1 - at, br.start[lo], br.start[lo + 1] - br.start[lo], br.keys[lo]);
+}
+
+__device__ void write_pieces(const ChunkParams& p, const ChunkEntry& r, int e, int k, int at, int part_row) {
+#pragma unroll 1
+    for (int i = 0; i < k; ++i) {
+        const ChunkPiece x = chunk_piece(r, e, i, k, part_row);
+        const int4* src = reinterpret_cast<const int4*>(&x);
+        int4* dst = reinterpret_cast<int4*>(p.pieces + at + i);
+        dst[0] = src[0]; dst[1] = src[1]; dst[2] = src[2];
+    }
 }
 
 __global__ void __launch_bounds__(kThreads)
 chunk_plan_kernel(const ChunkParams p) {
     grid_dependency_wait();
     grid_launch_dependents();
-    __shared__ int first[kMaxBranches + 1];            // first entry of each branch
-    __shared__ int bucket[kBuckets];
-    __shared__ int sums[33];
-    __shared__ float est[32];
-    __shared__ int bad, longest, shortest, rows_used;
-    __shared__ unsigned long long tiles_sum;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    if (tid == 0) { bad = 0; longest = 0; shortest = 0x7fffffff; rows_used = 0; tiles_sum = 0; }
-    for (int i = tid; i < kBuckets; i += kThreads) bucket[i] = 0;
-    __syncthreads();
+    __shared__ Branches br;
+    __shared__ Scan sc;
+    const int tid = threadIdx.x;
 
-    // entries of each branch; a call whose row starts or lengths make no sense computes nothing
+    // entries of each branch
     int n_mine = 0;
+    bool bad = false;
     if (tid < p.n_branches) {
         const int lo = p.row_start[tid], hi = p.row_start[tid + 1], L = p.branch_lens[tid];
-        if (lo < 0 || hi < lo || hi > p.total_rows || L < 0 || (long)p.prefix_len + L > (long)p.max_blocks * kPage) bad = 1;
-        else n_mine = ceil_div(hi - lo, 2 * p.T);
+        br.start[tid] = lo; br.keys[tid] = p.prefix_len + L;
+        if (tid == p.n_branches - 1) br.start[p.n_branches] = hi;
+        bad = !chunk_branch_ok(p, lo, hi, L);
+        n_mine = ceil_div(hi - lo, 2 * p.T);
     }
-    __syncthreads();
-    if (bad) n_mine = 0;
-    int n_entries;
-    const int at = block_scan(n_mine, sums, &n_entries);
-    if (tid < p.n_branches) first[tid] = at;
+    bad = __syncthreads_or(bad);                       // then nothing is computed
+    unsigned long long sum;
+    const bool wide = tid < p.n_branches && br.start[tid] + p.T < p.row_start[tid + 1];
+    const unsigned long long at_branch = block_scan(bad ? 0ull : (unsigned long long)n_mine << (wide ? 32 : 0), sc, &sum);
+    const int n_wide = (int)(sum >> 32), n = (int)(sum & 0xffffffffu) + n_wide;
+    if (tid <= p.n_branches) { br.first[0][tid] = (int)(at_branch & 0xffffffffu); br.first[1][tid] = (int)(at_branch >> 32); }
     if (tid == 0) {
-        first[p.n_branches] = n_entries;
+        if (p.n_branches == kThreads) { br.first[0][kThreads] = n - n_wide; br.first[1][kThreads] = n_wide; }
+        p.head->next = p.grid;
         if (bad) atomicMin(p.status, (int)TTS_ERR_DEVICE_BOUNDS);
     }
     __syncthreads();
-
-    struct Entry { int b, row0, n_tok, limit0, keys, tiles, once; };
-    auto entry = [&](int e) {
-        int lo = 0, hi = p.n_branches - 1;             // the last branch whose first entry is <= e
-        while (lo < hi) { const int mid = (lo + hi + 1) >> 1; if (first[mid] <= e) lo = mid; else hi = mid - 1; }
-        const int start = p.row_start[lo], c = p.row_start[lo + 1] - start, tok0 = (e - first[lo]) * 2 * p.T;
-        Entry r;
-        r.b = lo; r.row0 = start + tok0; r.n_tok = min(2 * p.T, c - tok0);
-        r.keys = p.prefix_len + p.branch_lens[lo];
-        r.limit0 = r.keys - c + tok0 + 1;
-        r.tiles = ceil_div(min(r.keys, max(0, r.limit0 + r.n_tok - 1)), kChunkTile);
-        r.once = c <= 2 * p.T;
-        return r;
-    };
-    {
-        int mx = 0, mn = 0x7fffffff;
-        long sum = 0;
-        for (int e = tid; e < n_entries; e += kThreads) {
-            const Entry r = entry(e);
-            const int n = r.tiles;
-            p.entry_tiles[e] = make_int2(n, r.n_tok);
-            mx = max(mx, n); mn = min(mn, n); sum += n;
-        }
-        if (tid < n_entries) { atomicMax(&longest, mx); atomicMin(&shortest, mn); atomicAdd(&tiles_sum, (unsigned long long)sum); }
-        for (long i = tid; i < 2l * n_entries * p.Hkv; i += kThreads) p.arrived[i] = 0;
+    if (n > kMaxCut) {
+#pragma unroll 1
+        for (int e = tid; e < n; e += kThreads) write_pieces(p, entry_of(p, br, e, n_wide), e, 1, e, 0);
+        if (tid == 0) { p.head->pieces = n; p.head->part_rows = 0; }
+        return;
     }
-    __syncthreads();
 
-    // the length of a piece
-    {
-        const int C = max(1, ceil_div(longest, kCuts[warp]));
-        long pieces = 0, rows = 0;
-        for (int e = lane; e < n_entries; e += 32) {
-            const int2 t = p.entry_tiles[e];
-            const int k = max(1, ceil_div(t.x, C));
-            pieces += k;
-            if (k > 1) rows += (long)k * t.y * p.G;
-        }
+    ChunkEntry r[kPer];
+    int cost[kPer] = {0, 0};
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) { pieces += __shfl_xor_sync(0xffffffffu, pieces, o); rows += __shfl_xor_sync(0xffffffffu, rows, o); }
-        if (lane == 0) {
-            const float over = kOverhead + (C < longest ? kSplitOverhead : 0.f);
-            const float P = (float)pieces * p.Hkv, avg = ((float)tiles_sum * p.Hkv + P * over) / p.grid;
-            float t;
-            if (P <= p.grid) t = C + over;
-            else if (longest == shortest) t = ceilf(P / p.grid) * (C + over);
-            else t = avg + 0.5f * (C + over);
-            const bool fits = warp == 0 || (pieces <= p.max_pieces && rows * p.Hkv <= p.part_rows);
-            est[warp] = fits ? t : 3.0e38f;
+    for (int i = 0; i < kPer; ++i)
+        if (kPer * tid + i < n) { r[i] = entry_of(p, br, kPer * tid + i, n_wide); cost[i] = chunk_cost(r[i], p.T); }
+    const unsigned long long ahead = block_scan((unsigned)cost[0] + (unsigned)cost[1], sc, &sum);
+    const float total = (float)sum, left[kPer] = {(float)(sum - ahead), (float)(sum - ahead - cost[0])};
+    int bound = chunk_bound(p, total);
+    for (;;) {
+        int k[kPer] = {0, 0};
+        unsigned long long mine = 0;                   // pieces, and from bit 20 on partial-result rows
+        int rows0 = 0;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+            if (kPer * tid + i < n) {
+                k[i] = chunk_cuts(p, r[i], left[i], bound);
+                const int rows = k[i] > 1 ? k[i] * r[i].n_tok * p.G : 0;
+                if (i == 0) rows0 = rows;
+                mine += (unsigned)k[i] + ((unsigned long long)rows << 20);
+            }
+        const unsigned long long at = block_scan(mine, sc, &sum);
+        const int pieces = (int)(sum & 0xfffffu);
+        const long rows = (long)(sum >> 20);
+        if (bound != kChunkNoBound && (pieces > p.max_pieces || rows * p.Hkv > p.part_rows)) {
+            bound = bound >= 4096 ? kChunkNoBound : bound * 4;        // too much for the workspace: larger pieces
+            continue;
         }
+        const int at0 = (int)(at & 0xfffffu), row0 = (int)(at >> 20);
+        if (k[0] > 0) write_pieces(p, r[0], kPer * tid, k[0], at0, row0);
+        if (k[1] > 0) write_pieces(p, r[1], kPer * tid + 1, k[1], at0 + k[0], row0 + rows0);
+        if (tid == 0) { p.head->pieces = pieces; p.head->part_rows = (int)rows; }
+        break;
     }
-    __syncthreads();
-    int best = 0;
-    for (int i = 1; i < 32; ++i) if (est[i] < est[best]) best = i;
-    const int C = max(1, ceil_div(longest, kCuts[best]));
-
-    // places: longest entries first
-    for (int e = tid; e < n_entries; e += kThreads)
-        atomicAdd(&bucket[kBuckets - 1 - min(p.entry_tiles[e].x, kBuckets - 1)], max(1, ceil_div(p.entry_tiles[e].x, C)));
-    __syncthreads();
-    int total;
-    const int place = block_scan(bucket[tid], sums, &total);
-    bucket[tid] = place;
-    __syncthreads();
-    for (int e = tid; e < n_entries; e += kThreads) {
-        const Entry r = entry(e);
-        const int k = max(1, ceil_div(r.tiles, C));
-        const int at_piece = atomicAdd(&bucket[kBuckets - 1 - min(r.tiles, kBuckets - 1)], k);
-        const int part_row = k > 1 ? atomicAdd(&rows_used, k * r.n_tok * p.G) : 0;
-        for (int i = 0; i < k; ++i) {
-            ChunkPiece x;
-            x.branch = r.b; x.row0 = r.row0; x.n_tok = r.n_tok; x.limit0 = r.limit0; x.keys = r.keys;
-            x.tile_begin = (int)((long)r.tiles * i / k); x.tile_end = (int)((long)r.tiles * (i + 1) / k);
-            x.parts = k; x.part = i; x.part_row = part_row; x.entry = e; x.once = r.once;
-            p.pieces[at_piece + i] = x;
-        }
-    }
-    __syncthreads();
-    if (tid == 0) { p.head->pieces_per_head = total; p.head->next = p.grid; p.head->rows_per_head = rows_used; p.head->entries = n_entries; }
 }
-static_assert(kBuckets == kThreads, "one bucket per thread in the scan");
 
 }  // namespace
 

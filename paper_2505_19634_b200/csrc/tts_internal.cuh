@@ -296,10 +296,11 @@ struct Ctx {
     void* tmap_cache;                  // opaque: tensor maps keyed by pool pointer
     // cache operators
     int32_t* page_work;                // PageWork (kv_pages.cu)
-    struct ChunkHead* chunk_head; struct ChunkPiece* chunk_pieces; int2* chunk_entries; int* chunk_arrived;   // chunk attention,
+    struct ChunkHead* chunk_head; struct ChunkPiece* chunk_pieces; unsigned* chunk_arrived;   // chunk attention,
     float* chunk_part_o; float2* chunk_part_ml;                                                               // from tts_chunk_reserve on
-    int chunk_rows, chunk_max_entries, chunk_max_pieces;
+    int chunk_rows, chunk_max_pieces;
     long chunk_part_rows;
+    size_t chunk_arrived_bytes;
     // profiling aid
     int profiling, prof_n;
     cudaEvent_t* prof_ev;              // 3 events per recorded call
