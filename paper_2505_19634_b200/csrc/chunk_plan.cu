@@ -2,9 +2,9 @@
 // tiles are cut into pieces, and the order in which the pieces are handed out.
 //
 // The unit of cost is one KV tile of a narrow entry; a wide entry's tile costs two (256 query rows instead of
-// 128).  First come the branches with wide entries, then the others; a branch's last (costliest) entry goes
-// first, and all KV heads of a piece one after the other, so that CTAs that run at the same time read
-// neighbouring keys.  An entry is cut so that no
+// 128).  Entries are handed out in four classes of cost, the costliest first, and within a class branch by
+// branch, all KV heads of a piece one after the other, so that CTAs that run at the same time read neighbouring
+// keys.  An entry is cut so that no
 // piece costs more than the work that is still to be handed out when its turn comes, divided by kChunkGuide x
 // CTAs: early pieces are whole entries, later ones smaller and smaller, down to the call's bound
 // (chunk_bound), and all CTAs end within about one small piece of each other.  With whole entries alone the
@@ -13,7 +13,7 @@
 // and with them the results, do not depend on timing.
 //
 // The kernel is latency: its code runs once, cold.  Sorting the entries and trying 32 bounds took 15 us where
-// this takes about 6, for no better balance.
+// this takes 7, for no better balance.
 #include "chunk_attn.cuh"
 #include "launch.cuh"
 
@@ -50,16 +50,14 @@ __device__ unsigned long long block_scan(unsigned long long v, Scan& sc, unsigne
 }
 
 struct Branches {
-    int first[2][kMaxBranches + 1];                    // entries ahead of branch b's among those of its kind: narrow (0), wide (1)
+    int first[kMaxBranches + 1];                       // first entry of each branch
     int start[kMaxBranches + 1], keys[kMaxBranches];
 };
 
-__device__ ChunkEntry entry_of(const ChunkParams& p, const Branches& br, int e, int n_wide) {
-    const int* first = br.first[e < n_wide];
-    const int at = e < n_wide ? e : e - n_wide;
+__device__ ChunkEntry entry_of(const ChunkParams& p, const Branches& br, int e) {
     int lo = 0, hi = p.n_branches - 1;                 // the last branch whose first entry is at or before this one
-    while (lo < hi) { const int mid = (lo + hi + 1) >> 1; if (first[mid] <= at) lo = mid; else hi = mid - 1; }
-    return chunk_entry(p.T, lo, first[lo + 1] - 1 - at, br.start[lo], br.start[lo + 1] - br.start[lo], br.keys[lo]);
+    while (lo < hi) { const int mid = (lo + hi + 1) >> 1; if (br.first[mid] <= e) lo = mid; else hi = mid - 1; }
+    return chunk_entry(p.T, lo, br.first[lo + 1] - 1 - e, br.start[lo], br.start[lo + 1] - br.start[lo], br.keys[lo]);
 }
 
 __device__ void write_pieces(const ChunkParams& p, const ChunkEntry& r, int e, int k, int at, int part_row) {
@@ -78,7 +76,10 @@ chunk_plan_kernel(const ChunkParams p) {
     grid_launch_dependents();
     __shared__ Branches br;
     __shared__ Scan sc;
+    __shared__ unsigned short order[kMaxCut];
+    __shared__ int largest;
     const int tid = threadIdx.x;
+    if (tid == 0) largest = 0;
 
     // entries of each branch
     int n_mine = 0;
@@ -92,28 +93,58 @@ chunk_plan_kernel(const ChunkParams p) {
     }
     bad = __syncthreads_or(bad);                       // then nothing is computed
     unsigned long long sum;
-    const bool wide = tid < p.n_branches && br.start[tid] + p.T < p.row_start[tid + 1];
-    const unsigned long long at_branch = block_scan(bad ? 0ull : (unsigned long long)n_mine << (wide ? 32 : 0), sc, &sum);
-    const int n_wide = (int)(sum >> 32), n = (int)(sum & 0xffffffffu) + n_wide;
-    if (tid <= p.n_branches) { br.first[0][tid] = (int)(at_branch & 0xffffffffu); br.first[1][tid] = (int)(at_branch >> 32); }
+    const int at_branch = (int)block_scan(bad ? 0 : n_mine, sc, &sum);
+    const int n = (int)sum;
+    if (tid < p.n_branches) br.first[tid] = at_branch;
     if (tid == 0) {
-        if (p.n_branches == kThreads) { br.first[0][kThreads] = n - n_wide; br.first[1][kThreads] = n_wide; }
+        br.first[p.n_branches] = n;
         p.head->next = p.grid;
         if (bad) atomicMin(p.status, (int)TTS_ERR_DEVICE_BOUNDS);
     }
     __syncthreads();
     if (n > kMaxCut) {
 #pragma unroll 1
-        for (int e = tid; e < n; e += kThreads) write_pieces(p, entry_of(p, br, e, n_wide), e, 1, e, 0);
+        for (int e = tid; e < n; e += kThreads) write_pieces(p, entry_of(p, br, e), e, 1, e, 0);
         if (tid == 0) { p.head->pieces = n; p.head->part_rows = 0; }
         return;
     }
 
-    ChunkEntry r[kPer];
-    int cost[kPer] = {0, 0};
+    // classes of cost: above three quarters of the largest, above a half, above a quarter, the rest
+    int mine[kPer], most = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        mine[i] = kPer * tid + i < n ? chunk_cost(entry_of(p, br, kPer * tid + i), p.T) : -1;
+        most = max(most, mine[i]);
+    }
+    most = __reduce_max_sync(0xffffffffu, most);
+    if ((tid & 31) == 0) atomicMax(&largest, most);
+    __syncthreads();
+    unsigned long long in_class = 0;                   // 16 bits for each class
+    int cls[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        cls[i] = 3 - min(3, (int)(4.f * mine[i] / (largest + 1)));
+        if (mine[i] >= 0) in_class += 1ull << (16 * cls[i]);
+    }
+    unsigned long long at_class = block_scan(in_class, sc, &sum);
+    at_class += (sum << 16) + (sum << 32) + (sum << 48);         // each class begins where those before it end
 #pragma unroll
     for (int i = 0; i < kPer; ++i)
-        if (kPer * tid + i < n) { r[i] = entry_of(p, br, kPer * tid + i, n_wide); cost[i] = chunk_cost(r[i], p.T); }
+        if (mine[i] >= 0) {
+            order[at_class >> (16 * cls[i]) & 0xffffu] = (unsigned short)(kPer * tid + i);
+            at_class += 1ull << (16 * cls[i]);
+        }
+    __syncthreads();
+
+    ChunkEntry r[kPer];
+    int e[kPer], cost[kPer] = {0, 0};
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+        if (kPer * tid + i < n) {
+            e[i] = order[kPer * tid + i];
+            r[i] = entry_of(p, br, e[i]);
+            cost[i] = chunk_cost(r[i], p.T);
+        }
     const unsigned long long ahead = block_scan((unsigned)cost[0] + (unsigned)cost[1], sc, &sum);
     const float total = (float)sum, left[kPer] = {(float)(sum - ahead), (float)(sum - ahead - cost[0])};
     int bound = chunk_bound(p, total);
@@ -137,8 +168,8 @@ chunk_plan_kernel(const ChunkParams p) {
             continue;
         }
         const int at0 = (int)(at & 0xfffffu), row0 = (int)(at >> 20);
-        if (k[0] > 0) write_pieces(p, r[0], kPer * tid, k[0], at0, row0);
-        if (k[1] > 0) write_pieces(p, r[1], kPer * tid + 1, k[1], at0 + k[0], row0 + rows0);
+        if (k[0] > 0) write_pieces(p, r[0], e[0], k[0], at0, row0);
+        if (k[1] > 0) write_pieces(p, r[1], e[1], k[1], at0 + k[0], row0 + rows0);
         if (tid == 0) { p.head->pieces = pieces; p.head->part_rows = (int)rows; }
         break;
     }
