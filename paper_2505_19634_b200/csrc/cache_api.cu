@@ -240,7 +240,7 @@ int tts_kv_compact(tts_ctx* ctx, int n_layers, void* const* k_pools, void* const
     Ctx* c = reinterpret_cast<Ctx*>(ctx);
     PagePools pools;
     if (!c || !page_refs || !new_table || !new_refs || !page_map || !n_used || !branches_ok(c, block_table, 0, n_branches)) return TTS_ERR_INVALID;
-    if (!aligned16(page_refs) || !aligned4(new_table) || !aligned16(new_refs) || !aligned4(page_map) || !aligned4(n_used)) return TTS_ERR_INVALID;
+    if (!aligned16(page_refs) || !aligned4(new_table) || !aligned16(new_refs) || !aligned16(page_map) || !aligned4(n_used)) return TTS_ERR_INVALID;
     if (!pools_from(n_layers, k_pools, v_pools, &pools)) return TTS_ERR_INVALID;
     const tts_config& f = c->cfg;
     const size_t table = (size_t)n_branches * f.max_blocks_per_branch * 4, refs = (size_t)f.num_pages * 4;

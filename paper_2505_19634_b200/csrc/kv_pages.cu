@@ -64,13 +64,13 @@ __device__ __forceinline__ void load_refs(const int32_t* refs, int num_pages, lo
 }
 
 // The `need` lowest pages without a reference, ascending, into `list` (global).  Returns whether there are as
-// many.  All threads of the block; ends with the list visible to the block.
-__device__ bool lowest_free(const int32_t* refs, int num_pages, int need, int32_t* list, int* warp_sums) {
+// many.  `r`: the counts of this thread's first kPerThread pages, which the caller has asked for ahead of its
+// own chain of loads.  All threads of the block; ends with the list visible to the block.
+__device__ bool lowest_free(const int32_t* refs, int num_pages, int need, int32_t* list, int* warp_sums, int (&r)[kPerThread]) {
     int found = 0;
     for (long base = 0; base < num_pages && found < need; base += kScanThreads * kPerThread) {
-        int r[kPerThread];
         const long first = base + (long)threadIdx.x * kPerThread;
-        load_refs(refs, num_pages, first, 1, r);
+        if (base > 0) load_refs(refs, num_pages, first, 1, r);
         int n = 0;
 #pragma unroll
         for (int i = 0; i < kPerThread; ++i) n += r[i] == 0;
@@ -137,6 +137,8 @@ fork_plan_kernel(const int32_t* __restrict__ table, int max_blocks, int prefix_l
     __shared__ int first[kMaxBranches];                 // lowest child of each parent
     __shared__ int sums[33];
     const int c = threadIdx.x;
+    int free_refs[kPerThread];
+    load_refs(refs, num_pages, (long)c * kPerThread, 1, free_refs);
     for (int i = c; i < n_branches; i += kScanThreads) first[i] = 0x7fffffff;
     __syncthreads();
     int p = -1, len = 0;
@@ -159,7 +161,7 @@ fork_plan_kernel(const int32_t* __restrict__ table, int max_blocks, int prefix_l
     }
     int need;
     const int rank = block_scan(src >= 0, sums, &need);
-    const bool ok = lowest_free(refs, num_pages, need, wk.list_dst, sums);
+    const bool ok = lowest_free(refs, num_pages, need, wk.list_dst, sums, free_refs);
     if (c == 0) {
         wk.head[0] = ok ? need : 0;
         wk.head[1] = ok;
@@ -224,6 +226,8 @@ grow_kernel(int32_t* table, int max_blocks, int prefix_len, int32_t* lens, const
     __shared__ int bad;
     const int b = threadIdx.x;
     if (b == 0) bad = 0;
+    int free_refs[kPerThread];
+    load_refs(refs, num_pages, (long)b * kPerThread, 1, free_refs);
     __syncthreads();
     int lo = 0, hi = 0, more = 0, len = 0;
     if (b < n_branches) {
@@ -239,7 +243,7 @@ grow_kernel(int32_t* table, int max_blocks, int prefix_len, int32_t* lens, const
     if (bad) { if (b == 0) atomicMin(status, (int)TTS_ERR_DEVICE_BOUNDS); return; }
     int need;
     int at = block_scan(want, sums, &need);
-    if (!lowest_free(refs, num_pages, need, wk.list_dst, sums)) { if (b == 0) atomicMin(status, (int)TTS_ERR_DEVICE_PAGES); return; }
+    if (!lowest_free(refs, num_pages, need, wk.list_dst, sums, free_refs)) { if (b == 0) atomicMin(status, (int)TTS_ERR_DEVICE_PAGES); return; }
     for (int i = lo; i < hi; ++i)
         if (row[i] < 0) {
             const int page = wk.list_dst[at++];
@@ -273,9 +277,8 @@ compact_plan_kernel(const int32_t* refs, int32_t* new_refs, int num_pages, int32
     grid_dependency_wait();
     grid_launch_dependents();
     __shared__ int sums[33];
-    int mine = 0, used;
+    int mine = 0, used, r[kPerThread];
     for (long base = (long)threadIdx.x * kPerThread; base < num_pages; base += kScanThreads * kPerThread) {
-        int r[kPerThread];
         load_refs(refs, num_pages, base, 0, r);
 #pragma unroll
         for (int i = 0; i < kPerThread; ++i) mine += r[i] > 0;
@@ -283,9 +286,9 @@ compact_plan_kernel(const int32_t* refs, int32_t* new_refs, int num_pages, int32
     block_scan(mine, sums, &used);
     int holes = 0, movers = 0;
     for (long base = 0; base < num_pages; base += kScanThreads * kPerThread) {
-        int r[kPerThread];
         const long first = base + (long)threadIdx.x * kPerThread;
-        load_refs(refs, num_pages, first, 0, r);
+        if (num_pages > kScanThreads * kPerThread) load_refs(refs, num_pages, first, 0, r);
+        else if (first >= num_pages) { for (int i = 0; i < kPerThread; ++i) r[i] = 0; }      // (else they are still at hand)
         int hole = 0, mover = 0;
 #pragma unroll
         for (int i = 0; i < kPerThread; ++i) {
@@ -299,13 +302,29 @@ compact_plan_kernel(const int32_t* refs, int32_t* new_refs, int num_pages, int32
 #pragma unroll
         for (int i = 0; i < kPerThread; ++i) {
             const long p = first + i;
-            if (p >= num_pages) break;
             if (p < used && r[i] <= 0) wk.list_dst[at_h++] = (int)p;
             if (p >= used && r[i] > 0) wk.list_src[at_m++] = (int)p;
-            page_map[p] = r[i] > 0 ? (int)p : -1;       // movers are entered below
-            if (new_refs != refs) new_refs[p] = r[i] > 0 && p < used ? r[i] : 0;
         }
         holes += total_h; movers += total_m;
+    }
+    // the map and the counts of the pages that stay, in coalesced steps of four pages per thread; movers follow
+    for (long p = (long)threadIdx.x * 4; p < num_pages; p += kScanThreads * 4) {
+        if (p + 4 <= num_pages) {
+            const int4 c = *reinterpret_cast<const int4*>(refs + p);
+            const int v[4] = {c.x, c.y, c.z, c.w};
+            int m[4], k[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { const bool stays = v[i] > 0 && p + i < used; m[i] = stays ? (int)p + i : -1; k[i] = stays ? v[i] : 0; }
+            *reinterpret_cast<int4*>(page_map + p) = make_int4(m[0], m[1], m[2], m[3]);
+            if (new_refs != refs) *reinterpret_cast<int4*>(new_refs + p) = make_int4(k[0], k[1], k[2], k[3]);
+        } else {
+            for (long i = p; i < num_pages; ++i) {
+                const int v = refs[i];
+                const bool stays = v > 0 && i < used;
+                page_map[i] = stays ? (int)i : -1;
+                if (new_refs != refs) new_refs[i] = stays ? v : 0;
+            }
+        }
     }
     __syncthreads();
     for (int k = threadIdx.x; k < movers; k += kScanThreads) {

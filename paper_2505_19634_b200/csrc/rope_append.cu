@@ -11,7 +11,8 @@
 // Bound by HBM: q, k and v are read once, q, K and V written once; there is no reuse between rows.  Eight
 // lanes handle one head vector, each two 16-byte chunks that hold both members of its pairs, so a rotation
 // needs no exchange between lanes; a lane's eight sines and cosines serve all heads of the row that its
-// warp walks through, four heads at a time.
+// warp walks through, sixteen at a time, whose loads are issued before the row's branch, page and angles are
+// looked up.
 #include "launch.cuh"
 #include "tts_internal.cuh"
 
@@ -21,6 +22,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
+constexpr int kBatch = 4;                              // head vectors that a group of eight lanes has in flight
 
 // The branch whose rows [row_start[b], row_start[b+1]) hold `row`, or -1: the whole warp looks at 32 starts
 // per step (two steps for up to 1024 branches).
@@ -71,9 +73,28 @@ append_rope_kernel(const __grid_constant__ RopeParams p) {
     const int vectors = p.Hq + 2 * p.Hkv;
     for (long w = blockIdx.x * (long)kWarps + (threadIdx.x >> 5); w < (long)p.total_rows * p.parts; w += (long)gridDim.x * kWarps) {
         const int row = (int)(w / p.parts), part = (int)(w - (long)row * p.parts);
+        const int step = p.parts * 4;
+        auto source = [&](int h) -> const __nv_bfloat16* {
+            return h < p.Hq ? p.q + (size_t)row * p.q_stride + (size_t)h * kHeadDim
+                 : h < p.Hq + p.Hkv ? p.k + (size_t)row * p.kv_stride + (size_t)(h - p.Hq) * kHeadDim
+                                    : p.v + (size_t)row * p.kv_stride + (size_t)(h - p.Hq - p.Hkv) * kHeadDim;
+        };
+        uint4 lo4[kBatch], hi4[kBatch];
+        auto load = [&](int h0) {                       // kBatch head vectors per group of eight lanes, before anything else is waited for
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                const int h = h0 + i * step + group;
+                lo4[i] = hi4[i] = make_uint4(0, 0, 0, 0);
+                if (h < vectors) {
+                    const uint4* src = reinterpret_cast<const uint4*>(source(h));
+                    lo4[i] = src[sub]; hi4[i] = src[sub + 8];
+                }
+            }
+        };
+        if (kMode != 2) load(part * 4);
+        // where the row's key and value go
         const int b = branch_of_row(p.row_start, p.n_branches, row, lane);
         if (b < 0) continue;                            // a row of no branch: left as it is
-        // where the row's key and value go
         const int start = p.row_start[b], c = p.row_start[b + 1] - start, L = p.branch_lens[b];
         const long tok = (long)p.prefix_len + L - c + (row - start);
         int page = -1;
@@ -81,30 +102,46 @@ append_rope_kernel(const __grid_constant__ RopeParams p) {
         const bool store_kv = page >= 0 && page < p.num_pages;
         if (!store_kv && lane == 0) atomicMin(p.status, (int)TTS_ERR_DEVICE_BOUNDS);
 
-        // mode 0 and 2: chunk sub holds the low members of pairs 8 sub .. 8 sub + 7 (mode 2: where there are
-        // such pairs); mode 1: chunk sub holds pairs 4 sub .. + 3 and chunk sub + 8 pairs 32 + 4 sub .. + 3
-        float cs[8], sn[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int pair = kMode == 1 ? (i < 4 ? 4 * sub + i : 32 + 4 * sub + i - 4) : 8 * sub + i;
+        auto angle = [&](int pair, float& s, float& co) {
             double t = (double)p.positions[(size_t)axis_of[pair] * p.total_rows + row] * turns[pair];
             t -= rint(t);
-            sincospif(2.f * (float)t, &sn[i], &cs[i]);
+            sincospif(2.f * (float)t, &s, &co);
+        };
+        // mode 0 and 2: chunk sub holds the low members of pairs 8 sub .. 8 sub + 7 (mode 2: where there are
+        // such pairs); mode 1: chunk sub holds pairs 4 sub .. + 3 and chunk sub + 8 pairs 32 + 4 sub .. + 3.
+        // The four groups of lanes need the same eight sines and cosines per `sub`: each works out two.
+        float cs[8], sn[8];
+        {
+            float s2[2], c2[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int k = 2 * group + i;
+                angle(kMode == 1 ? (k < 4 ? 4 * sub + k : 32 + 4 * sub + k - 4) : 8 * sub + k, s2[i], c2[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                sn[i] = __shfl_sync(0xffffffffu, s2[i & 1], (i >> 1) * 8 + sub);
+                cs[i] = __shfl_sync(0xffffffffu, c2[i & 1], (i >> 1) * 8 + sub);
+            }
         }
-        for (int h0 = part * 4; h0 < vectors; h0 += p.parts * 4) {
-            const int h = h0 + group;
-            const bool live = h < vectors;
+        auto store = [&](int h, const uint4& lo, const uint4& hi) {
             const bool is_q = h < p.Hq, is_v = h >= p.Hq + p.Hkv;
-            const int hk = is_q ? 0 : is_v ? h - p.Hq - p.Hkv : h - p.Hq;
-            const __nv_bfloat16* src = is_q ? p.q + (size_t)row * p.q_stride + (size_t)h * kHeadDim
-                                            : (is_v ? p.v : p.k) + (size_t)row * p.kv_stride + (size_t)hk * kHeadDim;
-            uint4 lo4 = make_uint4(0, 0, 0, 0), hi4 = lo4;
-            if (live) { lo4 = reinterpret_cast<const uint4*>(src)[sub]; hi4 = reinterpret_cast<const uint4*>(src)[sub + 8]; }
-            if (kMode == 2) {
-                // this lane writes the same two chunks; each dim's partner is n_pairs away
-                float lo[8], hi[8];
-                unpack(lo4, lo); unpack(hi4, hi);
-                if (live && !is_v) {
+            if (h >= vectors || (!is_q && !store_kv)) return;
+            uint4* dst = is_q ? reinterpret_cast<uint4*>(p.q_out + ((size_t)row * p.Hq + h) * kHeadDim)
+                              : reinterpret_cast<uint4*>((is_v ? p.v_pages : p.k_pages) +
+                                                         ((((size_t)page * p.Hkv + h - p.Hq - (is_v ? p.Hkv : 0)) * kPage + (size_t)(tok % kPage)) * kHeadDim));
+            dst[sub] = lo; dst[sub + 8] = hi;
+        };
+        if (kMode == 2) {
+            for (int h0 = part * 4; h0 < vectors; h0 += step) {
+                const int h = h0 + group;
+                const bool live = h < vectors;
+                const __nv_bfloat16* src = source(live ? h : 0);
+                uint4 a4 = reinterpret_cast<const uint4*>(src)[sub], z4 = reinterpret_cast<const uint4*>(src)[sub + 8];
+                if (live && h < p.Hq + p.Hkv) {
+                    // this lane writes the same two chunks; each dim's partner is n_pairs away
+                    float lo[8], hi[8];
+                    unpack(a4, lo); unpack(z4, hi);
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
                         float(&x)[8] = half ? hi : lo;
@@ -116,48 +153,50 @@ append_rope_kernel(const __grid_constant__ RopeParams p) {
                             const int pair = low ? dim : dim - p.n_pairs;
                             const float other = __bfloat162float(src[low ? dim + p.n_pairs : pair]);
                             float s = sn[i], co = cs[i];
-                            if (pair != 8 * sub + i) {          // not one of this lane's own angles
-                                double t = (double)p.positions[(size_t)axis_of[pair] * p.total_rows + row] * turns[pair];
-                                t -= rint(t);
-                                sincospif(2.f * (float)t, &s, &co);
-                            }
+                            if (pair != 8 * sub + i) angle(pair, s, co);        // not one of this lane's own angles
                             x[i] = low ? x[i] * co - other * s : other * s + x[i] * co;
                         }
                     }
+                    a4 = pack(lo); z4 = pack(hi);
                 }
-                lo4 = pack(lo); hi4 = pack(hi);
                 __syncwarp();                           // the partners have been read before anything is written in place
-            } else if (!is_v) {
-                float lo[8], hi[8];
-                unpack(lo4, lo); unpack(hi4, hi);
-                if (kMode == 0) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float a = lo[i], z = hi[i];
-                        lo[i] = a * cs[i] - z * sn[i];
-                        hi[i] = a * sn[i] + z * cs[i];
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float a = lo[2 * i], z = lo[2 * i + 1], d = hi[2 * i], e = hi[2 * i + 1];
-                        if (4 * sub + i < p.n_pairs) {
-                            lo[2 * i] = a * cs[i] - z * sn[i];
-                            lo[2 * i + 1] = a * sn[i] + z * cs[i];
-                        }
-                        if (32 + 4 * sub + i < p.n_pairs) {
-                            hi[2 * i] = d * cs[4 + i] - e * sn[4 + i];
-                            hi[2 * i + 1] = d * sn[4 + i] + e * cs[4 + i];
-                        }
-                    }
-                }
-                lo4 = pack(lo); hi4 = pack(hi);
+                store(h, a4, z4);
             }
-            if (!live || (!is_q && !store_kv)) continue;
-            uint4* dst = is_q ? reinterpret_cast<uint4*>(p.q_out + ((size_t)row * p.Hq + h) * kHeadDim)
-                              : reinterpret_cast<uint4*>((is_v ? p.v_pages : p.k_pages) +
-                                                         ((((size_t)page * p.Hkv + hk) * kPage + (size_t)(tok % kPage)) * kHeadDim));
-            dst[sub] = lo4; dst[sub + 8] = hi4;
+            continue;
+        }
+        for (int h0 = part * 4; h0 < vectors; h0 += kBatch * step) {
+            if (h0 > part * 4) load(h0);
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                const int h = h0 + i * step + group;
+                if (h < p.Hq + p.Hkv) {
+                    float lo[8], hi[8];
+                    unpack(lo4[i], lo); unpack(hi4[i], hi);
+                    if (kMode == 0) {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            const float a = lo[k], z = hi[k];
+                            lo[k] = a * cs[k] - z * sn[k];
+                            hi[k] = a * sn[k] + z * cs[k];
+                        }
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const float a = lo[2 * k], z = lo[2 * k + 1], d = hi[2 * k], e = hi[2 * k + 1];
+                            if (4 * sub + k < p.n_pairs) {
+                                lo[2 * k] = a * cs[k] - z * sn[k];
+                                lo[2 * k + 1] = a * sn[k] + z * cs[k];
+                            }
+                            if (32 + 4 * sub + k < p.n_pairs) {
+                                hi[2 * k] = d * cs[4 + k] - e * sn[4 + k];
+                                hi[2 * k + 1] = d * sn[4 + k] + e * cs[4 + k];
+                            }
+                        }
+                    }
+                    lo4[i] = pack(lo); hi4[i] = pack(hi);
+                }
+                store(h, lo4[i], hi4[i]);
+            }
         }
     }
 }
