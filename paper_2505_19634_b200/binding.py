@@ -57,6 +57,7 @@ class TtsRope(ctypes.Structure):
         if not 1 <= len(inv_freq) <= 64 or len(axis) != len(inv_freq) or min(axis) < 0 or max(axis) > 7:
             raise ValueError("one axis (0..7) and one frequency for each of 1..64 pairs")
         super().__init__(max(axis) + 1, len(inv_freq), 1 if interleaved else 0, (c_uint8 * 64)(*axis), (c_double * 64)(*inv_freq))
+        self.address = ctypes.addressof(self)
 
 
 class TtsPools:
@@ -109,7 +110,7 @@ def load_library() -> ctypes.CDLL:
     pp, i64 = POINTER(c_void_p), c_int64
     lib.tts_chunk_reserve.argtypes = [vp, c_int]
     lib.tts_chunk_attn.argtypes = [vp, vp, i64, vp, vp, vp, c_int, vp, vp, c_int, c_int, vp, vp]
-    lib.tts_kv_append_rope.argtypes = [vp, POINTER(TtsRope), vp, i64, vp, vp, i64, vp, vp, vp, vp, c_int, vp, vp, c_int, c_int, vp]
+    lib.tts_kv_append_rope.argtypes = [vp, vp, vp, i64, vp, vp, i64, vp, vp, vp, vp, c_int, vp, vp, c_int, c_int, vp]
     lib.tts_kv_copy_pages.argtypes = [vp, c_int, pp, pp, vp, vp, c_int]
     lib.tts_kv_fork.argtypes = [vp, c_int, pp, pp, vp, c_int, vp, c_int, vp, c_int, vp, vp, vp, vp]
     lib.tts_kv_grow.argtypes = [vp, vp, c_int, vp, vp, c_int, vp]
@@ -163,10 +164,10 @@ def _ptr(x) -> c_void_p:
 
 def _addr(x):
     """The same as a plain integer (None stays None): cheaper where a call's time is its latency."""
-    if x is None or isinstance(x, int):
-        return x
-    data_ptr = getattr(x, "data_ptr", None)
-    return data_ptr() if data_ptr is not None else _ptr(x).value
+    try:
+        return x.data_ptr()
+    except AttributeError:
+        return x if x is None or isinstance(x, int) else _ptr(x).value
 
 
 class TtsContext:
@@ -294,7 +295,7 @@ class TtsContext:
 
     def tts_kv_append_rope(self, rope: TtsRope, q, q_row_stride: int, k, v, kv_row_stride: int, positions, k_pages, v_pages, block_table,
                            prefix_len: int, branch_lens, row_start, n_branches: int, total_rows: int, q_out):
-        rc = self._lib.tts_kv_append_rope(self._h, byref(rope), _addr(q), q_row_stride, _addr(k), _addr(v), kv_row_stride, _addr(positions),
+        rc = self._lib.tts_kv_append_rope(self._h, rope.address, _addr(q), q_row_stride, _addr(k), _addr(v), kv_row_stride, _addr(positions),
                                           _addr(k_pages), _addr(v_pages), _addr(block_table), prefix_len, _addr(branch_lens),
                                           _addr(row_start), n_branches, total_rows, _addr(q_out))
         if rc:

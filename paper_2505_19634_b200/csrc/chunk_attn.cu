@@ -279,8 +279,8 @@ __device__ __forceinline__ uint64_t exp2_sfu2(uint64_t y) {
     return pack2(ex2(f.x), ex2(f.y));
 }
 __global__ void __launch_bounds__(kThreadsChunk, 1)
-chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
-                  const __grid_constant__ CUtensorMap tm_v) {
+chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_q1,
+                  const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v) {
     extern __shared__ unsigned char smem_dyn[];
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~(uintptr_t)1023);
     const uint32_t sbase = smem_u32(smem);
@@ -290,6 +290,10 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const Abort ab{misc, p.status};
 
+    // Rows of a single token's tile that hold no query: zeros cost the tensor cores less power than what they would find
+    // there, and power is what bounds most calls of this kernel.
+    for (int i = tid; i < kOperandBytes / 16; i += kThreadsChunk) *reinterpret_cast<uint4*>(smem + kOffQ + i * 16) = make_uint4(0, 0, 0, 0);
+    fence_proxy_async();
     if (tid == 0) {
         misc[0] = 0;
         for (int i = 0; i < kRingK; ++i) { mbar_init(bar(K_FULL + i), 1); mbar_init(bar(K_EMPTY + i), 1); }
@@ -357,10 +361,12 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                         alive = mbar_wait(bar(Q_EMPTY + s), (used[s] & 1) ^ 1, ab);
                         if (!alive) break;
                         ++used[s];
-                        mbar_arrive_expect_tx(bar(Q_FULL + s), (uint32_t)(p.T * p.G) * 256u);
+                        const bool single = w.x.n_tok == 1;
+                        const CUtensorMap* tm = single ? &tm_q1 : &tm_q;
+                        mbar_arrive_expect_tx(bar(Q_FULL + s), (uint32_t)(single ? p.G : p.T * p.G) * 256u);
                         const uint32_t dst = sbase + kOffQ + s * kOperandBytes;
-                        tma_load_rows(dst, &tm_q, 0, w.kvh * p.G, w.x.row0 + s * p.T, bar(Q_FULL + s));
-                        tma_load_rows(dst + kHalfBytes, &tm_q, 64, w.kvh * p.G, w.x.row0 + s * p.T, bar(Q_FULL + s));
+                        tma_load_rows(dst, tm, 0, w.kvh * p.G, w.x.row0 + s * p.T, bar(Q_FULL + s));
+                        tma_load_rows(dst + kHalfBytes, tm, 64, w.kvh * p.G, w.x.row0 + s * p.T, bar(Q_FULL + s));
                     }
                 }
             }
@@ -461,62 +467,73 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
             const bool wide = __shfl_sync(0xffffffffu, (int)w.wide, 0) != 0;
             const int n0 = __shfl_sync(0xffffffffu, w.n0, 0), n1 = __shfl_sync(0xffffffffu, w.n1, 0), loads = __shfl_sync(0xffffffffu, w.loads, 0);
             const int n_max = max(n0, n1);
-            // S of side `s`, its jj-th tile
-            auto scores = [&](auto side, int jj) {
+            const auto wait = [&](int i, int phase) { alive = alive && mbar_wait(bar(i), phase, ab); };
+            // One turn of side s: O (+)= P V of its jj-th tile (jj >= 0), then S of the next one.  An issuing lane is held
+            // back while the tensor pipe is busy, its queue being short; what is waited for between two groups of MMAs is
+            // time the pipe stands still, so it is looked at while the first half of P V runs.  In a wide piece side 0
+            // has waited for the tiles that both sides read.
+            auto turn = [&](auto side, int jj) {
                 constexpr int s = decltype(side)::value;
                 const int n = s ? n1 : n0;
                 const bool own_q = wide || s == 0;                       // a narrow piece has one Q tile for both sides
-                if (jj == 0 && own_q) { alive = mbar_wait(bar(Q_FULL + s), q_phase[s], ab); q_phase[s] ^= 1; }
-                alive = alive && mbar_wait(bar(K_FULL + k_slot), k_round, ab);
-                if (!__all_sync(0xffffffffu, alive)) { alive = false; return; }
-                tc_fence_after();
+                const bool last_kv = s == 1 || !wide;                    // the last reader of a K or V tile gives it back
+                const bool more = jj + 1 < n, has_k = s == 1 && wide && jj + 1 < n0, has_v = s == 1 && wide && jj < n0;
+                if (jj >= 0) {
+                    const uint32_t vd = v_lo + (uint32_t)(v_slot * (kOperandBytes / 16));     // one page (16 tokens) per step
+                    if (!has_v) wait(V_FULL + v_slot, v_round);
+                    wait(P_HALF + s, p_phase[s]);
+                    alive = __all_sync(0xffffffffu, alive);
+                    if (!alive) return;
+                    tc_fence_after();
+                    if (elect_one()) {
+#pragma unroll
+                        for (int ks = 0; ks < 4; ++ks)
+                            umma_ts(tm + 256u + s * 128u, tm + s * 128u + ks * 8u, vd + ks * 4096 / 16, v_hi, idesc_pv, ks > 0 || jj > 0);
+                    }
+                    __syncwarp();
+                    wait(P_FULL + s, p_phase[s]);
+                    if (more && !has_k) wait(K_FULL + k_slot, k_round);
+                    alive = __all_sync(0xffffffffu, alive);
+                    if (!alive) return;
+                    tc_fence_after();
+                    if (elect_one()) {
+#pragma unroll
+                        for (int ks = 4; ks < 8; ++ks)
+                            umma_ts(tm + 256u + s * 128u, tm + s * 128u + ks * 8u, vd + ks * 4096 / 16, v_hi, idesc_pv, 1u);
+                        if (last_kv) umma_commit(bar(V_EMPTY + v_slot));
+                        if (!more) umma_commit(bar(O_FULL + s));
+                    }
+                    __syncwarp();
+                    p_phase[s] ^= 1;
+                    if (last_kv && ++v_slot == kRingV) { v_slot = 0; v_round ^= 1; }
+                } else {
+                    if (own_q && more) { wait(Q_FULL + s, q_phase[s]); q_phase[s] ^= 1; }
+                    if (more && !has_k) wait(K_FULL + k_slot, k_round);
+                    alive = __all_sync(0xffffffffu, alive);
+                    if (!alive) return;
+                    tc_fence_after();
+                }
+                if (!more) return;
                 // Q: two 64-dim blocks of 128 rows, K: dim halves 1 KiB apart inside a page
                 const uint32_t qd = q_lo + (own_q ? s * kOperandBytes / 16 : 0), kd = k_lo + (uint32_t)(k_slot * (kOperandBytes / 16));
-                const bool last_k = s == 1 || !wide;                     // the last reader of a K or V tile, and of a Q tile, gives it back
-                const bool last_q = wide ? jj + 1 == n : 2 * jj + s + 1 == loads;
+                const bool last_q = wide ? jj + 2 == n : 2 * (jj + 1) + s + 1 == loads;
                 if (elect_one()) {
 #pragma unroll
                     for (int ks = 0; ks < 8; ++ks)
                         umma_ss(tm + s * 128u, qd + ((ks >> 2) * kHalfBytes + (ks & 3) * 32) / 16, q_hi, kd + ((ks >> 2) * 1024 + (ks & 3) * 32) / 16, k_hi, idesc_qk, ks > 0);
                     umma_commit(bar(S_FULL + s));
-                    if (last_k) umma_commit(bar(K_EMPTY + k_slot));
+                    if (last_kv) umma_commit(bar(K_EMPTY + k_slot));
                     if (last_q) umma_commit(bar(Q_EMPTY + (own_q ? s : 0)));
                 }
                 __syncwarp();
-                if (last_k && ++k_slot == kRingK) { k_slot = 0; k_round ^= 1; }
-            };
-            auto values = [&](auto side, int jj) {
-                constexpr int s = decltype(side)::value;
-                const bool last_v = s == 1 || !wide, last = jj + 1 == (s ? n1 : n0);
-                alive = mbar_wait(bar(V_FULL + v_slot), v_round, ab);
-                const uint32_t vd = v_lo + (uint32_t)(v_slot * (kOperandBytes / 16));       // one page (16 tokens) per step
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {       // the first 64 keys' probabilities are there before the others
-                    alive = alive && mbar_wait(bar((half ? P_FULL : P_HALF) + s), p_phase[s], ab);
-                    if (!__all_sync(0xffffffffu, alive)) { alive = false; return; }
-                    tc_fence_after();
-                    if (elect_one()) {
-#pragma unroll
-                        for (int ks = 4 * half; ks < 4 * half + 4; ++ks)
-                            umma_ts(tm + 256u + s * 128u, tm + s * 128u + ks * 8u, vd + ks * 4096 / 16, v_hi, idesc_pv, ks > 0 || jj > 0);
-                        if (half) {
-                            if (last_v) umma_commit(bar(V_EMPTY + v_slot));
-                            if (last) umma_commit(bar(O_FULL + s));
-                        }
-                    }
-                    __syncwarp();
-                }
-                p_phase[s] ^= 1;
-                if (last_v && ++v_slot == kRingV) { v_slot = 0; v_round ^= 1; }
+                if (last_kv && ++k_slot == kRingK) { k_slot = 0; k_round ^= 1; }
             };
             const std::integral_constant<int, 0> side0;
             const std::integral_constant<int, 1> side1;
 #pragma unroll 1
             for (int jj = -1; jj < n_max && alive; ++jj) {
-                if (jj >= 0 && jj < n0) values(side0, jj);
-                if (alive && jj + 1 < n0) scores(side0, jj + 1);
-                if (alive && jj >= 0 && jj < n1) values(side1, jj);
-                if (alive && jj + 1 < n1) scores(side1, jj + 1);
+                if (jj < n0) turn(side0, jj);
+                if (alive && jj < n1) turn(side1, jj);
             }
         }
     }
@@ -533,13 +550,14 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
         bool alive = true;
         for (int it = 0; alive; ++it) {
             int n, key0, step, limit, limit_min;
-            bool idle;
+            bool idle, hollow;
             {
                 Work w;
                 if (!next_piece<true>(w, it, smem, bar0, lane, p.T, ab)) break;
                 const int tok0 = w.wide ? side * p.T : 0;                           // first token of this side's rows
                 const int tl = ((warp & 3) * 32 + lane) / p.G, last = min(p.T, w.x.n_tok - tok0) - 1;
                 idle = (warp & 3) * 32 >= (last + 1) * p.G;                         // no row of this piece is this warp's
+                hollow = tl > last;                                                 // nor is any this thread's: its weights are zeros
                 n = side ? w.n1 : w.n0;
                 step = w.wide ? kTile : 2 * kTile;
                 key0 = w.x.tile_begin * kTile + (w.wide ? 0 : side * kTile);
@@ -600,7 +618,7 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                             tmem_st32(t_o + 32u * ch, ov);
                         }
                 }
-                const float neg_m = (m_ref == -INFINITY) ? 0.f : -m_ref;
+                const float neg_m = hollow ? -INFINITY : m_ref == -INFINITY ? 0.f : -m_ref;
                 const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2), neg2 = pack2(neg_m, neg_m);
                 uint64_t sum2[2] = {0, 0};
                 uint32_t pw[kTile / 2];
@@ -846,13 +864,13 @@ bool encode(CUtensorMap* map, const void* base, int rank, const cuuint64_t* dims
 }  // namespace
 
 cudaError_t launch_chunk_attn(const ChunkParams& p, const void* q, long q_stride, const void* k_pages, const void* v_pages, cudaStream_t st) {
-    CUtensorMap tm_q, tm_k, tm_v;
+    CUtensorMap tm_q, tm_q1, tm_k, tm_v;
     {
-        // queries: (dim, head, row); a box is half the dims of G heads of T rows
+        // queries: (dim, head, row); a box is half the dims of G heads of T rows, or of one
         const cuuint64_t dims[3] = {(cuuint64_t)kHeadDim, (cuuint64_t)p.Hq, (cuuint64_t)p.total_rows};
         const cuuint64_t strides[2] = {kHeadDim * 2, (cuuint64_t)q_stride * 2};
-        const cuuint32_t box[3] = {64, (cuuint32_t)p.G, (cuuint32_t)p.T};
-        if (!encode(&tm_q, q, 3, dims, strides, box)) return cudaErrorInvalidValue;
+        const cuuint32_t box[3] = {64, (cuuint32_t)p.G, (cuuint32_t)p.T}, box1[3] = {64, (cuuint32_t)p.G, 1};
+        if (!encode(&tm_q, q, 3, dims, strides, box) || !encode(&tm_q1, q, 3, dims, strides, box1)) return cudaErrorInvalidValue;
     }
     {
         // pages: (64 dims, 8 tokens, dim half, token half, page-head); a box is one page of one head, laid out
@@ -866,7 +884,7 @@ cudaError_t launch_chunk_attn(const ChunkParams& p, const void* q, long q_stride
     if (e != cudaSuccess) return e;
     static const int regs = [] { cudaFuncAttributes a; return cudaFuncGetAttributes(&a, chunk_attn_kernel) == cudaSuccess ? a.numRegs : 0; }();
     if (regs < kLaunchRegs) return cudaErrorInvalidConfiguration;       // the register split needs what it was computed from
-    return launch_dependent(chunk_attn_kernel, p.grid, kThreadsChunk, kSmemBytes, st, p, tm_q, tm_k, tm_v);
+    return launch_dependent(chunk_attn_kernel, p.grid, kThreadsChunk, kSmemBytes, st, p, tm_q, tm_q1, tm_k, tm_v);
 }
 
 }  // namespace tts

@@ -90,14 +90,14 @@ constexpr int kChunkNoBound = 1 << 30;                // leaves every entry whol
 // less than that, about the share, so that every CTA has one piece.
 __device__ __forceinline__ int chunk_bound(const ChunkParams& p, float total) {
     const float share = total * p.Hkv / p.grid;
-    return share < 6.f ? max(2, (int)ceilf(share)) : max(6, (int)(share / 16.f));
+    return share < 6.f ? max(4, (int)ceilf(share)) : max(6, (int)(share / 16.f));
 }
 // Pieces of entry r when `left` per KV head is still to be handed out, its own cost included.  A wide piece's partial
-// result is 256 rows to write and to join, worth three times a narrow one's bound.
+// result is 256 rows to write and to join, worth twice a narrow one's bound.
 __device__ __forceinline__ int chunk_cuts(const ChunkParams& p, const ChunkEntry& r, float left, int bound) {
     if (bound == kChunkNoBound) return 1;
     const bool wide = r.n_tok > p.T;
-    const float limit = fmaxf((float)(wide ? 3 * bound : bound), left * p.Hkv / (kChunkGuide * p.grid));
+    const float limit = fmaxf((float)(wide ? 2 * bound : bound), left * p.Hkv / (kChunkGuide * p.grid));
     return max(1, min(r.tiles, (int)ceilf((float)(wide ? 2 * r.tiles : r.tiles) / limit)));
 }
 
