@@ -20,7 +20,7 @@
 //                   (l carries the same reference, so the result is the same), and at the end divides and
 //                   stores its row, or leaves (m, l, O) for the last piece of the entry to join.
 //   warp 8          takes pieces, hands them to the other roles through a ring of two, loads Q
-//   warp 9, 10      load the K and V tiles: one TMA box per 4 KiB page tile, rings of three and two slots
+//   warp 9, 10      load the K and V tiles: one TMA box per 4 KiB page tile, rings of two and three slots
 //   warp 11         issues the MMAs.  Per side the order is S(0); then for each tile P V(j), S(j+1): the tensor
 //                   pipe keeps issue order, so S(j+1) may overwrite the columns that held P(j), and when S(j+1)
 //                   is complete P V(j) is as well -- the only wait on O that the softmax needs.
@@ -49,7 +49,7 @@ constexpr int kThreadsChunk = 2 * kSideThreads + 128;
 constexpr int kTakeWarp = 8, kKWarp = 9, kVWarp = 10, kMmaWarp = 11;
 constexpr int kHalfBytes = kRows * 128;
 constexpr int kOperandBytes = 2 * kHalfBytes;
-constexpr int kRingK = 3, kRingV = 2, kRingPiece = 2;
+constexpr int kRingK = 2, kRingV = 3, kRingPiece = 2;
 #ifndef AFTER
 #define AFTER 16
 #endif
