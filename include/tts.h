@@ -374,7 +374,8 @@ TTS_API int tts_kv_rollback(tts_ctx* ctx, int32_t* branch_lens, const int32_t* a
  *
  * tts_chunk_reserve allocates what tts_chunk_attn needs for calls of up to max_rows rows (about 80 MB of partial
  *   results and the schedule's tables).  Call it once per context; a later call with a smaller or equal number
- *   returns TTS_OK, a larger one TTS_ERR_INVALID (captured graphs hold the workspace's addresses).
+ *   returns TTS_OK, a larger one TTS_ERR_INVALID (captured graphs hold the workspace's addresses).  It allocates and waits
+ *   for its allocation: not inside a stream capture.
  *   TTS_ERR_UNSUPPORTED when more than 128 query heads share a KV head.
  *
  * tts_chunk_attn: exact softmax attention of the chunks over the paged cache, keys and values of the chunk being in
@@ -385,7 +386,7 @@ TTS_API int tts_kv_rollback(tts_ctx* ctx, int32_t* branch_lens, const int32_t* a
  *   lse = -infinity.
  *     q            device  rows of [Hq][128] bf16, q_row_stride elements from row to row (>= Hq * 128, a multiple of
  *                          8), so that q may be a slice of a fused projection; 16-byte aligned
- *     out          device  [total_rows][Hq][128], cfg.out_dtype
+ *     out          device  [total_rows][Hq][128], cfg.out_dtype; must not overlap q (TTS_ERR_INVALID)
  *     lse          device  [total_rows][Hq] fp32, or NULL
  *     total_rows   host    rows of the arrays, <= the reserved number; 0 launches nothing
  *     k_pages, v_pages, block_table, prefix_len (host, a multiple of 16; the first prefix_len / 16 entries of the rows

@@ -118,6 +118,9 @@ int tts_chunk_attn(tts_ctx* ctx, const void* q, int64_t q_row_stride, const void
         return TTS_ERR_INVALID;
     if (q_row_stride < (int64_t)f.n_q_heads * kHeadDim || q_row_stride % 8 != 0 || q_row_stride >= (1ll << 38)) return TTS_ERR_INVALID;
     if (total_rows == 0) return TTS_OK;
+    const size_t q_bytes = ((size_t)(total_rows - 1) * q_row_stride + (size_t)f.n_q_heads * kHeadDim) * 2;
+    const size_t out_bytes = (size_t)total_rows * f.n_q_heads * kHeadDim * (f.out_dtype == TTS_OUT_FP32 ? 4 : 2);
+    if (overlap(q, q_bytes, out, out_bytes)) return TTS_ERR_INVALID;
     const OnDevice on(c->device);
     if (on.error() != cudaSuccess) return finish(c, on.error(), 0);
     ChunkParams p;

@@ -277,3 +277,64 @@ def test_pages_outside_the_pool_read_as_zeros(bad):
     c.k[spare], c.v[spare] = 0, 0
     check(c, out, lse)
     ctx.close()
+
+
+def test_as_many_branches_as_a_context_takes():
+    g = torch.Generator().manual_seed(1)
+    chunk = torch.randint(0, 4, (1024,), generator=g).tolist()
+    lens = [x + int(torch.randint(0, 40, (1,), generator=g)) for x in chunk]
+    c = Cache(8, 2, chunk=chunk, lens=lens, seed=5)
+    check(c, *run(c))
+
+
+def test_more_row_blocks_than_are_cut_into_pieces():
+    c = Cache(128, 1, chunk=[10] * 500, lens=[10 + i % 30 for i in range(500)], seed=5)      # 2500 blocks of two tokens
+    check(c, *run(c))
+
+
+def test_partial_results_that_would_not_fit_make_larger_pieces():
+    """142 tokens of 128 heads over 12 700 keys: cut as fine as the balance asks for, the partial results of the 256-row
+    pieces would exceed the workspace."""
+    c = Cache(128, 1, chunk=[142], lens=[12842], seed=6, poison=False)
+    check(c, *run(c))
+
+
+def test_output_over_its_own_queries_is_refused():
+    c = Cache(8, 2, chunk=[3, 4], lens=[30, 40], seed=1)
+    ctx = context(c)
+    with pytest.raises(tts.TtsError) as e:
+        call(ctx, c, c.q)
+    assert e.value.status == -1
+    ctx.close()
+
+
+def test_two_graphs_of_one_context():
+    """Captured calls share the context's workspace: replayed one after the other, each gives its own result."""
+    a = Cache(8, 1, chunk=[1, 90], lens=[9000, 5000], seed=1)
+    b = Cache(8, 1, chunk=[70, 3], lens=[8000, 100], seed=2)
+    width, pages = max(a.width, b.width), max(a.num_pages, b.num_pages)
+    for c in (a, b):
+        c.table = torch.nn.functional.pad(c.table, (0, width - c.width), value=-1)
+        pad = lambda x: torch.cat([x, torch.zeros(pages - c.num_pages, *x.shape[1:], dtype=x.dtype, device="cuda")])
+        c.k, c.v = pad(c.k), pad(c.v)
+    ctx = tts.TtsContext(8, 1, 2, 1, width, pages)
+    ctx.tts_chunk_reserve(200)
+    graphs, outs = [], []
+    side = torch.cuda.Stream()
+    ctx.tts_set_stream(side)
+    for c in (a, b):
+        out, lse = torch.zeros_like(c.q), torch.zeros(c.total_rows, 8, device="cuda")
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            call(ctx, c, out, lse)
+        graphs.append(graph), outs.append((out, lse))
+    for order in ([0, 1], [1, 0, 0], [1, 1, 0]):
+        for out, lse in outs:
+            out.zero_(), lse.zero_()
+        for i in order:
+            graphs[i].replay()
+        torch.cuda.synchronize()
+        check(a, *outs[0])
+        check(b, *outs[1])
+    assert ctx.tts_last_status() == 0
+    ctx.close()
