@@ -65,6 +65,12 @@ cudaError_t cache_alloc(Ctx* c) {
     return cudaMalloc(&c->page_work, 16 + nb * sizeof(int4) + align16(nb * 4) + 2 * align16(np * 4));
 }
 
+cudaError_t cache_reset(Ctx* c) {
+    if (c->chunk_rows == 0) return cudaSuccess;
+    const cudaError_t e = cudaMemsetAsync(c->chunk_arrived, 0, c->chunk_arrived_bytes, c->stream);
+    return e == cudaSuccess ? cudaMemsetAsync(c->chunk_head, 0, sizeof(ChunkHead), c->stream) : e;
+}
+
 void cache_release(Ctx* c) {
     cudaFree(c->page_work);
     cudaFree(c->chunk_head); cudaFree(c->chunk_pieces); cudaFree(c->chunk_arrived);
@@ -94,6 +100,7 @@ int tts_chunk_reserve(tts_ctx* ctx, int max_rows) {
     const size_t arrived = (size_t)entries * f.n_kv_heads * 2 * sizeof(unsigned);
     if (e == cudaSuccess) e = cudaMalloc(&c->chunk_arrived, arrived);
     if (e == cudaSuccess) e = cudaMemset(c->chunk_arrived, 0, arrived);
+    if (e == cudaSuccess) e = cudaMemset(c->chunk_head, 0, sizeof(ChunkHead));
     if (e == cudaSuccess) e = cudaStreamSynchronize(cudaStreamLegacy);       // before work on a stream that does not wait for it
     if (e == cudaSuccess) e = cudaMalloc(&c->chunk_part_o, (size_t)part_rows * kHeadDim * sizeof(float));
     if (e == cudaSuccess) e = cudaMalloc(&c->chunk_part_ml, (size_t)part_rows * sizeof(float2));
@@ -129,7 +136,8 @@ int tts_chunk_attn(tts_ctx* ctx, const void* q, int64_t q_row_stride, const void
     p.out = out; p.lse = lse;
     // the entries of a call: at most one per branch and one per 2 T rows
     const bool small = (long)total_rows / (2 * (128 / (f.n_q_heads / f.n_kv_heads))) + n_branches <= kChunkSmall;
-    p.head = small ? nullptr : c->chunk_head; p.pieces = c->chunk_pieces; p.arrived = c->chunk_arrived;
+    p.small = small;
+    p.head = c->chunk_head; p.pieces = c->chunk_pieces; p.arrived = c->chunk_arrived;
     p.part_o = c->chunk_part_o; p.part_ml = c->chunk_part_ml;
     p.status = c->d_status;
     p.Hq = f.n_q_heads; p.Hkv = f.n_kv_heads; p.G = p.Hq / p.Hkv; p.T = 128 / p.G;

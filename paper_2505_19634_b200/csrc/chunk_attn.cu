@@ -59,6 +59,15 @@ constexpr uint32_t kTmemCols = 512;
 constexpr int kLaunchRegs = 168, kSoftmaxRegs = 216, kHelperRegs = 72;
 static_assert(2 * kSoftmaxRegs + kHelperRegs <= 3 * kLaunchRegs, "the split draws on what the block was launched with");
 
+// The schedule of a call of up to kChunkSmall entries, made by every CTA for itself: smaller calls are one launch, and
+// their time is latency (64 single tokens: 12 us less than with a launch of its own for the plan).
+struct SmallTable {
+    int pieces, part_rows;             // of one KV head
+    int start[kChunkSmall + 1], keys[kChunkSmall];                                // rows and cached tokens of the branches
+    unsigned short first[kChunkSmall + 1], at[kChunkSmall], cuts[kChunkSmall];    // first entry of a branch; an entry's first piece and their number
+    int row[kChunkSmall];              // first partial-result row
+};
+
 constexpr int kOffQ = 0;                                       // two row tiles
 constexpr int kOffK = kOffQ + 2 * kOperandBytes;
 constexpr int kOffV = kOffK + kRingK * kOperandBytes;
@@ -72,7 +81,8 @@ constexpr int kOffMisc = kOffBar + ((kNumBars * 8 + 15) & ~15);   // [0] abort, 
 constexpr int kOffPiece = kOffMisc + 32;                       // ring of pieces (+ their KV head)
 constexpr int kPieceBytes = 64;
 constexpr int kOffJoin = kOffPiece + kRingPiece * kPieceBytes; // side 1's (m, l) of a narrow piece
-constexpr int kSmemBytes = kOffJoin + kRows * 8 + 1024;
+constexpr int kOffSmall = kOffJoin + kRows * 8;
+constexpr int kSmemBytes = kOffSmall + ((sizeof(SmallTable) + 15) & ~15);     // the base is 1024-byte aligned: the kernel has no static shared memory
 static_assert(kSmemBytes <= 227 * 1024, "shared memory");
 
 // tcgen05.mma with descriptors as two words each; `accumulate` 0: the first step of a sum
@@ -144,13 +154,16 @@ __device__ __forceinline__ bool next_piece(Work& w, int it, const unsigned char*
     return true;
 }
 
-// The schedule of a call of up to kChunkSmall entries, one entry per lane: made by every CTA for itself, so that the
-// smallest calls, whose time is latency, are one launch.
-struct SmallPlan {
-    ChunkEntry e;      // this lane's entry
-    int k, at, row;    // its pieces, its first piece's place, its first partial row
-    int pieces, part_rows;
-};
+__device__ __forceinline__ int small_branch(const SmallTable& t, int n_branches, int e) {
+    int lo = 0, hi = n_branches - 1;   // the last branch whose first entry is at or before e
+    while (lo < hi) { const int mid = (lo + hi + 1) >> 1; if (t.first[mid] <= e) lo = mid; else hi = mid - 1; }
+    return lo;
+}
+
+__device__ __forceinline__ ChunkEntry small_entry(const ChunkParams& p, const SmallTable& t, int e) {
+    const int b = small_branch(t, p.n_branches, e);
+    return chunk_entry(p.T, b, t.first[b + 1] - 1 - e, t.start[b], t.start[b + 1] - t.start[b], t.keys[b]);
+}
 
 __device__ __forceinline__ int warp_scan(int v, int lane, int* total) {        // exclusive
     int s = v;
@@ -160,57 +173,97 @@ __device__ __forceinline__ int warp_scan(int v, int lane, int* total) {        /
     return s - v;
 }
 
-__device__ SmallPlan small_plan(const ChunkParams& p, int lane) {
-    SmallPlan sp;
-    int lo = 0, c = 0, keys = 0;
+// One warp, two branches and two entries per lane.
+__device__ void small_plan(const ChunkParams& p, SmallTable& t, int lane) {
+    constexpr int kPer = kChunkSmall / 32;
+    int count[kPer], mine = 0;
     bool bad = false;
-    if (lane < p.n_branches) {
-        lo = p.row_start[lane];
-        const int hi = p.row_start[lane + 1], len = p.branch_lens[lane];
-        bad = !chunk_branch_ok(p, lo, hi, len);
-        c = hi - lo; keys = p.prefix_len + len;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int b = kPer * lane + i;
+        count[i] = 0;
+        if (b < p.n_branches) {
+            const int lo = p.row_start[b], hi = p.row_start[b + 1], len = p.branch_lens[b];
+            bad |= !chunk_branch_ok(p, lo, hi, len);
+            t.start[b] = lo; t.keys[b] = p.prefix_len + len;
+            if (b == p.n_branches - 1) t.start[b + 1] = hi;
+            count[i] = ceil_div(hi - lo, 2 * p.T);
+        }
+        mine += count[i];
     }
     bad = __any_sync(0xffffffffu, bad);
     if (bad && lane == 0) atomicMin(p.status, (int)TTS_ERR_DEVICE_BOUNDS);
-    int n;
-    const int first = warp_scan(bad ? 0 : ceil_div(c, 2 * p.T), lane, &n);
-    // the branch of entry `lane`: the last one that starts at or before it
-    int b = 0;
-    for (int i = 0; i < min(p.n_branches, 32); ++i) if (__shfl_sync(0xffffffffu, first, i) <= lane) b = i;
-    sp.e = chunk_entry(p.T, b, ceil_div(__shfl_sync(0xffffffffu, c, b), 2 * p.T) - 1 - (lane - __shfl_sync(0xffffffffu, first, b)), __shfl_sync(0xffffffffu, lo, b), __shfl_sync(0xffffffffu, c, b),
-                       __shfl_sync(0xffffffffu, keys, b));
-    const bool mine = lane < n;
-    const int cost = mine ? chunk_cost(sp.e, p.T) : -1, rows = mine ? sp.e.n_tok * p.G : 0;
-    // costliest first, equal ones in their order
-    int after = 0, total = 0;                           // cost of this entry and those behind it; of all
-    unsigned ahead = 0;                                 // the lanes whose entries come before this one
-    for (int i = 0; i < n; ++i) {
-        const int c_i = __shfl_sync(0xffffffffu, cost, i);
-        total += c_i;
-        if (c_i > cost || (c_i == cost && i < lane)) ahead |= 1u << i; else after += c_i;
-    }
-    for (int bound = chunk_bound(p, (float)total);; bound = bound >= 4096 ? kChunkNoBound : bound * 4) {
-        sp.k = mine ? chunk_cuts(p, sp.e, (float)after, bound) : 0;
-        sp.part_rows = __reduce_add_sync(0xffffffffu, sp.k > 1 ? sp.k * rows : 0);
-        if (bound == kChunkNoBound || (long)sp.part_rows * p.Hkv <= p.part_rows) break;     // else too much for the workspace
-    }
-    sp.pieces = __reduce_add_sync(0xffffffffu, sp.k);
-    sp.at = sp.row = 0;
-    for (int i = 0; i < n; ++i) {
-        const int k_i = __shfl_sync(0xffffffffu, sp.k, i), rows_i = __shfl_sync(0xffffffffu, sp.k > 1 ? sp.k * rows : 0, i);
-        if (ahead >> i & 1) { sp.at += k_i; sp.row += rows_i; }
-    }
-    return sp;
-}
-
-__device__ ChunkPiece small_piece(const ChunkParams& p, const SmallPlan& sp, int i, int lane) {
-    const bool here = sp.at <= i && i < sp.at + sp.k;
-    const int e = __ffs(__ballot_sync(0xffffffffu, here)) - 1;
-    ChunkPiece x = chunk_piece(sp.e, lane, i - sp.at, max(1, sp.k), sp.row);
-    int* w = reinterpret_cast<int*>(&x);
+    int n, first = warp_scan(bad ? 0 : mine, lane, &n);
 #pragma unroll
-    for (int k = 0; k < (int)(sizeof x / 4); ++k) w[k] = __shfl_sync(0xffffffffu, w[k], e);
-    return x;
+    for (int i = 0; i < kPer; ++i) {
+        const int b = kPer * lane + i;
+        if (b < p.n_branches) t.first[b] = (unsigned short)first;
+        if (!bad) first += count[i];
+        if (b == p.n_branches - 1) t.first[b + 1] = (unsigned short)n;
+    }
+    __syncwarp();
+    ChunkEntry r[kPer];
+    int cost[kPer], after[kPer] = {}, total = 0;       // cost of an entry, of it and those handed out behind it, of all
+    unsigned long long ahead[kPer] = {};               // the entries handed out before it: costliest first, equal ones in their order
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        const int e = j * 32 + lane;
+        cost[j] = -1;
+        if (e < n) { r[j] = small_entry(p, t, e); cost[j] = chunk_cost(r[j], p.T); }
+    }
+#pragma unroll
+    for (int h = 0; h < kPer; ++h)
+        for (int l = 0; l < min(32, n - 32 * h); ++l) {
+            const int c = __shfl_sync(0xffffffffu, cost[h], l), i = 32 * h + l;
+            total += c;
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) {
+                if (c > cost[j] || (c == cost[j] && i < j * 32 + lane)) ahead[j] |= 1ull << i;
+                else after[j] += c;
+            }
+        }
+    int k[kPer], rows[kPer], part_rows;
+    for (int bound = chunk_bound(p, (float)total);; bound = bound >= 4096 ? kChunkNoBound : bound * 4) {
+        int sum = 0;
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            k[j] = cost[j] >= 0 ? chunk_cuts(p, r[j], (float)after[j], bound) : 0;
+            rows[j] = k[j] > 1 ? k[j] * r[j].n_tok * p.G : 0;
+            sum += rows[j];
+        }
+        part_rows = __reduce_add_sync(0xffffffffu, sum);
+        if (bound == kChunkNoBound || (long)part_rows * p.Hkv <= p.part_rows) break;    // else too much for the workspace
+    }
+    int at[kPer] = {}, row[kPer] = {}, pieces = 0;
+#pragma unroll
+    for (int h = 0; h < kPer; ++h)
+        for (int l = 0; l < min(32, n - 32 * h); ++l) {
+            const int k_i = __shfl_sync(0xffffffffu, k[h], l), rows_i = __shfl_sync(0xffffffffu, rows[h], l), i = 32 * h + l;
+            pieces += k_i;
+#pragma unroll
+            for (int j = 0; j < kPer; ++j)
+                if (ahead[j] >> i & 1) { at[j] += k_i; row[j] += rows_i; }
+        }
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        const int e = j * 32 + lane;
+        if (e < n) { t.at[e] = (unsigned short)at[j]; t.cuts[e] = (unsigned short)k[j]; t.row[e] = row[j]; }
+    }
+    if (lane == 0) { t.pieces = pieces; t.part_rows = part_rows; }
+    __syncwarp();
+}
+static_assert(kChunkSmall == 64, "two branches and two entries per lane, the order in 64 bits");
+
+// One warp.
+__device__ ChunkPiece small_piece(const ChunkParams& p, const SmallTable& t, int i, int lane) {
+    const int n = t.first[p.n_branches];
+    int e = 0;
+    for (int j = 0; j < n; j += 32) {
+        const bool here = j + lane < n && t.at[j + lane] <= i && i < t.at[j + lane] + t.cuts[j + lane];
+        const unsigned found = __ballot_sync(0xffffffffu, here);
+        if (found) e = j + __ffs(found) - 1;
+    }
+    return chunk_piece(small_entry(p, t, e), e, i - t.at[e], t.cuts[e], t.row[e]);
 }
 
 __device__ __forceinline__ void tma_load_rows(uint32_t dst, const CUtensorMap* map, int dim, int head, int row, uint32_t bar) {
@@ -281,8 +334,7 @@ __device__ __forceinline__ uint64_t exp2_sfu2(uint64_t y) {
 __global__ void __launch_bounds__(kThreadsChunk, 1)
 chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_q1,
                   const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v) {
-    extern __shared__ unsigned char smem_dyn[];
-    unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~(uintptr_t)1023);
+    extern __shared__ __align__(1024) unsigned char smem[];
     const uint32_t sbase = smem_u32(smem);
     const uint32_t bar0 = sbase + kOffBar;
     auto bar = [&](int i) { return bar0 + 8u * i; };
@@ -322,9 +374,9 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kHelperRegs));
     if (warp == kTakeWarp) {
         // =========================== takes pieces, loads Q ===========================
-        SmallPlan small;
-        if (!p.head) small = small_plan(p, lane);
-        const int total = (p.head ? p.head->pieces : small.pieces) * p.Hkv, part_rows = p.head ? p.head->part_rows : small.part_rows;
+        SmallTable& small = *reinterpret_cast<SmallTable*>(smem + kOffSmall);
+        if (p.small) small_plan(p, small, lane);
+        const int total = (p.small ? small.pieces : p.head->pieces) * p.Hkv, part_rows = p.small ? small.part_rows : p.head->part_rows;
         int index = blockIdx.x, used[2] = {0, 0};
         bool alive = true;
         for (int it = 0; alive; ++it) {
@@ -334,7 +386,7 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
             if (index < total) {
                 const int i = index / p.Hkv;                            // all KV heads of a piece follow one another
                 w.kvh = index - i * p.Hkv;
-                if (p.head) {
+                if (!p.small) {
                     const int4* src = reinterpret_cast<const int4*>(p.pieces + i);
                     int4* dst = reinterpret_cast<int4*>(&w.x);
                     dst[0] = src[0]; dst[1] = src[1]; dst[2] = src[2];
@@ -352,9 +404,8 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                     mbar_arrive(bar(PIECE_FULL + slot));
                     if (w.kvh < 0) alive = false;
                 }
-                // the next one, while this one is worked on; a small call has few pieces, which need no counter
                 if (alive) {
-                    index = p.head ? atomicAdd(&p.head->next, 1) : index + p.grid;
+                    index = p.grid + (int)atomicInc(&p.head->next, (unsigned)total - 1u);       // the next one; one for each piece, and back to 0
                     derive(w, p.T);
                     for (int s = 0; s < (w.wide ? 2 : 1) && alive; ++s) {
                         if ((s ? w.n1 : w.n0) == 0) continue;

@@ -26,11 +26,11 @@ static_assert(sizeof(ChunkPiece) == 48, "read as three 16-byte words");
 
 constexpr int kChunkTile = 128;                       // KV tokens per tile
 constexpr int kChunkPartsPerSm = 4;                   // wide pieces with partial results that the workspace has room for, per SM
-constexpr int kChunkSmall = 32;                       // calls of up to so many entries are scheduled inside the attention kernel
+constexpr int kChunkSmall = 64;                       // calls of up to so many entries are scheduled inside the attention kernel
 
 struct ChunkHead {
     int pieces;        // per KV head
-    int next;          // the next piece that nobody has taken yet
+    unsigned next;     // pieces taken from the list, apart from each CTA's first; wraps to 0 with the last one
     int part_rows;     // partial-result rows of one KV head
     int pad;
 };
@@ -41,8 +41,9 @@ struct ChunkParams {
     const int32_t* row_start;
     void* out;
     float* lse;                    // may be null
-    ChunkHead* head;               // null: small, see kChunkSmall
+    ChunkHead* head;
     ChunkPiece* pieces;
+    int small;                     // see kChunkSmall
     unsigned* arrived;             // [entries][Hkv][2] pieces that have left their partial result; the last one sets it back to 0
     float* part_o;                 // [part_rows][128]
     float2* part_ml;               // [part_rows] (max in log2 units, sum)

@@ -98,7 +98,6 @@ chunk_plan_kernel(const ChunkParams p) {
     if (tid < p.n_branches) br.first[tid] = at_branch;
     if (tid == 0) {
         br.first[p.n_branches] = n;
-        p.head->next = p.grid;
         if (bad) atomicMin(p.status, (int)TTS_ERR_DEVICE_BOUNDS);
     }
     __syncthreads();

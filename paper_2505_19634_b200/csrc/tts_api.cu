@@ -583,9 +583,7 @@ int tts_last_status(tts_ctx* ctx, int* device_status) {
     cudaError_t e = cudaMemcpyAsync(&h, c->d_status, sizeof h, cudaMemcpyDeviceToHost, c->stream);
     if (e == cudaSuccess) e = cudaMemsetAsync(c->d_status, 0, sizeof h, c->stream);
     if (e == cudaSuccess) e = cudaStreamSynchronize(c->stream);
-    // a chunk call that ran out of time has left its counters where they were
-    if (e == cudaSuccess && h == TTS_ERR_DEVICE_TIMEOUT && c->chunk_arrived)
-        e = cudaMemsetAsync(c->chunk_arrived, 0, c->chunk_arrived_bytes, c->stream);
+    if (e == cudaSuccess && h == TTS_ERR_DEVICE_TIMEOUT) e = cache_reset(c);
     if (e != cudaSuccess) return cuda_fail(c, e);
     *device_status = h;
     return TTS_OK;

@@ -364,6 +364,7 @@ cudaError_t launch_compact(const PagePools& pools, const int32_t* table, int max
 cudaError_t launch_append_rope(RopeParams p, int n_sms, cudaStream_t st);
 cudaError_t cache_alloc(Ctx* c);       // page_work
 void cache_release(Ctx* c);
+cudaError_t cache_reset(Ctx* c);       // the chunk attention's counters, after a call that did not end
 cudaError_t launch_wait_probe(int32_t* status, long long limit_ns, int* gave_up, cudaStream_t st);
 int simt_rb_rows(int nr);
 constexpr int kSimtTileTokens = 64;
