@@ -203,27 +203,17 @@ __device__ void small_plan(const ChunkParams& p, SmallTable& t, int lane) {
     }
     __syncwarp();
     ChunkEntry r[kPer];
-    int cost[kPer], after[kPer] = {}, total = 0;       // cost of an entry, of it and those handed out behind it, of all
-    unsigned long long ahead[kPer] = {};               // the entries handed out before it: costliest first, equal ones in their order
+    int cost[kPer], total = 0;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
         const int e = j * 32 + lane;
         cost[j] = -1;
-        if (e < n) { r[j] = small_entry(p, t, e); cost[j] = chunk_cost(r[j], p.T); }
+        if (e < n) { r[j] = small_entry(p, t, e); cost[j] = chunk_cost(r[j], p.T); total += cost[j]; }
     }
-#pragma unroll
-    for (int h = 0; h < kPer; ++h)
-        for (int l = 0; l < min(32, n - 32 * h); ++l) {
-            const int c = __shfl_sync(0xffffffffu, cost[h], l), i = 32 * h + l;
-            total += c;
-#pragma unroll
-            for (int j = 0; j < kPer; ++j) {
-                if (c > cost[j] || (c == cost[j] && i < j * 32 + lane)) ahead[j] |= 1ull << i;
-                else after[j] += c;
-            }
-        }
-    int k[kPer], rows[kPer], part_rows;
-    for (int bound = chunk_bound(p, (float)total);; bound = bound >= 4096 ? kChunkNoBound : bound * 4) {
+    total = __reduce_add_sync(0xffffffffu, total);
+    ChunkBound bound = chunk_bound(p, (float)total, n, (float)__reduce_max_sync(0xffffffffu, max(cost[0], cost[1])));
+    int k[kPer], rows[kPer], at[kPer] = {}, row[kPer] = {}, pieces = 0, part_rows = 0;
+    auto cut = [&](const int (&after)[kPer]) {
         int sum = 0;
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
@@ -232,18 +222,47 @@ __device__ void small_plan(const ChunkParams& p, SmallTable& t, int lane) {
             sum += rows[j];
         }
         part_rows = __reduce_add_sync(0xffffffffu, sum);
-        if (bound == kChunkNoBound || (long)part_rows * p.Hkv <= p.part_rows) break;    // else too much for the workspace
-    }
-    int at[kPer] = {}, row[kPer] = {}, pieces = 0;
+    };
+    const int none[kPer] = {};
+    if ((float)total * p.Hkv <= kChunkGuide * p.grid * bound.narrow) cut(none);
+    else part_rows = -1;
+    if (part_rows >= 0 && (long)part_rows * p.Hkv <= p.part_rows) {
+        // so little work that the bound alone says how entries are cut: their order does not matter
+        int rows_so_far = 0;
 #pragma unroll
-    for (int h = 0; h < kPer; ++h)
-        for (int l = 0; l < min(32, n - 32 * h); ++l) {
-            const int k_i = __shfl_sync(0xffffffffu, k[h], l), rows_i = __shfl_sync(0xffffffffu, rows[h], l), i = 32 * h + l;
-            pieces += k_i;
-#pragma unroll
-            for (int j = 0; j < kPer; ++j)
-                if (ahead[j] >> i & 1) { at[j] += k_i; row[j] += rows_i; }
+        for (int j = 0; j < kPer; ++j) {
+            int sum_k, sum_rows;
+            at[j] = pieces + warp_scan(k[j], lane, &sum_k);
+            row[j] = rows_so_far + warp_scan(rows[j], lane, &sum_rows);
+            pieces += sum_k; rows_so_far += sum_rows;
         }
+    } else {
+        int after[kPer] = {};                          // cost of an entry and those handed out behind it
+        unsigned long long ahead[kPer] = {};           // the entries handed out before it: costliest first, equal ones in their order
+#pragma unroll
+        for (int h = 0; h < kPer; ++h)
+            for (int l = 0; l < min(32, n - 32 * h); ++l) {
+                const int c = __shfl_sync(0xffffffffu, cost[h], l), i = 32 * h + l;
+#pragma unroll
+                for (int j = 0; j < kPer; ++j) {
+                    if (c > cost[j] || (c == cost[j] && i < j * 32 + lane)) ahead[j] |= 1ull << i;
+                    else after[j] += c;
+                }
+            }
+        for (;; bound = chunk_coarser(bound)) {
+            cut(after);
+            if (bound.narrow == kChunkNoBound || (long)part_rows * p.Hkv <= p.part_rows) break;    // else too much for the workspace
+        }
+#pragma unroll
+        for (int h = 0; h < kPer; ++h)
+            for (int l = 0; l < min(32, n - 32 * h); ++l) {
+                const int k_i = __shfl_sync(0xffffffffu, k[h], l), rows_i = __shfl_sync(0xffffffffu, rows[h], l), i = 32 * h + l;
+                pieces += k_i;
+#pragma unroll
+                for (int j = 0; j < kPer; ++j)
+                    if (ahead[j] >> i & 1) { at[j] += k_i; row[j] += rows_i; }
+            }
+    }
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
         const int e = j * 32 + lane;
@@ -767,30 +786,44 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                     y0[i] = __shfl_sync(0xffffffffu, f0, (lane >> 2) + 8 * i);
                     y1[i] = __shfl_sync(0xffffffffu, f1, (lane >> 2) + 8 * i);
                 }
-#pragma unroll 1
-                for (int col = 0; col < kHeadDim && !idle; col += 32) {
-                    uint32_t a[2][16], b[2][16];            // rows 0-15 and 16-31 of this warp's
-                    tmem_ld_frag(t_o + col, a[0]);
-                    tmem_ld_frag(t_o + (16u << 16) + col, a[1]);
-                    tmem_ld_frag(t_o1 + col, b[0]);
-                    tmem_ld_frag(t_o1 + (16u << 16) + col, b[1]);
-                    tmem_wait_ld();
+                const bool both = (warp & 3) * 32 + 16 < rows;          // rows 16-31 of this warp's as well as 0-15
+                uint32_t a[2][16], b[2][16];
+                auto load = [&](int i, int col) {
+                    tmem_ld_frag(t_o + ((uint32_t)(16 * i) << 16) + col, a[i]);
+                    tmem_ld_frag(t_o1 + ((uint32_t)(16 * i) << 16) + col, b[i]);
+                };
+                auto leave = [&](int i, int col) {
+                    uint32_t e[2][4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        uint32_t e[4];
+                    for (int h = 0; h < 2; ++h)                         // rows lane / 4 and lane / 4 + 8 of the 16
 #pragma unroll
                         for (int g = 0; g < 4; ++g) {
                             float v[2];
 #pragma unroll
                             for (int c = 0; c < 2; ++c) {
-                                v[c] = __uint_as_float(a[i >> 1][4 * g + 2 * (i & 1) + c]) * y0[i];
-                                if (joined) v[c] = fmaf(__uint_as_float(b[i >> 1][4 * g + 2 * (i & 1) + c]), y1[i], v[c]);
+                                v[c] = __uint_as_float(a[i][4 * g + 2 * h + c]) * y0[2 * i + h];
+                                if (joined) v[c] = fmaf(__uint_as_float(b[i][4 * g + 2 * h + c]), y1[2 * i + h], v[c]);
                             }
-                            e[g] = bf16_pair(v[0], v[1]);
+                            e[h][g] = bf16_pair(v[0], v[1]);
                         }
-                        transpose4(e, lane);
-                        if (at[i] >= 0) *reinterpret_cast<uint4*>(to + (size_t)at[i] * kHeadDim + col) = make_uint4(e[0], e[1], e[2], e[3]);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        transpose4(e[h], lane);
+                        if (at[2 * i + h] >= 0) *reinterpret_cast<uint4*>(to + (size_t)at[2 * i + h] * kHeadDim + col) = make_uint4(e[h][0], e[h][1], e[h][2], e[h][3]);
                     }
+                };
+                if (!idle) {
+                    load(0, 0);
+#pragma unroll 1
+                    for (int col = 0; col < kHeadDim; col += 32) {
+                        tmem_wait_ld();
+                        load(1, col);                                   // (whether there are such rows or not)
+                        leave(0, col);
+                        tmem_wait_ld();
+                        load(0, (col + 32) & (kHeadDim - 1));           // (after the last one, the first again)
+                        if (both) leave(1, col);
+                    }
+                    tmem_wait_ld();
                 }
             } else
 #pragma unroll 1

@@ -73,7 +73,9 @@ __device__ __forceinline__ ChunkEntry chunk_entry(int T, int b, int index, int s
 __device__ __forceinline__ ChunkPiece chunk_piece(const ChunkEntry& r, int e, int part, int parts, int part_row) {
     ChunkPiece x;
     x.branch = r.b; x.row0 = r.row0; x.n_tok = r.n_tok; x.limit0 = r.limit0; x.keys = r.keys;
-    x.tile_begin = (int)((long)r.tiles * part / parts); x.tile_end = (int)((long)r.tiles * (part + 1) / parts);
+    // as even as whole tiles go, the longer ones first
+    const int each = r.tiles / parts, longer = r.tiles - each * parts;
+    x.tile_begin = part * each + min(part, longer); x.tile_end = x.tile_begin + each + (part < longer);
     x.parts = parts; x.part = part; x.part_row = part_row; x.entry = e; x.once = r.once;
     return x;
 }
@@ -86,19 +88,33 @@ __device__ __forceinline__ int chunk_cost(const ChunkEntry& r, int T) { return r
 constexpr float kChunkGuide = 1.5f;
 constexpr int kChunkNoBound = 1 << 30;                // leaves every entry whole
 
-// How small the pieces of a call may become, `total` being the cost of all its entries per KV head: a sixteenth of a
-// CTA's share, but not less than six tiles, whose time is several times what a piece costs by itself; where a share is
-// less than that, about the share, so that every CTA has one piece.
-__device__ __forceinline__ int chunk_bound(const ChunkParams& p, float total) {
-    const float share = total * p.Hkv / p.grid;
-    return share < 6.f ? max(4, (int)ceilf(share)) : max(6, (int)(share / 16.f));
+// How small the pieces of a call may become.  `total`: the cost of its n entries per KV head, `largest` the costliest.
+//   one wave   fewer entries than CTAs, and no piece of it much longer than a CTA's share: at most `narrow` = total /
+//              (CTAs per KV head - n) per piece makes no more pieces than CTAs, whatever the entries are.  (200 tokens of
+//              40 heads over 4000 keys: 46 us in one wave of 128 pieces, 82 us as 192 shorter ones.)
+//   guided     otherwise pieces get smaller towards the end of the list (chunk_cuts), down to a sixteenth of a CTA's
+//              share, but not below six tiles, whose time is several times what a piece costs by itself.  A wide piece's
+//              partial result is 256 rows to write and to join: its bound is twice a narrow one's.
+struct ChunkBound { int narrow, wide; };
+__device__ __forceinline__ ChunkBound chunk_bound(const ChunkParams& p, float total, int n, float largest) {
+    const float share = total * p.Hkv / p.grid, spare = (float)p.grid / p.Hkv - n;
+    if (spare >= 1.f && fminf(total / spare, largest) <= share + 12.f) {
+        const int b = max(4, (int)ceilf(total / spare));
+        return {b, max(b, 8)};
+    }
+    const int b = max(6, (int)(share / 16.f));
+    return {b, 2 * b};
 }
-// Pieces of entry r when `left` per KV head is still to be handed out, its own cost included.  A wide piece's partial
-// result is 256 rows to write and to join, worth twice a narrow one's bound.
-__device__ __forceinline__ int chunk_cuts(const ChunkParams& p, const ChunkEntry& r, float left, int bound) {
-    if (bound == kChunkNoBound) return 1;
+// larger pieces, when the partial results would not fit the workspace
+__device__ __forceinline__ ChunkBound chunk_coarser(ChunkBound b) {
+    const int n = b.narrow >= 4096 ? kChunkNoBound : b.narrow * 4;
+    return {n, n == kChunkNoBound ? n : b.wide * 4};
+}
+// Pieces of entry r when `left` per KV head is still to be handed out, its own cost included.
+__device__ __forceinline__ int chunk_cuts(const ChunkParams& p, const ChunkEntry& r, float left, ChunkBound bound) {
+    if (bound.narrow == kChunkNoBound) return 1;
     const bool wide = r.n_tok > p.T;
-    const float limit = fmaxf((float)(wide ? 2 * bound : bound), left * p.Hkv / (kChunkGuide * p.grid));
+    const float limit = fmaxf((float)(wide ? bound.wide : bound.narrow), left * p.Hkv / (kChunkGuide * p.grid));
     return max(1, min(r.tiles, (int)ceilf((float)(wide ? 2 * r.tiles : r.tiles) / limit)));
 }
 

@@ -146,7 +146,7 @@ chunk_plan_kernel(const ChunkParams p) {
         }
     const unsigned long long ahead = block_scan((unsigned)cost[0] + (unsigned)cost[1], sc, &sum);
     const float total = (float)sum, left[kPer] = {(float)(sum - ahead), (float)(sum - ahead - cost[0])};
-    int bound = chunk_bound(p, total);
+    ChunkBound bound = chunk_bound(p, total, n, (float)largest);
     for (;;) {
         int k[kPer] = {0, 0};
         unsigned long long mine = 0;                   // pieces, and from bit 20 on partial-result rows
@@ -162,8 +162,8 @@ chunk_plan_kernel(const ChunkParams p) {
         const unsigned long long at = block_scan(mine, sc, &sum);
         const int pieces = (int)(sum & 0xfffffu);
         const long rows = (long)(sum >> 20);
-        if (bound != kChunkNoBound && (pieces > p.max_pieces || rows * p.Hkv > p.part_rows)) {
-            bound = bound >= 4096 ? kChunkNoBound : bound * 4;        // too much for the workspace: larger pieces
+        if (bound.narrow != kChunkNoBound && (pieces > p.max_pieces || rows * p.Hkv > p.part_rows)) {
+            bound = chunk_coarser(bound);
             continue;
         }
         const int at0 = (int)(at & 0xfffffu), row0 = (int)(at >> 20);
