@@ -372,7 +372,7 @@ TTS_API int tts_kv_rollback(tts_ctx* ctx, int32_t* branch_lens, const int32_t* a
  * c_b may be 0.  Rows before row_start[0] and from row_start[n_branches] on belong to no branch and their results
  * are left as they were.  branch_lens[b] counts the private tokens INCLUDING the chunk, as in tts_verify_attn.
  *
- * tts_chunk_reserve allocates what tts_chunk_attn needs for calls of up to max_rows rows (about 80 MB of partial
+ * tts_chunk_reserve allocates what tts_chunk_attn needs for calls of up to max_rows rows (about 160 MB of partial
  *   results and the schedule's tables).  Call it once per context; a later call with a smaller or equal number
  *   returns TTS_OK, a larger one TTS_ERR_INVALID (captured graphs hold the workspace's addresses).  It allocates and waits
  *   for its allocation: not inside a stream capture.

@@ -213,21 +213,21 @@ __device__ void small_plan(const ChunkParams& p, SmallTable& t, int lane) {
     total = __reduce_add_sync(0xffffffffu, total);
     ChunkBound bound = chunk_bound(p, (float)total, n, (float)__reduce_max_sync(0xffffffffu, max(cost[0], cost[1])));
     int k[kPer], rows[kPer], at[kPer] = {}, row[kPer] = {}, pieces = 0, part_rows = 0;
-    auto cut = [&](const int (&after)[kPer]) {
+    auto cut = [&](const int (&place)[kPer], const int (&after)[kPer]) {
         int sum = 0;
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
-            k[j] = cost[j] >= 0 ? chunk_cuts(p, r[j], (float)after[j], bound) : 0;
+            k[j] = cost[j] >= 0 ? chunk_cuts(p, r[j], place[j], (float)after[j], (float)total, bound) : 0;
             rows[j] = k[j] > 1 ? k[j] * r[j].n_tok * p.G : 0;
             sum += rows[j];
         }
         part_rows = __reduce_add_sync(0xffffffffu, sum);
     };
     const int none[kPer] = {};
-    if ((float)total * p.Hkv <= kChunkGuide * p.grid * bound.narrow) cut(none);
+    if (bound.one_wave) cut(none, none);
     else part_rows = -1;
     if (part_rows >= 0 && (long)part_rows * p.Hkv <= p.part_rows) {
-        // so little work that the bound alone says how entries are cut: their order does not matter
+        // the bound alone says how entries are cut: their order does not matter
         int rows_so_far = 0;
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
@@ -249,8 +249,11 @@ __device__ void small_plan(const ChunkParams& p, SmallTable& t, int lane) {
                     else after[j] += c;
                 }
             }
+        int place[kPer];
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) place[j] = __popcll(ahead[j]);
         for (;; bound = chunk_coarser(bound)) {
-            cut(after);
+            cut(place, after);
             if (bound.narrow == kChunkNoBound || (long)part_rows * p.Hkv <= p.part_rows) break;    // else too much for the workspace
         }
 #pragma unroll
@@ -888,8 +891,9 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                         }
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            if (ml[i].x == -INFINITY) continue;             // that piece holds no key this row sees
-                            const float m_new = fmaxf(m[i], ml[i].x), fa = m[i] == -INFINITY ? 0.f : ex2(m[i] - m_new), fb = ex2(ml[i].x - m_new);
+                            // a piece without a key that this row sees counts 0 (and holds zeros); no branch, which would tear the loads apart
+                            const float m_new = fmaxf(m[i], ml[i].x);
+                            const float fa = m[i] == -INFINITY ? 0.f : ex2(m[i] - m_new), fb = ml[i].x == -INFINITY ? 0.f : ex2(ml[i].x - m_new);
                             const float v[8] = {va[i].x, va[i].y, va[i].z, va[i].w, vb[i].x, vb[i].y, vb[i].z, vb[i].w};
 #pragma unroll
                             for (int c = 0; c < 8; ++c) acc[i][c] = acc[i][c] * fa + v[c] * fb;

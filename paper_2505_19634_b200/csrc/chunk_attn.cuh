@@ -25,7 +25,7 @@ struct ChunkPiece {
 static_assert(sizeof(ChunkPiece) == 48, "read as three 16-byte words");
 
 constexpr int kChunkTile = 128;                       // KV tokens per tile
-constexpr int kChunkPartsPerSm = 4;                   // wide pieces with partial results that the workspace has room for, per SM
+constexpr int kChunkPartsPerSm = 8;                   // wide pieces with partial results that the workspace has room for, per SM
 constexpr int kChunkSmall = 64;                       // calls of up to so many entries are scheduled inside the attention kernel
 
 struct ChunkHead {
@@ -85,36 +85,39 @@ __device__ __forceinline__ bool chunk_branch_ok(const ChunkParams& p, int lo, in
 }
 __device__ __forceinline__ int chunk_cost(const ChunkEntry& r, int T) { return r.tiles * (r.n_tok > T ? 2 : 1); }
 
-constexpr float kChunkGuide = 1.5f;
+constexpr float kChunkSlack = 10.f;                   // what the pieces of a call cost a CTA beside their tiles, about
 constexpr int kChunkNoBound = 1 << 30;                // leaves every entry whole
 
 // How small the pieces of a call may become.  `total`: the cost of its n entries per KV head, `largest` the costliest.
 //   one wave   fewer entries than CTAs, and no piece of it much longer than a CTA's share: at most `narrow` = total /
 //              (CTAs per KV head - n) per piece makes no more pieces than CTAs, whatever the entries are.  (200 tokens of
-//              40 heads over 4000 keys: 46 us in one wave of 128 pieces, 82 us as 192 shorter ones.)
+//              40 heads over 4000 keys: 44 us in one wave of 128 pieces, 82 us as 192 shorter ones.)
 //   guided     otherwise pieces get smaller towards the end of the list (chunk_cuts), down to a sixteenth of a CTA's
 //              share, but not below six tiles, whose time is several times what a piece costs by itself.  A wide piece's
 //              partial result is 256 rows to write and to join: its bound is twice a narrow one's.
-struct ChunkBound { int narrow, wide; };
+struct ChunkBound { int narrow, wide; bool one_wave; };
 __device__ __forceinline__ ChunkBound chunk_bound(const ChunkParams& p, float total, int n, float largest) {
     const float share = total * p.Hkv / p.grid, spare = (float)p.grid / p.Hkv - n;
     if (spare >= 1.f && fminf(total / spare, largest) <= share + 12.f) {
         const int b = max(4, (int)ceilf(total / spare));
-        return {b, max(b, 8)};
+        return {b, max(b, 8), true};
     }
     const int b = max(6, (int)(share / 16.f));
-    return {b, 2 * b};
+    return {b, 2 * b, false};
 }
 // larger pieces, when the partial results would not fit the workspace
 __device__ __forceinline__ ChunkBound chunk_coarser(ChunkBound b) {
-    const int n = b.narrow >= 4096 ? kChunkNoBound : b.narrow * 4;
-    return {n, n == kChunkNoBound ? n : b.wide * 4};
+    const int n = b.narrow >= 4096 ? kChunkNoBound : b.narrow * 2;
+    return {n, n == kChunkNoBound ? n : b.wide * 2, b.one_wave};
 }
-// Pieces of entry r when `left` per KV head is still to be handed out, its own cost included.
-__device__ __forceinline__ int chunk_cuts(const ChunkParams& p, const ChunkEntry& r, float left, ChunkBound bound) {
+// Pieces of entry r, the `place`-th to be handed out, when `left` per KV head is still to be, its own cost included.
+// Guided: a piece may cost what is left for each CTA, so that it ends with the others; those that every CTA starts with
+// may cost a CTA's whole share.
+__device__ __forceinline__ int chunk_cuts(const ChunkParams& p, const ChunkEntry& r, int place, float left, float total, ChunkBound bound) {
     if (bound.narrow == kChunkNoBound) return 1;
-    const bool wide = r.n_tok > p.T;
-    const float limit = fmaxf((float)(wide ? bound.wide : bound.narrow), left * p.Hkv / (kChunkGuide * p.grid));
+    const bool wide = r.n_tok > p.T, starts = (place + 1) * p.Hkv <= p.grid;
+    float limit = (float)(wide ? bound.wide : bound.narrow);
+    if (!bound.one_wave) limit = fmaxf(limit, (starts ? total : left) * p.Hkv / p.grid + kChunkSlack);
     return max(1, min(r.tiles, (int)ceilf((float)(wide ? 2 * r.tiles : r.tiles) / limit)));
 }
 

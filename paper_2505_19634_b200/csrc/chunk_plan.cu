@@ -4,12 +4,12 @@
 // The unit of cost is one KV tile of a narrow entry; a wide entry's tile costs two (256 query rows instead of
 // 128).  Entries are handed out in four classes of cost, the costliest first, and within a class branch by
 // branch, all KV heads of a piece one after the other, so that CTAs that run at the same time read neighbouring
-// keys.  An entry is cut so that no
-// piece costs more than the work that is still to be handed out when its turn comes, divided by kChunkGuide x
-// CTAs: early pieces are whole entries, later ones smaller and smaller, down to the call's bound
-// (chunk_bound), and all CTAs end within about one small piece of each other.  With whole entries alone the
-// last CTA ended 8 % behind the mean at 8192 new tokens over 24576 (1280 entries for 148 CTAs), 30 % behind it
-// with 64 single tokens over 1 k to 8 k keys.  Everything here is a function of the lengths alone: the cuts,
+// keys.  The first
+// entries, with which every CTA starts, stay whole; later ones are cut so that a piece costs what is left for
+// each CTA when its turn comes (chunk_cuts), down to the call's bound (chunk_bound), and all CTAs end within
+// about one small piece of each other.  With whole entries alone the last CTA ended 8 % behind the mean at
+// 8192 new tokens over 24576 (1280 entries for 148 CTAs), 30 % behind it with 64 single tokens over 1 k to 8 k
+// keys.  Everything here is a function of the lengths alone: the cuts,
 // and with them the results, do not depend on timing.
 //
 // The kernel is latency: its code runs once, cold.  Sorting the entries and trying 32 bounds took 15 us where
@@ -154,7 +154,7 @@ chunk_plan_kernel(const ChunkParams p) {
 #pragma unroll
         for (int i = 0; i < kPer; ++i)
             if (kPer * tid + i < n) {
-                k[i] = chunk_cuts(p, r[i], left[i], bound);
+                k[i] = chunk_cuts(p, r[i], kPer * tid + i, left[i], total, bound);
                 const int rows = k[i] > 1 ? k[i] * r[i].n_tok * p.G : 0;
                 if (i == 0) rows0 = rows;
                 mine += (unsigned)k[i] + ((unsigned long long)rows << 20);
