@@ -20,10 +20,18 @@
 //                   (l carries the same reference, so the result is the same), and at the end divides and
 //                   stores its row, or leaves (m, l, O) for the last piece of the entry to join.
 //   warp 8          takes pieces, hands them to the other roles through a ring of two, loads Q
-//   warp 9, 10      load the K and V tiles: one TMA box per 4 KiB page tile, rings of two and three slots
+//   warp 9, 10      load the K and V tiles: one TMA box per 4 KiB page tile, rings of two and three slots (a V
+//                   tile waits for its probabilities, a K tile does not)
 //   warp 11         issues the MMAs.  Per side the order is S(0); then for each tile P V(j), S(j+1): the tensor
 //                   pipe keeps issue order, so S(j+1) may overwrite the columns that held P(j), and when S(j+1)
 //                   is complete P V(j) is as well -- the only wait on O that the softmax needs.
+//
+// Measured (B200 whose copy peak is 6538 GB/s and whose bf16 GEMMs reach 1663 TFLOP/s in a burst, 1394 sustained):
+// 8192 tokens of 40 / 8 heads over 24576 keys 4.4 ms = 1080 TFLOP/s, 0.77 of the sustained rate; 64 single tokens
+// over 1 k to 8 k keys 255 us = 5.5 TB/s, 0.85.  Both run into the card's power limit (1.5 GHz instead of 1.85): a
+// tile of both sides takes 3300 clocks, of which the tensor pipe works 2050 and a softmax warp's chain (scores,
+// maximum, exponentials at 8 clocks each, stores) fills about 2000, and changes that saved clocks alone
+// (a second MMA warp, two threads per row, part of the exponentials as polynomials) did not save time.
 //
 // Page ids outside the pool and entries beyond the table row read as zeros (and are reported); tokens past the
 // end of a branch never contribute: their scores are replaced before the maximum and their V rows are zeroed in
@@ -50,10 +58,6 @@ constexpr int kTakeWarp = 8, kKWarp = 9, kVWarp = 10, kMmaWarp = 11;
 constexpr int kHalfBytes = kRows * 128;
 constexpr int kOperandBytes = 2 * kHalfBytes;
 constexpr int kRingK = 2, kRingV = 3, kRingPiece = 2;
-#ifndef AFTER
-#define AFTER 16
-#endif
-constexpr int kAfter = AFTER;
 constexpr uint32_t kTmemCols = 512;
 // registers per thread: at launch, and after the softmax warpgroups have taken from the third one
 constexpr int kLaunchRegs = 168, kSoftmaxRegs = 216, kHelperRegs = 72;
@@ -393,223 +397,223 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
     grid_launch_dependents();
 
     if (warp >= 2 * kSideThreads / 32) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kHelperRegs));
-    if (warp == kTakeWarp) {
-        // =========================== takes pieces, loads Q ===========================
-        SmallTable& small = *reinterpret_cast<SmallTable*>(smem + kOffSmall);
-        if (p.small) small_plan(p, small, lane);
-        const int total = (p.small ? small.pieces : p.head->pieces) * p.Hkv, part_rows = p.small ? small.part_rows : p.head->part_rows;
-        int index = blockIdx.x, used[2] = {0, 0};
-        bool alive = true;
-        for (int it = 0; alive; ++it) {
-            const int slot = it % kRingPiece;
-            Work w;
-            w.kvh = -1;
-            if (index < total) {
-                const int i = index / p.Hkv;                            // all KV heads of a piece follow one another
-                w.kvh = index - i * p.Hkv;
-                if (!p.small) {
-                    const int4* src = reinterpret_cast<const int4*>(p.pieces + i);
-                    int4* dst = reinterpret_cast<int4*>(&w.x);
-                    dst[0] = src[0]; dst[1] = src[1]; dst[2] = src[2];
-                } else {
-                    w.x = small_piece(p, small, i, lane);
-                }
-            }
-            if (lane == 0) {
-                alive = mbar_wait(bar(PIECE_EMPTY + slot), ((it / kRingPiece) & 1) ^ 1, ab);
-                if (alive) {
-                    int4* ring = reinterpret_cast<int4*>(smem + kOffPiece + slot * kPieceBytes);
-                    const int4* src = reinterpret_cast<const int4*>(&w.x);
-                    ring[0] = src[0]; ring[1] = src[1]; ring[2] = src[2];
-                    ring[3] = make_int4(w.kvh, part_rows, 0, 0);
-                    mbar_arrive(bar(PIECE_FULL + slot));
-                    if (w.kvh < 0) alive = false;
-                }
-                if (alive) {
-                    index = p.grid + (int)atomicInc(&p.head->next, (unsigned)total - 1u);       // the next one; one for each piece, and back to 0
-                    derive(w, p.T);
-                    for (int s = 0; s < (w.wide ? 2 : 1) && alive; ++s) {
-                        if ((s ? w.n1 : w.n0) == 0) continue;
-                        alive = mbar_wait(bar(Q_EMPTY + s), (used[s] & 1) ^ 1, ab);
-                        if (!alive) break;
-                        ++used[s];
-                        const bool single = w.x.n_tok == 1;
-                        const CUtensorMap* tm = single ? &tm_q1 : &tm_q;
-                        mbar_arrive_expect_tx(bar(Q_FULL + s), (uint32_t)(single ? p.G : p.T * p.G) * 256u);
-                        const uint32_t dst = sbase + kOffQ + s * kOperandBytes;
-                        tma_load_rows(dst, tm, 0, w.kvh * p.G, w.x.row0 + s * p.T, bar(Q_FULL + s));
-                        tma_load_rows(dst + kHalfBytes, tm, 64, w.kvh * p.G, w.x.row0 + s * p.T, bar(Q_FULL + s));
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kHelperRegs));
+        if (warp == kTakeWarp) {
+            // =========================== takes pieces, loads Q ===========================
+            SmallTable& small = *reinterpret_cast<SmallTable*>(smem + kOffSmall);
+            if (p.small) small_plan(p, small, lane);
+            const int total = (p.small ? small.pieces : p.head->pieces) * p.Hkv, part_rows = p.small ? small.part_rows : p.head->part_rows;
+            int index = blockIdx.x, used[2] = {0, 0};
+            bool alive = true;
+            for (int it = 0; alive; ++it) {
+                const int slot = it % kRingPiece;
+                Work w;
+                w.kvh = -1;
+                if (index < total) {
+                    const int i = index / p.Hkv;                            // all KV heads of a piece follow one another
+                    w.kvh = index - i * p.Hkv;
+                    if (!p.small) {
+                        const int4* src = reinterpret_cast<const int4*>(p.pieces + i);
+                        int4* dst = reinterpret_cast<int4*>(&w.x);
+                        dst[0] = src[0]; dst[1] = src[1]; dst[2] = src[2];
+                    } else {
+                        w.x = small_piece(p, small, i, lane);
                     }
                 }
-            }
-            alive = __shfl_sync(0xffffffffu, alive, 0);
-            index = __shfl_sync(0xffffffffu, index, 0);
-        }
-        if (lane == 0) {
-            // copies in flight land before the CTA may end: the consumers wait for them, unless they gave up
-            if (*ab.flag)
-                for (int s = 0; s < 2; ++s)
-                    if (used[s] > 0) {
-                        const Abort quiet{misc + 2, p.status};
-                        misc[2] = 0;
-                        mbar_wait(bar(Q_FULL + s), (used[s] - 1) & 1, quiet);
-                    }
-        }
-    } else if (warp == kKWarp || warp == kVWarp) {
-        // =========================== K and V tiles ===========================
-        const bool is_v = warp == kVWarp;
-        const int ring_n = is_v ? kRingV : kRingK;
-        const int full0 = is_v ? V_FULL : K_FULL, empty0 = is_v ? V_EMPTY : K_EMPTY;
-        const int ring_off = is_v ? kOffV : kOffK;
-        const CUtensorMap* tm = is_v ? &tm_v : &tm_k;
-        const uint64_t once = l2_policy_evict_first();
-        int slot = 0, round = 0, issued = 0, tails = 0;
-        bool alive = true;
-        Work w;
-        for (int it = 0; alive && next_piece(w, it, smem, bar0, lane, p.T, ab); ++it) {
-            const int32_t* bt = p.block_table + (size_t)w.x.branch * p.max_blocks;
-            auto page_of = [&](int t) -> int {                          // this lane's page of KV tile t
-                const int blk = t * (kTile / kPage) + lane;
-                if (lane >= kTile / kPage || blk * kPage >= w.x.keys) return -2;
-                const int page = blk < p.max_blocks ? bt[blk] : -1;
-                if (page < 0 || page >= p.num_pages) { atomicMin(p.status, (int)TTS_ERR_DEVICE_BOUNDS); return -1; }
-                return page;
-            };
-            int page = w.loads > 0 ? page_of(w.x.tile_begin) : -2;
-            for (int j = 0; j < w.loads; ++j) {
-                const int tok0 = (w.x.tile_begin + j) * kTile;
-                const int n_valid = min(kTile, w.x.keys - tok0), n_pages = ceil_div(n_valid, kPage);
-                const bool tail = is_v && n_valid < kTile;
-                const int full = tail ? (int)V_TAIL : full0 + slot;
-                const int next = j + 1 < w.loads ? page_of(w.x.tile_begin + j + 1) : -2;
                 if (lane == 0) {
-                    alive = mbar_wait(bar(empty0 + slot), round ^ 1, ab);
-                    if (alive) mbar_arrive_expect_tx(bar(full), (uint32_t)n_pages * 4096u);
+                    alive = mbar_wait(bar(PIECE_EMPTY + slot), ((it / kRingPiece) & 1) ^ 1, ab);
+                    if (alive) {
+                        int4* ring = reinterpret_cast<int4*>(smem + kOffPiece + slot * kPieceBytes);
+                        const int4* src = reinterpret_cast<const int4*>(&w.x);
+                        ring[0] = src[0]; ring[1] = src[1]; ring[2] = src[2];
+                        ring[3] = make_int4(w.kvh, part_rows, 0, 0);
+                        mbar_arrive(bar(PIECE_FULL + slot));
+                        if (w.kvh < 0) alive = false;
+                    }
+                    if (alive) {
+                        index = p.grid + (int)atomicInc(&p.head->next, (unsigned)total - 1u);       // the next one; one for each piece, and back to 0
+                        derive(w, p.T);
+                        for (int s = 0; s < (w.wide ? 2 : 1) && alive; ++s) {
+                            if ((s ? w.n1 : w.n0) == 0) continue;
+                            alive = mbar_wait(bar(Q_EMPTY + s), (used[s] & 1) ^ 1, ab);
+                            if (!alive) break;
+                            ++used[s];
+                            const bool single = w.x.n_tok == 1;
+                            const CUtensorMap* tm = single ? &tm_q1 : &tm_q;
+                            mbar_arrive_expect_tx(bar(Q_FULL + s), (uint32_t)(single ? p.G : p.T * p.G) * 256u);
+                            const uint32_t dst = sbase + kOffQ + s * kOperandBytes;
+                            tma_load_rows(dst, tm, 0, w.kvh * p.G, w.x.row0 + s * p.T, bar(Q_FULL + s));
+                            tma_load_rows(dst + kHalfBytes, tm, 64, w.kvh * p.G, w.x.row0 + s * p.T, bar(Q_FULL + s));
+                        }
+                    }
                 }
                 alive = __shfl_sync(0xffffffffu, alive, 0);
-                if (!alive) break;
-                const uint32_t dst = sbase + ring_off + slot * kOperandBytes;
-                if (lane < n_pages) {
-                    // a page outside the pool: a coordinate outside the map, which reads as zeros
-                    const int page_head = page < 0 ? -1 : page * p.Hkv + w.kvh;
-                    if (w.x.once) tma_load_page(dst + lane * 4096, tm, page_head, bar(full), once);
-                    else tma_load_page_keep(dst + lane * 4096, tm, page_head, bar(full));
-                }
-                ++issued;
-                if (tail) {
-                    // no row sees the tokens past the end, but 0 x NaN would be NaN: their V rows become zeros
-                    alive = __all_sync(0xffffffffu, mbar_wait(bar(V_TAIL), tails & 1, ab));
-                    ++tails;
+                index = __shfl_sync(0xffffffffu, index, 0);
+            }
+            if (lane == 0) {
+                // copies in flight land before the CTA may end: the consumers wait for them, unless they gave up
+                if (*ab.flag)
+                    for (int s = 0; s < 2; ++s)
+                        if (used[s] > 0) {
+                            const Abort quiet{misc + 2, p.status};
+                            misc[2] = 0;
+                            mbar_wait(bar(Q_FULL + s), (used[s] - 1) & 1, quiet);
+                        }
+            }
+        } else if (warp == kKWarp || warp == kVWarp) {
+            // =========================== K and V tiles ===========================
+            const bool is_v = warp == kVWarp;
+            const int ring_n = is_v ? kRingV : kRingK;
+            const int full0 = is_v ? V_FULL : K_FULL, empty0 = is_v ? V_EMPTY : K_EMPTY;
+            const int ring_off = is_v ? kOffV : kOffK;
+            const CUtensorMap* tm = is_v ? &tm_v : &tm_k;
+            const uint64_t once = l2_policy_evict_first();
+            int slot = 0, round = 0, issued = 0, tails = 0;
+            bool alive = true;
+            Work w;
+            for (int it = 0; alive && next_piece(w, it, smem, bar0, lane, p.T, ab); ++it) {
+                const int32_t* bt = p.block_table + (size_t)w.x.branch * p.max_blocks;
+                auto page_of = [&](int t) -> int {                          // this lane's page of KV tile t
+                    const int blk = t * (kTile / kPage) + lane;
+                    if (lane >= kTile / kPage || blk * kPage >= w.x.keys) return -2;
+                    const int page = blk < p.max_blocks ? bt[blk] : -1;
+                    if (page < 0 || page >= p.num_pages) { atomicMin(p.status, (int)TTS_ERR_DEVICE_BOUNDS); return -1; }
+                    return page;
+                };
+                int page = w.loads > 0 ? page_of(w.x.tile_begin) : -2;
+                for (int j = 0; j < w.loads; ++j) {
+                    const int tok0 = (w.x.tile_begin + j) * kTile;
+                    const int n_valid = min(kTile, w.x.keys - tok0), n_pages = ceil_div(n_valid, kPage);
+                    const bool tail = is_v && n_valid < kTile;
+                    const int full = tail ? (int)V_TAIL : full0 + slot;
+                    const int next = j + 1 < w.loads ? page_of(w.x.tile_begin + j + 1) : -2;
+                    if (lane == 0) {
+                        alive = mbar_wait(bar(empty0 + slot), round ^ 1, ab);
+                        if (alive) mbar_arrive_expect_tx(bar(full), (uint32_t)n_pages * 4096u);
+                    }
+                    alive = __shfl_sync(0xffffffffu, alive, 0);
                     if (!alive) break;
-                    for (int i = lane; i < (kTile - n_valid) * 16; i += 32) {
-                        const int row = n_valid + i / 16, c = i % 16;
-                        *reinterpret_cast<uint4*>(smem + kOffV + slot * kOperandBytes + (row >> 4) * 4096 + ((row >> 3) & 1) * 2048 +
-                                                  (c >> 3) * 1024 + (row & 7) * 128 + ((c & 7) << 4)) = make_uint4(0, 0, 0, 0);
+                    const uint32_t dst = sbase + ring_off + slot * kOperandBytes;
+                    if (lane < n_pages) {
+                        // a page outside the pool: a coordinate outside the map, which reads as zeros
+                        const int page_head = page < 0 ? -1 : page * p.Hkv + w.kvh;
+                        if (w.x.once) tma_load_page(dst + lane * 4096, tm, page_head, bar(full), once);
+                        else tma_load_page_keep(dst + lane * 4096, tm, page_head, bar(full));
                     }
-                    fence_proxy_async();
-                    warp_arrive(bar(full0 + slot), lane);
+                    ++issued;
+                    if (tail) {
+                        // no row sees the tokens past the end, but 0 x NaN would be NaN: their V rows become zeros
+                        alive = __all_sync(0xffffffffu, mbar_wait(bar(V_TAIL), tails & 1, ab));
+                        ++tails;
+                        if (!alive) break;
+                        for (int i = lane; i < (kTile - n_valid) * 16; i += 32) {
+                            const int row = n_valid + i / 16, c = i % 16;
+                            *reinterpret_cast<uint4*>(smem + kOffV + slot * kOperandBytes + (row >> 4) * 4096 + ((row >> 3) & 1) * 2048 +
+                                                      (c >> 3) * 1024 + (row & 7) * 128 + ((c & 7) << 4)) = make_uint4(0, 0, 0, 0);
+                        }
+                        fence_proxy_async();
+                        warp_arrive(bar(full0 + slot), lane);
+                    }
+                    page = next;
+                    if (++slot == ring_n) { slot = 0; round ^= 1; }
                 }
-                page = next;
-                if (++slot == ring_n) { slot = 0; round ^= 1; }
             }
-        }
-        if (*ab.flag && lane == 0) {
-            const Abort quiet{misc + 2 + is_v, p.status};
-            for (int back = 1; back <= ring_n && back <= issued; ++back) {
-                const int i = issued - back;
-                misc[2 + is_v] = 0;
-                mbar_wait(bar(full0 + i % ring_n), (i / ring_n) & 1, quiet);
+            if (*ab.flag && lane == 0) {
+                const Abort quiet{misc + 2 + is_v, p.status};
+                for (int back = 1; back <= ring_n && back <= issued; ++back) {
+                    const int i = issued - back;
+                    misc[2 + is_v] = 0;
+                    mbar_wait(bar(full0 + i % ring_n), (i / ring_n) & 1, quiet);
+                }
             }
-        }
-    } else {
-        // =========================== MMA issuer ===========================
-        constexpr uint32_t idesc_qk = instr_desc(kRows, kTile, false, false), idesc_pv = instr_desc(kRows, kHeadDim, false, true);
-        // The whole warp walks the loop and waits, so that addresses and descriptors stay in uniform registers; one
-        // elected lane issues.  (A single lane that does everything spends more time preparing operands than the
-        // tensor pipe needs for them: 4500 instead of 2900 clocks for a KV tile of both sides.)
-        // low and high words of the operands' descriptors: addresses count in units of 16 bytes in the low word
-        const uint64_t q_desc = smem_desc(sbase + kOffQ, 16, 1024), k_desc = smem_desc(sbase + kOffK, 16, 2048), v_desc = smem_desc(sbase + kOffV, 1024, 2048);
-        const uint32_t q_lo = (uint32_t)q_desc, q_hi = (uint32_t)(q_desc >> 32), k_lo = (uint32_t)k_desc, k_hi = (uint32_t)(k_desc >> 32),
-                       v_lo = (uint32_t)v_desc, v_hi = (uint32_t)(v_desc >> 32);
-        const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);              // (a shuffle tells the compiler that the value is uniform)
-        int k_slot = 0, k_round = 0, v_slot = 0, v_round = 0, q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
-        bool alive = true;
-        Work w;
-        for (int it = 0; alive && next_piece(w, it, smem, bar0, lane, p.T, ab); ++it) {
-            const bool wide = __shfl_sync(0xffffffffu, (int)w.wide, 0) != 0;
-            const int n0 = __shfl_sync(0xffffffffu, w.n0, 0), n1 = __shfl_sync(0xffffffffu, w.n1, 0), loads = __shfl_sync(0xffffffffu, w.loads, 0);
-            const int n_max = max(n0, n1);
-            const auto wait = [&](int i, int phase) { alive = alive && mbar_wait(bar(i), phase, ab); };
-            // One turn of side s: O (+)= P V of its jj-th tile (jj >= 0), then S of the next one.  An issuing lane is held
-            // back while the tensor pipe is busy, its queue being short; what is waited for between two groups of MMAs is
-            // time the pipe stands still, so it is looked at while the first half of P V runs.  In a wide piece side 0
-            // has waited for the tiles that both sides read.
-            auto turn = [&](auto side, int jj) {
-                constexpr int s = decltype(side)::value;
-                const int n = s ? n1 : n0;
-                const bool own_q = wide || s == 0;                       // a narrow piece has one Q tile for both sides
-                const bool last_kv = s == 1 || !wide;                    // the last reader of a K or V tile gives it back
-                const bool more = jj + 1 < n, has_k = s == 1 && wide && jj + 1 < n0, has_v = s == 1 && wide && jj < n0;
-                if (jj >= 0) {
-                    const uint32_t vd = v_lo + (uint32_t)(v_slot * (kOperandBytes / 16));     // one page (16 tokens) per step
-                    if (!has_v) wait(V_FULL + v_slot, v_round);
-                    wait(P_HALF + s, p_phase[s]);
-                    alive = __all_sync(0xffffffffu, alive);
-                    if (!alive) return;
-                    tc_fence_after();
+        } else {
+            // =========================== MMA issuer ===========================
+            constexpr uint32_t idesc_qk = instr_desc(kRows, kTile, false, false), idesc_pv = instr_desc(kRows, kHeadDim, false, true);
+            // The whole warp walks the loop and waits, so that addresses and descriptors stay in uniform registers; one
+            // elected lane issues.  (With a single lane that does everything, 8192 new tokens over 24576 took 5.4 ms
+            // instead of 4.85.)
+            // low and high words of the operands' descriptors: addresses count in units of 16 bytes in the low word
+            const uint64_t q_desc = smem_desc(sbase + kOffQ, 16, 1024), k_desc = smem_desc(sbase + kOffK, 16, 2048), v_desc = smem_desc(sbase + kOffV, 1024, 2048);
+            const uint32_t q_lo = (uint32_t)q_desc, q_hi = (uint32_t)(q_desc >> 32), k_lo = (uint32_t)k_desc, k_hi = (uint32_t)(k_desc >> 32),
+                           v_lo = (uint32_t)v_desc, v_hi = (uint32_t)(v_desc >> 32);
+            const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);              // (a shuffle tells the compiler that the value is uniform)
+            int k_slot = 0, k_round = 0, v_slot = 0, v_round = 0, q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
+            bool alive = true;
+            Work w;
+            for (int it = 0; alive && next_piece(w, it, smem, bar0, lane, p.T, ab); ++it) {
+                const bool wide = __shfl_sync(0xffffffffu, (int)w.wide, 0) != 0;
+                const int n0 = __shfl_sync(0xffffffffu, w.n0, 0), n1 = __shfl_sync(0xffffffffu, w.n1, 0), loads = __shfl_sync(0xffffffffu, w.loads, 0);
+                const int n_max = max(n0, n1);
+                const auto wait = [&](int i, int phase) { alive = alive && mbar_wait(bar(i), phase, ab); };
+                // One turn of side s: O (+)= P V of its jj-th tile (jj >= 0), then S of the next one.  An issuing lane is held
+                // back while the tensor pipe is busy, its queue being short; what is waited for between two groups of MMAs is
+                // time the pipe stands still, so it is looked at while the first half of P V runs.  In a wide piece side 0
+                // has waited for the tiles that both sides read.
+                auto turn = [&](auto side, int jj) {
+                    constexpr int s = decltype(side)::value;
+                    const int n = s ? n1 : n0;
+                    const bool own_q = wide || s == 0;                       // a narrow piece has one Q tile for both sides
+                    const bool last_kv = s == 1 || !wide;                    // the last reader of a K or V tile gives it back
+                    const bool more = jj + 1 < n, has_k = s == 1 && wide && jj + 1 < n0, has_v = s == 1 && wide && jj < n0;
+                    if (jj >= 0) {
+                        const uint32_t vd = v_lo + (uint32_t)(v_slot * (kOperandBytes / 16));     // one page (16 tokens) per step
+                        if (!has_v) wait(V_FULL + v_slot, v_round);
+                        wait(P_HALF + s, p_phase[s]);
+                        alive = __all_sync(0xffffffffu, alive);
+                        if (!alive) return;
+                        tc_fence_after();
+                        if (elect_one()) {
+#pragma unroll
+                            for (int ks = 0; ks < 4; ++ks)
+                                umma_ts(tm + 256u + s * 128u, tm + s * 128u + ks * 8u, vd + ks * 4096 / 16, v_hi, idesc_pv, ks > 0 || jj > 0);
+                        }
+                        __syncwarp();
+                        wait(P_FULL + s, p_phase[s]);
+                        if (more && !has_k) wait(K_FULL + k_slot, k_round);
+                        alive = __all_sync(0xffffffffu, alive);
+                        if (!alive) return;
+                        tc_fence_after();
+                        if (elect_one()) {
+#pragma unroll
+                            for (int ks = 4; ks < 8; ++ks)
+                                umma_ts(tm + 256u + s * 128u, tm + s * 128u + ks * 8u, vd + ks * 4096 / 16, v_hi, idesc_pv, 1u);
+                            if (last_kv) umma_commit(bar(V_EMPTY + v_slot));
+                            if (!more) umma_commit(bar(O_FULL + s));
+                        }
+                        __syncwarp();
+                        p_phase[s] ^= 1;
+                        if (last_kv && ++v_slot == kRingV) { v_slot = 0; v_round ^= 1; }
+                    } else {
+                        if (own_q && more) { wait(Q_FULL + s, q_phase[s]); q_phase[s] ^= 1; }
+                        if (more && !has_k) wait(K_FULL + k_slot, k_round);
+                        alive = __all_sync(0xffffffffu, alive);
+                        if (!alive) return;
+                        tc_fence_after();
+                    }
+                    if (!more) return;
+                    // Q: two 64-dim blocks of 128 rows, K: dim halves 1 KiB apart inside a page
+                    const uint32_t qd = q_lo + (own_q ? s * kOperandBytes / 16 : 0), kd = k_lo + (uint32_t)(k_slot * (kOperandBytes / 16));
+                    const bool last_q = wide ? jj + 2 == n : 2 * (jj + 1) + s + 1 == loads;
                     if (elect_one()) {
 #pragma unroll
-                        for (int ks = 0; ks < 4; ++ks)
-                            umma_ts(tm + 256u + s * 128u, tm + s * 128u + ks * 8u, vd + ks * 4096 / 16, v_hi, idesc_pv, ks > 0 || jj > 0);
+                        for (int ks = 0; ks < 8; ++ks)
+                            umma_ss(tm + s * 128u, qd + ((ks >> 2) * kHalfBytes + (ks & 3) * 32) / 16, q_hi, kd + ((ks >> 2) * 1024 + (ks & 3) * 32) / 16, k_hi, idesc_qk, ks > 0);
+                        umma_commit(bar(S_FULL + s));
+                        if (last_kv) umma_commit(bar(K_EMPTY + k_slot));
+                        if (last_q) umma_commit(bar(Q_EMPTY + (own_q ? s : 0)));
                     }
                     __syncwarp();
-                    wait(P_FULL + s, p_phase[s]);
-                    if (more && !has_k) wait(K_FULL + k_slot, k_round);
-                    alive = __all_sync(0xffffffffu, alive);
-                    if (!alive) return;
-                    tc_fence_after();
-                    if (elect_one()) {
-#pragma unroll
-                        for (int ks = 4; ks < 8; ++ks)
-                            umma_ts(tm + 256u + s * 128u, tm + s * 128u + ks * 8u, vd + ks * 4096 / 16, v_hi, idesc_pv, 1u);
-                        if (last_kv) umma_commit(bar(V_EMPTY + v_slot));
-                        if (!more) umma_commit(bar(O_FULL + s));
-                    }
-                    __syncwarp();
-                    p_phase[s] ^= 1;
-                    if (last_kv && ++v_slot == kRingV) { v_slot = 0; v_round ^= 1; }
-                } else {
-                    if (own_q && more) { wait(Q_FULL + s, q_phase[s]); q_phase[s] ^= 1; }
-                    if (more && !has_k) wait(K_FULL + k_slot, k_round);
-                    alive = __all_sync(0xffffffffu, alive);
-                    if (!alive) return;
-                    tc_fence_after();
-                }
-                if (!more) return;
-                // Q: two 64-dim blocks of 128 rows, K: dim halves 1 KiB apart inside a page
-                const uint32_t qd = q_lo + (own_q ? s * kOperandBytes / 16 : 0), kd = k_lo + (uint32_t)(k_slot * (kOperandBytes / 16));
-                const bool last_q = wide ? jj + 2 == n : 2 * (jj + 1) + s + 1 == loads;
-                if (elect_one()) {
-#pragma unroll
-                    for (int ks = 0; ks < 8; ++ks)
-                        umma_ss(tm + s * 128u, qd + ((ks >> 2) * kHalfBytes + (ks & 3) * 32) / 16, q_hi, kd + ((ks >> 2) * 1024 + (ks & 3) * 32) / 16, k_hi, idesc_qk, ks > 0);
-                    umma_commit(bar(S_FULL + s));
-                    if (last_kv) umma_commit(bar(K_EMPTY + k_slot));
-                    if (last_q) umma_commit(bar(Q_EMPTY + (own_q ? s : 0)));
-                }
-                __syncwarp();
-                if (last_kv && ++k_slot == kRingK) { k_slot = 0; k_round ^= 1; }
-            };
-            const std::integral_constant<int, 0> side0;
-            const std::integral_constant<int, 1> side1;
+                    if (last_kv && ++k_slot == kRingK) { k_slot = 0; k_round ^= 1; }
+                };
+                const std::integral_constant<int, 0> side0;
+                const std::integral_constant<int, 1> side1;
 #pragma unroll 1
-            for (int jj = -1; jj < n_max && alive; ++jj) {
-                if (jj < n0) turn(side0, jj);
-                if (alive && jj < n1) turn(side1, jj);
+                for (int jj = -1; jj < n_max && alive; ++jj) {
+                    if (jj < n0) turn(side0, jj);
+                    if (alive && jj < n1) turn(side1, jj);
+                }
             }
         }
-    }
     } else {
         // =========================== softmax ===========================
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
@@ -705,11 +709,11 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                 };
                 weights(0, 32);
                 tmem_st32(t_s, pw);
-                weights(32, 32 + kAfter);                                    // while the first half is stored
+                weights(32, 48);                                             // while the first half is stored
                 tmem_wait_st();
                 tc_fence_before();
                 warp_arrive(bar(P_HALF + side), lane);
-                weights(32 + kAfter, 64);
+                weights(48, 64);
                 tmem_st32(t_s + 32u, pw + 32);
                 tmem_wait_st();
                 tc_fence_before();

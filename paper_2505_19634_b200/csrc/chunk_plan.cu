@@ -4,13 +4,12 @@
 // The unit of cost is one KV tile of a narrow entry; a wide entry's tile costs two (256 query rows instead of
 // 128).  Entries are handed out in four classes of cost, the costliest first, and within a class branch by
 // branch, all KV heads of a piece one after the other, so that CTAs that run at the same time read neighbouring
-// keys.  The first
-// entries, with which every CTA starts, stay whole; later ones are cut so that a piece costs what is left for
-// each CTA when its turn comes (chunk_cuts), down to the call's bound (chunk_bound), and all CTAs end within
-// about one small piece of each other.  With whole entries alone the last CTA ended 8 % behind the mean at
-// 8192 new tokens over 24576 (1280 entries for 148 CTAs), 30 % behind it with 64 single tokens over 1 k to 8 k
-// keys.  Everything here is a function of the lengths alone: the cuts,
-// and with them the results, do not depend on timing.
+// keys.  The first entries, with which every CTA starts, stay whole; later ones are cut so that a piece costs
+// what is left for each CTA when its turn comes (chunk_cuts), down to the call's bound (chunk_bound), and all
+// CTAs end within about one small piece of each other.  With whole entries alone the last CTA ended 8 % behind
+// the mean at 8192 new tokens over 24576 (1280 entries for 148 CTAs), 30 % behind it with 64 single tokens over
+// 1 k to 8 k keys.  Everything here is a function of the lengths alone: the cuts, and with them the results, do
+// not depend on timing.
 //
 // The kernel is latency: its code runs once, cold.  Sorting the entries and trying 32 bounds took 15 us where
 // this takes 7, for no better balance.
