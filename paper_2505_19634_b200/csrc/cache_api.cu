@@ -134,8 +134,9 @@ int tts_chunk_attn(tts_ctx* ctx, const void* q, int64_t q_row_stride, const void
     memset(&p, 0, sizeof p);
     p.block_table = block_table; p.branch_lens = branch_lens; p.row_start = row_start;
     p.out = out; p.lse = lse;
-    // the entries of a call: at most one per branch and one per 2 T rows
-    const bool small = (long)total_rows / (2 * (128 / (f.n_q_heads / f.n_kv_heads))) + n_branches <= kChunkSmall;
+    // the entries of a call: at most one per branch and one per 2 T rows, and not more than rows
+    const long entries = (long)total_rows / (2 * (128 / (f.n_q_heads / f.n_kv_heads))) + n_branches;
+    const bool small = n_branches <= kChunkSmall && (entries <= kChunkSmall || total_rows <= kChunkSmall);
     p.small = small;
     p.head = c->chunk_head; p.pieces = c->chunk_pieces; p.arrived = c->chunk_arrived;
     p.part_o = c->chunk_part_o; p.part_ml = c->chunk_part_ml;
