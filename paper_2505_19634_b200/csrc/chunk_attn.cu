@@ -235,9 +235,10 @@ __device__ void small_plan(const ChunkParams& p, SmallTable& t, int lane) {
         int rows_so_far = 0;
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
-            int sum_k, sum_rows;
+            if (32 * j >= n) break;
+            int sum_k, sum_rows = 0;
             at[j] = pieces + warp_scan(k[j], lane, &sum_k);
-            row[j] = rows_so_far + warp_scan(rows[j], lane, &sum_rows);
+            if (part_rows > 0) row[j] = rows_so_far + warp_scan(rows[j], lane, &sum_rows);
             pieces += sum_k; rows_so_far += sum_rows;
         }
     } else {

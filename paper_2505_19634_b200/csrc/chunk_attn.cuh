@@ -53,6 +53,7 @@ struct ChunkParams {
     int max_pieces;                // capacity: pieces per KV head
     long part_rows;                // capacity: partial-result rows
     int grid;
+    float heads_per_cta, ctas_per_head;   // Hkv / grid, grid / Hkv
     int out_dtype;
     float scale_log2;
 };
@@ -74,7 +75,7 @@ __device__ __forceinline__ ChunkPiece chunk_piece(const ChunkEntry& r, int e, in
     ChunkPiece x;
     x.branch = r.b; x.row0 = r.row0; x.n_tok = r.n_tok; x.limit0 = r.limit0; x.keys = r.keys;
     // as even as whole tiles go, the longer ones first
-    const int each = r.tiles / parts, longer = r.tiles - each * parts;
+    const int each = parts == 1 ? r.tiles : r.tiles / parts, longer = r.tiles - each * parts;
     x.tile_begin = part * each + min(part, longer); x.tile_end = x.tile_begin + each + (part < longer);
     x.parts = parts; x.part = part; x.part_row = part_row; x.entry = e; x.once = r.once;
     return x;
@@ -97,9 +98,9 @@ constexpr int kChunkNoBound = 1 << 30;                // leaves every entry whol
 //              partial result is 256 rows to write and to join: its bound is twice a narrow one's.
 struct ChunkBound { int narrow, wide; bool one_wave; };
 __device__ __forceinline__ ChunkBound chunk_bound(const ChunkParams& p, float total, int n, float largest) {
-    const float share = total * p.Hkv / p.grid, spare = (float)p.grid / p.Hkv - n;
-    if (spare >= 1.f && fminf(total / spare, largest) <= share + 12.f) {
-        const int b = max(4, (int)ceilf(total / spare));
+    const float share = total * p.heads_per_cta, spare = p.ctas_per_head - n, one = __fdividef(total, fmaxf(spare, 1.f));
+    if (spare >= 1.f && fminf(one, largest) <= share + 12.f) {
+        const int b = max(4, (int)ceilf(one));
         return {b, max(b, 8), true};
     }
     const int b = max(6, (int)(share / 16.f));
@@ -117,8 +118,8 @@ __device__ __forceinline__ int chunk_cuts(const ChunkParams& p, const ChunkEntry
     if (bound.narrow == kChunkNoBound) return 1;
     const bool wide = r.n_tok > p.T, starts = (place + 1) * p.Hkv <= p.grid;
     float limit = (float)(wide ? bound.wide : bound.narrow);
-    if (!bound.one_wave) limit = fmaxf(limit, (starts ? total : left) * p.Hkv / p.grid + kChunkSlack);
-    return max(1, min(r.tiles, (int)ceilf((float)(wide ? 2 * r.tiles : r.tiles) / limit)));
+    if (!bound.one_wave) limit = fmaxf(limit, (starts ? total : left) * p.heads_per_cta + kChunkSlack);
+    return max(1, min(r.tiles, (int)ceilf(__fdividef((float)(wide ? 2 * r.tiles : r.tiles), limit))));
 }
 
 cudaError_t launch_chunk_plan(const ChunkParams& p, cudaStream_t st);
