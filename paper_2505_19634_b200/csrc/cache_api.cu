@@ -145,6 +145,7 @@ int tts_chunk_attn(tts_ctx* ctx, const void* q, int64_t q_row_stride, const void
     p.prefix_len = prefix_len; p.n_branches = n_branches; p.total_rows = total_rows; p.max_blocks = f.max_blocks_per_branch; p.num_pages = f.num_pages;
     p.max_pieces = c->chunk_max_pieces; p.part_rows = c->chunk_part_rows;
     p.grid = f.max_ctas > 0 && f.max_ctas < c->n_sms ? f.max_ctas : c->n_sms;
+    p.g_inv = 65536u / (unsigned)p.G + 1u;
     p.heads_per_cta = (float)p.Hkv / p.grid; p.ctas_per_head = (float)p.grid / p.Hkv;
     p.out_dtype = f.out_dtype;
     p.scale_log2 = (f.softmax_scale > 0.f ? f.softmax_scale : 1.0f / sqrtf((float)f.head_dim)) * 1.4426950408889634f;

@@ -633,7 +633,7 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                 Work w;
                 if (!next_piece<true>(w, it, smem, bar0, lane, p.T, ab)) break;
                 const int tok0 = w.wide ? side * p.T : 0;                           // first token of this side's rows
-                const int tl = ((warp & 3) * 32 + lane) / p.G, last = min(p.T, w.x.n_tok - tok0) - 1;
+                const int tl = (int)(((warp & 3) * 32 + lane) * p.g_inv >> 16), last = min(p.T, w.x.n_tok - tok0) - 1;
                 idle = (warp & 3) * 32 >= (last + 1) * p.G;                         // no row of this piece is this warp's
                 hollow = tl > last;                                                 // nor is any this thread's: its weights are zeros
                 n = side ? w.n1 : w.n0;
@@ -661,6 +661,22 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                 }
                 const bool masked = key0 + kTile > limit_min;               // uniform over the side
                 const int seen = limit - key0;
+                if (masked) {
+                    // in TMEM and in a loop: unrolled over the registers below it is twice the code of all the rest, which
+                    // short pieces wait for (instruction cache misses)
+                    const int first = max(0, (int)__reduce_min_sync(0xffffffffu, seen)) >> 5;
+#pragma unroll 1
+                    for (int ch = first; ch < 4; ++ch) {
+                        uint32_t v[32];
+                        tmem_ld32(t_s + 32u * ch, v);
+                        tmem_wait_ld();
+                        const int left = seen - 32 * ch;
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) if (c >= left) v[c] = 0xff800000u;       // -inf
+                        tmem_st32(t_s + 32u * ch, v);
+                    }
+                    tmem_wait_st();
+                }
                 float sv[kTile];
                 float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
                 tmem_ld32(t_s, reinterpret_cast<uint32_t*>(sv));
@@ -671,10 +687,6 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
                     if (half) tmem_wait_ld();
-                    if (masked) {
-#pragma unroll
-                        for (int c = 64 * half; c < 64 * half + 64; ++c) if (c >= seen) sv[c] = -INFINITY;
-                    }
 #pragma unroll
                     for (int c = 32 * half; c < 32 * half + 32; ++c) mx4[c & 3] = max3(mx4[c & 3], sv[2 * c], sv[2 * c + 1]);
                 }
@@ -735,7 +747,7 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
             }
             const ChunkPiece& x = w.x;
             const int L = (warp & 3) * 32 + lane;           // row of the tile = TMEM lane
-            const int tl = L / p.G, gl = L - tl * p.G;      // token of the tile and head of the group
+            const int tl = (int)(L * p.g_inv >> 16), gl = L - tl * p.G;      // token of the tile and head of the group
             const int tok0 = w.wide ? side * p.T : 0, n_tok = min(p.T, x.n_tok - tok0);
             const bool valid = tl < n_tok;                  // (L >= T G has tl >= T)
             const bool joined = !w.wide && w.n1 > 0;        // both sides hold a part of the same rows
@@ -910,7 +922,7 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                     for (int i = 0; i < 4; ++i) {
                         const int u = u0 + i * kSideThreads;
                         if (u >= units) continue;
-                        const int row = u / (kHeadDim / 8), col = (u % (kHeadDim / 8)) * 8, t = row / p.G;
+                        const int row = u / (kHeadDim / 8), col = (u % (kHeadDim / 8)) * 8, t = (int)(row * p.g_inv >> 16);
                         const float scale = l[i] > 0.f ? 1.f / l[i] : (l[i] == 0.f ? 0.f : l[i]);
 #pragma unroll
                         for (int c = 0; c < 8; ++c) acc[i][c] *= scale;
