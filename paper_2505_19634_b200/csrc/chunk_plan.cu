@@ -11,18 +11,21 @@
 // 1 k to 8 k keys.  Everything here is a function of the lengths alone: the cuts, and with them the results, do
 // not depend on timing.
 //
-// The kernel is latency: its code runs once, cold.  Sorting the entries and trying 32 bounds took 15 us where
+// The kernel is latency: its code runs once, cold, and every warp more is issue time for the others, so that it has no
+// more threads than the call may need (the attention of 24 prompts, some 360 entries: 56.1 us with 1024 threads, 55.0 with 192).  Sorting the entries and trying 32 bounds took 15 us where
 // this takes 7, for no better balance.
 #include "chunk_attn.cuh"
 #include "launch.cuh"
+
+#include <algorithm>
 
 namespace tts {
 
 namespace {
 
-constexpr int kThreads = 1024;
+constexpr int kMaxThreads = 1024;
 constexpr int kPer = 2;                               // entries per thread
-constexpr int kMaxCut = kThreads * kPer;              // calls with more entries do not cut them: 14 and more per CTA even
+constexpr int kMaxCut = kMaxThreads * kPer;             // calls with more entries do not cut them: 14 and more per CTA even
                                                       // themselves out
 
 struct Scan { unsigned long long warp[33]; };
@@ -36,7 +39,7 @@ __device__ unsigned long long block_scan(unsigned long long v, Scan& sc, unsigne
     if (lane == 31) sc.warp[warp] = s;
     __syncthreads();
     if (warp == 0) {
-        const unsigned long long w = sc.warp[lane];
+        const unsigned long long w = lane < (int)(blockDim.x >> 5) ? sc.warp[lane] : 0;
         unsigned long long t = w;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) { const unsigned long long n = __shfl_up_sync(0xffffffffu, t, o); if (lane >= o) t += n; }
@@ -69,7 +72,7 @@ __device__ void write_pieces(const ChunkParams& p, const ChunkEntry& r, int e, i
     }
 }
 
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kMaxThreads)
 chunk_plan_kernel(const ChunkParams p) {
     grid_dependency_wait();
     grid_launch_dependents();
@@ -102,7 +105,7 @@ chunk_plan_kernel(const ChunkParams p) {
     __syncthreads();
     if (n > kMaxCut) {
 #pragma unroll 1
-        for (int e = tid; e < n; e += kThreads) write_pieces(p, entry_of(p, br, e), e, 1, e, 0);
+        for (int e = tid; e < n; e += blockDim.x) write_pieces(p, entry_of(p, br, e), e, 1, e, 0);
         if (tid == 0) { p.head->pieces = n; p.head->part_rows = 0; }
         return;
     }
@@ -176,7 +179,10 @@ chunk_plan_kernel(const ChunkParams p) {
 }  // namespace
 
 cudaError_t launch_chunk_plan(const ChunkParams& p, cudaStream_t st) {
-    return launch_dependent(chunk_plan_kernel, 1, kThreads, 0, st, p);
+    // a thread for each branch and one for every two entries that there may be
+    const long entries = (long)p.total_rows / (2 * p.T) + p.n_branches;
+    const long threads = entries > kMaxCut ? kMaxThreads : std::max((long)p.n_branches, (entries + kPer - 1) / kPer);
+    return launch_dependent(chunk_plan_kernel, 1, (int)((threads + 31) / 32 * 32), 0, st, p);
 }
 
 }  // namespace tts
