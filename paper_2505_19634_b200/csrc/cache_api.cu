@@ -19,9 +19,11 @@ int finish(Ctx* c, cudaError_t e, int launches) {
     return TTS_OK;
 }
 
+constexpr int kMaxBlocks = 1 << 26;                    // 2^30 tokens per branch: token numbers and their sums fit 32 bits
+
 bool branches_ok(const Ctx* c, const int32_t* block_table, int prefix_len, int n_branches) {
     const tts_config& f = c->cfg;
-    return block_table && aligned4(block_table) && n_branches >= 1 && n_branches <= f.max_branches && prefix_len >= 0 &&
+    return block_table && aligned4(block_table) && f.max_blocks_per_branch <= kMaxBlocks && n_branches >= 1 && n_branches <= f.max_branches && prefix_len >= 0 &&
            prefix_len % f.page_size == 0 && prefix_len / f.page_size <= f.max_blocks_per_branch;
 }
 
@@ -127,7 +129,9 @@ int tts_chunk_attn(tts_ctx* ctx, const void* q, int64_t q_row_stride, const void
     if (total_rows == 0) return TTS_OK;
     const size_t q_bytes = ((size_t)(total_rows - 1) * q_row_stride + (size_t)f.n_q_heads * kHeadDim) * 2;
     const size_t out_bytes = (size_t)total_rows * f.n_q_heads * kHeadDim * (f.out_dtype == TTS_OUT_FP32 ? 4 : 2);
-    if (overlap(q, q_bytes, out, out_bytes)) return TTS_ERR_INVALID;
+    const size_t lse_bytes = lse ? (size_t)total_rows * f.n_q_heads * 4 : 0;
+    if (overlap(q, q_bytes, out, out_bytes) || (lse && (overlap(lse, lse_bytes, out, out_bytes) || overlap(lse, lse_bytes, q, q_bytes))))
+        return TTS_ERR_INVALID;
     const OnDevice on(c->device);
     if (on.error() != cudaSuccess) return finish(c, on.error(), 0);
     ChunkParams p;
@@ -178,6 +182,8 @@ int tts_kv_append_rope(tts_ctx* ctx, const tts_rope* rope, const void* q, int64_
     // q_out may be q itself, when q is dense; any other overlap would be read after it is written
     const size_t out_bytes = (size_t)total_rows * q_row * 2, q_bytes = ((size_t)(total_rows - 1) * q_row_stride + q_row) * 2;
     if (overlap(q, q_bytes, q_out, out_bytes) && !(q == q_out && q_row_stride == q_row)) return TTS_ERR_INVALID;
+    const size_t kv_bytes = ((size_t)(total_rows - 1) * kv_row_stride + kv_row) * 2;
+    if (overlap(k, kv_bytes, q_out, out_bytes) || overlap(v, kv_bytes, q_out, out_bytes)) return TTS_ERR_INVALID;
     const OnDevice on(c->device);
     if (on.error() != cudaSuccess) return finish(c, on.error(), 0);
     RopeParams p;

@@ -338,3 +338,37 @@ def test_two_graphs_of_one_context():
         check(b, *outs[1])
     assert ctx.tts_last_status() == 0
     ctx.close()
+
+
+def test_lse_over_queries_or_output_is_refused():
+    c = Cache(8, 2, chunk=[3, 4], lens=[30, 40], seed=1)
+    ctx = context(c)
+    buffer = torch.full((c.total_rows * 8 * 128 * 2 + 64,), 3.0, dtype=torch.bfloat16, device="cuda")
+    out = buffer[:c.total_rows * 8 * 128]
+    last = out.data_ptr() + out.numel() * 2
+    for lse in (out.data_ptr(), last - 4, c.q.data_ptr() + 64, out.data_ptr() - c.total_rows * 8 * 4 + 4):
+        with pytest.raises(tts.TtsError) as e:
+            call(ctx, c, out, lse)
+        assert e.value.status == -1
+    torch.cuda.synchronize()
+    assert (buffer == 3).all()
+    call(ctx, c, out, last)                                      # next to it is fine
+    torch.cuda.synchronize()
+    assert ctx.tts_last_status() == 0 and not (out == 3).all()
+    ctx.close()
+
+
+def test_tables_that_32_bit_token_numbers_do_not_reach_are_refused():
+    """2^26 blocks of 16 tokens are 2^30 tokens; nothing is read before the refusal."""
+    c = Cache(8, 2, chunk=[3, 4], lens=[30, 40], seed=1)
+    out, refs = torch.zeros_like(c.q), torch.zeros(c.num_pages + 16, dtype=torch.int32, device="cuda")
+    ctx = tts.TtsContext(8, 2, 2, 1, (1 << 26) + 1, c.num_pages)
+    ctx.tts_chunk_reserve(7)
+    with pytest.raises(tts.TtsError) as e:
+        call(ctx, c, out)
+    assert e.value.status == -1
+    for grow in (lambda: ctx.tts_kv_grow(c.table, 0, c.branch_lens, c.row_start, 2, refs), lambda: ctx.tts_kv_free(c.table, c.branch_lens, c.row_start, 2, refs)):
+        with pytest.raises(tts.TtsError) as e:
+            grow()
+        assert e.value.status == -1
+    ctx.close()

@@ -208,3 +208,17 @@ def test_bad_places_write_no_key_and_are_reported():
         assert ctx.tts_last_status() == -4
         check(c, ([0] * 64, freq, False), c.k, c.v, k, v, pos, q_out, k_new, v_new, skip=(1,))
         ctx.close()
+
+
+def test_rotated_queries_over_the_new_keys_or_values_are_refused():
+    c = Cache(8, 2, chunk=[3, 4], lens=[30, 40], seed=1)
+    k_new, v_new, pos = inputs(c, 1)
+    ctx = tts.TtsContext(8, 2, 2, 1, c.width, c.num_pages)
+    rope, before = tts.TtsRope([0] * 64, inv_freq(64)), (k_new.clone(), v_new.clone())
+    for out in (k_new.data_ptr(), v_new.data_ptr() + v_new.numel() * 2 - 16, k_new.data_ptr() - 7 * 1024 * 2 + 16):
+        with pytest.raises(tts.TtsError) as e:
+            ctx.tts_kv_append_rope(rope, c.q, 1024, k_new, v_new, 256, pos, c.k, c.v, c.table, 0, c.branch_lens, c.row_start, 2, 7, out)
+        assert e.value.status == -1
+    torch.cuda.synchronize()
+    assert torch.equal(k_new, before[0]) and torch.equal(v_new, before[1])
+    ctx.close()
