@@ -151,7 +151,7 @@ int tts_chunk_attn(tts_ctx* ctx, const void* q, int64_t q_row_stride, const void
     p.grid = f.max_ctas > 0 && f.max_ctas < c->n_sms ? f.max_ctas : c->n_sms;
     p.g_inv = 65536u / (unsigned)p.G + 1u;
     p.heads_per_cta = (float)p.Hkv / p.grid; p.ctas_per_head = (float)p.grid / p.Hkv;
-    p.out_dtype = f.out_dtype;
+    p.out_dtype = f.out_dtype; p.out_32 = (reinterpret_cast<uintptr_t>(out) & 31u) == 0;
     p.scale_log2 = (f.softmax_scale > 0.f ? f.softmax_scale : 1.0f / sqrtf((float)f.head_dim)) * 1.4426950408889634f;
     cudaError_t e;
     if (!small) {

@@ -309,28 +309,6 @@ __device__ __forceinline__ void st_global_32(void* to, const float* v) {
     asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
                  ::"l"(to), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]) : "memory");
 }
-// 16 TMEM lanes x 32 columns as fragments: registers 4 g .. 4 g + 3 are columns 8 g + 2 (lane % 4), + 1 of rows lane / 4
-// and lane / 4 + 8
-__device__ __forceinline__ void tmem_ld_frag(uint32_t taddr, uint32_t (&r)[16]) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
-          "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-        : "r"(taddr) : "memory");
-}
-// Four lanes' 4 x 4 words, transposed: e[j] becomes lane j's e[this lane of the four]
-__device__ __forceinline__ void transpose4(uint32_t (&e)[4], int lane) {
-#pragma unroll
-    for (int m = 1; m <= 2; m <<= 1)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (i & m) continue;
-            const bool up = lane & m;
-            const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? e[i] : e[i | m], m);
-            if (up) e[i] = got; else e[i | m] = got;
-        }
-}
-
 __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&h);
@@ -789,79 +767,39 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
             const size_t part0 = (size_t)w.kvh * w.part_rows + x.part_row + (side == 1 ? (size_t)x.parts * p.T * p.G : 0);
             const size_t part_at = part0 + (size_t)x.part * rows + L;
             const size_t row_head = (size_t)(x.row0 + tok0 + tl) * p.Hq + w.kvh * p.G + gl;
-            // side 1's O, which a joined piece adds.  It is read, if only to be dropped, whether the piece is joined or not: registers
-            // that a branch may leave unwritten would be held through the loop over the tiles.
-            const uint32_t t_o1 = tmem + 384u + lane_base;
-            if (n > 0 && direct && p.out_dtype == TTS_OUT_BF16) {
-                // The usual way out.  One thread per row would send every 16 bytes to a line of its own; read from TMEM as
-                // fragments (two neighbouring columns of rows lane / 4 and lane / 4 + 8) and transposed within four lanes,
-                // a store covers 64 bytes of eight rows.
-                const int rel = valid ? (tok0 + tl) * p.Hq + gl : -1;
-                __nv_bfloat16* to = static_cast<__nv_bfloat16*>(p.out) + ((size_t)x.row0 * p.Hq + w.kvh * p.G) * kHeadDim + (lane & 3) * 8;
-                int at[4];                                  // this lane's rows: lane / 4 + 8 i
-                float y0[4], y1[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    at[i] = __shfl_sync(0xffffffffu, rel, (lane >> 2) + 8 * i);
-                    y0[i] = __shfl_sync(0xffffffffu, f0, (lane >> 2) + 8 * i);
-                    y1[i] = __shfl_sync(0xffffffffu, f1, (lane >> 2) + 8 * i);
-                }
-                const bool both = (warp & 3) * 32 + 16 < rows;          // rows 16-31 of this warp's as well as 0-15
-                uint32_t a[2][16], b[2][16];
-                auto load = [&](int i, int col) {
-                    tmem_ld_frag(t_o + ((uint32_t)(16 * i) << 16) + col, a[i]);
-                    tmem_ld_frag(t_o1 + ((uint32_t)(16 * i) << 16) + col, b[i]);
-                };
-                auto leave = [&](int i, int col) {
-                    uint32_t e[2][4];
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)                         // rows lane / 4 and lane / 4 + 8 of the 16
-#pragma unroll
-                        for (int g = 0; g < 4; ++g) {
-                            float v[2];
-#pragma unroll
-                            for (int c = 0; c < 2; ++c) {
-                                v[c] = __uint_as_float(a[i][4 * g + 2 * h + c]) * y0[2 * i + h];
-                                if (joined) v[c] = fmaf(__uint_as_float(b[i][4 * g + 2 * h + c]), y1[2 * i + h], v[c]);
-                            }
-                            e[h][g] = bf16_pair(v[0], v[1]);
-                        }
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        transpose4(e[h], lane);
-                        if (at[2 * i + h] >= 0) *reinterpret_cast<uint4*>(to + (size_t)at[2 * i + h] * kHeadDim + col) = make_uint4(e[h][0], e[h][1], e[h][2], e[h][3]);
-                    }
-                };
-                if (!idle) {
-                    load(0, 0);
-#pragma unroll 1
-                    for (int col = 0; col < kHeadDim; col += 32) {
-                        tmem_wait_ld();
-                        load(1, col);                                   // (whether there are such rows or not)
-                        leave(0, col);
-                        tmem_wait_ld();
-                        load(0, (col + 32) & (kHeadDim - 1));           // (after the last one, the first again)
-                        if (both) leave(1, col);
-                    }
-                    tmem_wait_ld();
-                }
-            } else
+            const uint32_t t_o1 = tmem + 384u + lane_base;  // side 1's O, which a joined piece adds
+            // A thread writes its own row, whole sectors of 32 bytes at a time where the array's alignment allows it.  (Rows
+            // gathered from neighbouring threads by shuffles make fuller lines, but take about 560 instructions per warp where this
+            // takes about 240, and short pieces wait for instructions: 24 prompts 55.0 us, 54.4 this way.)
 #pragma unroll 1
             for (int ch = 0; ch < 4 && !idle; ++ch) {
-                uint32_t ov[32], oj[32];
-                tmem_ld32(t_o + 32u * ch, ov);
-                tmem_ld32(t_o1 + 32u * ch, oj);
-                tmem_wait_ld();
                 float o[32];
+                tmem_ld32(t_o + 32u * ch, reinterpret_cast<uint32_t*>(o));
+                tmem_wait_ld();
 #pragma unroll
-                for (int c = 0; c < 32; ++c) {
-                    o[c] = n > 0 && f0 != 0.f ? __uint_as_float(ov[c]) * f0 : 0.f;
-                    if (joined && f1 != 0.f) o[c] = fmaf(__uint_as_float(oj[c]), f1, o[c]);
+                for (int c = 0; c < 32; ++c) o[c] = n > 0 && f0 != 0.f ? o[c] * f0 : 0.f;
+                if (joined) {
+                    float oj[32];
+                    tmem_ld32(t_o1 + 32u * ch, reinterpret_cast<uint32_t*>(oj));
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) o[c] = f1 != 0.f ? fmaf(oj[c], f1, o[c]) : o[c];
                 }
                 if (!valid) continue;
                 if (!direct) {
 #pragma unroll
                     for (int c = 0; c < 4; ++c) st_global_32(p.part_o + part_at * kHeadDim + 32 * ch + 8 * c, o + 8 * c);
+                } else if (p.out_dtype == TTS_OUT_BF16) {
+                    float w2[16];
+#pragma unroll
+                    for (int c = 0; c < 16; ++c) w2[c] = __uint_as_float(bf16_pair(o[2 * c], o[2 * c + 1]));
+                    __nv_bfloat16* to = static_cast<__nv_bfloat16*>(p.out) + row_head * kHeadDim + 32 * ch;
+                    if (p.out_32) {
+                        st_global_32(to, w2); st_global_32(to + 16, w2 + 8);
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) reinterpret_cast<float4*>(to)[c] = make_float4(w2[4 * c], w2[4 * c + 1], w2[4 * c + 2], w2[4 * c + 3]);
+                    }
                 } else {
 #pragma unroll
                     for (int c = 0; c < 4; ++c) store_out8(p, row_head, 32 * ch + 8 * c, o + 8 * c);

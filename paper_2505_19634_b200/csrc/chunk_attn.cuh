@@ -56,6 +56,7 @@ struct ChunkParams {
     float heads_per_cta, ctas_per_head;   // Hkv / grid, grid / Hkv
     unsigned g_inv;                // x * g_inv >> 16 is x / G for x < 128: the error, x / 65536 at most, is below 1 / G
     int out_dtype;
+    int out_32;                    // out is 32-byte aligned
     float scale_log2;
 };
 

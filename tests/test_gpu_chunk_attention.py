@@ -372,3 +372,20 @@ def test_tables_that_32_bit_token_numbers_do_not_reach_are_refused():
             grow()
         assert e.value.status == -1
     ctx.close()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_output_aligned_to_16_bytes_only(dtype):
+    """The same values to the bit as in an array that starts on a larger boundary, and nothing beside it."""
+    c = Cache(8, 2, chunk=[1, 70, 9], lens=[300, 400, 20], seed=5)
+    ctx = context(c, out_dtype=tts.OUT_FP32 if dtype == torch.float32 else tts.OUT_BF16)
+    pad = 16 // dtype.itemsize
+    want, buffer = torch.zeros(c.total_rows, 8, 128, dtype=dtype, device="cuda"), torch.full((c.total_rows * 8 * 128 + 2 * pad,), 3.0, dtype=dtype, device="cuda")
+    assert buffer.data_ptr() % 32 == 0
+    call(ctx, c, want)
+    call(ctx, c, buffer[pad:])
+    torch.cuda.synchronize()
+    assert ctx.tts_last_status() == 0 and (want != 0).any()
+    assert torch.equal(buffer[pad:-pad].view_as(want), want)
+    assert (buffer[:pad] == 3).all() and (buffer[-pad:] == 3).all()
+    ctx.close()
