@@ -28,10 +28,12 @@
 //
 // Measured (B200 whose copy peak is 6538 GB/s and whose bf16 GEMMs reach 1663 TFLOP/s in a burst, 1394 sustained):
 // 8192 tokens of 40 / 8 heads over 24576 keys 4.4 ms = 1080 TFLOP/s, 0.77 of the sustained rate; 64 single tokens
-// over 1 k to 8 k keys 255 us = 5.5 TB/s, 0.85.  Both run into the card's power limit (1.5 GHz instead of 1.85): a
+// over 1 k to 8 k keys 246 us = 5.7 TB/s, 0.88.  Both run into the card's power limit (1.5 GHz instead of 1.85): a
 // tile of both sides takes 3300 clocks, of which the tensor pipe works 2050 and a softmax warp's chain (scores,
 // maximum, exponentials at 8 clocks each, stores) fills about 2000, and changes that saved clocks alone
-// (a second MMA warp, two threads per row, part of the exponentials as polynomials) did not save time.
+// (a second MMA warp, two threads per row, part of the exponentials as polynomials) did not save time.  Short pieces
+// (24 prompts of up to 800 tokens: 54 us) wait for instructions as much as for anything else: two sides in different
+// parts of the code miss the instruction cache at 22 % of its lookups, so code that is not the loop's is kept small.
 //
 // Page ids outside the pool and entries beyond the table row read as zeros (and are reported); tokens past the
 // end of a branch never contribute: their scores are replaced before the maximum and their V rows are zeroed in
