@@ -383,6 +383,12 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
             // =========================== takes pieces, loads Q ===========================
             SmallTable& small = *reinterpret_cast<SmallTable*>(smem + kOffSmall);
             if (p.small) small_plan(p, small, lane);
+            // the first piece of a schedule made elsewhere, asked for together with their number
+            int4 ahead[3];
+            if (!p.small) {
+                const int4* src = reinterpret_cast<const int4*>(p.pieces + min((int)blockIdx.x / p.Hkv, p.max_pieces - 1));
+                ahead[0] = src[0]; ahead[1] = src[1]; ahead[2] = src[2];
+            }
             const int total = (p.small ? small.pieces : p.head->pieces) * p.Hkv, part_rows = p.small ? small.part_rows : p.head->part_rows;
             int index = blockIdx.x, used[2] = {0, 0};
             bool alive = true;
@@ -394,9 +400,12 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                     const int i = index / p.Hkv;                            // all KV heads of a piece follow one another
                     w.kvh = index - i * p.Hkv;
                     if (!p.small) {
-                        const int4* src = reinterpret_cast<const int4*>(p.pieces + i);
                         int4* dst = reinterpret_cast<int4*>(&w.x);
-                        dst[0] = src[0]; dst[1] = src[1]; dst[2] = src[2];
+                        if (it > 0) {
+                            const int4* src = reinterpret_cast<const int4*>(p.pieces + i);
+                            ahead[0] = src[0]; ahead[1] = src[1]; ahead[2] = src[2];
+                        }
+                        dst[0] = ahead[0]; dst[1] = ahead[1]; dst[2] = ahead[2];
                     } else {
                         w.x = small_piece(p, small, i, lane);
                     }
