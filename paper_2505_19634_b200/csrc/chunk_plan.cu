@@ -28,27 +28,22 @@ constexpr int kPer = 2;                               // entries per thread
 constexpr int kMaxCut = kMaxThreads * kPer;             // calls with more entries do not cut them: 14 and more per CTA even
                                                       // themselves out
 
-struct Scan { unsigned long long warp[33]; };
+struct Scan { unsigned long long warp[32]; };
 
-__device__ unsigned long long block_scan(unsigned long long v, Scan& sc, unsigned long long* total) {       // exclusive, over the block
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    unsigned long long s = v;
+__device__ unsigned long long warp_scan(unsigned long long v, int lane) {              // inclusive
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) { const unsigned long long n = __shfl_up_sync(0xffffffffu, s, o); if (lane >= o) s += n; }
-    __syncthreads();
+    for (int o = 1; o < 32; o <<= 1) { const unsigned long long n = __shfl_up_sync(0xffffffffu, v, o); if (lane >= o) v += n; }
+    return v;
+}
+// Exclusive, over the block.  Every warp adds up the warps' sums for itself: one barrier.  A scan has an `sc` of its own.
+__device__ unsigned long long block_scan(unsigned long long v, Scan& sc, unsigned long long* total) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const unsigned long long s = warp_scan(v, lane);
     if (lane == 31) sc.warp[warp] = s;
     __syncthreads();
-    if (warp == 0) {
-        const unsigned long long w = lane < (int)(blockDim.x >> 5) ? sc.warp[lane] : 0;
-        unsigned long long t = w;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) { const unsigned long long n = __shfl_up_sync(0xffffffffu, t, o); if (lane >= o) t += n; }
-        sc.warp[lane] = t - w;
-        if (lane == 31) sc.warp[32] = t;
-    }
-    __syncthreads();
-    *total = sc.warp[32];
-    return sc.warp[warp] + s - v;
+    const unsigned long long w = lane < (int)(blockDim.x >> 5) ? sc.warp[lane] : 0, t = warp_scan(w, lane);
+    *total = __shfl_sync(0xffffffffu, t, 31);
+    return __shfl_sync(0xffffffffu, t - w, warp) + s - v;
 }
 
 struct Branches {
@@ -77,7 +72,7 @@ chunk_plan_kernel(const ChunkParams p) {
     grid_dependency_wait();
     grid_launch_dependents();
     __shared__ Branches br;
-    __shared__ Scan sc;
+    __shared__ Scan sc[4];
     __shared__ unsigned short order[kMaxCut];
     __shared__ int largest;
     const int tid = threadIdx.x;
@@ -95,7 +90,7 @@ chunk_plan_kernel(const ChunkParams p) {
     }
     bad = __syncthreads_or(bad);                       // then nothing is computed
     unsigned long long sum;
-    const int at_branch = (int)block_scan(bad ? 0 : n_mine, sc, &sum);
+    const int at_branch = (int)block_scan(bad ? 0 : n_mine, sc[0], &sum);
     const int n = (int)sum;
     if (tid < p.n_branches) br.first[tid] = at_branch;
     if (tid == 0) {
@@ -127,7 +122,7 @@ chunk_plan_kernel(const ChunkParams p) {
         cls[i] = 3 - min(3, (int)(4.f * mine[i] / (largest + 1)));
         if (mine[i] >= 0) in_class += 1ull << (16 * cls[i]);
     }
-    unsigned long long at_class = block_scan(in_class, sc, &sum);
+    unsigned long long at_class = block_scan(in_class, sc[1], &sum);
     at_class += (sum << 16) + (sum << 32) + (sum << 48);         // each class begins where those before it end
 #pragma unroll
     for (int i = 0; i < kPer; ++i)
@@ -146,7 +141,7 @@ chunk_plan_kernel(const ChunkParams p) {
             r[i] = entry_of(p, br, e[i]);
             cost[i] = chunk_cost(r[i], p.T);
         }
-    const unsigned long long ahead = block_scan((unsigned)cost[0] + (unsigned)cost[1], sc, &sum);
+    const unsigned long long ahead = block_scan((unsigned)cost[0] + (unsigned)cost[1], sc[2], &sum);
     const float total = (float)sum, left[kPer] = {(float)(sum - ahead), (float)(sum - ahead - cost[0])};
     ChunkBound bound = chunk_bound(p, total, n, (float)largest);
     for (;;) {
@@ -161,11 +156,12 @@ chunk_plan_kernel(const ChunkParams p) {
                 if (i == 0) rows0 = rows;
                 mine += (unsigned)k[i] + ((unsigned long long)rows << 20);
             }
-        const unsigned long long at = block_scan(mine, sc, &sum);
+        const unsigned long long at = block_scan(mine, sc[3], &sum);
         const int pieces = (int)(sum & 0xfffffu);
         const long rows = (long)(sum >> 20);
         if (bound.narrow != kChunkNoBound && (pieces > p.max_pieces || rows * p.Hkv > p.part_rows)) {
             bound = chunk_coarser(bound);
+            __syncthreads();                           // everyone has read the sums
             continue;
         }
         const int at0 = (int)(at & 0xfffffu), row0 = (int)(at >> 20);
