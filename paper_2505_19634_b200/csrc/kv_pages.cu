@@ -23,32 +23,24 @@ constexpr int kTileBytes = kPage * kHeadDim * 2;       // one page of one KV hea
 constexpr int kTileChunks = kTileBytes / 16 / 32;      // 16-byte chunks of a tile per lane
 constexpr int kCopyThreads = 256;
 
-// Exclusive scan over the block; *total gets the sum.  `warp_sums`: 33 ints.
-__device__ int block_scan(int v, int* warp_sums, int* total) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int s = v;
+__device__ __forceinline__ int warp_scan(int v, int lane) {                            // inclusive
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int n = __shfl_up_sync(0xffffffffu, s, o);
-        if (lane >= o) s += n;
+        const int n = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += n;
     }
+    return v;
+}
+// Exclusive scan over the block; *total gets the sum.  `warp_sums`: 32 ints, which every warp adds up for itself.
+__device__ int block_scan(int v, int* warp_sums, int* total) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int s = warp_scan(v, lane);
     __syncthreads();                                    // the previous scan's sums have been read
     if (lane == 31) warp_sums[warp] = s;
     __syncthreads();
-    if (warp == 0) {
-        const int w = lane < (int)(blockDim.x >> 5) ? warp_sums[lane] : 0;
-        int t = w;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int n = __shfl_up_sync(0xffffffffu, t, o);
-            if (lane >= o) t += n;
-        }
-        warp_sums[lane] = t - w;
-        if (lane == 31) warp_sums[32] = t;
-    }
-    __syncthreads();
-    *total = warp_sums[32];
-    return warp_sums[warp] + s - v;
+    const int w = lane < (int)(blockDim.x >> 5) ? warp_sums[lane] : 0, t = warp_scan(w, lane);
+    *total = __shfl_sync(0xffffffffu, t, 31);
+    return __shfl_sync(0xffffffffu, t - w, warp) + s - v;
 }
 
 // The counts refs[first .. first + kPerThread) of a thread; pages past the pool count as `pad`.
@@ -137,7 +129,7 @@ fork_plan_kernel(const int32_t* __restrict__ table, int max_blocks, int prefix_l
         return;
     }
     __shared__ int first[kMaxBranches];                 // lowest child of each parent
-    __shared__ int sums[33];
+    __shared__ int sums[32];
     const int c = threadIdx.x;
     int free_refs[kPerThread];
     load_refs(refs, num_pages, (long)c * kPerThread, 1, free_refs);
@@ -224,7 +216,7 @@ grow_kernel(int32_t* table, int max_blocks, int prefix_len, int32_t* lens, const
             int num_pages, PageWork wk, int32_t* status) {
     grid_dependency_wait();
     grid_launch_dependents();
-    __shared__ int sums[33];
+    __shared__ int sums[32];
     __shared__ int bad;
     const int b = threadIdx.x;
     if (b == 0) bad = 0;
@@ -278,7 +270,7 @@ __global__ void __launch_bounds__(kMaxScanThreads)
 compact_plan_kernel(const int32_t* refs, int32_t* new_refs, int num_pages, int32_t* page_map, int32_t* n_used, PageWork wk) {
     grid_dependency_wait();
     grid_launch_dependents();
-    __shared__ int sums[33];
+    __shared__ int sums[32];
     int mine = 0, used, r[kPerThread];
     for (long base = (long)threadIdx.x * kPerThread; base < num_pages; base += (int)blockDim.x * kPerThread) {
         load_refs(refs, num_pages, base, 0, r);
