@@ -32,7 +32,7 @@
 // tile of both sides takes 3300 clocks, of which the tensor pipe works 2050 and a softmax warp's chain (scores,
 // maximum, exponentials at 8 clocks each, stores) fills about 2000, and changes that saved clocks alone
 // (a second MMA warp, two threads per row, part of the exponentials as polynomials) did not save time.  Short pieces
-// (24 prompts of up to 800 tokens: 54 us) wait for instructions as much as for anything else: two sides in different
+// (24 prompts of up to 800 tokens: 53 us) wait for instructions as much as for anything else: two sides in different
 // parts of the code miss the instruction cache at 22 % of its lookups, so code that is not the loop's is kept small.
 //
 // Page ids outside the pool and entries beyond the table row read as zeros (and are reported); tokens past the
