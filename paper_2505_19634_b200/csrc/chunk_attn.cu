@@ -784,17 +784,14 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
             // takes about 240, and short pieces wait for instructions: 24 prompts 55.0 us, 54.4 this way.)
 #pragma unroll 1
             for (int ch = 0; ch < 4 && !idle; ++ch) {
-                float o[32];
+                float o[32], oj[32];                        // (both are read, if only to be dropped: a branch here cost more)
                 tmem_ld32(t_o + 32u * ch, reinterpret_cast<uint32_t*>(o));
+                tmem_ld32(t_o1 + 32u * ch, reinterpret_cast<uint32_t*>(oj));
                 tmem_wait_ld();
 #pragma unroll
-                for (int c = 0; c < 32; ++c) o[c] = n > 0 && f0 != 0.f ? o[c] * f0 : 0.f;
-                if (joined) {
-                    float oj[32];
-                    tmem_ld32(t_o1 + 32u * ch, reinterpret_cast<uint32_t*>(oj));
-                    tmem_wait_ld();
-#pragma unroll
-                    for (int c = 0; c < 32; ++c) o[c] = f1 != 0.f ? fmaf(oj[c], f1, o[c]) : o[c];
+                for (int c = 0; c < 32; ++c) {
+                    o[c] = n > 0 && f0 != 0.f ? o[c] * f0 : 0.f;
+                    o[c] = joined && f1 != 0.f ? fmaf(oj[c], f1, o[c]) : o[c];
                 }
                 if (!valid) continue;
                 if (!direct) {
