@@ -23,22 +23,24 @@ constexpr int kTileBytes = kPage * kHeadDim * 2;       // one page of one KV hea
 constexpr int kTileChunks = kTileBytes / 16 / 32;      // 16-byte chunks of a tile per lane
 constexpr int kCopyThreads = 256;
 
-__device__ __forceinline__ int warp_scan(int v, int lane) {                            // inclusive
+template <typename T>
+__device__ __forceinline__ T warp_scan(T v, int lane) {                                // inclusive
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int n = __shfl_up_sync(0xffffffffu, v, o);
+        const T n = __shfl_up_sync(0xffffffffu, v, o);
         if (lane >= o) v += n;
     }
     return v;
 }
-// Exclusive scan over the block; *total gets the sum.  `warp_sums`: 32 ints, which every warp adds up for itself.
-__device__ int block_scan(int v, int* warp_sums, int* total) {
+// Exclusive scan over the block; *total gets the sum.  `warp_sums`: 32 values, which every warp adds up for itself.
+template <typename T>
+__device__ T block_scan(T v, T* warp_sums, T* total) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int s = warp_scan(v, lane);
+    const T s = warp_scan(v, lane);
     __syncthreads();                                    // the previous scan's sums have been read
     if (lane == 31) warp_sums[warp] = s;
     __syncthreads();
-    const int w = lane < (int)(blockDim.x >> 5) ? warp_sums[lane] : 0, t = warp_scan(w, lane);
+    const T w = lane < (int)(blockDim.x >> 5) ? warp_sums[lane] : 0, t = warp_scan(w, lane);
     *total = __shfl_sync(0xffffffffu, t, 31);
     return __shfl_sync(0xffffffffu, t - w, warp) + s - v;
 }
@@ -154,7 +156,7 @@ fork_plan_kernel(const int32_t* __restrict__ table, int max_blocks, int prefix_l
         if (!page_ok(src, num_pages)) { atomicMin(status, (int)TTS_ERR_DEVICE_BOUNDS); src = -1; }
     }
     int need;
-    const int rank = block_scan(src >= 0, sums, &need);
+    const int rank = block_scan((int)(src >= 0), sums, &need);
     const bool ok = lowest_free(refs, num_pages, need, wk.list_dst, sums, free_refs);
     if (c == 0) {
         wk.head[0] = ok ? need : 0;
@@ -217,6 +219,7 @@ grow_kernel(int32_t* table, int max_blocks, int prefix_len, int32_t* lens, const
     grid_dependency_wait();
     grid_launch_dependents();
     __shared__ int sums[32];
+    __shared__ long long wants[32];
     __shared__ int bad;
     const int b = threadIdx.x;
     if (b == 0) bad = 0;
@@ -231,13 +234,14 @@ grow_kernel(int32_t* table, int max_blocks, int prefix_len, int32_t* lens, const
         else if (more > 0) { lo = ceil_div(prefix_len + len, kPage); hi = ceil_div((int)after, kPage); }
     }
     int32_t* row = table + (size_t)b * max_blocks;
-    int want = 0;
-    for (int i = lo; i < hi; ++i) want += row[i] < 0;
+    // A branch that lacks more pages than there are is refused whatever the others ask for, so the count may stop there;
+    // 1024 such counts and rows of 2^26 entries add up to more than 32 bits hold.
+    long long want = 0, need;
+    for (int i = lo; i < hi && want <= num_pages; ++i) want += row[i] < 0;
     __syncthreads();
     if (bad) { if (b == 0) atomicMin(status, (int)TTS_ERR_DEVICE_BOUNDS); return; }
-    int need;
-    int at = block_scan(want, sums, &need);
-    if (!lowest_free(refs, num_pages, need, wk.list_dst, sums, free_refs)) { if (b == 0) atomicMin(status, (int)TTS_ERR_DEVICE_PAGES); return; }
+    long long at = block_scan(want, wants, &need);
+    if (need > num_pages || !lowest_free(refs, num_pages, (int)need, wk.list_dst, sums, free_refs)) { if (b == 0) atomicMin(status, (int)TTS_ERR_DEVICE_PAGES); return; }
     for (int i = lo; i < hi; ++i)
         if (row[i] < 0) {
             const int page = wk.list_dst[at++];

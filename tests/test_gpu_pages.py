@@ -309,3 +309,21 @@ def test_refusals():
     torch.cuda.synchronize()
     assert s.ctx.tts_last_status() == 0
     s.ctx.close()
+
+
+def test_grow_that_lacks_more_pages_than_32_bits_count():
+    """32 rows of the largest table, 2^26 entries each and none with a page, lack 2^31 of them together."""
+    n, width, pages = 32, 1 << 26, 64
+    ctx = tts.TtsContext(2, 2, n, 1, width, pages)
+    table = torch.full((n, width), -1, dtype=torch.int32, device="cuda")
+    lens, refs = i32([0] * n), i32([0] * pages)
+    ctx.tts_kv_grow(table, 0, lens, i32([16 * width] * n), n, refs)
+    torch.cuda.synchronize()
+    assert ctx.tts_last_status() == -7
+    assert not lens.any() and not refs.any() and int(table.max()) == -1
+    ctx.tts_kv_grow(table, 0, lens, i32([16] * n), n, refs)               # one page each
+    torch.cuda.synchronize()
+    assert ctx.tts_last_status() == 0
+    assert table[:, 0].tolist() == list(range(n)) and int(table[:, 1:].max()) == -1 and lens.tolist() == [16] * n
+    assert refs.tolist() == [1] * n + [0] * (pages - n)
+    ctx.close()
