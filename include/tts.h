@@ -425,7 +425,8 @@ TTS_API int tts_chunk_attn(tts_ctx* ctx, const void* q, int64_t q_row_stride, co
  *                        refused
  *   k_pages, v_pages are written, the other arguments as in tts_chunk_attn (total_rows is not bounded by a reserve)
  * A branch shorter than its chunk, a token beyond the table row or a page outside the pool writes no key and value for
- * that row and raises TTS_ERR_DEVICE_BOUNDS; the query is rotated all the same.
+ * that row and raises TTS_ERR_DEVICE_BOUNDS; the query is rotated all the same.  Row starts that decrease or leave
+ * [0, total_rows] write nothing at all and raise TTS_ERR_DEVICE_BOUNDS.
  */
 typedef struct {
     int32_t n_axes, n_pairs, interleaved;

@@ -24,18 +24,17 @@ constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kBatch = 4;                              // head vectors that a group of eight lanes has in flight
 
-// The branch whose rows [row_start[b], row_start[b+1]) hold `row`, or -1: the whole warp looks at 32 starts
-// per step (two steps for up to 1024 branches).
+// Row starts that decrease or leave the rows make a call of which nothing is computed: a row taken for a branch's that
+// starts behind it would have its key written before the branch's first token, or before the pool.
+__device__ __forceinline__ bool bad_rows(const RopeParams& p, int lo, int hi) { return lo < 0 || hi < lo || hi > p.total_rows; }
+
+// The last branch whose rows start at or before `row`, or -1, among more than 32: the whole warp looks at 32
+// starts per step (two steps for up to 1024 branches).
 __device__ __forceinline__ int branch_of_row(const int32_t* row_start, int n, int row, int lane) {
-    int lo = 0;
-    if (n > 32) {                                       // 32 blocks of 32 starts
-        const int at = lane * 32;
-        lo = (__popc(__ballot_sync(0xffffffffu, at < n && row_start[at] <= row)) - 1) * 32;
-        if (lo < 0) return -1;
-    }
+    const int lo = (__popc(__ballot_sync(0xffffffffu, lane * 32 < n && row_start[lane * 32] <= row)) - 1) * 32;      // 32 blocks of 32 starts
+    if (lo < 0) return -1;
     const int at = lo + lane;
-    const int b = lo + __popc(__ballot_sync(0xffffffffu, at < n && row_start[at] <= row)) - 1;
-    return b < lo || row >= row_start[b + 1] ? -1 : b;
+    return lo + __popc(__ballot_sync(0xffffffffu, at < n && row_start[at] <= row)) - 1;
 }
 
 __device__ __forceinline__ void unpack(const uint4& v, float (&x)[8]) {
@@ -71,6 +70,16 @@ append_rope_kernel(const __grid_constant__ RopeParams p) {
     grid_launch_dependents();
     const int lane = threadIdx.x & 31, sub = lane & 7, group = lane >> 3;
     const int vectors = p.Hq + 2 * p.Hkv;
+    // up to 32 branches are checked by each warp with the starts that it looks the row up in, more by the block
+    const bool few = p.n_branches <= 32;
+    if (!few) {
+        bool bad = false;
+        for (int i = threadIdx.x; i < p.n_branches; i += kThreads) bad |= bad_rows(p, p.row_start[i], p.row_start[i + 1]);
+        if (__syncthreads_or(bad)) {
+            if (threadIdx.x == 0) atomicMin(p.status, (int)TTS_ERR_DEVICE_BOUNDS);
+            return;
+        }
+    }
     for (long w = blockIdx.x * (long)kWarps + (threadIdx.x >> 5); w < (long)p.total_rows * p.parts; w += (long)gridDim.x * kWarps) {
         const int row = (int)(w / p.parts), part = (int)(w - (long)row * p.parts);
         const int step = p.parts * 4;
@@ -93,9 +102,21 @@ append_rope_kernel(const __grid_constant__ RopeParams p) {
         };
         if (kMode != 2) load(part * 4);
         // where the row's key and value go
-        const int b = branch_of_row(p.row_start, p.n_branches, row, lane);
-        if (b < 0) continue;                            // a row of no branch: left as it is
-        const int start = p.row_start[b], c = p.row_start[b + 1] - start, L = p.branch_lens[b];
+        int b, start, end;
+        if (few) {
+            const int lo = lane < p.n_branches ? p.row_start[lane] : p.total_rows, hi = lane < p.n_branches ? p.row_start[lane + 1] : p.total_rows;
+            if (__any_sync(0xffffffffu, bad_rows(p, lo, hi))) {
+                if (lane == 0) atomicMin(p.status, (int)TTS_ERR_DEVICE_BOUNDS);
+                return;
+            }
+            b = __popc(__ballot_sync(0xffffffffu, lo <= row)) - 1;
+            start = __shfl_sync(0xffffffffu, lo, b); end = __shfl_sync(0xffffffffu, hi, b);
+        } else {
+            b = branch_of_row(p.row_start, p.n_branches, row, lane);
+            start = b < 0 ? 0 : p.row_start[b]; end = b < 0 ? 0 : p.row_start[b + 1];
+        }
+        if (b < 0 || row >= end) continue;              // a row of no branch: left as it is
+        const int c = end - start, L = p.branch_lens[b];
         const long tok = (long)p.prefix_len + L - c + (row - start);
         int page = -1;
         if (L >= c && tok < (long)p.max_blocks * kPage) page = p.block_table[(size_t)b * p.max_blocks + tok / kPage];

@@ -222,3 +222,33 @@ def test_rotated_queries_over_the_new_keys_or_values_are_refused():
     torch.cuda.synchronize()
     assert torch.equal(k_new, before[0]) and torch.equal(v_new, before[1])
     ctx.close()
+
+
+@pytest.mark.parametrize("n", [4, 32, 33, 100])
+@pytest.mark.parametrize("kind", ["swapped", "swapped_last", "negative", "behind"])
+@pytest.mark.parametrize("pairs,inter", [(64, False), (20, False), (64, True)])
+def test_malformed_rows_write_nothing(n, kind, pairs, inter):
+    """Among them the starts 0, 9, 10, 1: row 3 would be found in the branch of rows 9 .. 9 and its key belong 6 tokens before
+    that branch's first."""
+    c = Cache(4, 1, chunk=[3] * n, lens=[3] * n, seed=n, spare=0, poison=False)
+    k_new, v_new, pos = inputs(c, 1)
+    ctx = tts.TtsContext(4, 1, n, 1, c.width, c.num_pages)
+    starts = c.row_start.clone()
+    if kind == "swapped":
+        starts[:4] = torch.tensor([0, 9, 10, 1])
+    elif kind == "swapped_last":
+        starts[n - 1] = starts[n] + 1
+    elif kind == "negative":
+        starts[0] = -2 ** 31
+    else:
+        starts[n] = c.total_rows + 1
+    k0, v0, q_out, rope = c.k.clone(), c.v.clone(), torch.full_like(c.q, 7.0), tts.TtsRope([0] * pairs, inv_freq(pairs), inter)
+    ctx.tts_kv_append_rope(rope, c.q, 512, k_new, v_new, 128, pos, c.k, c.v, c.table, 0, c.branch_lens, starts, n, c.total_rows, q_out)
+    torch.cuda.synchronize()
+    assert ctx.tts_last_status() == -4
+    assert (q_out == 7).all() and torch.equal(c.k, k0) and torch.equal(c.v, v0)
+    ctx.tts_kv_append_rope(rope, c.q, 512, k_new, v_new, 128, pos, c.k, c.v, c.table, 0, c.branch_lens, c.row_start, n, c.total_rows, q_out)
+    torch.cuda.synchronize()
+    assert ctx.tts_last_status() == 0
+    check(c, ([0] * pairs, inv_freq(pairs), inter), k0, v0, c.k, c.v, pos, q_out, k_new, v_new)
+    ctx.close()
