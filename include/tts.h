@@ -284,8 +284,10 @@ TTS_API int tts_greedy_search(tts_task_fn tts_task, void* user, const tts_search
 TTS_API int tts_grid_search(tts_task_fn tts_task, void* user, const tts_search_limits* limits,
                     int* best_branches, int* best_gamma, double* best_acc, int* evaluations);
 
-/* Synchronises the stream and reads the device status word: TTS_OK, TTS_ERR_DEVICE_BOUNDS or
- * TTS_ERR_DEVICE_TIMEOUT, written to *device_status; clears it.  Host pointers. */
+/* Synchronises the stream and reads the device status: TTS_OK, TTS_ERR_DEVICE_BOUNDS, TTS_ERR_DEVICE_TIMEOUT (which
+ * comes before TTS_ERR_DEVICE_BOUNDS) or TTS_ERR_DEVICE_PAGES, written to *device_status; clears what it reports.
+ * TTS_ERR_DEVICE_PAGES beside one of the others is reported by the next call.  After a TTS_ERR_DEVICE_TIMEOUT the
+ * results of every call up to this one are in doubt; the context works as before from here on.  Host pointers. */
 TTS_API int tts_last_status(tts_ctx* ctx, int* device_status);
 /* cudaError_t of the last failed CUDA call seen by this context (0 if none). */
 TTS_API int tts_last_cuda_error(tts_ctx* ctx);
@@ -307,8 +309,9 @@ TTS_API int tts_profile_read(tts_ctx* ctx, float* attn_main_us, float* attn_merg
  * on another warp role) is bounded: when its limit runs out the kernel raises TTS_ERR_DEVICE_TIMEOUT in
  * the device status word, lets go of what it holds and returns, so a lost signal never hangs the GPU.
  * tts_debug_wait_timeout runs a separate one-warp kernel on the context's stream that waits, through the
- * same routine, limit_ns nanoseconds (1 us .. 1 s) for a signal that is never sent.  Afterwards
- * tts_last_status reports TTS_ERR_DEVICE_TIMEOUT and the context works as before.
+ * same routine, limit_ns nanoseconds (1 us .. 1 s) for a signal that is never sent, and leaves the chunk
+ * attention's counters in disorder, as a call that gave up does.  tts_last_status then reports
+ * TTS_ERR_DEVICE_TIMEOUT and sets them right: the context works as before.
  */
 TTS_API int tts_debug_wait_timeout(tts_ctx* ctx, int64_t limit_ns);
 /* Static, NUL-terminated description of a tts_status. */

@@ -69,8 +69,15 @@ cudaError_t cache_alloc(Ctx* c) {
 
 cudaError_t cache_reset(Ctx* c) {
     if (c->chunk_rows == 0) return cudaSuccess;
-    const cudaError_t e = cudaMemsetAsync(c->chunk_arrived, 0, c->chunk_arrived_bytes, c->stream);
-    return e == cudaSuccess ? cudaMemsetAsync(c->chunk_head, 0, sizeof(ChunkHead), c->stream) : e;
+    cudaError_t e = cudaMemsetAsync(c->chunk_arrived, 0, c->chunk_arrived_bytes, c->stream);
+    if (e == cudaSuccess) e = cudaMemsetAsync(c->chunk_head, 0, sizeof(ChunkHead), c->stream);
+    return e == cudaSuccess ? cudaStreamSynchronize(c->stream) : e;      // before work on another stream
+}
+
+cudaError_t cache_disturb(Ctx* c) {
+    if (c->chunk_rows == 0) return cudaSuccess;
+    const cudaError_t e = cudaMemsetAsync(c->chunk_arrived, 1, c->chunk_arrived_bytes, c->stream);
+    return e == cudaSuccess ? cudaMemsetAsync(c->chunk_head, 1, sizeof(ChunkHead), c->stream) : e;
 }
 
 void cache_release(Ctx* c) {

@@ -81,6 +81,9 @@ __device__ bool lowest_free(const int32_t* refs, int num_pages, int need, int32_
     return found >= need;
 }
 
+// In the word behind the others' errors, which take the lowest code: too few pages must not hide a wait that ran out.
+__device__ __forceinline__ void raise_pages(int32_t* status) { status[1] = TTS_ERR_DEVICE_PAGES; }
+
 __device__ __forceinline__ bool page_ok(int page, int num_pages) { return page >= 0 && page < num_pages; }
 
 // One 4 KiB tile by one warp.
@@ -161,7 +164,7 @@ fork_plan_kernel(const int32_t* __restrict__ table, int max_blocks, int prefix_l
     if (c == 0) {
         wk.head[0] = ok ? need : 0;
         wk.head[1] = ok;
-        if (!ok) atomicMin(status, (int)TTS_ERR_DEVICE_PAGES);
+        if (!ok) raise_pages(status);
     }
     if (!ok) return;
     if (c < n_children) {
@@ -241,7 +244,7 @@ grow_kernel(int32_t* table, int max_blocks, int prefix_len, int32_t* lens, const
     __syncthreads();
     if (bad) { if (b == 0) atomicMin(status, (int)TTS_ERR_DEVICE_BOUNDS); return; }
     long long at = block_scan(want, wants, &need);
-    if (need > num_pages || !lowest_free(refs, num_pages, (int)need, wk.list_dst, sums, free_refs)) { if (b == 0) atomicMin(status, (int)TTS_ERR_DEVICE_PAGES); return; }
+    if (need > num_pages || !lowest_free(refs, num_pages, (int)need, wk.list_dst, sums, free_refs)) { if (b == 0) raise_pages(status); return; }
     for (int i = lo; i < hi; ++i)
         if (row[i] < 0) {
             const int page = wk.list_dst[at++];

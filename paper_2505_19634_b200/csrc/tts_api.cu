@@ -302,8 +302,8 @@ int tts_create(const tts_config* cfg, tts_ctx** out) {
     c->cfg = *cfg;
     cudaError_t e = cudaGetDevice(&c->device);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&c->n_sms, cudaDevAttrMultiProcessorCount, c->device);
-    if (e == cudaSuccess) e = cudaMalloc(&c->d_status, sizeof(int32_t));
-    if (e == cudaSuccess) e = cudaMemset(c->d_status, 0, sizeof(int32_t));
+    if (e == cudaSuccess) e = cudaMalloc(&c->d_status, 2 * sizeof(int32_t));
+    if (e == cudaSuccess) e = cudaMemset(c->d_status, 0, 2 * sizeof(int32_t));
     if (e == cudaSuccess) e = alloc_workspace(c);
     if (e == cudaSuccess) e = cache_alloc(c);
     if (e != cudaSuccess) {
@@ -579,20 +579,22 @@ int tts_grid_search(tts_task_fn tts_task, void* user, const tts_search_limits* l
 int tts_last_status(tts_ctx* ctx, int* device_status) {
     Ctx* c = reinterpret_cast<Ctx*>(ctx);
     if (!c || !device_status) return TTS_ERR_INVALID;
-    int32_t h = 0;
-    cudaError_t e = cudaMemcpyAsync(&h, c->d_status, sizeof h, cudaMemcpyDeviceToHost, c->stream);
-    if (e == cudaSuccess) e = cudaMemsetAsync(c->d_status, 0, sizeof h, c->stream);
+    int32_t h[2] = {0, 0};
+    cudaError_t e = cudaMemcpyAsync(h, c->d_status, sizeof h, cudaMemcpyDeviceToHost, c->stream);
+    if (e == cudaSuccess) e = cudaMemsetAsync(c->d_status, 0, sizeof h[0], c->stream);
     if (e == cudaSuccess) e = cudaStreamSynchronize(c->stream);
-    if (e == cudaSuccess && h == TTS_ERR_DEVICE_TIMEOUT) e = cache_reset(c);
+    if (e == cudaSuccess && h[0] == TTS_ERR_DEVICE_TIMEOUT) e = cache_reset(c);
+    if (e == cudaSuccess && h[0] == 0 && h[1] != 0) e = cudaMemsetAsync(c->d_status + 1, 0, sizeof h[1], c->stream);
     if (e != cudaSuccess) return cuda_fail(c, e);
-    *device_status = h;
+    *device_status = h[0] != 0 ? h[0] : h[1];
     return TTS_OK;
 }
 
 int tts_debug_wait_timeout(tts_ctx* ctx, int64_t limit_ns) {
     Ctx* c = reinterpret_cast<Ctx*>(ctx);
     if (!c || limit_ns < 1000 || limit_ns > 1000ll * 1000 * 1000) return TTS_ERR_INVALID;
-    const cudaError_t e = launch_wait_probe(c->d_status, limit_ns, nullptr, c->stream);
+    cudaError_t e = launch_wait_probe(c->d_status, limit_ns, nullptr, c->stream);
+    if (e == cudaSuccess) e = cache_disturb(c);
     if (e != cudaSuccess) return cuda_fail(c, e);
     c->launches += 1;
     return TTS_OK;

@@ -279,7 +279,7 @@ struct Ctx {
     cudaStream_t stream;
     int last_cuda_error;
     long long launches;
-    int32_t* d_status;
+    int32_t* d_status;                 // [0] the lowest code that a kernel raised, [1] TTS_ERR_DEVICE_PAGES or 0
     // split-KV workspace
     float* part_o_pre; float2* part_ml_pre; float* part_o_priv; float2* part_ml_priv;
     size_t pre_rows, priv_rows;       // allocated partial rows (each 128 fp32 + one float2)
@@ -365,6 +365,7 @@ cudaError_t launch_append_rope(RopeParams p, int n_sms, cudaStream_t st);
 cudaError_t cache_alloc(Ctx* c);       // page_work
 void cache_release(Ctx* c);
 cudaError_t cache_reset(Ctx* c);       // the chunk attention's counters, after a call that did not end
+cudaError_t cache_disturb(Ctx* c);     // leaves them as such a call does (tts_debug_wait_timeout)
 cudaError_t launch_wait_probe(int32_t* status, long long limit_ns, int* gave_up, cudaStream_t st);
 int simt_rb_rows(int nr);
 constexpr int kSimtTileTokens = 64;
