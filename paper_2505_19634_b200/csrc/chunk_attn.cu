@@ -81,7 +81,7 @@ constexpr int kOffBar = kOffV + kRingV * kOperandBytes;
 enum Bar {
     K_FULL = 0, K_EMPTY = K_FULL + kRingK, V_FULL = K_EMPTY + kRingK, V_EMPTY = V_FULL + kRingV, V_TAIL = V_EMPTY + kRingV,
     Q_FULL, Q_EMPTY = Q_FULL + 2, S_FULL = Q_EMPTY + 2, P_HALF = S_FULL + 2, P_FULL = P_HALF + 2, O_FULL = P_FULL + 2, PIECE_FULL = O_FULL + 2,
-    PIECE_EMPTY = PIECE_FULL + kRingPiece, JOIN_FULL = PIECE_EMPTY + kRingPiece, JOIN_EMPTY, kNumBars
+    PIECE_EMPTY = PIECE_FULL + kRingPiece, JOIN_FULL = PIECE_EMPTY + kRingPiece, JOIN_EMPTY, PART_DONE, PART_LAST = PART_DONE + 2, kNumBars = PART_LAST + 2
 };
 constexpr int kOffMisc = kOffBar + ((kNumBars * 8 + 15) & ~15);   // [0] abort, [1] TMEM base, [2, 3] scratch, [4, 5] last-piece flags
 constexpr int kOffPiece = kOffMisc + 32;                       // ring of pieces (+ their KV head)
@@ -361,6 +361,7 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
         for (int i = 0; i < 2; ++i) {
             mbar_init(bar(Q_FULL + i), 1); mbar_init(bar(Q_EMPTY + i), 1); mbar_init(bar(S_FULL + i), 1);
             mbar_init(bar(P_HALF + i), kSideThreads / 32); mbar_init(bar(P_FULL + i), kSideThreads / 32); mbar_init(bar(O_FULL + i), 1);
+            mbar_init(bar(PART_DONE + i), kSideThreads / 32); mbar_init(bar(PART_LAST + i), 1);
         }
         for (int i = 0; i < kRingPiece; ++i) { mbar_init(bar(PIECE_FULL + i), 1); mbar_init(bar(PIECE_EMPTY + i), 11); }   // all warps but the taker
         mbar_init(bar(JOIN_FULL), kSideThreads / 32); mbar_init(bar(JOIN_EMPTY), kSideThreads / 32);
@@ -612,8 +613,8 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
         const int side = warp >> 2;
         const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t t_s = tmem + side * 128u + lane_base, t_o = t_s + 256u;
-        uint32_t phases = 0;                                // bits: S_FULL, O_FULL of this side, O_FULL of the other, JOIN, a JOIN has been
-        enum { S_PHASE = 1, O_PHASE = 2, OTHER_PHASE = 4, JOIN_PHASE = 8, JOINED = 16 };
+        uint32_t phases = 0;                                // bits: S_FULL, O_FULL of this side, O_FULL of the other, JOIN, a JOIN has been, PART
+        enum { S_PHASE = 1, O_PHASE = 2, OTHER_PHASE = 4, JOIN_PHASE = 8, JOINED = 16, PART_PHASE = 32 };
         bool alive = true;
         for (int it = 0; alive; ++it) {
             int n, key0, step, limit, limit_min;
@@ -821,14 +822,23 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                 continue;
             }
             if (valid) p.part_ml[part_at] = make_float2(m_ref, l_sum);
-            // the last piece of the entry to arrive here joins all of them, in their order
+            // The last piece of the entry to arrive here joins all of them, in their order.  The side's warps meet through
+            // waits that are bounded like all others, and not at a named barrier: when a wait has run out somewhere, one of
+            // them may have left already while the others, whose waits came true at that moment, still arrive here.
             __threadfence();
-            asm volatile("barrier.cta.sync %0, %1;" ::"r"(1 + side), "n"(kSideThreads) : "memory");
-            if ((tid & (kSideThreads - 1)) == 0) {
-                unsigned* counter = p.arrived + ((size_t)x.entry * p.Hkv + w.kvh) * 2 + side;
-                misc[4 + side] = atomicInc(counter, (unsigned)x.parts - 1u) == (unsigned)x.parts - 1u;   // back to 0 for the next call
+            warp_arrive(bar(PART_DONE + side), lane);
+            const bool leads = (warp & 3) == 0;             // counts the piece when all four have left their rows, and tells the others
+            alive = __all_sync(0xffffffffu, mbar_wait(bar((leads ? PART_DONE : PART_LAST) + side), phases & PART_PHASE ? 1 : 0, ab));
+            if (!alive) break;
+            phases ^= PART_PHASE;
+            if (leads) {
+                if (lane == 0) {
+                    unsigned* counter = p.arrived + ((size_t)x.entry * p.Hkv + w.kvh) * 2 + side;
+                    misc[4 + side] = atomicInc(counter, (unsigned)x.parts - 1u) == (unsigned)x.parts - 1u;   // back to 0 for the next call
+                    mbar_arrive(bar(PART_LAST + side));     // (the word is written again when all four are past the next PART_DONE)
+                }
+                __syncwarp();
             }
-            asm volatile("barrier.cta.sync %0, %1;" ::"r"(1 + side), "n"(kSideThreads) : "memory");
             if (misc[4 + side]) {
                 __threadfence();
                 // a unit is 8 columns of a row; four units and two parts at a time keep 16 loads in flight per thread
@@ -879,7 +889,6 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                     }
                 }
             }
-            asm volatile("barrier.cta.sync %0, %1;" ::"r"(1 + side), "n"(kSideThreads) : "memory");   // the flag is free again
         }
     }
 

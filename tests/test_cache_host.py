@@ -4,6 +4,7 @@ work out another way."""
 import ctypes
 import math
 import random
+from pathlib import Path
 
 import pytest
 import torch
@@ -113,3 +114,13 @@ def test_plain_fork():
     assert children.lens == [16, 20, 20, 16, 0, 20] and copies == [(5, 1), (5, 2)]
     assert children.refs() == [5, 1, 1, 3, 2, 1, 0, 0, 0, 0]
     assert book.fork([0] * 8, refs) is None                     # seven copies, five free pages
+
+
+def test_every_wait_of_the_chunk_attention_is_bounded():
+    """A warp may leave the kernel's loop on its own when a wait somewhere has run out, so no other may be waiting for it at
+    a barrier without a limit; the two block-wide ones are where all warps begin and where all end."""
+    source = (Path(tts.library_path()).parent / "csrc" / "chunk_attn.cu").read_text()
+    code = "\n".join(line.split("//")[0] for line in source.splitlines())
+    assert "barrier.cta" not in code and "bar.sync" not in code and "bar.red" not in code
+    assert code.count("__syncthreads") == 2
+    assert "try_wait" not in code                               # mbar_wait alone, which has the limit
