@@ -795,25 +795,27 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                     o[c] = n > 0 && f0 != 0.f ? o[c] * f0 : 0.f;
                     o[c] = joined && f1 != 0.f ? fmaf(oj[c], f1, o[c]) : o[c];
                 }
-                if (!valid) continue;
-                if (!direct) {
+                if (valid) {
+                    if (!direct) {
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) st_global_32(p.part_o + part_at * kHeadDim + 32 * ch + 8 * c, o + 8 * c);
-                } else if (p.out_dtype == TTS_OUT_BF16) {
-                    float w2[16];
+                        for (int c = 0; c < 4; ++c) st_global_32(p.part_o + part_at * kHeadDim + 32 * ch + 8 * c, o + 8 * c);
+                    } else if (p.out_dtype == TTS_OUT_BF16) {
+                        float w2[16];
 #pragma unroll
-                    for (int c = 0; c < 16; ++c) w2[c] = __uint_as_float(bf16_pair(o[2 * c], o[2 * c + 1]));
-                    __nv_bfloat16* to = static_cast<__nv_bfloat16*>(p.out) + row_head * kHeadDim + 32 * ch;
-                    if (p.out_32) {
-                        st_global_32(to, w2); st_global_32(to + 16, w2 + 8);
+                        for (int c = 0; c < 16; ++c) w2[c] = __uint_as_float(bf16_pair(o[2 * c], o[2 * c + 1]));
+                        __nv_bfloat16* to = static_cast<__nv_bfloat16*>(p.out) + row_head * kHeadDim + 32 * ch;
+                        if (p.out_32) {
+                            st_global_32(to, w2); st_global_32(to + 16, w2 + 8);
+                        } else {
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) reinterpret_cast<float4*>(to)[c] = make_float4(w2[4 * c], w2[4 * c + 1], w2[4 * c + 2], w2[4 * c + 3]);
+                        }
                     } else {
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) reinterpret_cast<float4*>(to)[c] = make_float4(w2[4 * c], w2[4 * c + 1], w2[4 * c + 2], w2[4 * c + 3]);
+                        for (int c = 0; c < 4; ++c) store_out8(p, row_head, 32 * ch + 8 * c, o + 8 * c);
                     }
-                } else {
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) store_out8(p, row_head, 32 * ch + 8 * c, o + 8 * c);
                 }
+                __syncwarp();                           // TMEM is read by whole warps
             }
             tc_fence_before();
             if (joined) warp_arrive(bar(JOIN_EMPTY), lane);

@@ -389,3 +389,11 @@ def test_output_aligned_to_16_bytes_only(dtype):
     assert torch.equal(buffer[pad:-pad].view_as(want), want)
     assert (buffer[:pad] == 3).all() and (buffer[-pad:] == 3).all()
     ctx.close()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("hq", [1, 3, 5, 31, 33])
+def test_tiles_that_a_warp_shares_with_no_query(hq, dtype):
+    """Warps some of whose threads have a row of the result and some none: whole, joined from both sides, and cut."""
+    c = Cache(hq, 1, chunk=[1, 2, 3, 7, 1, 1], lens=[9, 300, 3, 40, 20000, 129], seed=hq)
+    check(c, *run(c, dtype))
