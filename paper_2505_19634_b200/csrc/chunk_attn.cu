@@ -81,9 +81,9 @@ constexpr int kOffBar = kOffV + kRingV * kOperandBytes;
 enum Bar {
     K_FULL = 0, K_EMPTY = K_FULL + kRingK, V_FULL = K_EMPTY + kRingK, V_EMPTY = V_FULL + kRingV, V_TAIL = V_EMPTY + kRingV,
     Q_FULL, Q_EMPTY = Q_FULL + 2, S_FULL = Q_EMPTY + 2, P_HALF = S_FULL + 2, P_FULL = P_HALF + 2, O_FULL = P_FULL + 2, PIECE_FULL = O_FULL + 2,
-    PIECE_EMPTY = PIECE_FULL + kRingPiece, JOIN_FULL = PIECE_EMPTY + kRingPiece, JOIN_EMPTY, PART_DONE, PART_LAST = PART_DONE + 2, kNumBars = PART_LAST + 2
+    PIECE_EMPTY = PIECE_FULL + kRingPiece, JOIN_FULL = PIECE_EMPTY + kRingPiece, JOIN_EMPTY, PART_DONE, PART_LAST = PART_DONE + 2, DRAINED = PART_LAST + 2, kNumBars
 };
-constexpr int kOffMisc = kOffBar + ((kNumBars * 8 + 15) & ~15);   // [0] abort, [1] TMEM base, [2, 3] scratch, [4, 5] last-piece flags
+constexpr int kOffMisc = kOffBar + ((kNumBars * 8 + 15) & ~15);   // [0] abort, [1] TMEM base, [2, 3] scratch of the K and V warps, [4, 5] last-piece flags, [6, 7] scratch of the taker and the MMA warp
 constexpr int kOffPiece = kOffMisc + 32;                       // ring of pieces (+ their KV head)
 constexpr int kPieceBytes = 64;
 constexpr int kOffJoin = kOffPiece + kRingPiece * kPieceBytes; // side 1's (m, l) of a narrow piece
@@ -364,7 +364,7 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
             mbar_init(bar(PART_DONE + i), kSideThreads / 32); mbar_init(bar(PART_LAST + i), 1);
         }
         for (int i = 0; i < kRingPiece; ++i) { mbar_init(bar(PIECE_FULL + i), 1); mbar_init(bar(PIECE_EMPTY + i), 11); }   // all warps but the taker
-        mbar_init(bar(JOIN_FULL), kSideThreads / 32); mbar_init(bar(JOIN_EMPTY), kSideThreads / 32);
+        mbar_init(bar(JOIN_FULL), kSideThreads / 32); mbar_init(bar(JOIN_EMPTY), kSideThreads / 32); mbar_init(bar(DRAINED), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == kMmaWarp) {
@@ -446,8 +446,8 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                 if (*ab.flag)
                     for (int s = 0; s < 2; ++s)
                         if (used[s] > 0) {
-                            const Abort quiet{misc + 2, p.status};
-                            misc[2] = 0;
+                            const Abort quiet{misc + 6, p.status};
+                            misc[6] = 0;
                             mbar_wait(bar(Q_FULL + s), (used[s] - 1) & 1, quiet);
                         }
             }
@@ -603,6 +603,16 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                     if (jj < n0) turn(side0, jj);
                     if (alive && jj < n1) turn(side1, jj);
                 }
+            }
+            if (__any_sync(0xffffffffu, *ab.flag != 0)) {
+                // products in flight end before their operands' shared memory and TMEM are someone else's
+                if (elect_one()) {
+                    misc[7] = 0;
+                    umma_commit(bar(DRAINED));
+                }
+                __syncwarp();
+                mbar_wait(bar(DRAINED), 0, Abort{misc + 7, p.status});
+                __syncwarp();
             }
         }
     } else {

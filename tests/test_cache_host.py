@@ -4,6 +4,7 @@ work out another way."""
 import ctypes
 import math
 import random
+import re
 from pathlib import Path
 
 import pytest
@@ -124,3 +125,12 @@ def test_every_wait_of_the_chunk_attention_is_bounded():
     assert "barrier.cta" not in code and "bar.sync" not in code and "bar.red" not in code
     assert code.count("__syncthreads") == 2
     assert "try_wait" not in code                               # mbar_wait alone, which has the limit
+
+
+def test_the_chunk_attention_waits_for_what_it_has_in_flight_when_it_gives_up():
+    """Each warp that starts copies or products waits for them with a word of its own: a wait given up in one of them must
+    not cut another's short."""
+    source = (Path(tts.library_path()).parent / "csrc" / "chunk_attn.cu").read_text()
+    words = re.findall(r"Abort(?: quiet)?\{(misc \+ [^,]*),", source)
+    assert sorted(words) == ["misc + 2 + is_v", "misc + 6", "misc + 7"]
+    assert source.index("umma_commit(bar(DRAINED))") < source.index("tcgen05.dealloc")
