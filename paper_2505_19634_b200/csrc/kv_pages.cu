@@ -124,8 +124,8 @@ copy_pages_kernel(const __grid_constant__ PagePools pools, const int32_t* src, c
 // Block 0 decides, the other blocks carry the counts over into new_refs.  Per child: its parent (or -1),
 // how many leading entries it shares, and the page that takes the copy of the parent's part-filled one.
 __global__ void __launch_bounds__(kMaxScanThreads)
-fork_plan_kernel(const int32_t* __restrict__ table, int max_blocks, int prefix_len, const int32_t* __restrict__ lens, int n_branches,
-                 const int32_t* __restrict__ parents, int n_children, const int32_t* refs, int32_t* new_refs, int num_pages, PageWork wk, int32_t* status) {
+fork_plan_kernel(const int32_t* table, int max_blocks, int prefix_len, const int32_t* lens, int n_branches,
+                 const int32_t* parents, int n_children, const int32_t* refs, int32_t* new_refs, int num_pages, PageWork wk, int32_t* status) {
     grid_dependency_wait();
     grid_launch_dependents();
     if (blockIdx.x > 0) {
@@ -177,7 +177,7 @@ fork_plan_kernel(const int32_t* __restrict__ table, int max_blocks, int prefix_l
 // Blocks [0, n_children): the children's table rows; the next n_branches: references of branches without a
 // child are dropped; the rest copy pages.
 __global__ void __launch_bounds__(kCopyThreads)
-fork_kernel(const __grid_constant__ PagePools pools, const int32_t* __restrict__ table, int max_blocks, int n_branches, int n_children,
+fork_kernel(const __grid_constant__ PagePools pools, const int32_t* table, int max_blocks, int n_branches, int n_children,
             int32_t* new_table, int32_t* new_lens, int32_t* new_refs, int Hkv, int num_pages, PageWork wk, int32_t* status) {
     grid_dependency_wait();
     grid_launch_dependents();
@@ -217,7 +217,7 @@ fork_kernel(const __grid_constant__ PagePools pools, const int32_t* __restrict__
 // ------------------------------------------------------------------------------------------------ grow
 // One CTA, one thread per branch: which entries of its row lack a page, then pages in that order.
 __global__ void __launch_bounds__(kMaxScanThreads)
-grow_kernel(int32_t* table, int max_blocks, int prefix_len, int32_t* lens, const int32_t* __restrict__ n_new, int n_branches, int32_t* refs,
+grow_kernel(int32_t* table, int max_blocks, int prefix_len, int32_t* lens, const int32_t* n_new, int n_branches, int32_t* refs,
             int num_pages, PageWork wk, int32_t* status) {
     grid_dependency_wait();
     grid_launch_dependents();
@@ -256,7 +256,7 @@ grow_kernel(int32_t* table, int max_blocks, int prefix_len, int32_t* lens, const
 
 // One block per branch.
 __global__ void __launch_bounds__(kCopyThreads)
-free_kernel(int32_t* table, int max_blocks, int32_t* lens, const int32_t* __restrict__ freed, int32_t* refs, int num_pages, int32_t* status) {
+free_kernel(int32_t* table, int max_blocks, int32_t* lens, const int32_t* freed, int32_t* refs, int num_pages, int32_t* status) {
     grid_dependency_wait();
     grid_launch_dependents();
     const int b = blockIdx.x;
@@ -340,7 +340,7 @@ compact_plan_kernel(const int32_t* refs, int32_t* new_refs, int num_pages, int32
 // Blocks [0, n_branches): table rows through the map; the rest copy pages.
 __global__ void __launch_bounds__(kCopyThreads)
 compact_kernel(const __grid_constant__ PagePools pools, const int32_t* table, int max_blocks, int n_branches, int32_t* new_table,
-               const int32_t* __restrict__ page_map, int Hkv, int num_pages, PageWork wk, int32_t* status) {
+               const int32_t* page_map, int Hkv, int num_pages, PageWork wk, int32_t* status) {
     grid_dependency_wait();
     grid_launch_dependents();
     if ((int)blockIdx.x < n_branches) {

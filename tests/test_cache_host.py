@@ -134,3 +134,11 @@ def test_the_chunk_attention_waits_for_what_it_has_in_flight_when_it_gives_up():
     words = re.findall(r"Abort(?: quiet)?\{(misc \+ [^,]*),", source)
     assert sorted(words) == ["misc + 2 + is_v", "misc + 6", "misc + 7"]
     assert source.index("umma_commit(bar(DRAINED))") < source.index("tcgen05.dealloc")
+
+
+@pytest.mark.parametrize("name", ["chunk_attn.cu", "chunk_plan.cu", "rope_append.cu", "kv_pages.cu"])
+def test_kernels_that_start_early_read_coherently(name):
+    """Blocks of a programmatic dependent are resident while the kernel before it writes: the read-only path, which const and
+    __restrict__ together or __ldg allow, is for data that nothing writes meanwhile."""
+    source = (Path(tts.library_path()).parent / "csrc" / name).read_text()
+    assert "launch_dependent(" in source and not re.search(r"__restrict__|__ldg\(|ld\.global\.nc", source)
