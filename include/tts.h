@@ -463,9 +463,12 @@ TTS_API int tts_kv_append_rope(tts_ctx* ctx, const tts_rope* rope, const void* q
  *                      branch_lens, page_refs; writes new_table [n_children][max_blocks_per_branch], new_lens, new_refs
  *                      (which may be page_refs).  Pages given back by the call are not handed out by it.  With too few
  *                      free pages new_table and new_lens are left as they were and new_refs equals page_refs.
- *   tts_kv_grow        room for n_new[b] >= 0 more tokens of every branch (device [n_branches] i32): entries up to the
- *                      new length that hold no page get a free one, and branch_lens[b] += n_new[b].  All or nothing: a
- *                      bad length or too few pages change nothing.
+ *   tts_kv_grow        room for n_new[b] >= 0 more tokens of every branch (device [n_branches] i32): entries between the
+ *                      present and the new length that hold no page get a free one, and branch_lens[b] += n_new[b].
+ *                      Every entry up to the present length, the prefix's among them, has to hold a page: a row that
+ *                      tts_kv_free or a fork from -1 left empty grows where prefix_len is 0, and takes a prefix again by
+ *                      tts_kv_fork, or by the caller, who writes the prefix's pages into it and counts them.  All or
+ *                      nothing: a bad length, a missing or bad page in a growing row, or too few pages change nothing.
  *   tts_kv_free        gives back all pages of the branches with freed[b] != 0 (device [n_branches] i32): the row
  *                      becomes -1, the length 0.
  *   tts_kv_compact     closes the holes of the pool: with n_used pages in use, the pages from n_used on move to the

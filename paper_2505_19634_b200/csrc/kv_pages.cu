@@ -215,7 +215,11 @@ fork_kernel(const __grid_constant__ PagePools pools, const int32_t* table, int m
 }
 
 // ------------------------------------------------------------------------------------------------ grow
-// One CTA, one thread per branch: which entries of its row lack a page, then pages in that order.
+// One CTA, one thread per branch: which entries of its row lack a page, then pages in that order.  A row that lacks
+// one in front of its new tokens (the prefix's, after tts_kv_free or a fork from -1) is refused: the tokens
+// would stand behind a hole.  That look is the warps', a row each, 256 entries in flight,
+// the first of them before the row's length is known (16 rows of 240 entries: 2.0 us without, 2.7 with it; 64 rows 2.7 and 5.7;
+// units of 32 entries that any warp takes, 3.9 and 7.6).
 __global__ void __launch_bounds__(kMaxScanThreads)
 grow_kernel(int32_t* table, int max_blocks, int prefix_len, int32_t* lens, const int32_t* n_new, int n_branches, int32_t* refs,
             int num_pages, PageWork wk, int32_t* status) {
@@ -223,27 +227,46 @@ grow_kernel(int32_t* table, int max_blocks, int prefix_len, int32_t* lens, const
     grid_launch_dependents();
     __shared__ int sums[32];
     __shared__ long long wants[32];
-    __shared__ int bad;
-    const int b = threadIdx.x;
-    if (b == 0) bad = 0;
-    int free_refs[kPerThread];
+    __shared__ int held[kMaxBranches];                  // entries of each growing row that have to hold a page
+    const int b = threadIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int free_refs[kPerThread], e[8];
     load_refs(refs, num_pages, (long)b * kPerThread, 1, free_refs);
-    __syncthreads();
+    auto entries = [&](int r, int i0, int n, int (&to)[8]) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) to[k] = i0 + 32 * k < n ? table[(size_t)r * max_blocks + i0 + 32 * k] : 0;
+    };
+    entries(warp, lane, warp < n_branches ? max_blocks : 0, e);
+    bool bad = false;
     int lo = 0, hi = 0, more = 0, len = 0;
     if (b < n_branches) {
         more = n_new[b]; len = lens[b];
         const long after = (long)prefix_len + len + more;
-        if (more < 0 || len < 0 || after > (long)max_blocks * kPage) bad = 1;
-        else if (more > 0) { lo = ceil_div(prefix_len + len, kPage); hi = ceil_div((int)after, kPage); }
+        bad = more < 0 || len < 0 || after > (long)max_blocks * kPage;
+        if (!bad && more > 0) { lo = ceil_div(prefix_len + len, kPage); hi = ceil_div((int)after, kPage); }
+        held[b] = lo;
     }
+    __syncthreads();
     int32_t* row = table + (size_t)b * max_blocks;
+    const int next = lo < hi ? row[lo] : 0;             // (asked for ahead of the look)
+    for (int r = warp; r < n_branches; r += (int)blockDim.x >> 5) {
+        const int n = held[r];
+        for (int i0 = lane; i0 < n; i0 += 8 * 32) {
+            if (r != warp || i0 != lane) entries(r, i0, n, e);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) bad |= i0 + 32 * k < n && !page_ok(e[k], num_pages);
+        }
+    }
     // A branch that lacks more pages than there are is refused whatever the others ask for, so the count may stop there;
     // 1024 such counts and rows of 2^26 entries add up to more than 32 bits hold.
+    constexpr long long kBad = 1ll << 50;               // above any sum of counts
     long long want = 0, need;
-    for (int i = lo; i < hi && want <= num_pages; ++i) want += row[i] < 0;
-    __syncthreads();
-    if (bad) { if (b == 0) atomicMin(status, (int)TTS_ERR_DEVICE_BOUNDS); return; }
-    long long at = block_scan(want, wants, &need);
+    for (int i = lo; i < hi && want <= num_pages; ++i) {
+        const int page = i == lo ? next : row[i];
+        if (page < 0) ++want;
+        else bad |= page >= num_pages || refs[page] <= 0;
+    }
+    long long at = block_scan(bad ? kBad : want, wants, &need);
+    if (need >= kBad) { if (b == 0) atomicMin(status, (int)TTS_ERR_DEVICE_BOUNDS); return; }
     if (need > num_pages || !lowest_free(refs, num_pages, (int)need, wk.list_dst, sums, free_refs)) { if (b == 0) raise_pages(status); return; }
     for (int i = lo; i < hi; ++i)
         if (row[i] < 0) {
@@ -392,7 +415,8 @@ cudaError_t launch_fork(const PagePools& pools, const int32_t* table, int max_bl
 
 cudaError_t launch_grow(int32_t* table, int max_blocks, int prefix_len, int32_t* lens, const int32_t* n_new, int n_branches, int32_t* refs,
                         int num_pages, const PageWork& wk, int32_t* status, cudaStream_t st) {
-    return launch_dependent(grow_kernel, 1, scan_threads(n_branches, num_pages), 0, st, table, max_blocks, prefix_len, lens, n_new, n_branches, refs, num_pages, wk, status);
+    const int threads = std::max(scan_threads(n_branches, num_pages), 32 * std::min(32, n_branches));       // and a warp for each row
+    return launch_dependent(grow_kernel, 1, threads, 0, st, table, max_blocks, prefix_len, lens, n_new, n_branches, refs, num_pages, wk, status);
 }
 
 cudaError_t launch_free(int32_t* table, int max_blocks, int32_t* lens, const int32_t* freed, int n_branches, int32_t* refs, int num_pages,

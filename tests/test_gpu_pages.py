@@ -327,3 +327,52 @@ def test_grow_that_lacks_more_pages_than_32_bits_count():
     assert table[:, 0].tolist() == list(range(n)) and int(table[:, 1:].max()) == -1 and lens.tolist() == [16] * n
     assert refs.tolist() == [1] * n + [0] * (pages - n)
     ctx.close()
+
+
+@pytest.mark.parametrize("emptied_by", ["free", "fork"])
+@pytest.mark.parametrize("prefix", [16, 48])
+def test_a_row_without_its_prefix_does_not_grow(emptied_by, prefix):
+    s = Setup(9, 4, prefix, [5, 16, 37, 160], spare=30)
+    if emptied_by == "free":
+        s.ctx.tts_kv_free(s.table, s.lens, i32([0, 1, 0, 0]), 4, s.refs)
+    else:
+        assert s.fork([0, -1, 2, 3]) == 0
+        s.table, s.lens, s.refs = s.new_table, s.new_lens, s.new_refs
+    before = s.table.clone(), s.lens.clone(), s.refs.clone()
+    s.ctx.tts_kv_grow(s.table, prefix, s.lens, i32([1, 20, 1, 1]), 4, s.refs)
+    torch.cuda.synchronize()
+    assert s.ctx.tts_last_status() == -4
+    assert all(torch.equal(a, b) for a, b in zip(before, (s.table, s.lens, s.refs)))
+    book = Book(s.table.tolist(), prefix, s.lens.tolist(), s.pages)
+    s.ctx.tts_kv_grow(s.table, prefix, s.lens, i32([12, 0, 1, 0]), 4, s.refs)           # the others grow beside it
+    torch.cuda.synchronize()
+    want = book.grow([12, 0, 1, 0], book.refs())
+    assert s.ctx.tts_last_status() == 0
+    assert s.table.tolist() == want.table and s.lens.tolist() == want.lens and s.refs.tolist() == want.refs()
+    shared = prefix // PAGE                                   # the caller gives the row its prefix back
+    s.table[1, :shared] = s.table[0, :shared]
+    s.refs[s.table[0, :shared].long()] += 1
+    book = Book(s.table.tolist(), prefix, s.lens.tolist(), s.pages)
+    s.ctx.tts_kv_grow(s.table, prefix, s.lens, i32([0, 20, 0, 0]), 4, s.refs)
+    torch.cuda.synchronize()
+    want = book.grow([0, 20, 0, 0], book.refs())
+    assert s.ctx.tts_last_status() == 0
+    assert s.table.tolist() == want.table and s.lens.tolist() == want.lens and s.refs.tolist() == want.refs()
+    s.ctx.close()
+
+
+@pytest.mark.parametrize("branch,entry,page", [(0, 0, -1), (3, 1, -1), (3, 7, -1), (3, 7, "pool"), (3, 12, "free"), (3, 12, "pool"), (3, 12, 2 ** 31 - 1)])
+def test_grow_looks_at_the_pages_that_a_row_holds(branch, entry, page):
+    """Branch 3 has 32 + 160 tokens, entries 0 .. 11, and an entry behind them that its new tokens would use."""
+    s = Setup(9, 4, 32, [5, 16, 37, 160], spare=30, held_back=[(3, 1)])
+    s.table[branch, entry] = {"pool": s.pages, "free": s.book.refs().index(0)}.get(page, page)
+    before = s.table.clone(), s.lens.clone(), s.refs.clone()
+    s.ctx.tts_kv_grow(s.table, 32, s.lens, i32([1, 1, 1, 1]), 4, s.refs)
+    torch.cuda.synchronize()
+    assert s.ctx.tts_last_status() == -4
+    assert all(torch.equal(a, b) for a, b in zip(before, (s.table, s.lens, s.refs)))
+    more = [0 if b == branch else 1 for b in range(4)]
+    s.ctx.tts_kv_grow(s.table, 32, s.lens, i32(more), 4, s.refs)                        # a row that does not grow is not looked at
+    torch.cuda.synchronize()
+    assert s.ctx.tts_last_status() == 0 and s.lens.tolist() == [n + m for n, m in zip([5, 16, 37, 160], more)]
+    s.ctx.close()
