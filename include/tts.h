@@ -462,7 +462,9 @@ TTS_API int tts_kv_append_rope(tts_ctx* ctx, const tts_rope* rope, const void* q
  *                      the pages of branches without a child are given back.  Reads block_table [n_branches],
  *                      branch_lens, page_refs; writes new_table [n_children][max_blocks_per_branch], new_lens, new_refs
  *                      (which may be page_refs).  Pages given back by the call are not handed out by it.  With too few
- *                      free pages new_table and new_lens are left as they were and new_refs equals page_refs.
+ *                      free pages new_table and new_lens are left as they were and new_refs equals page_refs.  A parent
+ *                      that does not exist gives an empty row, one of a bad length too, but its pages keep their
+ *                      references.
  *   tts_kv_grow        room for n_new[b] >= 0 more tokens of every branch (device [n_branches] i32): entries between the
  *                      present and the new length that hold no page get a free one, and branch_lens[b] += n_new[b].
  *                      Every entry up to the present length, the prefix's among them, has to hold a page: a row that

@@ -146,7 +146,11 @@ fork_plan_kernel(const int32_t* table, int max_blocks, int prefix_len, const int
         if (p < -1 || p >= n_branches) { atomicMin(status, (int)TTS_ERR_DEVICE_BOUNDS); p = -1; }
         if (p >= 0) {
             len = lens[p];
-            if (len < 0 || (long)prefix_len + len > (long)max_blocks * kPage) { atomicMin(status, (int)TTS_ERR_DEVICE_BOUNDS); p = -1; len = 0; }
+            if (len < 0 || (long)prefix_len + len > (long)max_blocks * kPage) {
+                atomicMin(status, (int)TTS_ERR_DEVICE_BOUNDS);
+                atomicMin(&first[p], c);                // an empty row for the child, but the parent's pages are not given back
+                p = -1; len = 0;
+            }
         }
         if (p >= 0) atomicMin(&first[p], c);
     }

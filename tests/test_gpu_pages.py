@@ -376,3 +376,14 @@ def test_grow_looks_at_the_pages_that_a_row_holds(branch, entry, page):
     torch.cuda.synchronize()
     assert s.ctx.tts_last_status() == 0 and s.lens.tolist() == [n + m for n, m in zip([5, 16, 37, 160], more)]
     s.ctx.close()
+
+
+@pytest.mark.parametrize("alias", [False, True])
+def test_fork_does_not_give_away_the_pages_of_a_parent_of_a_bad_length(alias):
+    for length in (-1, 16 * 100, 2 ** 31 - 1):
+        s = Setup(1, 4, 32, [5, 16, 37, 160])
+        assert s.fork([3, 0, 3], alias, lens=i32([5, 16, 37, length])) == -4
+        want = Book([[-1] * s.width, s.book.table[0], [-1] * s.width], 32, [0, 5, 0], s.pages)
+        assert s.new_table.tolist() == want.table and s.new_lens.tolist() == want.lens
+        assert s.new_refs.tolist() == Book(want.table + [s.book.table[3]], 32, [0] * 4, s.pages).refs()
+        s.ctx.close()
