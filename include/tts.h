@@ -450,8 +450,9 @@ TTS_API int tts_kv_append_rope(tts_ctx* ctx, const tts_rope* rope, const void* q
  *   page_refs    device [num_pages] i32, 16-byte aligned: how many table entries name each page; 0 = free.  Free pages
  *                are handed out lowest id first, to the branches in their order, so results do not depend on timing
  *   k_pools, v_pools  host arrays of n_layers (1..128) device pointers: a page id names the same page in all of them
- * A page id outside the pool, a length outside the table row, or an entry that page_refs does not know raises
- * TTS_ERR_DEVICE_BOUNDS (tts_last_status).  A call that needs more pages than are free raises TTS_ERR_DEVICE_PAGES.
+ * A page id outside the pool, a length outside the table row, or an entry that page_refs does not know (its count is 0)
+ * raises TTS_ERR_DEVICE_BOUNDS (tts_last_status) where the call comes upon it; such an entry is taken for -1 and changes
+ * no count.  A call that needs more pages than are free raises TTS_ERR_DEVICE_PAGES.
  *
  *   tts_kv_copy_pages  page src_pages[i] -> dst_pages[i] in every pool (device arrays, n_copies entries; a negative id
  *                      on either side skips the entry).  A page must not be the target of two entries, nor the target

@@ -86,6 +86,14 @@ __device__ __forceinline__ void raise_pages(int32_t* status) { status[1] = TTS_E
 
 __device__ __forceinline__ bool page_ok(int page, int num_pages) { return page >= 0 && page < num_pages; }
 
+// One reference less; false, and the counts as they were, for a page outside the pool or one that nothing refers to.
+__device__ __forceinline__ bool give_back(int32_t* refs, int page, int num_pages) {
+    if (page >= num_pages) return false;
+    if (atomicSub(refs + page, 1) > 0) return true;
+    atomicAdd(refs + page, 1);
+    return false;
+}
+
 // One 4 KiB tile by one warp.
 __device__ __forceinline__ void copy_tile(const uint4* src, uint4* dst, int lane) {
     uint4 x[kTileChunks];
@@ -194,7 +202,8 @@ fork_kernel(const __grid_constant__ PagePools pools, const int32_t* table, int m
             int e = -1;
             if (i < ch.y) {
                 e = table[(size_t)ch.x * max_blocks + i];
-                if (e >= num_pages) { atomicMin(status, (int)TTS_ERR_DEVICE_BOUNDS); e = -1; }
+                // (a page whose entries are counted has one reference at all times, the first child's)
+                if (e >= num_pages || (e >= 0 && __ldcg(new_refs + e) <= 0)) { atomicMin(status, (int)TTS_ERR_DEVICE_BOUNDS); e = -1; }
                 e = e < 0 ? -1 : e;
                 if (shares && e >= 0) atomicAdd(new_refs + e, 1);
             } else if (i == ch.y && ch.z >= 0) {
@@ -209,7 +218,7 @@ fork_kernel(const __grid_constant__ PagePools pools, const int32_t* table, int m
         if (!wk.childless[b]) return;
         for (int i = threadIdx.x; i < max_blocks; i += kCopyThreads) {
             const int e = table[(size_t)b * max_blocks + i];
-            if (page_ok(e, num_pages)) atomicSub(new_refs + e, 1);
+            if (e >= 0 && !give_back(new_refs, e, num_pages)) atomicMin(status, (int)TTS_ERR_DEVICE_BOUNDS);
         }
     } else {
         const int blk0 = n_children + n_branches;
@@ -292,7 +301,7 @@ free_kernel(int32_t* table, int max_blocks, int32_t* lens, const int32_t* freed,
         const int e = table[(size_t)b * max_blocks + i];
         table[(size_t)b * max_blocks + i] = -1;
         if (e < 0) continue;
-        if (e >= num_pages || atomicSub(refs + e, 1) <= 0) atomicMin(status, (int)TTS_ERR_DEVICE_BOUNDS);
+        if (!give_back(refs, e, num_pages)) atomicMin(status, (int)TTS_ERR_DEVICE_BOUNDS);
     }
     if (threadIdx.x == 0) lens[b] = 0;
 }

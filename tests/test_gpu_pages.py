@@ -387,3 +387,30 @@ def test_fork_does_not_give_away_the_pages_of_a_parent_of_a_bad_length(alias):
         assert s.new_table.tolist() == want.table and s.new_lens.tolist() == want.lens
         assert s.new_refs.tolist() == Book(want.table + [s.book.table[3]], 32, [0] * 4, s.pages).refs()
         s.ctx.close()
+
+
+@pytest.mark.parametrize("branch,entry", [(0, 1), (1, 1), (2, 4)])
+@pytest.mark.parametrize("page", ["pool", "free", 2 ** 31 - 1])
+def test_fork_reports_bad_entries_of_every_row(branch, entry, page):
+    """Branch 0 has two children, branch 1 one, branch 2 none.  A bad entry counts as none: the children's are -1."""
+    s = Setup(1, 4, 32, [5, 16, 37, 160])
+    free = max(p for p, n in enumerate(s.book.refs()) if n == 0)
+    table = s.table.clone()
+    table[branch, entry] = {"pool": s.pages, "free": free}.get(page, page)
+    refs = Book([[-1 if (b, i) == (branch, entry) else e for i, e in enumerate(row)] for b, row in enumerate(s.book.table)], 32, s.book.lens, s.pages)
+    s.refs.copy_(i32(refs.refs()))
+    want, _ = refs.fork([0, 1, 0, 3], refs.refs())
+    assert s.fork([0, 1, 0, 3], table=table) == -4
+    assert s.new_table.tolist() == want.table and s.new_refs.tolist() == want.refs()
+    s.ctx.close()
+
+
+@pytest.mark.parametrize("page", ["pool", "free"])
+def test_free_of_an_entry_that_nothing_counts_leaves_the_counts(page):
+    s = Setup(4, 3, 32, [5, 16, 37])
+    s.table[1, 6] = {"pool": s.pages, "free": s.book.refs().index(0)}[page]
+    s.ctx.tts_kv_free(s.table, s.lens, i32([0, 1, 0]), 3, s.refs)
+    torch.cuda.synchronize()
+    assert s.ctx.tts_last_status() == -4
+    assert s.refs.tolist() == Book([s.book.table[0], s.book.table[2]], 32, [5, 37], s.pages).refs() and s.table[1].tolist() == [-1] * s.width
+    s.ctx.close()
