@@ -479,7 +479,9 @@ TTS_API int tts_kv_append_rope(tts_ctx* ctx, const tts_rope* rope, const void* q
  *                      device [num_pages] i32 gets the new id of every page (-1: free), for tables of the caller's own;
  *                      n_used device [1] i32.  block_table must hold all references that page_refs counts, or the
  *                      others have to be mapped by the caller.  new_table may be block_table, new_refs page_refs.
- * TTS_ERR_INVALID for null or misaligned pointers, sizes outside the context's limits and overlaps not named above.
+ * TTS_ERR_INVALID for null or misaligned pointers, sizes outside the context's limits, arrays that overlap one another
+ * where one is written and it is not named above, and pools that overlap an array or each other (the same pool may
+ * be given twice).
  */
 TTS_API int tts_kv_copy_pages(tts_ctx* ctx, int n_layers, void* const* k_pools, void* const* v_pools,
                               const int32_t* src_pages, const int32_t* dst_pages, int n_copies);

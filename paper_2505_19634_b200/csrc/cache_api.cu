@@ -2,6 +2,10 @@
 #include <math.h>
 #include <string.h>
 
+#include <algorithm>
+#include <functional>
+#include <initializer_list>
+
 #include "chunk_attn.cuh"
 #include "launch.cuh"
 #include "tts_internal.cuh"
@@ -31,6 +35,35 @@ bool branches_ok(const Ctx* c, const int32_t* block_table, int prefix_len, int n
 bool overlap(const void* a, size_t na, const void* b, size_t nb) {
     const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
     return x < y + nb && y < x + na;
+}
+
+struct Span { const void* at; size_t bytes; };
+// Does `written` share memory with one of the others?
+bool clash(const Span& written, std::initializer_list<Span> others) {
+    for (const Span& o : others) if (overlap(written.at, written.bytes, o.at, o.bytes)) return true;
+    return false;
+}
+size_t pool_bytes(const tts_config& f) { return (size_t)f.num_pages * f.n_kv_heads * kPage * kHeadDim * 2; }
+size_t table_bytes(const tts_config& f, int n) { return (size_t)n * f.max_blocks_per_branch * 4; }
+
+// What the page calls copy: pools that overlap without being the same one, or that share memory with one of the arrays,
+// would be read after they are written.
+bool pools_clash(const PagePools& pools, size_t bytes, std::initializer_list<Span> arrays) {
+    const int n = 2 * pools.n_layers, half = pools.n_layers;
+    const std::less<const void*> before;
+    const void* kv[2 * kMaxLayers], *at[2 * kMaxLayers];
+    for (int i = 0; i < half; ++i) { kv[i] = pools.p[2 * i]; kv[half + i] = pools.p[2 * i + 1]; }
+    // (a program that allocates its layers in order has two runs in order: 128 pools take 0.3 us to merge, 2 to sort)
+    if (!std::is_sorted(kv, kv + half, before)) std::sort(kv, kv + half, before);
+    if (!std::is_sorted(kv + half, kv + n, before)) std::sort(kv + half, kv + n, before);
+    std::merge(kv, kv + half, kv + half, kv + n, at, before);
+    for (int i = 1; i < n; ++i)
+        if (at[i] != at[i - 1] && overlap(at[i - 1], bytes, at[i], bytes)) return true;
+    for (const Span& a : arrays) {
+        const int i = (int)(std::upper_bound(at, at + n, a.at, before) - at);        // the first pool behind the array's start
+        if ((i > 0 && overlap(at[i - 1], bytes, a.at, a.bytes)) || (i < n && overlap(at[i], bytes, a.at, a.bytes))) return true;
+    }
+    return false;
 }
 
 bool pools_from(int n_layers, void* const* k_pools, void* const* v_pools, PagePools* out) {
@@ -212,6 +245,7 @@ int tts_kv_copy_pages(tts_ctx* ctx, int n_layers, void* const* k_pools, void* co
     if (!c || !src_pages || !dst_pages || n_copies < 0 || !aligned4(src_pages) || !aligned4(dst_pages)) return TTS_ERR_INVALID;
     if (!pools_from(n_layers, k_pools, v_pools, &pools)) return TTS_ERR_INVALID;
     if (n_copies == 0) return TTS_OK;
+    if (pools_clash(pools, pool_bytes(c->cfg), {{src_pages, (size_t)n_copies * 4}, {dst_pages, (size_t)n_copies * 4}})) return TTS_ERR_INVALID;
     const OnDevice on(c->device);
     if (on.error() != cudaSuccess) return finish(c, on.error(), 0);
     return finish(c, launch_copy_pages(pools, src_pages, dst_pages, n_copies, c->cfg.n_kv_heads, c->cfg.num_pages, c->n_sms, c->d_status, c->stream), 1);
@@ -228,10 +262,13 @@ int tts_kv_fork(tts_ctx* ctx, int n_layers, void* const* k_pools, void* const* v
         return TTS_ERR_INVALID;
     if (!pools_from(n_layers, k_pools, v_pools, &pools)) return TTS_ERR_INVALID;
     const tts_config& f = c->cfg;
-    const size_t row = (size_t)f.max_blocks_per_branch * 4;
     // children are written while their parents' rows are read
-    if (overlap(block_table, n_branches * row, new_table, n_children * row) || overlap(branch_lens, n_branches * 4, new_lens, n_children * 4) ||
-        (page_refs != new_refs && overlap(page_refs, (size_t)f.num_pages * 4, new_refs, (size_t)f.num_pages * 4)))
+    const Span table{block_table, table_bytes(f, n_branches)}, lens{branch_lens, (size_t)n_branches * 4}, who{parents, (size_t)n_children * 4},
+        refs{page_refs, (size_t)f.num_pages * 4}, out_table{new_table, table_bytes(f, n_children)}, out_lens{new_lens, (size_t)n_children * 4},
+        out_refs{new_refs, refs.bytes};
+    if (clash(out_table, {table, lens, who, refs, out_lens, out_refs}) || clash(out_lens, {table, lens, who, refs, out_refs}) ||
+        clash(out_refs, {table, lens, who}) || (page_refs != new_refs && clash(out_refs, {refs})) ||
+        pools_clash(pools, pool_bytes(f), {table, lens, who, refs, out_table, out_lens, out_refs}))
         return TTS_ERR_INVALID;
     c->plan_explicit = 0;
     const OnDevice on(c->device);
@@ -244,6 +281,9 @@ int tts_kv_grow(tts_ctx* ctx, int32_t* block_table, int prefix_len, int32_t* bra
     Ctx* c = reinterpret_cast<Ctx*>(ctx);
     if (!c || !branch_lens || !n_new || !page_refs || !branches_ok(c, block_table, prefix_len, n_branches)) return TTS_ERR_INVALID;
     if (!aligned4(branch_lens) || !aligned4(n_new) || !aligned16(page_refs)) return TTS_ERR_INVALID;
+    const Span table{block_table, table_bytes(c->cfg, n_branches)}, lens{branch_lens, (size_t)n_branches * 4}, more{n_new, lens.bytes},
+        refs{page_refs, (size_t)c->cfg.num_pages * 4};
+    if (clash(table, {lens, more, refs}) || clash(lens, {more, refs}) || clash(refs, {more})) return TTS_ERR_INVALID;
     c->plan_explicit = 0;                               // the lengths and the table change
     const OnDevice on(c->device);
     if (on.error() != cudaSuccess) return finish(c, on.error(), 0);
@@ -255,6 +295,9 @@ int tts_kv_free(tts_ctx* ctx, int32_t* block_table, int32_t* branch_lens, const 
     Ctx* c = reinterpret_cast<Ctx*>(ctx);
     if (!c || !branch_lens || !freed || !page_refs || !branches_ok(c, block_table, 0, n_branches)) return TTS_ERR_INVALID;
     if (!aligned4(branch_lens) || !aligned4(freed) || !aligned16(page_refs)) return TTS_ERR_INVALID;
+    const Span table{block_table, table_bytes(c->cfg, n_branches)}, lens{branch_lens, (size_t)n_branches * 4}, which{freed, lens.bytes},
+        refs{page_refs, (size_t)c->cfg.num_pages * 4};
+    if (clash(table, {lens, which, refs}) || clash(lens, {which, refs}) || clash(refs, {which})) return TTS_ERR_INVALID;
     c->plan_explicit = 0;
     const OnDevice on(c->device);
     if (on.error() != cudaSuccess) return finish(c, on.error(), 0);
@@ -270,8 +313,11 @@ int tts_kv_compact(tts_ctx* ctx, int n_layers, void* const* k_pools, void* const
     if (!aligned16(page_refs) || !aligned4(new_table) || !aligned16(new_refs) || !aligned16(page_map) || !aligned4(n_used)) return TTS_ERR_INVALID;
     if (!pools_from(n_layers, k_pools, v_pools, &pools)) return TTS_ERR_INVALID;
     const tts_config& f = c->cfg;
-    const size_t table = (size_t)n_branches * f.max_blocks_per_branch * 4, refs = (size_t)f.num_pages * 4;
-    if ((block_table != new_table && overlap(block_table, table, new_table, table)) || (page_refs != new_refs && overlap(page_refs, refs, new_refs, refs)))
+    const Span table{block_table, table_bytes(f, n_branches)}, refs{page_refs, (size_t)f.num_pages * 4}, out_table{new_table, table.bytes},
+        out_refs{new_refs, refs.bytes}, map{page_map, refs.bytes}, used{n_used, 4};
+    if ((block_table != new_table && clash(out_table, {table})) || (page_refs != new_refs && clash(out_refs, {refs})) ||
+        clash(out_table, {refs, out_refs}) || clash(out_refs, {table}) || clash(map, {table, refs, out_table, out_refs, used}) ||
+        clash(used, {table, refs, out_table, out_refs}) || pools_clash(pools, pool_bytes(f), {table, refs, out_table, out_refs, map, used}))
         return TTS_ERR_INVALID;
     c->plan_explicit = 0;
     const OnDevice on(c->device);

@@ -414,3 +414,70 @@ def test_free_of_an_entry_that_nothing_counts_leaves_the_counts(page):
     assert s.ctx.tts_last_status() == -4
     assert s.refs.tolist() == Book([s.book.table[0], s.book.table[2]], 32, [5, 37], s.pages).refs() and s.table[1].tolist() == [-1] * s.width
     s.ctx.close()
+
+
+def test_overlaps_are_refused():
+    """Whatever a call writes shares no memory with anything else it is given, but for what the header names."""
+    s = Setup(8, 4, 32, [5, 16, 37, 160])
+    p, m = i32([0, 0, 1, 3]), i32([1, 1, 1, 1])
+    nt, nl, nr, pm, nu = torch.empty_like(s.table), i32([0] * 4), torch.empty_like(s.refs), torch.empty_like(s.refs), i32([0])
+    calls = {
+        "fork": (s.ctx.tts_kv_fork, dict(pools=s.pools, table=s.table, prefix=32, lens=s.lens, n=4, parents=p, m=4, refs=s.refs, new_table=nt, new_lens=nl, new_refs=nr)),
+        "grow": (s.ctx.tts_kv_grow, dict(table=s.table, prefix=32, lens=s.lens, more=m, n=4, refs=s.refs)),
+        "free": (s.ctx.tts_kv_free, dict(table=s.table, lens=s.lens, freed=m, n=4, refs=s.refs)),
+        "compact": (s.ctx.tts_kv_compact, dict(pools=s.pools, table=s.table, n=4, refs=s.refs, new_table=nt, new_refs=nr, page_map=pm, n_used=nu)),
+        "copy": (s.ctx.tts_kv_copy_pages, dict(pools=s.pools, src=p, dst=m, n=4)),
+    }
+    written = {"fork": ["new_table", "new_lens", "new_refs"], "grow": ["table", "lens", "refs"], "free": ["table", "lens", "refs"],
+               "compact": ["new_table", "new_refs", "page_map", "n_used"], "copy": []}
+    same = {("fork", "new_refs", "refs"), ("compact", "new_table", "table"), ("compact", "new_refs", "refs")}
+    before = [x.clone() for x in (s.table, s.lens, s.refs, p, m, nt, nl, nr, pm, nu, s.k, s.v)]
+
+    def refused(name, **kw):
+        fn, args = calls[name]
+        with pytest.raises(tts.TtsError) as e:
+            fn(*(args | kw).values())
+        assert e.value.status == -1, (name, kw)
+
+    bytes_of = lambda t: t.numel() * t.element_size()
+    for name, (_, args) in calls.items():
+        arrays = {k: v for k, v in args.items() if isinstance(v, torch.Tensor)}
+        for w in written[name]:
+            for other, t in arrays.items():
+                if other == w:
+                    continue
+                wide = 16 if {w, other} & {"refs", "new_refs", "page_map"} else 4
+                end = t.data_ptr() + (bytes_of(t) - 1) // wide * wide       # the last place that the alignment allows
+                for at in (t.data_ptr(), end):
+                    if (name, w, other) in same and at == t.data_ptr():
+                        continue
+                    refused(name, **{w: at})
+        if "pools" in args:
+            size = bytes_of(s.k[0])
+            for w, t in arrays.items():
+                for at in (s.k.data_ptr(), s.k[1].data_ptr() + size - 16, s.v[2].data_ptr() + size - 16):
+                    refused(name, **{w: at})
+            shifted = s.k[0].data_ptr() + 4096
+            refused(name, pools=tts.TtsPools([s.k[0], shifted], [s.v[0], s.v[1]]))
+            refused(name, pools=tts.TtsPools([s.v[2], s.v[0]], [s.k[0], s.v[2].data_ptr() - 4096]))
+    torch.cuda.synchronize()
+    bits = lambda x: x.view(torch.int16) if x.dtype == torch.bfloat16 else x
+    assert all(torch.equal(bits(a), bits(b)) for a, b in zip(before, (s.table, s.lens, s.refs, p, m, nt, nl, nr, pm, nu, s.k, s.v)))
+    assert s.ctx.tts_last_status() == 0
+    # the same pool twice, and arrays and pools that touch, are fine
+    k0, v0 = s.k.clone(), s.v.clone()
+    s.ctx.tts_kv_copy_pages(tts.TtsPools([s.k[2], s.k[0], s.k[2]], [s.v[1], s.v[1], s.v[0]]), i32([3]), i32([4]), 1)
+    both = torch.empty(2, 4, s.width, dtype=torch.int32, device="cuda")
+    both[0] = s.table
+    s.ctx.tts_kv_fork(s.pools, both[0], 32, s.lens, 4, p, 4, s.refs, both[1], nl, nr)
+    torch.cuda.synchronize()
+    want, copies = s.book.fork(p.tolist(), s.book.refs())
+    assert s.ctx.tts_last_status() == 0 and both[1].tolist() == want.table and nr.tolist() == want.refs()
+    for layer in (0, 2):
+        k0[layer, 4] = k0[layer, 3]
+    for layer in (0, 1):
+        v0[layer, 4] = v0[layer, 3]
+    for a, b in copies:
+        k0[:, b], v0[:, b] = k0[:, a], v0[:, a]
+    assert torch.equal(s.k, k0) and torch.equal(s.v, v0)
+    s.ctx.close()
