@@ -389,8 +389,8 @@ TTS_API int tts_kv_rollback(tts_ctx* ctx, int32_t* branch_lens, const int32_t* a
  *   lse = -infinity.
  *     q            device  rows of [Hq][128] bf16, q_row_stride elements from row to row (>= Hq * 128, a multiple of
  *                          8), so that q may be a slice of a fused projection; 16-byte aligned
- *     out          device  [total_rows][Hq][128], cfg.out_dtype; must not overlap q (TTS_ERR_INVALID)
- *     lse          device  [total_rows][Hq] fp32, or NULL; must not overlap q or out
+ *     out          device  [total_rows][Hq][128], cfg.out_dtype; must not overlap any other array (TTS_ERR_INVALID)
+ *     lse          device  [total_rows][Hq] fp32, or NULL; must not either
  *     total_rows   host    rows of the arrays, <= the reserved number; 0 launches nothing
  *     k_pages, v_pages, block_table, prefix_len (host, a multiple of 16; the first prefix_len / 16 entries of the rows
  *     may, but need not be equal), branch_lens: as in tts_verify_attn
@@ -424,8 +424,8 @@ TTS_API int tts_chunk_attn(tts_ctx* ctx, const void* q, int64_t q_row_stride, co
  *   q, k, v      device  rows of [Hq][128], [Hkv][128], [Hkv][128] bf16; q_row_stride / kv_row_stride elements from row
  *                        to row (multiples of 8); 16-byte aligned
  *   positions    device  [n_axes][total_rows] i32, any values; the angle is formed in 64 bits
- *   q_out        device  [total_rows][Hq][128] bf16; may be q itself when q is dense; other overlaps with q, k or v are
- *                        refused
+ *   q_out        device  [total_rows][Hq][128] bf16; may be q itself when q is dense; other overlaps of q_out, k_pages or
+ *                        v_pages with each other or with what is read are refused (TTS_ERR_INVALID)
  *   k_pages, v_pages are written, the other arguments as in tts_chunk_attn (total_rows is not bounded by a reserve)
  * A branch shorter than its chunk, a token beyond the table row or a page outside the pool writes no key and value for
  * that row and raises TTS_ERR_DEVICE_BOUNDS; the query is rotated all the same.  Row starts that decrease or leave

@@ -170,7 +170,9 @@ int tts_chunk_attn(tts_ctx* ctx, const void* q, int64_t q_row_stride, const void
     const size_t q_bytes = ((size_t)(total_rows - 1) * q_row_stride + (size_t)f.n_q_heads * kHeadDim) * 2;
     const size_t out_bytes = (size_t)total_rows * f.n_q_heads * kHeadDim * (f.out_dtype == TTS_OUT_FP32 ? 4 : 2);
     const size_t lse_bytes = lse ? (size_t)total_rows * f.n_q_heads * 4 : 0;
-    if (overlap(q, q_bytes, out, out_bytes) || (lse && (overlap(lse, lse_bytes, out, out_bytes) || overlap(lse, lse_bytes, q, q_bytes))))
+    const Span queries{q, q_bytes}, keys{k_pages, pool_bytes(f)}, values{v_pages, keys.bytes}, table{block_table, table_bytes(f, n_branches)},
+        lens{branch_lens, (size_t)n_branches * 4}, starts{row_start, (size_t)(n_branches + 1) * 4}, result{out, out_bytes}, logs{lse, lse_bytes};
+    if (clash(result, {queries, keys, values, table, lens, starts}) || (lse && clash(logs, {result, queries, keys, values, table, lens, starts})))
         return TTS_ERR_INVALID;
     const OnDevice on(c->device);
     if (on.error() != cudaSuccess) return finish(c, on.error(), 0);
@@ -220,10 +222,15 @@ int tts_kv_append_rope(tts_ctx* ctx, const tts_rope* rope, const void* q, int64_
     if (q_row_stride < q_row || q_row_stride % 8 != 0 || kv_row_stride < kv_row || kv_row_stride % 8 != 0) return TTS_ERR_INVALID;
     if (total_rows == 0) return TTS_OK;
     // q_out may be q itself, when q is dense; any other overlap would be read after it is written
-    const size_t out_bytes = (size_t)total_rows * q_row * 2, q_bytes = ((size_t)(total_rows - 1) * q_row_stride + q_row) * 2;
-    if (overlap(q, q_bytes, q_out, out_bytes) && !(q == q_out && q_row_stride == q_row)) return TTS_ERR_INVALID;
     const size_t kv_bytes = ((size_t)(total_rows - 1) * kv_row_stride + kv_row) * 2;
-    if (overlap(k, kv_bytes, q_out, out_bytes) || overlap(v, kv_bytes, q_out, out_bytes)) return TTS_ERR_INVALID;
+    const Span queries{q, ((size_t)(total_rows - 1) * q_row_stride + q_row) * 2}, new_k{k, kv_bytes}, new_v{v, kv_bytes},
+        at{positions, (size_t)rope->n_axes * total_rows * 4}, turned{q_out, (size_t)total_rows * q_row * 2}, keys{k_pages, pool_bytes(f)},
+        values{v_pages, keys.bytes}, table{block_table, table_bytes(f, n_branches)}, lens{branch_lens, (size_t)n_branches * 4},
+        starts{row_start, (size_t)(n_branches + 1) * 4};
+    if (clash(turned, {queries}) && !(q == q_out && q_row_stride == q_row)) return TTS_ERR_INVALID;
+    if (clash(turned, {new_k, new_v, at, keys, values, table, lens, starts}) || clash(keys, {queries, new_k, new_v, at, values, table, lens, starts}) ||
+        clash(values, {queries, new_k, new_v, at, table, lens, starts}))
+        return TTS_ERR_INVALID;
     const OnDevice on(c->device);
     if (on.error() != cudaSuccess) return finish(c, on.error(), 0);
     RopeParams p;

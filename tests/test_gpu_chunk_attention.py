@@ -397,3 +397,23 @@ def test_tiles_that_a_warp_shares_with_no_query(hq, dtype):
     """Warps some of whose threads have a row of the result and some none: whole, joined from both sides, and cut."""
     c = Cache(hq, 1, chunk=[1, 2, 3, 7, 1, 1], lens=[9, 300, 3, 40, 20000, 129], seed=hq)
     check(c, *run(c, dtype))
+
+
+def test_results_over_what_is_read_are_refused():
+    c = Cache(8, 2, chunk=[3, 4], lens=[30, 40], seed=1, poison=False)
+    ctx = context(c)
+    out, lse = torch.zeros_like(c.q), torch.zeros(c.total_rows, c.hq, device="cuda")
+    read = [c.k, c.v, c.table, c.branch_lens, c.row_start]
+    before = [x.clone() for x in read]
+    for x in read:
+        first, last = x.data_ptr() // 16 * 16, (x.data_ptr() + x.numel() * x.element_size() - 1) // 16 * 16
+        for at in (first, last, first - out.numel() * 2 + 16):
+            for o, l in ((at, None), (out, at), (at, lse)):
+                if at == first - out.numel() * 2 + 16 and l is at:
+                    l = first - lse.numel() * 4 + 4
+                with pytest.raises(tts.TtsError) as e:
+                    call(ctx, c, o, l)
+                assert e.value.status == -1
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(before, read)) and not out.any() and not lse.any() and ctx.tts_last_status() == 0
+    ctx.close()

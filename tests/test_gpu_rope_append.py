@@ -252,3 +252,29 @@ def test_malformed_rows_write_nothing(n, kind, pairs, inter):
     assert ctx.tts_last_status() == 0
     check(c, ([0] * pairs, inv_freq(pairs), inter), k0, v0, c.k, c.v, pos, q_out, k_new, v_new)
     ctx.close()
+
+
+def test_what_is_written_over_what_is_read_is_refused():
+    c = Cache(8, 2, chunk=[3, 4], lens=[30, 40], seed=1, poison=False)
+    k_new, v_new, pos = inputs(c, 1)
+    ctx = tts.TtsContext(8, 2, 2, 1, c.width, c.num_pages)
+    a = dict(rope=tts.TtsRope([0] * 64, inv_freq(64)), q=c.q, qs=1024, k=k_new, v=v_new, ks=256, pos=pos, kp=c.k, vp=c.v, table=c.table, prefix=0,
+             lens=c.branch_lens, starts=c.row_start, n=2, rows=7, out=torch.zeros_like(c.q))
+    arrays = {k: x for k, x in a.items() if isinstance(x, torch.Tensor)}
+    before = {k: x.clone() for k, x in arrays.items()}
+    for w in ("out", "kp", "vp"):
+        for other, x in arrays.items():
+            if other == w:
+                continue
+            for at in (x.data_ptr() // 16 * 16, (x.data_ptr() + x.numel() * x.element_size() - 1) // 16 * 16):
+                if (w, other) == ("out", "q") and at == x.data_ptr():
+                    continue                                 # in place
+                with pytest.raises(tts.TtsError) as e:
+                    ctx.tts_kv_append_rope(*(a | {w: at}).values())
+                assert e.value.status == -1, (w, other)
+    torch.cuda.synchronize()
+    assert all(torch.equal(before[k], x) for k, x in arrays.items()) and ctx.tts_last_status() == 0
+    ctx.tts_kv_append_rope(*a.values())
+    torch.cuda.synchronize()
+    assert ctx.tts_last_status() == 0
+    ctx.close()
