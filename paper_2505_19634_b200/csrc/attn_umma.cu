@@ -242,6 +242,10 @@ attn_umma_kernel(const AttnParams p, const __grid_constant__ CUtensorMap tm_k, c
         int it = 0;
         int g = g_begin;
         bool alive = true;
+        // The softmax warps meet at a named barrier, which has no time limit.  A warp whose wait has run out tells the others
+        // at the one that they come to next, and all leave together: those whose waits came true at that moment would
+        // otherwise be left behind there.  All go through the same barriers in the same order.
+        auto leave = [&] { bar_red_or<kSoftmaxThreads>(1, true); };
         SegInfo seg = segment_of_tile(p, cum, g);
         for (bool first_piece = true; g < g_end && alive; first_piece = false) {
             if (!first_piece) seg = next_segment(p, cum, seg);
@@ -278,7 +282,7 @@ attn_umma_kernel(const AttnParams p, const __grid_constant__ CUtensorMap tm_k, c
                 const int tok0 = t * kTile;
                 const bool need_mask = tok0 + kTile > tail0;        // uniform: tile touches masked / missing tokens
                 alive = __all_sync(0xffffffffu, mbar_wait(bar(S_FULL + sb), (it >> 1) & 1, ab));
-                if (!alive) break;
+                if (!alive) { leave(); break; }
                 tc_fence_after();
 
                 // this thread's 64 scores, read once; masked ones become -inf
@@ -301,7 +305,7 @@ attn_umma_kernel(const AttnParams p, const __grid_constant__ CUtensorMap tm_k, c
                 // the row maximum over both halves
                 float* x = xch + (it & 1) * 2 * kRows;
                 x[half * kRows + L] = mx;
-                asm volatile("barrier.cta.sync 1, %0;" ::"n"(kSoftmaxThreads) : "memory");
+                if (bar_red_or<kSoftmaxThreads>(1, false)) { alive = false; break; }
                 mx = fmaxf(x[L], x[kRows + L]) * p.scale_log2;      // scale > 0; -inf stays -inf
                 const bool move = mx > m_ref + 8.f || (m_ref == -INFINITY && mx > -INFINITY);
                 const float m_new = move ? mx : m_ref;
@@ -310,7 +314,7 @@ attn_umma_kernel(const AttnParams p, const __grid_constant__ CUtensorMap tm_k, c
                 if (t > t_first && __any_sync(0xffffffffu, factor != 1.f)) {     // this thread's half of its O row
                     // O is touched: the previous tile's second contraction must have finished
                     alive = __all_sync(0xffffffffu, mbar_wait(bar(PV_DONE + ((it - 1) & 1)), ((it - 1) >> 1) & 1, ab));
-                    if (!alive) break;
+                    if (!alive) { leave(); break; }
                     tc_fence_after();
                     for (int ch = 0; ch < 2; ++ch) {
                         uint32_t ov[32];
@@ -350,7 +354,7 @@ attn_umma_kernel(const AttnParams p, const __grid_constant__ CUtensorMap tm_k, c
                     if (n_valid < n_loaded) {
                         const int slot = it % kRingV;
                         alive = __all_sync(0xffffffffu, mbar_wait(bar(V_FULL + slot), (it / kRingV) & 1, ab));
-                        if (!alive) break;
+                        if (!alive) { leave(); break; }
                         for (int idx = tid; idx < (n_loaded - n_valid) * 16; idx += kSoftmaxThreads) {
                             const int row = n_valid + idx / 16, c = idx % 16;
                             // token `row` of the staged tile: page, token half, 8-token group row; both dim halves
@@ -366,7 +370,7 @@ attn_umma_kernel(const AttnParams p, const __grid_constant__ CUtensorMap tm_k, c
 
             // ---- piece epilogue: partial (m, l, O) ----
             alive = __all_sync(0xffffffffu, mbar_wait(bar(PV_DONE + ((it - 1) & 1)), ((it - 1) >> 1) & 1, ab));
-            if (!alive) break;
+            if (!alive) { leave(); break; }
             tc_fence_after();
             float* po; float2* pml;
             piece_slot(p, seg, blockIdx.x, po, pml);
@@ -384,9 +388,9 @@ attn_umma_kernel(const AttnParams p, const __grid_constant__ CUtensorMap tm_k, c
                                              __uint_as_float(ov[4 * c + 2]), __uint_as_float(ov[4 * c + 3]));
                 }
             }
-            asm volatile("barrier.cta.sync 1, %0;" ::"n"(kSoftmaxThreads) : "memory");
+            if (bar_red_or<kSoftmaxThreads>(1, false)) { alive = false; break; }
             if (valid && half == 0) pml[L] = make_float2(m_ref, l_sum + lx[L]);
-            asm volatile("barrier.cta.sync 1, %0;" ::"n"(kSoftmaxThreads) : "memory");   // lx is free for the next piece
+            bar_sync_id<kSoftmaxThreads>(1);                 // lx is free for the next piece
             tc_fence_before();
             g = seg.tile_begin + t_last;
         }

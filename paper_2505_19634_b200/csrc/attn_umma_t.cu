@@ -86,21 +86,6 @@ struct Lay {
                          L_FULL = O_FREE + 2, L_FREE = L_FULL + 2;
 };
 
-// reducing / plain named barrier `id` over NT threads
-template <int NT>
-__device__ __forceinline__ bool bar_red_or(int id, bool pred) {
-    uint32_t out;
-    asm volatile(
-        "{\n\t.reg .pred p, q;\n\t"
-        "setp.ne.u32 q, %1, 0;\n\t"
-        "barrier.cta.red.or.pred p, %2, %3, q;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(out) : "r"((uint32_t)pred), "r"(id), "n"(NT) : "memory");
-    return out != 0;
-}
-template <int NT>
-__device__ __forceinline__ void bar_sync_id(int id) { asm volatile("barrier.cta.sync %0, %1;" ::"r"(id), "n"(NT) : "memory"); }
-
 // One mbarrier arrival for the whole warp, after every lane's preceding work (arrivals of single
 // threads on one barrier serialise, so the barriers count warps).
 __device__ __forceinline__ void warp_arrive(uint32_t bar, int lane) {

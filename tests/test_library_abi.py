@@ -173,3 +173,13 @@ def test_entry_points_reject_null_contexts_and_bad_groups_without_a_gpu():
     for sizes, pre, n in (((2, 1), (16, 0), 4), ((2, 0, 2), (16, 0, 16), 4), ((1,) * 65, (0,) * 65, 65)):
         assert lib.tts_verify_attn_groups(z, z, z, z, z, i32(*sizes), i32(*pre), len(sizes), z, n, 1, z) == -1
         assert lib.tts_attn_plan_groups(z, z, i32(*sizes), i32(*pre), len(sizes), z, n, 2) == -1
+
+
+def test_softmax_warps_of_the_row_major_kernel_leave_together():
+    """They meet at a named barrier, which has no time limit: one that leaves on its own after a wait has run out would leave
+    the others there for good."""
+    source = (ROOT / "paper_2505_19634_b200" / "csrc" / "attn_umma.cu").read_text()
+    lines = [line.split("//")[0].strip() for line in source[source.index("softmax warps ="):].splitlines()]
+    waits = [i for i, line in enumerate(lines) if "mbar_wait(" in line]
+    assert len(waits) == 4 and all(lines[i + 1] == "if (!alive) { leave(); break; }" for i in waits)
+    assert "barrier.cta" not in source and source.count("bar_sync_id<") == 1 and source.count("bar_red_or<kSoftmaxThreads>(1, false)") == 2
