@@ -417,3 +417,67 @@ def test_results_over_what_is_read_are_refused():
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(before, read)) and not out.any() and not lse.any() and ctx.tts_last_status() == 0
     ctx.close()
+
+
+@pytest.mark.parametrize("branch", [0, 50, 99])
+@pytest.mark.parametrize("what", ["start", "end", "short", "long"])
+def test_malformed_rows_or_lengths_among_many_branches_compute_nothing(branch, what):
+    """More entries than the schedule inside the attention kernel takes: the plan kernel's own look at them."""
+    c = Cache(8, 2, chunk=[3] * 100, lens=[30] * 100, seed=1)
+    ctx = context(c)
+    out, lse = torch.full_like(c.q, 3.0), torch.full((c.total_rows, 8), 3.0, device="cuda")
+    starts, lens = c.row_start.clone(), c.branch_lens.clone()
+    if what == "start":
+        starts[branch] = starts[branch + 1] + 1
+    elif what == "end":
+        starts[branch + 1] = c.total_rows + 1
+    else:
+        lens[branch] = -1 if what == "short" else 16 * c.width + 1
+    call(ctx, c, out, lse, row_start=starts, lens=lens)
+    torch.cuda.synchronize()
+    assert ctx.tts_last_status() == -4 and (out == 3).all() and (lse == 3).all()
+    check(c, *run(c, ctx=ctx))                               # the context works as before
+    ctx.close()
+
+
+def test_capture_and_replay_with_a_plan_kernel():
+    """Two dependent launches in one graph; the replay goes by the lengths and rows that the device holds then."""
+    n = 100
+    c = Cache(8, 2, chunk=[1 + 7 * (i % 13) for i in range(n)], lens=[200 + 31 * (i % 40) for i in range(n)], seed=2)
+    ctx = context(c)
+    out, lse = torch.full_like(c.q, 7.0), torch.full((c.total_rows, 8), 7.0, device="cuda")
+    side = torch.cuda.Stream()
+    ctx.tts_set_stream(side)
+    before = ctx.tts_launch_count()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        call(ctx, c, out, lse)
+    assert ctx.tts_launch_count() - before == 2
+    for lens, chunk in ((c.lens, c.chunk), ([100 + 7 * (i % 9) for i in range(n)], c.chunk), ([90] * n, [0 if i % 5 else 60 for i in range(n)]), (c.lens, [1] * n)):
+        d = c
+        d.lens, d.chunk, d.starts = list(lens), list(chunk), [0]
+        for x in chunk:
+            d.starts.append(d.starts[-1] + x)
+        c.branch_lens.copy_(torch.tensor(lens)), c.row_start.copy_(torch.tensor(d.starts))
+        full = c.rows
+        c.rows = [r[:-(-x // PAGE)] for r, x in zip(full, lens)]
+        for _ in range(2):
+            out.fill_(7), lse.fill_(7)
+            graph.replay()
+            torch.cuda.synchronize()
+            check(c, out, lse)
+        c.rows = full
+    assert ctx.tts_last_status() == 0
+    ctx.close()
+
+
+def test_uneven_branches_beyond_what_is_cut_into_pieces():
+    """4100 blocks of rows, whole: one branch with 9000 keys behind branches of a few."""
+    n = 1024
+    c = Cache(128, 1, chunk=[8] * (n - 1) + [40], lens=[8 + i % 30 for i in range(n - 1)] + [9000], seed=5)
+    check(c, *run(c))
+
+
+def test_a_row_sees_every_key_below_it_where_most_branches_are_empty():
+    c = Cache(8, 1, chunk=[0] * 500 + [33] + [0] * 499 + [1], lens=[0] * 500 + [5000] + [16] * 499 + [1], seed=6)
+    check(c, *run(c))

@@ -481,3 +481,18 @@ def test_overlaps_are_refused():
         k0[:, b], v0[:, b] = k0[:, a], v0[:, a]
     assert torch.equal(s.k, k0) and torch.equal(s.v, v0)
     s.ctx.close()
+
+
+def test_fork_of_as_many_branches_as_a_context_takes():
+    r = random.Random(5)
+    lens = [r.randrange(0, 100) for _ in range(1024)]
+    s = Setup(11, 1024, 16, lens, layers=1, hkv=1, spare=1100)
+    parents = [r.randrange(-1, 1024) for _ in range(1024)]
+    want, copies = s.book.fork(parents, s.book.refs())
+    k0 = s.k.clone()
+    assert s.fork(parents) == 0
+    assert s.new_table.tolist() == want.table and s.new_lens.tolist() == want.lens and s.new_refs.tolist() == want.refs()
+    for a, b in copies:
+        k0[:, b] = k0[:, a]
+    assert torch.equal(s.k, k0)
+    s.ctx.close()
