@@ -395,6 +395,12 @@ TTS_API int tts_kv_rollback(tts_ctx* ctx, int32_t* branch_lens, const int32_t* a
  *     k_pages, v_pages, block_table, prefix_len (host, a multiple of 16; the first prefix_len / 16 entries of the rows
  *     may, but need not be equal), branch_lens: as in tts_verify_attn
  *   cfg.max_ctas bounds the grid, cfg.softmax_scale and cfg.out_dtype apply; cfg.attn_impl does not.
+ *   Scores, sums and accumulators are fp32; the probabilities are rounded to bf16 on their way into the second
+ *   contraction, as in tts_verify_attn, so an element is off by up to 2^-8 of the softmax mean of |V| (about 1.6e-3 of the
+ *   result's size for independent errors) with TTS_OUT_FP32 too.
+ *   Where every branch has the same few rows, tts_verify_attn computes the same: it reads a shared prefix once for all its
+ *   branches, this call once per branch (from L2 where it fits).  Behind a prefix of 512 tokens, 16 branches of 4096 of 40 / 8
+ *   heads: four rows each 52 us either way (there with tts_attn_plan), one row 52 us here, 215 there.
  *   Reported through tts_last_status, whatever cfg.debug_bounds: row starts that decrease or leave [0, total_rows],
  *   negative lengths, or branches longer than the table row compute nothing (TTS_ERR_DEVICE_BOUNDS); a page id outside
  *   the pool is read as zeros (TTS_ERR_DEVICE_BOUNDS).  Slots past a branch's end may hold anything, NaN included.
@@ -446,7 +452,9 @@ TTS_API int tts_kv_append_rope(tts_ctx* ctx, const tts_rope* rope, const void* q
  * several copies, grow, and finish at different times.  These calls keep the books on the device, asynchronously on
  * the context's stream and without reading anything back:
  *   block_table  a row holds the pages of its branch, entries >= 0, and -1 where it has none.  Pages a branch holds
- *                beyond its length (after tts_kv_rollback) stay its own
+ *                beyond its length (after tts_kv_rollback) stay its own.  A row that a call empties is -1 throughout, its
+ *                prefix's entries too: tts_chunk_attn and tts_kv_append_rope take it with a chunk of no rows,
+ *                tts_verify_attn, whose branches hold their new rows, does not (a fork puts the live branches in front)
  *   page_refs    device [num_pages] i32, 16-byte aligned: how many table entries name each page; 0 = free.  Free pages
  *                are handed out lowest id first, to the branches in their order, so results do not depend on timing
  *   k_pools, v_pools  host arrays of n_layers (1..128) device pointers: a page id names the same page in all of them
@@ -465,7 +473,8 @@ TTS_API int tts_kv_append_rope(tts_ctx* ctx, const tts_rope* rope, const void* q
  *                      (which may be page_refs).  Pages given back by the call are not handed out by it.  With too few
  *                      free pages new_table and new_lens are left as they were and new_refs equals page_refs.  A parent
  *                      that does not exist gives an empty row, one of a bad length too, but its pages keep their
- *                      references.
+ *                      references.  Fork after tts_kv_rollback, not before it: the children share full pages, and one
+ *                      that is cut back into such a page would write its next tokens over the others'.
  *   tts_kv_grow        room for n_new[b] >= 0 more tokens of every branch (device [n_branches] i32): entries between the
  *                      present and the new length that hold no page get a free one, and branch_lens[b] += n_new[b].
  *                      Every entry up to the present length, the prefix's among them, has to hold a page: a row that

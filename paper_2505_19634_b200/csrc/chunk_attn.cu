@@ -27,8 +27,8 @@
 //                   is complete P V(j) is as well -- the only wait on O that the softmax needs.
 //
 // Measured (B200 whose copy peak is 6538 GB/s and whose bf16 GEMMs reach 1663 TFLOP/s in a burst, 1394 sustained):
-// 8192 tokens of 40 / 8 heads over 24576 keys 4.4 ms = 1080 TFLOP/s, 0.77 of the sustained rate; 64 single tokens
-// over 1 k to 8 k keys 246 us = 5.7 TB/s, 0.88.  Both run into the card's power limit (1.5 GHz instead of 1.85): a
+// 8192 tokens of 40 / 8 heads over 24576 keys 4.5 ms = 1070 TFLOP/s, 0.77 of the sustained rate; 64 single tokens
+// over 1 k to 8 k keys 250 us = 5.65 TB/s, 0.86.  Both run into the card's power limit (1.5 GHz instead of 1.85): a
 // tile of both sides takes 3300 clocks, of which the tensor pipe works 2050 and a softmax warp's chain (scores,
 // maximum, exponentials at 8 clocks each, stores) fills about 2000, and changes that saved clocks alone
 // (a second MMA warp, two threads per row, part of the exponentials as polynomials) did not save time.  Short pieces
@@ -37,7 +37,8 @@
 //
 // Page ids outside the pool and entries beyond the table row read as zeros (and are reported); tokens past the
 // end of a branch never contribute: their scores are replaced before the maximum and their V rows are zeroed in
-// shared memory, whatever the page holds there.  All waits are bounded (umma_ptx.cuh).
+// shared memory, whatever the page holds there.  All waits between warps are bounded (umma_ptx.cuh), so a warp may leave
+// at any of them: there is no barrier between the one where all begin and the one where all end.
 #include <cuda.h>
 
 #include <type_traits>

@@ -20,7 +20,7 @@ struct ChunkPiece {
     int part;          // which of them this is
     int part_row;      // first row of the entry's partial results, within its KV head's
     int entry;
-    int once;          // the branch's keys are read by this entry alone
+    int once;          // the branch has no other entry in this call (a prefix that it shares with other branches is theirs as well)
 };
 static_assert(sizeof(ChunkPiece) == 48, "read as three 16-byte words");
 

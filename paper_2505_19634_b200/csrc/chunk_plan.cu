@@ -26,7 +26,7 @@ namespace {
 constexpr int kMaxThreads = 1024;
 constexpr int kPer = 2;                               // entries per thread
 constexpr int kMaxCut = kMaxThreads * kPer;             // calls with more entries do not cut them: 14 and more per CTA even
-                                                      // themselves out
+                                                      // themselves out, if they are alike (a long branch behind short ones ends alone)
 
 struct Scan { unsigned long long warp[32]; };
 
