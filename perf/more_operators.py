@@ -269,7 +269,7 @@ def prepare(case, seed):
         rows = case["groups"] * case["beams"] if op == "select" else case.get("n", 1)
         s["ctx"] = tts.TtsContext(case.get("hq", 8), case.get("hkv", 2), rows, case.get("rows", 1), s["table"].shape[1] if "table" in s else 1, plan.get("pages", 1))
         if op == "select":
-            s["ctx"].tts_beam_reserve(rows, case["vocab"], case["select"])
+            s["ctx"].tts_beam_reserve(rows, case["select"])
         elif op == "reorder":
             s["states"] = tts.TtsStates(s["src"], s["dst"], s["bytes"])
         elif op == "append" and case["rope"]:
