@@ -53,6 +53,9 @@ typedef enum {
 enum { TTS_MASK_CAUSAL = 0, TTS_MASK_TREE = 1 };
 enum { TTS_OUT_BF16 = 0, TTS_OUT_FP32 = 1 };
 enum { TTS_LOGITS_BF16 = 0, TTS_LOGITS_FP32 = 1 };
+/* Codes of the 8-bit cache (tts_kv8_append), and the bytes that one page of one KV head takes in it. */
+enum { TTS_KV8_E4M3 = 0, TTS_KV8_INT8 = 1 };
+#define TTS_KV8_RECORD 4224
 /* Which attention kernel runs: AUTO picks tensor cores (tcgen05, TMEM accumulators) when the
  * stacked query rows per KV head make it worthwhile and CUDA cores otherwise.  TCGEN05 picks
  * between the two tensor-core kernels: TOKEN_MAJOR (KV tokens on the MMA M dimension, for at most
@@ -505,6 +508,94 @@ TTS_API int tts_kv_free(tts_ctx* ctx, int32_t* block_table, int32_t* branch_lens
 TTS_API int tts_kv_compact(tts_ctx* ctx, int n_layers, void* const* k_pools, void* const* v_pools,
                            const int32_t* block_table, int n_branches, const int32_t* page_refs, int32_t* new_table,
                            int32_t* new_refs, int32_t* page_map, int32_t* n_used);
+
+/*
+ * The cache in 8 bits.  Section 3.1: a step is dominated by streaming the KV cache, so half its bytes is close to half the time of the
+ * attention, or twice the branches.  Every token's K and V vector of a KV head has a scale of its own:
+ *   value = code * scale,   scale = max(max |x| / Q, 2^-120) (fp32),   code = x / scale rounded to nearest, ties to even,
+ * with codes e4m3 and Q = 448 (TTS_KV8_E4M3: off by at most 2^-4 of the value, or 2^-10 of the scale), or whole numbers and Q = 127
+ * (TTS_KV8_INT8: off by at most half a scale).  A vector with a NaN or an infinity in it has the scale NaN.
+ *   kv8_pages   device  [num_pages][n_kv_heads][TTS_KV8_RECORD] bytes, 16-byte aligned: one pool for K and V.  A record holds the codes of
+ *               16 tokens' K ([16][128] bytes), then V, then the scales of K ([16] fp32) and V.  Within a token's 128 codes the 16-byte
+ *               chunk c stands at place c ^ ((t & 1) | (t >> 2 << 1)), t being the token's number in the page.  The format is an argument
+ *               of every call that looks into a pool, and the same for all of them.
+ * block_table, prefix_len, branch_lens, page_refs and the order of the calls on one context are those of the bf16 cache (page ids name
+ * pages of this pool); tts_kv_grow, tts_kv_free and tts_kv_rollback, which touch tables and lengths alone, serve both.
+ *
+ *   tts_kv8_append      tts_kv_append_rope into the 8-bit pool: the keys are rotated in fp32 and rounded once, to their codes.  rope
+ *                       may be NULL: the keys are stored as they come, and q, positions and q_out must be NULL.
+ *   tts_kv8_read        page src_pages[i] of the pool as bf16 page dst_pages[i] of k_pages and v_pages ([num_dst_pages][n_kv_heads][16][128]):
+ *                       code * scale, rounded once.  Device arrays of n_pages entries, such as rows of two block tables; a negative id on
+ *                       either side skips the entry; a page must not be the target of two.  This is how a long chunk attends to
+ *                       an 8-bit context: its pages are read back into a pool of the caller's and tts_chunk_attn runs on that.
+ *   tts_kv8_attn        tts_verify_attn (tree_parents NULL) and tts_verify_attn_tree over the 8-bit pool: exact softmax attention of
+ *                       rows_per_branch rows per branch, 1 .. cfg.max_rows_per_branch, over the values that the codes stand for.
+ *                         q     device  rows of [Hq][128] bf16, q_row_stride elements from row to row (>= Hq * 128, a multiple of 8): row
+ *                                       i of branch b is row b * rows_per_branch + i
+ *                         out   device  [n_branches * rows_per_branch][Hq][128], cfg.out_dtype
+ *                         lse   device  [n_branches * rows_per_branch][Hq] fp32, the natural logarithm of the sum, or NULL
+ *                       A branch shorter than its rows is allowed: row i sees the tokens t <= prefix_len + branch_lens[b] -
+ *                       rows_per_branch + i (in a tree: those of its ancestors' places that exist), and a row that sees none gets out = 0
+ *                       and lse = -infinity.  Scores and sums are fp32, probabilities times V's scale are rounded to fp16 (2^-11).
+ *                       Slots past a branch's end may hold anything; a token whose scale is NaN makes NaN the rows that see it and no
+ *                       others.  cfg.max_ctas, softmax_scale and out_dtype apply, attn_impl does not.
+ *   tts_kv8_copy_pages, tts_kv8_fork, tts_kv8_compact
+ *                       tts_kv_copy_pages, tts_kv_fork, tts_kv_compact over n_layers (1..128) 8-bit pools, one per layer.
+ * Reported through tts_last_status as TTS_ERR_DEVICE_BOUNDS, whatever cfg.debug_bounds: what the bf16 calls report; by tts_kv8_attn a
+ * branch of negative length or beyond the table row, which counts as empty, and a page id outside the pool, which is read as zeros.
+ * TTS_ERR_INVALID for null or misaligned pointers, sizes outside the context's limits, and results that overlap anything else
+ * (q_out may be q itself when q is dense); TTS_ERR_UNSUPPORTED for an unknown format.
+ */
+TTS_API int tts_kv8_append(tts_ctx* ctx, int format, const tts_rope* rope, const void* q, int64_t q_row_stride, const void* k,
+                           const void* v, int64_t kv_row_stride, const int32_t* positions, void* kv8_pages, const int32_t* block_table,
+                           int prefix_len, const int32_t* branch_lens, const int32_t* row_start, int n_branches, int total_rows, void* q_out);
+TTS_API int tts_kv8_read(tts_ctx* ctx, int format, const void* kv8_pages, const int32_t* src_pages, const int32_t* dst_pages, int n_pages,
+                         void* k_pages, void* v_pages, int num_dst_pages);
+TTS_API int tts_kv8_attn(tts_ctx* ctx, int format, const void* q, int64_t q_row_stride, const void* kv8_pages, const int32_t* block_table,
+                         int prefix_len, const int32_t* branch_lens, const int32_t* tree_parents, int n_branches, int rows_per_branch,
+                         void* out, float* lse);
+TTS_API int tts_kv8_copy_pages(tts_ctx* ctx, int n_layers, void* const* kv8_pools, const int32_t* src_pages, const int32_t* dst_pages,
+                               int n_copies);
+TTS_API int tts_kv8_fork(tts_ctx* ctx, int n_layers, void* const* kv8_pools, const int32_t* block_table, int prefix_len,
+                         const int32_t* branch_lens, int n_branches, const int32_t* parents, int n_children, const int32_t* page_refs,
+                         int32_t* new_table, int32_t* new_lens, int32_t* new_refs);
+TTS_API int tts_kv8_compact(tts_ctx* ctx, int n_layers, void* const* kv8_pools, const int32_t* block_table, int n_branches,
+                            const int32_t* page_refs, int32_t* new_table, int32_t* new_refs, int32_t* page_map, int32_t* n_used);
+
+/*
+ * Beam search over the branches of a question (Section 3.2's branches, continued by score instead of independently): which branches go
+ * on, with which token, and their states in the new order.
+ *   tts_beam_select  for each of n_groups questions, the n_select continuations with the largest
+ *                        score = beam_scores[r] + logits[r][x] - log sum_y exp(logits[r][y])
+ *                    over its beams r = g * n_beams .. g * n_beams + n_beams - 1 and all tokens x, in descending order; of equal scores
+ *                    (formed and compared in 64 bits) the lowest beam, then the lowest token, comes first.
+ *                      logits       device  rows of `vocab` bf16 or fp32 (logits_dtype), row_stride elements from row to row; any alignment
+ *                                           of their type, 16-byte aligned rows are read faster.  -infinity rules a token out
+ *                      beam_scores  device  [rows] fp32: the beams' sums of logarithms so far.  A beam whose score is not finite is no beam
+ *                      finished     device  [rows] i32 or NULL: a beam with a value != 0 is not continued but stays in the race as it is, with
+ *                                           pad_token (0 <= pad_token < vocab) and its score unchanged; its logits are not read
+ *                      parents      device  [n_groups][n_select] i32: the row that was continued, ready for tts_kv_fork,
+ *                                           tts_kv8_fork and tts_beam_reorder, which take questions and their branches in this order
+ *                      tokens, scores  device  [n_groups][n_select] i32, fp32
+ *                    Where a question has fewer candidates, the places behind them get parents = tokens = -1, scores = -infinity.  A row with a
+ *                    NaN or +infinity among its logits, or nothing but -infinity, has no candidate.
+ *                    n_beams * n_select <= 8192 and n_beams * vocab < 2^31 (TTS_ERR_UNSUPPORTED).
+ *   tts_beam_reserve allocates what tts_beam_select needs for up to max_rows rows (n_groups * n_beams, <= cfg.max_branches) and max_select
+ *                    (<= 128) continuations per question.  Call it once per context; a later call with smaller or equal numbers returns
+ *                    TTS_OK, with a larger one TTS_ERR_INVALID.  Not inside a stream capture.  The context's calls of tts_beam_select share that
+ *                    memory: order them on the GPU.
+ *   tts_beam_reorder dst[s][i] = src[s][parents[i]] for n_states (1..128) arrays of rows (token histories, hidden states, dense caches of
+ *                    a draft model): src[s] has n_rows rows of row_bytes[s] bytes, dst[s] n_children.  src, dst, row_bytes are host arrays, their
+ *                    entries device pointers of any alignment (rows of whole 16-byte units move fastest).  A parent of -1 leaves the row of
+ *                    dst as it was; one outside the rows does so too and raises TTS_ERR_DEVICE_BOUNDS.
+ * TTS_ERR_INVALID for null or misaligned pointers, sizes outside what was reserved, and results that overlap anything else.
+ */
+TTS_API int tts_beam_reserve(tts_ctx* ctx, int max_rows, int max_select);
+TTS_API int tts_beam_select(tts_ctx* ctx, const void* logits, int logits_dtype, int64_t row_stride, int vocab, const float* beam_scores,
+                            const int32_t* finished, int pad_token, int n_groups, int n_beams, int n_select, int32_t* parents,
+                            int32_t* tokens, float* scores);
+TTS_API int tts_beam_reorder(tts_ctx* ctx, int n_states, const void* const* src, void* const* dst, const int64_t* row_bytes,
+                             const int32_t* parents, int n_rows, int n_children);
 
 /*
  * One whole verify step from HOST buffers (the end-to-end path): for each of n_layers layers,

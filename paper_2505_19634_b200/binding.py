@@ -17,6 +17,8 @@ _LIB_PATH = _PKG / "libtts_b200.so"
 MASK_CAUSAL, MASK_TREE = 0, 1
 OUT_BF16, OUT_FP32 = 0, 1
 LOGITS_BF16, LOGITS_FP32 = 0, 1
+KV8_E4M3, KV8_INT8 = 0, 1
+KV8_RECORD = 4224
 ATTN_AUTO, ATTN_SIMT, ATTN_TCGEN05, ATTN_TCGEN05_TOKEN_MAJOR, ATTN_TCGEN05_ROW_MAJOR = 0, 1, 2, 3, 4
 
 EXPORTED_SYMBOLS = (
@@ -26,6 +28,8 @@ EXPORTED_SYMBOLS = (
     "tts_last_cuda_error", "tts_launch_count", "tts_strerror", "tts_verify_step_host",
     "tts_profile_enable", "tts_profile_read", "tts_debug_wait_timeout", "tts_verify_attn_noalloc", "tts_kv_append", "tts_kv_rollback", "tts_accept_tree",
     "tts_chunk_reserve", "tts_chunk_attn", "tts_kv_append_rope", "tts_kv_copy_pages", "tts_kv_fork", "tts_kv_grow", "tts_kv_free", "tts_kv_compact",
+    "tts_kv8_append", "tts_kv8_read", "tts_kv8_attn", "tts_kv8_copy_pages", "tts_kv8_fork", "tts_kv8_compact",
+    "tts_beam_reserve", "tts_beam_select", "tts_beam_reorder",
 )
 
 
@@ -72,6 +76,29 @@ class TtsPools:
         self.v = (c_void_p * self.n_layers)(*[_ptr(x).value for x in v_pools])
 
 
+class TtsKv8Pools:
+    """The 8-bit pools of all layers, one per layer, as the page calls take them."""
+
+    def __init__(self, pools: Sequence):
+        self.n_layers = len(pools)
+        self._alive = list(pools)
+        self.p = (c_void_p * self.n_layers)(*[_ptr(x).value for x in pools])
+
+
+class TtsStates:
+    """Arrays of rows that follow the beams: src[s] and dst[s] (tensors or addresses; it keeps the tensors alive) with rows of
+    row_bytes[s] bytes."""
+
+    def __init__(self, src: Sequence, dst: Sequence, row_bytes: Sequence[int]):
+        if not len(src) == len(dst) == len(row_bytes):
+            raise ValueError("as many sources as targets and row sizes")
+        self.n = len(src)
+        self._alive = (list(src), list(dst))
+        self.src = (c_void_p * self.n)(*[_ptr(x).value for x in src])
+        self.dst = (c_void_p * self.n)(*[_ptr(x).value for x in dst])
+        self.row_bytes = (c_int64 * self.n)(*row_bytes)
+
+
 _TASK_FN = ctypes.CFUNCTYPE(c_double, c_int, c_int, c_void_p)
 _lib: Optional[ctypes.CDLL] = None
 
@@ -116,6 +143,15 @@ def load_library() -> ctypes.CDLL:
     lib.tts_kv_grow.argtypes = [vp, vp, c_int, vp, vp, c_int, vp]
     lib.tts_kv_free.argtypes = [vp, vp, vp, vp, c_int, vp]
     lib.tts_kv_compact.argtypes = [vp, c_int, pp, pp, vp, c_int, vp, vp, vp, vp, vp]
+    lib.tts_kv8_append.argtypes = [vp, c_int, vp, vp, i64, vp, vp, i64, vp, vp, vp, c_int, vp, vp, c_int, c_int, vp]
+    lib.tts_kv8_read.argtypes = [vp, c_int, vp, vp, vp, c_int, vp, vp, c_int]
+    lib.tts_kv8_attn.argtypes = [vp, c_int, vp, i64, vp, vp, c_int, vp, vp, c_int, c_int, vp, vp]
+    lib.tts_kv8_copy_pages.argtypes = [vp, c_int, pp, vp, vp, c_int]
+    lib.tts_kv8_fork.argtypes = [vp, c_int, pp, vp, c_int, vp, c_int, vp, c_int, vp, vp, vp, vp]
+    lib.tts_kv8_compact.argtypes = [vp, c_int, pp, vp, c_int, vp, vp, vp, vp, vp]
+    lib.tts_beam_reserve.argtypes = [vp, c_int, c_int]
+    lib.tts_beam_select.argtypes = [vp, vp, c_int, i64, c_int, vp, vp, c_int, c_int, c_int, c_int, vp, vp, vp]
+    lib.tts_beam_reorder.argtypes = [vp, c_int, pp, pp, POINTER(c_int64), vp, c_int, c_int]
     lib.tts_majority_vote.argtypes = [POINTER(c_int64), POINTER(c_float), c_int, POINTER(c_int64), POINTER(c_int)]
     lib.tts_confidence_max.argtypes = lib.tts_majority_vote.argtypes
     lib.tts_greedy_search.argtypes = [_TASK_FN, vp, POINTER(TtsSearchLimits), POINTER(c_int), POINTER(c_int),
@@ -328,6 +364,62 @@ class TtsContext:
                                       _addr(new_table), _addr(new_refs), _addr(page_map), _addr(n_used))
         if rc:
             self._check(rc, "tts_kv_compact")
+
+    def tts_kv8_append(self, format: int, rope: Optional[TtsRope], q, q_row_stride: int, k, v, kv_row_stride: int, positions, kv8_pages, block_table,
+                       prefix_len: int, branch_lens, row_start, n_branches: int, total_rows: int, q_out):
+        """rope, q, positions and q_out may all be None: keys are stored as they come."""
+        rc = self._lib.tts_kv8_append(self._h, format, rope and rope.address, _addr(q), q_row_stride, _addr(k), _addr(v), kv_row_stride,
+                                      _addr(positions), _addr(kv8_pages), _addr(block_table), prefix_len, _addr(branch_lens), _addr(row_start),
+                                      n_branches, total_rows, _addr(q_out))
+        if rc:
+            self._check(rc, "tts_kv8_append")
+
+    def tts_kv8_read(self, format: int, kv8_pages, src_pages, dst_pages, n_pages: int, k_pages, v_pages, num_dst_pages: int):
+        rc = self._lib.tts_kv8_read(self._h, format, _addr(kv8_pages), _addr(src_pages), _addr(dst_pages), n_pages, _addr(k_pages), _addr(v_pages),
+                                    num_dst_pages)
+        if rc:
+            self._check(rc, "tts_kv8_read")
+
+    def tts_kv8_attn(self, format: int, q, q_row_stride: int, kv8_pages, block_table, prefix_len: int, branch_lens, tree_parents, n_branches: int,
+                     rows_per_branch: int, out, lse=None):
+        """tree_parents None: a chain."""
+        rc = self._lib.tts_kv8_attn(self._h, format, _addr(q), q_row_stride, _addr(kv8_pages), _addr(block_table), prefix_len, _addr(branch_lens),
+                                    _addr(tree_parents), n_branches, rows_per_branch, _addr(out), _addr(lse))
+        if rc:
+            self._check(rc, "tts_kv8_attn")
+
+    def tts_kv8_copy_pages(self, pools: TtsKv8Pools, src_pages, dst_pages, n_copies: int):
+        rc = self._lib.tts_kv8_copy_pages(self._h, pools.n_layers, pools.p, _addr(src_pages), _addr(dst_pages), n_copies)
+        if rc:
+            self._check(rc, "tts_kv8_copy_pages")
+
+    def tts_kv8_fork(self, pools: TtsKv8Pools, block_table, prefix_len: int, branch_lens, n_branches: int, parents, n_children: int, page_refs,
+                     new_table, new_lens, new_refs):
+        rc = self._lib.tts_kv8_fork(self._h, pools.n_layers, pools.p, _addr(block_table), prefix_len, _addr(branch_lens), n_branches, _addr(parents),
+                                    n_children, _addr(page_refs), _addr(new_table), _addr(new_lens), _addr(new_refs))
+        if rc:
+            self._check(rc, "tts_kv8_fork")
+
+    def tts_kv8_compact(self, pools: TtsKv8Pools, block_table, n_branches: int, page_refs, new_table, new_refs, page_map, n_used):
+        rc = self._lib.tts_kv8_compact(self._h, pools.n_layers, pools.p, _addr(block_table), n_branches, _addr(page_refs), _addr(new_table),
+                                       _addr(new_refs), _addr(page_map), _addr(n_used))
+        if rc:
+            self._check(rc, "tts_kv8_compact")
+
+    def tts_beam_reserve(self, max_rows: int, max_select: int):
+        self._check(self._lib.tts_beam_reserve(self._h, int(max_rows), int(max_select)), "tts_beam_reserve")
+
+    def tts_beam_select(self, logits, logits_dtype: int, row_stride: int, vocab: int, beam_scores, finished, pad_token: int, n_groups: int, n_beams: int,
+                        n_select: int, parents, tokens, scores):
+        rc = self._lib.tts_beam_select(self._h, _addr(logits), logits_dtype, row_stride, vocab, _addr(beam_scores), _addr(finished), pad_token,
+                                       n_groups, n_beams, n_select, _addr(parents), _addr(tokens), _addr(scores))
+        if rc:
+            self._check(rc, "tts_beam_select")
+
+    def tts_beam_reorder(self, states: TtsStates, parents, n_rows: int, n_children: int):
+        rc = self._lib.tts_beam_reorder(self._h, states.n, states.src, states.dst, states.row_bytes, _addr(parents), n_rows, n_children)
+        if rc:
+            self._check(rc, "tts_beam_reorder")
 
     def tts_last_status(self) -> int:
         st = c_int(0)

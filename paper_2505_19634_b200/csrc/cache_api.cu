@@ -6,7 +6,9 @@
 #include <functional>
 #include <initializer_list>
 
+#include "api_checks.cuh"
 #include "chunk_attn.cuh"
+#include "kv8.cuh"
 #include "launch.cuh"
 #include "tts_internal.cuh"
 
@@ -14,45 +16,15 @@ using namespace tts;
 
 namespace {
 
-inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
-
-int finish(Ctx* c, cudaError_t e, int launches) {
-    if (e != cudaSuccess) { c->last_cuda_error = (int)e; return TTS_ERR_CUDA; }
-    c->launches += launches;
-    return TTS_OK;
-}
-
-constexpr int kMaxBlocks = 1 << 26;                    // 2^30 tokens per branch: token numbers and their sums fit 32 bits
-
-bool branches_ok(const Ctx* c, const int32_t* block_table, int prefix_len, int n_branches) {
-    const tts_config& f = c->cfg;
-    return block_table && aligned4(block_table) && f.max_blocks_per_branch <= kMaxBlocks && n_branches >= 1 && n_branches <= f.max_branches && prefix_len >= 0 &&
-           prefix_len % f.page_size == 0 && prefix_len / f.page_size <= f.max_blocks_per_branch;
-}
-
-// Both arrays as [p, p + bytes): do they share memory?
-bool overlap(const void* a, size_t na, const void* b, size_t nb) {
-    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-    return x < y + nb && y < x + na;
-}
-
-struct Span { const void* at; size_t bytes; };
-// Does `written` share memory with one of the others?
-bool clash(const Span& written, std::initializer_list<Span> others) {
-    for (const Span& o : others) if (overlap(written.at, written.bytes, o.at, o.bytes)) return true;
-    return false;
-}
-size_t pool_bytes(const tts_config& f) { return (size_t)f.num_pages * f.n_kv_heads * kPage * kHeadDim * 2; }
-size_t table_bytes(const tts_config& f, int n) { return (size_t)n * f.max_blocks_per_branch * 4; }
-
 // What the page calls copy: pools that overlap without being the same one, or that share memory with one of the arrays,
 // would be read after they are written.
-bool pools_clash(const PagePools& pools, size_t bytes, std::initializer_list<Span> arrays) {
-    const int n = 2 * pools.n_layers, half = pools.n_layers;
+bool pools_clash(const tts_config& f, const PagePools& pools, std::initializer_list<Span> arrays) {
+    const int n = pools.n_pools, half = n / 2;
+    const size_t bytes = (size_t)f.num_pages * f.n_kv_heads * pools.tile_bytes;
     const std::less<const void*> before;
     const void* kv[2 * kMaxLayers], *at[2 * kMaxLayers];
     for (int i = 0; i < half; ++i) { kv[i] = pools.p[2 * i]; kv[half + i] = pools.p[2 * i + 1]; }
+    if (n > 2 * half) kv[n - 1] = pools.p[n - 1];
     // (a program that allocates its layers in order has two runs in order: 128 pools take 0.3 us to merge, 2 to sort)
     if (!std::is_sorted(kv, kv + half, before)) std::sort(kv, kv + half, before);
     if (!std::is_sorted(kv + half, kv + n, before)) std::sort(kv + half, kv + n, before);
@@ -69,10 +41,21 @@ bool pools_clash(const PagePools& pools, size_t bytes, std::initializer_list<Spa
 bool pools_from(int n_layers, void* const* k_pools, void* const* v_pools, PagePools* out) {
     if (n_layers < 1 || n_layers > kMaxLayers || !k_pools || !v_pools) return false;
     memset(out, 0, sizeof *out);
-    out->n_layers = n_layers;
+    out->n_pools = 2 * n_layers; out->tile_bytes = kPage * kHeadDim * 2;
     for (int i = 0; i < n_layers; ++i) {
         if (!k_pools[i] || !v_pools[i] || !aligned16(k_pools[i]) || !aligned16(v_pools[i])) return false;
         out->p[2 * i] = k_pools[i]; out->p[2 * i + 1] = v_pools[i];
+    }
+    return true;
+}
+
+bool pools_from_kv8(int n_layers, void* const* pools, PagePools* out) {
+    if (n_layers < 1 || n_layers > kMaxLayers || !pools) return false;
+    memset(out, 0, sizeof *out);
+    out->n_pools = n_layers; out->tile_bytes = kKv8Record;
+    for (int i = 0; i < n_layers; ++i) {
+        if (!pools[i] || !aligned16(pools[i])) return false;
+        out->p[i] = pools[i];
     }
     return true;
 }
@@ -91,13 +74,73 @@ PageWork page_work(const Ctx* c) {
     return w;
 }
 
+// The page calls over whatever pools there are.
+int copy_pages(Ctx* c, const PagePools& pools, const int32_t* src_pages, const int32_t* dst_pages, int n_copies) {
+    if (!src_pages || !dst_pages || n_copies < 0 || !aligned4(src_pages) || !aligned4(dst_pages)) return TTS_ERR_INVALID;
+    if (n_copies == 0) return TTS_OK;
+    if (pools_clash(c->cfg, pools, {{src_pages, (size_t)n_copies * 4}, {dst_pages, (size_t)n_copies * 4}})) return TTS_ERR_INVALID;
+    const OnDevice on(c->device);
+    if (on.error() != cudaSuccess) return finish(c, on.error(), 0);
+    return finish(c, launch_copy_pages(pools, src_pages, dst_pages, n_copies, c->cfg.n_kv_heads, c->cfg.num_pages, c->n_sms, c->d_status, c->stream), 1);
+}
+
+int fork_pages(Ctx* c, const PagePools& pools, const int32_t* block_table, int prefix_len, const int32_t* branch_lens, int n_branches,
+               const int32_t* parents, int n_children, const int32_t* page_refs, int32_t* new_table, int32_t* new_lens, int32_t* new_refs) {
+    if (!branch_lens || !parents || !page_refs || !new_table || !new_lens || !new_refs) return TTS_ERR_INVALID;
+    if (!branches_ok(c, block_table, prefix_len, n_branches) || n_children < 1 || n_children > c->cfg.max_branches) return TTS_ERR_INVALID;
+    if (!aligned4(branch_lens) || !aligned4(parents) || !aligned16(page_refs) || !aligned4(new_table) || !aligned4(new_lens) || !aligned16(new_refs))
+        return TTS_ERR_INVALID;
+    const tts_config& f = c->cfg;
+    // children are written while their parents' rows are read
+    const Span table{block_table, table_bytes(f, n_branches)}, lens{branch_lens, (size_t)n_branches * 4}, who{parents, (size_t)n_children * 4},
+        refs{page_refs, (size_t)f.num_pages * 4}, out_table{new_table, table_bytes(f, n_children)}, out_lens{new_lens, (size_t)n_children * 4},
+        out_refs{new_refs, refs.bytes};
+    if (clash(out_table, {table, lens, who, refs, out_lens, out_refs}) || clash(out_lens, {table, lens, who, refs, out_refs}) ||
+        clash(out_refs, {table, lens, who}) || (page_refs != new_refs && clash(out_refs, {refs})) ||
+        pools_clash(f, pools, {table, lens, who, refs, out_table, out_lens, out_refs}))
+        return TTS_ERR_INVALID;
+    c->plan_explicit = 0;
+    const OnDevice on(c->device);
+    if (on.error() != cudaSuccess) return finish(c, on.error(), 0);
+    return finish(c, launch_fork(pools, block_table, f.max_blocks_per_branch, prefix_len, branch_lens, n_branches, parents, n_children, page_refs,
+                                 new_table, new_lens, new_refs, f.n_kv_heads, f.num_pages, c->n_sms, page_work(c), c->d_status, c->stream), 2);
+}
+
+int compact_pages(Ctx* c, const PagePools& pools, const int32_t* block_table, int n_branches, const int32_t* page_refs, int32_t* new_table,
+                  int32_t* new_refs, int32_t* page_map, int32_t* n_used) {
+    if (!page_refs || !new_table || !new_refs || !page_map || !n_used || !branches_ok(c, block_table, 0, n_branches)) return TTS_ERR_INVALID;
+    if (!aligned16(page_refs) || !aligned4(new_table) || !aligned16(new_refs) || !aligned16(page_map) || !aligned4(n_used)) return TTS_ERR_INVALID;
+    const tts_config& f = c->cfg;
+    const Span table{block_table, table_bytes(f, n_branches)}, refs{page_refs, (size_t)f.num_pages * 4}, out_table{new_table, table.bytes},
+        out_refs{new_refs, refs.bytes}, map{page_map, refs.bytes}, used{n_used, 4};
+    if ((block_table != new_table && clash(out_table, {table})) || (page_refs != new_refs && clash(out_refs, {refs})) ||
+        clash(out_table, {refs, out_refs}) || clash(out_refs, {table}) || clash(map, {table, refs, out_table, out_refs, used}) ||
+        clash(used, {table, refs, out_table, out_refs}) || pools_clash(f, pools, {table, refs, out_table, out_refs, map, used}))
+        return TTS_ERR_INVALID;
+    c->plan_explicit = 0;
+    const OnDevice on(c->device);
+    if (on.error() != cudaSuccess) return finish(c, on.error(), 0);
+    return finish(c, launch_compact(pools, block_table, f.max_blocks_per_branch, n_branches, page_refs, new_table, new_refs, page_map, n_used,
+                                    f.n_kv_heads, f.num_pages, c->n_sms, page_work(c), c->d_status, c->stream), 2);
+}
+
 }  // namespace
 
 namespace tts {
 
 cudaError_t cache_alloc(Ctx* c) {
-    const size_t nb = c->cfg.max_branches, np = c->cfg.num_pages;
-    return cudaMalloc(&c->page_work, 16 + nb * sizeof(int4) + align16(nb * 4) + 2 * align16(np * 4));
+    const tts_config& f = c->cfg;
+    const size_t nb = f.max_branches, np = f.num_pages;
+    cudaError_t e = cudaMalloc(&c->page_work, 16 + nb * sizeof(int4) + align16(nb * 4) + 2 * align16(np * 4));
+    // attention over the 8-bit cache: two partial results for each CTA, a counter for each (branch, KV head, row block)
+    const size_t slots = 2 * (size_t)c->n_sms * kKv8MaxRows;
+    const size_t items = nb * f.n_kv_heads * ceil_div(f.max_rows_per_branch * (f.n_q_heads / f.n_kv_heads), kKv8MaxRows);
+    if (e == cudaSuccess) e = cudaMalloc(&c->kv8_part_o, slots * kHeadDim * sizeof(float));
+    if (e == cudaSuccess) e = cudaMalloc(&c->kv8_part_ml, slots * sizeof(float2));
+    if (e == cudaSuccess) e = cudaMalloc(&c->kv8_arrived, items * sizeof(unsigned));
+    if (e == cudaSuccess) e = cudaMemset(c->kv8_arrived, 0, items * sizeof(unsigned));
+    if (e == cudaSuccess) e = cudaStreamSynchronize(cudaStreamLegacy);       // before work on a stream that does not wait for it
+    return e;
 }
 
 cudaError_t cache_reset(Ctx* c) {
@@ -115,6 +158,8 @@ cudaError_t cache_disturb(Ctx* c) {
 
 void cache_release(Ctx* c) {
     cudaFree(c->page_work);
+    cudaFree(c->kv8_part_o); cudaFree(c->kv8_part_ml); cudaFree(c->kv8_arrived); cudaFree(c->beam_work);
+    c->kv8_part_o = nullptr; c->kv8_part_ml = nullptr; c->kv8_arrived = nullptr; c->beam_work = nullptr; c->beam_rows = 0;
     cudaFree(c->chunk_head); cudaFree(c->chunk_pieces); cudaFree(c->chunk_arrived);
     cudaFree(c->chunk_part_o); cudaFree(c->chunk_part_ml);
     c->page_work = nullptr; c->chunk_head = nullptr; c->chunk_pieces = nullptr; c->chunk_arrived = nullptr;
@@ -247,41 +292,18 @@ int tts_kv_append_rope(tts_ctx* ctx, const tts_rope* rope, const void* q, int64_
 
 int tts_kv_copy_pages(tts_ctx* ctx, int n_layers, void* const* k_pools, void* const* v_pools, const int32_t* src_pages, const int32_t* dst_pages,
                       int n_copies) {
-    Ctx* c = reinterpret_cast<Ctx*>(ctx);
     PagePools pools;
-    if (!c || !src_pages || !dst_pages || n_copies < 0 || !aligned4(src_pages) || !aligned4(dst_pages)) return TTS_ERR_INVALID;
-    if (!pools_from(n_layers, k_pools, v_pools, &pools)) return TTS_ERR_INVALID;
-    if (n_copies == 0) return TTS_OK;
-    if (pools_clash(pools, pool_bytes(c->cfg), {{src_pages, (size_t)n_copies * 4}, {dst_pages, (size_t)n_copies * 4}})) return TTS_ERR_INVALID;
-    const OnDevice on(c->device);
-    if (on.error() != cudaSuccess) return finish(c, on.error(), 0);
-    return finish(c, launch_copy_pages(pools, src_pages, dst_pages, n_copies, c->cfg.n_kv_heads, c->cfg.num_pages, c->n_sms, c->d_status, c->stream), 1);
+    if (!ctx || !pools_from(n_layers, k_pools, v_pools, &pools)) return TTS_ERR_INVALID;
+    return copy_pages(reinterpret_cast<Ctx*>(ctx), pools, src_pages, dst_pages, n_copies);
 }
 
 int tts_kv_fork(tts_ctx* ctx, int n_layers, void* const* k_pools, void* const* v_pools, const int32_t* block_table, int prefix_len,
                 const int32_t* branch_lens, int n_branches, const int32_t* parents, int n_children, const int32_t* page_refs,
                 int32_t* new_table, int32_t* new_lens, int32_t* new_refs) {
-    Ctx* c = reinterpret_cast<Ctx*>(ctx);
     PagePools pools;
-    if (!c || !branch_lens || !parents || !page_refs || !new_table || !new_lens || !new_refs) return TTS_ERR_INVALID;
-    if (!branches_ok(c, block_table, prefix_len, n_branches) || n_children < 1 || n_children > c->cfg.max_branches) return TTS_ERR_INVALID;
-    if (!aligned4(branch_lens) || !aligned4(parents) || !aligned16(page_refs) || !aligned4(new_table) || !aligned4(new_lens) || !aligned16(new_refs))
-        return TTS_ERR_INVALID;
-    if (!pools_from(n_layers, k_pools, v_pools, &pools)) return TTS_ERR_INVALID;
-    const tts_config& f = c->cfg;
-    // children are written while their parents' rows are read
-    const Span table{block_table, table_bytes(f, n_branches)}, lens{branch_lens, (size_t)n_branches * 4}, who{parents, (size_t)n_children * 4},
-        refs{page_refs, (size_t)f.num_pages * 4}, out_table{new_table, table_bytes(f, n_children)}, out_lens{new_lens, (size_t)n_children * 4},
-        out_refs{new_refs, refs.bytes};
-    if (clash(out_table, {table, lens, who, refs, out_lens, out_refs}) || clash(out_lens, {table, lens, who, refs, out_refs}) ||
-        clash(out_refs, {table, lens, who}) || (page_refs != new_refs && clash(out_refs, {refs})) ||
-        pools_clash(pools, pool_bytes(f), {table, lens, who, refs, out_table, out_lens, out_refs}))
-        return TTS_ERR_INVALID;
-    c->plan_explicit = 0;
-    const OnDevice on(c->device);
-    if (on.error() != cudaSuccess) return finish(c, on.error(), 0);
-    return finish(c, launch_fork(pools, block_table, f.max_blocks_per_branch, prefix_len, branch_lens, n_branches, parents, n_children, page_refs,
-                                 new_table, new_lens, new_refs, f.n_kv_heads, f.num_pages, c->n_sms, page_work(c), c->d_status, c->stream), 2);
+    if (!ctx || !pools_from(n_layers, k_pools, v_pools, &pools)) return TTS_ERR_INVALID;
+    return fork_pages(reinterpret_cast<Ctx*>(ctx), pools, block_table, prefix_len, branch_lens, n_branches, parents, n_children, page_refs, new_table,
+                      new_lens, new_refs);
 }
 
 int tts_kv_grow(tts_ctx* ctx, int32_t* block_table, int prefix_len, int32_t* branch_lens, const int32_t* n_new, int n_branches, int32_t* page_refs) {
@@ -314,23 +336,32 @@ int tts_kv_free(tts_ctx* ctx, int32_t* block_table, int32_t* branch_lens, const 
 
 int tts_kv_compact(tts_ctx* ctx, int n_layers, void* const* k_pools, void* const* v_pools, const int32_t* block_table, int n_branches,
                    const int32_t* page_refs, int32_t* new_table, int32_t* new_refs, int32_t* page_map, int32_t* n_used) {
-    Ctx* c = reinterpret_cast<Ctx*>(ctx);
     PagePools pools;
-    if (!c || !page_refs || !new_table || !new_refs || !page_map || !n_used || !branches_ok(c, block_table, 0, n_branches)) return TTS_ERR_INVALID;
-    if (!aligned16(page_refs) || !aligned4(new_table) || !aligned16(new_refs) || !aligned16(page_map) || !aligned4(n_used)) return TTS_ERR_INVALID;
-    if (!pools_from(n_layers, k_pools, v_pools, &pools)) return TTS_ERR_INVALID;
-    const tts_config& f = c->cfg;
-    const Span table{block_table, table_bytes(f, n_branches)}, refs{page_refs, (size_t)f.num_pages * 4}, out_table{new_table, table.bytes},
-        out_refs{new_refs, refs.bytes}, map{page_map, refs.bytes}, used{n_used, 4};
-    if ((block_table != new_table && clash(out_table, {table})) || (page_refs != new_refs && clash(out_refs, {refs})) ||
-        clash(out_table, {refs, out_refs}) || clash(out_refs, {table}) || clash(map, {table, refs, out_table, out_refs, used}) ||
-        clash(used, {table, refs, out_table, out_refs}) || pools_clash(pools, pool_bytes(f), {table, refs, out_table, out_refs, map, used}))
-        return TTS_ERR_INVALID;
-    c->plan_explicit = 0;
-    const OnDevice on(c->device);
-    if (on.error() != cudaSuccess) return finish(c, on.error(), 0);
-    return finish(c, launch_compact(pools, block_table, f.max_blocks_per_branch, n_branches, page_refs, new_table, new_refs, page_map, n_used,
-                                    f.n_kv_heads, f.num_pages, c->n_sms, page_work(c), c->d_status, c->stream), 2);
+    if (!ctx || !pools_from(n_layers, k_pools, v_pools, &pools)) return TTS_ERR_INVALID;
+    return compact_pages(reinterpret_cast<Ctx*>(ctx), pools, block_table, n_branches, page_refs, new_table, new_refs, page_map, n_used);
+}
+
+int tts_kv8_copy_pages(tts_ctx* ctx, int n_layers, void* const* kv8_pools, const int32_t* src_pages, const int32_t* dst_pages,
+                      int n_copies) {
+    PagePools pools;
+    if (!ctx || !pools_from_kv8(n_layers, kv8_pools, &pools)) return TTS_ERR_INVALID;
+    return copy_pages(reinterpret_cast<Ctx*>(ctx), pools, src_pages, dst_pages, n_copies);
+}
+
+int tts_kv8_fork(tts_ctx* ctx, int n_layers, void* const* kv8_pools, const int32_t* block_table, int prefix_len,
+                const int32_t* branch_lens, int n_branches, const int32_t* parents, int n_children, const int32_t* page_refs,
+                int32_t* new_table, int32_t* new_lens, int32_t* new_refs) {
+    PagePools pools;
+    if (!ctx || !pools_from_kv8(n_layers, kv8_pools, &pools)) return TTS_ERR_INVALID;
+    return fork_pages(reinterpret_cast<Ctx*>(ctx), pools, block_table, prefix_len, branch_lens, n_branches, parents, n_children, page_refs, new_table,
+                      new_lens, new_refs);
+}
+
+int tts_kv8_compact(tts_ctx* ctx, int n_layers, void* const* kv8_pools, const int32_t* block_table, int n_branches,
+                   const int32_t* page_refs, int32_t* new_table, int32_t* new_refs, int32_t* page_map, int32_t* n_used) {
+    PagePools pools;
+    if (!ctx || !pools_from_kv8(n_layers, kv8_pools, &pools)) return TTS_ERR_INVALID;
+    return compact_pages(reinterpret_cast<Ctx*>(ctx), pools, block_table, n_branches, page_refs, new_table, new_refs, page_map, n_used);
 }
 
 }  // extern "C"

@@ -4,9 +4,9 @@
 // pages are handed out lowest id first, to branches in their order.
 //
 // What bounds these calls: the page copies are HBM traffic (one page of the 32B shape is 4 MiB over 64
-// layers' K and V); the integer work on tables and reference counts is latency (one CTA that scans the
-// counts, then one kernel over table rows and copies).  Copies are cut into 4 KiB page-head tiles, one warp
-// each, eight 16-byte loads per lane in flight before the first store, so that one page of a few layers
+// layers' K and V, half of it in 8 bits); the integer work on tables and reference counts is latency (one CTA that scans the
+// counts, then one kernel over table rows and copies).  Copies are cut into page-head tiles of 4 KiB (4224 bytes
+// in the 8-bit cache), one warp each, eight 16-byte loads per lane in flight before the first store, so that one page of a few layers
 // already spreads over many SMs.
 #include "launch.cuh"
 #include "tts_internal.cuh"
@@ -19,8 +19,7 @@ namespace {
 
 constexpr int kMaxScanThreads = 1024;
 constexpr int kPerThread = 16;                         // reference counts a thread looks at per step of a scan
-constexpr int kTileBytes = kPage * kHeadDim * 2;       // one page of one KV head: 4 KiB
-constexpr int kTileChunks = kTileBytes / 16 / 32;      // 16-byte chunks of a tile per lane
+constexpr int kTileChunks = kPage * kHeadDim * 2 / 16 / 32;      // 16-byte chunks of a 4 KiB tile per lane
 constexpr int kCopyThreads = 256;
 
 template <typename T>
@@ -94,30 +93,33 @@ __device__ __forceinline__ bool give_back(int32_t* refs, int page, int num_pages
     return false;
 }
 
-// One 4 KiB tile by one warp.
-__device__ __forceinline__ void copy_tile(const uint4* src, uint4* dst, int lane) {
-    uint4 x[kTileChunks];
+// One tile by one warp: 4 KiB, and `rest` (0 to 32) chunks of 16 bytes behind them.
+__device__ __forceinline__ void copy_tile(const uint4* src, uint4* dst, int rest, int lane) {
+    uint4 x[kTileChunks + 1];
 #pragma unroll
     for (int i = 0; i < kTileChunks; ++i) x[i] = __ldcs(src + i * 32 + lane);
+    if (lane < rest) x[kTileChunks] = __ldcs(src + kTileChunks * 32 + lane);
 #pragma unroll
     for (int i = 0; i < kTileChunks; ++i) __stcs(dst + i * 32 + lane, x[i]);
+    if (lane < rest) __stcs(dst + kTileChunks * 32 + lane, x[kTileChunks]);
 }
 
 // Copies list entry k (src[k] -> dst[k]) in all pools, for k < n; a negative page on either side is skipped.
 __device__ void copy_pages(const PagePools& pools, const int32_t* src, const int32_t* dst, int n, int Hkv, int num_pages,
                            int32_t* status, int worker, int n_workers) {
     const int lane = threadIdx.x & 31;
-    const int per_page = 2 * pools.n_layers * Hkv;      // tiles of one page: (K or V, layer, head)
+    const int per_page = pools.n_pools * Hkv;           // tiles of one page: (K or V, layer, head)
+    const int tile = pools.tile_bytes, rest = tile / 16 - kTileChunks * 32;
     const long total = (long)n * per_page;
     for (long w = worker; w < total; w += n_workers) {
-        const int k = (int)(w / per_page), rest = (int)(w - (long)k * per_page);
-        const int pool = rest / Hkv, h = rest - pool * Hkv;
+        const int k = (int)(w / per_page), within = (int)(w - (long)k * per_page);
+        const int pool = within / Hkv, h = within - pool * Hkv;
         const int s = src[k], d = dst[k];
         if (s < 0 || d < 0 || s == d) continue;
         if (s >= num_pages || d >= num_pages) { if (lane == 0) atomicMin(status, (int)TTS_ERR_DEVICE_BOUNDS); continue; }
         char* base = static_cast<char*>(pools.p[pool]);
-        copy_tile(reinterpret_cast<const uint4*>(base + ((size_t)s * Hkv + h) * kTileBytes),
-                  reinterpret_cast<uint4*>(base + ((size_t)d * Hkv + h) * kTileBytes), lane);
+        copy_tile(reinterpret_cast<const uint4*>(base + ((size_t)s * Hkv + h) * tile),
+                  reinterpret_cast<uint4*>(base + ((size_t)d * Hkv + h) * tile), rest, lane);
     }
 }
 
@@ -398,7 +400,7 @@ compact_kernel(const __grid_constant__ PagePools pools, const int32_t* table, in
 
 // Blocks for n copies: one warp per tile, at most 8 blocks of 8 warps per SM (the register file's worth).
 int copy_blocks(long n, const PagePools& pools, int Hkv, int n_sms) {
-    const long tiles = n * 2 * pools.n_layers * Hkv, blocks = (tiles + kCopyThreads / 32 - 1) / (kCopyThreads / 32);
+    const long tiles = n * pools.n_pools * Hkv, blocks = (tiles + kCopyThreads / 32 - 1) / (kCopyThreads / 32);
     return (int)(blocks < 8l * n_sms ? blocks : 8l * n_sms);
 }
 

@@ -1,5 +1,6 @@
 // Rotary positions on the way into the cache: the queries and keys of ragged chunks of new tokens are
-// rotated, the keys and values go to their page slots, the rotated queries to a dense array.
+// rotated, the keys and values go to their page slots, the rotated queries to a dense array.  The slots are those of
+// a bf16 cache or of the 8-bit one (kv8.cuh), whose codes and scales are formed here from the rotated keys in fp32.
 //
 //   pair i of a head vector x is turned by angle a = positions[axis[i]][row] * inv_freq[i]:
 //       (x_lo, x_hi) -> (x_lo cos a - x_hi sin a, x_lo sin a + x_hi cos a)
@@ -13,6 +14,9 @@
 // needs no exchange between lanes; a lane's eight sines and cosines serve all heads of the row that its
 // warp walks through, sixteen at a time, whose loads are issued before the row's branch, page and angles are
 // looked up.
+#include <type_traits>
+
+#include "kv8.cuh"
 #include "launch.cuh"
 #include "tts_internal.cuh"
 
@@ -22,6 +26,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
+constexpr int kBf16Pages = -1;
 constexpr int kBatch = 4;                              // head vectors that a group of eight lanes has in flight
 
 // Row starts that decrease or leave the rows make a call of which nothing is computed: a row taken for a branch's that
@@ -52,11 +57,40 @@ __device__ __forceinline__ uint4 pack(const float (&x)[8]) {
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// One vector of the 8-bit cache by eight lanes, lane `sub` with its dims 8 sub .. 8 sub + 7 (lo) and 64 above them (hi):
+// scale = max |x| / the largest code, at least 2^-120, and codes x / scale, both divisions correctly rounded.  The largest
+// magnitude is taken on the bits, where a NaN is above every number: a vector with a NaN or an infinity in it gets the
+// scale NaN and codes of zero, so that whatever is read of it shows the fault and nothing else does.
+template <int kFormat>
+__device__ __forceinline__ void store_codes(unsigned char* record, bool is_v, int t, int sub, const float (&lo)[8], const float (&hi)[8], bool store) {
+    int top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, max(__float_as_int(lo[i]) & 0x7fffffff, __float_as_int(hi[i]) & 0x7fffffff));
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const bool fine = top < 0x7f800000;
+    const float scale = fine ? fmaxf(__fdiv_rn(__int_as_float(top), kv8_largest<kFormat>()), kKv8LeastScale) : __int_as_float(0x7fc00000);
+    auto codes = [&](const float (&x)[8]) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = fine ? kv8_encode2<kFormat>(__fdiv_rn(x[2 * i], scale), __fdiv_rn(x[2 * i + 1], scale)) : 0u;
+        return make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
+    };
+    const uint2 a = codes(lo), z = codes(hi);
+    if (!store) return;
+    unsigned char* row = record + (is_v ? kKv8Codes : 0) + t * kHeadDim + 8 * (sub & 1);
+    const int place = kv8_chunk_place(t);
+    *reinterpret_cast<uint2*>(row + 16 * ((sub >> 1) ^ place)) = a;
+    *reinterpret_cast<uint2*>(row + 16 * ((4 + (sub >> 1)) ^ place)) = z;
+    if (sub == 0) reinterpret_cast<float*>(record + 2 * kKv8Codes)[(is_v ? kPage : 0) + t] = scale;
+}
+
 // kMode 0: all 64 pairs, pair i = dims (i, i + 64); 1: neighbours (2i, 2i+1), any number of pairs; 2: pair i =
-// dims (i, i + n_pairs) with fewer than 64 pairs (partners fetched one by one).
+// dims (i, i + n_pairs) with fewer than 64 pairs (partners fetched one by one); 3: nothing is turned (and there are no queries).
+// kFormat: kBf16Pages, or the codes of the 8-bit pool.
 // A warp takes one row and every parts-th group of four head vectors of it; with few rows several warps share
 // a row, so that small calls still fill the GPU.
-template <int kMode>
+template <int kMode, int kFormat>
 __global__ void __launch_bounds__(kThreads)
 append_rope_kernel(const __grid_constant__ RopeParams p) {
     __shared__ double turns[kHeadDim / 2];              // inv_freq / (2 pi)
@@ -132,7 +166,7 @@ append_rope_kernel(const __grid_constant__ RopeParams p) {
         // such pairs); mode 1: chunk sub holds pairs 4 sub .. + 3 and chunk sub + 8 pairs 32 + 4 sub .. + 3.
         // The four groups of lanes need the same eight sines and cosines per `sub`: each works out two.
         float cs[8], sn[8];
-        {
+        if (kMode != 3) {
             float s2[2], c2[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
@@ -147,11 +181,19 @@ append_rope_kernel(const __grid_constant__ RopeParams p) {
         }
         auto store = [&](int h, const uint4& lo, const uint4& hi) {
             const bool is_q = h < p.Hq, is_v = h >= p.Hq + p.Hkv;
-            if (h >= vectors || (!is_q && !store_kv)) return;
+            if (h >= vectors || (!is_q && (kFormat != kBf16Pages || !store_kv))) return;
             uint4* dst = is_q ? reinterpret_cast<uint4*>(p.q_out + ((size_t)row * p.Hq + h) * kHeadDim)
                               : reinterpret_cast<uint4*>((is_v ? p.v_pages : p.k_pages) +
                                                          ((((size_t)page * p.Hkv + h - p.Hq - (is_v ? p.Hkv : 0)) * kPage + (size_t)(tok % kPage)) * kHeadDim));
             dst[sub] = lo; dst[sub + 8] = hi;
+        };
+        // the same of the 8-bit cache: all lanes come here, those without a key or value for the exchange alone
+        auto store_kv8 = [&](int h, const float (&lo)[8], const float (&hi)[8]) {
+            if constexpr (kFormat != kBf16Pages) {
+                const bool is_v = h >= p.Hq + p.Hkv, mine = h >= p.Hq && h < vectors && store_kv;
+                const int head = mine ? h - p.Hq - (is_v ? p.Hkv : 0) : 0;
+                store_codes<kFormat>(p.kv8_pages + ((size_t)(mine ? page : 0) * p.Hkv + head) * kKv8Record, is_v, (int)(tok % kPage), sub, lo, hi, mine);
+            }
         };
         if (kMode == 2) {
             for (int h0 = part * 4; h0 < vectors; h0 += step) {
@@ -159,10 +201,10 @@ append_rope_kernel(const __grid_constant__ RopeParams p) {
                 const bool live = h < vectors;
                 const __nv_bfloat16* src = source(live ? h : 0);
                 uint4 a4 = reinterpret_cast<const uint4*>(src)[sub], z4 = reinterpret_cast<const uint4*>(src)[sub + 8];
+                float lo[8], hi[8];
+                unpack(a4, lo); unpack(z4, hi);
                 if (live && h < p.Hq + p.Hkv) {
                     // this lane writes the same two chunks; each dim's partner is n_pairs away
-                    float lo[8], hi[8];
-                    unpack(a4, lo); unpack(z4, hi);
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
                         float(&x)[8] = half ? hi : lo;
@@ -182,6 +224,7 @@ append_rope_kernel(const __grid_constant__ RopeParams p) {
                 }
                 __syncwarp();                           // the partners have been read before anything is written in place
                 store(h, a4, z4);
+                if (kFormat != kBf16Pages && h0 + 3 >= p.Hq) store_kv8(h, lo, hi);
             }
             continue;
         }
@@ -190,9 +233,9 @@ append_rope_kernel(const __grid_constant__ RopeParams p) {
 #pragma unroll
             for (int i = 0; i < kBatch; ++i) {
                 const int h = h0 + i * step + group;
-                if (h < p.Hq + p.Hkv) {
-                    float lo[8], hi[8];
-                    unpack(lo4[i], lo); unpack(hi4[i], hi);
+                float lo[8], hi[8];
+                unpack(lo4[i], lo); unpack(hi4[i], hi);
+                if (kMode != 3 && h < p.Hq + p.Hkv) {
                     if (kMode == 0) {
 #pragma unroll
                         for (int k = 0; k < 8; ++k) {
@@ -217,6 +260,7 @@ append_rope_kernel(const __grid_constant__ RopeParams p) {
                     lo4[i] = pack(lo); hi4[i] = pack(hi);
                 }
                 store(h, lo4[i], hi4[i]);
+                if (kFormat != kBf16Pages && h0 + i * step + 3 >= p.Hq && h0 + i * step < vectors) store_kv8(h, lo, hi);
             }
         }
     }
@@ -233,9 +277,16 @@ cudaError_t launch_append_rope(RopeParams p, int n_sms, cudaStream_t st) {
     const long warps = (long)p.total_rows * p.parts;
     const long blocks = (warps + kWarps - 1) / kWarps;
     const int grid = (int)(blocks < 16l * n_sms ? blocks : 16l * n_sms);
-    if (p.interleaved) return launch_dependent(append_rope_kernel<1>, grid, kThreads, 0, st, p);
-    if (p.n_pairs == kHeadDim / 2) return launch_dependent(append_rope_kernel<0>, grid, kThreads, 0, st, p);
-    return launch_dependent(append_rope_kernel<2>, grid, kThreads, 0, st, p);
+    auto launch = [&](auto format) {
+        constexpr int kFormat = decltype(format)::value;
+        if constexpr (kFormat != kBf16Pages)
+            if (p.n_pairs == 0) return launch_dependent(append_rope_kernel<3, kFormat>, grid, kThreads, 0, st, p);
+        if (p.interleaved) return launch_dependent(append_rope_kernel<1, kFormat>, grid, kThreads, 0, st, p);
+        if (p.n_pairs == kHeadDim / 2) return launch_dependent(append_rope_kernel<0, kFormat>, grid, kThreads, 0, st, p);
+        return launch_dependent(append_rope_kernel<2, kFormat>, grid, kThreads, 0, st, p);
+    };
+    if (!p.kv8_pages) return launch(std::integral_constant<int, kBf16Pages>{});
+    return p.kv8_format == TTS_KV8_E4M3 ? launch(std::integral_constant<int, TTS_KV8_E4M3>{}) : launch(std::integral_constant<int, TTS_KV8_INT8>{});
 }
 
 }  // namespace tts

@@ -301,6 +301,11 @@ struct Ctx {
     int chunk_rows, chunk_max_pieces;
     long chunk_part_rows;
     size_t chunk_arrived_bytes;
+    // attention over the 8-bit cache (kv8.cuh)
+    float* kv8_part_o; float2* kv8_part_ml; unsigned* kv8_arrived;
+    // beam selection, from tts_beam_reserve on (beam.cuh)
+    void* beam_work;
+    int beam_rows, beam_select;
     // profiling aid
     int profiling, prof_n;
     cudaEvent_t* prof_ev;              // 3 events per recorded call
@@ -330,7 +335,8 @@ cudaError_t launch_kv_rollback(int32_t* branch_lens, const int32_t* accepted_len
                                cudaStream_t st);
 // cache operators (kv_pages.cu, rope_append.cu, cache_api.cu)
 constexpr int kMaxLayers = 128;
-struct PagePools { void* p[2 * kMaxLayers]; int n_layers; };       // K and V pools of the layers, in any order
+struct PagePools { void* p[2 * kMaxLayers]; int n_pools, tile_bytes; };       // K and V pools of the layers, or 8-bit ones, in any order;
+                                                                             // bytes of one page of one KV head
 struct PageWork {
     int32_t* head;          // [0] pages to copy, [1] the plan stands
     int4* child;            // [max_branches] (parent, entries kept, fresh page or -1, length)
@@ -343,8 +349,10 @@ struct RopeParams {
     long q_stride, kv_stride;          // elements from row to row
     const int32_t* positions;          // [n_axes][total_rows]
     __nv_bfloat16 *q_out, *k_pages, *v_pages;
+    unsigned char* kv8_pages;          // the 8-bit pool that takes the place of k_pages and v_pages, or null
     const int32_t *block_table, *branch_lens, *row_start;
     int32_t* status;
+    int kv8_format;
     int Hq, Hkv, n_pairs, interleaved, prefix_len, n_branches, total_rows, max_blocks, num_pages, parts;
     unsigned char axis[kHeadDim / 2];
     double turns[kHeadDim / 2];        // inv_freq / (2 pi)
