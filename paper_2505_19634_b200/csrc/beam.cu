@@ -2,18 +2,18 @@
 //
 //   score(r, x) = beam_score[r] + logit[r][x] - log sum_y exp(logit[r][y]),   ties to the lowest (beam, token)
 //
-// Within a row the score rises with the logit, so a question's n best are among the n largest logits of each row: a first
-// kernel reads every logit once and leaves, per row, the logarithm of the sum and the n largest; a second one, a block per
-// question, puts the rows together.
+// Within a row the score rises with the logit, so a question's n best are among the n largest logits of each row.
 //
-// Rows: bound by HBM (or, for few rows, by latency).  A row is one cluster of 1 to 8 CTAs, each with a contiguous part of it in
-// chunks of 8192 logits that stay in registers: 32 for each thread, whose largest serves both the running sum of exponentials
-// and the search.  A thread looks at its 32 one by one only if its largest passes the threshold, a lower bound of the n-th best
-// logit so far; those that pass go to a list in shared memory.  The threshold is a logit and a token number in one 64-bit
-// word, so that no two entries are equal and the lists stay short whatever the logits are (all equal, rising, ..).
-// Exponentials are fp32; 32 of them are summed in fp32, everything beyond in 64 bits, as are the scores: which of two
-// candidates is better does not hang on a rounding to 32 bits.
-#include <cooperative_groups.h>
+// Bound by HBM (or, for few rows, by latency).  A row is cut into 1 to 8 parts, one CTA each, read once in chunks of four 16-byte loads a
+// thread (what lies behind the last whole chunk one by one): their exponentials go to a running sum, their largest to shared memory.  The n-th largest of the threads' maxima is a lower
+// bound of the n-th largest logit; of the few places whose maximum reaches it the logits are read again (from L2) and listed.  The CTA that
+// ends a question's last part does the same with the entries of all of them, whose scores it forms in 64 bits (which of two candidates is
+// better does not hang on a rounding to 32 bits), and ranks what is left by comparing each with each.  Where numbers are so alike or so
+// ordered that a list would overflow, the n-th largest is found by bisection instead.
+//
+// Which thread adds up which logits does not depend on where a row lies in memory: equal rows have equal sums, bit for bit, and equal scores.
+// Exponentials are fp32 (2^-22); 32 of them are summed in fp32, everything beyond in 64 bits.  For few rows the time is that of fetching
+// every instruction once (about 20 cycles each), which is why there are few phases and little unrolled code outside the pass.
 #include <math.h>
 
 #include <type_traits>
@@ -28,15 +28,13 @@ namespace {
 typedef unsigned long long u64;
 
 constexpr int kThreads = 256;
-constexpr int kPer = 32;                                            // logits of a thread per chunk
-constexpr int kChunk = kThreads * kPer;
-constexpr int kSlackThreads = 16;                                   // threads that may pass the threshold beyond n_select before it is raised
-constexpr int kDirect = 512;                                        // entries that are ranked by comparing each with each
+constexpr int kLoads = 4;                                           // 16-byte loads of a thread per chunk
+constexpr int kPlaces = 16;                                         // maxima that a thread keeps, of one chunk or several
+constexpr int kTasks = 1024;                                        // places to read again, at most
+constexpr int kList = 1024;                                         // entries of a list in shared memory
+static_assert(kMaxSelect <= kThreads && 1 << beam_cap_log2(kMaxSelect) <= kList, "");
 
-__host__ __device__ constexpr int per_chunk(int n) { return kPer * (n + kSlackThreads); }       // entries that a chunk adds at most
-__host__ __device__ constexpr int capacity(int n) { return n + 2 * per_chunk(n); }
-
-// Order-preserving map of fp32 to unsigned words; -infinity is the least number.
+// Order-preserving maps of floating point to unsigned words; -infinity is the least number, and 0 is below it.
 __device__ __forceinline__ uint32_t key_of(float x) {
     const uint32_t b = __float_as_uint(x);
     return b & 0x80000000u ? ~b : b | 0x80000000u;
@@ -48,317 +46,352 @@ __device__ __forceinline__ u64 key_of(double x) {
 }
 __device__ __forceinline__ double value_of(u64 k) { return __longlong_as_double((long long)(k >> 63 ? k & ~(1ull << 63) : ~k)); }
 
-__device__ __forceinline__ u64 entry(float x, int token) { return (u64)key_of(x) << 32 | (0xffffffffu - (uint32_t)token); }
-constexpr u64 kLeast = (u64)(0x007fffffu + 1u) << 32;               // above every entry of -infinity
-
 __device__ __forceinline__ float exp2_approx(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+__device__ __forceinline__ float log2_approx(float x) { float y; asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+__device__ __forceinline__ uint64_t pack2(float a, float b) { uint64_t r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ float2 unpack2(uint64_t v) { float2 r; asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v)); return r; }
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) { uint64_t r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) { uint64_t r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) { uint32_t r; asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b)); return r; }
 
-struct RowShared {
-    u64 maxima[kThreads];
+// A candidate: its key (of the logit within a row, of the score within a question) and its place (token; beam * vocab + token).  Of equal
+// keys the lowest place is better, so no two candidates are equal.
+template <int kN>
+struct Lists {
+    u64 keys[kN];
+    uint32_t places[kN];
+    int n;                                                          // candidates that wanted to the list
+    __device__ __forceinline__ void put(u64 key, uint32_t place) {
+        const int at = atomicAdd(&n, 1);
+        if (at < kN) { keys[at] = key; places[at] = place; }
+    }
+};
+struct Shared {
+    union {
+        float maxima[kPlaces + 1][kThreads];                        // (the last of what is read one by one)
+        double base[kMaxBranches];                                  // of every row: its score so far less the logarithm of its sum
+    };
+    Lists<kList> list;
+    Lists<kThreads> few;
+    u64 groups[kThreads];
     double sums[kThreads / 32];
     float tops[kThreads / 32];
     u64 threshold;
-    int n;                                                          // entries of the list
-    int count;                                                      // scratch of the pruning
-    // what the cluster's first CTA reads
-    double sum;
-    float top;
-    int n_best;
+    int word, n_tasks;
+    int tasks[kTasks];
 };
 
-__device__ __forceinline__ u64 max64(u64 a, u64 b) { return a > b ? a : b; }
+// The sum over the block, known to all threads.
+__device__ __noinline__ int block_sum(int c, int* word) {
+    c = __reduce_add_sync(0xffffffffu, c);
+    __syncthreads();
+    if (threadIdx.x == 0) *word = 0;
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0 && c) atomicAdd(word, c);
+    __syncthreads();
+    return *word;
+}
 
-// Sorts the list into best[0 .. min(n, k)) (descending) and returns that number.  All threads; `list` has sh.n entries.
-__device__ int prune(RowShared& sh, u64* list, u64* best, int k) {
+// The k-th largest of the maxima of 2^a threads each, as many of them as can be with at least 2 k: not above the k-th largest key of all.
+// 0 where there are fewer.
+__device__ __noinline__ u64 lower_bound(Shared& sh, u64 m, int k) {
     const int tid = threadIdx.x;
-    int n = sh.n;
-    if (n > kDirect) {
-        // the k-th largest, bit by bit from the top (entries differ, so exactly k are at or above it)
-        u64 t = 0;
-        for (int bit = 63; bit >= 0; --bit) {
-            const u64 trial = t | 1ull << bit;
-            int c = 0;
-            for (int i = tid; i < n; i += kThreads) c += list[i] >= trial;
-            c = __reduce_add_sync(0xffffffffu, c);
-            if (tid == 0) sh.count = 0;
-            __syncthreads();
-            if ((tid & 31) == 0 && c) atomicAdd(&sh.count, c);
-            __syncthreads();
-            if (sh.count >= k) t = trial;
-            __syncthreads();
-        }
-        if (tid == 0) sh.count = 0;
-        __syncthreads();
-        for (int i = tid; i < n; i += kThreads)
-            if (list[i] >= t) sh.maxima[atomicAdd(&sh.count, 1)] = list[i];       // (n_select <= kThreads of them)
-        __syncthreads();
-        n = sh.count;
-        for (int i = tid; i < n; i += kThreads) list[i] = sh.maxima[i];
-        __syncthreads();
-    }
-    for (int i = tid; i < n; i += kThreads) {
-        const u64 mine = list[i];
-        int rank = 0;
-        for (int j = 0; j < n; ++j) rank += list[j] > mine;
-        if (rank < k) best[rank] = mine;
+    int shift = 0;
+    while (shift < 5 && (kThreads >> (shift + 1)) >= 2 * k) { m = max(m, __shfl_xor_sync(0xffffffffu, m, 1 << shift)); ++shift; }
+    const int groups = kThreads >> shift;
+    if (tid == 0) sh.threshold = 0;
+    if ((tid & ((1 << shift) - 1)) == 0) sh.groups[tid >> shift] = m;
+    __syncthreads();
+    if (tid < groups) {
+        const u64 own = sh.groups[tid];
+        int r = 0;
+#pragma unroll 8
+        for (int j = 0; j < groups; ++j) { const u64 other = sh.groups[j]; r += other > own || (other == own && j < tid); }
+        if (r == k - 1) sh.threshold = own;
     }
     __syncthreads();
-    return min(n, k);
+    return sh.threshold;
+}
+
+// The k best of more candidates than the list holds, by bisection over their keys (of kBits), then over the places of those equal to the
+// k-th.  `each(f)` calls f(key, place) for this thread's candidates; a key of 0 is none.  They are listed.
+template <int kBits, typename List, typename Each>
+__device__ void bisect(Shared& sh, List& list, int k, Each each) {
+    auto count = [&](auto holds) {
+        int c = 0;
+        each([&](u64 key, uint32_t place) { c += key != 0 && holds(key, place); });
+        return block_sum(c, &sh.word);
+    };
+    u64 t = 0;
+#pragma unroll 1
+    for (int bit = kBits - 1; bit >= 0; --bit) {
+        const u64 trial = t | 1ull << bit;
+        if (count([&](u64 key, uint32_t) { return key >= trial; }) >= k) t = trial;
+    }
+    const int above = count([&](u64 key, uint32_t) { return key > t; });
+    uint32_t last = 0;                                              // the (k - above)-th lowest place of those equal
+#pragma unroll 1
+    for (int bit = 31; bit >= 0; --bit) {
+        const uint32_t trial = last | ((1u << bit) - 1u);           // all places of this prefix with a 0 here
+        if (count([&](u64 key, uint32_t place) { return key == t && place <= trial; }) < k - above) last |= 1u << bit;
+    }
+    if (threadIdx.x == 0) list.n = 0;
+    __syncthreads();
+    each([&](u64 key, uint32_t place) { if (key != 0 && (key > t || (key == t && place <= last))) list.put(key, place); });
+    __syncthreads();
+}
+
+// Maxima and sums relative to them of kN lanes, joined in every one of them.
+template <int kN>
+__device__ __forceinline__ void join_sums(float& top, double& sum) {
+    float all = top;
+#pragma unroll
+    for (int o = kN / 2; o; o >>= 1) all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, o));
+    sum = top == -INFINITY && sum == 0.0 ? 0.0 : sum * exp2_approx((top - all) * kLog2e);
+#pragma unroll
+    for (int o = kN / 2; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    top = all;
+}
+
+// A question's parts put together by one block.
+__device__ void join_parts(const BeamParams& p, Shared& sh, int group) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, k = p.n_select, row0 = group * p.n_beams;
+    const size_t out = (size_t)group * k;
+    const u64* entries = p.entries + ((size_t)row0 << (p.parts_log2 + p.cap_log2));
+    const int n = __ldcg(p.n_entries + group);
+    u64 e = tid < n ? __ldcg(entries + tid) : 0;                    // (asked for ahead of the logarithms)
+    if (tid == 0) sh.few.n = 0;
+    // the rows' logarithms, a warp each; NaN for a row that offers nothing.  (A finished beam's candidate has a logit of 0.)
+    for (int b = warp; b < p.n_beams; b += kThreads / 32) {
+        const int row = row0 + b;
+        float top = -INFINITY;
+        double sum = 0.0;
+        if (lane < 1 << p.parts_log2) {
+            const size_t part = ((size_t)row << p.parts_log2) + lane;
+            top = __ldcg(p.part_top + part); sum = __ldcg(p.part_sum + part);
+        }
+        const float before = p.beam_scores[row];
+        const bool done = p.finished && p.finished[row];
+        join_sums<8>(top, sum);
+        if (lane == 0) sh.base[b] = (double)before - (done ? 0.0 : (double)top + (double)(log2_approx((float)sum) * kLn2));
+    }
+    if (tid < k) { p.parents[out + tid] = -1; p.tokens[out + tid] = -1; p.scores[out + tid] = -INFINITY; }      // where there are too few candidates
+    __syncthreads();
+    auto score = [&](u64 entry) -> u64 {                            // as a key; 0 is no candidate
+        const double x = sh.base[(uint32_t)entry / (uint32_t)p.vocab] + (double)value_of((uint32_t)(entry >> 32));
+        return isfinite(x) ? key_of(x) : 0;
+    };
+    if (n > kList)
+        bisect<64>(sh, sh.few, k, [&](auto f) { for (int i = tid; i < n; i += kThreads) { const u64 x = __ldcg(entries + i); f(score(x), (uint32_t)x); } });
+    else {
+        u64 best = 0;
+#pragma unroll 1
+        for (int i = tid; i < n; i += kThreads) {
+            const u64 key = score(e);
+            sh.list.keys[i] = key; sh.list.places[i] = (uint32_t)e;
+            best = max(best, key);
+            if (i + kThreads < n) e = __ldcg(entries + i + kThreads);
+        }
+        const u64 least = max(lower_bound(sh, best, k), (u64)1);
+        auto listed = [&](auto f) { for (int i = tid; i < n; i += kThreads) f(sh.list.keys[i], sh.list.places[i]); };
+        listed([&](u64 key, uint32_t place) { if (key >= least) sh.few.put(key, place); });
+        __syncthreads();
+        if (sh.few.n > kThreads) bisect<64>(sh, sh.few, k, listed);
+    }
+    const int n_few = sh.few.n;
+    if (tid < n_few) {
+        const u64 key = sh.few.keys[tid];
+        const uint32_t place = sh.few.places[tid];
+        int rank = 0;
+#pragma unroll 4
+        for (int j = 0; j < n_few; ++j) rank += sh.few.keys[j] > key || (sh.few.keys[j] == key && sh.few.places[j] < place);
+        if (rank < k) {
+            const uint32_t b = place / (uint32_t)p.vocab;
+            p.parents[out + rank] = row0 + (int)b;
+            p.tokens[out + rank] = (int)(place - b * (uint32_t)p.vocab);
+            p.scores[out + rank] = (float)value_of(key);
+        }
+    }
 }
 
 template <typename T, bool kAligned>
-__global__ void __launch_bounds__(kThreads)
-beam_rows_kernel(const __grid_constant__ BeamParams p) {
-    extern __shared__ __align__(16) unsigned char smem[];
-    RowShared& sh = *reinterpret_cast<RowShared*>(smem);
-    u64* list = reinterpret_cast<u64*>(smem + (sizeof(RowShared) + 15) / 16 * 16);
-    u64* best = list + capacity(p.n_select);
-    namespace cg = cooperative_groups;
-    const cg::cluster_group cluster = cg::this_cluster();
+__global__ void __launch_bounds__(kThreads, 4)
+beam_select_kernel(const __grid_constant__ BeamParams p) {
+    __shared__ Shared sh;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, row = blockIdx.y, k = p.n_select;
-    const int rank = (int)cluster.block_rank(), ranks = (int)cluster.num_blocks();
+    const size_t part = ((size_t)row << p.parts_log2) + blockIdx.x;
     grid_dependency_wait();
     grid_launch_dependents();
-    if (!isfinite(p.beam_scores[row]) || (p.finished && p.finished[row])) return;      // (the whole cluster)
-
-    const T* x = static_cast<const T*>(p.logits) + (size_t)row * p.row_stride;
-    const int begin = min(p.vocab, rank * p.per_cta), end = min(p.vocab, begin + p.per_cta);
-    if (tid == 0) { sh.threshold = kLeast; sh.n = 0; }
-    __syncthreads();
-
-    constexpr int kVec = 16 / sizeof(T);                            // logits of a 16-byte load
-    auto index = [&](int base, int i) { return kAligned ? base + (i / kVec) * (kThreads * kVec) + tid * kVec + i % kVec : base + i * kThreads + tid; };
-    float top = -INFINITY;                                          // of this thread's logits so far
-    double sum = 0.0;                                               // of exp(logit - top)
-    for (int base = begin; base < end; base += kChunk) {
-        float v[kPer];
-        if constexpr (kAligned) {
+    if (isfinite(p.beam_scores[row]) && !(p.finished && p.finished[row])) {
+        const T* x = static_cast<const T*>(p.logits) + (size_t)row * p.row_stride;
+        const int begin = min(p.vocab, (int)blockIdx.x * p.per_part), end = min(p.vocab, begin + p.per_part);
+        constexpr int kVec = 16 / sizeof(T), kChunk = kThreads * kLoads * kVec;       // logits of a load, of a chunk
+        const int chunks = (end - begin) / kChunk, behind = begin + chunks * kChunk, singles = end - behind;
+        const int per_place = (chunks + kPlaces - 1) / kPlaces;     // chunks of a maximum
+        auto index = [&](int chunk, int i) { return begin + chunk * kChunk + (i / kVec) * (kThreads * kVec) + tid * kVec + i % kVec; };
+        auto fetch = [&](int chunk, uint4 (&raw)[kLoads]) {
 #pragma unroll
-            for (int c = 0; c < kPer / kVec; ++c) {
-                const int at = index(base, c * kVec);
-                if (at + kVec <= end) {
-                    const uint4 w = *reinterpret_cast<const uint4*>(x + at);
-                    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+            for (int c = 0; c < kLoads; ++c) {
+                const T* from = x + index(chunk, c * kVec);
+                if constexpr (kAligned) raw[c] = *reinterpret_cast<const uint4*>(from);
+                else {
+                    uint32_t w[4];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        if constexpr (sizeof(T) == 2) { v[c * kVec + 2 * j] = __uint_as_float(u[j] << 16); v[c * kVec + 2 * j + 1] = __uint_as_float(u[j] & 0xffff0000u); }
-                        else v[c * kVec + j] = __uint_as_float(u[j]);
+                        if constexpr (sizeof(T) == 4) w[j] = __float_as_uint(from[j]);
+                        else w[j] = reinterpret_cast<const unsigned short*>(from)[2 * j] | (uint32_t)reinterpret_cast<const unsigned short*>(from)[2 * j + 1] << 16;
                     }
+                    raw[c] = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+            }
+        };
+        // word c of a thread's loads, and the logits in a word
+        auto word = [](const uint4 (&raw)[kLoads], int c) { const uint4& r = raw[c >> 2]; return (c & 3) == 0 ? r.x : (c & 3) == 1 ? r.y : (c & 3) == 2 ? r.z : r.w; };
+        auto logit = [&](const uint4 (&raw)[kLoads], int i) {
+            const uint32_t w = word(raw, sizeof(T) == 2 ? i >> 1 : i);
+            return __uint_as_float(sizeof(T) == 4 ? w : i & 1 ? w & 0xffff0000u : w << 16);
+        };
+        auto largest = [&](const uint4 (&raw)[kLoads]) {
+            uint32_t h[4] = {word(raw, 0), word(raw, 1), word(raw, 2), word(raw, 3)};
+            auto larger = [](uint32_t a, uint32_t b) { return sizeof(T) == 2 ? max_bf16x2(a, b) : __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); };
+#pragma unroll
+            for (int c = 4; c < 4 * kLoads; ++c) h[c & 3] = larger(h[c & 3], word(raw, c));
+            const uint32_t m = larger(larger(h[0], h[1]), larger(h[2], h[3]));
+            return sizeof(T) == 4 ? __uint_as_float(m) : fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
+        };
+
+        // ---- one pass: sums of exponentials and maxima
+        float top = -INFINITY;                                      // of this thread's logits so far
+        double sum = 0.0;                                           // of exp(logit - top)
+        auto raise = [&](float high) {
+            if (high > top) {
+                sum *= exp2_approx((top - high) * kLog2e);
+                top = high;
+            }
+            return top == -INFINITY ? 0.f : -top;
+        };
+        {
+            uint4 next[kLoads];
+            if (chunks > 0) fetch(0, next);
+            // (the singles while the first chunk is on its way)
+            float high_here = -INFINITY;
+#pragma unroll 1
+            for (int j0 = tid; j0 < singles; j0 += 4 * kThreads) {
+                float v[4], part4 = 0.f;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) v[c] = j0 + c * kThreads < singles ? (float)x[behind + j0 + c * kThreads] : -INFINITY;
+                const float high = fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), ref = raise(high);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) part4 += exp2_approx((v[c] + ref) * kLog2e);
+                sum += part4;
+                high_here = fmaxf(high_here, high);
+            }
+            sh.maxima[kPlaces][tid] = high_here;
+            high_here = -INFINITY;
+            int place = 0, left = per_place;
+#pragma unroll 1
+            for (int chunk = 0; chunk < chunks; ++chunk) {
+                uint4 raw[kLoads];
+#pragma unroll
+                for (int c = 0; c < kLoads; ++c) raw[c] = next[c];
+                if (chunk + 1 < chunks) fetch(chunk + 1, next);
+                const float high = largest(raw), ref = raise(high);
+                const uint64_t ref2 = pack2(ref, ref), log2e = pack2(kLog2e, kLog2e);
+                uint64_t part2[2] = {0, 0};
+#pragma unroll
+                for (int i = 0; i < kLoads * kVec; i += 2) {
+                    const float2 y = unpack2(mul2(add2(pack2(logit(raw, i), logit(raw, i + 1)), ref2), log2e));
+                    part2[(i >> 1) & 1] = add2(part2[(i >> 1) & 1], pack2(exp2_approx(y.x), exp2_approx(y.y)));
+                }
+                const float2 s2 = unpack2(add2(part2[0], part2[1]));
+                sum += s2.x + s2.y;
+                high_here = fmaxf(high_here, high);
+                if (--left == 0 || chunk + 1 == chunks) { sh.maxima[place++][tid] = high_here; high_here = -INFINITY; left = per_place; }
+            }
+        }
+
+        // ---- what reaches the lower bound is read again and listed
+        if (tid == 0) { sh.list.n = 0; sh.n_tasks = 0; }
+        const u64 bound = lower_bound(sh, key_of(top), k);
+        const float least = fmaxf(value_of((uint32_t)bound), -3.402823466e38f);      // (-infinity is nobody's choice; of 0 the value is a NaN)
+        // (whose 32 logits of which chunk: four threads look at them, so that all of them are on their way at once)
+        if (chunks > 0)
+#pragma unroll 1
+            for (int place = 0; place * per_place < chunks; ++place)
+                if (sh.maxima[place][tid] >= least)
+                    for (int chunk = place * per_place; chunk < min(chunks, (place + 1) * per_place); ++chunk) {
+                        const int at = atomicAdd(&sh.n_tasks, 1);
+                        if (at < kTasks) sh.tasks[at] = chunk * kThreads + tid;
+                    }
+        if (sh.maxima[kPlaces][tid] >= least)
+#pragma unroll 1
+            for (int j = tid; j < singles; j += kThreads) {
+                const float v = (float)x[behind + j];
+                if (v >= least) sh.list.put(key_of(v), (uint32_t)(behind + j));
+            }
+        __syncthreads();
+        const int n_tasks = sh.n_tasks;
+        if (n_tasks <= kTasks)
+#pragma unroll 1
+            for (int i = tid >> 2; i < n_tasks; i += kThreads / 4) {
+                const int chunk = sh.tasks[i] / kThreads, who = sh.tasks[i] % kThreads, at = begin + chunk * kChunk + (tid & 3) * (kThreads * kVec) + who * kVec;
+                float v[kVec];
+                if constexpr (kAligned) {
+                    const uint4 r = *reinterpret_cast<const uint4*>(x + at);
+                    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+                    for (int j = 0; j < kVec; ++j) v[j] = __uint_as_float(sizeof(T) == 4 ? w[j] : j & 1 ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16);
                 } else {
 #pragma unroll
-                    for (int j = 0; j < kVec; ++j) v[c * kVec + j] = at + j < end ? (float)x[at + j] : -INFINITY;
+                    for (int j = 0; j < kVec; ++j) v[j] = (float)x[at + j];
                 }
+#pragma unroll
+                for (int j = 0; j < kVec; ++j) if (v[j] >= least) sh.list.put(key_of(v[j]), (uint32_t)(at + j));
             }
-        } else {
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) v[i] = index(base, i) < end ? (float)x[index(base, i)] : -INFINITY;
-        }
-        float high = v[0];
-#pragma unroll
-        for (int i = 1; i < kPer; ++i) high = fmaxf(high, v[i]);
-        if (high > top) {
-            sum *= exp2_approx((top - high) * 1.4426950408889634f);
-            top = high;
-        }
-        float part = 0.f;
-        const float ref = top == -INFINITY ? 0.f : top;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) part += exp2_approx((v[i] - ref) * 1.4426950408889634f);
-        sum += part;
-
-        // ---- candidates
-        u64 t = sh.threshold;
-        bool pass = key_of(high) >= (uint32_t)(t >> 32);
-        int passing = __syncthreads_count(pass);
-        if (passing == 0) continue;
-        auto largest = [&]() {                                      // this thread's largest entry, the lowest token of equal ones
-            u64 e = 0;
-#pragma unroll
-            for (int i = kPer - 1; i >= 0; --i) if (v[i] == high) e = entry(v[i], index(base, i));
-            return e;
-        };
-        if (passing > k + kSlackThreads) {
-            // raise the threshold: the k-th largest of the maxima of 2^a groups of threads is not above the k-th largest logit
-            int width = 1;
-            while (kThreads / (2 * width) >= 2 * k && width < 32) width *= 2;
-            u64 m = pass ? largest() : 0;
-            for (int o = 1; o < width; o <<= 1) m = max64(m, __shfl_xor_sync(0xffffffffu, m, o));
-            for (;;) {
-                const int groups = kThreads / width;
-                if (tid % width == 0) sh.maxima[tid / width] = m;
-                __syncthreads();
-                if (tid < groups) {
-                    const u64 mine = sh.maxima[tid];
-                    int r = 0;
-                    for (int j = 0; j < groups; ++j) r += sh.maxima[j] > mine;
-                    if (r == k - 1 && mine > sh.threshold) sh.threshold = mine;      // (one thread: nonzero entries differ)
-                }
-                __syncthreads();
-                t = sh.threshold;
-                pass = pass && key_of(high) >= (uint32_t)(t >> 32) && largest() >= t;
-                passing = __syncthreads_count(pass);
-                if (passing <= k + kSlackThreads || width == 1) break;
-                width = 1;                                          // the logits lie together: once more, thread by thread
-                m = pass ? largest() : 0;
-            }
-        }
-        if (pass) {
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) {
-                const u64 e = entry(v[i], index(base, i));
-                if (e >= t) list[atomicAdd(&sh.n, 1)] = e;
-            }
-        }
+        // the CTA's sum
+        join_sums<32>(top, sum);
+        if (lane == 0) { sh.tops[warp] = top; sh.sums[warp] = sum; }
         __syncthreads();
-        if (sh.n > capacity(k) - per_chunk(k)) {
-            const int n = prune(sh, list, best, k);
-            for (int i = tid; i < n; i += kThreads) list[i] = best[i];
-            if (tid == 0) { sh.n = n; if (n == k) sh.threshold = max64(sh.threshold, best[k - 1]); }
-            __syncthreads();
+        if (sh.list.n > 1 << p.cap_log2 || n_tasks > kTasks)        // more than the part's list holds: its k best
+            bisect<32>(sh, sh.list, k, [&](auto f) {
+                for (int i = begin + tid; i < end; i += kThreads) { const float v = (float)x[i]; f(v > -INFINITY ? (u64)key_of(v) : 0, (uint32_t)i); }
+            });
+        const int group = row / p.n_beams, n = min(sh.list.n, 1 << p.cap_log2);
+        if (tid == 0) sh.word = atomicAdd(p.n_entries + group, n);
+        __syncthreads();
+        u64* to = p.entries + ((size_t)group * p.n_beams << (p.parts_log2 + p.cap_log2)) + sh.word;
+        const uint32_t at = (uint32_t)(row - group * p.n_beams) * (uint32_t)p.vocab;
+        for (int i = tid; i < n; i += kThreads) to[i] = sh.list.keys[i] << 32 | (at + sh.list.places[i]);
+        if (warp == 0) {
+            float m = lane < kThreads / 32 ? sh.tops[lane] : -INFINITY;
+            double z = lane < kThreads / 32 ? sh.sums[lane] : 0.0;
+            join_sums<8>(m, z);
+            if (lane == 0) { p.part_top[part] = m; p.part_sum[part] = z; }
         }
+    } else if (isfinite(p.beam_scores[row]) && blockIdx.x == 0 && tid == 0) {      // a finished beam: itself
+        const int group = row / p.n_beams, at = atomicAdd(p.n_entries + group, 1);
+        p.entries[((size_t)group * p.n_beams << (p.parts_log2 + p.cap_log2)) + at] =
+            (u64)key_of(0.f) << 32 | ((uint32_t)(row - group * p.n_beams) * (uint32_t)p.vocab + (uint32_t)p.pad_token);
     }
-
-    // ---- this CTA's sum and best
-    float all = top;
-#pragma unroll
-    for (int o = 16; o; o >>= 1) all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, o));
-    if (lane == 0) sh.tops[warp] = all;
+    // ---- the CTA that ends the question's last part puts them together
     __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kThreads / 32; ++w) all = fmaxf(all, sh.tops[w]);
-    double s = top == -INFINITY && sum == 0.0 ? 0.0 : sum * exp((double)top - (double)all);
-#pragma unroll
-    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    if (lane == 0) sh.sums[warp] = s;
-    const int mine = prune(sh, list, best, k);                      // (its barriers stand between the sums and their reader)
-    __syncthreads();
+    const int group = row / p.n_beams;
     if (tid == 0) {
-        s = 0.0;
-        for (int w = 0; w < kThreads / 32; ++w) s += sh.sums[w];
-        sh.sum = s; sh.top = all; sh.n_best = mine;
-    }
-    cluster.sync();
-    if (rank == 0) {
-        // ---- the row's: the others' lists behind this one's
-        if (tid == 0) {
-            float m = -INFINITY;
-            for (int c = 0; c < ranks; ++c) m = fmaxf(m, cluster.map_shared_rank(&sh, c)->top);
-            double z = 0.0;
-            for (int c = 0; c < ranks; ++c) {
-                const RowShared* other = cluster.map_shared_rank(&sh, c);
-                if (!(other->top == -INFINITY && other->sum == 0.0)) z += other->sum * exp((double)other->top - (double)m);
-            }
-            p.lse[row] = (double)m + log(z);                        // NaN where a logit was, or all were -infinity
+        __threadfence();                                            // the block's writes, which the barrier put before this
+        const bool last = atomicAdd(p.arrived + group, 1) + 1 == p.n_beams << p.parts_log2;
+        if (last) {
+            p.arrived[group] = 0;                                   // as the next call expects it
+            __threadfence();
         }
-        int n = 0;
-        for (int c = 0; c < ranks; ++c) {
-            const int from = cluster.map_shared_rank(&sh, c)->n_best;
-            const u64* theirs = cluster.map_shared_rank(best, c);
-            for (int i = tid; i < from; i += kThreads) list[n + i] = theirs[i];        // (at most 8 k, which the list holds)
-            n += from;
-        }
-        if (tid == 0) sh.n = n;
-        __syncthreads();
-        if (ranks > 1) n = prune(sh, list, best, k);
-        for (int i = tid; i < n; i += kThreads) p.best[(size_t)row * k + i] = best[i];
-        if (tid == 0) p.count[row] = n;
-    }
-    cluster.sync();                                                 // nobody leaves while its lists are read
-}
-
-// One block per question: candidates of all rows with their scores in 64 bits, ranked.
-constexpr int kJoinThreads = 1024;
-
-__global__ void __launch_bounds__(kJoinThreads)
-beam_join_kernel(const __grid_constant__ BeamParams p) {
-    extern __shared__ __align__(16) unsigned char smem[];
-    const int cap = p.n_beams * p.n_select;
-    u64* keys = reinterpret_cast<u64*>(smem);                       // [cap] of the scores
-    uint32_t* places = reinterpret_cast<uint32_t*>(keys + cap);     // [cap] beam * vocab + token
-    u64* few_keys = reinterpret_cast<u64*>(smem + (size_t)(cap * 12 + 15) / 16 * 16);      // [n_select]
-    uint32_t* few_places = reinterpret_cast<uint32_t*>(few_keys + p.n_select);
-    __shared__ int n_all, n_few, counted;
-    const int tid = threadIdx.x, k = p.n_select, row0 = blockIdx.x * p.n_beams;
-    grid_dependency_wait();
-    grid_launch_dependents();
-    if (tid == 0) n_all = n_few = 0;
-    __syncthreads();
-    auto put = [&](double score, uint32_t place) {
-        if (!(score > -INFINITY) || !isfinite(score)) return;
-        const int at = atomicAdd(&n_all, 1);
-        keys[at] = key_of(score); places[at] = place;
-    };
-    for (int i = tid; i < cap; i += kJoinThreads) {
-        const int b = i / k, j = i - b * k, row = row0 + b;
-        const float before = p.beam_scores[row];
-        if (!isfinite(before)) continue;
-        if (p.finished && p.finished[row]) {
-            if (j == 0) put((double)before, (uint32_t)b * (uint32_t)p.vocab + (uint32_t)p.pad_token);
-        } else if (j < p.count[row]) {
-            const u64 e = p.best[(size_t)row * k + j];
-            put((double)before + ((double)value_of((uint32_t)(e >> 32)) - p.lse[row]), (uint32_t)b * (uint32_t)p.vocab + (0xffffffffu - (uint32_t)e));
-        }
+        sh.word = last;
     }
     __syncthreads();
-    int n = n_all;
-    const u64* from_keys = keys;
-    const uint32_t* from_places = places;
-    // how many entries satisfy a condition; all threads
-    auto count = [&](auto holds) {
-        int c = 0;
-        for (int i = tid; i < n; i += kJoinThreads) c += holds(i);
-        c = __reduce_add_sync(0xffffffffu, c);
-        __syncthreads();
-        if (tid == 0) counted = 0;
-        __syncthreads();
-        if ((tid & 31) == 0 && c) atomicAdd(&counted, c);
-        __syncthreads();
-        return counted;
-    };
-    if (n > kJoinThreads) {
-        // the k-th largest score, bit by bit; of the entries equal to it, those of the lowest places
-        u64 t = 0;
-        for (int bit = 63; bit >= 0; --bit) {
-            const u64 trial = t | 1ull << bit;
-            if (count([&](int i) { return keys[i] >= trial; }) >= k) t = trial;
-        }
-        const int above = count([&](int i) { return keys[i] > t; });
-        uint32_t last = 0;                                          // the (k - above)-th lowest place of those
-        for (int bit = 31; bit >= 0; --bit) {
-            const uint32_t trial = last | ((1u << bit) - 1u);       // all places of this prefix with a 0 here
-            if (count([&](int i) { return keys[i] == t && places[i] <= trial; }) < k - above) last |= 1u << bit;
-        }
-        for (int i = tid; i < n; i += kJoinThreads)
-            if (keys[i] > t || (keys[i] == t && places[i] <= last)) {
-                const int at = atomicAdd(&n_few, 1);
-                few_keys[at] = keys[i]; few_places[at] = places[i];
-            }
-        __syncthreads();
-        n = n_few; from_keys = few_keys; from_places = few_places;
-    }
-    // ranks by comparing each with each, `share` threads to an entry
-    int share = 1;
-    while (share < 32 && n * share * 2 <= kJoinThreads) share *= 2;
-    const int i = tid / share;
-    int rank = 0;
-    u64 key = 0;
-    uint32_t place = 0;
-    if (i < n) {
-        key = from_keys[i]; place = from_places[i];
-        for (int j = tid % share; j < n; j += share) {
-            const u64 other = from_keys[j];
-            rank += other > key || (other == key && from_places[j] < place);
-        }
-    }
-    for (int o = 1; o < share; o <<= 1) rank += __shfl_xor_sync(0xffffffffu, rank, o);
-    const size_t out = (size_t)blockIdx.x * k;
-    if (i < n && tid % share == 0 && rank < k) {
-        const uint32_t b = place / (uint32_t)p.vocab;
-        p.parents[out + rank] = row0 + (int)b;
-        p.tokens[out + rank] = (int)(place - b * (uint32_t)p.vocab);
-        p.scores[out + rank] = (float)value_of(key);
-    }
-    if (tid >= n && tid < k) { p.parents[out + tid] = -1; p.tokens[out + tid] = -1; p.scores[out + tid] = -INFINITY; }
+    const bool last = sh.word;
+    __syncthreads();
+    if (!last) return;
+    join_parts(p, sh, group);
+    if (tid == 0) p.n_entries[group] = 0;                           // as the next call expects it (all threads have read it)
 }
 
 // Rows of many arrays: dst[i] = src[parents[i]].  Bound by HBM; a block moves 32 KiB of a row (8 loads of 16 bytes a thread before
@@ -408,37 +441,14 @@ beam_reorder_kernel(const __grid_constant__ ReorderParams p) {
 
 }  // namespace
 
-cudaError_t launch_beam_select(BeamParams p, int logits_dtype, int n_sms, cudaStream_t st) {
-    const int rows = p.n_groups * p.n_beams;
+cudaError_t launch_beam_select(BeamParams p, int logits_dtype, cudaStream_t st) {
+    p.per_part = ceil_div(ceil_div(p.vocab, 1 << p.parts_log2), 8) * 8;
+    const dim3 grid(1 << p.parts_log2, p.n_groups * p.n_beams);
     const size_t elt = logits_dtype == TTS_LOGITS_BF16 ? 2 : 4;
-    const bool vectors = ((reinterpret_cast<uintptr_t>(p.logits) | (uintptr_t)(p.row_stride * elt)) & 15) == 0;
-    // CTAs to a row: until there are four to an SM, and as long as each has half a chunk
-    int ctas = 1;
-    while (ctas < 8 && rows * ctas < 4 * n_sms && p.vocab / (2 * ctas) >= kChunk / 2) ctas *= 2;
-    p.per_cta = ceil_div(ceil_div(p.vocab, ctas), 8) * 8;
-    const size_t smem = (sizeof(RowShared) + 15) / 16 * 16 + (size_t)(capacity(p.n_select) + p.n_select) * 8;
-    auto rows_kernel = [&](auto kernel) {
-        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        if (e != cudaSuccess) return e;
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3(ctas, rows); cfg.blockDim = kThreads; cfg.dynamicSmemBytes = smem; cfg.stream = st;
-        cudaLaunchAttribute attr[2];
-        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr[0].val.programmaticStreamSerializationAllowed = 1;
-        attr[1].id = cudaLaunchAttributeClusterDimension;
-        attr[1].val.clusterDim.x = ctas; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
-        cfg.attrs = attr; cfg.numAttrs = 2;
-        return cudaLaunchKernelEx(&cfg, kernel, p);
-    };
-    cudaError_t e;
-    if (logits_dtype == TTS_LOGITS_BF16) e = vectors ? rows_kernel(beam_rows_kernel<__nv_bfloat16, true>) : rows_kernel(beam_rows_kernel<__nv_bfloat16, false>);
-    else e = vectors ? rows_kernel(beam_rows_kernel<float, true>) : rows_kernel(beam_rows_kernel<float, false>);
-    if (e != cudaSuccess) return e;
-    const int cap = p.n_beams * p.n_select;
-    const size_t join = (size_t)(cap * 12 + 15) / 16 * 16 + (size_t)p.n_select * 12;
-    e = cudaFuncSetAttribute(beam_join_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)join);
-    if (e != cudaSuccess) return e;
-    return launch_dependent(beam_join_kernel, p.n_groups, kJoinThreads, join, st, p);
+    const bool aligned = ((reinterpret_cast<uintptr_t>(p.logits) | (uintptr_t)(p.row_stride * elt)) & 15) == 0;
+    if (logits_dtype == TTS_LOGITS_BF16)
+        return aligned ? launch_dependent(beam_select_kernel<__nv_bfloat16, true>, grid, kThreads, 0, st, p) : launch_dependent(beam_select_kernel<__nv_bfloat16, false>, grid, kThreads, 0, st, p);
+    return aligned ? launch_dependent(beam_select_kernel<float, true>, grid, kThreads, 0, st, p) : launch_dependent(beam_select_kernel<float, false>, grid, kThreads, 0, st, p);
 }
 
 cudaError_t launch_beam_reorder(const ReorderParams& p, cudaStream_t st) {

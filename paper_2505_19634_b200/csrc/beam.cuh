@@ -5,19 +5,30 @@
 namespace tts {
 
 constexpr int kMaxSelect = 128;        // continuations that a question may keep
-constexpr int kMaxBeamCandidates = 8192;   // beams of a question times continuations: what the joining block sorts in shared memory
+constexpr int kMaxBeamCandidates = 8192;   // beams of a question times continuations
+// Candidates that a part of a row may leave for the question's last CTA, a power of two: more than the n best, for what the bound lets through.
+__host__ __device__ constexpr int beam_cap_log2(int n) { return n <= 16 ? 6 : n <= 48 ? 7 : n <= 96 ? 8 : 9; }
+// Parts of a row, 2^0 to 2^3: as long as the GPU takes all of them at once, four CTAs to an SM, and each has 4096 logits.
+inline int beam_parts_log2(int rows, int vocab, int n_sms) {
+    int log2 = 0;
+    while (log2 < 3 && (long)rows << (log2 + 1) <= 4l * n_sms && vocab >> (log2 + 1) >= 4096) ++log2;
+    return log2;
+}
+inline long beam_max_parts(int rows, int n_sms) { return rows > 4 * n_sms ? rows : 4l * n_sms; }       // of all rows of a call
 
 struct BeamParams {
     const void* logits;
     long row_stride;                   // elements
     const float* beam_scores;
     const int32_t* finished;           // or null
-    double* lse;                       // [rows] logarithm of the sum of the row's exponentials
-    int32_t* count;                    // [rows] entries of `best`
-    unsigned long long* best;          // [rows][n_select] (key of the logit, 2^32 - 1 - token)
+    double* part_sum;                  // of every part of a row: the sum of exp(logit - the largest),
+    float* part_top;                   // the largest logit
+    unsigned long long* entries;       // of every question: its parts' candidates (key of the logit, beam * vocab + token), in any order,
+    int32_t* n_entries;                // their number,
+    int32_t* arrived;                  // and the parts that have ended; the last two are zero between calls
     int32_t *parents, *tokens;
     float* scores;
-    int vocab, pad_token, n_groups, n_beams, n_select, per_cta;
+    int vocab, pad_token, n_groups, n_beams, n_select, parts_log2, cap_log2, per_part;
 };
 constexpr int kMaxStates = 128;
 struct ReorderParams {
@@ -36,7 +47,7 @@ inline int reorder_unit(const void* src, const void* dst, long row_bytes) {
     const uintptr_t x = reinterpret_cast<uintptr_t>(src) | reinterpret_cast<uintptr_t>(dst) | (uintptr_t)row_bytes;
     return x & 3 ? 1 : x & 15 ? 4 : 16;
 }
-cudaError_t launch_beam_select(BeamParams p, int logits_dtype, int n_sms, cudaStream_t st);
+cudaError_t launch_beam_select(BeamParams p, int logits_dtype, cudaStream_t st);
 cudaError_t launch_beam_reorder(const ReorderParams& p, cudaStream_t st);
 
 }  // namespace tts

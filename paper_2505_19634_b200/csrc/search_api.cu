@@ -104,6 +104,9 @@ int tts_kv8_attn(tts_ctx* ctx, int format, const void* q, int64_t q_row_stride, 
     const Span queries{q, ((rows - 1) * q_row_stride + (size_t)f.n_q_heads * kHeadDim) * 2}, pool{kv8_pages, kv8_bytes(f)},
         table{block_table, table_bytes(f, n_branches)}, lens{branch_lens, (size_t)n_branches * 4}, parents{tree_parents, tree_parents ? rows * 4 : 0},
         result{out, rows * f.n_q_heads * kHeadDim * (f.out_dtype == TTS_OUT_FP32 ? 4 : 2)}, logs{lse, lse ? rows * f.n_q_heads * 4 : 0};
+    // (units of a CTA are counted in 32 bits)
+    const int n_rb = ceil_div(rows_per_branch * (f.n_q_heads / f.n_kv_heads), kKv8MaxRows), grid = f.max_ctas > 0 && f.max_ctas < c->n_sms ? f.max_ctas : c->n_sms;
+    if ((double)n_branches * f.max_blocks_per_branch * f.n_kv_heads * n_rb / grid >= 2e9) return TTS_ERR_UNSUPPORTED;
     if (clash(result, {queries, pool, table, lens}) || (tree_parents && clash(result, {parents})) ||
         (lse && (clash(logs, {result, queries, pool, table, lens}) || (tree_parents && clash(logs, {parents})))))
         return TTS_ERR_INVALID;
@@ -115,9 +118,9 @@ int tts_kv8_attn(tts_ctx* ctx, int format, const void* q, int64_t q_row_stride, 
     p.block_table = block_table; p.branch_lens = branch_lens; p.tree_parents = tree_parents; p.out = out; p.lse = lse;
     p.part_o = c->kv8_part_o; p.part_ml = c->kv8_part_ml; p.arrived = c->kv8_arrived; p.status = c->d_status;
     p.Hq = f.n_q_heads; p.Hkv = f.n_kv_heads; p.G = p.Hq / p.Hkv; p.R = rows_per_branch; p.nr = p.R * p.G;
-    p.n_rb = ceil_div(p.nr, kKv8MaxRows); p.rb_rows = ceil_div(p.nr, p.n_rb);
+    p.n_rb = n_rb; p.rb_rows = ceil_div(p.nr, p.n_rb);
     p.prefix_len = prefix_len; p.n_branches = n_branches; p.max_blocks = f.max_blocks_per_branch; p.num_pages = f.num_pages; p.out_dtype = f.out_dtype;
-    p.grid = f.max_ctas > 0 && f.max_ctas < c->n_sms ? f.max_ctas : c->n_sms;
+    p.grid = grid;
     p.scale_log2 = (f.softmax_scale > 0.f ? f.softmax_scale : 1.0f / sqrtf((float)f.head_dim)) * 1.4426950408889634f;
     return finish(c, launch_kv8_attn(p, format, c->stream), 1);
 }
@@ -129,8 +132,13 @@ int tts_beam_reserve(tts_ctx* ctx, int max_rows, int max_select) {
     if (c->beam_rows > 0) return max_rows <= c->beam_rows && max_select <= c->beam_select ? TTS_OK : TTS_ERR_INVALID;
     const OnDevice on(c->device);
     if (on.error() != cudaSuccess) return finish(c, on.error(), 0);
-    const cudaError_t e = cudaMalloc(&c->beam_work, (size_t)max_rows * (8 + 8 * (size_t)max_select + 4));
+    // candidates, a sum and a maximum for every part of a row, two counters for every question
+    const size_t bytes = (size_t)beam_max_parts(max_rows, c->n_sms) * ((8 << beam_cap_log2(max_select)) + 12) + (size_t)max_rows * 8;
+    cudaError_t e = cudaMalloc(&c->beam_work, bytes);
     if (e != cudaSuccess) { c->beam_work = nullptr; return finish(c, e, 0); }
+    e = cudaMemset(c->beam_work, 0, bytes);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(cudaStreamLegacy);       // before work on a stream that does not wait for it
+    if (e != cudaSuccess) { cudaFree(c->beam_work); c->beam_work = nullptr; return finish(c, e, 0); }
     c->beam_rows = max_rows; c->beam_select = max_select;
     return TTS_OK;
 }
@@ -156,12 +164,16 @@ int tts_beam_select(tts_ctx* ctx, const void* logits, int logits_dtype, int64_t 
     BeamParams p;
     memset(&p, 0, sizeof p);
     p.logits = logits; p.row_stride = (long)row_stride; p.beam_scores = beam_scores; p.finished = finished;
-    p.lse = static_cast<double*>(c->beam_work);
-    p.best = reinterpret_cast<unsigned long long*>(p.lse + c->beam_rows);
-    p.count = reinterpret_cast<int32_t*>(p.best + (size_t)c->beam_rows * c->beam_select);
+    const size_t parts = (size_t)beam_max_parts(c->beam_rows, c->n_sms);
+    p.entries = static_cast<unsigned long long*>(c->beam_work);
+    p.part_sum = reinterpret_cast<double*>(p.entries + (parts << beam_cap_log2(c->beam_select)));
+    p.part_top = reinterpret_cast<float*>(p.part_sum + parts);
+    p.n_entries = reinterpret_cast<int32_t*>(p.part_top + parts);
+    p.arrived = p.n_entries + c->beam_rows;
     p.parents = parents; p.tokens = tokens; p.scores = scores;
     p.vocab = vocab; p.pad_token = pad_token; p.n_groups = n_groups; p.n_beams = n_beams; p.n_select = n_select;
-    return finish(c, launch_beam_select(p, logits_dtype, c->n_sms, c->stream), 2);
+    p.parts_log2 = beam_parts_log2(n_groups * n_beams, vocab, c->n_sms); p.cap_log2 = beam_cap_log2(n_select);
+    return finish(c, launch_beam_select(p, logits_dtype, c->stream), 1);
 }
 
 int tts_beam_reorder(tts_ctx* ctx, int n_states, const void* const* src, void* const* dst, const int64_t* row_bytes, const int32_t* parents,
