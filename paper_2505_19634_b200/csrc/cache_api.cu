@@ -137,22 +137,26 @@ cudaError_t cache_alloc(Ctx* c) {
     const size_t items = nb * f.n_kv_heads * ceil_div(f.max_rows_per_branch * (f.n_q_heads / f.n_kv_heads), kKv8MaxRows);
     if (e == cudaSuccess) e = cudaMalloc(&c->kv8_part_o, slots * kHeadDim * sizeof(float));
     if (e == cudaSuccess) e = cudaMalloc(&c->kv8_part_ml, slots * sizeof(float2));
-    if (e == cudaSuccess) e = cudaMalloc(&c->kv8_arrived, items * sizeof(unsigned));
-    if (e == cudaSuccess) e = cudaMemset(c->kv8_arrived, 0, items * sizeof(unsigned));
+    c->kv8_arrived_bytes = items * sizeof(unsigned);
+    if (e == cudaSuccess) e = cudaMalloc(&c->kv8_arrived, c->kv8_arrived_bytes);
+    if (e == cudaSuccess) e = cudaMemset(c->kv8_arrived, 0, c->kv8_arrived_bytes);
     if (e == cudaSuccess) e = cudaStreamSynchronize(cudaStreamLegacy);       // before work on a stream that does not wait for it
     return e;
 }
 
 cudaError_t cache_reset(Ctx* c) {
-    if (c->chunk_rows == 0) return cudaSuccess;
-    cudaError_t e = cudaMemsetAsync(c->chunk_arrived, 0, c->chunk_arrived_bytes, c->stream);
-    if (e == cudaSuccess) e = cudaMemsetAsync(c->chunk_head, 0, sizeof(ChunkHead), c->stream);
+    cudaError_t e = cudaMemsetAsync(c->kv8_arrived, 0, c->kv8_arrived_bytes, c->stream);
+    if (c->chunk_rows > 0) {
+        if (e == cudaSuccess) e = cudaMemsetAsync(c->chunk_arrived, 0, c->chunk_arrived_bytes, c->stream);
+        if (e == cudaSuccess) e = cudaMemsetAsync(c->chunk_head, 0, sizeof(ChunkHead), c->stream);
+    }
     return e == cudaSuccess ? cudaStreamSynchronize(c->stream) : e;      // before work on another stream
 }
 
 cudaError_t cache_disturb(Ctx* c) {
-    if (c->chunk_rows == 0) return cudaSuccess;
-    const cudaError_t e = cudaMemsetAsync(c->chunk_arrived, 1, c->chunk_arrived_bytes, c->stream);
+    cudaError_t e = cudaMemsetAsync(c->kv8_arrived, 1, c->kv8_arrived_bytes, c->stream);
+    if (e != cudaSuccess || c->chunk_rows == 0) return e;
+    e = cudaMemsetAsync(c->chunk_arrived, 1, c->chunk_arrived_bytes, c->stream);
     return e == cudaSuccess ? cudaMemsetAsync(c->chunk_head, 1, sizeof(ChunkHead), c->stream) : e;
 }
 

@@ -43,7 +43,8 @@ template <int kFormat>
 __device__ __forceinline__ uint32_t kv8_decode2(uint32_t w, int half) {
     uint32_t r;
     if constexpr (kFormat == TTS_KV8_E4M3) {
-        asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\t}" : "=r"(r) : "r"(half ? w >> 16 : w));
+        if (half) asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, hi;\n\t}" : "=r"(r) : "r"(w));
+        else asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\t}" : "=r"(r) : "r"(w));
     } else {
         const uint32_t x = __byte_perm(w, 0x64646464u, half ? 0x4342 : 0x4140), bias = 0x64806480u;
         asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(bias));
