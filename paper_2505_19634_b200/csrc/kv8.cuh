@@ -61,14 +61,14 @@ struct Kv8AttnParams {
     const int32_t *block_table, *branch_lens, *tree_parents;
     void* out;
     float* lse;
-    float* part_o;                     // [2 * grid][32][128] normalised partial results
-    float2* part_ml;                   // [2 * grid][32] their maximum (log2 units) and sum
+    float* part_o;                     // [2 * grid][24][128] normalised partial results
+    float2* part_ml;                   // [2 * grid][24] their maximum (log2 units) and sum
     unsigned* arrived;                 // [branch][KV head][row block] parts written so far; zero between calls
     int32_t* status;
     int Hq, Hkv, G, R, nr, n_rb, rb_rows, prefix_len, n_branches, max_blocks, num_pages, out_dtype, grid;
     float scale_log2;
 };
-constexpr int kKv8MaxRows = 32;        // rows of one KV head that a block works on at a time
+constexpr int kKv8MaxRows = 24;        // rows of one KV head that a block works on at a time
 struct Kv8ReadParams {
     const unsigned char* pool;
     const int32_t *src, *dst;

@@ -3,13 +3,13 @@
 //   out[r] = sum_t softmax_t(scale <q_r, ck_t> sk_t) cv_t sv_t,   codes c and scales s of kv8.cuh
 //
 // Bound by HBM where a branch has few rows per KV head: a record of 4224 bytes (16 tokens) is read once for all rows
-// of the branch.  Work is cut into items (branch, KV head, block of up to 32 stacked rows) of as many units as the branch
-// has pages; a CTA of 8 warps owns a contiguous run of all units, warp w takes its pages w, w + 8, .. and works on them
-// without meeting the other warps: they come by asynchronous copies into a ring of the warp's own.  At the end of an item
+// of the branch.  Work is cut into items (branch, KV head, block of up to 24 stacked rows) of as many units as the branch
+// has pages; a CTA of 8 warps owns a contiguous run of all units, warp w takes its pairs of pages w, w + 8, .. and works on them
+// without meeting the other warps: they come by bulk copies into a ring of the warp's own.  At the end of an item
 // (or of the run) the warps join their results through shared memory; items cut between CTAs are joined by the last CTA
 // to finish one of their parts, which the others leave in global memory.
 //
-// Per page, with tokens on the M side and rows on the N side of the warp-level matrix instruction m16n8k16 (fp16 operands,
+// Per page (and two at a time, for what one leaves idle), with tokens on the M side and rows on the N side of the warp-level matrix instruction m16n8k16 (fp16 operands,
 // fp32 sums):
 //     S^T[16 tokens][rows] = K Q^T      O^T[128 dims][rows] += V^T P^T
 // Codes are exact in fp16, so K and V need no rounding; a row of Q is scaled by a power of two so that bf16 fits fp16 too.
@@ -26,47 +26,52 @@
 
 #include "kv8.cuh"
 #include "launch.cuh"
+#include "umma_ptx.cuh"
 
 namespace tts {
 
 namespace {
 
+using namespace ptx;
+
+constexpr int kWarps = 8, kThreads = 32 * kWarps;
+constexpr int kPair = 2 * kKv8Record;                               // a warp works on two pages at a time
 constexpr float kFar = -1e30f;                                      // "no key yet": finite, so that differences are never NaN
 constexpr float kSlack = 8.f;                                       // log2 of how far a score may exceed the running maximum
 constexpr int kRoom = 6;                                            // p sv is held times 2^kRoom
 
-// Warps of a CTA and pages that each has in its ring, for up to 8 kNB rows, and the shared memory (bytes).  The sums of O take
-// 32 kNB registers a thread: with one group of rows 12 warps fit the register file, else 8.
+// Pairs of pages that a warp has in its ring, for up to 8 kNB rows, and the shared memory (bytes).
 template <int kNB>
 struct Lay {
-    static constexpr int kWarps = kNB == 1 ? 12 : 8, kThreads = kWarps * 32;
-    static constexpr int kStages = kNB == 1 ? 3 : kNB == 2 ? 5 : 4;
-    static constexpr int kOffQ = kWarps * kStages * kKv8Record;     // (behind the ring) [rows][256]: fp16 rows, 16-byte chunks exchanged (q_place)
+    static constexpr int kStages = kNB == 1 ? 3 : 2;
+    // the join: 16-byte chunks of a row and round, threads to a row
+    static constexpr int kRounds = kNB == 2 ? 1 : 2;                // the warps' sums are joined all dims at once, or half of them twice
+    static constexpr int kOffQ = kWarps * kStages * kPair;              // (behind the ring) [rows][256]: fp16 rows, 16-byte chunks exchanged (q_place)
+    static constexpr int kChunks = 32 / kRounds, kPerRow = kNB <= 2 ? 16 : 8;
     static constexpr int kRows = kNB * 8;
     static constexpr int kOffMask = kOffQ + kRows * 256;            // [rows] which of the branch's last rows each row sees
     static constexpr int kOffFactor = kOffMask + kRows * 8;         // [rows] what a row's scores are multiplied by
     static constexpr int kOffRowAt = kOffFactor + kRows * 4;        // [rows] (branch, row, head) of the results, as one number
     static constexpr int kOffMl = kOffRowAt + kRows * 4;            // [warps][rows] (maximum, sum)
-    static constexpr int kOffTotal = kOffMl + kWarps * kRows * 8;   // [rows] of all warps
-    static constexpr int kOffBack = kOffTotal + kRows * 8;          // [warps][rows] what a warp's sums are multiplied by
-    static constexpr int kOffExp = kOffBack + kWarps * kRows * 4;   // [warps] exponent of the sums' unit; then a flag
+    static constexpr int kOffExp = kOffMl + kWarps * kRows * 8;   // [warps] exponent of the sums' unit; then a flag
     static constexpr int kOffCum = kOffExp + 64;                    // [branches + 1] units before each branch
-    static constexpr int kOffJoin = kOffCum + (kMaxBranches + 8) * 8;   // [warps][rows][64] floats
-    static constexpr int kBytes = kOffJoin + kWarps * kRows * 64 * 4;
+    static constexpr int kOffJoin = kOffCum + (kMaxBranches + 8) * 8;   // [warps][rows][128 / rounds] floats
+    static constexpr int kOffBar = kOffJoin + kWarps * kRows * kHeadDim / kRounds * 4;   // [warps][stages]
+    static constexpr int kOffAbort = kOffBar + kWarps * kStages * 8;   // [0] flag; [1 ..] scratch of each warp
+    static constexpr int kBytes = kOffAbort + (1 + kWarps) * 4 + 12;
     static_assert(kBytes <= 232448 && kOffJoin % 16 == 0 && kWarps * 4 + 4 <= 64, "shared memory of a CTA");
 };
 
+// Where chunk c of row r of a warp's sums lies: rows 2 t of the four t of a lane's group, and two groups, hit eight different bank groups.
+template <int kRounds>
+__device__ __forceinline__ int join_place(int c, int r) { const int t = (r & 7) >> 1; return c ^ (kRounds == 1 ? t : (t & 1) << 2 | t >> 1); }
 // Where chunk (u, t) of a row of Q lies (8 halves: dims 32 t + 8 u ..), so that the lanes of a quarter warp, two rows and
 // four t of one u, read eight different bank groups.
 __device__ __forceinline__ int q_place(int u, int t, int row) { return (u * 4 + t) ^ ((row & 1) << 2); }
 
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-// 16 bytes to shared memory, asynchronously; zeros where `there` is false
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int kLeft> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
 
 __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -77,7 +82,6 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
-__device__ __forceinline__ float exp2_approx(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 __device__ __forceinline__ float log2_approx(float x) { float y; asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 __device__ __forceinline__ uint64_t pack2(float a, float b) { uint64_t r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
 __device__ __forceinline__ float2 unpack2(uint64_t v) { float2 r; asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v)); return r; }
@@ -90,9 +94,6 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
-
-// A place in the list of units: unit `page` of item `item` (KV head * n_rb + row block) of branch b.
-struct Place { int b, item, page, units, tokens; };
 
 // Tokens of a branch; a bad length raises the status and counts as an empty branch.
 __device__ __forceinline__ int branch_tokens(const Kv8AttnParams& p, int b, bool raise) {
@@ -107,7 +108,6 @@ __device__ __forceinline__ int branch_tokens(const Kv8AttnParams& p, int b, bool
 __device__ __forceinline__ int units_of(int tokens) { return max(1, (tokens + kPage - 1) / kPage); }
 
 // Units before each branch (per KV head and row block together), in 64 bits; all threads of the block.
-template <int kThreads>
 __device__ void scan_units(const Kv8AttnParams& p, long long* cum, long long* warp_sums) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, per = p.Hkv * p.n_rb;
     long long carry = 0;
@@ -135,75 +135,87 @@ __device__ void scan_units(const Kv8AttnParams& p, long long* cum, long long* wa
     __syncthreads();
 }
 
-__device__ __forceinline__ void load_branch(const Kv8AttnParams& p, Place& at) {
-    at.tokens = branch_tokens(p, at.b, false);
-    at.units = units_of(at.tokens);
-}
-__device__ Place place_of(const Kv8AttnParams& p, const long long* cum, long long unit) {
-    int lo = 0, hi = p.n_branches - 1;                              // the last branch that starts at or before the unit
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (cum[mid] <= unit) lo = mid; else hi = mid - 1;
+// The pieces of a CTA's run, one after another, each its part of an item (KV head * n_rb + row block) of a branch.
+struct Walk {
+    int b, item;
+    int units, tokens;      // of the branch
+    int page, pages;        // first page of the piece, pages
+    int left;               // units of the run from the piece on
+    int nth;                // number of the piece
+    __device__ void init(const Kv8AttnParams& p, const long long* cum, long long begin, int n) {
+        int lo = 0, hi = p.n_branches - 1;                          // the last branch that starts at or before the unit
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (cum[mid] <= begin) lo = mid; else hi = mid - 1;
+        }
+        b = lo; left = n; nth = 0;
+        tokens = branch_tokens(p, b, false); units = units_of(tokens);
+        const unsigned within = (unsigned)(begin - cum[lo]);       // (of one branch: below 2^31)
+        item = (int)(within / (unsigned)units);
+        page = (int)(within - (unsigned)item * (unsigned)units);
+        pages = min(units - page, left);
     }
-    Place at;
-    at.b = lo;
-    load_branch(p, at);
-    const unsigned within = (unsigned)(unit - cum[lo]);            // (of one branch: below 2^31)
-    at.item = (int)(within / (unsigned)at.units);
-    at.page = (int)(within - (unsigned)at.item * (unsigned)at.units);
-    return at;
-}
-// `n` units further (the caller knows that they are there)
-__device__ __forceinline__ void advance(const Kv8AttnParams& p, Place& at, int n) {
-    at.page += n;
-    while (at.page >= at.units) {
-        at.page -= at.units;
-        if (++at.item == p.Hkv * p.n_rb) { at.item = 0; ++at.b; load_branch(p, at); }
+    __device__ __forceinline__ bool next(const Kv8AttnParams& p) {
+        left -= pages;
+        if (left <= 0) return false;
+        ++nth; page = 0;
+        if (++item == p.Hkv * p.n_rb) { item = 0; ++b; tokens = branch_tokens(p, b, false); units = units_of(tokens); }
+        pages = min(units, left);
+        return true;
     }
-}
+    __device__ __forceinline__ int pairs() const { return (pages + 1) >> 1; }
+};
 
-// S^T = K Q^T of one page: s[n][j], j: (token a or b) * 2 + (row 2 t or 2 t + 1)
+// S^T = K Q^T of two pages: s[page][n][j], j: (token a or b) * 2 + (row 2 t or 2 t + 1)
 template <int kFormat, int kNB>
-__device__ __forceinline__ void scores(const unsigned char* rec, const unsigned char* q_rows, int g, int t, float (&s)[kNB][4]) {
+__device__ __forceinline__ void scores(const unsigned char* pair, const unsigned char* q_rows, int g, int t, float (&s)[2][kNB][4]) {
     const int tok_a = 4 * (g >> 1) + (g & 1), tok_b = tok_a + 2;    // both have chunk_place g
-    uint4 xa[2], xb[2];
+#pragma unroll
+    for (int pg = 0; pg < 2; ++pg)
+#pragma unroll
+        for (int n = 0; n < kNB; ++n)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[pg][n][j] = 0.f;
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
         const int place = ((2 * t + c) ^ g) * 16;
-        xa[c] = *reinterpret_cast<const uint4*>(rec + tok_a * kHeadDim + place);
-        xb[c] = *reinterpret_cast<const uint4*>(rec + tok_b * kHeadDim + place);
-    }
+        uint4 xa[2], xb[2];
 #pragma unroll
-    for (int n = 0; n < kNB; ++n)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) s[n][j] = 0.f;
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-        const uint32_t wa[4] = {xa[c].x, xa[c].y, xa[c].z, xa[c].w}, wb[4] = {xb[c].x, xb[c].y, xb[c].z, xb[c].w};
+        for (int pg = 0; pg < 2; ++pg) {
+            xa[pg] = *reinterpret_cast<const uint4*>(pair + pg * kKv8Record + tok_a * kHeadDim + place);
+            xb[pg] = *reinterpret_cast<const uint4*>(pair + pg * kKv8Record + tok_b * kHeadDim + place);
+        }
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            uint32_t a[2][4];
+            uint32_t a[2][2][4];
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const uint32_t x = kv8_biased<kFormat>(wa[2 * half + k]), y = kv8_biased<kFormat>(wb[2 * half + k]);
-                a[k][0] = kv8_decode2<kFormat>(x, 0); a[k][2] = kv8_decode2<kFormat>(x, 1);
-                a[k][1] = kv8_decode2<kFormat>(y, 0); a[k][3] = kv8_decode2<kFormat>(y, 1);
-            }
+            for (int pg = 0; pg < 2; ++pg)
 #pragma unroll
-            for (int n = 0; n < kNB; ++n) {
-                const uint4 q = *reinterpret_cast<const uint4*>(q_rows + (n * 8 + g) * 256 + q_place(2 * c + half, t, g) * 16);
-                mma(s[n], a[0][0], a[0][1], a[0][2], a[0][3], q.x, q.y);
-                mma(s[n], a[1][0], a[1][1], a[1][2], a[1][3], q.z, q.w);
-            }
+                for (int k = 0; k < 2; ++k) {
+                    const uint32_t x = kv8_biased<kFormat>(half == 0 ? (k == 0 ? xa[pg].x : xa[pg].y) : (k == 0 ? xa[pg].z : xa[pg].w));
+                    const uint32_t y = kv8_biased<kFormat>(half == 0 ? (k == 0 ? xb[pg].x : xb[pg].y) : (k == 0 ? xb[pg].z : xb[pg].w));
+                    a[pg][k][0] = kv8_decode2<kFormat>(x, 0); a[pg][k][2] = kv8_decode2<kFormat>(x, 1);
+                    a[pg][k][1] = kv8_decode2<kFormat>(y, 0); a[pg][k][3] = kv8_decode2<kFormat>(y, 1);
+                }
+            uint4 q[kNB];
+#pragma unroll
+            for (int n = 0; n < kNB; ++n) q[n] = *reinterpret_cast<const uint4*>(q_rows + (n * 8 + g) * 256 + q_place(2 * c + half, t, g) * 16);
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int n = 0; n < kNB; ++n)
+#pragma unroll
+                    for (int pg = 0; pg < 2; ++pg)
+                        mma(s[pg][n], a[pg][k][0], a[pg][k][1], a[pg][k][2], a[pg][k][3], k == 0 ? q[n].x : q[n].z, k == 0 ? q[n].y : q[n].w);
         }
     }
 }
 
 template <int kFormat, int kNB>
-__global__ void __launch_bounds__(Lay<kNB>::kThreads, 1)
+__global__ void __launch_bounds__(kThreads, 1)
 kv8_attn_kernel(const __grid_constant__ Kv8AttnParams p) {
     using L = Lay<kNB>;
-    constexpr int kWarps = L::kWarps, kThreads = L::kThreads, kStages = L::kStages, kRows = L::kRows;
+    constexpr int kStages = L::kStages, kRows = L::kRows;
     extern __shared__ __align__(128) unsigned char smem[];
     long long* cum = reinterpret_cast<long long*>(smem + L::kOffCum);
     unsigned char* q_rows = smem + L::kOffQ;
@@ -211,51 +223,86 @@ kv8_attn_kernel(const __grid_constant__ Kv8AttnParams p) {
     float* factors = reinterpret_cast<float*>(smem + L::kOffFactor);
     int* row_at = reinterpret_cast<int*>(smem + L::kOffRowAt);
     float2* ml = reinterpret_cast<float2*>(smem + L::kOffMl);
-    float2* totals = reinterpret_cast<float2*>(smem + L::kOffTotal);
-    float* backs = reinterpret_cast<float*>(smem + L::kOffBack);
     int* exps = reinterpret_cast<int*>(smem + L::kOffExp);
     float* join = reinterpret_cast<float*>(smem + L::kOffJoin);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
 
+    if (threadIdx.x < kWarps * kStages) mbar_init(smem_u32(smem + L::kOffBar) + threadIdx.x * 8, 1);
+    if (threadIdx.x == 0) *reinterpret_cast<int*>(smem + L::kOffAbort) = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_proxy_async();
     grid_dependency_wait();
     grid_launch_dependents();
-    scan_units<kThreads>(p, cum, reinterpret_cast<long long*>(join));
+    scan_units(p, cum, reinterpret_cast<long long*>(join));
     const long long total = cum[p.n_branches];
-    const long long per_cta = max((long long)kWarps, (total + gridDim.x - 1) / gridDim.x);       // at least a page for each warp
-    const long long begin = (long long)blockIdx.x * per_cta;
-    if (begin >= total) return;
-    const int n_units = (int)min(total - begin, per_cta);           // (at most 2^26 pages of 1024 branches x 128 heads x 2 row blocks over 148 CTAs)
+    // A contiguous run of at least two pages for each warp; or, where there are no more items than CTAs and none has more than eight pages
+    // for a warp, an item each: joining parts takes about as long as four pages.
+    const long long per_cta = max(2ll * kWarps, (total + gridDim.x - 1) / gridDim.x);
+    long long begin = (long long)blockIdx.x * per_cta;
+    int n_units = (int)min(max(total - begin, 0ll), per_cta);       // (fits: the host refuses more than 2^31 units to a CTA)
+    const int per_branch = p.Hkv * p.n_rb;
+    if (p.n_branches * per_branch <= (int)gridDim.x) {
+        bool large = false;
+        for (int b = threadIdx.x; b < p.n_branches; b += kThreads) large |= cum[b + 1] - cum[b] > 8ll * kWarps * per_branch;
+        if (!__syncthreads_or(large)) {
+            const int b = blockIdx.x / per_branch;
+            n_units = b < p.n_branches ? (int)((cum[b + 1] - cum[b]) / per_branch) : 0;
+            if (b < p.n_branches) begin = cum[b] + (long long)(blockIdx.x - b * per_branch) * n_units;
+        }
+    }
+    if (n_units <= 0) return;
 
-    // ---- the warp's own pages: begin + warp, + 8, ..; `next` runs kStages ahead of the work
-    unsigned char* ring = smem + warp * kStages * kKv8Record;
-    Place next = place_of(p, cum, begin + min(warp, n_units - 1));
-    int next_unit = warp;                                           // (counted from `begin`, as all units below)
-    int next_page = -1;                                             // of the pool, asked for one copy ahead
-    auto look_up = [&]() {
+    // ---- the warp's own pairs: of all pairs of the run's pieces, laid end to end, warp, warp + 8, ..; `ahead` runs kStages ahead
+    unsigned char* ring = smem + warp * kStages * kPair;
+    const uint32_t bars = smem_u32(smem + L::kOffBar) + warp * kStages * 8;
+    volatile int* flags = reinterpret_cast<volatile int*>(smem + L::kOffAbort);
+    const Abort ab{flags, p.status};
+    bool alive = true;                                              // no wait has run out; else the work goes on with whatever is there
+    Walk item, ahead;
+    item.init(p, cum, begin, n_units);
+    ahead = item;
+    int ahead_pair = warp;
+    bool more = true;
+    int next_page = -1;                                             // lanes 0 and 1: the pool's page, asked for one copy ahead
+    unsigned flying = 0, phases = 0;                                // bit of a stage: a copy into it has not been waited for; its barrier's phase
+    auto look_up = [&]() {                                          // where the next pair is
+        while (ahead_pair >= ahead.pairs()) {
+            ahead_pair -= ahead.pairs();
+            more = ahead.next(p);
+            if (!more) return;
+        }
+        const int page = 2 * ahead_pair + lane;                     // (of the piece)
         next_page = -1;
-        if (next_unit < n_units && next.page * kPage < next.tokens) next_page = p.block_table[(size_t)next.b * p.max_blocks + next.page];
+        if (lane < 2 && page < ahead.pages && (ahead.page + page) * kPage < ahead.tokens)
+            next_page = p.block_table[(size_t)ahead.b * p.max_blocks + ahead.page + page];
     };
-    auto copy = [&](int stage) {                                    // the page that was looked up, and on to the one after it
-        if (next_unit < n_units) {
-            const bool there = next_page >= 0 && next_page < p.num_pages;
-            if (!there && next.page * kPage < next.tokens && lane == 0) atomicMin(p.status, (int)TTS_ERR_DEVICE_BOUNDS);
-            const unsigned char* src = p.pool + ((size_t)(there ? next_page : 0) * p.Hkv + next.item / p.n_rb) * kKv8Record + lane * 16;
-            const uint32_t dst = smem_u32(ring + stage * kKv8Record) + lane * 16;
-#pragma unroll
-            for (int i = 0; i < kKv8Record / 512; ++i) copy16(dst + i * 512, src + i * 512, there);
-            if (lane < (kKv8Record % 512) / 16) copy16(dst + kKv8Record / 512 * 512, src + kKv8Record / 512 * 512, there);
-            next_unit += kWarps;
-            if (next_unit < n_units) advance(p, next, kWarps);
+    auto copy = [&](int stage) {                                    // the pair that was looked up, and on to the one after it
+        if (more && alive) {
+            unsigned char* dst = ring + stage * kPair;
+            const uint32_t bar = bars + stage * 8;
+            const bool wanted = lane < 2 && 2 * ahead_pair + lane < ahead.pages && (ahead.page + 2 * ahead_pair + lane) * kPage < ahead.tokens;
+            const bool there = next_page >= 0 && next_page < p.num_pages && wanted;
+            const unsigned good = __ballot_sync(0xffffffffu, there), bad = __ballot_sync(0xffffffffu, wanted && !there);
+            if (bad) {                                              // a page outside the pool counts as zeros
+                if (lane == 0) atomicMin(p.status, (int)TTS_ERR_DEVICE_BOUNDS);
+                for (int i = lane; i < kPair / 16; i += 32)
+                    if (bad >> (i >= kKv8Record / 16) & 1) *reinterpret_cast<uint4*>(dst + i * 16) = make_uint4(0, 0, 0, 0);
+                fence_proxy_async();                                // (before a later copy into the stage)
+                __syncwarp();
+            }
+            if (lane == 0) { if (good) mbar_arrive_expect_tx(bar, __popc(good) * kKv8Record); else mbar_arrive(bar); }
+            __syncwarp();
+            if (there) bulk_load(smem_u32(dst) + lane * kKv8Record, p.pool + ((size_t)next_page * p.Hkv + ahead.item / p.n_rb) * kKv8Record, kKv8Record, bar);
+            flying |= 1u << stage;
+            ahead_pair += kWarps;
             look_up();
         }
-        copy_commit();
     };
     look_up();
-#pragma unroll
+#pragma unroll 1
     for (int i = 0; i < kStages; ++i) copy(i);
-    int stage = 0;
+    int stage = 0, pairs_before = 0;                                // pairs of the run before the piece
 
-    Place item = place_of(p, cum, begin);                           // the item that is worked on, at its first unit here
     // rows warp, warp + kWarps, .. of the item's queries (4 dims a lane), asked for ahead
     constexpr int kQPer = (kRows + kWarps - 1) / kWarps;
     uint2 q_raw[kQPer];
@@ -269,11 +316,10 @@ kv8_attn_kernel(const __grid_constant__ Kv8AttnParams p) {
         }
     };
     ask_q();
-    int unit = 0;
-    for (int nth = 0; unit < n_units; ++nth) {
+    for (bool more_items = true; more_items;) {
         const int h = item.item / p.n_rb, rb = item.item - h * p.n_rb, b = item.b;
         const int row0 = rb * p.rb_rows, rows = min(p.rb_rows, p.nr - row0), tokens = item.tokens, units = item.units;
-        const int item_begin = unit - item.page, stop = min(n_units, item_begin + units);
+        const int page0 = item.page, pages = item.pages, pairs = item.pairs(), nth = item.nth;
         const int tail = tokens - p.R;                              // the first of the branch's last R tokens (may be negative)
 
         // ---- Q, scaled to fp16 by the power of two that puts a row's largest at 2^14
@@ -326,82 +372,101 @@ kv8_attn_kernel(const __grid_constant__ Kv8AttnParams p) {
                 for (int j = 0; j < 4; ++j) o[d][n][j] = 0.f;
         }
 
-        // ---- this warp's pages of the item; the next page's scores are under way while a page's probabilities are formed
-        const int first_unit = unit + (warp - unit % kWarps + kWarps) % kWarps;
-        float s[kNB][4];
-        // the page in the ring's stage `at`: it has come, and what it holds beyond the branch's end is made harmless (the codes of V;
-        // K's are never looked at, for their scores are replaced)
-        auto arrive = [&](auto behind, int at, int left) {           // (copies behind it that may be in flight)
-            copy_wait<decltype(behind)::value>();
-            __syncwarp();
-            if (left < kPage) {
-                unsigned char* rec = ring + at * kKv8Record;
-                for (int r = max(0, left); r < kPage; ++r) {
-                    if (lane < 8) *reinterpret_cast<uint4*>(rec + kKv8Codes + r * kHeadDim + lane * 16) = make_uint4(0, 0, 0, 0);
-                    if (lane < 2) reinterpret_cast<float*>(rec + 2 * kKv8Codes)[lane * kPage + r] = 0.f;
+        // ---- this warp's pairs of the piece
+        for (int u = (warp - pairs_before % kWarps + kWarps) % kWarps; u < pairs; u += kWarps) {
+            const int first = (page0 + 2 * u) * kPage;              // the first token
+            const int left = min(tokens - first, min(2, pages - 2 * u) * kPage);       // tokens here, at most 32 (may be 0)
+            unsigned char* pair = ring + stage * kPair;
+            if (flying >> stage & 1) {
+                alive = alive && mbar_wait(bars + stage * 8, phases >> stage & 1, ab);
+                alive = __all_sync(0xffffffffu, alive);
+                if (alive) { flying &= ~(1u << stage); phases ^= 1u << stage; }
+            }
+            const bool masked = first + 2 * kPage > tail || left < 2 * kPage;
+            if (left < 2 * kPage) {                                 // what is not there is made harmless: V's codes and all scales (K's scores are replaced)
+                for (int r = max(0, left); r < 2 * kPage; ++r) {
+                    unsigned char* rec = pair + (r >> 4) * kKv8Record;
+                    if (lane < 8) *reinterpret_cast<uint4*>(rec + kKv8Codes + (r & 15) * kHeadDim + lane * 16) = make_uint4(0, 0, 0, 0);
+                    if (lane < 2) reinterpret_cast<float*>(rec + 2 * kKv8Codes)[lane * kPage + (r & 15)] = 0.f;
                 }
+                fence_proxy_async();                                // (before the next copy into the stage)
                 __syncwarp();
             }
-        };
-        if (first_unit < stop) {
-            arrive(std::integral_constant<int, kStages - 1>{}, stage, tokens - (first_unit - item_begin) * kPage);
-            scores<kFormat, kNB>(ring + stage * kKv8Record, q_rows, g, t, s);
-        }
-        for (int u = first_unit; u < stop; u += kWarps) {
-            const int first = (u - item_begin) * kPage, left = tokens - first;       // the page's first token; tokens from it on
-            const unsigned char* rec = ring + stage * kKv8Record;
-            const int after = stage + 1 == kStages ? 0 : stage + 1;
+            float s[2][kNB][4];
+            scores<kFormat, kNB>(pair, q_rows, g, t, s);
             const int tok_a = 4 * (g >> 1) + (g & 1), tok_b = tok_a + 2;
-            const float* scales = reinterpret_cast<const float*>(rec + 2 * kKv8Codes);
-            const float ka = scales[tok_a], kb = scales[tok_b], va = scales[kPage + tok_a], vb = scales[kPage + tok_b];
-            // d: scores less the running maximum, in log2 units, [row group][token a, b] of rows 2 t and 2 t + 1
-            float2 d[kNB][2];
-            uint64_t x[kNB][2];
-            const uint64_t ka2 = pack2(ka, ka), kb2 = pack2(kb, kb);
+            float sk[2][2], sv[2][2];                               // [page][token a, b]
 #pragma unroll
-            for (int n = 0; n < kNB; ++n) {
-                x[n][0] = mul2(pack2(s[n][0], s[n][1]), ka2); x[n][1] = mul2(pack2(s[n][2], s[n][3]), kb2);
-                d[n][0] = unpack2(fma2(x[n][0], factor[n], neg_m[n])); d[n][1] = unpack2(fma2(x[n][1], factor[n], neg_m[n]));
+            for (int pg = 0; pg < 2; ++pg) {
+                const float* scales = reinterpret_cast<const float*>(pair + pg * kKv8Record + 2 * kKv8Codes);
+                sk[pg][0] = scales[tok_a]; sk[pg][1] = scales[tok_b]; sv[pg][0] = scales[kPage + tok_a]; sv[pg][1] = scales[kPage + tok_b];
             }
-            unsigned seen = ~0u;                                    // bit 4 n + 2 (token b) + (row 2 t + 1)
-            const bool masked = first + kPage > tail;
-            if (masked) {
-                seen = 0;
+            // d: scores less the running maximum, in log2 units, [page][row group][token a, b] of rows 2 t and 2 t + 1
+            float2 d[2][kNB][2];
+            uint64_t x[2][kNB][2];
+            float over = -INFINITY;
+#pragma unroll
+            for (int pg = 0; pg < 2; ++pg)
 #pragma unroll
                 for (int n = 0; n < kNB; ++n)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int tok = j < 2 ? tok_a : tok_b, a = first + tok - tail;
-                        if (tok < left && (a < 0 || (a < 64 && (masks[n * 8 + 2 * t + (j & 1)] >> a & 1)))) seen |= 1u << (4 * n + j);
-                        else if (j & 1) d[n][j >> 1].y = -INFINITY;
-                        else d[n][j >> 1].x = -INFINITY;
+                    for (int j = 0; j < 2; ++j) {
+                        x[pg][n][j] = mul2(pack2(s[pg][n][2 * j], s[pg][n][2 * j + 1]), pack2(sk[pg][j], sk[pg][j]));
+                        d[pg][n][j] = unpack2(fma2(x[pg][n][j], factor[n], neg_m[n]));
                     }
-            }
-            float over = -INFINITY;
+            unsigned seen = ~0u;                                    // bit 16 page + 4 n + 2 (token b) + (row 2 t + 1)
+            if (masked) {
+                seen = 0;
 #pragma unroll
-            for (int n = 0; n < kNB; ++n) over = fmaxf(over, fmaxf(fmaxf(d[n][0].x, d[n][0].y), fmaxf(d[n][1].x, d[n][1].y)));
-            if (__any_sync(0xffffffffu, over > kSlack || fmaxf(va, vb) >= unit_end)) {
+                for (int pg = 0; pg < 2; ++pg)
+#pragma unroll
+                    for (int n = 0; n < kNB; ++n)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const int tok = pg * kPage + (j < 2 ? tok_a : tok_b), a = first + tok - tail;
+                            if (tok < left && (a < 0 || (a < 64 && (masks[n * 8 + 2 * t + (j & 1)] >> a & 1)))) seen |= 1u << (16 * pg + 4 * n + j);
+                            else if (j & 1) d[pg][n][j >> 1].y = -INFINITY;
+                            else d[pg][n][j >> 1].x = -INFINITY;
+                        }
+            }
+#pragma unroll
+            for (int pg = 0; pg < 2; ++pg)
+#pragma unroll
+                for (int n = 0; n < kNB; ++n) over = fmaxf(over, fmaxf(fmaxf(d[pg][n][0].x, d[pg][n][0].y), fmaxf(d[pg][n][1].x, d[pg][n][1].y)));
+            const float sv_top = fmaxf(fmaxf(sv[0][0], sv[0][1]), fmaxf(sv[1][0], sv[1][1]));
+            if (__any_sync(0xffffffffu, over > kSlack || sv_top >= unit_end)) {
                 // ---- seldom: the maximum moves, or the unit (the largest exponent in sv so far; a NaN or an infinity is not a unit)
-                const int ea = __float_as_int(va) >> 23 & 255, eb = __float_as_int(vb) >> 23 & 255;
-                const int e = max(unit_exp, __reduce_max_sync(0xffffffffu, max(ea == 255 ? 0 : ea, eb == 255 ? 0 : eb)));
+                int ev = 0;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) { const int e = __float_as_int(sv[k >> 1][k & 1]) >> 23 & 255; ev = max(ev, e == 255 ? 0 : e); }
+                const int e = max(unit_exp, __reduce_max_sync(0xffffffffu, ev));
                 const float unit_back = unit_exp - e < -126 ? 0.f : power_of_two(unit_exp - e);
                 unit_exp = e; unit_end = __int_as_float((e + 1) << 23); up = power_of_two(kRoom + 127 - e);
 #pragma unroll
                 for (int n = 0; n < kNB; ++n) {
-                    const float2 xa = unpack2(mul2(x[n][0], factor[n])), xb = unpack2(mul2(x[n][1], factor[n])), old = unpack2(neg_m[n]);
-                    const float v[4] = {seen >> (4 * n) & 1 ? xa.x : -INFINITY, seen >> (4 * n + 1) & 1 ? xa.y : -INFINITY,
-                                        seen >> (4 * n + 2) & 1 ? xb.x : -INFINITY, seen >> (4 * n + 3) & 1 ? xb.y : -INFINITY};
-                    float neg[2], back[2];
+                    const float2 old = unpack2(neg_m[n]);
+                    float v[2][4], neg[2], back[2];
+#pragma unroll
+                    for (int pg = 0; pg < 2; ++pg) {
+                        const float2 xa = unpack2(mul2(x[pg][n][0], factor[n])), xb = unpack2(mul2(x[pg][n][1], factor[n]));
+                        const float y[4] = {xa.x, xa.y, xb.x, xb.y};
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) v[pg][j] = seen >> (16 * pg + 4 * n + j) & 1 ? y[j] : -INFINITY;
+                    }
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        float top = fmaxf(v[j], v[2 + j]);
+                        float top = fmaxf(fmaxf(v[0][j], v[0][2 + j]), fmaxf(v[1][j], v[1][2 + j]));
 #pragma unroll
                         for (int i = 4; i < 32; i <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, i));
                         const float was = j ? old.y : old.x;
                         neg[j] = fminf(was, -top);
-                        back[j] = exp2_approx(neg[j] - was);
+                        back[j] = ex2(neg[j] - was);
                     }
-                    d[n][0] = make_float2(v[0] + neg[0], v[1] + neg[1]); d[n][1] = make_float2(v[2] + neg[0], v[3] + neg[1]);
+#pragma unroll
+                    for (int pg = 0; pg < 2; ++pg) {
+                        d[pg][n][0] = make_float2(v[pg][0] + neg[0], v[pg][1] + neg[1]);
+                        d[pg][n][1] = make_float2(v[pg][2] + neg[0], v[pg][3] + neg[1]);
+                    }
                     neg_m[n] = pack2(neg[0], neg[1]);
                     l[n] = mul2(l[n], pack2(back[0], back[1]));
 #pragma unroll
@@ -410,54 +475,57 @@ kv8_attn_kernel(const __grid_constant__ Kv8AttnParams p) {
                         for (int j = 0; j < 4; ++j) o[i][n][j] *= back[j & 1] * unit_back;
                 }
             }
-            if (u + kWarps < stop) {
-                arrive(std::integral_constant<int, kStages - 2>{}, after, left - kWarps * kPage);
-                scores<kFormat, kNB>(ring + after * kKv8Record, q_rows, g, t, s);
-            }
-            const float fa = va * up, fb = vb * up;
-            const uint64_t fa2 = pack2(fa, fa), fb2 = pack2(fb, fb);
-            uint32_t pb[kNB][2];                                    // P^T as the B operand: tokens 4 t, 4 t + 1 and 4 t + 2, 4 t + 3 of row g
+            uint32_t pb[2][kNB][2];                                 // P^T as the B operand: tokens 4 t, 4 t + 1 and 4 t + 2, 4 t + 3 of row g
 #pragma unroll
-            for (int n = 0; n < kNB; ++n)
+            for (int pg = 0; pg < 2; ++pg)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    const uint64_t e = pack2(exp2_approx(d[n][j].x), exp2_approx(d[n][j].y));
-                    l[n] = add2(l[n], e);
-                    float2 w = unpack2(mul2(e, j ? fb2 : fa2));
-                    if (masked) {                                   // a hidden token's scale may be a NaN
-                        if (!(seen >> (4 * n + 2 * j) & 1)) w.x = 0.f;
-                        if (!(seen >> (4 * n + 2 * j + 1) & 1)) w.y = 0.f;
+                    const float f = sv[pg][j] * up;
+                    const uint64_t f2 = pack2(f, f);
+#pragma unroll
+                    for (int n = 0; n < kNB; ++n) {
+                        const uint64_t e = pack2(ex2(d[pg][n][j].x), ex2(d[pg][n][j].y));
+                        l[n] = add2(l[n], e);
+                        float2 w = unpack2(mul2(e, f2));
+                        if (masked) {                               // a hidden token's scale may be a NaN
+                            if (!(seen >> (16 * pg + 4 * n + 2 * j) & 1)) w.x = 0.f;
+                            if (!(seen >> (16 * pg + 4 * n + 2 * j + 1) & 1)) w.y = 0.f;
+                        }
+                        pb[pg][n][j] = transpose8x8(pack_half2(w.x, w.y));
                     }
-                    pb[n][j] = transpose8x8(pack_half2(w.x, w.y));
                 }
             // O^T += V^T P^T: four bytes (tokens 4 t ..) of dims 2 e, 2 e + 1 of the lane's 16 make the A operand of tile e
-            uint4 v[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                v[j] = *reinterpret_cast<const uint4*>(rec + kKv8Codes + (4 * t + j) * kHeadDim + (g ^ ((j & 1) | 2 * t)) * 16);
+            for (int pg = 0; pg < 2; ++pg) {
+                uint4 v[4];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                uint32_t y[4];
+                for (int j = 0; j < 4; ++j)
+                    v[j] = *reinterpret_cast<const uint4*>(pair + pg * kKv8Record + kKv8Codes + (4 * t + j) * kHeadDim + (g ^ ((j & 1) | 2 * t)) * 16);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) y[j] = kv8_biased<kFormat>(q == 0 ? v[j].x : q == 1 ? v[j].y : q == 2 ? v[j].z : v[j].w);
+                for (int q = 0; q < 4; ++q) {
+                    uint32_t y[4];
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const uint32_t lo = __byte_perm(y[0], y[1], half ? 0x7362 : 0x5140), hi = __byte_perm(y[2], y[3], half ? 0x7362 : 0x5140);
-                    const uint32_t a0 = kv8_decode2<kFormat>(lo, 0), a1 = kv8_decode2<kFormat>(lo, 1), a2 = kv8_decode2<kFormat>(hi, 0), a3 = kv8_decode2<kFormat>(hi, 1);
+                    for (int j = 0; j < 4; ++j) y[j] = kv8_biased<kFormat>(q == 0 ? v[j].x : q == 1 ? v[j].y : q == 2 ? v[j].z : v[j].w);
 #pragma unroll
-                    for (int n = 0; n < kNB; ++n) mma(o[2 * q + half][n], a0, a1, a2, a3, pb[n][0], pb[n][1]);
+                    for (int half = 0; half < 2; ++half) {
+                        const uint32_t lo = __byte_perm(y[0], y[1], half ? 0x7362 : 0x5140), hi = __byte_perm(y[2], y[3], half ? 0x7362 : 0x5140);
+                        const uint32_t a0 = kv8_decode2<kFormat>(lo, 0), a1 = kv8_decode2<kFormat>(lo, 1), a2 = kv8_decode2<kFormat>(hi, 0), a3 = kv8_decode2<kFormat>(hi, 1);
+#pragma unroll
+                        for (int n = 0; n < kNB; ++n) mma(o[2 * q + half][n], a0, a1, a2, a3, pb[pg][n][0], pb[pg][n][1]);
+                    }
                 }
             }
-            __syncwarp();                                           // all lanes have read the page
+            __syncwarp();                                           // all lanes have read the pair
             copy(stage);
-            stage = after;
+            stage = stage + 1 == kStages ? 0 : stage + 1;
         }
 
-        // ---- join the warps: of every row the maximum and the sum, and from them what each warp's O is multiplied by
-        const bool whole = item.page == 0 && stop == item_begin + units;
-        const long long item0 = begin + item_begin;
-        if (stop < n_units) { advance(p, item, stop - unit); ask_q(); }
-        unit = stop;
+        // ---- join the warps: maxima, sums and O of every row
+        const bool whole = pages == units;
+        const long long item0 = begin + (n_units - item.left) - page0;
+        pairs_before += pairs;
+        more_items = item.next(p);
+        if (more_items) ask_q();
 #pragma unroll
         for (int n = 0; n < kNB; ++n) {
             const float2 sums = unpack2(l[n]), neg = unpack2(neg_m[n]);
@@ -467,20 +535,6 @@ kv8_attn_kernel(const __grid_constant__ Kv8AttnParams p) {
             if (g == 0) *reinterpret_cast<float4*>(ml + warp * kRows + n * 8 + 2 * t) = make_float4(-neg.x, a, -neg.y, z);
         }
         if (lane == 0) exps[warp] = unit_exp;
-        __syncthreads();
-        if (threadIdx.x < kRows) {
-            const int r = threadIdx.x;
-            float top = kFar, sum = 0.f;
-#pragma unroll 4
-            for (int w = 0; w < kWarps; ++w) top = fmaxf(top, ml[w * kRows + r].x);
-#pragma unroll 4
-            for (int w = 0; w < kWarps; ++w) { const float2 x = ml[w * kRows + r]; sum += x.y * exp2_approx(x.x - top); }
-            totals[r] = make_float2(top, sum);
-            const float inv = sum == 0.f ? 0.f : 1.f / sum;         // (a row that saw nothing: m = kFar and l = 0 everywhere; zeros)
-#pragma unroll 4
-            for (int w = 0; w < kWarps; ++w) backs[w * kRows + r] = exp2_approx(ml[w * kRows + r].x - top) * inv * power_of_two(exps[w] - 127 - kRoom);
-        }
-        __syncthreads();
         const int slot = 2 * blockIdx.x + (nth == 0 ? 0 : 1);       // a CTA leaves parts of its first and of its last item only
         auto write_out = [&](int r, int dim, const float4& x) {
             const size_t at = (size_t)row_at[r] * kHeadDim + dim;
@@ -493,88 +547,112 @@ kv8_attn_kernel(const __grid_constant__ Kv8AttnParams p) {
         auto write_lse = [&](int r, float top, float sum) {         // natural logarithm
             p.lse[row_at[r]] = sum == 0.f ? -INFINITY : (top + log2_approx(sum)) * 0.6931471805599453f;
         };
-        float2 back[kNB];
-#pragma unroll
-        for (int n = 0; n < kNB; ++n) back[n] = *reinterpret_cast<const float2*>(backs + warp * kRows + n * 8 + 2 * t);
+        // kPerRow threads to a row: what each warp's sums are multiplied by
+        const int r = threadIdx.x / L::kPerRow, c0 = threadIdx.x % L::kPerRow;
+        float back[kWarps];
 #pragma unroll 1
-        for (int round = 0; round < 2; ++round) {                   // dims 16 g + 8 round .. + 7 of every g
+        for (int round = 0; round < L::kRounds; ++round) {          // all dims, or 16 g + 8 round .. + 7 of every g
             auto put = [&](auto half) {
                 constexpr int kHalf = decltype(half)::value;
 #pragma unroll
                 for (int n = 0; n < kNB; ++n)
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        float4* to = reinterpret_cast<float4*>(join + ((warp * kNB + n) * 8 + 2 * t + j) * 64 + g * 8);
-                        const float f = j ? back[n].y : back[n].x;
+                        const int row = n * 8 + 2 * t + j;
+                        float4* to = reinterpret_cast<float4*>(join + (warp * kRows + row) * (L::kChunks * 4));
 #pragma unroll
-                        for (int k = 0; k < 2; ++k) {
+                        for (int k = 0; k < 4 / L::kRounds; ++k) {
                             const float(&a)[4] = o[4 * kHalf + 2 * k][n], (&z)[4] = o[4 * kHalf + 2 * k + 1][n];
-                            to[k] = make_float4(a[j] * f, a[2 + j] * f, z[j] * f, z[2 + j] * f);
+                            to[join_place<L::kRounds>(g * (4 / L::kRounds) + k, row)] = make_float4(a[j], a[2 + j], z[j], z[2 + j]);
                         }
                     }
             };
-            if (round == 0) put(std::integral_constant<int, 0>{}); else put(std::integral_constant<int, 1>{});
+            if (round == 0) put(std::integral_constant<int, 0>{});
+            if constexpr (L::kRounds == 2) { if (round == 1) put(std::integral_constant<int, 1>{}); }
             __syncthreads();
-#pragma unroll 1
-            for (int i = threadIdx.x; i < rows * 16; i += kThreads) {
-                const int r = i >> 4, c = i & 15, dim = (c >> 1) * 16 + round * 8 + (c & 1) * 4;
-                float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (r < rows) {
+                if (round == 0) {
+                    float top = kFar, sum = 0.f;
+                    float2 x[kWarps];
 #pragma unroll
-                for (int w = 0; w < kWarps; ++w) {
-                    const float4 x = *reinterpret_cast<const float4*>(join + (w * kRows + r) * 64 + c * 4);
-                    sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
+                    for (int w = 0; w < kWarps; ++w) { x[w] = ml[w * kRows + r]; top = fmaxf(top, x[w].x); }
+#pragma unroll
+                    for (int w = 0; w < kWarps; ++w) { back[w] = ex2(x[w].x - top); sum += x[w].y * back[w]; }
+                    const float inv = sum == 0.f ? 0.f : 1.f / sum;      // (a row that saw nothing: m = kFar and l = 0 everywhere; zeros)
+#pragma unroll
+                    for (int w = 0; w < kWarps; ++w) back[w] *= inv * power_of_two(exps[w] - 127 - kRoom);
+                    if (c0 == 0) {
+                        if (!whole) p.part_ml[slot * kKv8MaxRows + r] = make_float2(top, sum);
+                        else if (p.lse) write_lse(r, top, sum);
+                    }
                 }
-                if (whole) write_out(r, dim, sum);
-                else *reinterpret_cast<float4*>(p.part_o + ((size_t)slot * kKv8MaxRows + r) * kHeadDim + dim) = sum;
+#pragma unroll 1
+                for (int c = c0; c < L::kChunks; c += L::kPerRow) {
+                    const int dim = L::kRounds == 1 ? c * 4 : (c >> 1) * 16 + round * 8 + (c & 1) * 4;
+                    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                    for (int w = 0; w < kWarps; ++w) {
+                        const float4 x = *reinterpret_cast<const float4*>(join + ((w * kRows + r) * L::kChunks + join_place<L::kRounds>(c, r)) * 4);
+                        sum.x = fmaf(x.x, back[w], sum.x); sum.y = fmaf(x.y, back[w], sum.y); sum.z = fmaf(x.z, back[w], sum.z); sum.w = fmaf(x.w, back[w], sum.w);
+                    }
+                    if (whole) write_out(r, dim, sum);
+                    else *reinterpret_cast<float4*>(p.part_o + ((size_t)slot * kKv8MaxRows + r) * kHeadDim + dim) = sum;
+                }
             }
-            if (round == 0) __syncthreads();
+            __syncthreads();
         }
-        if (threadIdx.x < rows) {
-            const int r = threadIdx.x;
-            if (!whole) p.part_ml[slot * kKv8MaxRows + r] = totals[r];
-            else if (p.lse) write_lse(r, totals[r].x, totals[r].y);
-        }
-        __syncthreads();
         if (!whole) {
             // ---- the last CTA to leave a part of the item joins them all
             const int cta0 = (int)(item0 / per_cta), parts = (int)((item0 + units - 1) / per_cta) - cta0 + 1;
             const size_t id = ((size_t)b * p.Hkv + h) * p.n_rb + rb;
             if (threadIdx.x == 0) {
-                __threadfence();                                    // the block's writes, which the barrier put before this
-                const bool last = atomicAdd(p.arrived + id, 1u) + 1 == (unsigned)parts;
+                // (releases the block's writes, which the barrier put before it, and acquires the others')
+                unsigned before;
+                asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(before) : "l"(p.arrived + id) : "memory");
+                const bool last = before + 1 == (unsigned)parts;
                 if (last) p.arrived[id] = 0;                        // as the next call expects it
-                __threadfence();
                 exps[kWarps] = last;
             }
             __syncthreads();
             if (exps[kWarps]) {
                 // a part is the first item of its CTA unless it starts the item behind the CTA's first unit
                 auto slot_of = [&](int k) { return 2 * (cta0 + k) + (k == 0 && item0 != cta0 * per_cta ? 1 : 0); };
-#pragma unroll 1
-                for (int i = threadIdx.x; i < rows * 32; i += kThreads) {
-                    const int r = i >> 5, dim = (i & 31) * 4;       // a warp takes a row
-                    float top = kFar;
-                    for (int k = lane; k < parts; k += 32) top = fmaxf(top, __ldcg(p.part_ml + slot_of(k) * kKv8MaxRows + r).x);
+                if (r < rows) {
+                    float top = kFar, sum = 0.f;
+                    float4 acc[32 / L::kPerRow];
 #pragma unroll
-                    for (int x = 16; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-                    float sum = 0.f;
-                    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-                    for (int k = 0; k < parts; ++k) {
-                        const size_t at = (size_t)slot_of(k) * kKv8MaxRows + r;
-                        const float2 x = __ldcg(p.part_ml + at);
-                        const float4 y = __ldcg(reinterpret_cast<const float4*>(p.part_o + at * kHeadDim + dim));
-                        const float w = x.y * exp2_approx(x.x - top);
-                        sum += w;
-                        acc.x += w * y.x; acc.y += w * y.y; acc.z += w * y.z; acc.w += w * y.w;
+                    for (int x = 0; x < 32 / L::kPerRow; ++x) acc[x] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+                    for (int k = 0; k < parts; ++k) {               // (a running maximum: parts are few)
+                        const size_t from = (size_t)slot_of(k) * kKv8MaxRows + r;
+                        const float2 x = __ldcg(p.part_ml + from);
+                        float4 y[32 / L::kPerRow];
+#pragma unroll
+                        for (int i = 0; i < 32 / L::kPerRow; ++i) y[i] = __ldcg(reinterpret_cast<const float4*>(p.part_o + from * kHeadDim) + c0 + i * L::kPerRow);
+                        const float now = fmaxf(top, x.x), keep = ex2(top - now), w = x.y * ex2(x.x - now);
+                        top = now; sum = sum * keep + w;
+#pragma unroll
+                        for (int i = 0; i < 32 / L::kPerRow; ++i) {
+                            acc[i].x = acc[i].x * keep + w * y[i].x; acc[i].y = acc[i].y * keep + w * y[i].y;
+                            acc[i].z = acc[i].z * keep + w * y[i].z; acc[i].w = acc[i].w * keep + w * y[i].w;
+                        }
                     }
                     const float inv = sum == 0.f ? 0.f : 1.f / sum;
-                    write_out(r, dim, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
-                    if (p.lse && lane == 0) write_lse(r, top, sum);
+#pragma unroll
+                    for (int i = 0; i < 32 / L::kPerRow; ++i)
+                        write_out(r, (c0 + i * L::kPerRow) * 4, make_float4(acc[i].x * inv, acc[i].y * inv, acc[i].z * inv, acc[i].w * inv));
+                    if (p.lse && c0 == 0) write_lse(r, top, sum);
                 }
             }
             __syncthreads();                                        // Q, the masks and the sums are free again
         }
+    }
+    // after a wait that ran out: copies in flight land before the CTA ends
+    if (!alive) {
+        flags[1 + warp] = 0;
+        const Abort quiet{flags + 1 + warp, p.status};
+        for (int i = 0; i < kStages; ++i)
+            if (flying >> i & 1) mbar_wait(bars + i * 8, phases >> i & 1, quiet);
     }
 }
 
@@ -586,15 +664,11 @@ cudaError_t launch_kv8_attn(const Kv8AttnParams& p, int format, cudaStream_t st)
         auto kernel = kv8_attn_kernel<kFormat, kNB>;
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Lay<kNB>::kBytes);
         if (e != cudaSuccess) return e;
-        return launch_dependent(kernel, p.grid, Lay<kNB>::kThreads, Lay<kNB>::kBytes, st, p);
+        return launch_dependent(kernel, p.grid, kThreads, Lay<kNB>::kBytes, st, p);
     };
     auto by_rows = [&](auto fmt) {
-        switch ((p.rb_rows + 7) / 8) {
-            case 1: return launch(fmt, std::integral_constant<int, 1>{});
-            case 2: return launch(fmt, std::integral_constant<int, 2>{});
-            case 3: return launch(fmt, std::integral_constant<int, 3>{});
-            default: return launch(fmt, std::integral_constant<int, 4>{});
-        }
+        return p.rb_rows <= 8 ? launch(fmt, std::integral_constant<int, 1>{})
+             : p.rb_rows <= 16 ? launch(fmt, std::integral_constant<int, 2>{}) : launch(fmt, std::integral_constant<int, 3>{});
     };
     return format == TTS_KV8_E4M3 ? by_rows(std::integral_constant<int, TTS_KV8_E4M3>{}) : by_rows(std::integral_constant<int, TTS_KV8_INT8>{});
 }

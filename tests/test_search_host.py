@@ -132,7 +132,11 @@ def test_kernels_that_start_early_read_coherently(name):
     assert "launch_dependent(" in source and not re.search(r"__restrict__|__ldg\(|ld\.global\.nc", source)
 
 
-def test_the_attention_over_the_8bit_cache_waits_for_nothing_but_its_own_copies():
-    """No flag or barrier of another block is polled, so there is no wait that would need a limit."""
+def test_every_wait_of_the_attention_over_the_8bit_cache_is_bounded():
+    """A warp waits for its own copies alone, through mbar_wait, which has the limit; a warp that gave up works on to the block's barriers, and
+    waits in the end for what it has in flight with a word of its own."""
     source = (Path(tts.library_path()).parent / "csrc" / "kv8_attn.cu").read_text()
-    assert not re.search(r"while\s*\(.*(volatile|atomic|ld\.acquire)|try_wait|mbarrier", source)
+    code = "\n".join(line.split("//")[0] for line in source.splitlines())
+    assert code.count("mbar_wait(") == 2 and not re.search(r"try_wait|test_wait|barrier\.cta|bar\.sync", code)
+    assert re.findall(r"Abort quiet\{(flags \+ [^,]*),", code) == ["flags + 1 + warp"]
+    assert "break" not in code[code.index("for (bool more_items"):code.index("if (!alive)")].replace("if (r >= kRows) break", "")
