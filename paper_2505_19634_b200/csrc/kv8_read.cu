@@ -2,7 +2,7 @@
 //
 // Bound by HBM: 4224 bytes in and 8192 out per page and KV head, each touched once.  A warp takes one of them: K and V
 // are 128 chunks of 16 codes each, so a lane has eight loads of 16 bytes and the scales of its tokens in flight before it
-// stores; a lane's 16 values are one 32-byte sector, written by one instruction.
+// stores; a lane's 16 values are one 32-byte sector, written by one instruction where the pools start on such a boundary.
 #include "kv8.cuh"
 #include "launch.cuh"
 
@@ -20,6 +20,7 @@ kv8_read_kernel(const __grid_constant__ Kv8ReadParams p) {
     grid_dependency_wait();
     grid_launch_dependents();
     const int lane = threadIdx.x & 31;
+    const bool wide = ((reinterpret_cast<uintptr_t>(p.k_pages) | reinterpret_cast<uintptr_t>(p.v_pages)) & 31) == 0;
     const long total = (long)p.n * p.Hkv;
     for (long w = (blockIdx.x * (long)kThreads + threadIdx.x) >> 5; w < total; w += (long)gridDim.x * (kThreads / 32)) {
         const int i = (int)(w / p.Hkv), h = (int)(w - (long)i * p.Hkv);
@@ -50,8 +51,13 @@ kv8_read_kernel(const __grid_constant__ Kv8ReadParams p) {
                 }
             }
             uint4* to = reinterpret_cast<uint4*>((k < 4 ? p.k_pages : p.v_pages) + (((size_t)d * p.Hkv + h) * kPage + t) * kHeadDim + 16 * c);
-            __stcs(to, make_uint4(out[0], out[1], out[2], out[3]));
-            __stcs(to + 1, make_uint4(out[4], out[5], out[6], out[7]));
+            if (wide) {
+                asm volatile("st.global.cs.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(out[0]), "r"(out[1]), "r"(out[2]), "r"(out[3]), "r"(out[4]),
+                             "r"(out[5]), "r"(out[6]), "r"(out[7]) : "memory");
+            } else {
+                __stcs(to, make_uint4(out[0], out[1], out[2], out[3]));
+                __stcs(to + 1, make_uint4(out[4], out[5], out[6], out[7]));
+            }
         }
     }
 }

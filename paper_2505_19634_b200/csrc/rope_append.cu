@@ -13,7 +13,8 @@
 // lanes handle one head vector, each two 16-byte chunks that hold both members of its pairs, so a rotation
 // needs no exchange between lanes; a lane's eight sines and cosines serve all heads of the row that its
 // warp walks through, sixteen at a time, whose loads are issued before the row's branch, page and angles are
-// looked up.
+// looked up.  Keys and values of the 8-bit cache come behind the queries, four at a time: their codes cost a division each, which
+// sixteen times over in the code would be registers and instructions for the queries to wait for.
 #include <type_traits>
 
 #include "kv8.cuh"
@@ -91,7 +92,7 @@ __device__ __forceinline__ void store_codes(unsigned char* record, bool is_v, in
 // A warp takes one row and every parts-th group of four head vectors of it; with few rows several warps share
 // a row, so that small calls still fill the GPU.
 template <int kMode, int kFormat>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 3)
 append_rope_kernel(const __grid_constant__ RopeParams p) {
     __shared__ double turns[kHeadDim / 2];              // inv_freq / (2 pi)
     __shared__ int axis_of[kHeadDim / 2];
@@ -122,13 +123,15 @@ append_rope_kernel(const __grid_constant__ RopeParams p) {
                  : h < p.Hq + p.Hkv ? p.k + (size_t)row * p.kv_stride + (size_t)(h - p.Hq) * kHeadDim
                                     : p.v + (size_t)row * p.kv_stride + (size_t)(h - p.Hq - p.Hkv) * kHeadDim;
         };
+        // those that are read ahead and walked through in batches: all, or the queries
+        const int ahead = kFormat == kBf16Pages ? vectors : p.Hq;
         uint4 lo4[kBatch], hi4[kBatch];
         auto load = [&](int h0) {                       // kBatch head vectors per group of eight lanes, before anything else is waited for
 #pragma unroll
             for (int i = 0; i < kBatch; ++i) {
                 const int h = h0 + i * step + group;
                 lo4[i] = hi4[i] = make_uint4(0, 0, 0, 0);
-                if (h < vectors) {
+                if (h < ahead) {
                     const uint4* src = reinterpret_cast<const uint4*>(source(h));
                     lo4[i] = src[sub]; hi4[i] = src[sub + 8];
                 }
@@ -181,7 +184,7 @@ append_rope_kernel(const __grid_constant__ RopeParams p) {
         }
         auto store = [&](int h, const uint4& lo, const uint4& hi) {
             const bool is_q = h < p.Hq, is_v = h >= p.Hq + p.Hkv;
-            if (h >= vectors || (!is_q && (kFormat != kBf16Pages || !store_kv))) return;
+            if (h >= ahead || (!is_q && !store_kv)) return;
             uint4* dst = is_q ? reinterpret_cast<uint4*>(p.q_out + ((size_t)row * p.Hq + h) * kHeadDim)
                               : reinterpret_cast<uint4*>((is_v ? p.v_pages : p.k_pages) +
                                                          ((((size_t)page * p.Hkv + h - p.Hq - (is_v ? p.Hkv : 0)) * kPage + (size_t)(tok % kPage)) * kHeadDim));
@@ -228,39 +231,58 @@ append_rope_kernel(const __grid_constant__ RopeParams p) {
             }
             continue;
         }
-        for (int h0 = part * 4; h0 < vectors; h0 += kBatch * step) {
+        auto turn = [&](float (&lo)[8], float (&hi)[8]) {
+            if (kMode == 0) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const float a = lo[k], z = hi[k];
+                    lo[k] = a * cs[k] - z * sn[k];
+                    hi[k] = a * sn[k] + z * cs[k];
+                }
+            } else if (kMode == 1) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float a = lo[2 * k], z = lo[2 * k + 1], d = hi[2 * k], e = hi[2 * k + 1];
+                    if (4 * sub + k < p.n_pairs) {
+                        lo[2 * k] = a * cs[k] - z * sn[k];
+                        lo[2 * k + 1] = a * sn[k] + z * cs[k];
+                    }
+                    if (32 + 4 * sub + k < p.n_pairs) {
+                        hi[2 * k] = d * cs[4 + k] - e * sn[4 + k];
+                        hi[2 * k + 1] = d * sn[4 + k] + e * cs[4 + k];
+                    }
+                }
+            }
+        };
+        for (int h0 = part * 4; h0 < ahead; h0 += kBatch * step) {
             if (h0 > part * 4) load(h0);
 #pragma unroll
             for (int i = 0; i < kBatch; ++i) {
                 const int h = h0 + i * step + group;
-                float lo[8], hi[8];
-                unpack(lo4[i], lo); unpack(hi4[i], hi);
-                if (kMode != 3 && h < p.Hq + p.Hkv) {
-                    if (kMode == 0) {
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            const float a = lo[k], z = hi[k];
-                            lo[k] = a * cs[k] - z * sn[k];
-                            hi[k] = a * sn[k] + z * cs[k];
-                        }
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const float a = lo[2 * k], z = lo[2 * k + 1], d = hi[2 * k], e = hi[2 * k + 1];
-                            if (4 * sub + k < p.n_pairs) {
-                                lo[2 * k] = a * cs[k] - z * sn[k];
-                                lo[2 * k + 1] = a * sn[k] + z * cs[k];
-                            }
-                            if (32 + 4 * sub + k < p.n_pairs) {
-                                hi[2 * k] = d * cs[4 + k] - e * sn[4 + k];
-                                hi[2 * k + 1] = d * sn[4 + k] + e * cs[4 + k];
-                            }
-                        }
-                    }
+                if (h < p.Hq + p.Hkv) {
+                    float lo[8], hi[8];
+                    unpack(lo4[i], lo); unpack(hi4[i], hi);
+                    turn(lo, hi);
                     lo4[i] = pack(lo); hi4[i] = pack(hi);
                 }
                 store(h, lo4[i], hi4[i]);
-                if (kFormat != kBf16Pages && h0 + i * step + 3 >= p.Hq && h0 + i * step < vectors) store_kv8(h, lo, hi);
+            }
+        }
+        if constexpr (kFormat != kBf16Pages) {
+            auto fetch = [&](int h, uint4& a, uint4& z) {
+                a = z = make_uint4(0, 0, 0, 0);
+                if (h < vectors) { const uint4* src = reinterpret_cast<const uint4*>(source(h)); a = src[sub]; z = src[sub + 8]; }
+            };
+            uint4 a4, z4;
+            fetch(p.Hq + part * 4 + group, a4, z4);
+#pragma unroll 1
+            for (int h0 = p.Hq + part * 4; h0 < vectors; h0 += step) {
+                const int h = h0 + group;
+                float lo[8], hi[8];
+                unpack(a4, lo); unpack(z4, hi);
+                fetch(h + step, a4, z4);
+                if (h < p.Hq + p.Hkv) turn(lo, hi);
+                store_kv8(h, lo, hi);
             }
         }
     }
