@@ -133,8 +133,10 @@ cudaError_t cache_alloc(Ctx* c) {
     const size_t nb = f.max_branches, np = f.num_pages;
     cudaError_t e = cudaMalloc(&c->page_work, 16 + nb * sizeof(int4) + align16(nb * 4) + 2 * align16(np * 4));
     // attention over the 8-bit cache: two partial results for each CTA, a counter for each (branch, KV head, row block)
-    const size_t slots = 2 * (size_t)c->n_sms * kKv8MaxRows;
-    const size_t items = nb * f.n_kv_heads * ceil_div(f.max_rows_per_branch * (f.n_q_heads / f.n_kv_heads), kKv8MaxRows);
+    // (rows of a call with few per KV head; 128 for each of twice as many CTAs where calls may have more)
+    const int nr = f.max_rows_per_branch * (f.n_q_heads / f.n_kv_heads);
+    const size_t slots = 2 * (size_t)c->n_sms * (nr < kKv8WideFrom ? kKv8MaxRows : 2 * kKv8WideRows);
+    const size_t items = nb * f.n_kv_heads * ceil_div(nr, kKv8MaxRows);
     if (e == cudaSuccess) e = cudaMalloc(&c->kv8_part_o, slots * kHeadDim * sizeof(float));
     if (e == cudaSuccess) e = cudaMalloc(&c->kv8_part_ml, slots * sizeof(float2));
     c->kv8_arrived_bytes = items * sizeof(unsigned);

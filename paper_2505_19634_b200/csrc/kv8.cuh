@@ -61,14 +61,16 @@ struct Kv8AttnParams {
     const int32_t *block_table, *branch_lens, *tree_parents;
     void* out;
     float* lse;
-    float* part_o;                     // [2 * grid][24][128] normalised partial results
-    float2* part_ml;                   // [2 * grid][24] their maximum (log2 units) and sum
+    float* part_o;                     // [2 * grid][24 or 128 rows][128] normalised partial results
+    float2* part_ml;                   // [2 * grid][24 or 128] their maximum (log2 units) and sum
     unsigned* arrived;                 // [branch][KV head][row block] parts written so far; zero between calls
     int32_t* status;
     int Hq, Hkv, G, R, nr, n_rb, rb_rows, prefix_len, n_branches, max_blocks, num_pages, out_dtype, grid;
     float scale_log2;
 };
-constexpr int kKv8MaxRows = 24;        // rows of one KV head that a block works on at a time
+constexpr int kKv8MaxRows = 24;        // rows of one KV head that a block of kv8_attn.cu works on at a time
+constexpr int kKv8WideRows = 128;      // and one of kv8_attn_wide.cu, which takes over
+constexpr int kKv8WideFrom = 40;       // from this many rows on
 struct Kv8ReadParams {
     const unsigned char* pool;
     const int32_t *src, *dst;
@@ -77,6 +79,7 @@ struct Kv8ReadParams {
     int n, Hkv, num_pages, num_dst;
 };
 cudaError_t launch_kv8_attn(const Kv8AttnParams& p, int format, cudaStream_t st);
+cudaError_t launch_kv8_attn_wide(const Kv8AttnParams& p, int format, cudaStream_t st);
 cudaError_t launch_kv8_read(const Kv8ReadParams& p, int format, int n_sms, cudaStream_t st);
 
 }  // namespace tts

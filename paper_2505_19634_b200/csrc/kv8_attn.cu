@@ -24,7 +24,7 @@
 
 #include <type_traits>
 
-#include "kv8.cuh"
+#include "kv8_run.cuh"
 #include "launch.cuh"
 #include "umma_ptx.cuh"
 
@@ -95,76 +95,10 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
     return r;
 }
 
-// Tokens of a branch; a bad length raises the status and counts as an empty branch.
-__device__ __forceinline__ int branch_tokens(const Kv8AttnParams& p, int b, bool raise) {
-    const int L = p.branch_lens[b];
-    const long n = (long)p.prefix_len + L;
-    if (L < 0 || n > (long)p.max_blocks * kPage) {
-        if (raise) atomicMin(p.status, (int)TTS_ERR_DEVICE_BOUNDS);
-        return 0;
-    }
-    return (int)n;
-}
-__device__ __forceinline__ int units_of(int tokens) { return max(1, (tokens + kPage - 1) / kPage); }
-
-// Units before each branch (per KV head and row block together), in 64 bits; all threads of the block.
-__device__ void scan_units(const Kv8AttnParams& p, long long* cum, long long* warp_sums) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, per = p.Hkv * p.n_rb;
-    long long carry = 0;
-    for (int base = 0; base < p.n_branches; base += kThreads) {
-        const int b = base + threadIdx.x;
-        long long v = b < p.n_branches ? (long long)units_of(branch_tokens(p, b, blockIdx.x == 0)) * per : 0;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const long long n = __shfl_up_sync(0xffffffffu, v, o);
-            if (lane >= o) v += n;
-        }
-        if (lane == 31) warp_sums[warp] = v;
-        __syncthreads();
-        long long before = carry, all = 0;
-#pragma unroll
-        for (int w = 0; w < kThreads / 32; ++w) {
-            if (w < warp) before += warp_sums[w];
-            all += warp_sums[w];
-        }
-        if (b < p.n_branches) cum[b + 1] = before + v;
-        carry += all;
-        __syncthreads();
-    }
-    if (threadIdx.x == 0) cum[0] = 0;
-    __syncthreads();
-}
-
-// The pieces of a CTA's run, one after another, each its part of an item (KV head * n_rb + row block) of a branch.
-struct Walk {
-    int b, item;
-    int units, tokens;      // of the branch
-    int page, pages;        // first page of the piece, pages
-    int left;               // units of the run from the piece on
-    int nth;                // number of the piece
-    __device__ void init(const Kv8AttnParams& p, const long long* cum, long long begin, int n) {
-        int lo = 0, hi = p.n_branches - 1;                          // the last branch that starts at or before the unit
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (cum[mid] <= begin) lo = mid; else hi = mid - 1;
-        }
-        b = lo; left = n; nth = 0;
-        tokens = branch_tokens(p, b, false); units = units_of(tokens);
-        const unsigned within = (unsigned)(begin - cum[lo]);       // (of one branch: below 2^31)
-        item = (int)(within / (unsigned)units);
-        page = (int)(within - (unsigned)item * (unsigned)units);
-        pages = min(units - page, left);
-    }
-    __device__ __forceinline__ bool next(const Kv8AttnParams& p) {
-        left -= pages;
-        if (left <= 0) return false;
-        ++nth; page = 0;
-        if (++item == p.Hkv * p.n_rb) { item = 0; ++b; tokens = branch_tokens(p, b, false); units = units_of(tokens); }
-        pages = min(units, left);
-        return true;
-    }
-    __device__ __forceinline__ int pairs() const { return (pages + 1) >> 1; }
-};
+// An item's start and end (queries, join of the warps) take about as long as so many pages (kv8_run.cuh).  64 single tokens of 1024 to
+// 8192 keys: 120 us, 125 with 16, 137 with none; a drafted step of 20 rows 55.5, 56.3, 57.3.
+constexpr int kItemUnits = 48;
+using Walk = Kv8Walk<kPage, kItemUnits>;
 
 // S^T = K Q^T of two pages: s[page][n][j], j: (token a or b) * 2 + (row 2 t or 2 t + 1)
 template <int kFormat, int kNB>
@@ -233,23 +167,12 @@ kv8_attn_kernel(const __grid_constant__ Kv8AttnParams p) {
     fence_proxy_async();
     grid_dependency_wait();
     grid_launch_dependents();
-    scan_units(p, cum, reinterpret_cast<long long*>(join));
-    const long long total = cum[p.n_branches];
+    kv8_scan_units<kThreads, kPage, kItemUnits>(p, cum, reinterpret_cast<long long*>(join));
     // A contiguous run of at least two pages for each warp; or, where there are no more items than CTAs and none has more than eight pages
     // for a warp, an item each: joining parts takes about as long as four pages.
-    const long long per_cta = max(2ll * kWarps, (total + gridDim.x - 1) / gridDim.x);
-    long long begin = (long long)blockIdx.x * per_cta;
-    int n_units = (int)min(max(total - begin, 0ll), per_cta);       // (fits: the host refuses more than 2^31 units to a CTA)
-    const int per_branch = p.Hkv * p.n_rb;
-    if (p.n_branches * per_branch <= (int)gridDim.x) {
-        bool large = false;
-        for (int b = threadIdx.x; b < p.n_branches; b += kThreads) large |= cum[b + 1] - cum[b] > 8ll * kWarps * per_branch;
-        if (!__syncthreads_or(large)) {
-            const int b = blockIdx.x / per_branch;
-            n_units = b < p.n_branches ? (int)((cum[b + 1] - cum[b]) / per_branch) : 0;
-            if (b < p.n_branches) begin = cum[b] + (long long)(blockIdx.x - b * per_branch) * n_units;
-        }
-    }
+    const Kv8Run run = kv8_run<kThreads, kItemUnits>(p, cum, 2 * kWarps, 8 * kWarps);
+    const long long begin = run.begin, per_cta = run.per_cta;
+    const int n_units = run.n;
     if (n_units <= 0) return;
 
     // ---- the warp's own pairs: of all pairs of the run's pieces, laid end to end, warp, warp + 8, ..; `ahead` runs kStages ahead
@@ -259,28 +182,29 @@ kv8_attn_kernel(const __grid_constant__ Kv8AttnParams p) {
     const Abort ab{flags, p.status};
     bool alive = true;                                              // no wait has run out; else the work goes on with whatever is there
     Walk item, ahead;
-    item.init(p, cum, begin, n_units);
+    if (!item.init(p, cum, begin, n_units)) return;
     ahead = item;
     int ahead_pair = warp;
     bool more = true;
     int next_page = -1;                                             // lanes 0 and 1: the pool's page, asked for one copy ahead
     unsigned flying = 0, phases = 0;                                // bit of a stage: a copy into it has not been waited for; its barrier's phase
+    auto pairs_of = [](const Walk& w) { return (w.n + 1) >> 1; };
     auto look_up = [&]() {                                          // where the next pair is
-        while (ahead_pair >= ahead.pairs()) {
-            ahead_pair -= ahead.pairs();
+        while (ahead_pair >= pairs_of(ahead)) {
+            ahead_pair -= pairs_of(ahead);
             more = ahead.next(p);
             if (!more) return;
         }
         const int page = 2 * ahead_pair + lane;                     // (of the piece)
         next_page = -1;
-        if (lane < 2 && page < ahead.pages && (ahead.page + page) * kPage < ahead.tokens)
-            next_page = p.block_table[(size_t)ahead.b * p.max_blocks + ahead.page + page];
+        if (lane < 2 && page < ahead.n && (ahead.first + page) * kPage < ahead.tokens)
+            next_page = p.block_table[(size_t)ahead.b * p.max_blocks + ahead.first + page];
     };
     auto copy = [&](int stage) {                                    // the pair that was looked up, and on to the one after it
         if (more && alive) {
             unsigned char* dst = ring + stage * kPair;
             const uint32_t bar = bars + stage * 8;
-            const bool wanted = lane < 2 && 2 * ahead_pair + lane < ahead.pages && (ahead.page + 2 * ahead_pair + lane) * kPage < ahead.tokens;
+            const bool wanted = lane < 2 && 2 * ahead_pair + lane < ahead.n && (ahead.first + 2 * ahead_pair + lane) * kPage < ahead.tokens;
             const bool there = next_page >= 0 && next_page < p.num_pages && wanted;
             const unsigned good = __ballot_sync(0xffffffffu, there), bad = __ballot_sync(0xffffffffu, wanted && !there);
             if (bad) {                                              // a page outside the pool counts as zeros
@@ -318,8 +242,8 @@ kv8_attn_kernel(const __grid_constant__ Kv8AttnParams p) {
     ask_q();
     for (bool more_items = true; more_items;) {
         const int h = item.item / p.n_rb, rb = item.item - h * p.n_rb, b = item.b;
-        const int row0 = rb * p.rb_rows, rows = min(p.rb_rows, p.nr - row0), tokens = item.tokens, units = item.units;
-        const int page0 = item.page, pages = item.pages, pairs = item.pairs(), nth = item.nth;
+        const int row0 = rb * p.rb_rows, rows = min(p.rb_rows, p.nr - row0), tokens = item.tokens;
+        const int page0 = item.first, pages = item.n, pairs = pairs_of(item), nth = item.nth;
         const int tail = tokens - p.R;                              // the first of the branch's last R tokens (may be negative)
 
         // ---- Q, scaled to fp16 by the power of two that puts a row's largest at 2^14
@@ -521,8 +445,8 @@ kv8_attn_kernel(const __grid_constant__ Kv8AttnParams p) {
         }
 
         // ---- join the warps: maxima, sums and O of every row
-        const bool whole = pages == units;
-        const long long item0 = begin + (n_units - item.left) - page0;
+        const bool whole = item.whole();
+        const Kv8Parts cut = kv8_parts(item, begin + (n_units - item.left), per_cta);
         pairs_before += pairs;
         more_items = item.next(p);
         if (more_items) ask_q();
@@ -603,28 +527,25 @@ kv8_attn_kernel(const __grid_constant__ Kv8AttnParams p) {
         }
         if (!whole) {
             // ---- the last CTA to leave a part of the item joins them all
-            const int cta0 = (int)(item0 / per_cta), parts = (int)((item0 + units - 1) / per_cta) - cta0 + 1;
             const size_t id = ((size_t)b * p.Hkv + h) * p.n_rb + rb;
             if (threadIdx.x == 0) {
                 // (releases the block's writes, which the barrier put before it, and acquires the others')
                 unsigned before;
                 asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(before) : "l"(p.arrived + id) : "memory");
-                const bool last = before + 1 == (unsigned)parts;
+                const bool last = before + 1 == (unsigned)cut.n;
                 if (last) p.arrived[id] = 0;                        // as the next call expects it
                 exps[kWarps] = last;
             }
             __syncthreads();
             if (exps[kWarps]) {
-                // a part is the first item of its CTA unless it starts the item behind the CTA's first unit
-                auto slot_of = [&](int k) { return 2 * (cta0 + k) + (k == 0 && item0 != cta0 * per_cta ? 1 : 0); };
                 if (r < rows) {
                     float top = kFar, sum = 0.f;
                     float4 acc[32 / L::kPerRow];
 #pragma unroll
                     for (int x = 0; x < 32 / L::kPerRow; ++x) acc[x] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 2
-                    for (int k = 0; k < parts; ++k) {               // (a running maximum: parts are few)
-                        const size_t from = (size_t)slot_of(k) * kKv8MaxRows + r;
+                    for (int k = 0; k < cut.n; ++k) {               // (a running maximum: parts are few)
+                        const size_t from = (size_t)cut.slot(k) * kKv8MaxRows + r;
                         const float2 x = __ldcg(p.part_ml + from);
                         float4 y[32 / L::kPerRow];
 #pragma unroll

@@ -1,0 +1,137 @@
+// How attention over the 8-bit cache is cut into work.
+//
+// An item is a (branch, KV head, block of stacked rows).  It has a unit for every kUnitTokens tokens (an empty branch's: one), behind
+// kStart units for what a piece of an item costs besides (queries, the join of its parts): so a CTA with many short items gets
+// fewer tokens.  All items follow one another, a CTA owns a contiguous run of units and walks over its pieces of items; what it has of
+// an item that others work on too it leaves as a part, and the last one to do so joins them.
+#pragma once
+#include "kv8.cuh"
+
+namespace tts {
+
+namespace {
+
+// Tokens of a branch; a bad length raises the status and counts as an empty branch.
+__device__ __forceinline__ int kv8_tokens(const Kv8AttnParams& p, int b, bool raise) {
+    const int L = p.branch_lens[b];
+    const long n = (long)p.prefix_len + L;
+    if (L < 0 || n > (long)p.max_blocks * kPage) {
+        if (raise) atomicMin(p.status, (int)TTS_ERR_DEVICE_BOUNDS);
+        return 0;
+    }
+    return (int)n;
+}
+template <int kUnitTokens, int kStart>
+__device__ __forceinline__ int kv8_units(int tokens) { return kStart + max(1, (tokens + kUnitTokens - 1) / kUnitTokens); }
+
+// Units before each branch (per KV head and row block together), in 64 bits; all threads of the block.
+template <int kThreads, int kUnitTokens, int kStart>
+__device__ void kv8_scan_units(const Kv8AttnParams& p, long long* cum, long long* warp_sums) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, per = p.Hkv * p.n_rb;
+    long long carry = 0;
+    for (int base = 0; base < p.n_branches; base += kThreads) {
+        const int b = base + threadIdx.x;
+        long long v = b < p.n_branches ? (long long)kv8_units<kUnitTokens, kStart>(kv8_tokens(p, b, blockIdx.x == 0)) * per : 0;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long n = __shfl_up_sync(0xffffffffu, v, o);
+            if (lane >= o) v += n;
+        }
+        if (lane == 31) warp_sums[warp] = v;
+        __syncthreads();
+        long long before = carry, all = 0;
+#pragma unroll
+        for (int w = 0; w < kThreads / 32; ++w) {
+            if (w < warp) before += warp_sums[w];
+            all += warp_sums[w];
+        }
+        if (b < p.n_branches) cum[b + 1] = before + v;
+        carry += all;
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) cum[0] = 0;
+    __syncthreads();
+}
+
+// The CTA's run: n units from `begin` on; all threads of the block.  At least `least` units of tokens; or, where there are no more items
+// than CTAs and none has more than `whole` units of tokens, an item each.
+struct Kv8Run { long long begin, per_cta; int n; };
+template <int kThreads, int kStart>
+__device__ __forceinline__ Kv8Run kv8_run(const Kv8AttnParams& p, const long long* cum, int least, int whole) {
+    const long long total = cum[p.n_branches];
+    Kv8Run r;
+    r.per_cta = max((long long)kStart + least, (total + gridDim.x - 1) / gridDim.x);
+    r.begin = (long long)blockIdx.x * r.per_cta;
+    r.n = (int)min(max(total - r.begin, 0ll), r.per_cta);           // (fits: the host refuses more than 2^31 units to a CTA)
+    const int per_branch = p.Hkv * p.n_rb;
+    if (p.n_branches * per_branch <= (int)gridDim.x) {
+        bool large = false;
+        for (int b = threadIdx.x; b < p.n_branches; b += kThreads) large |= cum[b + 1] - cum[b] > (long long)(kStart + whole) * per_branch;
+        if (!__syncthreads_or(large)) {
+            const int b = blockIdx.x / per_branch;
+            r.n = b < p.n_branches ? (int)((cum[b + 1] - cum[b]) / per_branch) : 0;
+            if (b < p.n_branches) r.begin = cum[b] + (long long)(blockIdx.x - b * per_branch) * r.n;
+        }
+    }
+    return r;
+}
+
+// The pieces of a CTA's run, one after another, each its part of an item (KV head * n_rb + row block) of a branch.
+template <int kUnitTokens, int kStart>
+struct Kv8Walk {
+    int b, item;
+    int units, tokens;      // of the branch
+    int from;               // first unit of the piece within its item
+    int first, n;           // its units of tokens
+    int left;               // units of the run from the piece on
+    int nth;                // number of the piece
+    __device__ __forceinline__ void cut() {
+        first = max(0, from - kStart);
+        n = max(0, min(units, from + left) - kStart) - first;
+    }
+    // false where the run has no tokens (its units are an item's start)
+    __device__ bool init(const Kv8AttnParams& p, const long long* cum, long long begin, int run) {
+        int lo = 0, hi = p.n_branches - 1;                          // the last branch that starts at or before the unit
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (cum[mid] <= begin) lo = mid; else hi = mid - 1;
+        }
+        b = lo; left = run; nth = 0;
+        tokens = kv8_tokens(p, b, false); units = kv8_units<kUnitTokens, kStart>(tokens);
+        const unsigned long long within = begin - cum[lo];
+        item = (int)(within / (unsigned)units);
+        from = (int)(within - (unsigned long long)item * (unsigned)units);
+        cut();
+        return n > 0;
+    }
+    __device__ __forceinline__ bool next(const Kv8AttnParams& p) {
+        left -= units - from;
+        if (left <= kStart) return false;                           // none of the next item's tokens
+        ++nth; from = 0;
+        if (++item == p.Hkv * p.n_rb) { item = 0; ++b; tokens = kv8_tokens(p, b, false); units = kv8_units<kUnitTokens, kStart>(tokens); }
+        cut();
+        return true;
+    }
+    __device__ __forceinline__ bool whole() const { return first == 0 && n == units - kStart; }
+    static constexpr int kItemStart = kStart;
+};
+
+// The parts of a piece's item, where others have some of it.  A CTA leaves parts of its first and of its last item only, in two
+// places of its own; only the first part of an item may be the last of its CTA's run.
+struct Kv8Parts {
+    int cta0, n;
+    bool behind;            // the item begins behind its first CTA's first unit
+    __device__ __forceinline__ int slot(int k) const { return 2 * (cta0 + k) + (k == 0 && behind ? 1 : 0); }
+};
+template <class Walk>
+__device__ __forceinline__ Kv8Parts kv8_parts(const Walk& w, long long piece, long long per_cta) {     // piece: its first unit
+    const long long item = piece - w.from, tokens = item + Walk::kItemStart;
+    Kv8Parts c;
+    c.cta0 = (int)(tokens / per_cta); c.n = (int)((item + w.units - 1) / per_cta) - c.cta0 + 1;
+    c.behind = item > c.cta0 * per_cta;
+    return c;
+}
+
+}  // namespace
+
+}  // namespace tts

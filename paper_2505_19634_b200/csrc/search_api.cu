@@ -104,9 +104,11 @@ int tts_kv8_attn(tts_ctx* ctx, int format, const void* q, int64_t q_row_stride, 
     const Span queries{q, ((rows - 1) * q_row_stride + (size_t)f.n_q_heads * kHeadDim) * 2}, pool{kv8_pages, kv8_bytes(f)},
         table{block_table, table_bytes(f, n_branches)}, lens{branch_lens, (size_t)n_branches * 4}, parents{tree_parents, tree_parents ? rows * 4 : 0},
         result{out, rows * f.n_q_heads * kHeadDim * (f.out_dtype == TTS_OUT_FP32 ? 4 : 2)}, logs{lse, lse ? rows * f.n_q_heads * 4 : 0};
-    // (units of a CTA are counted in 32 bits)
-    const int n_rb = ceil_div(rows_per_branch * (f.n_q_heads / f.n_kv_heads), kKv8MaxRows), grid = f.max_ctas > 0 && f.max_ctas < c->n_sms ? f.max_ctas : c->n_sms;
-    if ((double)n_branches * f.max_blocks_per_branch * f.n_kv_heads * n_rb / grid >= 2e9) return TTS_ERR_UNSUPPORTED;
+    const int nr = rows_per_branch * (f.n_q_heads / f.n_kv_heads);
+    const bool wide = nr >= kKv8WideFrom;
+    const int n_rb = ceil_div(nr, wide ? kKv8WideRows : kKv8MaxRows), most = wide ? 2 * c->n_sms : c->n_sms, grid = f.max_ctas > 0 && f.max_ctas < most ? f.max_ctas : most;
+    // (units of a CTA, pages and at most 64 more for each item, are counted in 32 bits)
+    if ((double)n_branches * (f.max_blocks_per_branch + 64.0) * f.n_kv_heads * n_rb / grid >= 2e9) return TTS_ERR_UNSUPPORTED;
     if (clash(result, {queries, pool, table, lens}) || (tree_parents && clash(result, {parents})) ||
         (lse && (clash(logs, {result, queries, pool, table, lens}) || (tree_parents && clash(logs, {parents})))))
         return TTS_ERR_INVALID;
@@ -117,12 +119,12 @@ int tts_kv8_attn(tts_ctx* ctx, int format, const void* q, int64_t q_row_stride, 
     p.q = static_cast<const __nv_bfloat16*>(q); p.q_stride = (long)q_row_stride; p.pool = static_cast<const unsigned char*>(kv8_pages);
     p.block_table = block_table; p.branch_lens = branch_lens; p.tree_parents = tree_parents; p.out = out; p.lse = lse;
     p.part_o = c->kv8_part_o; p.part_ml = c->kv8_part_ml; p.arrived = c->kv8_arrived; p.status = c->d_status;
-    p.Hq = f.n_q_heads; p.Hkv = f.n_kv_heads; p.G = p.Hq / p.Hkv; p.R = rows_per_branch; p.nr = p.R * p.G;
+    p.Hq = f.n_q_heads; p.Hkv = f.n_kv_heads; p.G = p.Hq / p.Hkv; p.R = rows_per_branch; p.nr = nr;
     p.n_rb = n_rb; p.rb_rows = ceil_div(p.nr, p.n_rb);
     p.prefix_len = prefix_len; p.n_branches = n_branches; p.max_blocks = f.max_blocks_per_branch; p.num_pages = f.num_pages; p.out_dtype = f.out_dtype;
     p.grid = grid;
     p.scale_log2 = (f.softmax_scale > 0.f ? f.softmax_scale : 1.0f / sqrtf((float)f.head_dim)) * 1.4426950408889634f;
-    return finish(c, launch_kv8_attn(p, format, c->stream), 1);
+    return finish(c, wide ? launch_kv8_attn_wide(p, format, c->stream) : launch_kv8_attn(p, format, c->stream), 1);
 }
 
 int tts_beam_reserve(tts_ctx* ctx, int max_rows, int max_select) {
