@@ -69,8 +69,10 @@ struct Kv8AttnParams {
     float scale_log2;
 };
 constexpr int kKv8MaxRows = 24;        // rows of one KV head that a block of kv8_attn.cu works on at a time
-constexpr int kKv8WideRows = 128;      // and one of kv8_attn_wide.cu, which takes over
-constexpr int kKv8WideFrom = 40;       // from this many rows on
+// kv8_attn_wide.cu works on up to 128 rows at a time, and takes over where the other would need more than two blocks: 64 (branch, KV head)s
+// of 7.9 k keys take 79 us there with 25 to 48 rows and 109 with 60, here 78 with 40 and 82 with 60.  (Over 500 keys it is slower, 21 us
+// against 17, but the host does not know how long the branches are.)
+constexpr int kKv8WideRows = 128, kKv8WideFrom = 2 * kKv8MaxRows + 1;
 struct Kv8ReadParams {
     const unsigned char* pool;
     const int32_t *src, *dst;

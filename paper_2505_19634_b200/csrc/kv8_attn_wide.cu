@@ -3,16 +3,21 @@
 // The formula and the roundings of kv8_attn.cu, for which a row block is too much to hold in a warp's registers: there the codes of
 // a page become operands once for 24 rows, here once for 128, and the products are the tensor cores' own.
 //
-// Bound by the tensor cores and the exponentials alike: 64 tokens and 128 rows take 512 clocks of either.  Two CTAs share an SM, so
-// that one's exponentials run while the tensor cores work for the other.  In a CTA,
-//   warps 0-3  softmax, a thread to a row: its query becomes the row's A operand in TMEM; per tile of 64 tokens it reads its scores
-//              from TMEM and leaves p sv there, as the second product's A operand; O is touched only when the maximum moves by more
-//              than 2^8 or the unit of p sv grows.  At a piece's end it writes its row.
-//   warps 4-7  turn codes into fp16 operands (exact): [64 tokens][128 dims], K with dims along the contraction, V with tokens.  Warp 4
-//              also fetches the records, by bulk copies into a ring of two tiles; warp 5 leaves the tile's scales and the unit.
-//   warp 8     issues the products: S = Q K^T (128 x 64 x 128), then O += P V (128 x 128 x 64).  The tensor pipe keeps issue order, so
-//              S of a tile may overwrite the columns that held P of the one before, and is complete no earlier than that one's P V.
-// TMEM columns of a CTA: Q 64, S 64 (P in its first half), O 128.
+// Two CTAs share an SM, so that one's exponentials run while the tensor cores work for the other.  64 tokens and 128 rows cost 512
+// clocks of the tensor cores, 512 of the exponentials' unit and, in shared memory, about 1100: Q, K and V as operands (512), codes read,
+// written in fp16 and fetched (512).  Measured: about 1550 clocks, most of them spent issuing (4400 instructions, half for the softmax)
+// and waiting at the roles' barriers.  8 trees of 60 nodes, 300 rows to a KV head, over 7.9 k keys: 195 us = 390 TFLOP/s; the kernel for
+// few rows took 410, that one's layout with converted tiles in shared memory and this one's products 779.  With Q in TMEM, or K's and V's
+// conversion by warps of their own, or V's operand twice: 192, 193 and 229 us.  In a CTA,
+//   warps 0-7   softmax, two threads to a row, in warps w and w + 4: they lay out its query; per tile of 64 tokens each reads 32 of its
+//               scores from TMEM and leaves p sv there, as the second product's A operand; O is touched only when the maximum moves
+//               by more than 2^8 or the unit of p sv grows.  At a piece's end they write the row.
+//   warps 8-11  turn codes into fp16 operands (exact): [64 tokens][128 dims], two warps K with dims along the contraction, two V with
+//               tokens.  One of K's leaves the tile's scales and the unit.
+//   warp 12     issues the products: S = Q K^T (128 x 64 x 128) of the next tile, then O += P V (128 x 128 x 64) of this one.  The tensor
+//               pipe keeps issue order, so S of a tile may overwrite the columns that held P two tiles before.
+//   warp 13     fetches the records, by bulk copies: K with all scales into a ring of three tiles, V into one of two.
+// TMEM columns of a CTA: two S of 64 (P in the first half of its S), O 128.
 #include <cuda_fp16.h>
 
 #include "kv8_run.cuh"
@@ -27,23 +32,24 @@ using namespace ptx;
 
 constexpr int kTile = 64, kTilePages = kTile / kPage;
 constexpr int kRows = kKv8WideRows;
-constexpr int kSoftmaxWarps = 4, kConvertWarps = 4, kMmaWarp = kSoftmaxWarps + kConvertWarps;
-constexpr int kThreads = (kMmaWarp + 1) * 32;
-// registers per thread: at launch (two CTAs of nine warps, five to a scheduler), and after the softmax has taken from the converting warps
-constexpr int kLaunchRegs = 96, kSoftmaxRegs = 136, kConvertRegs = 56;
-static_assert(kSoftmaxRegs + kConvertRegs <= 2 * kLaunchRegs, "the split draws on what the block was launched with");
+constexpr int kSoftmaxWarps = 8, kConvertWarps = 4, kMmaWarp = kSoftmaxWarps + kConvertWarps, kLoadWarp = kMmaWarp + 1;
+constexpr int kThreads = (kLoadWarp + 1) * 32;
 constexpr float kFar = -1e30f;                                      // "no key yet": finite, so that differences are never NaN
 constexpr float kSlack = 8.f;                                       // log2 of how far a score may exceed the running maximum
 constexpr int kRoom = 6;                                            // p sv is held times 2^kRoom
-constexpr uint32_t kTmemCols = 256, kColQ = 0, kColS = 64, kColO = 128;
-// An item's start and end take about as long as so many tiles.
-constexpr int kItemUnits = 4;
-constexpr int kWholeTiles = 16;
+constexpr uint32_t kTmemCols = 256, kColS = 0, kColO = 128;
+// An item's start and end take about as long as so many tiles (kv8_run.cuh).  64 (branch, KV head)s of 120 tiles: 93 us with 12, 97 with 4,
+// 122 with 24 (125 rows); 197, 197 and 209 (300 rows, three blocks).
+constexpr int kItemUnits = 12;
+constexpr int kLeastTiles = 4, kWholeTiles = 16;                    // a run has no fewer tiles; items of no more are not cut where CTAs are plenty
 using Walk = Kv8Walk<kTile, kItemUnits>;
 
 constexpr int kOperand = kTile * kHeadDim * 2;                      // fp16 K, and V, of a tile: two blocks of 64 dims, rows of 128 bytes
 constexpr int kBlock = kOperand / 2;
-constexpr int kRawTile = kTilePages * kKv8Record;
+// a tile's records in shared memory: K codes and all scales, page after page; V codes
+constexpr int kCodesTile = kTilePages * kKv8Codes, kScalesPage = kKv8Record - 2 * kKv8Codes;
+constexpr int kRingK = 3, kRingV = 2;
+constexpr int kRawK = kCodesTile + kTilePages * kScalesPage, kRawV = kCodesTile;
 // what the softmax needs of a tile besides its scores
 struct Scales {
     float k[kTile], v[kTile];                                       // K's; V's in the unit, times 2^kRoom
@@ -51,21 +57,28 @@ struct Scales {
     int unit_exp;                                                   // exponent field of the unit
     int pad[2];
 };
-constexpr int kOffK = 0;                                            // two stages
-constexpr int kOffV = kOffK + 2 * kOperand;
-constexpr int kOffRaw = kOffV + 2 * kOperand;                       // two stages
-constexpr int kOffScales = kOffRaw + 2 * kRawTile;
-constexpr int kOffCum = kOffScales + 2 * (int)sizeof(Scales);
-constexpr int kOffSums = kOffCum + (kMaxBranches + 8) * 8;          // scratch of the scan
-enum Bar { RAW_FULL = 0, RAW_EMPTY = 2, KV_FULL = 4, KV_EMPTY = 6, Q_FULL = 8, S_FULL, P_FULL, O_FULL, PART_DONE, PART_LAST, DRAINED, kNumBars };
-constexpr int kOffBar = kOffSums + (kThreads / 32) * 8 + 8;
+constexpr int kOffQ = 0;                                            // fp16 rows, laid out as K's
+constexpr int kQBlock = kRows * 128;
+constexpr int kOffK = kOffQ + 2 * kQBlock;
+constexpr int kOffV = kOffK + kOperand;
+constexpr int kOffRawK = kOffV + kOperand;
+constexpr int kOffRawV = kOffRawK + kRingK * kRawK;
+constexpr int kOffScales = kOffRawV + kRingV * kRawV;
+constexpr int kScales = 4;                                          // tiles
+constexpr int kOffCum = kOffQ;                                      // [branches + 1] units before each branch, until every role has found its first piece
+constexpr int kOffSums = kOffScales + kScales * (int)sizeof(Scales);  // scratch of the scan
+enum Bar { RAWK_FULL = 0, RAWK_EMPTY = RAWK_FULL + kRingK, RAWV_FULL = RAWK_EMPTY + kRingK, RAWV_EMPTY = RAWV_FULL + kRingV, S_FULL = RAWV_EMPTY + kRingV, P_FULL = S_FULL + 2, SCALES = P_FULL + 2, K_FULL = SCALES + kScales, K_EMPTY, V_FULL, V_EMPTY, Q_FULL, O_FULL, PART_DONE, PART_LAST, DRAINED, kNumBars };
+static_assert((kMaxBranches + 1) * 8 <= 2 * kQBlock, "the branches' units lie where the queries will");
+constexpr int kOffPair = kOffSums + (kThreads / 32) * 8;            // [2][2][rows] what the two threads of a row tell one another: maxima; sums
+constexpr int kOffBar = kOffPair + 4 * kRows * 4;
 constexpr int kOffMisc = kOffBar + kNumBars * 8;                    // [0] abort, [1] TMEM base, [2] the last part, [3, 4] scratch of the copying and the MMA warp
 constexpr int kSmemBytes = kOffMisc + 32;
-static_assert(kOffBar % 8 == 0 && kOffRaw % 128 == 0 && sizeof(Scales) % 16 == 0 && 2 * (kSmemBytes + 1024) <= 228 * 1024, "two CTAs to an SM");
+static_assert(kOffBar % 8 == 0 && kOffRawK % 128 == 0 && kRawK % 128 == 0 && sizeof(Scales) % 16 == 0 && 2 * (kSmemBytes + 1024) <= 228 * 1024, "two CTAs to an SM");
 
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
+__device__ __forceinline__ float max3(float a, float b, float c) { float r; asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
 __device__ __forceinline__ uint64_t pack2(float a, float b) { uint64_t r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
 __device__ __forceinline__ float2 unpack2(uint64_t v) { float2 r; asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v)); return r; }
 __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) { uint64_t r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
@@ -81,6 +94,11 @@ __device__ __forceinline__ float log2_approx(float x) { float y; asm("lg2.approx
 __device__ __forceinline__ bool elect_one() {
     uint32_t ok;
     asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok));
+    return ok != 0;
+}
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
 __device__ __forceinline__ void warp_arrive(uint32_t bar, int lane) {
@@ -125,11 +143,14 @@ kv8_attn_wide_kernel(const __grid_constant__ Kv8AttnParams p) {
 
     if (threadIdx.x == 0) {
         misc[0] = 0;
+        for (int i = 0; i < kRingK; ++i) { mbar_init(bar(RAWK_FULL + i), 1); mbar_init(bar(RAWK_EMPTY + i), kConvertWarps); }
+        for (int i = 0; i < kRingV; ++i) { mbar_init(bar(RAWV_FULL + i), 1); mbar_init(bar(RAWV_EMPTY + i), kConvertWarps); }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(bar(RAW_FULL + i), 1); mbar_init(bar(RAW_EMPTY + i), kConvertWarps);
-            mbar_init(bar(KV_FULL + i), kConvertWarps); mbar_init(bar(KV_EMPTY + i), 1);
+            mbar_init(bar(S_FULL + i), 1); mbar_init(bar(P_FULL + i), kSoftmaxWarps);
         }
-        mbar_init(bar(Q_FULL), kSoftmaxWarps); mbar_init(bar(S_FULL), 1); mbar_init(bar(P_FULL), kSoftmaxWarps); mbar_init(bar(O_FULL), 1);
+        for (int i = 0; i < kScales; ++i) mbar_init(bar(SCALES + i), 1);
+        mbar_init(bar(K_FULL), kConvertWarps); mbar_init(bar(V_FULL), kConvertWarps); mbar_init(bar(K_EMPTY), 1); mbar_init(bar(V_EMPTY), 1);
+        mbar_init(bar(Q_FULL), kSoftmaxWarps); mbar_init(bar(O_FULL), 1);
         mbar_init(bar(PART_DONE), kSoftmaxWarps); mbar_init(bar(PART_LAST), 1); mbar_init(bar(DRAINED), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -145,135 +166,188 @@ kv8_attn_wide_kernel(const __grid_constant__ Kv8AttnParams p) {
     grid_dependency_wait();
     grid_launch_dependents();
     kv8_scan_units<kThreads, kTile, kItemUnits>(p, cum, reinterpret_cast<long long*>(smem + kOffSums));
-    const Kv8Run run = kv8_run<kThreads, kItemUnits>(p, cum, kItemUnits, kWholeTiles);
+    const Kv8Run run = kv8_run<kThreads, kItemUnits>(p, cum, kLeastTiles, kWholeTiles);
     Walk item;
-    bool alive = run.n > 0 && item.init(p, cum, run.begin, run.n);      // every role walks over the pieces for itself
+    const bool work = run.n > 0 && item.init(p, cum, run.begin, run.n);   // every role walks over the pieces for itself
+    bool alive = work;
+    __syncthreads();
 
     if (warp >= kSoftmaxWarps && warp < kMmaWarp) {
         // =========================== records to operands ===========================
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kConvertRegs));
+        // K of a tile before V of the one before it, which waits longer.
         const int w = warp - kSoftmaxWarps, ct = w * 32 + lane;
-        // warp 0 of these: the copies, two tiles ahead
-        Walk ahead = item;
-        int ahead_tile = 0, copied = 0;
-        bool more = alive;
-        auto copy = [&]() {                                             // the next tile of the run into stage copied mod 2
-            if (!more) return;
-            const int first = (ahead.first + ahead_tile) * kTile;
-            const uint32_t full = bar(RAW_FULL + (copied & 1));
-            const bool wanted = lane < kTilePages && first + lane * kPage < ahead.tokens;
-            const int page = wanted ? p.block_table[(size_t)ahead.b * p.max_blocks + first / kPage + lane] : 0;
-            const bool there = wanted && page >= 0 && page < p.num_pages;
-            const unsigned good = __ballot_sync(0xffffffffu, there), bad = __ballot_sync(0xffffffffu, wanted && !there);
-            unsigned char* dst = smem + kOffRaw + (copied & 1) * kRawTile;
-            if (bad) {                                                  // a page outside the pool counts as zeros
-                if (lane == 0) atomicMin(p.status, (int)TTS_ERR_DEVICE_BOUNDS);
-                for (int pg = 0; pg < kTilePages; ++pg)
-                    if (bad >> pg & 1)
-                        for (int i = lane; i < kKv8Record / 16; i += 32) *reinterpret_cast<uint4*>(dst + pg * kKv8Record + i * 16) = make_uint4(0, 0, 0, 0);
-                fence_proxy_async();                                    // (before a later copy into the stage)
-                __syncwarp();
+        // Eight lanes have a token's 128 codes; codes 16 c .. of a token become 16-byte chunks 2 c and 2 c + 1 of its row.
+        // Lanes with c >= 4 write the second one first: eight different bank groups.
+        auto convert = [&](const unsigned char* raw, unsigned char* operand, int left) {
+            uint4 x[kTile / (kConvertWarps * 4)];
+#pragma unroll
+            for (int i = 0; i < kTile / (kConvertWarps * 4); ++i) x[i] = *reinterpret_cast<const uint4*>(raw + (i * kConvertWarps * 4 + (ct >> 3)) * kHeadDim + (ct & 7) * 16);
+            if (left < kTile)                                           // what is not there: 0 x NaN would be NaN
+#pragma unroll
+                for (int i = 0; i < kTile / (kConvertWarps * 4); ++i)
+                    if (i * kConvertWarps * 4 + (ct >> 3) >= left) x[i] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < kTile / (kConvertWarps * 4); ++i) {
+                const int t = i * kConvertWarps * 4 + (ct >> 3), c = (ct & 7) ^ kv8_chunk_place(t & 15);
+                const bool odd = c >= 4;
+                unsigned char* to = operand + (c >> 2) * kBlock + t * 128;
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const bool second = odd != (half == 1);
+                    const uint32_t a = kv8_biased<kFormat>(second ? x[i].z : x[i].x), b = kv8_biased<kFormat>(second ? x[i].w : x[i].y);
+                    *reinterpret_cast<uint4*>(to + ((((2 * c + (second ? 1 : 0)) & 7) ^ (t & 7)) << 4)) =
+                        make_uint4(kv8_decode2<kFormat>(a, 0), kv8_decode2<kFormat>(a, 1), kv8_decode2<kFormat>(b, 0), kv8_decode2<kFormat>(b, 1));
+                }
             }
-            if (lane == 0) { if (good) mbar_arrive_expect_tx(full, __popc(good) * kKv8Record); else mbar_arrive(full); }
+            fence_proxy_async();                                        // the operand, for the tensor cores
             __syncwarp();
-            if (there) bulk_load(smem_u32(dst) + lane * kKv8Record, p.pool + ((size_t)page * p.Hkv + ahead.item / p.n_rb) * kKv8Record, kKv8Record, full);
-            ++copied;
-            if (++ahead_tile >= ahead.n) { ahead_tile = 0; more = ahead.next(p); }
         };
-        if (w == 0) { copy(); copy(); }
-        int n = 0;                                                      // tiles of the run so far
-        int unit_exp = 7;
-        for (bool more_items = alive; more_items && alive; more_items = item.next(p)) {
-            unit_exp = 7;
-            for (int j = 0; j < item.n; ++j, ++n) {
-                const int st = n & 1, round = n >> 1 & 1;
-                const int left = min(kTile, item.tokens - (item.first + j) * kTile);       // tokens here (may be 0)
-                const unsigned char* raw = smem + kOffRaw + st * kRawTile;
-                alive = mbar_wait(bar(RAW_FULL + st), round, ab) && mbar_wait(bar(KV_EMPTY + st), round ^ 1, ab);
-                alive = __all_sync(0xffffffffu, alive);
+        auto wait = [&](int i, uint32_t parity) { alive = __all_sync(0xffffffffu, alive && mbar_wait(bar(i), parity, ab)); };
+        int tile = 0, before = 0, unit_exp = 7;                         // tile of the piece; tokens of the tile before
+        int k_slot = 0, k_round = 0, v_slot = 0, v_round = 0;
+        bool more = alive;
+        for (int n = 0; alive && (more || n > 0); ++n) {                // tiles of the run
+            int left = 0;
+            const bool here = more;
+            if (more) {
+                left = min(kTile, item.tokens - (item.first + tile) * kTile);       // tokens here (may be 0)
+                const unsigned char* raw = smem + kOffRawK + k_slot * kRawK;
+                wait(RAWK_FULL + k_slot, k_round);
+                wait(K_EMPTY, (n & 1) ^ 1);
                 if (!alive) break;
                 if (w == 1) {
-                    Scales& to = *reinterpret_cast<Scales*>(smem + kOffScales + st * sizeof(Scales));
+                    // (S of the tile before is complete: P V of the third before was issued ahead of it, after its softmax)
+                    Scales& to = *reinterpret_cast<Scales*>(smem + kOffScales + n % kScales * sizeof(Scales));
                     float k[2], v[2];
                     int top = 0;
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         const int t = i * 32 + lane;
-                        const float* s = reinterpret_cast<const float*>(raw + (t >> 4) * kKv8Record + 2 * kKv8Codes) + (t & 15);
+                        const float* s = reinterpret_cast<const float*>(raw + kCodesTile + (t >> 4) * kScalesPage) + (t & 15);
                         k[i] = t < left ? s[0] : 0.f; v[i] = t < left ? s[kPage] : 0.f;
                         const int e = __float_as_int(v[i]) >> 23 & 255;
                         top = max(top, e == 255 ? 0 : e);               // (a NaN or an infinity is not a unit)
                     }
-                    const int e = max(unit_exp, __reduce_max_sync(0xffffffffu, top));
-                    const float back = j == 0 ? 1.f : unit_exp - e < -126 ? 0.f : power_of_two(unit_exp - e), up = power_of_two(kRoom + 127 - e);
+                    const int was = tile == 0 ? 7 : unit_exp, e = max(was, __reduce_max_sync(0xffffffffu, top));
+                    const float back = tile == 0 ? 1.f : was - e < -126 ? 0.f : power_of_two(was - e), up = power_of_two(kRoom + 127 - e);
                     unit_exp = e;
 #pragma unroll
                     for (int i = 0; i < 2; ++i) { to.k[i * 32 + lane] = k[i]; to.v[i * 32 + lane] = v[i] * up; }
                     if (lane == 0) { to.unit_back = back; to.unit_exp = e; }
+                    warp_arrive(bar(SCALES + n % kScales), lane);
                 }
-                // Eight lanes have a token's 128 codes; codes 16 c .. of a token become 16-byte chunks 2 c and 2 c + 1 of its row.
-                // Lanes with c >= 4 write the second one first: eight different bank groups.
-#pragma unroll
-                for (int kv = 0; kv < 2; ++kv)
-#pragma unroll
-                    for (int i = 0; i < kTile * 8 / (kConvertWarps * 32); ++i) {
-                        const int t = i * (kConvertWarps * 4) + (ct >> 3), c = (ct & 7) ^ kv8_chunk_place(t & 15);
-                        uint4 x = *reinterpret_cast<const uint4*>(raw + (t >> 4) * kKv8Record + kv * kKv8Codes + (t & 15) * kHeadDim + (ct & 7) * 16);
-                        if (kv == 1 && t >= left) x = make_uint4(0, 0, 0, 0);       // what is not there: 0 x NaN would be NaN (K's scores are replaced)
-                        const bool odd = c >= 4;
-                        unsigned char* to = smem + (kv ? kOffV : kOffK) + st * kOperand + (c >> 2) * kBlock + t * 128;
-#pragma unroll
-                        for (int half = 0; half < 2; ++half) {
-                            const bool second = odd != (half == 1);
-                            const uint32_t a = kv8_biased<kFormat>(second ? x.z : x.x), b = kv8_biased<kFormat>(second ? x.w : x.y);
-                            *reinterpret_cast<uint4*>(to + ((((2 * c + (second ? 1 : 0)) & 7) ^ (t & 7)) << 4)) =
-                                make_uint4(kv8_decode2<kFormat>(a, 0), kv8_decode2<kFormat>(a, 1), kv8_decode2<kFormat>(b, 0), kv8_decode2<kFormat>(b, 1));
-                        }
+                convert(raw, smem + kOffK, left);
+                if (lane == 0) { mbar_arrive(bar(K_FULL)); mbar_arrive(bar(RAWK_EMPTY + k_slot)); }
+                if (++k_slot == kRingK) { k_slot = 0; k_round ^= 1; }
+                if (++tile >= item.n) { tile = 0; more = item.next(p); }
+            }
+            if (n > 0) {
+                wait(RAWV_FULL + v_slot, v_round);
+                wait(V_EMPTY, n & 1);
+                if (!alive) break;
+                convert(smem + kOffRawV + v_slot * kRawV, smem + kOffV, before);
+                if (lane == 0) { mbar_arrive(bar(V_FULL)); mbar_arrive(bar(RAWV_EMPTY + v_slot)); }
+                if (++v_slot == kRingV) { v_slot = 0; v_round ^= 1; }
+            }
+            before = left;
+            if (!here) break;
+        }
+    } else if (warp == kLoadWarp) {
+        // =========================== records ===========================
+        // Half the lanes follow K's tiles, half V's, each as far ahead as their ring allows.
+        const int kv = lane >> 4, sub = lane & 15, ring = kv ? kRingV : kRingK;
+        const int full0 = kv ? RAWV_FULL : RAWK_FULL, empty0 = kv ? RAWV_EMPTY : RAWK_EMPTY;
+        auto of_mine = [&](bool x) { return __ballot_sync(0xffffffffu, x) >> (16 * kv) & 0xffffu; };
+        int tile = 0, slot = 0, round = 0, n = 0, page = -1;            // tile of the piece; the ring; tiles fetched
+        bool more = alive;
+        auto look_up = [&]() {                                          // the pages of the next tile
+            const int first = (item.first + tile) * kTile;
+            page = -1;
+            if (sub < kTilePages && first + sub * kPage < item.tokens) page = p.block_table[(size_t)item.b * p.max_blocks + first / kPage + sub];
+        };
+        if (more) look_up();
+        long long since = 0;                                            // of the last copy; this wait has its limit too
+        for (int spin = 0; __any_sync(0xffffffffu, more); ++spin) {
+            const bool go = of_mine(more && mbar_test(bar(empty0 + slot), round ^ 1)) == 0xffffu;
+            if (!__any_sync(0xffffffffu, go)) {
+                __nanosleep(100);                                       // (asking all the time was 40 % of all instructions)
+                if ((spin & 63) == 63) {
+                    const long long now = global_ns();
+                    if (since == 0) since = now;
+                    if (now - since > kWaitLimitNs) { *ab.flag = 1; atomicMin(p.status, (int)TTS_ERR_DEVICE_TIMEOUT); }
+                    if (__any_sync(0xffffffffu, *ab.flag != 0)) break;
+                }
+                continue;
+            }
+            spin = 0; since = 0;
+            const bool wanted = go && sub < kTilePages && (item.first + tile) * kTile + sub * kPage < item.tokens, there = wanted && page >= 0 && page < p.num_pages;
+            const unsigned good = of_mine(there), bad = of_mine(wanted && !there);
+            unsigned char* dst = smem + (kv ? kOffRawV + slot * kRawV : kOffRawK + slot * kRawK);
+            if (__any_sync(0xffffffffu, bad != 0)) {                    // a page outside the pool counts as zeros
+                if (bad && sub == 0) atomicMin(p.status, (int)TTS_ERR_DEVICE_BOUNDS);
+                for (int pg = 0; pg < kTilePages; ++pg)
+                    if (bad >> pg & 1) {
+                        for (int i = sub; i < kKv8Codes / 16; i += 16) *reinterpret_cast<uint4*>(dst + pg * kKv8Codes + i * 16) = make_uint4(0, 0, 0, 0);
+                        if (!kv && sub < kScalesPage / 16) *reinterpret_cast<uint4*>(dst + kCodesTile + pg * kScalesPage + sub * 16) = make_uint4(0, 0, 0, 0);
                     }
-                fence_proxy_async();                                    // the operands, for the tensor cores
+                fence_proxy_async();                                    // (before a later copy into the slot)
                 __syncwarp();
-                if (lane == 0) { mbar_arrive(bar(KV_FULL + st)); mbar_arrive(bar(RAW_EMPTY + st)); }
-                if (w == 0 && more) {
-                    alive = __all_sync(0xffffffffu, mbar_wait(bar(RAW_EMPTY + st), round, ab));
-                    if (!alive) break;
-                    copy();
-                }
+            }
+            const uint32_t full = bar(full0 + slot);
+            if (go && sub == 0) { if (good) mbar_arrive_expect_tx(full, __popc(good) * (kv ? kKv8Codes : kKv8Codes + kScalesPage)); else mbar_arrive(full); }
+            __syncwarp();
+            if (there) {
+                const unsigned char* src = p.pool + ((size_t)page * p.Hkv + item.item / p.n_rb) * kKv8Record;
+                bulk_load(smem_u32(dst) + sub * kKv8Codes, src + kv * kKv8Codes, kKv8Codes, full);
+                if (!kv) bulk_load(smem_u32(dst) + kCodesTile + sub * kScalesPage, src + 2 * kKv8Codes, kScalesPage, full);
+            }
+            if (go) {
+                ++n;
+                if (++slot == ring) { slot = 0; round ^= 1; }
+                if (++tile >= item.n) { tile = 0; more = item.next(p); }
+                if (more) look_up();
             }
         }
-        if (w == 0 && *ab.flag) {
+        if (__any_sync(0xffffffffu, *ab.flag != 0)) {
             // after a wait that ran out: copies in flight land before the CTA ends
             const Abort quiet{misc + 3, p.status};
-            for (int i = max(0, copied - 2); i < copied; ++i) { misc[3] = 0; mbar_wait(bar(RAW_FULL + (i & 1)), i >> 1 & 1, quiet); }
+            for (int i = max(0, n - ring); i < n; ++i) { misc[3] = 0; mbar_wait(bar(full0 + i % ring), i / ring & 1, quiet); }
         }
     } else if (warp == kMmaWarp) {
         // =========================== products ===========================
         constexpr uint32_t idesc_qk = f16_desc(kRows, kTile, false), idesc_pv = f16_desc(kRows, kHeadDim, true);
-        const uint64_t k_desc = smem_desc(sbase + kOffK, 16, 1024), v_desc = smem_desc(sbase + kOffV, kBlock, 1024);
+        const uint64_t q_desc = smem_desc(sbase + kOffQ, 16, 1024), k_desc = smem_desc(sbase + kOffK, 16, 1024), v_desc = smem_desc(sbase + kOffV, kBlock, 1024);
         const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);          // (a shuffle tells the compiler that the value is uniform)
         int n = 0, pieces = 0;
+        auto wait = [&](int i, uint32_t parity) { alive = __all_sync(0xffffffffu, alive && mbar_wait(bar(i), parity, ab)); };
+        auto scores = [&](int tile) {
+            wait(K_FULL, tile & 1);
+            if (!alive) return;
+            tc_fence_after();
+            if (elect_one()) {
+#pragma unroll
+                for (int ks = 0; ks < 8; ++ks)
+                    umma_bf16(tm + kColS + (tile & 1) * kTile, q_desc + ((ks >> 2) * kQBlock + (ks & 3) * 32) / 16, k_desc + ((ks >> 2) * kBlock + (ks & 3) * 32) / 16, idesc_qk, ks > 0);
+                umma_commit(bar(S_FULL + (tile & 1)));
+                umma_commit(bar(K_EMPTY));
+            }
+            __syncwarp();
+        };
         for (bool more_items = alive; more_items && alive; more_items = item.next(p), ++pieces) {
             const int tiles = __shfl_sync(0xffffffffu, item.n, 0);
-            alive = __all_sync(0xffffffffu, mbar_wait(bar(Q_FULL), pieces & 1, ab));
+            wait(Q_FULL, pieces & 1);
+            scores(n);
             for (int j = 0; alive && j < tiles; ++j, ++n) {
-                const uint32_t st = n & 1;
-                alive = __all_sync(0xffffffffu, mbar_wait(bar(KV_FULL + st), n >> 1 & 1, ab));
-                if (!alive) break;
-                tc_fence_after();
-                if (elect_one()) {
-#pragma unroll
-                    for (int ks = 0; ks < 8; ++ks)
-                        umma_bf16_tmem_a(tm + kColS, tm + kColQ + ks * 8u, k_desc + (st * kOperand + (ks >> 2) * kBlock + (ks & 3) * 32) / 16, idesc_qk, ks > 0);
-                    umma_commit(bar(S_FULL));
-                }
-                __syncwarp();
-                alive = __all_sync(0xffffffffu, mbar_wait(bar(P_FULL), n & 1, ab));
+                if (j + 1 < tiles) scores(n + 1);
+                wait(V_FULL, n & 1);
+                wait(P_FULL + (n & 1), n >> 1 & 1);
                 if (!alive) break;
                 tc_fence_after();
                 if (elect_one()) {
 #pragma unroll
                     for (int ks = 0; ks < kTilePages; ++ks)
-                        umma_bf16_tmem_a(tm + kColO, tm + kColS + ks * 8u, v_desc + (st * kOperand + ks * 2048) / 16, idesc_pv, ks > 0 || j > 0);
-                    umma_commit(bar(KV_EMPTY + st));
+                        umma_bf16_tmem_a(tm + kColO, tm + kColS + (n & 1) * kTile + ks * 8u, v_desc + ks * 2048 / 16, idesc_pv, ks > 0 || j > 0);
+                    umma_commit(bar(V_EMPTY));
                     if (j + 1 == tiles) umma_commit(bar(O_FULL));
                 }
                 __syncwarp();
@@ -291,36 +365,44 @@ kv8_attn_wide_kernel(const __grid_constant__ Kv8AttnParams p) {
         }
     } else if (warp < kSoftmaxWarps) {
         // =========================== softmax ===========================
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
-        const uint32_t lanes = (uint32_t)(warp * 32) << 16;
-        const uint32_t t_q = tmem + lanes + kColQ, t_s = tmem + lanes + kColS, t_o = tmem + lanes + kColO;
+        // The two warps of a row meet at barriers, so that neither leaves where a wait has run out: they go on, waiting no more, with
+        // whatever is there.
+        const int half = warp >> 2, meet = 1 + (warp & 3), r = (warp & 3) * 32 + lane;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t t_o = tmem + lanes + kColO + 64u * half;
+        float* mine = reinterpret_cast<float*>(smem + kOffPair) + half * kRows + r;
+        const float* other = reinterpret_cast<float*>(smem + kOffPair) + (half ^ 1) * kRows + r;
         int n = 0, pieces = 0, parts_left = 0;
-        for (bool more_items = alive; more_items && alive; more_items = item.next(p), ++pieces) {
+        auto wait = [&](int i, uint32_t parity) { alive = __all_sync(0xffffffffu, alive && mbar_wait(bar(i), parity, ab)); };
+        for (bool more_items = work; more_items; more_items = item.next(p), ++pieces) {
             const int h = item.item / p.n_rb, row0 = (item.item - h * p.n_rb) * p.rb_rows, rows = min(p.rb_rows, p.nr - row0);
-            const int r = threadIdx.x, stacked = row0 + min(r, rows - 1), i_row = stacked / p.G, head = h * p.G + stacked - i_row * p.G;
-            const bool idle = warp * 32 >= rows;                        // no row of the block is this warp's
+            const int stacked = row0 + min(r, rows - 1), i_row = stacked / p.G, head = h * p.G + stacked - i_row * p.G;
+            const bool idle = (warp & 3) * 32 >= rows;                  // no row of the block is these warps'
             const int tail = item.tokens - p.R;                         // the first of the branch's last R tokens (may be negative)
             float factor = 0.f;
             unsigned long long mask = 0;                                // which of the branch's last R tokens the row sees
             if (!idle) {
-                // ---- the query, scaled to fp16 by the power of two that puts its largest at 2^14
-                const uint4* src = reinterpret_cast<const uint4*>(p.q + ((size_t)item.b * p.R + i_row) * p.q_stride + (size_t)head * kHeadDim);
-                uint32_t x[64];
+                // ---- the query, scaled to fp16 by the power of two that puts its largest at 2^14; 64 dims to a thread
+                const uint4* src = reinterpret_cast<const uint4*>(p.q + ((size_t)item.b * p.R + i_row) * p.q_stride + (size_t)head * kHeadDim + 64 * half);
+                uint32_t x[32];
 #pragma unroll
-                for (int i = 0; i < 16; ++i) { const uint4 y = src[i]; x[4 * i] = y.x; x[4 * i + 1] = y.y; x[4 * i + 2] = y.z; x[4 * i + 3] = y.w; }
+                for (int i = 0; i < 8; ++i) { const uint4 y = src[i]; x[4 * i] = y.x; x[4 * i + 1] = y.y; x[4 * i + 2] = y.z; x[4 * i + 3] = y.w; }
                 uint32_t top = 0;                                       // the largest finite magnitude, as bits
 #pragma unroll
-                for (int i = 0; i < 64; ++i) {
+                for (int i = 0; i < 32; ++i) {
                     const uint32_t lo = x[i] << 16 & 0x7fffffffu, hi = x[i] & 0x7fff0000u;
                     top = max(top, max(lo < 0x7f800000u ? lo : 0u, hi < 0x7f800000u ? hi : 0u));
                 }
-                const int e = max(-100, min(126, (int)(top >> 23) - 127)) - 14;
+                *mine = __uint_as_float(top);
+                bar_sync_id<64>(meet);
+                const int e = max(-100, min(126, (int)(max(top, __float_as_uint(*other)) >> 23) - 127)) - 14;
                 const float down = power_of_two(-e);
 #pragma unroll
-                for (int i = 0; i < 64; ++i) x[i] = pack_half2(__uint_as_float(x[i] << 16) * down, __uint_as_float(x[i] & 0xffff0000u) * down);
-                tmem_st32(t_q, x);
-                tmem_st32(t_q + 32u, x + 32);
-                tmem_wait_st();
+                for (int i = 0; i < 32; ++i) x[i] = pack_half2(__uint_as_float(x[i] << 16) * down, __uint_as_float(x[i] & 0xffff0000u) * down);
+                unsigned char* to = smem + kOffQ + half * kQBlock + r * 128;
+#pragma unroll
+                for (int c = 0; c < 8; ++c) *reinterpret_cast<uint4*>(to + ((c ^ (r & 7)) << 4)) = make_uint4(x[4 * c], x[4 * c + 1], x[4 * c + 2], x[4 * c + 3]);
+                fence_proxy_async();
                 factor = power_of_two(e) * p.scale_log2;
                 if (p.tree_parents == nullptr) mask = i_row >= 63 ? ~0ull : (2ull << i_row) - 1ull;
                 else
@@ -330,7 +412,6 @@ kv8_attn_wide_kernel(const __grid_constant__ Kv8AttnParams p) {
                         a = parent < a ? parent : -1;                   // malformed parents end the walk
                     }
             }
-            tc_fence_before();
             warp_arrive(bar(Q_FULL), lane);
             float neg_m = -kFar, l = 0.f;
             int unit_exp = 7;
@@ -338,48 +419,54 @@ kv8_attn_wide_kernel(const __grid_constant__ Kv8AttnParams p) {
 #pragma unroll 1
             for (int j = 0; j < item.n; ++j, ++n) {
                 const int st = n & 1;
-                alive = __all_sync(0xffffffffu, mbar_wait(bar(S_FULL), n & 1, ab) && mbar_wait(bar(KV_FULL + st), n >> 1 & 1, ab));
-                if (!alive) break;
+                const uint32_t t_s = tmem + lanes + kColS + (uint32_t)st * kTile;
+                wait(S_FULL + st, n >> 1 & 1);
+                wait(SCALES + n % kScales, n / kScales & 1);
                 tc_fence_after();
-                if (idle) { warp_arrive(bar(P_FULL), lane); continue; }     // (what its rows hold reaches no row of the result)
-                const Scales& sc = *reinterpret_cast<const Scales*>(smem + kOffScales + st * sizeof(Scales));
+                if (idle) { warp_arrive(bar(P_FULL + st), lane); continue; }     // (what its rows hold reaches no row of the result)
+                const Scales& sc = *reinterpret_cast<const Scales*>(smem + kOffScales + n % kScales * sizeof(Scales));
                 const int first = (item.first + j) * kTile, left = item.tokens - first;
                 const bool masked = first + kTile > tail || left < kTile;
-                float s[kTile];
-                tmem_ld32(t_s, reinterpret_cast<uint32_t*>(s));
-                tmem_ld32(t_s + 32u, reinterpret_cast<uint32_t*>(s) + 32);
+                float s[32];
+                tmem_ld32(t_s + 32u * half, reinterpret_cast<uint32_t*>(s));
                 tmem_wait_ld();
 #pragma unroll
-                for (int c = 0; c < kTile; c += 4) {
-                    const float4 k = *reinterpret_cast<const float4*>(sc.k + c);
+                for (int c = 0; c < 32; c += 4) {
+                    const float4 k = *reinterpret_cast<const float4*>(sc.k + 32 * half + c);
                     const float2 lo = unpack2(mul2(pack2(s[c], s[c + 1]), pack2(k.x, k.y))), hi = unpack2(mul2(pack2(s[c + 2], s[c + 3]), pack2(k.z, k.w)));
                     s[c] = lo.x; s[c + 1] = lo.y; s[c + 2] = hi.x; s[c + 3] = hi.y;
                 }
-                unsigned long long seen = ~0ull;                        // tokens of the tile that the row sees
+                uint32_t seen = ~0u;                                    // of the thread's 32 tokens, those that the row sees
                 if (masked) {
                     const int before = tail - first;                    // tokens of the tile ahead of the last R (may be negative, or all)
-                    seen = before >= kTile ? ~0ull : before >= 0 ? mask << before | ((1ull << before) - 1ull) : before > -kTile ? mask >> -before : 0ull;
-                    if (left < kTile) seen &= left <= 0 ? 0ull : (1ull << left) - 1ull;
+                    unsigned long long all = before >= kTile ? ~0ull : before >= 0 ? mask << before | ((1ull << before) - 1ull) : before > -kTile ? mask >> -before : 0ull;
+                    if (left < kTile) all &= left <= 0 ? 0ull : (1ull << left) - 1ull;
+                    seen = (uint32_t)(all >> (32 * half));
 #pragma unroll
-                    for (int c = 0; c < kTile; ++c)
+                    for (int c = 0; c < 32; ++c)
                         if (!(seen >> c & 1)) s[c] = -INFINITY;
                 }
                 float top4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                for (int c = 0; c < kTile; c += 2) top4[c >> 1 & 3] = fmaxf(top4[c >> 1 & 3], fmaxf(s[c], s[c + 1]));
-                const float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3])) * factor;
+                for (int c = 0; c < 32; c += 2) top4[c >> 1 & 3] = max3(top4[c >> 1 & 3], s[c], s[c + 1]);
+                float top = max3(fmaxf(top4[0], top4[1]), top4[2], top4[3]) * factor;
                 const float unit_back = sc.unit_back;
                 unit_exp = sc.unit_exp;
-                if (__any_sync(0xffffffffu, top + neg_m > kSlack) || unit_back != 1.f) {
+                // (here both have their scores, so either may write P over them)
+                if (bar_red_or<64>(meet, top + neg_m > kSlack || unit_back != 1.f)) {
                     // ---- seldom: the maximum moves, or the unit
+                    *mine = top;
+                    bar_sync_id<64>(meet);
+                    top = fmaxf(top, *other);
                     const float was = neg_m;
                     neg_m = fminf(was, -top);
-                    const float back = ex2(neg_m - was);
+                    const float back = ex2(neg_m - was), both = back * unit_back;
                     l *= back;
-                    const float both = back * unit_back;
-                    if (j > 0)                                          // (S of this tile is complete, so the P V before it is as well)
+                    if (j > 0) {
+                        wait(V_EMPTY, (n - 1) & 1);                     // the P V before this tile's
+                        tc_fence_after();
 #pragma unroll 1
-                        for (int ch = 0; ch < 8; ++ch) {
+                        for (int ch = 0; ch < 4; ++ch) {
                             uint32_t o[16];
                             tmem_ld16(t_o + 16u * ch, o);
                             tmem_wait_ld();
@@ -387,13 +474,14 @@ kv8_attn_wide_kernel(const __grid_constant__ Kv8AttnParams p) {
                             for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * both);
                             tmem_st16(t_o + 16u * ch, o);
                         }
+                    }
                 }
                 const uint64_t neg2 = pack2(neg_m, neg_m);
                 uint64_t sum[2] = {0, 0};
-                uint32_t w[kTile / 2];
+                uint32_t w[16];
 #pragma unroll
-                for (int c = 0; c < kTile / 4; ++c) {
-                    const float4 v = *reinterpret_cast<const float4*>(sc.v + 4 * c);
+                for (int c = 0; c < 8; ++c) {
+                    const float4 v = *reinterpret_cast<const float4*>(sc.v + 32 * half + 4 * c);
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
                         const float2 d = unpack2(fma2(pack2(s[4 * c + 2 * k], s[4 * c + 2 * k + 1]), factor2, neg2));
@@ -405,56 +493,56 @@ kv8_attn_wide_kernel(const __grid_constant__ Kv8AttnParams p) {
                 }
                 if (masked)                                             // a hidden token's scale may be a NaN
 #pragma unroll
-                    for (int c = 0; c < kTile / 2; ++c)
+                    for (int c = 0; c < 16; ++c)
                         w[c] &= (seen >> (2 * c) & 1 ? 0xffffu : 0u) | (seen >> (2 * c + 1) & 1 ? 0xffff0000u : 0u);
-                tmem_st32(t_s, w);
+                tmem_st16(t_s + 16u * half, w);
                 tmem_wait_st();
                 tc_fence_before();
-                warp_arrive(bar(P_FULL), lane);
+                warp_arrive(bar(P_FULL + st), lane);
                 const float2 both = unpack2(add2(sum[0], sum[1]));
                 l += both.x + both.y;
             }
-            if (!alive) break;
 
             // ---- the piece's rows
-            alive = __all_sync(0xffffffffu, mbar_wait(bar(O_FULL), pieces & 1, ab));
-            if (!alive) break;
+            wait(O_FULL, pieces & 1);
             tc_fence_after();
-            const bool whole = item.whole(), mine = r < rows;
+            const bool whole = item.whole(), valid = r < rows;
             const Kv8Parts cut = kv8_parts(item, run.begin + (run.n - item.left), run.per_cta);
             const size_t slot = 2 * (size_t)blockIdx.x + (item.nth == 0 ? 0 : 1);
-            const size_t at = ((size_t)item.b * p.R + i_row) * p.Hq + head;
-            auto write_out = [&](size_t row, int dim, const float* v) {         // 16 values
-                if (p.out_dtype == TTS_OUT_FP32) {
-                    float* to = static_cast<float*>(p.out) + row * kHeadDim + dim;
-#pragma unroll
-                    for (int c = 0; c < 16; c += 4) *reinterpret_cast<float4*>(to + c) = make_float4(v[c], v[c + 1], v[c + 2], v[c + 3]);
-                } else {
-                    uint4* to = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + row * kHeadDim + dim);
-                    to[0] = make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
-                    to[1] = make_uint4(bf16_pair(v[8], v[9]), bf16_pair(v[10], v[11]), bf16_pair(v[12], v[13]), bf16_pair(v[14], v[15]));
-                }
-            };
             auto write_lse = [&](size_t row, float m, float sum) {      // natural logarithm
                 p.lse[row] = sum == 0.f ? -INFINITY : (m + log2_approx(sum)) * 0.6931471805599453f;
             };
             if (!idle) {
+                mine[2 * kRows] = l;
+                bar_sync_id<64>(meet);
+                l += other[2 * kRows];
                 const float inv = l == 0.f ? 0.f : 1.f / l, unit = power_of_two(unit_exp - 127 - kRoom);     // (a row that saw nothing: zeros)
+                const size_t at = ((size_t)item.b * p.R + i_row) * p.Hq + head;
 #pragma unroll 1
-                for (int ch = 0; ch < 8; ++ch) {
+                for (int ch = 0; ch < 4; ++ch) {
                     float o[16];
                     tmem_ld16(t_o + 16u * ch, reinterpret_cast<uint32_t*>(o));
                     tmem_wait_ld();
 #pragma unroll
                     for (int c = 0; c < 16; ++c) o[c] = l == 0.f ? 0.f : o[c] * inv * unit;
-                    if (mine && whole) write_out(at, 16 * ch, o);
-                    else if (mine) {
-                        float* to = p.part_o + (slot * kRows + r) * kHeadDim + 16 * ch;
-                        st_global_32(to, o); st_global_32(to + 8, o + 8);
+                    if (!valid) continue;
+                    const int dim = 64 * half + 16 * ch;
+                    if (!whole || p.out_dtype == TTS_OUT_FP32) {
+                        float* to = whole ? static_cast<float*>(p.out) + at * kHeadDim : p.part_o + (slot * kRows + r) * kHeadDim;
+                        if (whole)
+#pragma unroll
+                            for (int c = 0; c < 16; c += 4) *reinterpret_cast<float4*>(to + dim + c) = make_float4(o[c], o[c + 1], o[c + 2], o[c + 3]);
+                        else { st_global_32(to + dim, o); st_global_32(to + dim + 8, o + 8); }
+                    } else {
+                        uint4* to = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + at * kHeadDim + dim);
+                        to[0] = make_uint4(bf16_pair(o[0], o[1]), bf16_pair(o[2], o[3]), bf16_pair(o[4], o[5]), bf16_pair(o[6], o[7]));
+                        to[1] = make_uint4(bf16_pair(o[8], o[9]), bf16_pair(o[10], o[11]), bf16_pair(o[12], o[13]), bf16_pair(o[14], o[15]));
                     }
                 }
-                if (mine && !whole) p.part_ml[slot * kRows + r] = make_float2(-neg_m, l);
-                if (mine && whole && p.lse) write_lse(at, -neg_m, l);
+                if (valid && half == 0) {
+                    if (!whole) p.part_ml[slot * kRows + r] = make_float2(-neg_m, l);
+                    else if (p.lse) write_lse(at, -neg_m, l);
+                }
             }
             tc_fence_before();                                          // O and Q have been read, before the next piece's products
             if (!whole) {
@@ -464,7 +552,7 @@ kv8_attn_wide_kernel(const __grid_constant__ Kv8AttnParams p) {
                 warp_arrive(bar(PART_DONE), lane);
                 if (threadIdx.x == 0) {
                     int last = 0;
-                    if (mbar_wait(bar(PART_DONE), parts_left & 1, ab)) {
+                    if (alive && mbar_wait(bar(PART_DONE), parts_left & 1, ab)) {
                         unsigned before;
                         asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(before) : "l"(p.arrived + id) : "memory");
                         last = before + 1 == (unsigned)cut.n;
@@ -475,40 +563,50 @@ kv8_attn_wide_kernel(const __grid_constant__ Kv8AttnParams p) {
                     mbar_arrive(bar(PART_LAST));
                 }
                 __syncwarp();
-                alive = __all_sync(0xffffffffu, mbar_wait(bar(PART_LAST), parts_left & 1, ab));
+                wait(PART_LAST, parts_left & 1);
                 ++parts_left;
-                if (!alive) break;
-                if (misc[2]) {
+                if (alive && misc[2]) {
                     __threadfence();
-                    // a warp to a row, four dims a lane
-                    for (int q = warp; q < rows; q += kSoftmaxWarps) {
-                        float m = kFar, sum = 0.f;
-                        for (int k0 = 0; k0 < cut.n; k0 += 32) {
-                            const float2 x = k0 + lane < cut.n ? __ldcg(p.part_ml + (size_t)cut.slot(k0 + lane) * kRows + q) : make_float2(kFar, 0.f);
-                            float now = fmaxf(m, x.x);
-#pragma unroll
-                            for (int o = 1; o < 32; o <<= 1) now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, o));
-                            float add = x.y * ex2(x.x - now);
-#pragma unroll
-                            for (int o = 1; o < 32; o <<= 1) add += __shfl_xor_sync(0xffffffffu, add, o);
-                            sum = sum * ex2(m - now) + add;
+                    // sixteen rows to a warp: a lane finds one's maximum and sum, then four rows at a time, four dims a lane
+                    const int q = warp * 16 + (lane & 15);
+                    float m = kFar, sum = 0.f;
+                    if (q < rows)
+#pragma unroll 2
+                        for (int k = 0; k < cut.n; ++k) {
+                            const float2 x = __ldcg(p.part_ml + (size_t)cut.slot(k) * kRows + q);
+                            const float now = fmaxf(m, x.x);
+                            sum = sum * ex2(m - now) + x.y * ex2(x.x - now);
                             m = now;
                         }
-                        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
+                    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                    auto place = [&](int row) { const int s = row0 + row, i = s / p.G; return ((size_t)item.b * p.R + i) * p.Hq + h * p.G + s - i * p.G; };
+                    if (p.lse && lane < 16 && q < rows) write_lse(place(q), m, sum);
+#pragma unroll 1
+                    for (int g = 0; g < 16 && warp * 16 + g < rows; g += 4) {
+                        float4 acc[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
                         for (int k = 0; k < cut.n; ++k) {
-                            const size_t from = (size_t)cut.slot(k) * kRows + q;
-                            const float2 x = __ldcg(p.part_ml + from);
-                            const float4 y = __ldcg(reinterpret_cast<const float4*>(p.part_o + from * kHeadDim) + lane);
-                            const float f = x.y * ex2(x.x - m);
-                            acc.x = fmaf(f, y.x, acc.x); acc.y = fmaf(f, y.y, acc.y); acc.z = fmaf(f, y.z, acc.z); acc.w = fmaf(f, y.w, acc.w);
+                            const size_t from = (size_t)cut.slot(k) * kRows + warp * 16;
+                            const float2 x = __ldcg(p.part_ml + from + (lane & 15));
+                            const float weight = x.y * ex2(x.x - m) * inv;
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                // (rows behind the last one: whatever lies in the workspace, not written anywhere)
+                                const float4 y = __ldcg(reinterpret_cast<const float4*>(p.part_o + (from + g + i) * kHeadDim) + lane);
+                                const float f = __shfl_sync(0xffffffffu, weight, g + i);
+                                acc[i].x = fmaf(f, y.x, acc[i].x); acc[i].y = fmaf(f, y.y, acc[i].y); acc[i].z = fmaf(f, y.z, acc[i].z); acc[i].w = fmaf(f, y.w, acc[i].w);
+                            }
                         }
-                        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-                        const int s = row0 + q, i = s / p.G;
-                        const size_t row = ((size_t)item.b * p.R + i) * p.Hq + h * p.G + s - i * p.G, to = row * kHeadDim + lane * 4;
-                        if (p.out_dtype == TTS_OUT_FP32) *reinterpret_cast<float4*>(static_cast<float*>(p.out) + to) = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
-                        else *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + to) = make_uint2(bf16_pair(acc.x * inv, acc.y * inv), bf16_pair(acc.z * inv, acc.w * inv));
-                        if (p.lse && lane == 0) write_lse(row, m, sum);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            if (warp * 16 + g + i >= rows) break;
+                            const size_t to = place(warp * 16 + g + i) * kHeadDim + lane * 4;
+                            const float v[4] = {acc[i].x, acc[i].y, acc[i].z, acc[i].w};
+                            if (p.out_dtype == TTS_OUT_FP32) *reinterpret_cast<float4*>(static_cast<float*>(p.out) + to) = make_float4(v[0], v[1], v[2], v[3]);
+                            else *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + to) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
+                        }
                     }
                 }
             }
