@@ -156,25 +156,30 @@ __device__ __forceinline__ void join_sums(float& top, double& sum) {
 
 // A question's parts put together by one block.
 __device__ void join_parts(const BeamParams& p, Shared& sh, int group) {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, k = p.n_select, row0 = group * p.n_beams;
+    const int tid = threadIdx.x, k = p.n_select, row0 = group * p.n_beams;
     const size_t out = (size_t)group * k;
     const u64* entries = p.entries + ((size_t)row0 << (p.parts_log2 + p.cap_log2));
     const int n = __ldcg(p.n_entries + group);
-    u64 e = tid < n ? __ldcg(entries + tid) : 0;                    // (asked for ahead of the logarithms)
+    constexpr int kAhead = kList / kThreads;
+    u64 e[kAhead];                                                  // (asked for ahead of the logarithms)
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) e[i] = tid + i * kThreads < n ? __ldcg(entries + tid + i * kThreads) : 0;
     if (tid == 0) sh.few.n = 0;
-    // the rows' logarithms, a warp each; NaN for a row that offers nothing.  (A finished beam's candidate has a logit of 0.)
-    for (int b = warp; b < p.n_beams; b += kThreads / 32) {
-        const int row = row0 + b;
+    // the rows' logarithms, eight lanes each; NaN for a row that offers nothing.  (A finished beam's candidate has a logit of 0.)
+    const int sub = tid & 7;
+#pragma unroll 1
+    for (int b0 = 0; b0 < p.n_beams; b0 += kThreads / 8) {
+        const int b = min(b0 + (tid >> 3), p.n_beams - 1), row = row0 + b;
         float top = -INFINITY;
         double sum = 0.0;
-        if (lane < 1 << p.parts_log2) {
-            const size_t part = ((size_t)row << p.parts_log2) + lane;
+        if (sub < 1 << p.parts_log2) {
+            const size_t part = ((size_t)row << p.parts_log2) + sub;
             top = __ldcg(p.part_top + part); sum = __ldcg(p.part_sum + part);
         }
         const float before = p.beam_scores[row];
         const bool done = p.finished && p.finished[row];
         join_sums<8>(top, sum);
-        if (lane == 0) sh.base[b] = (double)before - (done ? 0.0 : (double)top + (double)(log2_approx((float)sum) * kLn2));
+        if (sub == 0) sh.base[b] = (double)before - (done ? 0.0 : (double)top + (double)(log2_approx((float)sum) * kLn2));
     }
     if (tid < k) { p.parents[out + tid] = -1; p.tokens[out + tid] = -1; p.scores[out + tid] = -INFINITY; }      // where there are too few candidates
     __syncthreads();
@@ -186,13 +191,13 @@ __device__ void join_parts(const BeamParams& p, Shared& sh, int group) {
         bisect<64>(sh, sh.few, k, [&](auto f) { for (int i = tid; i < n; i += kThreads) { const u64 x = __ldcg(entries + i); f(score(x), (uint32_t)x); } });
     else {
         u64 best = 0;
-#pragma unroll 1
-        for (int i = tid; i < n; i += kThreads) {
-            const u64 key = score(e);
-            sh.list.keys[i] = key; sh.list.places[i] = (uint32_t)e;
-            best = max(best, key);
-            if (i + kThreads < n) e = __ldcg(entries + i + kThreads);
-        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            if (tid + i * kThreads < n) {
+                const u64 key = score(e[i]);
+                sh.list.keys[tid + i * kThreads] = key; sh.list.places[tid + i * kThreads] = (uint32_t)e[i];
+                best = max(best, key);
+            }
         const u64 least = max(lower_bound(sh, best, k), (u64)1);
         auto listed = [&](auto f) { for (int i = tid; i < n; i += kThreads) f(sh.list.keys[i], sh.list.places[i]); };
         listed([&](u64 key, uint32_t place) { if (key >= least) sh.few.put(key, place); });
