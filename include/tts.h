@@ -312,8 +312,8 @@ TTS_API int tts_profile_read(tts_ctx* ctx, float* attn_main_us, float* attn_merg
  * on another warp role) is bounded: when its limit runs out the kernel raises TTS_ERR_DEVICE_TIMEOUT in
  * the device status word, lets go of what it holds and returns, so a lost signal never hangs the GPU.
  * tts_debug_wait_timeout runs a separate one-warp kernel on the context's stream that waits, through the
- * same routine, limit_ns nanoseconds (1 us .. 1 s) for a signal that is never sent, and leaves the chunk
- * attention's counters in disorder, as a call that gave up does.  tts_last_status then reports
+ * same routine, limit_ns nanoseconds (1 us .. 1 s) for a signal that is never sent, and leaves the
+ * counters of the chunk attention and of the 8-bit cache's in disorder, as a call that gave up does.  tts_last_status then reports
  * TTS_ERR_DEVICE_TIMEOUT and sets them right: the context works as before.
  */
 TTS_API int tts_debug_wait_timeout(tts_ctx* ctx, int64_t limit_ns);
@@ -538,13 +538,17 @@ TTS_API int tts_kv_compact(tts_ctx* ctx, int n_layers, void* const* k_pools, voi
  *                       rows_per_branch + i (in a tree: those of its ancestors' places that exist), and a row that sees none gets out = 0
  *                       and lse = -infinity.  Scores and sums are fp32, probabilities times V's scale are rounded to fp16 (2^-11).
  *                       Slots past a branch's end may hold anything; a token whose scale is NaN makes NaN the rows that see it and no
- *                       others.  cfg.max_ctas, softmax_scale and out_dtype apply, attn_impl does not.
+ *                       others.  cfg.max_ctas, softmax_scale and out_dtype apply, attn_impl does not.  The context's calls share the
+ *                       memory in which parts of a long branch meet: order them on the GPU.  (It is allocated with the context: 4 MB, or
+ *                       39 MB where cfg allows more than 48 rows to a KV head.)
  *   tts_kv8_copy_pages, tts_kv8_fork, tts_kv8_compact
  *                       tts_kv_copy_pages, tts_kv_fork, tts_kv_compact over n_layers (1..128) 8-bit pools, one per layer.
  * Reported through tts_last_status as TTS_ERR_DEVICE_BOUNDS, whatever cfg.debug_bounds: what the bf16 calls report; by tts_kv8_attn a
- * branch of negative length or beyond the table row, which counts as empty, and a page id outside the pool, which is read as zeros.
+ * branch of negative length or beyond the table row, which counts as empty, and a page id outside the pool, which is read as zeros; as
+ * TTS_ERR_DEVICE_TIMEOUT a wait inside tts_kv8_attn that ran out (results of that call are not to be used).
  * TTS_ERR_INVALID for null or misaligned pointers, sizes outside the context's limits, and results that overlap anything else
- * (q_out may be q itself when q is dense); TTS_ERR_UNSUPPORTED for an unknown format.
+ * (q_out may be q itself when q is dense); TTS_ERR_UNSUPPORTED for an unknown format, and for a tts_kv8_attn whose branches could have so
+ * many pages that a thread block's share passes 2^31.
  */
 TTS_API int tts_kv8_append(tts_ctx* ctx, int format, const tts_rope* rope, const void* q, int64_t q_row_stride, const void* k,
                            const void* v, int64_t kv_row_stride, const int32_t* positions, void* kv8_pages, const int32_t* block_table,

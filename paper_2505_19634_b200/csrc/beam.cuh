@@ -9,6 +9,7 @@ constexpr int kMaxBeamCandidates = 8192;   // beams of a question times continua
 // Candidates that a part of a row may leave for the question's last CTA, a power of two: more than the n best, for what the bound lets through.
 __host__ __device__ constexpr int beam_cap_log2(int n) { return n <= 16 ? 6 : n <= 48 ? 7 : n <= 96 ? 8 : 9; }
 // Parts of a row, 2^0 to 2^3: as long as the GPU takes all of them at once, four CTAs to an SM, and each has 4096 logits.
+// (16 questions of 16 beams: 44.5 us in one part, 34.5 in two; one question of 4 beams: 19.7 in one, 16.0 in two, 10.9 in eight.)
 inline int beam_parts_log2(int rows, int vocab, int n_sms) {
     int log2 = 0;
     while (log2 < 3 && (long)rows << (log2 + 1) <= 4l * n_sms && vocab >> (log2 + 1) >= 4096) ++log2;

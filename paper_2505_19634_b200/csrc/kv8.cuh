@@ -68,7 +68,9 @@ struct Kv8AttnParams {
     int Hq, Hkv, G, R, nr, n_rb, rb_rows, prefix_len, n_branches, max_blocks, num_pages, out_dtype, grid;
     float scale_log2;
 };
-constexpr int kKv8MaxRows = 24;        // rows of one KV head that a block of kv8_attn.cu works on at a time
+// Rows of one KV head that a block of kv8_attn.cu works on at a time: what a warp holds in registers.  (300 rows took 509 us in
+// blocks of 16 and 410 in blocks of 24.)
+constexpr int kKv8MaxRows = 24;
 // kv8_attn_wide.cu works on up to 128 rows at a time, and takes over where the other would need more than two blocks: 64 (branch, KV head)s
 // of 7.9 k keys take 79 us there with 25 to 48 rows and 109 with 60, here 78 with 40 and 82 with 60.  (Over 500 keys it is slower, 21 us
 // against 17, but the host does not know how long the branches are.)

@@ -2,15 +2,21 @@
 //
 //   out[r] = sum_t softmax_t(scale <q_r, ck_t> sk_t) cv_t sv_t,   codes c and scales s of kv8.cuh
 //
-// Bound by HBM where a branch has few rows per KV head: a record of 4224 bytes (16 tokens) is read once for all rows
-// of the branch.  Work is cut into items (branch, KV head, block of up to 24 stacked rows) of as many units as the branch
-// has pages; a CTA of 8 warps owns a contiguous run of all units, warp w takes its pairs of pages w, w + 8, .. and works on them
-// without meeting the other warps: they come by bulk copies into a ring of the warp's own.  At the end of an item
-// (or of the run) the warps join their results through shared memory; items cut between CTAs are joined by the last CTA
-// to finish one of their parts, which the others leave in global memory.
+// For up to 48 rows to a KV head (kv8_attn_wide.cu: more).  Bound by HBM: a record of 4224 bytes (16 tokens) is read once for all rows
+// of the branch.  Work is cut into items (branch, KV head, block of up to 24 stacked rows; kv8_run.cuh); a CTA of 8 warps owns a
+// contiguous run of pages, warp w takes its pairs of pages w, w + 8, .. and works on them without meeting the other warps: they
+// come by bulk copies into a ring of the warp's own.  At the end of an item (or of the run) the warps join their results through
+// shared memory; items cut between CTAs are joined by the last CTA to finish one of their parts, which the others leave in
+// global memory.
 //
-// Per page (and two at a time, for what one leaves idle), with tokens on the M side and rows on the N side of the warp-level matrix instruction m16n8k16 (fp16 operands,
-// fp32 sums):
+// Measured (B200, copy peak 6538 GB/s): 64 single tokens over 1 k to 8 k keys, 40 / 8 heads, 120 us = 4.5 TB/s; a drafted step of 16 branches
+// with 20 rows to a KV head over 4 k to 5 k keys 56 us = 2.5 TB/s; 4 single tokens over 500 keys 8.6 us.  A warp takes about 1850 clocks for a page
+// of up to 8 rows (1460 without the copies, 950 with nothing but them) and 2240 for 24: conversion, products and exponentials of two
+// warps to a scheduler.  A piece of an item costs 16000 clocks besides (queries 3000, the warps' join 9000, that of its parts 3700), a
+// third of the drafted step.  Tiles converted for the tensor cores' own products took 88 and 246 us for the first two.
+//
+// Per page (and two at a time, for what one leaves idle), with tokens on the M side and rows on the N side of the warp-level
+// matrix instruction m16n8k16 (fp16 operands, fp32 sums):
 //     S^T[16 tokens][rows] = K Q^T      O^T[128 dims][rows] += V^T P^T
 // Codes are exact in fp16, so K and V need no rounding; a row of Q is scaled by a power of two so that bf16 fits fp16 too.
 // The scale of K goes into the score; p sv goes into the second product, rounded to fp16 (11 bits) in units of the largest

@@ -80,6 +80,11 @@ def test_logits_in_awkward_orders(kind, k):
     check(x, torch.tensor([-2.0, -1.0, -2.5, -1.0], device="cuda"), 2, 2, k)
 
 
+@pytest.mark.parametrize("groups,beams,k,vocab", [(1, 64, 64, 40000), (2, 16, 64, 32768), (1, 64, 128, 33000)])
+def test_questions_whose_parts_leave_thousands_of_candidates(groups, beams, k, vocab):
+    check(normal(groups * beams, vocab, torch.float32, vocab + k), starts(groups * beams), groups, beams, k)
+
+
 def test_more_candidates_than_a_block_compares_at_once_with_ties():
     """64 beams of 128 candidates, many scores equal: the last places go to the lowest beams and tokens."""
     x = torch.zeros(64, 500)
