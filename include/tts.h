@@ -590,7 +590,7 @@ TTS_API int tts_kv8_compact(tts_ctx* ctx, int n_layers, void* const* kv8_pools, 
  *                    memory: order them on the GPU.
  *   tts_beam_reorder dst[s][i] = src[s][parents[i]] for n_states (1..128) arrays of rows (token histories, hidden states, dense caches of
  *                    a draft model): src[s] has n_rows rows of row_bytes[s] bytes, dst[s] n_children.  src, dst, row_bytes are host arrays, their
- *                    entries device pointers of any alignment (rows of whole 16-byte units move fastest).  A parent of -1 leaves the row of
+ *                    entries device pointers of any alignment.  A parent of -1 leaves the row of
  *                    dst as it was; one outside the rows does so too and raises TTS_ERR_DEVICE_BOUNDS.
  * TTS_ERR_INVALID for null or misaligned pointers, sizes outside what was reserved, and results that overlap anything else.
  */

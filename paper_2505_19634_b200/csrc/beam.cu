@@ -422,27 +422,73 @@ beam_select_kernel(const __grid_constant__ BeamParams p) {
     if (tid == 0) p.n_entries[group] = 0;                           // as the next call expects it (all threads have read it)
 }
 
-// Rows of many arrays: dst[i] = src[parents[i]].  Bound by HBM; a block moves 32 KiB of a row (8 loads of 16 bytes a thread before
-// the first store), or less where rows are not whole 16-byte units.  48 dense caches of 16 rows of 512 KiB: 103 us, the copy peak; 16 rows of five
-// small arrays 4.3 us, a launch.
-template <typename U>
-__device__ __forceinline__ void move_units(const unsigned char* src, unsigned char* dst, long units, long first) {
-    const U* from = reinterpret_cast<const U*>(src);
-    U* to = reinterpret_cast<U*>(dst);
-    U x[kReorderUnits / kReorderThreads];
+// Rows of many arrays: dst[i] = src[parents[i]].  Bound by HBM; a block writes 32 KiB of a row, eight aligned 16-byte units a thread, all
+// loaded before the first store.  Where a row of src starts elsewhere within 16 bytes than its row of dst, a unit is put together from two
+// aligned loads, of which the second is the next lane's first; what is left at a row's ends moves byte by byte.  48 dense caches of 16 rows
+// of 512 KiB: 103 us, the copy peak; of 512 KiB and a byte 114 (byte by byte 488); 16 rows of five small arrays 4.3 us, a launch.
+constexpr int kReorderLoads = kReorderUnits / kReorderThreads;
+__device__ __forceinline__ void move_aligned(const unsigned char* src, unsigned char* dst, long bytes, long first) {
+    const uint4* from = reinterpret_cast<const uint4*>(src);
+    uint4* to = reinterpret_cast<uint4*>(dst);
+    const long units = bytes / 16;
+    uint4 x[kReorderLoads];
 #pragma unroll
-    for (int i = 0; i < kReorderUnits / kReorderThreads; ++i) {
+    for (int i = 0; i < kReorderLoads; ++i) {
         const long at = first + i * kReorderThreads + threadIdx.x;
         if (at < units) x[i] = __ldcs(from + at);
     }
 #pragma unroll
-    for (int i = 0; i < kReorderUnits / kReorderThreads; ++i) {
+    for (int i = 0; i < kReorderLoads; ++i) {
         const long at = first + i * kReorderThreads + threadIdx.x;
         if (at < units) __stcs(to + at, x[i]);
     }
 }
+// Unit v of a row: the v-th 16 bytes of dst, counted from the aligned address at or before its start.  Whole units are those that lie
+// within the row with both aligned loads; fewer than 64 bytes ahead of them and behind them go one to a thread.
+__device__ __forceinline__ void move_shifted(const unsigned char* src, unsigned char* dst, long bytes, long first) {
+    const int lane = threadIdx.x & 31, lead = (int)(reinterpret_cast<uintptr_t>(dst) & 15);
+    const int off = (int)((reinterpret_cast<uintptr_t>(src) - lead) & 15);          // of a unit's first byte in src
+    const long begin = (off + lead + 15) >> 4, end = max(begin, (bytes - (off ? 32 - off : 16) + lead + 16) >> 4);
+    if (first == 0 && threadIdx.x < 128) {
+        const long from = end > begin ? 16 * end - lead : 0, to = end > begin ? 16 * begin - lead : 0;
+        const long j = threadIdx.x < 64 ? (long)threadIdx.x : from + threadIdx.x - 64;
+        if (j < (threadIdx.x < 64 ? to : bytes)) dst[j] = src[j];
+    }
+    constexpr int kAtOnce = kReorderLoads / 2;
+#pragma unroll 1
+    for (int part = 0; part < 2; ++part) {
+        const long v0 = begin + first + part * kAtOnce * kReorderThreads + threadIdx.x;
+        uint4 a[kAtOnce], b[kAtOnce];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            const long v = v0 + i * kReorderThreads;
+            a[i] = b[i] = make_uint4(0, 0, 0, 0);
+            if (v < end) {
+                const uint4* from = reinterpret_cast<const uint4*>(src + 16 * v - lead - off);
+                a[i] = __ldcs(from);
+                if (off != 0 && (lane == 31 || v + 1 == end)) b[i] = __ldcs(from + 1);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            const long v = v0 + i * kReorderThreads;
+            uint4 y = a[i], z = b[i];
+            if (off != 0) {
+                const uint4 n = make_uint4(__shfl_down_sync(0xffffffffu, y.x, 1), __shfl_down_sync(0xffffffffu, y.y, 1), __shfl_down_sync(0xffffffffu, y.z, 1), __shfl_down_sync(0xffffffffu, y.w, 1));
+                if (lane != 31 && v + 1 < end) z = n;
+                const int bits = 8 * (off & 3);
+                const uint32_t w[8] = {y.x, y.y, y.z, y.w, z.x, z.y, z.z, z.w};
+                uint32_t t[5];
+#pragma unroll
+                for (int j = 0; j < 5; ++j) t[j] = off < 4 ? w[j] : off < 8 ? w[min(j + 1, 7)] : off < 12 ? w[min(j + 2, 7)] : w[min(j + 3, 7)];
+                y = make_uint4(__funnelshift_r(t[0], t[1], bits), __funnelshift_r(t[1], t[2], bits), __funnelshift_r(t[2], t[3], bits), __funnelshift_r(t[3], t[4], bits));
+            }
+            if (v < end) __stcs(reinterpret_cast<uint4*>(dst + 16 * v - lead), y);
+        }
+    }
+}
 
-__global__ void __launch_bounds__(kReorderThreads)
+__global__ void __launch_bounds__(kReorderThreads, 4)
 beam_reorder_kernel(const __grid_constant__ ReorderParams p) {
     grid_dependency_wait();
     grid_launch_dependents();
@@ -461,11 +507,9 @@ beam_reorder_kernel(const __grid_constant__ ReorderParams p) {
     const long bytes = p.row_bytes[lo];
     const unsigned char* src = p.src[lo] + (size_t)from * bytes;
     unsigned char* dst = p.dst[lo] + (size_t)row * bytes;
-    const uintptr_t x = reinterpret_cast<uintptr_t>(p.src[lo]) | reinterpret_cast<uintptr_t>(p.dst[lo]) | (uintptr_t)bytes;
     const long first = (long)part * kReorderUnits;
-    if ((x & 15) == 0) move_units<uint4>(src, dst, bytes / 16, first);
-    else if ((x & 3) == 0) move_units<uint32_t>(src, dst, bytes / 4, first);
-    else move_units<unsigned char>(src, dst, bytes, first);
+    if (reorder_aligned(p.src[lo], p.dst[lo], bytes)) move_aligned(src, dst, bytes, first);
+    else move_shifted(src, dst, bytes, first);
 }
 
 }  // namespace

@@ -42,12 +42,13 @@ struct ReorderParams {
     int n_states, n_in, n_out;
 };
 constexpr int kReorderThreads = 256;
-constexpr int kReorderUnits = 8 * kReorderThreads;             // 16-byte (or 4-byte, or 1-byte) units of a row that a block moves
-// bytes of the widest unit that all rows of an array start and end on
-inline int reorder_unit(const void* src, const void* dst, long row_bytes) {
-    const uintptr_t x = reinterpret_cast<uintptr_t>(src) | reinterpret_cast<uintptr_t>(dst) | (uintptr_t)row_bytes;
-    return x & 3 ? 1 : x & 15 ? 4 : 16;
+constexpr int kReorderUnits = 8 * kReorderThreads;             // 16-byte units of a row that a block moves
+// all rows of an array start and end on 16-byte boundaries, in src and in dst
+__host__ __device__ inline bool reorder_aligned(const void* src, const void* dst, long row_bytes) {
+    return ((reinterpret_cast<uintptr_t>(src) | reinterpret_cast<uintptr_t>(dst) | (uintptr_t)row_bytes) & 15) == 0;
 }
+// units of a row; an unaligned one may start and end within a unit
+inline long reorder_units(const void* src, const void* dst, long row_bytes) { return reorder_aligned(src, dst, row_bytes) ? row_bytes / 16 : (row_bytes + 30) / 16; }
 cudaError_t launch_beam_select(BeamParams p, int logits_dtype, cudaStream_t st);
 cudaError_t launch_beam_reorder(const ReorderParams& p, cudaStream_t st);
 

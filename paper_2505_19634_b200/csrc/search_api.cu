@@ -189,7 +189,7 @@ int tts_beam_reorder(tts_ctx* ctx, int n_states, const void* const* src, void* c
     for (int i = 0; i < n_states; ++i) {
         if (!src[i] || !dst[i] || row_bytes[i] < 1 || row_bytes[i] >= (1ll << 40)) return TTS_ERR_INVALID;
         p.src[i] = static_cast<const unsigned char*>(src[i]); p.dst[i] = static_cast<unsigned char*>(dst[i]); p.row_bytes[i] = row_bytes[i];
-        const long units = row_bytes[i] / reorder_unit(src[i], dst[i], row_bytes[i]);
+        const long units = reorder_units(src[i], dst[i], row_bytes[i]);
         p.first[i] = (int)blocks;
         blocks += (units + kReorderUnits - 1) / kReorderUnits * n_children;
         if (blocks >= (1l << 31)) return TTS_ERR_UNSUPPORTED;

@@ -166,6 +166,24 @@ def test_reorder_of_rows_off_their_alignment(off):
     assert torch.equal(dst[16:48].view(2, 16), src[off:off + 112].view(7, 16)[[6, 0]]) and not dst[48:].any() and not dst[:16].any()
 
 
+@pytest.mark.parametrize("bytes_", [1, 15, 16, 17, 31, 32, 33, 47, 48, 49, 63, 500, 32767, 32769, 65541])
+def test_reorder_of_rows_at_every_shift(bytes_):
+    """Rows of src and dst that start at all pairs of places within 16 bytes; nothing beside them changes."""
+    gen = torch.Generator().manual_seed(bytes_)
+    src, dst = [], []
+    for shift in range(16):
+        src.append(torch.randint(0, 256, (4 * bytes_ + 16,), generator=gen, dtype=torch.uint8).cuda())
+        dst.append(torch.randint(0, 256, (3 * bytes_ + 32,), generator=gen, dtype=torch.uint8).cuda())
+    parents, want = [3, 0, 2], [x.clone() for x in dst]
+    for shift in range(16):
+        for i, p in enumerate(parents):
+            want[shift][(7 * shift) % 16 + i * bytes_:][:bytes_] = src[shift][shift + p * bytes_:][:bytes_]
+    ctx = tts.TtsContext(1, 1, 1, 1, 1, 1)
+    states = tts.TtsStates([x.data_ptr() + i for i, x in enumerate(src)], [x.data_ptr() + 7 * i % 16 for i, x in enumerate(dst)], [bytes_] * 16)
+    ctx.tts_beam_reorder(states, ints(parents), 4, 3)
+    assert all(torch.equal(a, b) for a, b in zip(dst, want)) and ctx.tts_last_status() == 0
+
+
 def test_reorder_reports_parents_outside():
     src, dst = torch.ones(3, 32, dtype=torch.uint8, device="cuda"), torch.zeros(3, 32, dtype=torch.uint8, device="cuda")
     ctx = tts.TtsContext(1, 1, 1, 1, 1, 1)
