@@ -5,7 +5,7 @@
 // Within a row the score rises with the logit, so a question's n best are among the n largest logits of each row.
 //
 // Bound by HBM (or, for few rows, by latency).  A row is cut into 1 to 8 parts, one CTA each, read once in chunks of four 16-byte loads a
-// thread (what lies behind the last whole chunk one by one): their exponentials go to a running sum, their largest to shared memory.  The n-th largest of the threads' maxima is a lower
+// thread (what is left of a load one by one, and short parts): their exponentials go to a running sum, their largest to shared memory.  The n-th largest of the threads' maxima is a lower
 // bound of the n-th largest logit; of the few places whose maximum reaches it the logits are read again (from L2) and listed.  The CTA that
 // ends a question's last part does the same with the entries of all of them, whose scores it forms in 64 bits (which of two candidates is
 // better does not hang on a rounding to 32 bits), and ranks what is left by comparing each with each.  Where numbers are so alike or so
@@ -255,13 +255,18 @@ beam_select_kernel(const __grid_constant__ BeamParams p) {
         const T* x = static_cast<const T*>(p.logits) + (size_t)row * p.row_stride;
         const int begin = min(p.vocab, (int)blockIdx.x * p.per_part), end = min(p.vocab, begin + p.per_part);
         constexpr int kVec = 16 / sizeof(T), kChunk = kThreads * kLoads * kVec;       // logits of a load, of a chunk
-        const int chunks = (end - begin) / kChunk, behind = begin + chunks * kChunk, singles = end - behind;
+        // (less than half a chunk goes one by one: the loads would leave threads without a logit, and the bound below would let too much through)
+        const int behind = end - begin < kChunk / 2 ? begin : begin + (end - begin) / kVec * kVec, singles = end - behind, chunks = (behind - begin + kChunk - 1) / kChunk;
         const int per_place = (chunks + kPlaces - 1) / kPlaces;     // chunks of a maximum
         auto index = [&](int chunk, int i) { return begin + chunk * kChunk + (i / kVec) * (kThreads * kVec) + tid * kVec + i % kVec; };
         auto fetch = [&](int chunk, uint4 (&raw)[kLoads]) {
 #pragma unroll
             for (int c = 0; c < kLoads; ++c) {
-                const T* from = x + index(chunk, c * kVec);
+                const int at = index(chunk, c * kVec);
+                const T* from = x + at;
+                constexpr uint32_t kNone = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;          // -infinity
+                raw[c] = make_uint4(kNone, kNone, kNone, kNone);
+                if (at >= behind) continue;                         // (behind the part's end in its last chunk)
                 if constexpr (kAligned) raw[c] = *reinterpret_cast<const uint4*>(from);
                 else {
                     uint32_t w[4];
@@ -364,6 +369,7 @@ beam_select_kernel(const __grid_constant__ BeamParams p) {
 #pragma unroll 1
             for (int i = tid >> 2; i < n_tasks; i += kThreads / 4) {
                 const int chunk = sh.tasks[i] / kThreads, who = sh.tasks[i] % kThreads, at = begin + chunk * kChunk + (tid & 3) * (kThreads * kVec) + who * kVec;
+                if (at >= behind) continue;
                 float v[kVec];
                 if constexpr (kAligned) {
                     const uint4 r = *reinterpret_cast<const uint4*>(x + at);
