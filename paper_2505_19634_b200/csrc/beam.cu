@@ -164,10 +164,14 @@ __device__ void join_parts(const BeamParams& p, Shared& sh, int group) {
     const size_t out = (size_t)group * k;
     const u64* entries = p.entries + ((size_t)row0 << (p.parts_log2 + p.cap_log2));
     const int n = __ldcg(p.n_entries + group);
+    // A thread looks at every 256th entry, from the one whose number is its own with the bits in reverse: few entries lie in all groups of
+    // threads alike then, and the bound does not fall to the least of them (4 beams of 32000 logits: 9.5 us instead of 14.0).
+    const int mine = (int)(__brev((unsigned)tid) >> 24);
+    static_assert(kThreads == 256, "eight bits");
     constexpr int kAhead = kList / kThreads;
     u64 e[kAhead];                                                  // (asked for ahead of the logarithms)
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) e[i] = tid + i * kThreads < n ? __ldcg(entries + tid + i * kThreads) : 0;
+    for (int i = 0; i < kAhead; ++i) e[i] = mine + i * kThreads < n ? __ldcg(entries + mine + i * kThreads) : 0;
     if (tid == 0) sh.few.n = 0;
     // the rows' logarithms, eight lanes each; NaN for a row that offers nothing.  (A finished beam's candidate has a logit of 0.)
     const int sub = tid & 7;
@@ -209,20 +213,20 @@ __device__ void join_parts(const BeamParams& p, Shared& sh, int group) {
         listed = sh.list.n;
         best = 0;
         if (listed <= kList)
-            for (int i = tid; i < listed; i += kThreads) best = max(best, sh.list.keys[i]);
+            for (int i = mine; i < listed; i += kThreads) best = max(best, sh.list.keys[i]);
     } else {
 #pragma unroll
         for (int i = 0; i < kAhead; ++i)
-            if (tid + i * kThreads < n) {
+            if (mine + i * kThreads < n) {
                 const u64 key = score(e[i]);
-                sh.list.keys[tid + i * kThreads] = key; sh.list.places[tid + i * kThreads] = (uint32_t)e[i];
+                sh.list.keys[mine + i * kThreads] = key; sh.list.places[mine + i * kThreads] = (uint32_t)e[i];
                 best = max(best, key);
             }
     }
     if (listed > kList) bisect<64>(sh, sh.few, k, all);
     else {
         const u64 least = max(lower_bound(sh, best, k), (u64)1);
-        auto each = [&](auto f) { for (int i = tid; i < listed; i += kThreads) f(sh.list.keys[i], sh.list.places[i]); };
+        auto each = [&](auto f) { for (int i = mine; i < listed; i += kThreads) f(sh.list.keys[i], sh.list.places[i]); };
         each([&](u64 key, uint32_t place) { if (key >= least) sh.few.put(key, place); });
         __syncthreads();
         if (sh.few.n > kThreads) bisect<64>(sh, sh.few, k, each);
