@@ -107,13 +107,14 @@ __device__ __noinline__ u64 lower_bound(Shared& sh, u64 m, int k) {
     if (tid == 0) sh.threshold = 0;
     if ((tid & ((1 << shift) - 1)) == 0) sh.groups[tid >> shift] = m;
     __syncthreads();
-    if (tid < groups) {
-        const u64 own = sh.groups[tid];
-        int r = 0;
-#pragma unroll 8
-        for (int j = 0; j < groups; ++j) { const u64 other = sh.groups[j]; r += other > own || (other == own && j < tid); }
-        if (r == k - 1) sh.threshold = own;
-    }
+    // 2^shift threads rank a group's maximum among the others
+    const int g = tid >> shift;
+    const u64 own = sh.groups[g];
+    int r = 0;
+#pragma unroll 4
+    for (int j = tid & ((1 << shift) - 1); j < groups; j += 1 << shift) { const u64 other = sh.groups[j]; r += other > own || (other == own && j < g); }
+    for (int o = 1; o < 1 << shift; o <<= 1) r += __shfl_xor_sync(0xffffffffu, r, o);
+    if (r == k - 1) sh.threshold = own;
     __syncthreads();
     return sh.threshold;
 }
@@ -232,13 +233,17 @@ __device__ void join_parts(const BeamParams& p, Shared& sh, int group) {
         if (sh.few.n > kThreads) bisect<64>(sh, sh.few, k, each);
     }
     const int n_few = sh.few.n;
-    if (tid < n_few) {
-        const u64 key = sh.few.keys[tid];
-        const uint32_t place = sh.few.places[tid];
+    int wide = 0;                                                   // 2^wide threads rank one of them
+    while (wide < 5 && n_few << (wide + 1) <= kThreads) ++wide;
+    {
+        const int i = tid >> wide;
+        const u64 key = i < n_few ? sh.few.keys[i] : 0;
+        const uint32_t place = i < n_few ? sh.few.places[i] : 0;
         int rank = 0;
 #pragma unroll 4
-        for (int j = 0; j < n_few; ++j) rank += sh.few.keys[j] > key || (sh.few.keys[j] == key && sh.few.places[j] < place);
-        if (rank < k) {
+        for (int j = tid & ((1 << wide) - 1); j < n_few; j += 1 << wide) rank += sh.few.keys[j] > key || (sh.few.keys[j] == key && sh.few.places[j] < place);
+        for (int o = 1; o < 1 << wide; o <<= 1) rank += __shfl_xor_sync(0xffffffffu, rank, o);
+        if (i < n_few && rank < k) {
             const uint32_t b = place / (uint32_t)p.vocab;
             p.parents[out + rank] = row0 + (int)b;
             p.tokens[out + rank] = (int)(place - b * (uint32_t)p.vocab);
