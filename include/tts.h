@@ -583,7 +583,7 @@ TTS_API int tts_kv8_compact(tts_ctx* ctx, int n_layers, void* const* kv8_pools, 
  *                      tokens, scores  device  [n_groups][n_select] i32, fp32
  *                    Where a question has fewer candidates, the places behind them get parents = tokens = -1, scores = -infinity.  A row with a
  *                    NaN or +infinity among its logits, or nothing but -infinity, has no candidate.
- *                    n_beams * n_select <= 8192 and n_beams * vocab < 2^31 (TTS_ERR_UNSUPPORTED).
+ *                    n_beams * n_select <= 8192 and n_beams * vocab < 2^31 - 2^16 (TTS_ERR_UNSUPPORTED).
  *   tts_beam_reserve allocates what tts_beam_select needs for up to max_rows rows (n_groups * n_beams, <= cfg.max_branches) and max_select
  *                    (<= 128) continuations per question.  Call it once per context; a later call with smaller or equal numbers returns
  *                    TTS_OK, with a larger one TTS_ERR_INVALID.  Not inside a stream capture.  The context's calls of tts_beam_select share that

@@ -104,6 +104,9 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
 // An item's start and end (queries, join of the warps) take about as long as so many pages (kv8_run.cuh).  64 single tokens of 1024 to
 // 8192 keys: 120 us, 125 with 16, 137 with none; a drafted step of 20 rows 55.5, 56.3, 57.3.
 constexpr int kItemUnits = 48;
+// Of a CTA's share of an item, where items are cut evenly: two to eight for a warp.  One branch of 1000 keys, 40 / 8 heads: 10.1 us with 16 pages to
+// a CTA, 12.3 with 64; 16 branches of 500 keys: 10.4 us uncut, 15.5 with 16.
+constexpr int kLeastPages = 2 * kWarps, kMostPages = 8 * kWarps;
 using Walk = Kv8Walk<kPage, kItemUnits>;
 
 // S^T = K Q^T of two pages: s[page][n][j], j: (token a or b) * 2 + (row 2 t or 2 t + 1)
@@ -174,10 +177,8 @@ kv8_attn_kernel(const __grid_constant__ Kv8AttnParams p) {
     grid_dependency_wait();
     grid_launch_dependents();
     kv8_scan_units<kThreads, kPage, kItemUnits>(p, cum, reinterpret_cast<long long*>(join));
-    // A contiguous run of at least two pages for each warp; or, where there are no more items than CTAs and none has more than eight pages
-    // for a warp, an item each: joining parts takes about as long as four pages.
-    const Kv8Run run = kv8_run<kThreads, kItemUnits>(p, cum, 2 * kWarps, 8 * kWarps);
-    const long long begin = run.begin, per_cta = run.per_cta;
+    const Kv8Run run = kv8_run<kThreads, kItemUnits>(p, cum, reinterpret_cast<int*>(join), kLeastPages, kMostPages);
+    const long long begin = run.begin;
     const int n_units = run.n;
     if (n_units <= 0) return;
 
@@ -452,7 +453,7 @@ kv8_attn_kernel(const __grid_constant__ Kv8AttnParams p) {
 
         // ---- join the warps: maxima, sums and O of every row
         const bool whole = item.whole();
-        const Kv8Parts cut = kv8_parts(item, begin + (n_units - item.left), per_cta);
+        const Kv8Parts cut = kv8_parts(item, run);
         pairs_before += pairs;
         more_items = item.next(p);
         if (more_items) ask_q();

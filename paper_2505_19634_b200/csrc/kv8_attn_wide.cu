@@ -41,7 +41,8 @@ constexpr uint32_t kTmemCols = 256, kColS = 0, kColO = 128;
 // An item's start and end take about as long as so many tiles (kv8_run.cuh).  64 (branch, KV head)s of 120 tiles: 93 us with 12, 97 with 4,
 // 122 with 24 (125 rows); 197, 197 and 209 (300 rows, three blocks).
 constexpr int kItemUnits = 12;
-constexpr int kLeastTiles = 4, kWholeTiles = 16;                    // a run has no fewer tiles; items of no more are not cut where CTAs are plenty
+// Of a CTA's share of an item, where items are cut evenly.  100 rows of 40 / 8 heads over 8 k keys: 48.6 us with 16, 53.4 with 12, 51.7 with 24.
+constexpr int kLeastTiles = 8, kMostTiles = 16;
 using Walk = Kv8Walk<kTile, kItemUnits>;
 
 constexpr int kOperand = kTile * kHeadDim * 2;                      // fp16 K, and V, of a tile: two blocks of 64 dims, rows of 128 bytes
@@ -166,7 +167,7 @@ kv8_attn_wide_kernel(const __grid_constant__ Kv8AttnParams p) {
     grid_dependency_wait();
     grid_launch_dependents();
     kv8_scan_units<kThreads, kTile, kItemUnits>(p, cum, reinterpret_cast<long long*>(smem + kOffSums));
-    const Kv8Run run = kv8_run<kThreads, kItemUnits>(p, cum, kLeastTiles, kWholeTiles);
+    const Kv8Run run = kv8_run<kThreads, kItemUnits>(p, cum, reinterpret_cast<int*>(smem + kOffSums), kLeastTiles, kMostTiles);
     Walk item;
     const bool work = run.n > 0 && item.init(p, cum, run.begin, run.n);   // every role walks over the pieces for itself
     bool alive = work;
@@ -507,7 +508,7 @@ kv8_attn_wide_kernel(const __grid_constant__ Kv8AttnParams p) {
             wait(O_FULL, pieces & 1);
             tc_fence_after();
             const bool whole = item.whole(), valid = r < rows;
-            const Kv8Parts cut = kv8_parts(item, run.begin + (run.n - item.left), run.per_cta);
+            const Kv8Parts cut = kv8_parts(item, run);
             const size_t slot = 2 * (size_t)blockIdx.x + (item.nth == 0 ? 0 : 1);
             auto write_lse = [&](size_t row, float m, float sum) {      // natural logarithm
                 p.lse[row] = sum == 0.f ? -INFINITY : (m + log2_approx(sum)) * 0.6931471805599453f;

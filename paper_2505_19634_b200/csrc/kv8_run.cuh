@@ -3,7 +3,8 @@
 // An item is a (branch, KV head, block of stacked rows).  It has a unit for every kUnitTokens tokens (an empty branch's: one), behind
 // kStart units for what a piece of an item costs besides (queries, the join of its parts): so a CTA with many short items gets
 // fewer tokens.  All items follow one another, a CTA owns a contiguous run of units and walks over its pieces of items; what it has of
-// an item that others work on too it leaves as a part, and the last one to do so joins them.
+// an item that others work on too it leaves as a part, and the last one to do so joins them.  Where there are CTAs enough to give each
+// a small share of one item only, items are cut evenly instead.
 #pragma once
 #include "kv8.cuh"
 
@@ -53,26 +54,42 @@ __device__ void kv8_scan_units(const Kv8AttnParams& p, long long* cum, long long
     __syncthreads();
 }
 
-// The CTA's run: n units from `begin` on; all threads of the block.  At least `least` units of tokens; or, where there are no more items
-// than CTAs and none has more than `whole` units of tokens, an item each.
-struct Kv8Run { long long begin, per_cta; int n; };
+// The CTA's run: n units from `begin` on; all threads of the block.  Joining an item's parts takes time in proportion to their number, so
+// an even cut makes shares of 1.5 times the root of the longest item's units, at least `least`, more where CTAs are few; it is for
+// shares of up to `most`.  Otherwise a CTA has at least `least` units of tokens.
+struct Kv8Run {
+    long long begin, per_cta;
+    int n;
+    int cut, each;          // an even cut: CTAs to an item, units of tokens to a CTA; or 0
+};
 template <int kThreads, int kStart>
-__device__ __forceinline__ Kv8Run kv8_run(const Kv8AttnParams& p, const long long* cum, int least, int whole) {
+__device__ __forceinline__ Kv8Run kv8_run(const Kv8AttnParams& p, const long long* cum, int* word, int least, int most) {
+    const int per_branch = p.Hkv * p.n_rb;
     const long long total = cum[p.n_branches];
     Kv8Run r;
+    r.cut = r.each = 0;
+    if (p.n_branches * per_branch <= (int)gridDim.x) {
+        if (threadIdx.x == 0) *word = 0;
+        __syncthreads();
+        for (int b = threadIdx.x; b < p.n_branches; b += kThreads) atomicMax(word, (int)((cum[b + 1] - cum[b]) / per_branch) - kStart);
+        __syncthreads();
+        const int longest = *word, share = max(least, (int)(1.5f * sqrtf((float)longest)));
+        const int cut = min((longest + share - 1) / share, (int)gridDim.x / (p.n_branches * per_branch)), each = (longest + cut - 1) / cut;
+        if (each <= max(most, share)) {
+            r.cut = cut; r.each = each; r.per_cta = 0;
+            const int item = blockIdx.x / cut, b = item / per_branch;
+            r.n = 0; r.begin = 0;
+            if (b < p.n_branches) {
+                const int units = (int)((cum[b + 1] - cum[b]) / per_branch), first = (int)(blockIdx.x - item * cut) * r.each;
+                r.n = min(units - kStart - first, r.each);          // (not positive where the branch has no tokens left for this CTA)
+                r.begin = cum[b] + (long long)(item - b * per_branch) * units + kStart + first;
+            }
+            return r;
+        }
+    }
     r.per_cta = max((long long)kStart + least, (total + gridDim.x - 1) / gridDim.x);
     r.begin = (long long)blockIdx.x * r.per_cta;
     r.n = (int)min(max(total - r.begin, 0ll), r.per_cta);           // (fits: the host refuses more than 2^31 units to a CTA)
-    const int per_branch = p.Hkv * p.n_rb;
-    if (p.n_branches * per_branch <= (int)gridDim.x) {
-        bool large = false;
-        for (int b = threadIdx.x; b < p.n_branches; b += kThreads) large |= cum[b + 1] - cum[b] > (long long)(kStart + whole) * per_branch;
-        if (!__syncthreads_or(large)) {
-            const int b = blockIdx.x / per_branch;
-            r.n = b < p.n_branches ? (int)((cum[b + 1] - cum[b]) / per_branch) : 0;
-            if (b < p.n_branches) r.begin = cum[b] + (long long)(blockIdx.x - b * per_branch) * r.n;
-        }
-    }
     return r;
 }
 
@@ -124,11 +141,15 @@ struct Kv8Parts {
     __device__ __forceinline__ int slot(int k) const { return 2 * (cta0 + k) + (k == 0 && behind ? 1 : 0); }
 };
 template <class Walk>
-__device__ __forceinline__ Kv8Parts kv8_parts(const Walk& w, long long piece, long long per_cta) {     // piece: its first unit
-    const long long item = piece - w.from, tokens = item + Walk::kItemStart;
+__device__ __forceinline__ Kv8Parts kv8_parts(const Walk& w, const Kv8Run& run) {
     Kv8Parts c;
-    c.cta0 = (int)(tokens / per_cta); c.n = (int)((item + w.units - 1) / per_cta) - c.cta0 + 1;
-    c.behind = item > c.cta0 * per_cta;
+    if (run.cut) {
+        c.cta0 = (int)blockIdx.x - (int)blockIdx.x % run.cut; c.n = (w.units - Walk::kItemStart + run.each - 1) / run.each; c.behind = false;
+        return c;
+    }
+    const long long item = run.begin + (run.n - w.left) - w.from, tokens = item + Walk::kItemStart;
+    c.cta0 = (int)(tokens / run.per_cta); c.n = (int)((item + w.units - 1) / run.per_cta) - c.cta0 + 1;
+    c.behind = item > c.cta0 * run.per_cta;
     return c;
 }
 

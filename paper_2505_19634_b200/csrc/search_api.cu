@@ -151,7 +151,7 @@ int tts_beam_select(tts_ctx* ctx, const void* logits, int logits_dtype, int64_t 
     if (!c || !logits || !beam_scores || !parents || !tokens || !scores) return TTS_ERR_INVALID;
     if (logits_dtype != TTS_LOGITS_BF16 && logits_dtype != TTS_LOGITS_FP32) return TTS_ERR_UNSUPPORTED;
     if (vocab < 1 || n_groups < 1 || n_beams < 1 || n_select < 1 || (long)n_groups * n_beams > c->beam_rows || n_select > c->beam_select) return TTS_ERR_INVALID;
-    if ((long)n_beams * n_select > kMaxBeamCandidates || (long)n_beams * vocab >= (1l << 31)) return TTS_ERR_UNSUPPORTED;
+    if ((long)n_beams * n_select > kMaxBeamCandidates || (long)n_beams * vocab >= (1l << 31) - (1l << 16)) return TTS_ERR_UNSUPPORTED;
     if (finished && (pad_token < 0 || pad_token >= vocab)) return TTS_ERR_INVALID;
     if (row_stride < vocab || row_stride >= (1ll << 38)) return TTS_ERR_INVALID;
     const size_t elt = logits_dtype == TTS_LOGITS_BF16 ? 2 : 4, rows = (size_t)n_groups * n_beams, picks = (size_t)n_groups * n_select * 4;
