@@ -4,11 +4,12 @@
 // a page become operands once for 24 rows, here once for 128, and the products are the tensor cores' own.
 //
 // Two CTAs share an SM, so that one's exponentials run while the tensor cores work for the other.  64 tokens and 128 rows cost 512
-// clocks of the tensor cores, 512 of the exponentials' unit and, in shared memory, about 1100: Q, K and V as operands (512), codes read,
-// written in fp16 and fetched (512).  Measured: about 1550 clocks, most of them spent issuing (4400 instructions, half for the softmax)
-// and waiting at the roles' barriers.  8 trees of 60 nodes, 300 rows to a KV head, over 7.9 k keys: 195 us = 390 TFLOP/s; the kernel for
-// few rows took 410, that one's layout with converted tiles in shared memory and this one's products 779.  With Q in TMEM, or K's and V's
-// conversion by warps of their own, or V's operand twice: 192, 193 and 229 us.  In a CTA,
+// clocks of the tensor cores, 512 of the exponentials' unit and, in shared memory, about 1200: Q, K and V as operands (512), codes read,
+// written in fp16 and fetched (512), scales, barriers.  Measured: about 1550 clocks, and a third of a call around them: 18000 clocks until the
+// first product (cold instructions and TLBs), up to 35000 behind a piece's last (its rows, the fence, the join).  8 trees of 60 nodes,
+// 300 rows to a KV head, over 7.9 k keys: 193 us = 394 TFLOP/s; the kernel for few rows took 410.  All of these took 190 to 200 us as well: Q in
+// TMEM and one S; K's and V's conversion by warps of their own; a warp for each product; waits that sleep.  V's operand twice 229, codes
+// loaded a tile ahead into registers 319.  In a CTA,
 //   warps 0-7   softmax, two threads to a row, in warps w and w + 4: they lay out its query; per tile of 64 tokens each reads 32 of its
 //               scores from TMEM and leaves p sv there, as the second product's A operand; O is touched only when the maximum moves
 //               by more than 2^8 or the unit of p sv grows.  At a piece's end they write the row.
@@ -42,7 +43,7 @@ constexpr uint32_t kTmemCols = 256, kColS = 0, kColO = 128;
 // 122 with 24 (125 rows); 197, 197 and 209 (300 rows, three blocks).
 constexpr int kItemUnits = 12;
 // Of a CTA's share of an item, where items are cut evenly.  100 rows of 40 / 8 heads over 8 k keys: 48.6 us with 16, 53.4 with 12, 51.7 with 24.
-constexpr int kLeastTiles = 8, kMostTiles = 16;
+constexpr int kLeastTiles = 12, kMostTiles = 16;
 using Walk = Kv8Walk<kTile, kItemUnits>;
 
 constexpr int kOperand = kTile * kHeadDim * 2;                      // fp16 K, and V, of a tile: two blocks of 64 dims, rows of 128 bytes
