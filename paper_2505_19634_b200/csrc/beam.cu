@@ -15,9 +15,9 @@
 // Exponentials are fp32 (2^-22); 32 of them are summed in fp32, everything beyond in 64 bits.  For few rows the time is that of fetching
 // every instruction once (about 20 cycles each), which is why there are few phases and little unrolled code outside the pass.
 //
-// Measured: one question of 4 beams, 151936 logits 10.8 us; 16 questions of 16 beams, 152064 bf16 logits 34.9 us (78 MB: 11.9 us at the copy
-// peak, 39 million exponentials: 8.7).  Clocks of a CTA there: start 1300, pass 18300, bound 1900, list 6600, out and arrival 4000, join of a
-// question 10100.  All CTAs are resident at once, so nothing covers what lies behind the pass.
+// Measured: one question of 4 beams, 151936 logits 10.6 us; 16 questions of 16 beams, 152064 bf16 logits 31.7 us (78 MB: 11.9 us at the copy
+// peak, 39 million exponentials: 8.7).  Clocks of a CTA there: start 1300, pass 18300, bound, list, output and arrival about 11000, join of a
+// question 9000.  All CTAs are resident at once, so nothing covers what lies behind the pass.
 #include <math.h>
 
 #include <type_traits>
