@@ -164,3 +164,31 @@ def test_a_call_that_gave_up_leaves_the_context_usable():
     assert ctx.tts_last_status() == -5
     _, again, lse2 = attend(c, 16, 8, q=q, ctx=ctx)
     assert torch.equal(again, good) and torch.equal(lse2, lse)
+
+
+@pytest.mark.parametrize("rows", [1, 8])
+def test_as_many_branches_as_there_can_be(rows):
+    """1024 of them, some of them empty but for the prefix, for both kernels (8 and 64 rows)."""
+    c = k8.Cache8(k8.INT8, 1, [i % 23 if i % 7 else 0 for i in range(1024)], prefix=32, seed=25 + rows)
+    q, out, lse = attend(c, 8, rows, seed=26)
+    k8.assert_attention(c, q, rows, out, lse)
+
+
+@pytest.mark.parametrize("hq,hkv,rows", [(8, 1, 1), (8, 1, 8)])
+def test_two_streams_with_a_context_each(hq, hkv, rows):
+    """The same pages read at the same time by two contexts on two streams."""
+    c = k8.Cache8(k8.E4M3, hkv, [3000, 170, 900], prefix=16, seed=27)
+    q = torch.randn(3 * rows, hq, 128, generator=torch.Generator().manual_seed(28)).bfloat16().cuda()
+    _, want, _ = attend(c, hq, rows, q=q)
+    streams, contexts, outs = [torch.cuda.Stream() for _ in range(2)], [], []
+    for s in streams:
+        ctx = context(hq, hkv, 3, rows, c.width, c.num_pages)
+        ctx.tts_set_stream(s)
+        contexts.append(ctx)
+        outs.append(torch.zeros_like(want))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for ctx, out in zip(contexts, outs):
+            ctx.tts_kv8_attn(c.fmt, q, q.stride(0), c.pool, c.table, 16, c.branch_lens, None, 3, rows, out, None)
+    torch.cuda.synchronize()
+    assert all(torch.equal(out, want) for out in outs) and all(ctx.tts_last_status() == 0 for ctx in contexts)
