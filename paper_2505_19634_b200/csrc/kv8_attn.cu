@@ -3,15 +3,15 @@
 //   out[r] = sum_t softmax_t(scale <q_r, ck_t> sk_t) cv_t sv_t,   codes c and scales s of kv8.cuh
 //
 // For up to 48 rows to a KV head (kv8_attn_wide.cu: more).  Bound by HBM: a record of 4224 bytes (16 tokens) is read once for all rows
-// of the branch.  Work is cut into items (branch, KV head, block of up to 24 stacked rows; kv8_run.cuh); a CTA of 8 warps owns a
-// contiguous run of pages, warp w takes its pairs of pages w, w + 8, .. and works on them without meeting the other warps: they
+// of the branch.  Work is cut into items (branch, KV head, block of up to 24 stacked rows; kv8_run.cuh); a CTA of 8 warps (or
+// 12) owns a contiguous run of pages, warp w takes its pairs of pages w, w + 8, .. and works on them without meeting the other warps: they
 // come by bulk copies into a ring of the warp's own.  At the end of an item (or of the run) the warps join their results through
 // shared memory; items cut between CTAs are joined by the last CTA to finish one of their parts, which the others leave in
 // global memory.
 //
-// Measured (B200, copy peak 6538 GB/s): 64 single tokens over 1 k to 8 k keys, 40 / 8 heads, 120 us = 4.5 TB/s; a drafted step of 16 branches
-// with 20 rows to a KV head over 4 k to 5 k keys 56 us = 2.5 TB/s; 4 single tokens over 500 keys 8.6 us.  A warp takes about 1850 clocks for a page
-// of up to 8 rows (1460 without the copies, 950 with nothing but them) and 2240 for 24: conversion, products and exponentials of two
+// Measured (B200, copy peak 6538 GB/s): 64 single tokens over 1 k to 8 k keys, 40 / 8 heads, 111 us = 4.9 TB/s (twelve warps); a drafted step of 16 branches
+// with 20 rows to a KV head over 4 k to 5 k keys 55 us = 2.5 TB/s; 4 single tokens over 500 keys 8.6 us.  Of eight, a warp takes about 1850 clocks for a
+// page of up to 8 rows (1460 without the copies, 950 with nothing but them) and 2240 for 24: conversion, products and exponentials of two
 // warps to a scheduler.  A piece of an item costs 16000 clocks besides (queries 3000, the warps' join 9000, that of its parts 3700), a
 // third of the drafted step.  Tiles converted for the tensor cores' own products took 88 and 246 us for the first two.
 //
@@ -40,16 +40,16 @@ namespace {
 
 using namespace ptx;
 
-constexpr int kWarps = 8, kThreads = 32 * kWarps;
 constexpr int kPair = 2 * kKv8Record;                               // a warp works on two pages at a time
 constexpr float kFar = -1e30f;                                      // "no key yet": finite, so that differences are never NaN
 constexpr float kSlack = 8.f;                                       // log2 of how far a score may exceed the running maximum
 constexpr int kRoom = 6;                                            // p sv is held times 2^kRoom
 
-// Pairs of pages that a warp has in its ring, for up to 8 kNB rows, and the shared memory (bytes).
-template <int kNB>
+// The warps of a CTA for up to 8 kNB rows, the pairs of pages that each has in its ring, and the shared memory (bytes).
+template <int kNB, int kCtaWarps>
 struct Lay {
-    static constexpr int kStages = kNB == 1 ? 3 : 2;
+    static constexpr int kWarps = kCtaWarps, kThreads = 32 * kWarps;
+    static constexpr int kStages = kNB == 1 && kWarps == 8 ? 3 : 2;
     // the join: 16-byte chunks of a row and round, threads to a row
     static constexpr int kRounds = kNB == 2 ? 1 : 2;                // the warps' sums are joined all dims at once, or half of them twice
     static constexpr int kOffQ = kWarps * kStages * kPair;              // (behind the ring) [rows][256]: fp16 rows, 16-byte chunks exchanged (q_place)
@@ -60,12 +60,13 @@ struct Lay {
     static constexpr int kOffRowAt = kOffFactor + kRows * 4;        // [rows] (branch, row, head) of the results, as one number
     static constexpr int kOffMl = kOffRowAt + kRows * 4;            // [warps][rows] (maximum, sum)
     static constexpr int kOffExp = kOffMl + kWarps * kRows * 8;   // [warps] exponent of the sums' unit; then a flag
-    static constexpr int kOffCum = kOffExp + 64;                    // [branches + 1] units before each branch
-    static constexpr int kOffJoin = kOffCum + (kMaxBranches + 8) * 8;   // [warps][rows][128 / rounds] floats
+    static constexpr int kOffJoin = kOffExp + 64;                   // [warps][rows][128 / rounds] floats
+    static constexpr int kOffCum = kOffJoin + 256;                  // [branches + 1] units before each branch, until the first piece is found
     static constexpr int kOffBar = kOffJoin + kWarps * kRows * kHeadDim / kRounds * 4;   // [warps][stages]
     static constexpr int kOffAbort = kOffBar + kWarps * kStages * 8;   // [0] flag; [1 ..] scratch of each warp
     static constexpr int kBytes = kOffAbort + (1 + kWarps) * 4 + 12;
     static_assert(kBytes <= 232448 && kOffJoin % 16 == 0 && kWarps * 4 + 4 <= 64, "shared memory of a CTA");
+    static_assert(256 + (kMaxBranches + 1) * 8 <= kWarps * kRows * kHeadDim / kRounds * 4 && kWarps * 8 <= 256, "the branches' units, where the sums will be");
 };
 
 // Where chunk c of row r of a warp's sums lies: rows 2 t of the four t of a lane's group, and two groups, hit eight different bank groups.
@@ -106,7 +107,7 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
 constexpr int kItemUnits = 48;
 // Of a CTA's share of an item, where items are cut evenly: two to eight for a warp.  One branch of 1000 keys, 40 / 8 heads: 10.1 us with 16 pages to
 // a CTA, 12.3 with 64; 16 branches of 500 keys: 10.4 us uncut, 15.5 with 16.
-constexpr int kLeastPages = 2 * kWarps, kMostPages = 8 * kWarps;
+constexpr int kLeastPages = 16, kMostPages = 64;
 using Walk = Kv8Walk<kPage, kItemUnits>;
 
 // S^T = K Q^T of two pages: s[page][n][j], j: (token a or b) * 2 + (row 2 t or 2 t + 1)
@@ -154,11 +155,11 @@ __device__ __forceinline__ void scores(const unsigned char* pair, const unsigned
     }
 }
 
-template <int kFormat, int kNB>
-__global__ void __launch_bounds__(kThreads, 1)
+template <int kFormat, int kNB, int kCtaWarps>
+__global__ void __launch_bounds__(32 * kCtaWarps, 1)
 kv8_attn_kernel(const __grid_constant__ Kv8AttnParams p) {
-    using L = Lay<kNB>;
-    constexpr int kStages = L::kStages, kRows = L::kRows;
+    using L = Lay<kNB, kCtaWarps>;
+    constexpr int kWarps = L::kWarps, kThreads = L::kThreads, kStages = L::kStages, kRows = L::kRows;
     extern __shared__ __align__(128) unsigned char smem[];
     long long* cum = reinterpret_cast<long long*>(smem + L::kOffCum);
     unsigned char* q_rows = smem + L::kOffQ;
@@ -587,16 +588,21 @@ kv8_attn_kernel(const __grid_constant__ Kv8AttnParams p) {
 }  // namespace
 
 cudaError_t launch_kv8_attn(const Kv8AttnParams& p, int format, cudaStream_t st) {
-    auto launch = [&](auto fmt, auto nb) {
-        constexpr int kFormat = decltype(fmt)::value, kNB = decltype(nb)::value;
-        auto kernel = kv8_attn_kernel<kFormat, kNB>;
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Lay<kNB>::kBytes);
+    auto launch = [&](auto fmt, auto nb, auto warps) {
+        constexpr int kFormat = decltype(fmt)::value, kNB = decltype(nb)::value, kWarps = decltype(warps)::value;
+        using L = Lay<kNB, kWarps>;
+        auto kernel = kv8_attn_kernel<kFormat, kNB, kWarps>;
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes);
         if (e != cudaSuccess) return e;
-        return launch_dependent(kernel, p.grid, kThreads, Lay<kNB>::kBytes, st, p);
+        return launch_dependent(kernel, p.grid, L::kThreads, L::kBytes, st, p);
     };
+    const std::integral_constant<int, 8> eight;
     auto by_rows = [&](auto fmt) {
-        return p.rb_rows <= 8 ? launch(fmt, std::integral_constant<int, 1>{})
-             : p.rb_rows <= 16 ? launch(fmt, std::integral_constant<int, 2>{}) : launch(fmt, std::integral_constant<int, 3>{});
+        // Twelve warps where there are more than three items to a CTA: 64 single tokens of 1 k to 8 k keys, 8 KV heads 111 us, with eight 120; 64 of
+        // 300 26.8 and 28.2; 32 of 500 21.9 and 20.3.  (More rows take more registers than twelve warps have.)
+        if (p.rb_rows <= 8 && (long)p.n_branches * p.Hkv * p.n_rb > 3l * p.grid) return launch(fmt, std::integral_constant<int, 1>{}, std::integral_constant<int, 12>{});
+        return p.rb_rows <= 8 ? launch(fmt, std::integral_constant<int, 1>{}, eight)
+             : p.rb_rows <= 16 ? launch(fmt, std::integral_constant<int, 2>{}, eight) : launch(fmt, std::integral_constant<int, 3>{}, eight);
     };
     return format == TTS_KV8_E4M3 ? by_rows(std::integral_constant<int, TTS_KV8_E4M3>{}) : by_rows(std::integral_constant<int, TTS_KV8_INT8>{});
 }

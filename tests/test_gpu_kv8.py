@@ -438,3 +438,14 @@ def test_refusals():
     refused(-1, ctx.tts_kv8_copy_pages, tts.TtsKv8Pools([c.pool] * 129), ints([0]), ints([1]), 1)
     ctx.tts_kv8_copy_pages(tts.TtsKv8Pools([c.pool, c.pool, c.pool]), ints([0]), ints([0]), 1)
     assert ctx.tts_last_status() == 0
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("max_ctas", [1, 3, 10])
+def test_single_tokens_of_more_items_than_ctas(fmt, max_ctas):
+    """Items cut between CTAs, several to a CTA, some of them a page long."""
+    c = k8.Cache8(fmt, 3, [700, 1, 2500, 16, 17, 90, 1300], prefix=16, seed=21)
+    q, out, lse = attend(c, 12, 1, seed=14, max_ctas=max_ctas, out_dtype=tts.OUT_FP32)
+    k8.assert_attention(c, q, 1, out, lse)
+    _, again, _ = attend(c, 12, 1, q=q, max_ctas=max_ctas, out_dtype=tts.OUT_FP32)
+    assert torch.equal(again, out)
