@@ -38,9 +38,10 @@ constexpr int kTasks = 1024;                                        // places to
 constexpr int kList = 1024;                                         // entries of a list in shared memory
 static_assert(kMaxSelect <= kThreads && 1 << beam_cap_log2(kMaxSelect) <= kList, "");
 
-// Order-preserving maps of floating point to unsigned words; -infinity is the least number, and 0 is below it.
+// Order-preserving maps of floating point to unsigned words; -infinity is the least number, and 0 is below it.  Zeros of both signs are one
+// number (adding 0 makes them +0); a double here is a sum with such a logit and never -0.
 __device__ __forceinline__ uint32_t key_of(float x) {
-    const uint32_t b = __float_as_uint(x);
+    const uint32_t b = __float_as_uint(x + 0.f);
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ float value_of(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
