@@ -2,7 +2,8 @@
 //
 //   score(r, x) = beam_score[r] + logit[r][x] - log sum_y exp(logit[r][y]),   ties to the lowest (beam, token)
 //
-// Within a row the score rises with the logit, so a question's n best are among the n largest logits of each row.
+// Within a row the score does not fall where the logit rises, so a question's n best scores are among those of the n largest logits of each row;
+// which tokens have them takes a look at the row again where its logits are so small beside the score that 64 bits do not hold both.
 //
 // Bound by HBM (or, for few rows, by latency).  A row is cut into 1 to 8 parts, one CTA each, read once in chunks of four 16-byte loads a
 // thread (what is left of a load one by one, and short parts): their exponentials go to a running sum, their largest to shared memory.  The n-th largest of the threads' maxima is a lower
@@ -17,7 +18,7 @@
 // beams that lie closer than that may change places.  For few rows the time is that of fetching
 // every instruction once (about 20 cycles each), which is why there are few phases and little unrolled code outside the pass.
 //
-// Measured: one question of 4 beams, 151936 logits 10.6 us; 16 questions of 16 beams, 152064 bf16 logits 31.7 us (78 MB: 11.9 us at the copy
+// Measured: one question of 4 beams, 151936 logits 11.0 us; 16 questions of 16 beams, 152064 bf16 logits 31.9 us (78 MB: 11.9 us at the copy
 // peak, 39 million exponentials: 8.7).  Clocks of a CTA there: start 1300, pass 18300, bound, list, output and arrival about 11000, join of a
 // question 9000.  All CTAs are resident at once, so nothing covers what lies behind the pass.
 #include <math.h>
@@ -76,7 +77,10 @@ struct Lists {
 struct Shared {
     union {
         float maxima[kPlaces + 1][kThreads];                        // (the last of what is read one by one)
-        double base[kMaxBranches];                                  // of every row: its score so far less the logarithm of its sum
+        struct {
+            double base[kMaxBranches];                              // of every row: its score so far less the logarithm of its sum
+            bool done[kMaxBranches];                                // and whether it is a finished beam
+        };
     };
     Lists<kList> list;
     Lists<kThreads> few;
@@ -161,7 +165,60 @@ __device__ __forceinline__ void join_sums(float& top, double& sum) {
     top = all;
 }
 
+// A candidate's score, as a key; 0 is no candidate.
+__device__ __forceinline__ u64 score_key(double base, float logit) {
+    const double x = base + (double)logit;
+    return isfinite(x) ? key_of(x) : 0;
+}
+
+// Where a logit is so small beside its score that others of its row have the same score in 64 bits, the lists, which go by logits, may lack
+// tokens that are as good as the k-th best and come before some of theirs.  (What is better than the k-th best is listed: a part that leaves
+// out a candidate lists k that are not worse.)  All candidates of that score are looked at in their order, and the places of the result
+// behind the `above` better ones go to the first of them.
+template <typename T>
+__device__ __noinline__ void place_equals(const BeamParams& p, Shared& sh, int row0, size_t out, int above) {
+    constexpr int kEach = 8;                                        // tokens of a thread at a time
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const u64 t = sh.threshold;
+    int at = above;
+#pragma unroll 1
+    for (int b = 0; b < p.n_beams && at < p.n_select; ++b) {
+        const double base = sh.base[b];
+        const bool done = sh.done[b];
+        if (!isfinite(base)) continue;
+        const T* x = static_cast<const T*>(p.logits) + (size_t)(row0 + b) * p.row_stride;
+        const int n = done ? 1 : p.vocab;
+#pragma unroll 1
+        for (int x0 = 0; x0 < n && at < p.n_select; x0 += kThreads * kEach) {
+            const int first = x0 + tid * kEach;
+            unsigned hits = 0;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i)
+                if (first + i < n && score_key(base, done ? 0.f : (float)x[first + i] + 0.f) == t) hits |= 1u << i;
+            int before = __popc(hits);
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int c = __shfl_up_sync(0xffffffffu, before, o);
+                if (lane >= o) before += c;
+            }
+            if (lane == 31) sh.tasks[warp] = before;
+            before += at - __popc(hits);
+            __syncthreads();
+            for (int w = 0; w < kThreads / 32; ++w) {
+                if (w < warp) before += sh.tasks[w];
+                at += sh.tasks[w];
+            }
+            for (; hits && before < p.n_select; hits &= hits - 1, ++before) {
+                p.parents[out + before] = row0 + b;
+                p.tokens[out + before] = done ? p.pad_token : first + __ffs(hits) - 1;
+            }
+            __syncthreads();
+        }
+    }
+}
+
 // A question's parts put together by one block.
+template <typename T>
 __device__ void join_parts(const BeamParams& p, Shared& sh, int group) {
     const int tid = threadIdx.x, k = p.n_select, row0 = group * p.n_beams;
     const size_t out = (size_t)group * k;
@@ -190,14 +247,11 @@ __device__ void join_parts(const BeamParams& p, Shared& sh, int group) {
         const float before = p.beam_scores[row];
         const bool done = p.finished && p.finished[row];
         join_sums<8>(top, sum);
-        if (sub == 0) sh.base[b] = (double)before - (done ? 0.0 : (double)top + log(sum));
+        if (sub == 0) { sh.base[b] = (double)before - (done ? 0.0 : (double)top + log(sum)); sh.done[b] = done; }
     }
     if (tid < k) { p.parents[out + tid] = -1; p.tokens[out + tid] = -1; p.scores[out + tid] = -INFINITY; }      // where there are too few candidates
     __syncthreads();
-    auto score = [&](u64 entry) -> u64 {                            // as a key; 0 is no candidate
-        const double x = sh.base[(uint32_t)entry / (uint32_t)p.vocab] + (double)value_of((uint32_t)(entry >> 32));
-        return isfinite(x) ? key_of(x) : 0;
-    };
+    auto score = [&](u64 entry) { return score_key(sh.base[(uint32_t)entry / (uint32_t)p.vocab], value_of((uint32_t)(entry >> 32))); };
     auto all = [&](auto f) {
 #pragma unroll 4
         for (int i = tid; i < n; i += kThreads) { const u64 x = __ldcg(entries + i); f(score(x), (uint32_t)x); }
@@ -237,6 +291,7 @@ __device__ void join_parts(const BeamParams& p, Shared& sh, int group) {
     const int n_few = sh.few.n;
     int wide = 0;                                                   // 2^wide threads rank one of them
     while (wide < 5 && n_few << (wide + 1) <= kThreads) ++wide;
+    bool vague = false;                                             // another logit may have this score
     {
         const int i = tid >> wide;
         const u64 key = i < n_few ? sh.few.keys[i] : 0;
@@ -250,7 +305,17 @@ __device__ void join_parts(const BeamParams& p, Shared& sh, int group) {
             p.parents[out + rank] = row0 + (int)b;
             p.tokens[out + rank] = (int)(place - b * (uint32_t)p.vocab);
             p.scores[out + rank] = (float)value_of(key);
+            // Neighbouring logits are 2^-25 of themselves apart or more, scores 2^-52 or less: with one that is over 2^-26 of the score there is a
+            // score between them.
+            const double x = value_of(key);
+            vague = !sh.done[b] && fabs(x - sh.base[b]) <= 0x1p-26 * fabs(x);
+            if (rank == k - 1) sh.threshold = key;
         }
+    }
+    if (__syncthreads_or(vague) && n_few >= k) {
+        const u64 t = sh.threshold;
+        const int above = block_sum(tid < n_few && sh.few.keys[tid] > t, &sh.word);
+        place_equals<T>(p, sh, row0, out, above);
     }
 }
 
@@ -435,7 +500,7 @@ beam_select_kernel(const __grid_constant__ BeamParams p) {
     const bool last = sh.word;
     __syncthreads();
     if (!last) return;
-    join_parts(p, sh, group);
+    join_parts<T>(p, sh, group);
     if (tid == 0) p.n_entries[group] = 0;                           // as the next call expects it (all threads have read it)
 }
 

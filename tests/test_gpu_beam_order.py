@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import kv8_plain as k8
-from test_gpu_beam import normal, pick, starts
+from test_gpu_beam import ints, normal, pick, starts
 
 pytestmark = pytest.mark.gpu
 
@@ -59,6 +59,33 @@ def test_beams_are_told_apart_in_64_bits():
     parents, tokens, _ = pick(x.cuda(), scores.cuda(), groups, 2, 1)
     assert parents[:, 0].tolist() == [w[0] for w in want]
     assert tokens[:, 0].tolist() == [first[w[0]] for w in want]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("k", [1, 5, 64])
+@pytest.mark.parametrize("vocab,beams", [(40007, 1), (9001, 4), (33, 2)])
+def test_scores_that_coincide_in_64_bits_go_to_the_lowest_tokens(dtype, k, vocab, beams):
+    """A logit adds nothing to a score of -1e30, and one of 1e-25 nothing to any: different logits of one score, in descending order of beams
+    that are clearly apart and of beams that are equal."""
+    scores = torch.full((2 * beams,), -1e30)
+    agrees(normal(2 * beams, vocab, dtype, vocab), scores.cuda(), 2, beams, k)
+    tiny = normal(2 * beams, vocab, dtype, vocab + 1) * 1e-25
+    agrees(tiny, torch.arange(2 * beams).neg().float().cuda(), 2, beams, k)
+    some = tiny.clone()
+    for b in range(2 * beams):
+        some[b, [(7 * b + 11 * i) % vocab for i in range(3)]] = 0.5 + b
+    agrees(some, torch.arange(2 * beams).neg().float().cuda(), 2, beams, k)
+    mixed = normal(2 * beams, vocab, dtype, vocab + 2) - 6
+    mixed[0::2] = tiny[0::2]
+    agrees(mixed, (torch.arange(2 * beams) * -1e-2).cuda(), 2, beams, k)
+
+
+def test_finished_beams_among_scores_that_coincide():
+    """A finished beam is one candidate, at its own place, whatever its logits are."""
+    x = normal(8, 3000, torch.float32, 3)
+    agrees(x, torch.full((8,), -1e30, device="cuda"), 2, 4, 9, ints([0, 1, 0, 0, 1, 1, 0, 0]), pad=17)
+    agrees(x, torch.full((8,), -1e30, device="cuda"), 1, 8, 128, ints([1, 1, 0, 1, 0, 0, 1, 1]), pad=2999)
+    agrees(x * 1e-25, torch.tensor([-8.0, 0.0] * 4, device="cuda"), 2, 4, 9, ints([0, 1] * 4), pad=5)
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
