@@ -536,7 +536,8 @@ TTS_API int tts_kv_compact(tts_ctx* ctx, int n_layers, void* const* k_pools, voi
  *                         lse   device  [n_branches * rows_per_branch][Hq] fp32, the natural logarithm of the sum, or NULL
  *                       A branch shorter than its rows is allowed: row i sees the tokens t <= prefix_len + branch_lens[b] -
  *                       rows_per_branch + i (in a tree: those of its ancestors' places that exist), and a row that sees none gets out = 0
- *                       and lse = -infinity.  Scores and sums are fp32, probabilities times V's scale are rounded to fp16 (2^-11).
+ *                       and lse = -infinity.  Scores and sums are fp32, probabilities times V's scale are rounded to fp16: to 2^-11 of themselves,
+ *                       or 2^-29 of the largest |V| that the row sees where that is more.  What a row does not see has no part in it.
  *                       Slots past a branch's end may hold anything; a token whose scale is NaN makes NaN the rows that see it and no
  *                       others.  cfg.max_ctas, softmax_scale and out_dtype apply, attn_impl does not.  The context's calls share the
  *                       memory in which parts of a long branch meet: order them on the GPU.  (It is allocated with the context: 4 MB, or

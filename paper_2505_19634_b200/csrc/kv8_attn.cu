@@ -20,7 +20,7 @@
 //     S^T[16 tokens][rows] = K Q^T      O^T[128 dims][rows] += V^T P^T
 // Codes are exact in fp16, so K and V need no rounding; a row of Q is scaled by a power of two so that bf16 fits fp16 too.
 // The scale of K goes into the score; p sv goes into the second product, rounded to fp16 (11 bits) in units of the largest
-// power of two in sv so far.  The order in which K's 128 dims are summed and V's tokens are numbered is free, and chosen so
+// power of two in sv that the row has seen so far (a token that it does not see is none of its business).  The order in which K's 128 dims are summed and V's tokens are numbered is free, and chosen so
 // that a lane's operands are 16-byte runs of the record: lane (g, t) = (lane / 4, lane mod 4) holds, of K, the dims 32 t ..
 // 32 t + 31 of the tokens 4 (g / 2) + (g mod 2) and two more, and of V the dims 16 g .. 16 g + 15 of the tokens 4 t .. 4 t + 3.
 //
@@ -44,6 +44,7 @@ constexpr int kPair = 2 * kKv8Record;                               // a warp wo
 constexpr float kFar = -1e30f;                                      // "no key yet": finite, so that differences are never NaN
 constexpr float kSlack = 8.f;                                       // log2 of how far a score may exceed the running maximum
 constexpr int kRoom = 6;                                            // p sv is held times 2^kRoom
+constexpr int kLargestUp = 126;                                     // so a unit is 2^(kRoom - 126) or more
 
 // The warps of a CTA for up to 8 kNB rows, the pairs of pages that each has in its ring, and the shared memory (bytes).
 template <int kNB, int kCtaWarps>
@@ -59,13 +60,14 @@ struct Lay {
     static constexpr int kOffFactor = kOffMask + kRows * 8;         // [rows] what a row's scores are multiplied by
     static constexpr int kOffRowAt = kOffFactor + kRows * 4;        // [rows] (branch, row, head) of the results, as one number
     static constexpr int kOffMl = kOffRowAt + kRows * 4;            // [warps][rows] (maximum, sum)
-    static constexpr int kOffExp = kOffMl + kWarps * kRows * 8;   // [warps] exponent of the sums' unit; then a flag
-    static constexpr int kOffJoin = kOffExp + 64;                   // [warps][rows][128 / rounds] floats
+    static constexpr int kOffUnit = kOffMl + kWarps * kRows * 8;    // [warps][rows] the sums' unit, over 2^kRoom
+    static constexpr int kOffLast = kOffUnit + kWarps * kRows * 4;  // a flag
+    static constexpr int kOffJoin = kOffLast + 64;                  // [warps][rows][128 / rounds] floats
     static constexpr int kOffCum = kOffJoin + 256;                  // [branches + 1] units before each branch, until the first piece is found
     static constexpr int kOffBar = kOffJoin + kWarps * kRows * kHeadDim / kRounds * 4;   // [warps][stages]
     static constexpr int kOffAbort = kOffBar + kWarps * kStages * 8;   // [0] flag; [1 ..] scratch of each warp
     static constexpr int kBytes = kOffAbort + (1 + kWarps) * 4 + 12;
-    static_assert(kBytes <= 232448 && kOffJoin % 16 == 0 && kWarps * 4 + 4 <= 64, "shared memory of a CTA");
+    static_assert(kBytes <= 232448 && kOffJoin % 16 == 0, "shared memory of a CTA");
     static_assert(256 + (kMaxBranches + 1) * 8 <= kWarps * kRows * kHeadDim / kRounds * 4 && kWarps * 8 <= 256, "the branches' units, where the sums will be");
 };
 
@@ -96,6 +98,7 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) { u
 __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) { uint64_t r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
 __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) { uint64_t r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
 __device__ __forceinline__ float power_of_two(int e) { return __int_as_float((e + 127) << 23); }      // -126 <= e <= 127
+__device__ __forceinline__ float inverse(float power) { return __int_as_float(0x7f000000 - __float_as_int(power)); }      // of 2^-126 .. 2^126
 __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
     uint32_t r;
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
@@ -167,7 +170,8 @@ kv8_attn_kernel(const __grid_constant__ Kv8AttnParams p) {
     float* factors = reinterpret_cast<float*>(smem + L::kOffFactor);
     int* row_at = reinterpret_cast<int*>(smem + L::kOffRowAt);
     float2* ml = reinterpret_cast<float2*>(smem + L::kOffMl);
-    int* exps = reinterpret_cast<int*>(smem + L::kOffExp);
+    float* units = reinterpret_cast<float*>(smem + L::kOffUnit);
+    int* is_last = reinterpret_cast<int*>(smem + L::kOffLast);
     float* join = reinterpret_cast<float*>(smem + L::kOffJoin);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
 
@@ -293,11 +297,11 @@ kv8_attn_kernel(const __grid_constant__ Kv8AttnParams p) {
 
         float o[8][kNB][4];
         uint64_t neg_m[kNB], l[kNB], factor[kNB];                   // of rows 2 t and 2 t + 1
-        int unit_exp = 7;                                           // exponent field of the power of two that p sv is held in units of,
-        float unit_end = 0.f, up = 0.f;                             // a scale from which on it is too small, and its reciprocal times 2^kRoom
+        uint64_t up[kNB];                                           // 2^kRoom over the power of two that p sv is held in units of
+        float unit_end = 0.f;                                       // a scale from which on the smallest of all rows' units is too small
 #pragma unroll
         for (int n = 0; n < kNB; ++n) {
-            neg_m[n] = pack2(-kFar, -kFar); l[n] = 0; factor[n] = pack2(factors[n * 8 + 2 * t], factors[n * 8 + 2 * t + 1]);
+            neg_m[n] = pack2(-kFar, -kFar); l[n] = 0; up[n] = pack2(power_of_two(kLargestUp), power_of_two(kLargestUp)); factor[n] = pack2(factors[n * 8 + 2 * t], factors[n * 8 + 2 * t + 1]);
 #pragma unroll
             for (int d = 0; d < 8; ++d)
 #pragma unroll
@@ -367,17 +371,15 @@ kv8_attn_kernel(const __grid_constant__ Kv8AttnParams p) {
                 for (int n = 0; n < kNB; ++n) over = fmaxf(over, fmaxf(fmaxf(d[pg][n][0].x, d[pg][n][0].y), fmaxf(d[pg][n][1].x, d[pg][n][1].y)));
             const float sv_top = fmaxf(fmaxf(sv[0][0], sv[0][1]), fmaxf(sv[1][0], sv[1][1]));
             if (__any_sync(0xffffffffu, over > kSlack || sv_top >= unit_end)) {
-                // ---- seldom: the maximum moves, or the unit (the largest exponent in sv so far; a NaN or an infinity is not a unit)
-                int ev = 0;
+                // ---- seldom: the maximum moves, or a row's unit (the largest power of two in the sv that it sees so far; a NaN or an infinity is none)
+                float pow2[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) { const int e = __float_as_int(sv[k >> 1][k & 1]) >> 23 & 255; ev = max(ev, e == 255 ? 0 : e); }
-                const int e = max(unit_exp, __reduce_max_sync(0xffffffffu, ev));
-                const float unit_back = unit_exp - e < -126 ? 0.f : power_of_two(unit_exp - e);
-                unit_exp = e; unit_end = __int_as_float((e + 1) << 23); up = power_of_two(kRoom + 127 - e);
+                for (int k = 0; k < 4; ++k) { const int e = __float_as_int(sv[k >> 1][k & 1]) & 0x7f800000; pow2[k] = e == 0x7f800000 ? 0.f : __int_as_float(e); }
+                float most_up = 0.f;                                // the largest of all rows
 #pragma unroll
                 for (int n = 0; n < kNB; ++n) {
-                    const float2 old = unpack2(neg_m[n]);
-                    float v[2][4], neg[2], back[2];
+                    const float2 old = unpack2(neg_m[n]), up_old = unpack2(up[n]);
+                    float v[2][4], neg[2], back[2], up_new[2], unit_back[2];
 #pragma unroll
                     for (int pg = 0; pg < 2; ++pg) {
                         const float2 xa = unpack2(mul2(x[pg][n][0], factor[n])), xb = unpack2(mul2(x[pg][n][1], factor[n]));
@@ -387,9 +389,17 @@ kv8_attn_kernel(const __grid_constant__ Kv8AttnParams p) {
                     }
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        float top = fmaxf(fmaxf(v[0][j], v[0][2 + j]), fmaxf(v[1][j], v[1][2 + j]));
+                        float top = fmaxf(fmaxf(v[0][j], v[0][2 + j]), fmaxf(v[1][j], v[1][2 + j])), unit = 0.f;
 #pragma unroll
-                        for (int i = 4; i < 32; i <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, i));
+                        for (int k = 0; k < 4; ++k)
+                            if (seen >> (16 * (k >> 1) + 4 * n + 2 * (k & 1) + j) & 1) unit = fmaxf(unit, pow2[k]);
+#pragma unroll
+                        for (int i = 4; i < 32; i <<= 1) { top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, i)); unit = fmaxf(unit, __shfl_xor_sync(0xffffffffu, unit, i)); }
+                        // (powers of two: their exponent fields are added and taken apart)
+                        const int was_up = __float_as_int(j ? up_old.y : up_old.x) >> 23, now_up = min(was_up, kRoom + 254 - (__float_as_int(unit) >> 23));
+                        up_new[j] = __int_as_float(now_up << 23);
+                        unit_back[j] = now_up - was_up < -126 ? 0.f : power_of_two(now_up - was_up);
+                        most_up = fmaxf(most_up, up_new[j]);
                         const float was = j ? old.y : old.x;
                         neg[j] = fminf(was, -top);
                         back[j] = ex2(neg[j] - was);
@@ -399,26 +409,29 @@ kv8_attn_kernel(const __grid_constant__ Kv8AttnParams p) {
                         d[pg][n][0] = make_float2(v[pg][0] + neg[0], v[pg][1] + neg[1]);
                         d[pg][n][1] = make_float2(v[pg][2] + neg[0], v[pg][3] + neg[1]);
                     }
-                    neg_m[n] = pack2(neg[0], neg[1]);
+                    neg_m[n] = pack2(neg[0], neg[1]); up[n] = pack2(up_new[0], up_new[1]);
                     l[n] = mul2(l[n], pack2(back[0], back[1]));
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) o[i][n][j] *= back[j & 1] * unit_back;
+                        for (int j = 0; j < 4; ++j) o[i][n][j] *= back[j & 1] * unit_back[j & 1];
                 }
+                // (all lanes of a t agree on their rows already)
+                most_up = fmaxf(most_up, __shfl_xor_sync(0xffffffffu, most_up, 1));
+                most_up = fmaxf(most_up, __shfl_xor_sync(0xffffffffu, most_up, 2));
+                unit_end = __int_as_float((kRoom + 255 - (__float_as_int(most_up) >> 23)) << 23);
             }
             uint32_t pb[2][kNB][2];                                 // P^T as the B operand: tokens 4 t, 4 t + 1 and 4 t + 2, 4 t + 3 of row g
 #pragma unroll
             for (int pg = 0; pg < 2; ++pg)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    const float f = sv[pg][j] * up;
-                    const uint64_t f2 = pack2(f, f);
+                    const uint64_t f = pack2(sv[pg][j], sv[pg][j]);
 #pragma unroll
                     for (int n = 0; n < kNB; ++n) {
                         const uint64_t e = pack2(ex2(d[pg][n][j].x), ex2(d[pg][n][j].y));
                         l[n] = add2(l[n], e);
-                        float2 w = unpack2(mul2(e, f2));
+                        float2 w = unpack2(mul2(e, mul2(f, up[n])));
                         if (masked) {                               // a hidden token's scale may be a NaN
                             if (!(seen >> (16 * pg + 4 * n + 2 * j) & 1)) w.x = 0.f;
                             if (!(seen >> (16 * pg + 4 * n + 2 * j + 1) & 1)) w.y = 0.f;
@@ -464,9 +477,12 @@ kv8_attn_kernel(const __grid_constant__ Kv8AttnParams p) {
             float a = sums.x, z = sums.y;
 #pragma unroll
             for (int i = 4; i < 32; i <<= 1) { a += __shfl_xor_sync(0xffffffffu, a, i); z += __shfl_xor_sync(0xffffffffu, z, i); }
-            if (g == 0) *reinterpret_cast<float4*>(ml + warp * kRows + n * 8 + 2 * t) = make_float4(-neg.x, a, -neg.y, z);
+            if (g == 0) {
+                const float2 u = unpack2(up[n]);
+                *reinterpret_cast<float4*>(ml + warp * kRows + n * 8 + 2 * t) = make_float4(-neg.x, a, -neg.y, z);
+                *reinterpret_cast<float2*>(units + warp * kRows + n * 8 + 2 * t) = make_float2(inverse(u.x), inverse(u.y));
+            }
         }
-        if (lane == 0) exps[warp] = unit_exp;
         const int slot = 2 * blockIdx.x + (nth == 0 ? 0 : 1);       // a CTA leaves parts of its first and of its last item only
         auto write_out = [&](int r, int dim, const float4& x) {
             const size_t at = (size_t)row_at[r] * kHeadDim + dim;
@@ -512,7 +528,7 @@ kv8_attn_kernel(const __grid_constant__ Kv8AttnParams p) {
                     for (int w = 0; w < kWarps; ++w) { back[w] = ex2(x[w].x - top); sum += x[w].y * back[w]; }
                     const float inv = sum == 0.f ? 0.f : 1.f / sum;      // (a row that saw nothing: m = kFar and l = 0 everywhere; zeros)
 #pragma unroll
-                    for (int w = 0; w < kWarps; ++w) back[w] *= inv * power_of_two(exps[w] - 127 - kRoom);
+                    for (int w = 0; w < kWarps; ++w) back[w] *= inv * units[w * kRows + r];
                     if (c0 == 0) {
                         if (!whole) p.part_ml[slot * kKv8MaxRows + r] = make_float2(top, sum);
                         else if (p.lse) write_lse(r, top, sum);
@@ -542,10 +558,10 @@ kv8_attn_kernel(const __grid_constant__ Kv8AttnParams p) {
                 asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(before) : "l"(p.arrived + id) : "memory");
                 const bool last = before + 1 == (unsigned)cut.n;
                 if (last) p.arrived[id] = 0;                        // as the next call expects it
-                exps[kWarps] = last;
+                *is_last = last;
             }
             __syncthreads();
-            if (exps[kWarps]) {
+            if (*is_last) {
                 if (r < rows) {
                     float top = kFar, sum = 0.f;
                     float4 acc[32 / L::kPerRow];

@@ -12,9 +12,9 @@
 // loaded a tile ahead into registers 319.  In a CTA,
 //   warps 0-7   softmax, two threads to a row, in warps w and w + 4: they lay out its query; per tile of 64 tokens each reads 32 of its
 //               scores from TMEM and leaves p sv there, as the second product's A operand; O is touched only when the maximum moves
-//               by more than 2^8 or the unit of p sv grows.  At a piece's end they write the row.
+//               by more than 2^8 or the row's unit of p sv grows: the largest V scale that it sees.  At a piece's end they write the row.
 //   warps 8-11  turn codes into fp16 operands (exact): [64 tokens][128 dims], two warps K with dims along the contraction, two V with
-//               tokens.  One of K's leaves the tile's scales and the unit.
+//               tokens.  One of K's leaves the tile's scales and the largest so far.
 //   warp 12     issues the products: S = Q K^T (128 x 64 x 128) of the next tile, then O += P V (128 x 128 x 64) of this one.  The tensor
 //               pipe keeps issue order, so S of a tile may overwrite the columns that held P two tiles before.
 //   warp 13     fetches the records, by bulk copies: K with all scales into a ring of three tiles, V into one of two.
@@ -38,6 +38,7 @@ constexpr int kThreads = (kLoadWarp + 1) * 32;
 constexpr float kFar = -1e30f;                                      // "no key yet": finite, so that differences are never NaN
 constexpr float kSlack = 8.f;                                       // log2 of how far a score may exceed the running maximum
 constexpr int kRoom = 6;                                            // p sv is held times 2^kRoom
+constexpr int kLeastUnit = 7;                                       // exponent field of the smallest unit of p sv: its reciprocal times 2^kRoom is a normal number
 constexpr uint32_t kTmemCols = 256, kColS = 0, kColO = 128;
 // An item's start and end take about as long as so many tiles (kv8_run.cuh).  64 (branch, KV head)s of 120 tiles: 93 us with 12, 97 with 4,
 // 122 with 24 (125 rows); 197, 197 and 209 (300 rows, three blocks).
@@ -54,10 +55,9 @@ constexpr int kRingK = 3, kRingV = 2;
 constexpr int kRawK = kCodesTile + kTilePages * kScalesPage, kRawV = kCodesTile;
 // what the softmax needs of a tile besides its scores
 struct Scales {
-    float k[kTile], v[kTile];                                       // K's; V's in the unit, times 2^kRoom
-    float unit_back;                                                // what O is multiplied by before the tile's P V: the unit has grown
-    int unit_exp;                                                   // exponent field of the unit
-    int pad[2];
+    float k[kTile], v[kTile];
+    int unit_exp;                                                   // exponent field of the largest power of two in V's scales so far
+    int pad[3];
 };
 constexpr int kOffQ = 0;                                            // fp16 rows, laid out as K's
 constexpr int kQBlock = kRows * 128;
@@ -71,7 +71,7 @@ constexpr int kOffCum = kOffQ;                                      // [branches
 constexpr int kOffSums = kOffScales + kScales * (int)sizeof(Scales);  // scratch of the scan
 enum Bar { RAWK_FULL = 0, RAWK_EMPTY = RAWK_FULL + kRingK, RAWV_FULL = RAWK_EMPTY + kRingK, RAWV_EMPTY = RAWV_FULL + kRingV, S_FULL = RAWV_EMPTY + kRingV, P_FULL = S_FULL + 2, SCALES = P_FULL + 2, K_FULL = SCALES + kScales, K_EMPTY, V_FULL, V_EMPTY, Q_FULL, O_FULL, PART_DONE, PART_LAST, DRAINED, kNumBars };
 static_assert((kMaxBranches + 1) * 8 <= 2 * kQBlock, "the branches' units lie where the queries will");
-constexpr int kOffPair = kOffSums + (kThreads / 32) * 8;            // [2][2][rows] what the two threads of a row tell one another: maxima; sums
+constexpr int kOffPair = kOffSums + (kThreads / 32) * 8;            // [2][2][rows] what the two threads of a row tell one another: maxima; units, then sums
 constexpr int kOffBar = kOffPair + 4 * kRows * 4;
 constexpr int kOffMisc = kOffBar + kNumBars * 8;                    // [0] abort, [1] TMEM base, [2] the last part, [3, 4] scratch of the copying and the MMA warp
 constexpr int kSmemBytes = kOffMisc + 32;
@@ -87,6 +87,10 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) { u
 __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) { uint64_t r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
 __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) { uint64_t r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
 __device__ __forceinline__ float power_of_two(int e) { return __int_as_float((e + 127) << 23); }      // -126 <= e <= 127
+// exponent field of a scale of V; a NaN or an infinity has no unit
+__device__ __forceinline__ int unit_of(float v) { const int e = __float_as_int(v) >> 23 & 255; return e == 255 ? 0 : e; }
+// 2^kRoom over the unit of this exponent field
+__device__ __forceinline__ float up_of(int unit_exp) { return power_of_two(kRoom + 127 - unit_exp); }
 __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
     uint32_t r;
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
@@ -205,7 +209,7 @@ kv8_attn_wide_kernel(const __grid_constant__ Kv8AttnParams p) {
             __syncwarp();
         };
         auto wait = [&](int i, uint32_t parity) { alive = __all_sync(0xffffffffu, alive && mbar_wait(bar(i), parity, ab)); };
-        int tile = 0, before = 0, unit_exp = 7;                         // tile of the piece; tokens of the tile before
+        int tile = 0, before = 0, unit_exp = kLeastUnit;                // tile of the piece; tokens of the tile before
         int k_slot = 0, k_round = 0, v_slot = 0, v_round = 0;
         bool more = alive;
         for (int n = 0; alive && (more || n > 0); ++n) {                // tiles of the run
@@ -220,22 +224,17 @@ kv8_attn_wide_kernel(const __grid_constant__ Kv8AttnParams p) {
                 if (w == 1) {
                     // (S of the tile before is complete: P V of the third before was issued ahead of it, after its softmax)
                     Scales& to = *reinterpret_cast<Scales*>(smem + kOffScales + n % kScales * sizeof(Scales));
-                    float k[2], v[2];
                     int top = 0;
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         const int t = i * 32 + lane;
                         const float* s = reinterpret_cast<const float*>(raw + kCodesTile + (t >> 4) * kScalesPage) + (t & 15);
-                        k[i] = t < left ? s[0] : 0.f; v[i] = t < left ? s[kPage] : 0.f;
-                        const int e = __float_as_int(v[i]) >> 23 & 255;
-                        top = max(top, e == 255 ? 0 : e);               // (a NaN or an infinity is not a unit)
+                        const float v = t < left ? s[kPage] : 0.f;
+                        to.k[t] = t < left ? s[0] : 0.f; to.v[t] = v;
+                        top = max(top, unit_of(v));
                     }
-                    const int was = tile == 0 ? 7 : unit_exp, e = max(was, __reduce_max_sync(0xffffffffu, top));
-                    const float back = tile == 0 ? 1.f : was - e < -126 ? 0.f : power_of_two(was - e), up = power_of_two(kRoom + 127 - e);
-                    unit_exp = e;
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) { to.k[i * 32 + lane] = k[i]; to.v[i * 32 + lane] = v[i] * up; }
-                    if (lane == 0) { to.unit_back = back; to.unit_exp = e; }
+                    unit_exp = max(tile == 0 ? kLeastUnit : unit_exp, __reduce_max_sync(0xffffffffu, top));
+                    if (lane == 0) to.unit_exp = unit_exp;
                     warp_arrive(bar(SCALES + n % kScales), lane);
                 }
                 convert(raw, smem + kOffK, left);
@@ -416,7 +415,7 @@ kv8_attn_wide_kernel(const __grid_constant__ Kv8AttnParams p) {
             }
             warp_arrive(bar(Q_FULL), lane);
             float neg_m = -kFar, l = 0.f;
-            int unit_exp = 7;
+            int unit_exp = kLeastUnit;                                  // of the row: the largest V scale that it has seen
             const uint64_t factor2 = pack2(factor, factor);
 #pragma unroll 1
             for (int j = 0; j < item.n; ++j, ++n) {
@@ -452,17 +451,23 @@ kv8_attn_wide_kernel(const __grid_constant__ Kv8AttnParams p) {
 #pragma unroll
                 for (int c = 0; c < 32; c += 2) top4[c >> 1 & 3] = max3(top4[c >> 1 & 3], s[c], s[c + 1]);
                 float top = max3(fmaxf(top4[0], top4[1]), top4[2], top4[3]) * factor;
-                const float unit_back = sc.unit_back;
-                unit_exp = sc.unit_exp;
                 // (here both have their scores, so either may write P over them)
-                if (bar_red_or<64>(meet, top + neg_m > kSlack || unit_back != 1.f)) {
-                    // ---- seldom: the maximum moves, or the unit
-                    *mine = top;
+                if (bar_red_or<64>(meet, top + neg_m > kSlack || sc.unit_exp > unit_exp)) {
+                    // ---- seldom: the maximum moves, or the unit (in a tile that the row does not see all of, by what it sees)
+                    int unit = sc.unit_exp;
+                    if (masked) {
+                        unit = unit_exp;
+#pragma unroll 4
+                        for (int c = 0; c < 32; ++c)
+                            if (seen >> c & 1) unit = max(unit, unit_of(sc.v[32 * half + c]));
+                    }
+                    *mine = top; mine[2 * kRows] = __int_as_float(unit);
                     bar_sync_id<64>(meet);
-                    top = fmaxf(top, *other);
+                    top = fmaxf(top, *other); unit = max(unit, __float_as_int(other[2 * kRows]));
                     const float was = neg_m;
                     neg_m = fminf(was, -top);
-                    const float back = ex2(neg_m - was), both = back * unit_back;
+                    const float back = ex2(neg_m - was), both = unit_exp - unit < -126 ? 0.f : back * power_of_two(unit_exp - unit);
+                    unit_exp = unit;
                     l *= back;
                     if (j > 0) {
                         wait(V_EMPTY, (n - 1) & 1);                     // the P V before this tile's
@@ -481,6 +486,7 @@ kv8_attn_wide_kernel(const __grid_constant__ Kv8AttnParams p) {
                 const uint64_t neg2 = pack2(neg_m, neg_m);
                 uint64_t sum[2] = {0, 0};
                 uint32_t w[16];
+                const float up = up_of(unit_exp);
 #pragma unroll
                 for (int c = 0; c < 8; ++c) {
                     const float4 v = *reinterpret_cast<const float4*>(sc.v + 32 * half + 4 * c);
@@ -489,7 +495,7 @@ kv8_attn_wide_kernel(const __grid_constant__ Kv8AttnParams p) {
                         const float2 d = unpack2(fma2(pack2(s[4 * c + 2 * k], s[4 * c + 2 * k + 1]), factor2, neg2));
                         const uint64_t e = pack2(ex2(d.x), ex2(d.y));
                         sum[k] = add2(sum[k], e);
-                        const float2 y = unpack2(mul2(e, k ? pack2(v.z, v.w) : pack2(v.x, v.y)));
+                        const float2 y = unpack2(mul2(e, mul2(k ? pack2(v.z, v.w) : pack2(v.x, v.y), pack2(up, up))));
                         w[2 * c + k] = pack_half2(y.x, y.y);
                     }
                 }
