@@ -130,20 +130,17 @@ namespace tts {
 
 cudaError_t cache_alloc(Ctx* c) {
     const tts_config& f = c->cfg;
-    const size_t nb = f.max_branches, np = f.num_pages;
-    cudaError_t e = cudaMalloc(&c->page_work, 16 + nb * sizeof(int4) + align16(nb * 4) + 2 * align16(np * 4));
-    // attention over the 8-bit cache: two partial results for each CTA, a counter for each (branch, KV head, row block)
-    // (rows of a call with few per KV head; 128 for each of twice as many CTAs where calls may have more)
+    const size_t nb = f.max_branches, np = f.num_pages, lists = align16(16 + nb * sizeof(int4) + align16(nb * 4) + 2 * align16(np * 4));
+    // behind the page calls' lists, attention over the 8-bit cache: a counter for each (branch, KV head, row block)
     const int nr = f.max_rows_per_branch * (f.n_q_heads / f.n_kv_heads);
-    const size_t slots = 2 * (size_t)c->n_sms * (nr < kKv8WideFrom ? kKv8MaxRows : 2 * kKv8WideRows);
-    const size_t items = nb * f.n_kv_heads * ceil_div(nr, kKv8MaxRows);
-    if (e == cudaSuccess) e = cudaMalloc(&c->kv8_part_o, slots * kHeadDim * sizeof(float));
-    if (e == cudaSuccess) e = cudaMalloc(&c->kv8_part_ml, slots * sizeof(float2));
-    c->kv8_arrived_bytes = items * sizeof(unsigned);
-    if (e == cudaSuccess) e = cudaMalloc(&c->kv8_arrived, c->kv8_arrived_bytes);
-    if (e == cudaSuccess) e = cudaMemset(c->kv8_arrived, 0, c->kv8_arrived_bytes);
-    if (e == cudaSuccess) e = cudaStreamSynchronize(cudaStreamLegacy);       // before work on a stream that does not wait for it
-    return e;
+    c->kv8_arrived_bytes = nb * f.n_kv_heads * ceil_div(nr, kKv8MaxRows) * sizeof(unsigned);
+    cudaError_t e = cudaMalloc(&c->page_work, lists + c->kv8_arrived_bytes);
+    if (e != cudaSuccess) return e;
+    c->kv8_arrived = reinterpret_cast<unsigned*>(reinterpret_cast<char*>(c->page_work) + lists);
+    // zero before work on any stream, by one that waits for nobody else's
+    e = cudaMemsetAsync(c->kv8_arrived, 0, c->kv8_arrived_bytes, cudaStreamPerThread);
+    if (e == cudaSuccess) e = cudaMemsetAsync(c->d_status, 0, 2 * sizeof(int32_t), cudaStreamPerThread);
+    return e == cudaSuccess ? cudaStreamSynchronize(cudaStreamPerThread) : e;
 }
 
 cudaError_t cache_reset(Ctx* c) {
@@ -164,8 +161,8 @@ cudaError_t cache_disturb(Ctx* c) {
 
 void cache_release(Ctx* c) {
     cudaFree(c->page_work);
-    cudaFree(c->kv8_part_o); cudaFree(c->kv8_part_ml); cudaFree(c->kv8_arrived); cudaFree(c->beam_work);
-    c->kv8_part_o = nullptr; c->kv8_part_ml = nullptr; c->kv8_arrived = nullptr; c->beam_work = nullptr; c->beam_rows = 0;
+    cudaFree(c->beam_work);
+    c->kv8_arrived = nullptr; c->beam_work = nullptr; c->beam_rows = 0;
     cudaFree(c->chunk_head); cudaFree(c->chunk_pieces); cudaFree(c->chunk_arrived);
     cudaFree(c->chunk_part_o); cudaFree(c->chunk_part_ml);
     c->page_work = nullptr; c->chunk_head = nullptr; c->chunk_pieces = nullptr; c->chunk_arrived = nullptr;

@@ -61,8 +61,8 @@ struct Kv8AttnParams {
     const int32_t *block_table, *branch_lens, *tree_parents;
     void* out;
     float* lse;
-    float* part_o;                     // [2 * grid][24 or 128 rows][128] normalised partial results
-    float2* part_ml;                   // [2 * grid][24 or 128] their maximum (log2 units) and sum
+    float* part_o;                     // [2 * grid][rb_rows, or 128 rows][128] normalised partial results
+    float2* part_ml;                   // [2 * grid][rb_rows, or 128] their maximum (log2 units) and sum
     unsigned* arrived;                 // [branch][KV head][row block] parts written so far; zero between calls
     int32_t* status;
     int Hq, Hkv, G, R, nr, n_rb, rb_rows, prefix_len, n_branches, max_blocks, num_pages, out_dtype, grid;
@@ -75,6 +75,11 @@ constexpr int kKv8MaxRows = 24;
 // of 7.9 k keys take 79 us there with 25 to 48 rows and 109 with 60, here 78 with 40 and 82 with 60.  (Over 500 keys it is slower, 21 us
 // against 17, but the host does not know how long the branches are.)
 constexpr int kKv8WideRows = 128, kKv8WideFrom = 2 * kKv8MaxRows + 1;
+// Rows of partial results of a context for up to nr rows per KV head: two parts for each CTA, of the first kernel one CTA to an SM, of the other two.
+inline size_t kv8_part_rows(int nr, int n_sms) {
+    const size_t few = 2 * (size_t)n_sms * (nr < kKv8MaxRows ? nr : kKv8MaxRows);
+    return nr < kKv8WideFrom ? few : 4 * (size_t)n_sms * kKv8WideRows;
+}
 struct Kv8ReadParams {
     const unsigned char* pool;
     const int32_t *src, *dst;

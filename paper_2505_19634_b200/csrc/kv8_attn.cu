@@ -530,7 +530,7 @@ kv8_attn_kernel(const __grid_constant__ Kv8AttnParams p) {
 #pragma unroll
                     for (int w = 0; w < kWarps; ++w) back[w] *= inv * units[w * kRows + r];
                     if (c0 == 0) {
-                        if (!whole) p.part_ml[slot * kKv8MaxRows + r] = make_float2(top, sum);
+                        if (!whole) p.part_ml[slot * p.rb_rows + r] = make_float2(top, sum);
                         else if (p.lse) write_lse(r, top, sum);
                     }
                 }
@@ -544,7 +544,7 @@ kv8_attn_kernel(const __grid_constant__ Kv8AttnParams p) {
                         sum.x = fmaf(x.x, back[w], sum.x); sum.y = fmaf(x.y, back[w], sum.y); sum.z = fmaf(x.z, back[w], sum.z); sum.w = fmaf(x.w, back[w], sum.w);
                     }
                     if (whole) write_out(r, dim, sum);
-                    else *reinterpret_cast<float4*>(p.part_o + ((size_t)slot * kKv8MaxRows + r) * kHeadDim + dim) = sum;
+                    else *reinterpret_cast<float4*>(p.part_o + ((size_t)slot * p.rb_rows + r) * kHeadDim + dim) = sum;
                 }
             }
             __syncthreads();
@@ -569,7 +569,7 @@ kv8_attn_kernel(const __grid_constant__ Kv8AttnParams p) {
                     for (int x = 0; x < 32 / L::kPerRow; ++x) acc[x] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 2
                     for (int k = 0; k < cut.n; ++k) {               // (a running maximum: parts are few)
-                        const size_t from = (size_t)cut.slot(k) * kKv8MaxRows + r;
+                        const size_t from = (size_t)cut.slot(k) * p.rb_rows + r;
                         const float2 x = __ldcg(p.part_ml + from);
                         float4 y[32 / L::kPerRow];
 #pragma unroll

@@ -118,7 +118,7 @@ int tts_kv8_attn(tts_ctx* ctx, int format, const void* q, int64_t q_row_stride, 
     memset(&p, 0, sizeof p);
     p.q = static_cast<const __nv_bfloat16*>(q); p.q_stride = (long)q_row_stride; p.pool = static_cast<const unsigned char*>(kv8_pages);
     p.block_table = block_table; p.branch_lens = branch_lens; p.tree_parents = tree_parents; p.out = out; p.lse = lse;
-    p.part_o = c->kv8_part_o; p.part_ml = c->kv8_part_ml; p.arrived = c->kv8_arrived; p.status = c->d_status;
+    p.part_o = c->part_o_priv; p.part_ml = c->part_ml_priv; p.arrived = c->kv8_arrived; p.status = c->d_status;
     p.Hq = f.n_q_heads; p.Hkv = f.n_kv_heads; p.G = p.Hq / p.Hkv; p.R = rows_per_branch; p.nr = nr;
     p.n_rb = n_rb; p.rb_rows = ceil_div(p.nr, p.n_rb);
     p.prefix_len = prefix_len; p.n_branches = n_branches; p.max_blocks = f.max_blocks_per_branch; p.num_pages = f.num_pages; p.out_dtype = f.out_dtype;

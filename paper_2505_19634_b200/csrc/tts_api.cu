@@ -8,6 +8,7 @@
 #include <string.h>
 
 #include "attn_plan.cuh"
+#include "kv8.cuh"
 #include "tts_internal.cuh"
 
 using namespace tts;
@@ -84,6 +85,8 @@ cudaError_t alloc_workspace(Ctx* c) {
     }
     // several prefix sets per call (token-major kernel): up to one more prefix row block per set and KV head
     pre += (size_t)kMaxPrefixSets * f.n_kv_heads * umma_t_rows(nr);
+    // attention over the 8-bit cache has its parts in the private ones' place
+    priv = std::max(priv, kv8_part_rows(nr, c->n_sms));
     cudaError_t e;
     if ((e = cudaMalloc(&c->part_o_pre, pre * kHeadDim * sizeof(float))) != cudaSuccess) return e;
     if ((e = cudaMalloc(&c->part_ml_pre, pre * sizeof(float2))) != cudaSuccess) return e;
@@ -303,7 +306,6 @@ int tts_create(const tts_config* cfg, tts_ctx** out) {
     cudaError_t e = cudaGetDevice(&c->device);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&c->n_sms, cudaDevAttrMultiProcessorCount, c->device);
     if (e == cudaSuccess) e = cudaMalloc(&c->d_status, 2 * sizeof(int32_t));
-    if (e == cudaSuccess) e = cudaMemset(c->d_status, 0, 2 * sizeof(int32_t));
     if (e == cudaSuccess) e = alloc_workspace(c);
     if (e == cudaSuccess) e = cache_alloc(c);
     if (e != cudaSuccess) {

@@ -302,7 +302,7 @@ struct Ctx {
     long chunk_part_rows;
     size_t chunk_arrived_bytes;
     // attention over the 8-bit cache (kv8.cuh)
-    float* kv8_part_o; float2* kv8_part_ml; unsigned* kv8_arrived; size_t kv8_arrived_bytes;
+    unsigned* kv8_arrived; size_t kv8_arrived_bytes;             // in page_work
     // beam selection, from tts_beam_reserve on (beam.cuh)
     void* beam_work;
     int beam_rows, beam_select;
@@ -370,7 +370,7 @@ cudaError_t launch_compact(const PagePools& pools, const int32_t* table, int max
                            int32_t* new_refs, int32_t* page_map, int32_t* n_used, int Hkv, int num_pages, int n_sms, const PageWork& wk,
                            int32_t* status, cudaStream_t st);
 cudaError_t launch_append_rope(RopeParams p, int n_sms, cudaStream_t st);
-cudaError_t cache_alloc(Ctx* c);       // page_work
+cudaError_t cache_alloc(Ctx* c);       // page_work; zeros the status
 void cache_release(Ctx* c);
 cudaError_t cache_reset(Ctx* c);       // the attentions' counters, after a call that did not end
 cudaError_t cache_disturb(Ctx* c);     // leaves them as such a call does (tts_debug_wait_timeout)
