@@ -309,11 +309,9 @@ kv8_attn_wide_kernel(const __grid_constant__ Kv8AttnParams p) {
                 if (more) look_up();
             }
         }
-        if (__any_sync(0xffffffffu, *ab.flag != 0)) {
-            // after a wait that ran out: copies in flight land before the CTA ends
-            const Abort quiet{misc + 3, p.status};
-            for (int i = max(0, n - ring); i < n; ++i) { misc[3] = 0; mbar_wait(bar(full0 + i % ring), i / ring & 1, quiet); }
-        }
+        // copies in flight land before the CTA ends, also where the warps that they are for have given up, or are about to
+        const Abort quiet{misc + 3, p.status};
+        for (int i = max(0, n - ring); i < n; ++i) { misc[3] = 0; mbar_wait(bar(full0 + i % ring), i / ring & 1, quiet); }
     } else if (warp == kMmaWarp) {
         // =========================== products ===========================
         constexpr uint32_t idesc_qk = f16_desc(kRows, kTile, false), idesc_pv = f16_desc(kRows, kHeadDim, true);
@@ -354,16 +352,14 @@ kv8_attn_wide_kernel(const __grid_constant__ Kv8AttnParams p) {
                 __syncwarp();
             }
         }
-        if (__any_sync(0xffffffffu, *ab.flag != 0)) {
-            // products in flight end before their operands' shared memory and TMEM are someone else's
-            if (elect_one()) {
-                misc[4] = 0;
-                umma_commit(bar(DRAINED));
-            }
-            __syncwarp();
-            mbar_wait(bar(DRAINED), 0, Abort{misc + 4, p.status});
-            __syncwarp();
+        // products in flight end before their operands' shared memory and TMEM are someone else's, whoever has given up
+        if (elect_one()) {
+            misc[4] = 0;
+            umma_commit(bar(DRAINED));
         }
+        __syncwarp();
+        mbar_wait(bar(DRAINED), 0, Abort{misc + 4, p.status});
+        __syncwarp();
     } else if (warp < kSoftmaxWarps) {
         // =========================== softmax ===========================
         // The two warps of a row meet at barriers, so that neither leaves where a wait has run out: they go on, waiting no more, with
