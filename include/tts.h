@@ -539,8 +539,10 @@ TTS_API int tts_kv_compact(tts_ctx* ctx, int n_layers, void* const* k_pools, voi
  *                       and lse = -infinity.  Scores and sums are fp32, probabilities times V's scale are rounded to fp16: to 2^-11 of themselves,
  *                       or 2^-29 of the largest |V| that the row sees where that is more.  What a row does not see has no part in it.
  *                       Slots past a branch's end may hold anything; a token whose scale is NaN makes NaN the rows that see it and no
- *                       others.  cfg.max_ctas, softmax_scale and out_dtype apply, attn_impl does not.  The memory in which parts of a
- *                       long branch meet is that of the context's other attention calls: order them all on the GPU.
+ *                       others, its codes being zeros as tts_kv8_append leaves them (e4m3's NaNs, 0x7f and 0xff, are no codes of this cache:
+ *                       where a token of a branch holds one in V, rows that do not see it may be NaN too).  cfg.max_ctas, softmax_scale and
+ *                       out_dtype apply, attn_impl does not.  The memory in which parts of a long branch meet is that of the context's other
+ *                       attention calls: order them all on the GPU.
  *   tts_kv8_copy_pages, tts_kv8_fork, tts_kv8_compact
  *                       tts_kv_copy_pages, tts_kv_fork, tts_kv_compact over n_layers (1..128) 8-bit pools, one per layer.
  * Reported through tts_last_status as TTS_ERR_DEVICE_BOUNDS, whatever cfg.debug_bounds: what the bf16 calls report; by tts_kv8_attn a

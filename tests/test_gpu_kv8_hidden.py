@@ -1,4 +1,5 @@
 """Attention over the 8-bit cache: what a row does not see does not change its result, whatever size it has."""
+import math
 import random
 
 import pytest
@@ -6,7 +7,7 @@ import torch
 
 import kv8_plain as k8
 import paper_2505_19634_b200 as tts
-from test_gpu_kv8 import FORMATS, attend
+from test_gpu_kv8 import FORMATS, attend, context, ints
 
 pytestmark = pytest.mark.gpu
 # rows of one KV head: those of one block of the kernel for few, those of the kernel for many
@@ -52,3 +53,36 @@ def test_rows_that_do_not_see_a_large_value(fmt, hq, hkv, rows, back, power, tre
             x, y = (want, bound) if hidden[i] else (want2, bound2)
             assert ((out[at].double() - x[at]).abs() <= y[at] + x[at].abs() * 2.0 ** -24).all(), (b, i, bool(hidden[i]))
     assert ((lse.double() - want_lse).abs() <= lse_bound).all()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("hq,hkv,rows", [(8, 2, 4), (40, 8, 4), (16, 1, 8), (8, 2, 40)])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("into", ["k", "v"])
+def test_appended_tokens_that_are_not_finite_spoil_the_rows_that_see_them_alone(fmt, hq, hkv, rows, bad, into):
+    """The last tokens are appended, one of them with a NaN or an infinity in head 0: what does not see it is what it is without."""
+    lens = [rows, 70 + rows]
+    gen = torch.Generator().manual_seed(rows)
+    new = torch.randn(2, 2 * rows, hkv, 128, generator=gen).bfloat16().cuda()
+    spoilt = new.clone()
+    spoilt["kv".index(into), rows - 2, 0, 5] = spoilt["kv".index(into), 2 * rows - 2, 0, 77] = bad
+    q, results = None, []
+    for kv in (new, spoilt):
+        c = k8.Cache8(fmt, hkv, lens, prefix=0, seed=rows)
+        ctx = context(hq, hkv, 2, rows, c.width, c.num_pages)
+        ctx.tts_kv8_append(fmt, None, None, 0, kv[0], kv[1], hkv * 128, None, c.pool, c.table, 0, c.branch_lens, ints([0, rows, 2 * rows]), 2, 2 * rows, None)
+        q, out, lse = attend(c, hq, rows, seed=2, q=q, ctx=ctx)
+        results.append((out, lse))
+    sees = torch.zeros(2 * rows, hq, dtype=torch.bool, device="cuda")
+    sees[rows - 2:rows, :hq // hkv] = sees[2 * rows - 2:, :hq // hkv] = True
+    (good, good_lse), (out, lse) = results
+    assert out.isnan().all(-1).equal(sees) and torch.isfinite(good).all()
+    assert torch.equal(out[~sees], good[~sees]) and torch.equal(lse[~sees], good_lse[~sees])
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("hq,hkv,rows,prefix", [(8, 2, 4, 8192), (10, 2, 1, 4096), (28, 2, 8, 8192), (8, 1, 16, 2048)])
+def test_a_long_prefix(fmt, hq, hkv, rows, prefix):
+    c = k8.Cache8(fmt, hkv, [rows, 37 + rows, 500 + rows, 130], prefix=prefix, seed=rows)
+    q, out, lse = attend(c, hq, rows, seed=3)
+    k8.assert_attention(c, q, rows, out, lse)
