@@ -538,6 +538,8 @@ TTS_API int tts_kv_compact(tts_ctx* ctx, int n_layers, void* const* k_pools, voi
  *                       rows_per_branch + i (in a tree: those of its ancestors' places that exist), and a row that sees none gets out = 0
  *                       and lse = -infinity.  Scores and sums are fp32, probabilities times V's scale are rounded to fp16: to 2^-11 of themselves,
  *                       or 2^-29 of the largest |V| that the row sees where that is more.  What a row does not see has no part in it.
+ *                       A prefix that branches share is worked through once for each of them (from L2 where it fits), unlike in
+ *                       tts_verify_attn, which does so once for all.
  *                       Slots past a branch's end may hold anything; a token whose scale is NaN makes NaN the rows that see it and no
  *                       others, its codes being zeros as tts_kv8_append leaves them (e4m3's NaNs, 0x7f and 0xff, are no codes of this cache:
  *                       where a token of a branch holds one in V, rows that do not see it may be NaN too).  cfg.max_ctas, softmax_scale and

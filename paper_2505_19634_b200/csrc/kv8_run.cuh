@@ -1,6 +1,7 @@
 // How attention over the 8-bit cache is cut into work.
 //
-// An item is a (branch, KV head, block of stacked rows).  It has a unit for every kUnitTokens tokens (an empty branch's: one), behind
+// An item is a (branch, KV head, block of stacked rows), from the prefix's first token on: what branches share is worked through for each.
+// It has a unit for every kUnitTokens tokens (an empty branch's: one), behind
 // kStart units for what a piece of an item costs besides (queries, the join of its parts): so a CTA with many short items gets
 // fewer tokens.  All items follow one another, a CTA owns a contiguous run of units and walks over its pieces of items; what it has of
 // an item that others work on too it leaves as a part, and the last one to do so joins them.  Where there are CTAs enough to give each
