@@ -45,6 +45,7 @@
 
 #include "chunk_attn.cuh"
 #include "launch.cuh"
+#include "packed.cuh"
 #include "umma_ptx.cuh"
 
 namespace tts {
@@ -327,12 +328,6 @@ __device__ __forceinline__ void store_out8(const ChunkParams& p, size_t row_head
     }
 }
 
-// two fp32 values in a 64-bit register pair: Blackwell's packed fma and add
-__device__ __forceinline__ uint64_t pack2(float a, float b) { uint64_t r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
-__device__ __forceinline__ float2 unpack2(uint64_t v) { float2 r; asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v)); return r; }
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) { uint64_t r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) { uint64_t r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
-__device__ __forceinline__ float max3(float a, float b, float c) { float r; asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
 __device__ __forceinline__ uint32_t bf16_pair2(uint64_t v) { const float2 f = unpack2(v); return bf16_pair(f.x, f.y); }
 
 __device__ __forceinline__ uint64_t exp2_sfu2(uint64_t y) {

@@ -88,6 +88,11 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map
         ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
 }
 
+// bytes that lie in one run, 16-byte aligned at both ends
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+
 // L2 policy for data that is read once: such lines are the first to be evicted, so that a stream of
 // K/V pages larger than the L2 does not push out what every launch needs again (the kernels' own
 // instructions, page tables, queries, partial results).
