@@ -9,8 +9,8 @@
 // shared memory; items cut between CTAs are joined by the last CTA to finish one of their parts, which the others leave in
 // global memory.
 //
-// Measured (B200, copy peak 6538 GB/s): 64 single tokens over 1 k to 8 k keys, 40 / 8 heads, 111 us = 4.9 TB/s (twelve warps); a drafted step of 16 branches
-// with 20 rows to a KV head over 4 k to 5 k keys 55 us = 2.5 TB/s; 4 single tokens over 500 keys 8.6 us.  Of eight, a warp takes about 1850 clocks for a
+// Measured (B200, copy peak 6538 GB/s): 64 single tokens over 1 k to 8 k keys, 40 / 8 heads, 110 to 118 us by the card = 4.6 to 4.9 TB/s (twelve warps); a drafted step
+// of 16 branches with 20 rows to a KV head over 4 k to 5 k keys 55.6 us = 2.5 TB/s; 4 single tokens over 500 keys 9.1 us.  Of eight, a warp takes about 1850 clocks for a
 // page of up to 8 rows (1460 without the copies, 950 with nothing but them) and 2240 for 24: conversion, products and exponentials of two
 // warps to a scheduler.  A piece of an item costs 16000 clocks besides (queries 3000, the warps' join 9000, that of its parts 3700), a
 // third of the drafted step.  Tiles converted for the tensor cores' own products took 88 and 246 us for the first two.

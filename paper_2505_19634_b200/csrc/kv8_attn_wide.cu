@@ -7,7 +7,7 @@
 // clocks of the tensor cores, 512 of the exponentials' unit and, in shared memory, about 1200: Q, K and V as operands (512), codes read,
 // written in fp16 and fetched (512), scales, barriers.  Measured: about 1550 clocks, and a third of a call around them: 18000 clocks until the
 // first product (cold instructions and TLBs), up to 35000 behind a piece's last (its rows, the fence, the join).  8 trees of 60 nodes,
-// 300 rows to a KV head, over 7.9 k keys: 193 us = 394 TFLOP/s; the kernel for few rows took 410.  All of these took 190 to 200 us as well: Q in
+// 300 rows to a KV head, over 7.9 k keys: 197 us = 386 TFLOP/s; the kernel for few rows took 410.  All of these took 190 to 200 us as well: Q in
 // TMEM and one S; K's and V's conversion by warps of their own; a warp for each product; waits that sleep.  V's operand twice 229, codes
 // loaded a tile ahead into registers 319.  In a CTA,
 //   warps 0-7   softmax, two threads to a row, in warps w and w + 4: they lay out its query; per tile of 64 tokens each reads 32 of its

@@ -3,7 +3,7 @@
 // Bound by HBM: 4224 bytes in and 8192 out per page and KV head, each touched once.  A warp takes one of them: K and V
 // are 128 chunks of 16 codes each, so a lane has eight loads of 16 bytes and the scales of its tokens in flight before it
 // stores; a lane's 16 values are one 32-byte sector, written by one instruction where the pools start on such a boundary
-// (4128 pages of 8 KV heads: 69.4 us, 0.90 of the copy peak; in 16-byte stores 80.8).  One prompt's 47 pages of 2 heads: 4.4 us, a launch.
+// (4128 pages of 8 KV heads: 69.4 us, 0.90 of the copy peak; in 16-byte stores 80.8).  One prompt's 47 pages of 2 heads: 4.4 to 4.8 us, a launch.
 #include "kv8.cuh"
 #include "launch.cuh"
 

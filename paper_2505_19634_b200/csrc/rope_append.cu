@@ -14,8 +14,8 @@
 // needs no exchange between lanes; a lane's eight sines and cosines serve all heads of the row that its
 // warp walks through, sixteen at a time, whose loads are issued before the row's branch, page and angles are
 // looked up.  Keys and values of the 8-bit cache come behind the queries, four at a time: their codes cost a division each, which
-// sixteen times over in the code would be registers and instructions for the queries to wait for (11 prompts, 40 / 8 heads: 82.8 us
-// with a floor of 63.9; 108.7 with keys and values among the queries).
+// sixteen times over in the code would be registers and instructions for the queries to wait for (11 prompts, 40 / 8 heads, and their pages read back: 82.8
+// us with a floor of 63.9, the append 68 of them; 108.7 with keys and values among the queries).
 #include <type_traits>
 
 #include "kv8.cuh"
