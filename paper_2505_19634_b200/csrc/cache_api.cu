@@ -137,7 +137,7 @@ cudaError_t cache_alloc(Ctx* c) {
     cudaError_t e = cudaMalloc(&c->page_work, lists + c->kv8_arrived_bytes);
     if (e != cudaSuccess) return e;
     c->kv8_arrived = reinterpret_cast<unsigned*>(reinterpret_cast<char*>(c->page_work) + lists);
-    // zero before work on any stream, by one that waits for nobody else's
+    // zero before work on any stream, by one that waits for no other than the legacy stream's
     e = cudaMemsetAsync(c->kv8_arrived, 0, c->kv8_arrived_bytes, cudaStreamPerThread);
     if (e == cudaSuccess) e = cudaMemsetAsync(c->d_status, 0, 2 * sizeof(int32_t), cudaStreamPerThread);
     return e == cudaSuccess ? cudaStreamSynchronize(cudaStreamPerThread) : e;
