@@ -578,7 +578,7 @@ TTS_API int tts_kv8_compact(tts_ctx* ctx, int n_layers, void* const* kv8_pools, 
  *                    over its beams r = g * n_beams .. g * n_beams + n_beams - 1 and all tokens x, in descending order; of equal scores
  *                    (formed and compared in 64 bits) the lowest beam, then the lowest token, comes first.  The exponentials in a row's sum are
  *                    fp32: its logarithm, the same for all of the beam's candidates, is off by up to 1.4e-7 (measured), and candidates of
- *                    different beams that lie closer than that may change places.  Beams of equal rows and scores stay equal.
+ *                    different beams that lie closer than 3e-7 may change places.  Beams of equal rows and scores stay equal.
  *                      logits       device  rows of `vocab` bf16 or fp32 (logits_dtype), row_stride elements from row to row; any alignment
  *                                           of their type, 16-byte aligned rows are read faster.  -infinity rules a token out
  *                      beam_scores  device  [rows] fp32: the beams' sums of logarithms so far.  A beam whose score is not finite is no beam

@@ -15,7 +15,7 @@
 // Which thread adds up which logits does not depend on where a row lies in memory: equal rows have equal sums, bit for bit, and equal scores.
 // Exponentials are fp32 (2^-22, and 2^-23 of their exponent); 32 of them are summed in fp32, everything beyond, the logarithm too, in 64 bits:
 // a beam's candidates are all off by the same 1.4e-7 at most (measured; rows of 300 to 152064 normal logits of size 1 to 30), so those of different
-// beams that lie closer than that may change places.  For few rows the time is that of fetching
+// beams that lie closer than twice that may change places.  For few rows the time is that of fetching
 // every instruction once (about 20 cycles each), which is why there are few phases and little unrolled code outside the pass.
 //
 // Measured: one question of 4 beams, 151936 logits 11.0 us; 16 questions of 16 beams, 152064 bf16 logits 31.9 us (78 MB: 11.9 us at the copy

@@ -7,7 +7,7 @@
 // clocks of the tensor cores, 512 of the exponentials' unit and, in shared memory, about 1200: Q, K and V as operands (512), codes read,
 // written in fp16 and fetched (512), scales, barriers.  Measured: about 1550 clocks, and a third of a call around them: 18000 clocks until the
 // first product (cold instructions and TLBs), up to 35000 behind a piece's last (its rows, the fence, the join).  8 trees of 60 nodes,
-// 300 rows to a KV head, over 7.9 k keys: 197 us = 386 TFLOP/s; the kernel for few rows took 410.  All of these took 190 to 200 us as well: Q in
+// 300 rows to a KV head, over 7.9 k keys: 196 us = 389 TFLOP/s; the kernel for few rows took 410.  All of these took 190 to 200 us as well: Q in
 // TMEM and one S; K's and V's conversion by warps of their own; a warp for each product; waits that sleep.  V's operand twice 229, codes
 // loaded a tile ahead into registers 319.  In a CTA,
 //   warps 0-7   softmax, two threads to a row, in warps w and w + 4: they lay out its query; per tile of 64 tokens each reads 32 of its
@@ -56,7 +56,7 @@ constexpr int kRingK = 3, kRingV = 2;
 constexpr int kRawK = kCodesTile + kTilePages * kScalesPage, kRawV = kCodesTile;
 // what the softmax needs of a tile besides its scores
 struct Scales {
-    float k[kTile], v[kTile];
+    float k[kTile], v[kTile];                                       // (K's times the softmax's scale, in log2 units)
     int unit_exp;                                                   // exponent field of the largest power of two in V's scales so far
     int pad[3];
 };
@@ -215,7 +215,7 @@ kv8_attn_wide_kernel(const __grid_constant__ Kv8AttnParams p) {
                         const int t = i * 32 + lane;
                         const float* s = reinterpret_cast<const float*>(raw + kCodesTile + (t >> 4) * kScalesPage) + (t & 15);
                         const float v = t < left ? s[kPage] : 0.f;
-                        to.k[t] = t < left ? s[0] : 0.f; to.v[t] = v;
+                        to.k[t] = t < left ? s[0] * p.scale_log2 : 0.f; to.v[t] = v;
                         top = max(top, unit_of(v));
                     }
                     unit_exp = max(tile == 0 ? kLeastUnit : unit_exp, __reduce_max_sync(0xffffffffu, top));
@@ -385,7 +385,9 @@ kv8_attn_wide_kernel(const __grid_constant__ Kv8AttnParams p) {
 #pragma unroll
                 for (int c = 0; c < 8; ++c) *reinterpret_cast<uint4*>(to + ((c ^ (r & 7)) << 4)) = make_uint4(x[4 * c], x[4 * c + 1], x[4 * c + 2], x[4 * c + 3]);
                 fence_proxy_async();
-                factor = power_of_two(e) * p.scale_log2;
+                // (a power of two alone: the product with it is not rounded, so the maximum is what the fused multiply-add below takes it for, even
+                // where it is so large that its own rounding would be more than an exponent that fp16 holds)
+                factor = power_of_two(e);
                 if (p.tree_parents == nullptr) mask = i_row >= 63 ? ~0ull : (2ull << i_row) - 1ull;
                 else
                     for (int a = i_row, guard = 0; a >= 0 && guard < kMaxTreeRows; ++guard) {
