@@ -504,7 +504,7 @@ beam_select_kernel(const __grid_constant__ BeamParams p) {
 // Rows of many arrays: dst[i] = src[parents[i]].  Bound by HBM; a block writes 32 KiB of a row, eight aligned 16-byte units a thread, all
 // loaded before the first store.  Where a row of src starts elsewhere within 16 bytes than its row of dst, a unit is put together from two
 // aligned loads, of which the second is the next lane's first; what is left at a row's ends moves byte by byte.  48 dense caches of 16 rows
-// of 512 KiB: 103 us, the copy peak; of 512 KiB and a byte 114 (byte by byte 488); 16 rows of five small arrays 4.3 to 4.9 us, a launch.
+// of 512 KiB: 103 us, the copy peak; of 512 KiB and a byte 114 (byte by byte 488); 16 rows of five small arrays 4.2 to 4.9 us, a launch.
 constexpr int kReorderLoads = kReorderUnits / kReorderThreads;
 __device__ __forceinline__ void move_aligned(const unsigned char* src, unsigned char* dst, long bytes, long first) {
     const uint4* from = reinterpret_cast<const uint4*>(src);
